@@ -400,6 +400,148 @@ termezo_status termezo_model_set_timing(termezo_model* model, int32_t enable);
 termezo_status termezo_model_timing(termezo_model* model, int32_t cls, double* ms,
                                     int64_t* launches, double* ops);
 
+/* ---- generation: 8-bit cache, attention over it, logits, beam selection ----------
+ * The calls that a decoder needs to generate tokens with the current codes (the
+ * rewards of the evolution-strategies variant are those of generated text).  They
+ * return as soon as their work is queued on the context's stream and may be called
+ * while another device is current.  Creating a cache allocates all that its calls need;
+ * termezo_beam_select and termezo_model_decode allocate when a call needs more scratch
+ * than every earlier one, so that after one of the largest size they can be captured in
+ * graphs, as the other calls here can at once.
+ *
+ * A cache holds the keys and values of groups * beams sequences of up to max_len
+ * tokens for n_layers attention layers.  The sequences of a group (the beams of a
+ * search) have the same length.  Tokens are held in blocks of 64:
+ *   - a complete block of a head holds 8-bit codes q = rne(x * s), s = 127 * (1 / a),
+ *     and the step d = a * (1 / 127) (fp32, each operation rounded), a = max(max |x|,
+ *     1e-30) over its 64 * head_dim values, keys and values apart; the cached value is
+ *     q * d.  A block with a non-finite value has the step NaN;
+ *   - the tokens of the incomplete last block are held in act_dtype.
+ * So every value is rounded to 8 bits once, and what a cache holds does not depend
+ * on how its tokens were split into calls.  With rope_base > 0 keys and queries are
+ * given unrotated: pairs (i, i + head_dim / 2) are turned by
+ * position * rope_base^(-2i/head_dim) (angles in fp64, cosine and sine in fp32) and
+ * keys rounded to act_dtype; rope_base = 0 stores them as they are. */
+typedef struct {
+  int32_t n_layers, n_heads, n_kv_heads, head_dim;  /* head_dim 64, 96 or 128       */
+  int32_t groups, beams;            /* beams: 1 to 64 sequences per group            */
+  int64_t max_len;                  /* tokens per sequence, at most 2^24             */
+  float rope_base;                  /* e.g. 10000; 0: no rotation                    */
+  termezo_dtype act_dtype;          /* F32 or BF16: q, k, v and out                  */
+} termezo_kvcache_config;
+
+typedef struct termezo_kvcache termezo_kvcache;
+
+/* Allocate a cache on ctx's device, empty.  Its calls run on ctx's stream; it must be
+ * destroyed before ctx.  Errors: INVALID_ARG (sizes not positive, n_heads no multiple
+ * of n_kv_heads, head_dim, beams, max_len, dtype, rope_base negative or not finite or
+ * in (0, 1], more than 2^31 - 1 pages or more than 65535 rows or layers), DEVICE, OOM. */
+termezo_status termezo_kvcache_create(termezo_ctx* ctx, const termezo_kvcache_config* cfg,
+                                      termezo_kvcache** out);
+/* Waits for the stream and frees the cache.  NULL is a no-op. */
+void termezo_kvcache_destroy(termezo_kvcache* cache);
+
+/* Empty one group (group >= 0), or all of them (-1), which also makes the first beam of
+ * every group the only one in use again.  Errors: INVALID_ARG (group out of range). */
+termezo_status termezo_kvcache_reset(termezo_kvcache* cache, int32_t group);
+
+/* Sequences in use: row r is sequence r.  After creation and a reset of all groups
+ * only the first beam of each group is in use (rows = groups), so a prompt is taken
+ * once per search; termezo_kvcache_fork gives every beam what the first one holds
+ * (rows = groups * beams, beams of a group next to each other).  Complete blocks are
+ * shared, not copied.  Errors: STATE (appended tokens not advanced; already forked;
+ * beams = 1 never needs it). */
+termezo_status termezo_kvcache_fork(termezo_kvcache* cache);
+
+/* Append counts[g] tokens (device int32 [groups], each 0 .. n; NULL: n) to every
+ * sequence of group g in one layer.  k, v: [rows][n][n_kv_heads][head_dim] in act_dtype;
+ * the rows' tokens from counts[g] on are not read.  The tokens are pending: attention
+ * and read see them, but the lengths stay until termezo_kvcache_advance (so that every
+ * layer appends at the same place); appending again before that replaces them.
+ * Counts outside 0 .. n and tokens past max_len raise a deferred INVALID_ARG and
+ * append nothing to their group.  Errors: INVALID_ARG (layer out of range, n <= 0 or
+ * > max_len, null or misaligned (16 bytes) pointers). */
+termezo_status termezo_kvcache_append(termezo_kvcache* cache, int32_t layer, const void* k,
+                                      const void* v, int64_t n, const int32_t* counts);
+
+/* Causal attention of the pending tokens over the cache and themselves: query i of
+ * a row (at position length + i) sees positions 0 .. length + i;
+ * out = sum_t softmax_t(q . k_t / sqrt(head_dim)) v_t, head h reading key/value head
+ * h / (n_heads / n_kv_heads).  q, out: [rows][n][n_heads][head_dim] in act_dtype; rows'
+ * queries from the pending count on are neither read nor written.  k and v, both or
+ * neither: when given, they are appended first (termezo_kvcache_append), for one token
+ * a row in the same launch.  counts: as in append; without k and v it may be NULL (the
+ * pending counts), and counts that differ from the pending ones, as pending counts above n,
+ * raise a deferred INVALID_ARG and leave their group's rows out.  out must not overlap q,
+ * k or v.  Errors: INVALID_ARG (as append; one of k, v null), STATE (k and v null and
+ * nothing pending). */
+termezo_status termezo_kvcache_attention(termezo_kvcache* cache, int32_t layer, const void* q,
+                                         const void* k, const void* v, int64_t n,
+                                         const int32_t* counts, void* out);
+
+/* The pending tokens become part of the sequences.  Errors: STATE (nothing pending). */
+termezo_status termezo_kvcache_advance(termezo_kvcache* cache);
+
+/* Beam reordering: sequence b of group g continues what sequence parents[g * beams + b]
+ * of the same group held (device int32 [groups * beams], 0 .. beams - 1 each; any other
+ * value raises a deferred INVALID_ARG and keeps its sequence).  Complete blocks are
+ * shared; of the tokens behind them only those of a parent's second and further
+ * children are copied.  Errors: INVALID_ARG (null), STATE (pending tokens; not forked). */
+termezo_status termezo_kvcache_reorder(termezo_kvcache* cache, const int32_t* parents);
+
+/* Values of positions first .. first + n - 1 of every row of one layer, pending tokens
+ * among them: k_out, v_out (nullable) [rows][n][n_kv_heads][head_dim] in dtype (F32: the
+ * cached values exactly; BF16: rounded).  Positions behind a row's last token are not
+ * written.  Errors: INVALID_ARG (layer, first < 0, n <= 0, first + n > max_len, dtype,
+ * misaligned). */
+termezo_status termezo_kvcache_read(termezo_kvcache* cache, int32_t layer, int64_t first, int64_t n,
+                                    void* k_out, void* v_out, termezo_dtype dtype);
+
+/* Host copy of the groups' lengths (without pending tokens).  Waits for the stream and
+ * reports deferred errors.  Errors: INVALID_ARG (null). */
+termezo_status termezo_kvcache_lengths(termezo_kvcache* cache, int32_t* lengths);
+
+/* Logits of M rows of hidden states over the (tied) embedding: logits[m][t] =
+ * sum_i x[m][i] E[t][i] in fp32.  x [M][d], E [vocab][d] in dtype (F32 or BF16), logits
+ * [M][vocab] fp32, M = 1 .. 65535.  d must be a multiple of 16.  logits must not overlap x or E.
+ * Errors: INVALID_ARG (sizes, dtype, null or misaligned (16 bytes) pointers). */
+termezo_status termezo_logits(termezo_ctx* ctx, const void* x, const void* E, termezo_dtype dtype,
+                              int64_t M, int64_t d, int64_t vocab, float* logits);
+
+/* Beam search's selection: of all beams' continuations the n_out best per group.
+ * logits: device fp32 [groups][beams][vocab]; scores: [groups][beams] fp32 summed log
+ * probabilities.  Continuation (b, t) has the score scores[b] + logits[b][t] -
+ * logsumexp(logits[b]); the best come first, equal ones by the lowest b * vocab + t.
+ * finished (nullable, [groups][beams], nonzero: finished): a finished beam's logits are not
+ * looked at, its only continuation is eos with its score unchanged.  A NaN logit counts as
+ * -inf; beams whose logsumexp is not finite and NaN scores give continuations of score -inf.
+ * Outputs, [groups][n_out]: out_scores fp32, out_tokens and out_parents (the beam) int32,
+ * out_finished (nullable; the parent was finished or the token is eos).  history (nullable,
+ * int32 [groups][beams][hist_len]) and out_history [groups][n_out][hist_len + 1]: the
+ * parent's tokens followed by the new one (hist_len 0: history may be null).  eos = -1: there
+ * is none (finished must be null).  No output may overlap an input.  Errors: INVALID_ARG (groups 1 .. 65535, beams
+ * 1 .. 64, vocab 1 .. 2^24, n_out 1 .. 64 and at most beams * vocab, hist_len 0 .. 2^24,
+ * eos < -1 or >= vocab, null pointers, history without out_history or the
+ * other way round, finished with eos -1). */
+termezo_status termezo_beam_select(termezo_ctx* ctx, const float* logits, const float* scores,
+                                   const uint8_t* finished, int32_t groups, int32_t beams,
+                                   int32_t vocab, int32_t n_out, int32_t eos, float* out_scores,
+                                   int32_t* out_tokens, int32_t* out_parents,
+                                   uint8_t* out_finished, const int32_t* history,
+                                   int32_t* out_history, int64_t hist_len);
+
+/* One generation step of the decoder with the current codes (clean or perturbed; a
+ * snapshot model reads the snapshot): the n tokens of every row (device int32 [rows][n],
+ * counts as in append) run through the blocks with attention over the cache, are
+ * appended to it and advanced; logits [rows][vocab] fp32 (16-byte aligned) of each row's last
+ * new token (0 for rows without one).  The cache's layers, heads, head size
+ * and act_dtype must be the model's, its rope_base too.  Token ids are checked as in
+ * termezo_model_loss.  The call allocates activations when rows * n exceeds every earlier
+ * call's.  Errors: INVALID_ARG, STATE (no current codes; tokens pending), OOM. */
+termezo_status termezo_model_decode(termezo_model* model, termezo_kvcache* cache,
+                                    const int32_t* tokens, int64_t n, const int32_t* counts,
+                                    float* logits);
+
 /* ---- inspection and support calls (not part of the four hot-path calls) ---- */
 
 /* Wait for the context's stream; reports a deferred NUMERIC error. */

@@ -1,0 +1,761 @@
+// Cache of keys and values in 8 bits and the attention that reads it.
+//
+// A block is 64 tokens of one key/value head.  Complete blocks are pages: codes u = q + 128 (a
+// byte), one step d per block for the keys and one for the values, value = q d.  The tokens behind
+// the last complete block lie in tails in the activation type.  A page is written once and never
+// again while its group lives, so the beams of a search share pages through a table
+// [slot][block] -> page; only tails have one owner each.  A slot's own page of block j is
+// tail_of[slot] * max_blocks + j: the beams of a group advance together and a tail has one owner
+// at a time, so no two slots write the same page.
+//
+// The byte order of a page is that of tmz_pages.h.
+// Tails are [64][head_dim] for keys and [head_dim][64] for values.
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <string>
+
+#include "tmz_device.h"
+#include "tmz_internal.h"
+#include "tmz_pages.h"
+
+namespace tmz {
+
+constexpr float kStepFloor = 1e-30f;  // a block's largest magnitude is taken as at least this
+
+// What the kernels see of a cache.
+struct CacheView {
+  uint8_t *kpage, *vpage;
+  float2* step;                       // (keys, values) per layer, page and head
+  void *ktail, *vtail;                // [layer][2][slot][head][64 x head_dim]
+  int32_t *len, *pend, *sel;          // [groups]: length, pending tokens, tail buffer in use
+  int32_t *tail_of, *table;
+  const float2* rope;                 // [position][head_dim / 2]; null: no rotation
+  int32_t* err;
+  int32_t groups, beams, width, heads_kv;
+  int64_t slots, max_blocks, max_len;
+
+  __device__ int64_t page_head(int layer, int64_t page, int head) const {
+    return ((int64_t)layer * slots * max_blocks + page) * heads_kv + head;
+  }
+  __device__ int64_t tail_head(int layer, int buf, int64_t slot, int head) const {
+    return (((int64_t)layer * 2 + buf) * slots + slot) * heads_kv + head;
+  }
+  __device__ int64_t own_page(int64_t slot, int64_t block) const {
+    return (int64_t)tail_of[slot] * max_blocks + block;
+  }
+  // Pages of blocks below the group's length come from the table; those that pending tokens
+  // complete are the slot's own.
+  __device__ int64_t page_of(int64_t slot, int64_t block, int64_t len) const {
+    return block < len / kBlock ? table[slot * max_blocks + block] : own_page(slot, block);
+  }
+};
+
+__device__ __forceinline__ float ld_val(const float* p) { return *p; }
+__device__ __forceinline__ float ld_val(const uint16_t* p) { return bf16_to_f32(*p); }
+__device__ __forceinline__ void st_val(float* p, float v) { *p = v; }
+__device__ __forceinline__ void st_val(uint16_t* p, float v) {
+  *p = __builtin_bit_cast(uint16_t, (__bf16)v);
+}
+__device__ __forceinline__ float as_type(const float*, float v) { return v; }
+__device__ __forceinline__ float as_type(const uint16_t*, float v) { return (float)(__bf16)v; }
+
+// Tokens that an append takes for group g: counts[g], or n; 0 and a deferred error for counts
+// outside 0 .. n and for tokens past the end.
+__device__ __forceinline__ int append_count(const CacheView& c, int g, int n, const int32_t* counts) {
+  const int k = counts ? counts[g] : n;
+  if (k < 0 || k > n || (int64_t)c.len[g] + k > c.max_len) {
+    if (threadIdx.x == 0) atomicOr(c.err, 16);
+    return 0;
+  }
+  return k;
+}
+// Queries that attention answers for group g: the pending tokens.
+__device__ __forceinline__ int query_count(const CacheView& c, int g, int n, const int32_t* counts) {
+  const int k = c.pend[g];
+  if (k > n || (counts && counts[g] != k)) {
+    if (threadIdx.x == 0) atomicOr(c.err, 16);
+    return 0;
+  }
+  return k;
+}
+
+__global__ void __launch_bounds__(256) k_cache_reset(CacheView c, int g0, int g1) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  const int n = (g1 - g0) * c.beams;
+  if (i < n) c.tail_of[g0 * c.beams + i] = g0 * c.beams + i;
+  if (i < g1 - g0) c.len[g0 + i] = c.pend[g0 + i] = c.sel[g0 + i] = 0;
+}
+
+// Rotary table: the angle p base^(-2i/hd) and its functions in fp64, rounded to fp32.
+struct RopeFreq {
+  double f[64];
+};
+__global__ void __launch_bounds__(256) k_rope_table(float2* t, int64_t n, int half, RopeFreq w) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n * half) return;
+  const double a = (double)(i / half) * w.f[i % half];
+  double s, c;
+  sincos(a, &s, &c);
+  t[i] = make_float2((float)c, (float)s);
+}
+
+// ---------------------------------------------------------------------------
+// Append: block y / head / row.  A work group takes one block of one head: the tokens that the tail
+// holds already and the new ones go to LDS (keys rotated and rounded to the activation type), and
+// the block leaves as a page when it is complete, else the new tokens go to a tail: the buffer in
+// use when the block had begun, the other one otherwise (so that the call can be made again until
+// the tokens are advanced).  Bound by the bytes moved; a block's 64 x hd values are read once.
+// ---------------------------------------------------------------------------
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) k_cache_append(CacheView c, int layer, const T* k, const T* v,
+                                                      int n, const int32_t* counts) {
+  constexpr int LD = HD + 8;
+  __shared__ T tile[kBlock * LD];
+  __shared__ float red[4];
+  __shared__ int bad[4];
+  const int head = blockIdx.y, row = blockIdx.z, tid = threadIdx.x;
+  const int g = row / c.width;
+  const int64_t slot = (int64_t)g * c.beams + row % c.width;
+  const int len = c.len[g], cnt = append_count(c, g, n, counts);
+  if (blockIdx.x == 0 && head == 0 && row % c.width == 0 && tid == 0) c.pend[g] = cnt;
+  const int64_t blk = len / kBlock + blockIdx.x;
+  const int64_t t0 = blk * kBlock;                       // first token of the block
+  if (cnt == 0 || t0 >= (int64_t)len + cnt) return;
+  const int begun = blockIdx.x == 0 ? len % kBlock : 0;  // tokens in the tail
+  const int end = (int)std::min<int64_t>((int64_t)len + cnt - t0, kBlock);
+  const int buf = c.sel[g];
+  const int64_t tail = c.tail_of[slot];
+  T* kt = (T*)c.ktail + c.tail_head(layer, blockIdx.x == 0 ? buf : buf ^ 1, tail, head) * (kBlock * HD);
+  T* vt = (T*)c.vtail + c.tail_head(layer, blockIdx.x == 0 ? buf : buf ^ 1, tail, head) * (kBlock * HD);
+  const bool whole = end == kBlock;
+  const int64_t ph = c.page_head(layer, c.own_page(slot, blk), head);
+  float steps[2];
+  for (int part = 0; part < 2; ++part) {
+    const T* src = part ? v : k;
+    // new tokens
+    for (int i = tid; i < (end - begun) * (HD / 2); i += 256) {
+      const int t = begun + i / (HD / 2), d = i % (HD / 2);
+      const int64_t pos = t0 + t;
+      const T* x = src + ((((int64_t)row * n + (pos - len)) * c.heads_kv + head) * HD);
+      float a = ld_val(x + d), b = ld_val(x + d + HD / 2);
+      if (part == 0 && c.rope) {
+        const float2 r = c.rope[pos * (HD / 2) + d];
+        const float a2 = a * r.x - b * r.y, b2 = b * r.x + a * r.y;
+        a = a2;
+        b = b2;
+      }
+      st_val(&tile[t * LD + d], a);
+      st_val(&tile[t * LD + d + HD / 2], b);
+    }
+    if (whole)
+      for (int i = tid; i < begun * HD; i += 256) {
+        const int t = i / HD, d = i % HD;
+        tile[t * LD + d] = part ? vt[d * kBlock + t] : kt[t * HD + d];
+      }
+    __syncthreads();
+    if (!whole) {
+      for (int i = tid; i < (end - begun) * HD; i += 256) {
+        const int t = begun + i / HD, d = i % HD;
+        if (part)
+          vt[d * kBlock + t] = tile[t * LD + d];
+        else
+          kt[t * HD + d] = tile[t * LD + d];
+      }
+    } else {
+      float a = 0.0f;
+      int inf = 0;
+      for (int i = tid; i < kBlock * HD; i += 256) {
+        const float x = fabsf(ld_val(&tile[(i / HD) * LD + i % HD]));
+        inf |= !(x < INFINITY);
+        a = fmaxf(a, x);
+      }
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor(a, o, 64));
+      inf = __any(inf);
+      if ((tid & 63) == 0) {
+        red[tid >> 6] = a;
+        bad[tid >> 6] = inf;
+      }
+      __syncthreads();
+      a = fmaxf(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])), kStepFloor);
+      inf = bad[0] | bad[1] | bad[2] | bad[3];
+      const float s = inf ? 0.0f : 127.0f * __fdiv_rn(1.0f, a);
+      steps[part] = inf ? __builtin_nanf("") : a * (1.0f / 127.0f);
+      uint8_t* page = (part ? c.vpage : c.kpage) + ph * (kBlock * HD);
+      for (int i = tid; i < kBlock * HD; i += 256) {
+        const int t = i / HD, d = i % HD;
+        const float x = inf ? 0.0f : ld_val(&tile[t * LD + d]);
+        const int q = (int)fminf(fmaxf(__builtin_rintf(x * s), -127.0f), 127.0f);
+        page[part ? value_at(t, d) : key_at<HD>(t, d)] = (uint8_t)(q + 128);
+      }
+    }
+    __syncthreads();
+  }
+  if (whole && tid == 0) c.step[ph] = make_float2(steps[0], steps[1]);
+}
+
+__global__ void __launch_bounds__(64) k_cache_begin(CacheView c, int n, const int32_t* counts) {
+  const int cnt = append_count(c, blockIdx.x, n, counts);
+  if (threadIdx.x == 0) c.pend[blockIdx.x] = cnt;
+}
+
+// The pending tokens join the sequences: own pages enter the table, a crossed block border changes
+// the tail buffer.
+__global__ void __launch_bounds__(256) k_cache_advance(CacheView c) {
+  const int g = blockIdx.x;
+  const int len = c.len[g], nl = len + c.pend[g];
+  __syncthreads();
+  for (int b = 0; b < c.width; ++b) {
+    const int64_t slot = (int64_t)g * c.beams + b;
+    for (int j = len / kBlock + threadIdx.x; j < nl / kBlock; j += 256)
+      c.table[slot * c.max_blocks + j] = (int32_t)c.own_page(slot, j);
+  }
+  if (threadIdx.x == 0) {
+    c.len[g] = nl;
+    c.pend[g] = 0;
+    if (nl / kBlock != len / kBlock) c.sel[g] ^= 1;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Reordering.  The first child of a sequence takes its tail over; further children take the tails
+// of sequences without children and get a copy of the tokens in it.  Every work group forms the
+// same assignment from the parents: tail[b] the tail of new beam b, from[b] the tail to copy into
+// it (-1: none).  parents null: all beams continue beam 0.
+// ---------------------------------------------------------------------------
+constexpr int kMaxBeams = 64;
+struct Assignment {
+  int parent[kMaxBeams], tail[kMaxBeams], from[kMaxBeams];
+};
+__device__ __forceinline__ void assign_tails(const CacheView& c, const int32_t* parents, int g,
+                                             Assignment& a) {
+  if (threadIdx.x == 0) {
+    const int W = c.beams;
+    const int64_t s0 = (int64_t)g * W;
+    unsigned long long used = 0;
+    for (int b = 0; b < W; ++b) {
+      int p = parents ? parents[s0 + b] : 0;
+      if (p < 0 || p >= W) {
+        atomicOr(c.err, 32);
+        p = b;
+      }
+      a.parent[b] = p;
+      a.tail[b] = -1;
+      a.from[b] = -1;
+      if (!(used >> p & 1)) a.tail[b] = c.tail_of[s0 + p];
+      used |= 1ull << p;
+    }
+    int spare = 0;
+    for (int b = 0; b < W; ++b)
+      if (a.tail[b] < 0) {
+        while (used >> spare & 1) ++spare;
+        a.tail[b] = c.tail_of[s0 + spare++];
+        a.from[b] = c.tail_of[s0 + a.parent[b]];
+      }
+  }
+  __syncthreads();
+}
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) k_reorder_tails(CacheView c, const int32_t* parents) {
+  __shared__ Assignment a;
+  const int layer = blockIdx.x, head = blockIdx.y, g = blockIdx.z;
+  const int t = c.len[g] % kBlock;
+  if (t == 0) return;
+  assign_tails(c, parents, g, a);
+  const int buf = c.sel[g];
+  constexpr int EPC = 16 / (int)sizeof(T);
+  const int vch = (t + EPC - 1) / EPC;                 // 16-byte pieces of a row of values
+  for (int b = 0; b < c.beams; ++b) {
+    if (a.from[b] < 0) continue;
+    const int64_t from = c.tail_head(layer, buf, a.from[b], head) * (kBlock * HD),
+                  to = c.tail_head(layer, buf, a.tail[b], head) * (kBlock * HD);
+    for (int i = threadIdx.x; i < t * HD / EPC; i += 256)
+      ((uint4*)((T*)c.ktail + to))[i] = ((const uint4*)((const T*)c.ktail + from))[i];
+    for (int i = threadIdx.x; i < HD * vch; i += 256) {
+      const int at = i / vch * (kBlock / EPC) + i % vch;
+      ((uint4*)((T*)c.vtail + to))[at] = ((const uint4*)((const T*)c.vtail + from))[at];
+    }
+  }
+}
+
+__global__ void __launch_bounds__(256) k_reorder_table(CacheView c, const int32_t* parents) {
+  __shared__ Assignment a;
+  const int g = blockIdx.x, W = c.beams;
+  assign_tails(c, parents, g, a);
+  const int64_t s0 = (int64_t)g * W;
+  int32_t old[kMaxBeams];
+  for (int64_t j = threadIdx.x; j < c.len[g] / kBlock; j += 256) {   // a thread, a column
+#pragma unroll
+    for (int b = 0; b < kMaxBeams; ++b)
+      if (b < W) old[b] = c.table[(s0 + a.parent[b]) * c.max_blocks + j];
+#pragma unroll
+    for (int b = 0; b < kMaxBeams; ++b)
+      if (b < W) c.table[(s0 + b) * c.max_blocks + j] = old[b];
+  }
+  if ((int)threadIdx.x < W) c.tail_of[s0 + threadIdx.x] = a.tail[threadIdx.x];
+}
+
+// ---------------------------------------------------------------------------
+// Values of a range of positions.  A work group takes up to 64 positions of one block of a head.
+// ---------------------------------------------------------------------------
+template <typename T, int HD, typename O>
+__global__ void __launch_bounds__(256) k_cache_read(CacheView c, int layer, int64_t first, int64_t n,
+                                                    O* ko, O* vo) {
+  const int head = blockIdx.y, row = blockIdx.z;
+  const int g = row / c.width;
+  const int64_t slot = (int64_t)g * c.beams + row % c.width;
+  const int len = c.len[g], total = len + c.pend[g];
+  const int64_t blk = first / kBlock + blockIdx.x;
+  const int64_t lo = std::max(first, blk * kBlock),
+                hi = std::min(std::min(first + n, (blk + 1) * kBlock), (int64_t)total);
+  if (lo >= hi) return;
+  const bool coded = (blk + 1) * kBlock <= total;
+  const int64_t ph = c.page_head(layer, coded ? c.page_of(slot, blk, len) : 0, head);
+  const float2 d = coded ? c.step[ph] : make_float2(0.0f, 0.0f);
+  const int buf = c.sel[g] ^ (blk != len / kBlock);
+  const int64_t th = c.tail_head(layer, buf, c.tail_of[slot], head) * (kBlock * HD);
+  for (int64_t i = threadIdx.x; i < (hi - lo) * HD; i += 256) {
+    const int64_t pos = lo + i / HD;
+    const int t = (int)(pos - blk * kBlock), e = (int)(i % HD);
+    const int64_t out = (((int64_t)row * n + (pos - first)) * c.heads_kv + head) * HD + e;
+    float kx, vx;
+    if (coded) {
+      kx = (float)((int)c.kpage[ph * (kBlock * HD) + key_at<HD>(t, e)] - 128) * d.x;
+      vx = (float)((int)c.vpage[ph * (kBlock * HD) + value_at(t, e)] - 128) * d.y;
+    } else {
+      kx = ld_val((const T*)c.ktail + th + t * HD + e);
+      vx = ld_val((const T*)c.vtail + th + e * kBlock + t);
+    }
+    if (ko) st_val(ko + out, kx);
+    if (vo) st_val(vo + out, vx);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Attention, one wave per query and head: a lane scores one token of a block, then owns dims.
+// ---------------------------------------------------------------------------
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) k_attend_plain(CacheView c, int layer, const T* q, T* out,
+                                                      int n, const int32_t* counts, int heads,
+                                                      float scale) {
+  __shared__ float qs[4][HD];
+  __shared__ float ps[4][kBlock];
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, row = blockIdx.y;
+  const int g = row / c.width;
+  const int cnt = query_count(c, g, n, counts);
+  const int64_t at = (int64_t)blockIdx.x * 4 + w;
+  const int i = (int)(at / heads), h = (int)(at % heads);
+  if (i >= cnt) return;                                  // whole wave
+  const int64_t slot = (int64_t)g * c.beams + row % c.width;
+  const int len = c.len[g], total = len + cnt, seen = len + i + 1;
+  const int head = h / (heads / c.heads_kv);
+  const T* qp = q + (((int64_t)row * n + i) * heads + h) * HD;
+  for (int d = lane; d < HD / 2; d += 64) {
+    float a = ld_val(qp + d), b = ld_val(qp + d + HD / 2);
+    if (c.rope) {
+      const float2 r = c.rope[(int64_t)(seen - 1) * (HD / 2) + d];
+      const float a2 = a * r.x - b * r.y, b2 = b * r.x + a * r.y;
+      a = a2;
+      b = b2;
+    }
+    qs[w][d] = a * scale;
+    qs[w][d + HD / 2] = b * scale;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  float m = -INFINITY, l = 0.0f, o[2] = {0.0f, 0.0f};
+  for (int t0 = 0; t0 < seen; t0 += kBlock) {
+    const int64_t blk = t0 / kBlock;
+    const bool coded = t0 + kBlock <= total;
+    const int64_t ph = c.page_head(layer, coded ? c.page_of(slot, blk, len) : 0, head);
+    const float2 d = coded ? c.step[ph] : make_float2(1.0f, 1.0f);
+    const int64_t th = c.tail_head(layer, c.sel[g] ^ (blk != len / kBlock), c.tail_of[slot], head) * (kBlock * HD);
+    const bool ok = t0 + lane < seen;
+    float s = -INFINITY;
+    if (ok) {
+      float acc = 0.0f;
+      for (int e = 0; e < HD; ++e) {
+        const float kx = coded ? (float)((int)c.kpage[ph * (kBlock * HD) + key_at<HD>(lane, e)] - 128)
+                               : ld_val((const T*)c.ktail + th + lane * HD + e);
+        acc = fmaf(qs[w][e], kx, acc);
+      }
+      s = acc * d.x;
+    }
+    float bm = s;
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) bm = fmaxf(bm, __shfl_xor(bm, x, 64));
+    const float nm = fmaxf(m, bm);
+    const float p = ok ? expf(s - nm) : 0.0f;
+    float ls = p;
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) ls += __shfl_xor(ls, x, 64);
+    const float al = m == -INFINITY ? 0.0f : expf(m - nm);
+    l = l * al + ls;
+    m = nm;
+    __builtin_amdgcn_wave_barrier();
+    ps[w][lane] = p;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const int tn = seen - t0 < kBlock ? seen - t0 : kBlock;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int e = lane + 64 * x;
+      if (e >= HD) break;
+      float acc = 0.0f;
+      for (int t = 0; t < tn; ++t) {
+        const float vx = coded ? (float)((int)c.vpage[ph * (kBlock * HD) + value_at(t, e)] - 128)
+                               : ld_val((const T*)c.vtail + th + e * kBlock + t);
+        acc = fmaf(ps[w][t], vx, acc);
+      }
+      o[x] = o[x] * al + acc * d.y;
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+  T* op = out + (((int64_t)row * n + i) * heads + h) * HD;
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+    if (lane + 64 * x < HD) st_val(op + lane + 64 * x, o[x] / l);
+}
+
+// ---------------------------------------------------------------------------
+// Launches
+// ---------------------------------------------------------------------------
+namespace {
+
+CacheView view_of(const termezo_kvcache* c) {
+  CacheView v;
+  v.kpage = c->kpage;
+  v.vpage = c->vpage;
+  v.step = c->step;
+  v.ktail = c->ktail;
+  v.vtail = c->vtail;
+  v.len = c->len;
+  v.pend = c->pend;
+  v.sel = c->sel;
+  v.tail_of = c->tail_of;
+  v.table = c->table;
+  v.rope = c->rope;
+  v.err = c->ctx->d_err;
+  v.groups = c->cfg.groups;
+  v.beams = c->cfg.beams;
+  v.width = c->width;
+  v.heads_kv = c->cfg.n_kv_heads;
+  v.slots = c->slots;
+  v.max_blocks = c->max_blocks;
+  v.max_len = c->cfg.max_len;
+  return v;
+}
+
+// f(T(), HD) with the cache's activation type and head size.
+#define TMZ_CACHE_TYPES(c, CALL)                                   \
+  if ((c)->cfg.act_dtype == TERMEZO_BF16) {                        \
+    if ((c)->cfg.head_dim == 64) { CALL(uint16_t, 64); }           \
+    else if ((c)->cfg.head_dim == 96) { CALL(uint16_t, 96); }      \
+    else { CALL(uint16_t, 128); }                                  \
+  } else {                                                         \
+    if ((c)->cfg.head_dim == 64) { CALL(float, 64); }              \
+    else if ((c)->cfg.head_dim == 96) { CALL(float, 96); }         \
+    else { CALL(float, 128); }                                     \
+  }
+
+int64_t rows_of(const termezo_kvcache* c) { return (int64_t)c->cfg.groups * c->width; }
+
+}  // namespace
+
+hipError_t cache_append_on(termezo_kvcache* c, int layer, const void* k, const void* v, int64_t n,
+                           const int32_t* counts, hipStream_t s) {
+  const CacheView w = view_of(c);
+  // blocks that n tokens can touch from any place in a block
+  const unsigned nb = (unsigned)((n + kBlock - 2) / kBlock + 1);
+  const dim3 grid(nb, (unsigned)c->cfg.n_kv_heads, (unsigned)rows_of(c));
+#define TMZ_CALL(T, HD)                                                                         \
+  hipLaunchKernelGGL((k_cache_append<T, HD>), grid, dim3(256), 0, s, w, layer, (const T*)k,      \
+                     (const T*)v, (int)n, counts)
+  TMZ_CACHE_TYPES(c, TMZ_CALL)
+#undef TMZ_CALL
+  return hipGetLastError();
+}
+
+hipError_t cache_attention_on(termezo_kvcache* c, int layer, const void* q, const void* k,
+                              const void* v, int64_t n, const int32_t* counts, void* out,
+                              hipStream_t s) {
+  if (k) {
+    const hipError_t e = cache_append_on(c, layer, k, v, n, counts, s);
+    if (e != hipSuccess) return e;
+    counts = nullptr;                                  // attention takes the pending counts
+  }
+  const CacheView w = view_of(c);
+  const int H = c->cfg.n_heads;
+  const float scale = (float)(1.0 / std::sqrt((double)c->cfg.head_dim));
+  const dim3 grid((unsigned)((n * H + 3) / 4), (unsigned)rows_of(c));
+#define TMZ_CALL(T, HD)                                                                       \
+  hipLaunchKernelGGL((k_attend_plain<T, HD>), grid, dim3(256), 0, s, w, layer, (const T*)q,    \
+                     (T*)out, (int)n, counts, H, scale)
+  TMZ_CACHE_TYPES(c, TMZ_CALL)
+#undef TMZ_CALL
+  return hipGetLastError();
+}
+
+hipError_t cache_begin_on(termezo_kvcache* c, int64_t n, const int32_t* counts, hipStream_t s) {
+  hipLaunchKernelGGL(k_cache_begin, dim3((unsigned)c->cfg.groups), dim3(64), 0, s, view_of(c), (int)n,
+                     counts);
+  return hipGetLastError();
+}
+
+hipError_t cache_advance_on(termezo_kvcache* c, hipStream_t s) {
+  hipLaunchKernelGGL(k_cache_advance, dim3((unsigned)c->cfg.groups), dim3(256), 0, s, view_of(c));
+  return hipGetLastError();
+}
+
+}  // namespace tmz
+
+// ===========================================================================
+// C ABI
+// ===========================================================================
+using namespace tmz;
+
+namespace {
+
+termezo_status cfail(termezo_kvcache* c, termezo_status st, const char* msg) {
+  c->ctx->last_error = msg;
+  return st;
+}
+
+termezo_status hip_status(termezo_kvcache* c, hipError_t e, const char* what) {
+  if (e == hipSuccess) return TERMEZO_OK;
+  c->ctx->last_error = std::string(what) + ": " + hipGetErrorString(e);
+  return e == hipErrorOutOfMemory ? TERMEZO_ERR_OOM : TERMEZO_ERR_DEVICE;
+}
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+void cache_free(termezo_kvcache* c) {
+  void* all[] = {c->kpage, c->vpage, c->step, c->ktail, c->vtail, c->len, c->tail_of, c->table,
+                 c->rope, c->part};
+  for (void* p : all)
+    if (p) (void)hipFree(p);
+}
+
+termezo_status cache_reset(termezo_kvcache* c, int g0, int g1) {
+  const unsigned nb = (unsigned)(((int64_t)(g1 - g0) * c->cfg.beams + 255) / 256);
+  hipLaunchKernelGGL(k_cache_reset, dim3(nb), dim3(256), 0, c->stream, view_of(c), g0, g1);
+  return hip_status(c, hipGetLastError(), "kvcache_reset");
+}
+
+termezo_status check_tokens(termezo_kvcache* c, int32_t layer, const void* a, const void* b, int64_t n,
+                            const int32_t* counts, const char* what) {
+  if (layer < 0 || layer >= c->cfg.n_layers || n <= 0 || n > c->cfg.max_len || !a || !b ||
+      !aligned16(a) || !aligned16(b) || (reinterpret_cast<uintptr_t>(counts) & 3u) != 0) {
+    c->ctx->last_error = std::string(what) + ": layer or n out of range, or a null or misaligned pointer";
+    return TERMEZO_ERR_INVALID_ARG;
+  }
+  return TERMEZO_OK;
+}
+
+termezo_status cache_reorder(termezo_kvcache* c, const int32_t* parents) {
+  const CacheView w = view_of(c);
+  const dim3 grid((unsigned)c->cfg.n_layers, (unsigned)c->cfg.n_kv_heads, (unsigned)c->cfg.groups);
+#define TMZ_CALL(T, HD) \
+  hipLaunchKernelGGL((k_reorder_tails<T, HD>), grid, dim3(256), 0, c->stream, w, parents)
+  TMZ_CACHE_TYPES(c, TMZ_CALL)
+#undef TMZ_CALL
+  hipLaunchKernelGGL(k_reorder_table, dim3((unsigned)c->cfg.groups), dim3(256), 0, c->stream, w, parents);
+  return hip_status(c, hipGetLastError(), "kvcache_reorder");
+}
+
+}  // namespace
+
+extern "C" {
+
+termezo_status termezo_kvcache_create(termezo_ctx* ctx, const termezo_kvcache_config* cfg,
+                                      termezo_kvcache** out) {
+  if (!out) return TERMEZO_ERR_INVALID_ARG;
+  *out = nullptr;
+  if (!ctx || !cfg) return TERMEZO_ERR_INVALID_ARG;
+  const termezo_kvcache_config& f = *cfg;
+  const int hd = f.head_dim;
+  const bool sizes = f.n_layers > 0 && f.n_layers <= 65535 && f.n_heads > 0 && f.n_heads <= 65535 &&
+                     f.n_kv_heads > 0 && f.n_heads % f.n_kv_heads == 0 &&
+                     (hd == 64 || hd == 96 || hd == 128) && f.groups > 0 && f.beams > 0 &&
+                     f.beams <= kMaxBeams && (int64_t)f.groups * f.beams <= 65535 && f.max_len > 0 &&
+                     f.max_len <= (int64_t(1) << 24);
+  if (!sizes || (f.act_dtype != TERMEZO_F32 && f.act_dtype != TERMEZO_BF16) ||
+      !(f.rope_base == 0.0f || (f.rope_base > 1.0f && std::isfinite(f.rope_base)))) {
+    ctx->last_error = "kvcache_create: a size, the type or rope_base is out of range";
+    return TERMEZO_ERR_INVALID_ARG;
+  }
+  const int64_t slots = (int64_t)f.groups * f.beams, nblk = (f.max_len + kBlock - 1) / kBlock;
+  if (slots * nblk > INT32_MAX) {
+    ctx->last_error = "kvcache_create: more than 2^31 - 1 pages";
+    return TERMEZO_ERR_INVALID_ARG;
+  }
+  termezo_kvcache* c = new (std::nothrow) termezo_kvcache();
+  if (!c) return TERMEZO_ERR_OOM;
+  c->ctx = ctx;
+  c->stream = ctx->stream;
+  c->device = ctx->device;
+  c->cfg = f;
+  c->slots = slots;
+  c->max_blocks = nblk;
+  c->width = 1;
+  DeviceScope scope(c->device);
+  hipError_t e = scope.err;
+  // sizes in doubles first: what no device holds must not wrap around
+  const double heads = (double)f.n_layers * slots * f.n_kv_heads, page = (double)kBlock * hd;
+  if (e == hipSuccess && heads * nblk * page * 2 > 1e13) e = hipErrorOutOfMemory;
+  auto A = [&](void** p, int64_t bytes) {
+    if (e == hipSuccess) e = hipMalloc(p, (size_t)bytes);
+  };
+  if (e == hipSuccess) {
+    const int64_t ph = (int64_t)f.n_layers * slots * f.n_kv_heads;
+    const int64_t es = f.act_dtype == TERMEZO_BF16 ? 2 : 4;
+    A((void**)&c->kpage, ph * nblk * kBlock * hd);
+    A((void**)&c->vpage, ph * nblk * kBlock * hd);
+    A((void**)&c->step, ph * nblk * 8);
+    A(&c->ktail, ph * 2 * kBlock * hd * es);
+    A(&c->vtail, ph * 2 * kBlock * hd * es);
+    A((void**)&c->len, (int64_t)f.groups * 12);
+    A((void**)&c->tail_of, slots * 4);
+    A((void**)&c->table, slots * nblk * 4);
+    if (f.rope_base > 0.0f) A((void**)&c->rope, f.max_len * (hd / 2) * 8);
+  }
+  termezo_status st = hip_status(c, e, "kvcache_create");
+  if (st == TERMEZO_OK) {
+    c->pend = c->len + f.groups;
+    c->sel = c->pend + f.groups;
+    if (c->rope) {
+      const int64_t n = f.max_len * (hd / 2);
+      RopeFreq w = {};
+      for (int i = 0; i < hd / 2; ++i) w.f[i] = std::pow((double)f.rope_base, -2.0 * i / (double)hd);
+      hipLaunchKernelGGL(k_rope_table, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, c->stream,
+                         c->rope, f.max_len, hd / 2, w);
+      st = hip_status(c, hipGetLastError(), "kvcache_create");
+    }
+    if (st == TERMEZO_OK) st = cache_reset(c, 0, f.groups);
+  }
+  if (st != TERMEZO_OK) {
+    cache_free(c);
+    delete c;
+    return st;
+  }
+  *out = c;
+  return TERMEZO_OK;
+}
+
+void termezo_kvcache_destroy(termezo_kvcache* c) {
+  if (!c) return;
+  DeviceScope scope(c->device);
+  (void)hipStreamSynchronize(c->stream);
+  cache_free(c);
+  delete c;
+}
+
+termezo_status termezo_kvcache_reset(termezo_kvcache* c, int32_t group) {
+  if (!c) return TERMEZO_ERR_INVALID_ARG;
+  if (group < -1 || group >= c->cfg.groups)
+    return cfail(c, TERMEZO_ERR_INVALID_ARG, "kvcache_reset: group out of range");
+  DeviceScope scope(c->device);
+  if (scope.err != hipSuccess) return hip_status(c, scope.err, "kvcache_reset");
+  if (group < 0) {
+    c->width = 1;
+    c->pending = false;
+  }
+  return cache_reset(c, group < 0 ? 0 : group, group < 0 ? c->cfg.groups : group + 1);
+}
+
+termezo_status termezo_kvcache_fork(termezo_kvcache* c) {
+  if (!c) return TERMEZO_ERR_INVALID_ARG;
+  if (c->pending) return cfail(c, TERMEZO_ERR_STATE, "kvcache_fork: appended tokens are pending");
+  if (c->width == c->cfg.beams) return cfail(c, TERMEZO_ERR_STATE, "kvcache_fork: every beam is in use");
+  DeviceScope scope(c->device);
+  if (scope.err != hipSuccess) return hip_status(c, scope.err, "kvcache_fork");
+  const termezo_status st = cache_reorder(c, nullptr);
+  if (st == TERMEZO_OK) c->width = c->cfg.beams;
+  return st;
+}
+
+termezo_status termezo_kvcache_append(termezo_kvcache* c, int32_t layer, const void* k, const void* v,
+                                      int64_t n, const int32_t* counts) {
+  if (!c) return TERMEZO_ERR_INVALID_ARG;
+  const termezo_status st = check_tokens(c, layer, k, v, n, counts, "kvcache_append");
+  if (st != TERMEZO_OK) return st;
+  DeviceScope scope(c->device);
+  if (scope.err != hipSuccess) return hip_status(c, scope.err, "kvcache_append");
+  c->pending = true;
+  return hip_status(c, cache_append_on(c, layer, k, v, n, counts, c->stream), "kvcache_append");
+}
+
+termezo_status termezo_kvcache_attention(termezo_kvcache* c, int32_t layer, const void* q,
+                                         const void* k, const void* v, int64_t n,
+                                         const int32_t* counts, void* out) {
+  if (!c) return TERMEZO_ERR_INVALID_ARG;
+  termezo_status st = check_tokens(c, layer, q, out, n, counts, "kvcache_attention");
+  if (st == TERMEZO_OK && (k || v)) st = check_tokens(c, layer, k, v, n, counts, "kvcache_attention");
+  if (st != TERMEZO_OK) return st;
+  if (!k && !c->pending)
+    return cfail(c, TERMEZO_ERR_STATE, "kvcache_attention: no tokens are pending");
+  DeviceScope scope(c->device);
+  if (scope.err != hipSuccess) return hip_status(c, scope.err, "kvcache_attention");
+  if (k) c->pending = true;
+  return hip_status(c, cache_attention_on(c, layer, q, k, v, n, counts, out, c->stream),
+                    "kvcache_attention");
+}
+
+termezo_status termezo_kvcache_advance(termezo_kvcache* c) {
+  if (!c) return TERMEZO_ERR_INVALID_ARG;
+  if (!c->pending) return cfail(c, TERMEZO_ERR_STATE, "kvcache_advance: no tokens are pending");
+  DeviceScope scope(c->device);
+  if (scope.err != hipSuccess) return hip_status(c, scope.err, "kvcache_advance");
+  c->pending = false;
+  return hip_status(c, cache_advance_on(c, c->stream), "kvcache_advance");
+}
+
+termezo_status termezo_kvcache_reorder(termezo_kvcache* c, const int32_t* parents) {
+  if (!c) return TERMEZO_ERR_INVALID_ARG;
+  if (!parents || (reinterpret_cast<uintptr_t>(parents) & 3u) != 0)
+    return cfail(c, TERMEZO_ERR_INVALID_ARG, "kvcache_reorder: null or misaligned parents");
+  if (c->pending) return cfail(c, TERMEZO_ERR_STATE, "kvcache_reorder: appended tokens are pending");
+  if (c->width != c->cfg.beams) return cfail(c, TERMEZO_ERR_STATE, "kvcache_reorder: not forked");
+  DeviceScope scope(c->device);
+  if (scope.err != hipSuccess) return hip_status(c, scope.err, "kvcache_reorder");
+  return cache_reorder(c, parents);
+}
+
+termezo_status termezo_kvcache_read(termezo_kvcache* c, int32_t layer, int64_t first, int64_t n,
+                                    void* k_out, void* v_out, termezo_dtype dtype) {
+  if (!c) return TERMEZO_ERR_INVALID_ARG;
+  if (layer < 0 || layer >= c->cfg.n_layers || first < 0 || n <= 0 || first > c->cfg.max_len - n ||
+      (dtype != TERMEZO_F32 && dtype != TERMEZO_BF16) || !aligned16(k_out) || !aligned16(v_out) ||
+      (!k_out && !v_out))
+    return cfail(c, TERMEZO_ERR_INVALID_ARG, "kvcache_read: an argument is out of range, null or misaligned");
+  DeviceScope scope(c->device);
+  if (scope.err != hipSuccess) return hip_status(c, scope.err, "kvcache_read");
+  const CacheView w = view_of(c);
+  const unsigned nb = (unsigned)((first + n - 1) / kBlock - first / kBlock + 1);
+  const dim3 grid(nb, (unsigned)c->cfg.n_kv_heads, (unsigned)rows_of(c));
+#define TMZ_CALL(T, HD)                                                                          \
+  if (dtype == TERMEZO_F32)                                                                      \
+    hipLaunchKernelGGL((k_cache_read<T, HD, float>), grid, dim3(256), 0, c->stream, w, layer, first, \
+                       n, (float*)k_out, (float*)v_out);                                         \
+  else                                                                                           \
+    hipLaunchKernelGGL((k_cache_read<T, HD, uint16_t>), grid, dim3(256), 0, c->stream, w, layer, \
+                       first, n, (uint16_t*)k_out, (uint16_t*)v_out)
+  TMZ_CACHE_TYPES(c, TMZ_CALL)
+#undef TMZ_CALL
+  return hip_status(c, hipGetLastError(), "kvcache_read");
+}
+
+termezo_status termezo_kvcache_lengths(termezo_kvcache* c, int32_t* lengths) {
+  if (!c) return TERMEZO_ERR_INVALID_ARG;
+  if (!lengths) return cfail(c, TERMEZO_ERR_INVALID_ARG, "kvcache_lengths: null");
+  DeviceScope scope(c->device);
+  if (scope.err != hipSuccess) return hip_status(c, scope.err, "kvcache_lengths");
+  const termezo_status st = termezo_sync(c->ctx);
+  if (st != TERMEZO_OK) return st;
+  return hip_status(c, hipMemcpy(lengths, c->len, (size_t)c->cfg.groups * 4, hipMemcpyDeviceToHost),
+                    "kvcache_lengths");
+}
+
+}  // extern "C"

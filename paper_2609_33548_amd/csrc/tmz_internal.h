@@ -222,6 +222,8 @@ struct termezo_ctx {
   bool has_mask = false;
   bool codes_valid = false;
   bool pending_perturb = false;
+  void* d_beam = nullptr;            // beam selection: the chunks' candidates, maxima and sums
+  int64_t beam_cap = 0;              // its bytes
   uint64_t last_seed = 0;
   float last_eps = 0.f;
   float delta = 1e-5f;
@@ -354,5 +356,59 @@ hipError_t launch_bitlinear_gemm(const int8_t* xq, const float* s, const int32_t
                                  hipStream_t st);
 // gemm_tiled_xq for the single output y of launch_bitlinear_gemm.
 bool bitlinear_tiled_xq(int64_t M, int64_t K, int64_t N, const void* y, termezo_dtype ydt, int n_cu);
+
+}  // namespace tmz
+
+// 8-bit cache of keys and values (tmz_cache.hip).  A slot is one sequence's place; slot
+// group * beams + b is beam b of a group.
+struct termezo_kvcache {
+  termezo_ctx* ctx = nullptr;
+  hipStream_t stream = nullptr;      // the context's (destroy never reads ctx)
+  int device = 0;
+  termezo_kvcache_config cfg{};
+  int width = 1;                     // sequences of a group in use: 1, after a fork beams
+  bool pending = false;              // tokens appended since the last advance
+  int64_t slots = 0, max_blocks = 0;
+  uint8_t *kpage = nullptr, *vpage = nullptr;
+  float2* step = nullptr;
+  void *ktail = nullptr, *vtail = nullptr;
+  int32_t *len = nullptr, *pend = nullptr, *sel = nullptr;      // [groups], one allocation
+  int32_t *tail_of = nullptr, *table = nullptr;                 // [slots], [slots][max_blocks]
+  float2* rope = nullptr;                                       // [max_len][head_dim / 2]
+  float* part = nullptr;             // partial results of attention split over the tokens
+  int64_t part_floats = 0;
+};
+
+namespace tmz {
+
+// Sets the current device for a scope.
+struct DeviceScope {
+  int prev = -1;
+  hipError_t err = hipSuccess;
+  explicit DeviceScope(int device) {
+    err = hipGetDevice(&prev);
+    if (err == hipSuccess && prev != device)
+      err = hipSetDevice(device);
+    else
+      prev = -1;
+  }
+  ~DeviceScope() {
+    if (prev >= 0) (void)hipSetDevice(prev);
+  }
+  DeviceScope(const DeviceScope&) = delete;
+  DeviceScope& operator=(const DeviceScope&) = delete;
+};
+
+// The cache's calls on a stream of the caller's choice (checked arguments).
+hipError_t cache_append_on(termezo_kvcache* c, int layer, const void* k, const void* v, int64_t n,
+                           const int32_t* counts, hipStream_t s);
+hipError_t cache_attention_on(termezo_kvcache* c, int layer, const void* q, const void* k,
+                              const void* v, int64_t n, const int32_t* counts, void* out,
+                              hipStream_t s);
+hipError_t cache_advance_on(termezo_kvcache* c, hipStream_t s);
+// Checks a step's counts once: afterwards c->pend holds the tokens that every group takes.
+hipError_t cache_begin_on(termezo_kvcache* c, int64_t n, const int32_t* counts, hipStream_t s);
+hipError_t launch_logits(const void* x, const void* E, termezo_dtype dt, int64_t M, int64_t d,
+                         int64_t V, float* out, int n_cu, hipStream_t s);
 
 }  // namespace tmz

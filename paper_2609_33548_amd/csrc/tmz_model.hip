@@ -96,6 +96,39 @@ __global__ void __launch_bounds__(256) k_embed(const int32_t* tok, const T* E, i
   }
 }
 
+// Hidden states of a generation step: row r's tokens are tok[r n ..], as many as its group has
+// pending; what lies behind them is zero and its id is not looked at.
+template <typename T>
+__global__ void __launch_bounds__(256) k_embed_rows(const int32_t* tok, const T* E, int64_t d,
+                                                    int64_t V, int n, int width, const int32_t* pend,
+                                                    T* h, int32_t* err) {
+  const int64_t m = blockIdx.x;
+  const bool live = (int)(m % n) < pend[m / n / width];
+  int64_t t = live ? tok[m] : 0;
+  if (t < 0 || t >= V) {
+    if (threadIdx.x == 0) atomicOr(err, 8);
+    t = 0;
+  }
+  constexpr int EPC = 16 / (int)sizeof(T);    // d is a multiple of 16 and both are aligned
+  const uint4* src = reinterpret_cast<const uint4*>(E + t * d);
+  uint4* dst = reinterpret_cast<uint4*>(h + m * d);
+  for (int64_t c = threadIdx.x; c < d / EPC; c += 256)
+    dst[c] = live ? src[c] : make_uint4(0u, 0u, 0u, 0u);
+}
+
+// out[r] = the hidden state of row r's last pending token, zero where there is none.
+template <typename T>
+__global__ void __launch_bounds__(256) k_last_rows(const T* h, int64_t d, int n, int width,
+                                                   const int32_t* pend, T* out) {
+  const int64_t r = blockIdx.x;
+  const int cnt = pend[r / width];
+  constexpr int EPC = 16 / (int)sizeof(T);
+  const uint4* src = reinterpret_cast<const uint4*>(h + (r * n + (cnt > 0 ? cnt - 1 : 0)) * d);
+  uint4* dst = reinterpret_cast<uint4*>(out + r * d);
+  for (int64_t c = threadIdx.x; c < d / EPC; c += 256)
+    dst[c] = cnt > 0 ? src[c] : make_uint4(0u, 0u, 0u, 0u);
+}
+
 // ---------------------------------------------------------------------------
 // Row kernels, one wave per token row, 8 elements (one 16-byte bf16 load, or
 // two 16-byte fp32 loads) per lane per chunk, the row kept in registers:
@@ -1729,6 +1762,15 @@ __global__ void __launch_bounds__(256) k_loss_mean(const float* row_loss, int64_
 // ===========================================================================
 using namespace tmz;
 
+// Activations of one forward over M tokens.
+struct Acts {
+  void *h = nullptr, *q = nullptr, *k = nullptr, *v = nullptr, *attn = nullptr, *g = nullptr,
+       *u = nullptr, *xf = nullptr;
+  int8_t* xq = nullptr;
+  float* xs = nullptr;
+  int32_t* xrs = nullptr;                    // per-token sums of the quantised activations
+};
+
 struct termezo_model {
   termezo_ctx* ctx = nullptr;
   hipStream_t stream = nullptr;   // the context's stream, or the model's own (destroy never reads ctx)
@@ -1742,11 +1784,10 @@ struct termezo_model {
   int hd = 0;
   int64_t cap_M = 0;
   int cap_S = 0;
-  void *h = nullptr, *q = nullptr, *k = nullptr, *v = nullptr, *vt = nullptr, *attn = nullptr,
-       *g = nullptr, *u = nullptr, *xf = nullptr;
-  int8_t* xq = nullptr;
-  float* xs = nullptr;
-  int32_t* xrs = nullptr;                    // per-token sums of the quantised activations
+  Acts a;
+  void* vt = nullptr;
+  Acts dec;                                  // of generation steps (termezo_model_decode)
+  int64_t cap_dec = 0;                       // tokens they hold
   float *pmax = nullptr, *psum = nullptr, *lab = nullptr, *row = nullptr;
   int32_t* labels = nullptr;
   float *rope_c = nullptr, *rope_s = nullptr;
@@ -1806,14 +1847,17 @@ LaunchEvents span_kernel(termezo_model* m, int cls, double ops) {
   return ev;
 }
 
+void acts_free(Acts& a) {
+  void* all[] = {a.h, a.q, a.k, a.v, a.attn, a.g, a.u, a.xf, a.xq, a.xs, a.xrs};
+  for (void* p : all)
+    if (p) (void)hipFree(p);
+  a = Acts();
+}
+
 void model_free_buffers(termezo_model* m) {
-  mfree(m->h); mfree(m->q); mfree(m->k); mfree(m->v); mfree(m->vt); mfree(m->attn); mfree(m->g);
-  mfree(m->u);
-  mfree(m->xf);
+  acts_free(m->a);
+  mfree(m->vt);
   void* p;
-  p = m->xq; mfree(p); m->xq = nullptr;
-  p = m->xs; mfree(p); m->xs = nullptr;
-  p = m->xrs; mfree(p); m->xrs = nullptr;
   p = m->pmax; mfree(p); m->pmax = nullptr;
   p = m->psum; mfree(p); m->psum = nullptr;
   p = m->lab; mfree(p); m->lab = nullptr;
@@ -1827,6 +1871,30 @@ void model_free_buffers(termezo_model* m) {
   m->cap_S = 0;
 }
 
+// Activations of M tokens; on an error acts_free frees what there is.
+hipError_t acts_alloc(Acts& a, const termezo_model_config& c, int hd, int64_t M) {
+  const size_t es = c.act_dtype == TERMEZO_BF16 ? 2 : 4;
+  const int64_t dq = (int64_t)c.n_heads * hd, dkv = (int64_t)c.n_kv_heads * hd;
+  const int64_t kmax = std::max<int64_t>(std::max<int64_t>(c.d_model, dq), c.d_ffn);
+  hipError_t e = hipSuccess;
+  auto A = [&](void** p, size_t bytes) {
+    if (e == hipSuccess) e = hipMalloc(p, bytes > 0 ? bytes : 1);
+  };
+  A(&a.h, M * c.d_model * es);
+  A(&a.q, M * dq * es);
+  A(&a.k, M * dkv * es);
+  A(&a.v, M * dkv * es);
+  A(&a.attn, M * dq * es);
+  A(&a.g, M * c.d_ffn * es);
+  A(&a.u, M * c.d_ffn * es);
+  A(&a.xf, M * c.d_model * es);
+  // row-major, or in fragment order for the small calls that this reservation also serves
+  A((void**)&a.xq, std::max(M * kmax, xq_bytes(std::min<int64_t>(M, kGemvMaxM), kmax)));
+  A((void**)&a.xs, M * 4);
+  A((void**)&a.xrs, rs_entries(M) * 4);
+  return e;
+}
+
 // Tokens of a row of V^T: whole 64-token tiles.
 int64_t vt_tokens(int64_t S) { return (S + 63) / 64 * 64; }
 
@@ -1835,28 +1903,15 @@ termezo_status model_reserve(termezo_model* m, int64_t M, int S) {
   model_free_buffers(m);
   const termezo_model_config& c = m->cfg;
   const size_t es = c.act_dtype == TERMEZO_BF16 ? 2 : 4;
-  const int64_t dq = (int64_t)c.n_heads * m->hd, dkv = (int64_t)c.n_kv_heads * m->hd;
-  const int64_t kmax = std::max<int64_t>(std::max<int64_t>(c.d_model, dq), c.d_ffn);
+  const int64_t dkv = (int64_t)c.n_kv_heads * m->hd;
   const int64_t nvt = c.act_dtype == TERMEZO_BF16 ? (c.vocab + kLmTile - 1) / kLmTile
                                                   : (c.vocab + kVT - 1) / kVT;
-  hipError_t e = hipSuccess;
+  hipError_t e = acts_alloc(m->a, c, m->hd, M);
   auto A = [&](void** p, size_t bytes) {
     if (e == hipSuccess) e = hipMalloc(p, bytes > 0 ? bytes : 1);
   };
-  A(&m->h, M * c.d_model * es);
-  A(&m->q, M * dq * es);
-  A(&m->k, M * dkv * es);
-  A(&m->v, M * dkv * es);
   // V^T of every sequence: M / S rows of whole tiles (S is part of the reservation's key)
   A(&m->vt, (M + S - 1) / S * vt_tokens(S) * dkv * es);
-  A(&m->attn, M * dq * es);
-  A(&m->g, M * c.d_ffn * es);
-  A(&m->u, M * c.d_ffn * es);
-  A(&m->xf, M * c.d_model * es);
-  // row-major, or in fragment order for the small calls that this reservation also serves
-  A((void**)&m->xq, std::max(M * kmax, xq_bytes(std::min<int64_t>(M, kGemvMaxM), kmax)));
-  A((void**)&m->xs, M * 4);
-  A((void**)&m->xrs, rs_entries(M) * 4);
   A((void**)&m->pmax, M * nvt * 4);
   A((void**)&m->psum, M * nvt * 4);
   A((void**)&m->lab, M * 4);
@@ -1897,8 +1952,8 @@ hipError_t run_attention(termezo_model* m, int B, int S, hipStream_t st) {
     // four queries per block while their scores fit the default 64 KB of LDS
     const int nw = S <= 4096 ? 4 : 1;
     hipLaunchKernelGGL(k_attn_f32, dim3((unsigned)((M + nw - 1) / nw), c.n_heads), dim3(64 * nw),
-                       nw * S * sizeof(float), st, (const float*)m->q, (const float*)m->k,
-                       (const float*)m->v, (float*)m->attn, M, S, c.n_heads, c.n_kv_heads, m->hd,
+                       nw * S * sizeof(float), st, (const float*)m->a.q, (const float*)m->a.k,
+                       (const float*)m->a.v, (float*)m->a.attn, M, S, c.n_heads, c.n_kv_heads, m->hd,
                        1.0f / std::sqrt((float)m->hd));
     return hipGetLastError();
   }
@@ -1907,11 +1962,11 @@ hipError_t run_attention(termezo_model* m, int B, int S, hipStream_t st) {
   dim3 pgrid((unsigned)((S + 63) / 64), (unsigned)(B * c.n_kv_heads));
   dim3 grid((unsigned)((S + 127) / 128), c.n_heads, B);
 #define TMZ_ATTN(HDV)                                                                        \
-  hipLaunchKernelGGL(k_kv_prep<HDV>, pgrid, dim3(256), 0, st, (uint16_t*)m->k,                  \
-                     (const uint16_t*)m->v, (uint16_t*)m->vt, S, vs, c.n_kv_heads, m->rope_c,      \
+  hipLaunchKernelGGL(k_kv_prep<HDV>, pgrid, dim3(256), 0, st, (uint16_t*)m->a.k,                  \
+                     (const uint16_t*)m->a.v, (uint16_t*)m->vt, S, vs, c.n_kv_heads, m->rope_c,      \
                      m->rope_s);                                                              \
-  hipLaunchKernelGGL(k_attn_bf16<HDV>, grid, dim3(512), 0, st, (const uint16_t*)m->q,          \
-                     (const uint16_t*)m->k, (const uint16_t*)m->vt, (uint16_t*)m->attn, S, vs, \
+  hipLaunchKernelGGL(k_attn_bf16<HDV>, grid, dim3(512), 0, st, (const uint16_t*)m->a.q,          \
+                     (const uint16_t*)m->a.k, (const uint16_t*)m->vt, (uint16_t*)m->a.attn, S, vs, \
                      c.n_heads, c.n_kv_heads, sl2, m->rope_c, m->rope_s)
   const int G = c.n_heads / c.n_kv_heads;
   const bool gqa = (m->hd == 64 || m->hd == 96 || m->hd == 128) &&
@@ -1920,21 +1975,21 @@ hipError_t run_attention(termezo_model* m, int B, int S, hipStream_t st) {
   if (gqa) {
     const int nbh = B * c.n_kv_heads, nqt = S / (256 / G);
     if (m->hd == 128)
-      hipLaunchKernelGGL(k_kv_prep<128>, pgrid, dim3(256), 0, st, (uint16_t*)m->k,
-                         (const uint16_t*)m->v, (uint16_t*)m->vt, S, vs, c.n_kv_heads, m->rope_c,
+      hipLaunchKernelGGL(k_kv_prep<128>, pgrid, dim3(256), 0, st, (uint16_t*)m->a.k,
+                         (const uint16_t*)m->a.v, (uint16_t*)m->vt, S, vs, c.n_kv_heads, m->rope_c,
                          m->rope_s);
     else if (m->hd == 96)
-      hipLaunchKernelGGL(k_kv_prep<96>, pgrid, dim3(256), 0, st, (uint16_t*)m->k,
-                         (const uint16_t*)m->v, (uint16_t*)m->vt, S, vs, c.n_kv_heads, m->rope_c,
+      hipLaunchKernelGGL(k_kv_prep<96>, pgrid, dim3(256), 0, st, (uint16_t*)m->a.k,
+                         (const uint16_t*)m->a.v, (uint16_t*)m->vt, S, vs, c.n_kv_heads, m->rope_c,
                          m->rope_s);
     else
-      hipLaunchKernelGGL(k_kv_prep<64>, pgrid, dim3(256), 0, st, (uint16_t*)m->k,
-                         (const uint16_t*)m->v, (uint16_t*)m->vt, S, vs, c.n_kv_heads, m->rope_c,
+      hipLaunchKernelGGL(k_kv_prep<64>, pgrid, dim3(256), 0, st, (uint16_t*)m->a.k,
+                         (const uint16_t*)m->a.v, (uint16_t*)m->vt, S, vs, c.n_kv_heads, m->rope_c,
                          m->rope_s);
 #define TMZ_GQA(HDV, GV)                                                                      \
   hipLaunchKernelGGL((k_attn_gqa<HDV, GV>), dim3((unsigned)(nqt * nbh)), dim3(512), 0, st,      \
-                     (const uint16_t*)m->q, (const uint16_t*)m->k, (const uint16_t*)m->vt,     \
-                     (uint16_t*)m->attn, S, c.n_kv_heads, nbh, nqt, sl2, m->rope_c, m->rope_s)
+                     (const uint16_t*)m->a.q, (const uint16_t*)m->a.k, (const uint16_t*)m->vt,     \
+                     (uint16_t*)m->a.attn, S, c.n_kv_heads, nbh, nqt, sl2, m->rope_c, m->rope_s)
     switch (m->hd * 16 + G) {
       case 128 * 16 + 1: TMZ_GQA(128, 1); break;
       case 128 * 16 + 2: TMZ_GQA(128, 2); break;
@@ -1961,6 +2016,138 @@ hipError_t run_attention(termezo_model* m, int B, int S, hipStream_t st) {
   }
 #undef TMZ_ATTN
   return hipGetLastError();
+}
+
+// RMSNorm of M rows of h (weight row wr of the norm weights nrm, one when there are none), then
+// the quantiser, or stored in xf (the LM-head input).
+hipError_t norm_rows(termezo_model* m, const void* h, int64_t M, const void* nrm, int wr, Acts& A,
+                     void* xf, bool tiled, hipStream_t s) {
+  const termezo_model_config& cf = m->cfg;
+  const int64_t d = cf.d_model;
+  const unsigned rowg = (unsigned)((M + 3) / 4);
+#define TMZ_NORM(T, MD, W)                                                                   \
+  row_launch<MD, T, W>(rowg, s, (const T*)h,                                                 \
+                       nrm ? (const T*)nrm + (int64_t)wr * d : (const T*)nullptr, M, d,      \
+                       cf.norm_eps, xf ? nullptr : A.xq, xf ? nullptr : A.xs, A.xrs, (T*)xf, \
+                       tiled, m->ctx->n_cu)
+  if (cf.act_dtype == TERMEZO_BF16) {
+    if (xf) {
+      if (nrm) TMZ_NORM(uint16_t, kRowNormStore, true); else TMZ_NORM(uint16_t, kRowNormStore, false);
+    } else {
+      if (nrm) TMZ_NORM(uint16_t, kRowNormQuant, true); else TMZ_NORM(uint16_t, kRowNormQuant, false);
+    }
+  } else {
+    if (xf) {
+      if (nrm) TMZ_NORM(float, kRowNormStore, true); else TMZ_NORM(float, kRowNormStore, false);
+    } else {
+      if (nrm) TMZ_NORM(float, kRowNormQuant, true); else TMZ_NORM(float, kRowNormQuant, false);
+    }
+  }
+#undef TMZ_NORM
+  return hipGetLastError();
+}
+
+// The blocks of a forward over the M tokens whose hidden states are in A.h: attend(blk) turns A.q,
+// A.k and A.v into A.attn.  timed: the GEMMs are recorded where the model's timing is on.
+template <typename Attend>
+hipError_t run_blocks(termezo_model* m, Acts& A, int64_t M, const uint32_t* codes, const float* betas,
+                      const void* nrm, hipStream_t s, bool timed, Attend attend) {
+  termezo_ctx* c = m->ctx;
+  const termezo_model_config& cf = m->cfg;
+  const termezo_dtype adt = cf.act_dtype;
+  const bool bf = adt == TERMEZO_BF16;
+  const int64_t d = cf.d_model, F = cf.d_ffn, dq = (int64_t)cf.n_heads * m->hd,
+                dkv = (int64_t)cf.n_kv_heads * m->hd;
+  hipError_t e = hipSuccess;
+  auto chk = [&](hipError_t x) {
+    if (e == hipSuccess) e = x;
+  };
+  auto span = [&](double ops) { return timed ? span_kernel(m, 0, ops) : LaunchEvents(); };
+  const unsigned rowg = (unsigned)((M + 3) / 4);
+  // the layout of the quantised activations that each projection's GEMM takes (whole output
+  // units: every width is a multiple of 16)
+  const bool t_qkv = gemm_tiled_xq(M, d, dq + 2 * dkv, true, c->n_cu),
+             t_o = gemm_tiled_xq(M, dq, d, true, c->n_cu),
+             t_gu = gemm_tiled_xq(M, d, 2 * F, true, c->n_cu),
+             t_d = gemm_tiled_xq(M, F, d, true, c->n_cu);
+  for (int blk = 0; blk < cf.n_blocks; ++blk) {
+    const int l0 = 7 * blk;
+    const LayerHost* Ls = &c->layers[l0];
+    // attention sub-block
+    chk(norm_rows(m, A.h, M, nrm, 2 * blk, A, nullptr, t_qkv, s));
+    GemmOut o3 = {};
+    o3.nseg = 3;
+    o3.y[0] = A.q; o3.ld[0] = dq; o3.beta[0] = betas + l0;
+    o3.y[1] = A.k; o3.ld[1] = dkv; o3.beta[1] = betas + l0 + 1;
+    o3.y[2] = A.v; o3.ld[2] = dkv; o3.beta[2] = betas + l0 + 2;
+    o3.nstart[0] = 0; o3.nstart[1] = dq; o3.nstart[2] = dq + dkv; o3.nstart[3] = dq + 2 * dkv;
+    chk(launch_gemm_i8(A.xq, A.xs, A.xrs, codes + Ls[0].code_off, M, d, dq + 2 * dkv, o3, adt,
+                       kGemmStore, nullptr, t_qkv, c->n_cu, s,
+                       span(2.0 * M * d * (dq + 2 * dkv))));
+    chk(attend(blk));
+    if (bf)
+      row_launch<kRowQuant, uint16_t>(rowg, s, (const uint16_t*)A.attn, (const uint16_t*)nullptr,
+                                      M, dq, 0.0f, A.xq, A.xs, A.xrs, (uint16_t*)nullptr, t_o,
+                                      c->n_cu);
+    else
+      row_launch<kRowQuant, float>(rowg, s, (const float*)A.attn, (const float*)nullptr, M, dq,
+                                   0.0f, A.xq, A.xs, A.xrs, (float*)nullptr, t_o);
+    chk(hipGetLastError());
+    GemmOut oo = {};
+    oo.nseg = 1;
+    oo.y[0] = A.h; oo.ld[0] = d; oo.beta[0] = betas + l0 + 3;
+    oo.nstart[0] = 0; oo.nstart[1] = d;
+    chk(launch_gemm_i8(A.xq, A.xs, A.xrs, codes + Ls[3].code_off, M, dq, d, oo, adt, kGemmResidual,
+                       nullptr, t_o, c->n_cu, s,
+                       span(2.0 * M * dq * d)));
+    // MLP sub-block
+    chk(norm_rows(m, A.h, M, nrm, 2 * blk + 1, A, nullptr, t_gu, s));
+    GemmOut o2 = {};
+    o2.nseg = 2;
+    o2.y[0] = A.g; o2.ld[0] = F; o2.beta[0] = betas + l0 + 4;
+    o2.y[1] = A.u; o2.ld[1] = F; o2.beta[1] = betas + l0 + 5;
+    o2.nstart[0] = 0; o2.nstart[1] = F; o2.nstart[2] = 2 * F;
+    // gate|up with the SwiGLU in the epilogue where the direct-load path applies (the
+    // product lands in g), else the two projections and the SwiGLU row kernel
+    const bool fused = !t_gu && gemm_swiglu_ok(M, d, 2 * F, adt, codes + Ls[4].code_off);
+    chk(launch_gemm_i8(A.xq, A.xs, A.xrs, codes + Ls[4].code_off, M, d, 2 * F, o2, adt,
+                       fused ? kGemmSwiGLU : kGemmStore, nullptr, t_gu, c->n_cu, s,
+                       span(2.0 * M * d * 2 * F)));
+    if (fused)
+      row_launch<kRowQuant, uint16_t>(rowg, s, (const uint16_t*)A.g, (const uint16_t*)nullptr, M,
+                                      F, 0.0f, A.xq, A.xs, A.xrs, (uint16_t*)nullptr, t_d,
+                                      c->n_cu);
+    else if (bf)
+      row_launch<kRowSwiGLU, uint16_t>(rowg, s, (const uint16_t*)A.g, (const uint16_t*)A.u, M,
+                                       F, 0.0f, A.xq, A.xs, A.xrs, (uint16_t*)nullptr, t_d);
+    else
+      row_launch<kRowSwiGLU, float>(rowg, s, (const float*)A.g, (const float*)A.u, M, F, 0.0f,
+                                    A.xq, A.xs, A.xrs, (float*)nullptr, t_d);
+    chk(hipGetLastError());
+    GemmOut od = {};
+    od.nseg = 1;
+    od.y[0] = A.h; od.ld[0] = d; od.beta[0] = betas + l0 + 6;
+    od.nstart[0] = 0; od.nstart[1] = d;
+    chk(launch_gemm_i8(A.xq, A.xs, A.xrs, codes + Ls[6].code_off, M, F, d, od, adt, kGemmResidual,
+                       nullptr, t_d, c->n_cu, s,
+                       span(2.0 * M * F * d)));
+  }
+  return e;
+}
+
+// The parameters that a forward reads now: a registered theta tensor at its current (possibly
+// perturbed) values.
+const void* current_values(const termezo_ctx* c, const void* p) {
+  if (!p || c->theta_sign == 0) return p;
+  for (const ThetaHost& t : c->theta)
+    if (t.data == p) return c->theta_sign > 0 ? t.plus : t.minus;
+  return p;
+}
+
+// Everything queued on the context's stream so far comes before the model's work.
+bool after_context(termezo_model* m) {
+  return !m->own_stream || (hipEventRecord(m->ev_in, m->ctx->stream) == hipSuccess &&
+                            hipStreamWaitEvent(m->stream, m->ev_in, 0) == hipSuccess);
 }
 
 }  // namespace
@@ -2052,6 +2239,7 @@ void termezo_model_destroy(termezo_model* m) {
   if (m->ev_in) (void)hipEventDestroy(m->ev_in);
   if (m->ev_out) (void)hipEventDestroy(m->ev_out);
   model_free_buffers(m);
+  acts_free(m->dec);
   delete m;
 }
 
@@ -2105,145 +2293,46 @@ termezo_status termezo_model_loss(termezo_model* m, const int32_t* tokens, int32
   termezo_status st = model_reserve(m, M, seq);
   if (st != TERMEZO_OK) return st;
   hipStream_t s = m->stream;
-  if (m->own_stream &&   // everything queued on the context's stream so far comes first
-      (hipEventRecord(m->ev_in, c->stream) != hipSuccess ||
-       hipStreamWaitEvent(s, m->ev_in, 0) != hipSuccess)) {
+  if (!after_context(m)) {
     c->last_error = "model_loss: event record / wait";
     return TERMEZO_ERR_DEVICE;
   }
   const uint32_t* codes = m->use_snap ? c->d_codes_snap : c->d_codes;
   const float* betas = m->use_snap ? c->d_beta_snap : c->d_beta_cur;
   const bool bf = cf.act_dtype == TERMEZO_BF16;
-  // full-precision parameters: a registered theta tensor is read at its current
-  // (possibly perturbed) values
-  auto current = [&](const void* p) -> const void* {
-    if (!p || c->theta_sign == 0) return p;
-    for (const ThetaHost& t : c->theta)
-      if (t.data == p) return c->theta_sign > 0 ? t.plus : t.minus;
-    return p;
-  };
-  const void* emb = current(m->emb);
-  const void* nrm = current(m->normw);
-  const int64_t d = cf.d_model, F = cf.d_ffn, dq = (int64_t)cf.n_heads * m->hd,
-                dkv = (int64_t)cf.n_kv_heads * m->hd;
+  const void* emb = current_values(c, m->emb);
+  const void* nrm = current_values(c, m->normw);
+  const int64_t d = cf.d_model;
   const int64_t nvt = bf ? (cf.vocab + kLmTile - 1) / kLmTile : (cf.vocab + kVT - 1) / kVT;
   hipError_t e = hipSuccess;
   auto chk = [&](hipError_t x) {
     if (e == hipSuccess) e = x;
   };
-  const termezo_dtype adt = cf.act_dtype;
 
   if (bf)
     hipLaunchKernelGGL(k_embed<uint16_t>, dim3((unsigned)M), dim3(256), 0, s, tokens,
-                       (const uint16_t*)emb, d, (int64_t)cf.vocab, seq, (uint16_t*)m->h, m->labels,
+                       (const uint16_t*)emb, d, (int64_t)cf.vocab, seq, (uint16_t*)m->a.h, m->labels,
                        c->d_err);
   else
     hipLaunchKernelGGL(k_embed<float>, dim3((unsigned)M), dim3(256), 0, s, tokens,
-                       (const float*)emb, d, (int64_t)cf.vocab, seq, (float*)m->h, m->labels,
+                       (const float*)emb, d, (int64_t)cf.vocab, seq, (float*)m->a.h, m->labels,
                        c->d_err);
   chk(hipGetLastError());
-  const unsigned rowg = (unsigned)((M + 3) / 4);
-  // the layout of the quantised activations that each projection's GEMM takes (whole output
-  // units: every width is a multiple of 16)
-  const bool t_qkv = gemm_tiled_xq(M, d, dq + 2 * dkv, true, c->n_cu),
-             t_o = gemm_tiled_xq(M, dq, d, true, c->n_cu),
-             t_gu = gemm_tiled_xq(M, d, 2 * F, true, c->n_cu),
-             t_d = gemm_tiled_xq(M, F, d, true, c->n_cu);
-  // RMSNorm (weight row wr of the norm weights, one when there are none), then
-  // the quantiser, or stored (the LM-head input)
-  auto rmsq = [&](int8_t* xq, float* xs, void* xf, int wr, bool tiled) {
-#define TMZ_NORM(T, MD, W)                                                                   \
-  row_launch<MD, T, W>(rowg, s, (const T*)m->h,                                              \
-                       nrm ? (const T*)nrm + (int64_t)wr * d : (const T*)nullptr, M, d,      \
-                       cf.norm_eps, xq, xs, m->xrs, (T*)xf, tiled, c->n_cu)
-    if (bf) {
-      if (xf) {
-        if (nrm) TMZ_NORM(uint16_t, kRowNormStore, true); else TMZ_NORM(uint16_t, kRowNormStore, false);
-      } else {
-        if (nrm) TMZ_NORM(uint16_t, kRowNormQuant, true); else TMZ_NORM(uint16_t, kRowNormQuant, false);
-      }
-    } else {
-      if (xf) {
-        if (nrm) TMZ_NORM(float, kRowNormStore, true); else TMZ_NORM(float, kRowNormStore, false);
-      } else {
-        if (nrm) TMZ_NORM(float, kRowNormQuant, true); else TMZ_NORM(float, kRowNormQuant, false);
-      }
-    }
-#undef TMZ_NORM
-    chk(hipGetLastError());
-  };
-  for (int blk = 0; blk < cf.n_blocks; ++blk) {
-    const int l0 = 7 * blk;
-    const LayerHost* Ls = &c->layers[l0];
-    // attention sub-block
-    rmsq(m->xq, m->xs, nullptr, 2 * blk, t_qkv);
-    GemmOut o3 = {};
-    o3.nseg = 3;
-    o3.y[0] = m->q; o3.ld[0] = dq; o3.beta[0] = betas + l0;
-    o3.y[1] = m->k; o3.ld[1] = dkv; o3.beta[1] = betas + l0 + 1;
-    o3.y[2] = m->v; o3.ld[2] = dkv; o3.beta[2] = betas + l0 + 2;
-    o3.nstart[0] = 0; o3.nstart[1] = dq; o3.nstart[2] = dq + dkv; o3.nstart[3] = dq + 2 * dkv;
-    chk(launch_gemm_i8(m->xq, m->xs, m->xrs, codes + Ls[0].code_off, M, d, dq + 2 * dkv, o3, adt,
-                       kGemmStore, nullptr, t_qkv, c->n_cu, s,
-                       span_kernel(m, 0, 2.0 * M * d * (dq + 2 * dkv))));
+  chk(run_blocks(m, m->a, M, codes, betas, nrm, s, true, [&](int) -> hipError_t {
     if (!bf) {   // bf16: the rotation is applied inside the attention kernel
       const unsigned rg = (unsigned)std::min<int64_t>(
           8192, (M * (cf.n_heads + cf.n_kv_heads) * (m->hd / 2) + 255) / 256);
-      hipLaunchKernelGGL(k_rope<float>, dim3(rg), dim3(256), 0, s, (float*)m->q, (float*)m->k, M,
+      hipLaunchKernelGGL(k_rope<float>, dim3(rg), dim3(256), 0, s, (float*)m->a.q, (float*)m->a.k, M,
                          cf.n_heads, cf.n_kv_heads, m->hd, seq, m->rope_c, m->rope_s);
-      chk(hipGetLastError());
+      const hipError_t er = hipGetLastError();
+      if (er != hipSuccess) return er;
     }
     const int sp = span_begin(m, 1, 4.0 * batch * cf.n_heads * m->hd * (0.5 * seq * (seq + 1.0)), s);
-    chk(run_attention(m, batch, seq, s));
+    const hipError_t ea = run_attention(m, batch, seq, s);
     span_end(m, sp, s);
-    if (bf)
-      row_launch<kRowQuant, uint16_t>(rowg, s, (const uint16_t*)m->attn, (const uint16_t*)nullptr,
-                                      M, dq, 0.0f, m->xq, m->xs, m->xrs, (uint16_t*)nullptr, t_o,
-                                      c->n_cu);
-    else
-      row_launch<kRowQuant, float>(rowg, s, (const float*)m->attn, (const float*)nullptr, M, dq,
-                                   0.0f, m->xq, m->xs, m->xrs, (float*)nullptr, t_o);
-    chk(hipGetLastError());
-    GemmOut oo = {};
-    oo.nseg = 1;
-    oo.y[0] = m->h; oo.ld[0] = d; oo.beta[0] = betas + l0 + 3;
-    oo.nstart[0] = 0; oo.nstart[1] = d;
-    chk(launch_gemm_i8(m->xq, m->xs, m->xrs, codes + Ls[3].code_off, M, dq, d, oo, adt, kGemmResidual,
-                       nullptr, t_o, c->n_cu, s,
-                       span_kernel(m, 0, 2.0 * M * dq * d)));
-    // MLP sub-block
-    rmsq(m->xq, m->xs, nullptr, 2 * blk + 1, t_gu);
-    GemmOut o2 = {};
-    o2.nseg = 2;
-    o2.y[0] = m->g; o2.ld[0] = F; o2.beta[0] = betas + l0 + 4;
-    o2.y[1] = m->u; o2.ld[1] = F; o2.beta[1] = betas + l0 + 5;
-    o2.nstart[0] = 0; o2.nstart[1] = F; o2.nstart[2] = 2 * F;
-    // gate|up with the SwiGLU in the epilogue where the direct-load path applies (the
-    // product lands in g), else the two projections and the SwiGLU row kernel
-    const bool fused = !t_gu && gemm_swiglu_ok(M, d, 2 * F, adt, codes + Ls[4].code_off);
-    chk(launch_gemm_i8(m->xq, m->xs, m->xrs, codes + Ls[4].code_off, M, d, 2 * F, o2, adt,
-                       fused ? kGemmSwiGLU : kGemmStore, nullptr, t_gu, c->n_cu, s,
-                       span_kernel(m, 0, 2.0 * M * d * 2 * F)));
-    if (fused)
-      row_launch<kRowQuant, uint16_t>(rowg, s, (const uint16_t*)m->g, (const uint16_t*)nullptr, M,
-                                      F, 0.0f, m->xq, m->xs, m->xrs, (uint16_t*)nullptr, t_d,
-                                      c->n_cu);
-    else if (bf)
-      row_launch<kRowSwiGLU, uint16_t>(rowg, s, (const uint16_t*)m->g, (const uint16_t*)m->u, M,
-                                       F, 0.0f, m->xq, m->xs, m->xrs, (uint16_t*)nullptr, t_d);
-    else
-      row_launch<kRowSwiGLU, float>(rowg, s, (const float*)m->g, (const float*)m->u, M, F, 0.0f,
-                                    m->xq, m->xs, m->xrs, (float*)nullptr, t_d);
-    chk(hipGetLastError());
-    GemmOut od = {};
-    od.nseg = 1;
-    od.y[0] = m->h; od.ld[0] = d; od.beta[0] = betas + l0 + 6;
-    od.nstart[0] = 0; od.nstart[1] = d;
-    chk(launch_gemm_i8(m->xq, m->xs, m->xrs, codes + Ls[6].code_off, M, F, d, od, adt, kGemmResidual,
-                       nullptr, t_d, c->n_cu, s,
-                       span_kernel(m, 0, 2.0 * M * F * d)));
-  }
-  rmsq(nullptr, nullptr, m->xf, 2 * cf.n_blocks, false);
+    return ea;
+  }));
+  chk(norm_rows(m, m->a.h, M, nrm, 2 * cf.n_blocks, m->a, m->a.xf, false, s));
   const LaunchEvents ev_lm = span_kernel(m, 2, 2.0 * M * d * cf.vocab);
   if (bf) {
     const unsigned nb = (unsigned)(nvt * ((M + kLmTile - 1) / kLmTile));
@@ -2252,16 +2341,16 @@ termezo_status termezo_model_loss(termezo_model* m, const int32_t* tokens, int32
     if (d % kLmDmaBK == 0)
       hipExtLaunchKernelGGL((k_lmhead_dma<kLmDmaStages, kLmDmaBK, kLmDmaNWN>), dim3(nbp),
                             dim3(128 * kLmDmaNWN), 0, s, ev_lm.start, ev_lm.stop, 0,
-                            (const uint16_t*)m->xf, (const uint16_t*)emb, M, d, (int64_t)cf.vocab,
+                            (const uint16_t*)m->a.xf, (const uint16_t*)emb, M, d, (int64_t)cf.vocab,
                             m->labels, m->pmax, m->psum, m->lab, nvt);
     else
       hipExtLaunchKernelGGL(k_lmhead_bf16<false>, dim3(nb), dim3(512), 0, s, ev_lm.start,
-                            ev_lm.stop, 0, (const uint16_t*)m->xf, (const uint16_t*)emb, M, d,
+                            ev_lm.stop, 0, (const uint16_t*)m->a.xf, (const uint16_t*)emb, M, d,
                             (int64_t)cf.vocab, m->labels, m->pmax, m->psum, m->lab, nvt);
   }
   else
     hipExtLaunchKernelGGL(k_lmhead_f32, dim3((unsigned)nvt, (unsigned)((M + 31) / 32)), dim3(512), 0,
-                          s, ev_lm.start, ev_lm.stop, 0, (const float*)m->xf, (const float*)emb, M,
+                          s, ev_lm.start, ev_lm.stop, 0, (const float*)m->a.xf, (const float*)emb, M,
                           d, (int64_t)cf.vocab, m->labels, m->pmax, m->psum, m->lab, nvt);
   chk(hipGetLastError());
   float* rows = row_loss_dev ? row_loss_dev : m->row;
@@ -2284,6 +2373,85 @@ termezo_status termezo_model_loss(termezo_model* m, const int32_t* tokens, int32
     *loss_host = (float)v;
   }
   return TERMEZO_OK;
+}
+
+
+termezo_status termezo_model_decode(termezo_model* m, termezo_kvcache* kv, const int32_t* tokens,
+                                    int64_t n, const int32_t* counts, float* logits) {
+  if (!m || !kv) return TERMEZO_ERR_INVALID_ARG;
+  termezo_ctx* c = m->ctx;
+  const termezo_model_config& cf = m->cfg;
+  auto refuse = [&](termezo_status st, const char* msg) {
+    c->last_error = msg;
+    return st;
+  };
+  if (!tokens || !logits || n <= 0 || (reinterpret_cast<uintptr_t>(logits) & 15u) != 0 ||
+      (reinterpret_cast<uintptr_t>(tokens) & 3u) != 0 || (reinterpret_cast<uintptr_t>(counts) & 3u) != 0)
+    return refuse(TERMEZO_ERR_INVALID_ARG, "model_decode: n <= 0, or a null or misaligned pointer");
+  const termezo_kvcache_config& kc = kv->cfg;
+  if (kv->ctx != c || kc.n_layers != cf.n_blocks || kc.n_heads != cf.n_heads ||
+      kc.n_kv_heads != cf.n_kv_heads || kc.head_dim != m->hd || kc.act_dtype != cf.act_dtype ||
+      kc.rope_base != cf.rope_base)
+    return refuse(TERMEZO_ERR_INVALID_ARG, "model_decode: the cache was not made for this model");
+  const int64_t rows = (int64_t)kc.groups * kv->width, M = rows * n;
+  if (n > kc.max_len || M > INT32_MAX / 4)
+    return refuse(TERMEZO_ERR_INVALID_ARG, "model_decode: more tokens than the cache or a call takes");
+  if (kv->pending) return refuse(TERMEZO_ERR_STATE, "model_decode: appended tokens are pending");
+  if (m->use_snap ? !c->snap_valid : !c->codes_valid)
+    return refuse(TERMEZO_ERR_STATE, m->use_snap ? "model_decode: no codes snapshot"
+                                                 : "model_decode: no current codes (perturb first)");
+  DeviceScope scope(c->device);
+  hipError_t e = scope.err;
+  auto chk = [&](hipError_t x) {
+    if (e == hipSuccess) e = x;
+  };
+  auto failed = [&]() {
+    c->last_error = std::string("model_decode: ") + hipGetErrorString(e);
+    return e == hipErrorOutOfMemory ? TERMEZO_ERR_OOM : TERMEZO_ERR_DEVICE;
+  };
+  if (e == hipSuccess && M > m->cap_dec) {
+    acts_free(m->dec);
+    m->cap_dec = 0;
+    e = acts_alloc(m->dec, cf, m->hd, M);
+    if (e != hipSuccess) acts_free(m->dec);
+    else m->cap_dec = M;
+  }
+  if (e != hipSuccess) return failed();
+  if (!after_context(m)) return refuse(TERMEZO_ERR_DEVICE, "model_decode: event record / wait");
+  hipStream_t s = m->stream;
+  const uint32_t* codes = m->use_snap ? c->d_codes_snap : c->d_codes;
+  const float* betas = m->use_snap ? c->d_beta_snap : c->d_beta_cur;
+  const bool bf = cf.act_dtype == TERMEZO_BF16;
+  const void* emb = current_values(c, m->emb);
+  const void* nrm = current_values(c, m->normw);
+  const int64_t d = cf.d_model;
+  Acts& A = m->dec;
+  chk(cache_begin_on(kv, n, counts, s));
+  const unsigned eg = (unsigned)M;
+#define TMZ_EMBED(T)                                                                              \
+  hipLaunchKernelGGL(k_embed_rows<T>, dim3(eg), dim3(256), 0, s, tokens, (const T*)emb, d,        \
+                     (int64_t)cf.vocab, (int)n, kv->width, kv->pend, (T*)A.h, c->d_err)
+  if (bf) TMZ_EMBED(uint16_t); else TMZ_EMBED(float);
+#undef TMZ_EMBED
+  chk(hipGetLastError());
+  chk(run_blocks(m, A, M, codes, betas, nrm, s, false, [&](int blk) {
+    return cache_attention_on(kv, blk, A.q, A.k, A.v, n, kv->pend, A.attn, s);
+  }));
+  // the last new token of every row: its hidden state (in A.q's place), norm and logits
+  const void* last = A.h;
+  if (n > 1 || counts) {
+    last = A.q;
+#define TMZ_LAST(T)                                                                               \
+  hipLaunchKernelGGL(k_last_rows<T>, dim3((unsigned)rows), dim3(256), 0, s, (const T*)A.h, d, (int)n, \
+                     kv->width, kv->pend, (T*)A.q)
+    if (bf) TMZ_LAST(uint16_t); else TMZ_LAST(float);
+#undef TMZ_LAST
+    chk(hipGetLastError());
+  }
+  chk(norm_rows(m, last, rows, nrm, 2 * cf.n_blocks, A, A.xf, false, s));
+  chk(launch_logits(A.xf, emb, cf.act_dtype, rows, d, cf.vocab, logits, c->n_cu, s));
+  chk(cache_advance_on(kv, s));
+  return e == hipSuccess ? TERMEZO_OK : failed();
 }
 
 }  // extern "C"

@@ -91,8 +91,12 @@ termezo_status report_error(termezo_ctx* c, int32_t err) {
     if (err & 4)
       msg += "compact mode: a layer's threshold moved by more than its frozen latents' margin "
              "(their codes were kept; rebuild the mask from full latents); ";
-    if (err & 8) msg += "model_loss: a token id lies outside [0, vocab) (read as id 0); ";
-    return fail(c, (err & ~8) ? TERMEZO_ERR_NUMERIC : TERMEZO_ERR_INVALID_ARG, msg);
+    if (err & 8) msg += "a model call: a token id lies outside [0, vocab) (read as id 0); ";
+    if (err & 16)
+      msg += "kvcache: a group's token count lies outside 0 .. n, is not the pending one, or its "
+             "tokens do not fit max_len (the group was left out); ";
+    if (err & 32) msg += "kvcache_reorder: a parent lies outside the group (its sequence was kept); ";
+    return fail(c, (err & 7) ? TERMEZO_ERR_NUMERIC : TERMEZO_ERR_INVALID_ARG, msg);
   }
   return TERMEZO_OK;
 }
@@ -208,6 +212,7 @@ void free_all(termezo_ctx* c) {
   dfree(c->d_shrink_flags);
   dfree(c->d_loss);
   dfree(c->d_scal);
+  dfree(c->d_beam);
   dfree(c->d_xq);
   dfree(c->d_xs);
   dfree(c->d_xrs);

@@ -46,6 +46,13 @@ class ModelConfig(ctypes.Structure):
                 ("act_dtype", ctypes.c_int32)]
 
 
+class KVCacheConfig(ctypes.Structure):
+    _fields_ = [("n_layers", ctypes.c_int32), ("n_heads", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("beams", ctypes.c_int32), ("max_len", ctypes.c_int64),
+                ("rope_base", ctypes.c_float), ("act_dtype", ctypes.c_int32)]
+
+
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2609_33548_amd.build`")
 
@@ -93,11 +100,25 @@ _SIGS = {
     "termezo_model_set_stream": [_P, _P],
     "termezo_model_use_snapshot": [_P, _i32],
     "termezo_model_join": [_P],
+    "termezo_kvcache_create": [_P, _P, ctypes.POINTER(_P)],
+    "termezo_kvcache_destroy": [_P],
+    "termezo_kvcache_reset": [_P, _i32],
+    "termezo_kvcache_fork": [_P],
+    "termezo_kvcache_append": [_P, _i32, _P, _P, _i64, _P],
+    "termezo_kvcache_attention": [_P, _i32, _P, _P, _P, _i64, _P, _P],
+    "termezo_kvcache_advance": [_P],
+    "termezo_kvcache_reorder": [_P, _P],
+    "termezo_kvcache_read": [_P, _i32, _i64, _i64, _P, _P, _i32],
+    "termezo_kvcache_lengths": [_P, _P],
+    "termezo_logits": [_P, _P, _P, _i32, _i64, _i64, _i64, _P],
+    "termezo_beam_select": [_P, _P, _P, _P, _i32, _i32, _i32, _i32, _i32, _P, _P, _P, _P, _P, _P, _i64],
+    "termezo_model_decode": [_P, _P, _P, _i64, _P, _P],
 }
 for _name, _args in _SIGS.items():
     _fn = getattr(_lib, _name)
     _fn.argtypes = _args
-    _fn.restype = None if _name in ("termezo_destroy", "termezo_model_destroy") else (
+    _fn.restype = None if _name in ("termezo_destroy", "termezo_model_destroy",
+                                    "termezo_kvcache_destroy") else (
         ctypes.c_char_p if _name == "termezo_last_error" else ctypes.c_int)
 
 lib = _lib
@@ -129,6 +150,17 @@ def _dtype_code(t) -> int:
     if t.dtype == torch.bfloat16:
         return BF16
     raise TypeError(f"unsupported dtype {t.dtype}")
+
+
+def _tensor(t, name, shape, dtypes, device):
+    """Device address of a contiguous tensor of one of the given types; None in shape: any size."""
+    dtypes = dtypes if isinstance(dtypes, tuple) else (dtypes,)
+    if (t.dtype not in dtypes or t.dim() != len(shape) or not t.is_contiguous() or t.device != device
+            or any(s is not None and s != n for s, n in zip(shape, t.shape))):
+        want = "x".join("*" if s is None else str(s) for s in shape)
+        raise ValueError(f"{name} must be a contiguous {'/'.join(str(d) for d in dtypes)} tensor "
+                         f"[{want}] on {device}, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return int(t.data_ptr())
 
 
 def _stream_handle(stream) -> Optional[int]:
@@ -171,6 +203,7 @@ class Context:
         self.handle = termezo_create([(w.data_ptr(), w.shape[0], w.shape[1]) for w in latents],
                                      self.dtype_code, int(self._stream.cuda_stream))
         self._models = weakref.WeakSet()
+        self.device = latents[0].device
         _LIVE.add(self)
 
     def _check(self, st: int, what: str):
@@ -365,6 +398,150 @@ class Context:
                                               _ptr(loss_dev)), "mse_loss_dev")
 
 
+    # -- choosing the next tokens -------------------------------------------------
+    def logits(self, x, embedding, out):
+        """out[m, t] = x[m] . embedding[t]: x [M, d] and embedding [vocab, d] in fp32 or bf16, out
+        fp32 [M, vocab]."""
+        import torch
+        types = (torch.float32, torch.bfloat16)
+        M, d = x.shape
+        V = embedding.shape[0]
+        px = _tensor(x, "x", (M, d), types, self.device)
+        pe = _tensor(embedding, "embedding", (V, d), x.dtype, self.device)
+        po = _tensor(out, "out", (M, V), torch.float32, self.device)
+        self._check(_lib.termezo_logits(self.handle, px, pe, _dtype_code(x), M, d, V, po), "logits")
+
+    def beam_select(self, logits, scores, out_scores, out_tokens, out_parents, eos: int = -1,
+                    finished=None, out_finished=None, history=None, out_history=None):
+        """The best continuations of every search (equal ones by the lowest beam * vocab + token):
+        logits [groups, beams, vocab] and scores [groups, beams] fp32 in; out_scores fp32, out_tokens
+        and out_parents int32, all [groups, n_out]; finished uint8 [groups, beams] and out_finished
+        [groups, n_out]; history int32 [groups, beams, T] and out_history [groups, n_out, T + 1]."""
+        import torch
+        B, W, V = logits.shape
+        n = out_scores.shape[-1]
+        f32, i32, u8 = torch.float32, torch.int32, torch.uint8
+        opt = lambda t, *a: None if t is None else _tensor(t, *a, self.device)
+        T = 0 if history is None else history.shape[-1]
+        self._check(_lib.termezo_beam_select(
+            self.handle, _tensor(logits, "logits", (B, W, V), f32, self.device),
+            _tensor(scores, "scores", (B, W), f32, self.device),
+            opt(finished, "finished", (B, W), u8), B, W, V, n, eos,
+            _tensor(out_scores, "out_scores", (B, n), f32, self.device),
+            _tensor(out_tokens, "out_tokens", (B, n), i32, self.device),
+            _tensor(out_parents, "out_parents", (B, n), i32, self.device),
+            opt(out_finished, "out_finished", (B, n), u8), opt(history, "history", (B, W, T), i32),
+            opt(out_history, "out_history", (B, n, T + 1), i32), T), "beam_select")
+
+
+class KVCache:
+    """Keys and values of ``groups * beams`` sequences in 8 bits (a step for each block of 64 tokens
+    and head; the incomplete last block in ``dtype``) and the attention over them.  Until ``fork``
+    only the first beam of every group is in use: ``rows`` tells how many sequences the calls take."""
+
+    def __init__(self, ctx: Context, n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int,
+                 max_len: int, groups: int, beams: int = 1, rope_base: float = 10000.0, dtype=None):
+        import torch
+        self.ctx = ctx
+        self.dtype = dtype = torch.bfloat16 if dtype is None else dtype
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError(f"unsupported dtype {dtype}")
+        self.groups, self.beams, self._width = groups, beams, 1
+        self.n_heads, self.n_kv_heads, self.head_dim, self.max_len = n_heads, n_kv_heads, head_dim, max_len
+        cfg = KVCacheConfig(n_layers, n_heads, n_kv_heads, head_dim, groups, beams, max_len, rope_base,
+                            F32 if dtype == torch.float32 else BF16)
+        out = _P()
+        ctx._check(_lib.termezo_kvcache_create(ctx.handle, ctypes.byref(cfg), ctypes.byref(out)),
+                   "kvcache_create")
+        self.handle = out.value
+        ctx._models.add(self)                 # closed before its context
+
+    @property
+    def rows(self) -> int:
+        return self.groups * self._width
+
+    def _counts(self, counts):
+        import torch
+        return None if counts is None else _tensor(counts, "counts", (self.groups,), torch.int32,
+                                                   self.ctx.device)
+
+    def _heads(self, t, name, heads, n=None):
+        return _tensor(t, name, (self.rows, n, heads, self.head_dim), self.dtype, self.ctx.device)
+
+    def append(self, layer: int, k, v, counts=None):
+        """k, v [rows, n, n_kv_heads, head_dim]: the first counts[g] (None: n) tokens of every row
+        become pending in one layer."""
+        n = k.shape[1]
+        self.ctx._check(_lib.termezo_kvcache_append(
+            self.handle, layer, self._heads(k, "k", self.n_kv_heads), self._heads(v, "v", self.n_kv_heads, n),
+            n, self._counts(counts)), "kvcache_append")
+
+    def attention(self, layer: int, q, out, k=None, v=None, counts=None):
+        """Causal attention of the pending tokens' queries q [rows, n, n_heads, head_dim] into out
+        (same shape); k and v, when given, are appended first."""
+        n = q.shape[1]
+        opt = lambda t, name: None if t is None else self._heads(t, name, self.n_kv_heads, n)
+        self.ctx._check(_lib.termezo_kvcache_attention(
+            self.handle, layer, self._heads(q, "q", self.n_heads), opt(k, "k"), opt(v, "v"), n,
+            self._counts(counts), self._heads(out, "out", self.n_heads, n)), "kvcache_attention")
+
+    def advance(self):
+        """The pending tokens become part of the sequences."""
+        self.ctx._check(_lib.termezo_kvcache_advance(self.handle), "kvcache_advance")
+
+    def reset(self, group: int = -1):
+        self.ctx._check(_lib.termezo_kvcache_reset(self.handle, group), "kvcache_reset")
+        if group < 0:
+            self._width = 1
+
+    def fork(self):
+        """Every beam continues what the first beam of its group holds."""
+        self.ctx._check(_lib.termezo_kvcache_fork(self.handle), "kvcache_fork")
+        self._width = self.beams
+
+    def reorder(self, parents):
+        """Beam b of a group continues what beam parents[group, b] held (int32 [groups, beams])."""
+        import torch
+        self.ctx._check(_lib.termezo_kvcache_reorder(
+            self.handle, _tensor(parents, "parents", (self.groups, self.beams), torch.int32,
+                                 self.ctx.device)), "kvcache_reorder")
+
+    def read(self, layer: int, first: int, k_out=None, v_out=None):
+        """Values at positions first .. into k_out and v_out [rows, n, n_kv_heads, head_dim] (fp32 or
+        bf16, one type); positions behind a row's last token are not written."""
+        import torch
+        some = k_out if k_out is not None else v_out
+        if some is None:
+            raise ValueError("read needs k_out or v_out")
+        if some.dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError(f"unsupported dtype {some.dtype}")
+        n = some.shape[1]
+        ptr = lambda t, name: None if t is None else _tensor(
+            t, name, (self.rows, n, self.n_kv_heads, self.head_dim), some.dtype, self.ctx.device)
+        self.ctx._check(_lib.termezo_kvcache_read(
+            self.handle, layer, first, n, ptr(k_out, "k_out"), ptr(v_out, "v_out"), _dtype_code(some)),
+            "kvcache_read")
+
+    def lengths(self) -> np.ndarray:
+        """Tokens of every group (waits for the stream)."""
+        buf = np.empty(self.groups, np.int32)
+        self.ctx._check(_lib.termezo_kvcache_lengths(self.handle, buf.ctypes.data), "kvcache_lengths")
+        return buf
+
+    def close(self):
+        if getattr(self, "handle", None):
+            _lib.termezo_kvcache_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            if _is_finalizing():
+                return
+            self.close()
+        except Exception:
+            pass
+
+
 class Model:
     """BitNet decoder bound to a Context whose layers are the 7 projections of
     each block (q, k, v, o, gate, up, down); ``embedding`` is the frozen tied
@@ -399,6 +576,18 @@ class Model:
                                      _ptr(row_loss_dev), ctypes.byref(out) if host else None)
         self.ctx._check(st, "model_loss")
         return float(np.float32(out.value)) if host else None
+
+    def decode(self, cache: KVCache, tokens, logits, counts=None):
+        """One generation step: the tokens (int32 [rows, n], counts[g] of them) join ``cache``;
+        logits fp32 [rows, vocab] of every row's last one (no wait)."""
+        import torch
+        dev = self.ctx.device
+        n = tokens.shape[1]
+        self.ctx._check(_lib.termezo_model_decode(
+            self.handle, cache.handle, _tensor(tokens, "tokens", (cache.rows, n), torch.int32, dev), n,
+            cache._counts(counts),
+            _tensor(logits, "logits", (cache.rows, self.embedding.shape[0]), torch.float32, dev)),
+            "model_decode")
 
     def set_stream(self, stream):
         """Run this model's forwards on ``stream`` (a torch stream; None: the context's)."""
