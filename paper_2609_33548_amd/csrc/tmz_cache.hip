@@ -420,6 +420,532 @@ __global__ void __launch_bounds__(256) k_attend_plain(CacheView c, int layer, co
 }
 
 // ---------------------------------------------------------------------------
+// Attention of a few queries (up to 32 (query, head) columns of a key/value head) over a long cache.
+//
+// Scores are formed as S^T = K Q^T and the output as O^T += V^T P^T with 16x16x32 fp16 matrix
+// instructions: a lane then holds the scores of one query (column lane % 16) for tokens
+// 4 (lane / 16) + r of each 16, which is the operand layout of P^T, so the probabilities never leave
+// their registers, and running maximum, sum and rescaling are a lane's own.
+//
+// Codes are exact in fp16: a byte u beside 0x64 is the fp16 number 1024 + u, less 1152 is q.  A query
+// is scaled by a power of two to a largest magnitude in [512, 1024) and rounded to fp16 (2^-11; one
+// rounding less than the bf16 that the rotated query would be stored in); fp32 activations take it in
+// two parts (2^-22).  Probabilities are scaled by 2^15 and rounded to fp16, again in two parts for
+// fp32.  Maxima, sums and outputs are fp32.  O is kept in units of the largest step of the values so
+// far (Lv): a block's probabilities take the ratio of its step to that one.  The newest tokens, not
+// coded yet, pass the same way: scaled by powers of two to magnitudes below 128, bf16 values are exact in
+// fp16 and fp32 ones taken in two parts.
+//
+// A non-finite value makes every query that sees it NaN and no other: a block with such a value has the
+// step NaN, which is put into the scores of its visible tokens, and so is a new token whose value row
+// is not finite; weights of hidden tokens are zero and so are the value rows they meet.
+// ---------------------------------------------------------------------------
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ v4f mma(v8h a, v8h b, v4f c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+// Eight codes (two words) as fp16.
+__device__ __forceinline__ v8h codes_f16(uint32_t w0, uint32_t w1) {
+  const v2h off = {(_Float16)1152.0f, (_Float16)1152.0f};
+  uint32_t x[4] = {__builtin_amdgcn_perm(0x64646464u, w0, 0x04010400u),
+                   __builtin_amdgcn_perm(0x64646464u, w0, 0x04030402u),
+                   __builtin_amdgcn_perm(0x64646464u, w1, 0x04010400u),
+                   __builtin_amdgcn_perm(0x64646464u, w1, 0x04030402u)};
+  v8h r;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const v2h h = __builtin_bit_cast(v2h, x[j]) - off;
+    r[2 * j] = h[0];
+    r[2 * j + 1] = h[1];
+  }
+  return r;
+}
+
+// v in NS parts of fp16.
+template <int NS>
+__device__ __forceinline__ void split_f16(const float (&v)[8], v8h (&out)[NS]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    out[0][j] = (_Float16)v[j];
+    if constexpr (NS == 2) out[1][j] = (_Float16)(v[j] - (float)out[0][j]);
+  }
+}
+
+// Exponent e with |m| < 2^e (m finite and positive, else 0), within what ldexp keeps normal.
+__device__ __forceinline__ int exponent_of(float m) {
+  const int e = (int)(__float_as_uint(m) >> 23 & 255) - 126;
+  return m > 0.0f ? (e < -100 ? -100 : e) : 0;
+}
+__device__ __forceinline__ float finite_abs(float x) {
+  const float a = fabsf(x);
+  return a < INFINITY ? a : 0.0f;
+}
+
+__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
+  const float4 a = ((const float4*)p)[0], b = ((const float4*)p)[1];
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ void load8(const uint16_t* p, float (&v)[8]) {
+  const uint4 r = *(const uint4*)p;
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    v[2 * j] = __uint_as_float(w[j] << 16);
+    v[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ void load4(const float* p, float* v) {
+  const float4 a = *(const float4*)p;
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+}
+__device__ __forceinline__ void load4(const uint16_t* p, float* v) {
+  const uint2 r = *(const uint2*)p;
+  v[0] = __uint_as_float(r.x << 16);
+  v[1] = __uint_as_float(r.x & 0xFFFF0000u);
+  v[2] = __uint_as_float(r.y << 16);
+  v[3] = __uint_as_float(r.y & 0xFFFF0000u);
+}
+__device__ __forceinline__ void store4(float* p, v4f v) {
+  *(float4*)p = make_float4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ void store4(uint16_t* p, v4f v) {
+  uint2 r;
+  r.x = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[0]) |
+        ((uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[1]) << 16);
+  r.y = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2]) |
+        ((uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[3]) << 16);
+  *(uint2*)p = r;
+}
+
+// Largest and sum over the four lanes of a column.
+__device__ __forceinline__ float col_max(float v) {
+  v = fmaxf(v, __shfl_xor(v, 16, 64));
+  return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+__device__ __forceinline__ float col_sum(float v) {
+  v += __shfl_xor(v, 16, 64);
+  return v + __shfl_xor(v, 32, 64);
+}
+
+// One column's query as operands (dims 32 k + 8 (lane / 16) .. + 7 of part s in f[k][s]): rotated in
+// fp32, scaled; the return value turns a product with codes of step 1 into a score times log2(e).
+template <typename T, int HD, int NS>
+__device__ __forceinline__ float query_operand(const T* q, const float2* rope, float scale,
+                                               v8h (&f)[HD / 32][NS]) {
+  const int lane = threadIdx.x & 63;
+  float x[HD / 32][8];
+  float m = 0.0f;
+#pragma unroll
+  for (int k = 0; k < HD / 32; ++k) {
+    const int d = k * 32 + (lane >> 4) * 8;
+    const bool low = d < HD / 2;
+    if (q) {
+      load8(q + d, x[k]);
+      if (rope) {
+        float o[8], r[16];
+        load8(q + (low ? d + HD / 2 : d - HD / 2), o);
+        const float* rp = (const float*)(rope + (low ? d : d - HD / 2));
+        load4(rp, r); load4(rp + 4, r + 4); load4(rp + 8, r + 8); load4(rp + 12, r + 12);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float a = x[k][j] * r[2 * j], b = o[j] * r[2 * j + 1];
+          x[k][j] = low ? a - b : a + b;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[k][j] = 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = fmaxf(m, finite_abs(x[k][j]));
+  }
+  const int e = exponent_of(col_max(m)) - 10;
+#pragma unroll
+  for (int k = 0; k < HD / 32; ++k) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[k][j] = ldexpf(x[k][j], -e);
+    split_f16<NS>(x[k], f[k]);
+  }
+  return ldexpf(scale * kLog2e, e);
+}
+
+// Running softmax of a wave over its blocks: NT tiles of 16 columns.
+template <int HD, int NT>
+struct Running {
+  float m[NT], l[NT];                 // l: this lane's tokens only
+  v4f o[NT][HD / 16];
+  float unit;                         // of o: the largest step of the values so far (0: none)
+};
+
+// Takes a block in: s[j][t] the products of column tile j with tokens 16 t + 4 (lane / 16) + r,
+// step its steps, qf the columns' factors, last[j] the last token of the block that the column sees
+// (63 and more: all), values(dt, h, part) the operand of dims 16 dt.. and tokens 32 h...
+// NV: parts of the values, NS: parts of the probabilities.
+template <int HD, int NT, int NS, int NV, typename Values>
+__device__ __forceinline__ void take_block(Running<HD, NT>& run, v4f (&s)[NT][4], float2 step,
+                                           const float (&qf)[NT], const int (&last)[NT], bool hidden,
+                                           uint32_t bad, Values values) {
+  const int tok = (threadIdx.x & 63) >> 4 << 2;
+  const bool nan = !(step.x < INFINITY) || !(step.y < INFINITY);
+  const float vstep = nan ? 0.0f : step.y;
+  const float unit = fmaxf(run.unit, vstep);
+  const float ratio = vstep > 0.0f ? vstep / unit : 0.0f;
+  const float shrink = run.unit > 0.0f ? run.unit / unit : 0.0f;
+  run.unit = unit;
+  v8h p[NT][2][NS];
+  float al[NT];
+  bool same = shrink == 1.0f;
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const float f = qf[j] * (nan ? __builtin_nanf("") : step.x);
+    float bm = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float x = s[j][t][r] * f;
+        if (bad >> (t * 4 + r) & 1) x = __builtin_nanf("");
+        if (hidden && t * 16 + tok + r > last[j]) x = -INFINITY;
+        s[j][t][r] = x;
+        bm = fmaxf(bm, x);
+      }
+    const float m = fmaxf(run.m[j], col_max(bm));
+    const float ref = m == -INFINITY ? 0.0f : m;
+    al[j] = exp2f(run.m[j] - ref);
+    run.m[j] = m;
+    same = same && al[j] == 1.0f;
+    float sum = 0.0f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float w[8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        const float e = __builtin_amdgcn_exp2f(s[j][2 * h + r / 4][r % 4] - ref + 15.0f);
+        sum += e;
+        w[r] = e * ratio;
+      }
+      split_f16<NS>(w, p[j][h]);
+    }
+    run.l[j] = run.l[j] * al[j] + sum;
+    al[j] *= shrink;
+  }
+  if (!__all(same)) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int d = 0; d < HD / 16; ++d) run.o[j][d] *= al[j];
+  }
+#pragma unroll
+  for (int d = 0; d < HD / 16; ++d)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int a = 0; a < NV; ++a) {
+        const v8h v = values(d, h, a);
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int b = 0; b < NS; ++b)
+            if (a + b < 2) run.o[j][d] = mma(v, p[j][h][b], run.o[j][d]);
+      }
+}
+
+// The split of a row's blocks (its last, incomplete one among them) over work groups: how many are
+// used and how many blocks each takes.  Attention and the joining of its parts share it.
+__device__ __forceinline__ int blocks_per_split(int items, int splits) {
+  return (items + splits - 1) / splits;
+}
+
+// grid: splits, key/value heads, rows.  A wave takes every fourth block of its work group's share.
+template <typename T, int HD, int NT>
+__global__ void __launch_bounds__(256) k_attend_rows(CacheView c, int layer, const T* q, T* out, int n,
+                                                     const int32_t* counts, int heads, float scale,
+                                                     float* part) {
+  constexpr int NS = sizeof(T) == 2 ? 1 : 2, NC = 16 * NT;
+  __shared__ float lo[2][NC][HD + 4];
+  __shared__ float lm[2][NC], ll[2][NC];
+  const int head = blockIdx.y, row = blockIdx.z, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = row / c.width;
+  const int cnt = query_count(c, g, n, counts);
+  if (cnt == 0) return;
+  const int64_t slot = (int64_t)g * c.beams + row % c.width;
+  const int len = c.len[g], total = len + cnt;
+  const int G = heads / c.heads_kv, cols = cnt * G;
+  const int full = total / kBlock, items = (total + kBlock - 1) / kBlock;
+  const int per = blocks_per_split(items, gridDim.x);
+  const int i0 = blockIdx.x * per, i1 = i0 + per < items ? i0 + per : items;
+  if (i0 >= i1) return;
+  // queries: column -> (query, head of the group)
+  v8h qf[NT][HD / 32][NS];
+  float qs[NT];
+  int pos[NT];                                           // the column's position
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const int col = j * 16 + (lane & 15);
+    const int i = col < cols ? col / G : cnt - 1, hq = col % G;
+    pos[j] = len + i;
+    const T* qp = col < cols ? q + (((int64_t)row * n + i) * heads + head * G + hq) * HD : nullptr;
+    qs[j] = query_operand<T, HD, NS>(qp, c.rope ? c.rope + (int64_t)pos[j] * (HD / 2) : nullptr, scale, qf[j]);
+  }
+  Running<HD, NT> run;
+  run.unit = 0.0f;
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    run.m[j] = -INFINITY;
+    run.l[j] = 0.0f;
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d) run.o[j][d] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  for (int it = i0 + wave; it < i1; it += 4) {
+    int last[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) last[j] = pos[j] - it * kBlock;
+    const bool hidden = it * kBlock + kBlock > len + 1;  // some column may not see all of it
+    v4f s[NT][4];
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) s[j][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    if (it < full) {
+      const int64_t ph = c.page_head(layer, c.page_of(slot, it, len), head);
+      const uint4* kp = (const uint4*)(c.kpage + ph * (kBlock * HD)) + lane;
+      const uint4* vp = (const uint4*)(c.vpage + ph * (kBlock * HD)) + lane;
+      uint4 kr[2][HD / 32], vr[HD / 16];
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int k = 0; k < HD / 32; ++k) kr[p][k] = kp[(p * (HD / 32) + k) * 64];
+#pragma unroll
+      for (int d = 0; d < HD / 16; ++d) vr[d] = vp[d * 64];
+      const float2 step = c.step[ph];
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int k = 0; k < HD / 32; ++k) {
+          const v8h a = codes_f16(kr[p][k].x, kr[p][k].y), b = codes_f16(kr[p][k].z, kr[p][k].w);
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int x = 0; x < NS; ++x) {
+              s[j][2 * p] = mma(a, qf[j][k][x], s[j][2 * p]);
+              s[j][2 * p + 1] = mma(b, qf[j][k][x], s[j][2 * p + 1]);
+            }
+        }
+      take_block<HD, NT, NS, 1>(run, s, step, qs, last, hidden, 0u, [&](int d, int h, int) {
+        return h == 0 ? codes_f16(vr[d].x, vr[d].y) : codes_f16(vr[d].z, vr[d].w);
+      });
+    } else {
+      const int64_t th = c.tail_head(layer, c.sel[g] ^ (it != len / kBlock), c.tail_of[slot], head) * (kBlock * HD);
+      const T* kt = (const T*)c.ktail + th;
+      const T* vt = (const T*)c.vtail + th;
+      const int have = total - it * kBlock;              // tokens of the block
+      float2 step;
+      {
+        // keys, a 16-token tile at a time: first their largest magnitude
+        float m = 0.0f;
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int k = 0; k < HD / 32; ++k) {
+            const int tk = t * 16 + (lane & 15);
+            float x[8];
+            if (tk < have) {
+              load8(kt + tk * HD + k * 32 + (lane >> 4) * 8, x);
+#pragma unroll
+              for (int j = 0; j < 8; ++j) m = fmaxf(m, finite_abs(x[j]));
+            }
+          }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+        const int e = exponent_of(m) - 7;
+        step.x = ldexpf(1.0f, e);
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int k = 0; k < HD / 32; ++k) {
+            const int tk = t * 16 + (lane & 15);
+            float x[8] = {};
+            if (tk < have) load8(kt + tk * HD + k * 32 + (lane >> 4) * 8, x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              x[j] = fabsf(x[j]) < INFINITY ? ldexpf(x[j], -e) : __builtin_nanf("");
+            v8h a[NS];
+            split_f16<NS>(x, a);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+              s[j][t] = mma(a[0], qf[j][k][0], s[j][t]);
+              if constexpr (NS == 2) {
+                s[j][t] = mma(a[0], qf[j][k][1], s[j][t]);
+                s[j][t] = mma(a[1], qf[j][k][0], s[j][t]);
+              }
+            }
+          }
+      }
+      // values: their largest magnitude, and which tokens have one that is not finite
+      auto value_rows = [&](int d, int h, float (&x)[8]) __attribute__((always_inline)) {
+        const T* p = vt + (d * 16 + (lane & 15)) * kBlock + h * 32 + (lane >> 4) * 4;
+        const int t0 = h * 32 + (lane >> 4) * 4;
+        load4(p, x);
+        load4(p + 16, x + 4);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (t0 + (j / 4) * 16 + j % 4 >= have) x[j] = 0.0f;
+      };
+      float m = 0.0f;
+      uint32_t bad = 0;
+#pragma unroll 1
+      for (int d = 0; d < HD / 16; ++d)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float x[8];
+          value_rows(d, h, x);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            m = fmaxf(m, finite_abs(x[j]));
+            if (!(fabsf(x[j]) < INFINITY)) bad |= 1u << (h * 8 + j);
+          }
+        }
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) bad |= __shfl_xor(bad, o, 64);
+      const int e = exponent_of(m) - 7;
+      step.y = ldexpf(1.0f, e);
+      v8h a[NS];
+      take_block<HD, NT, NS, NS>(run, s, step, qs, last, true, bad, [&](int d, int h, int b) {
+        if (b == 0) {
+          float x[8];
+          value_rows(d, h, x);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) x[j] = bad >> (h * 8 + j) & 1 ? 0.0f : ldexpf(x[j], -e);
+          split_f16<NS>(x, a);
+        }
+        return a[b];
+      });
+    }
+  }
+  // the wave's result: outputs as such, with maximum and sum; joined in two rounds
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const float l = run.l[j] = col_sum(run.l[j]);
+    const float f = l == 0.0f ? 0.0f : run.unit / l;
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d) run.o[j][d] *= f;
+  }
+#pragma unroll
+  for (int half = 2; half > 0; half >>= 1) {
+    if (wave >= half && wave < 2 * half) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const int col = j * 16 + (lane & 15);
+        if (lane < 16) {
+          lm[wave - half][col] = run.m[j];
+          ll[wave - half][col] = run.l[j];
+        }
+#pragma unroll
+        for (int d = 0; d < HD / 16; ++d)
+          *(v4f*)&lo[wave - half][col][d * 16 + (lane >> 4) * 4] = run.o[j][d];
+      }
+    }
+    __syncthreads();
+    if (wave < half) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const int col = j * 16 + (lane & 15);
+        const float m2 = lm[wave][col], l2 = ll[wave][col];
+        const float m = fmaxf(run.m[j], m2), ref = m == -INFINITY ? 0.0f : m;
+        const float a = run.l[j] * exp2f(run.m[j] - ref), b = l2 * exp2f(m2 - ref);
+        const float l = a + b, fa = l == 0.0f ? 0.0f : a / l, fb = l == 0.0f ? 0.0f : b / l;
+#pragma unroll
+        for (int d = 0; d < HD / 16; ++d)
+          run.o[j][d] = run.o[j][d] * fa + *(v4f*)&lo[wave][col][d * 16 + (lane >> 4) * 4] * fb;
+        run.m[j] = m;
+        run.l[j] = l;
+      }
+    }
+    __syncthreads();
+  }
+  if (wave != 0) return;
+  if (items <= per) {                                    // the only part
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const int col = j * 16 + (lane & 15);
+      if (col < cols) {
+        T* op = out + (((int64_t)row * n + col / G) * heads + head * G + col % G) * HD + (lane >> 4) * 4;
+#pragma unroll
+        for (int d = 0; d < HD / 16; ++d) store4(op + d * 16, run.o[j][d]);
+      }
+    }
+    return;
+  }
+  float* pp = part + (((int64_t)row * c.heads_kv + head) * gridDim.x + blockIdx.x) * NC * (HD + 2);
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const int col = j * 16 + (lane & 15);
+    if (col < cols) {
+#pragma unroll
+      for (int d = 0; d < HD / 16; ++d) store4(pp + col * HD + d * 16 + (lane >> 4) * 4, run.o[j][d]);
+      if (lane < 16) {
+        pp[NC * HD + col] = run.m[j];
+        pp[NC * HD + NC + col] = run.l[j];
+      }
+    }
+  }
+}
+
+// Joins the parts of a row's columns: a wave per column, a lane per split for the weights, then per
+// dim for the sum.
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) k_attend_join(CacheView c, const float* part, T* out, int n,
+                                                     const int32_t* counts, int heads, int splits,
+                                                     int nc) {
+  const int lane = threadIdx.x & 63, head = blockIdx.y, row = blockIdx.z;
+  const int g = row / c.width;
+  const int cnt = query_count(c, g, n, counts);
+  const int G = heads / c.heads_kv, cols = cnt * G;
+  const int col = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (col >= cols) return;                               // whole wave
+  const int items = (c.len[g] + cnt + kBlock - 1) / kBlock, per = blocks_per_split(items, splits);
+  if (items <= per) return;                              // written already
+  const int used = (items + per - 1) / per;
+  const float* pp = part + ((int64_t)row * c.heads_kv + head) * splits * nc * (HD + 2);
+  const int64_t stride = (int64_t)nc * (HD + 2);
+  float m = -INFINITY;
+  for (int s = lane; s < used; s += 64) m = fmaxf(m, pp[s * stride + nc * HD + col]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  const float ref = m == -INFINITY ? 0.0f : m;
+  float l = 0.0f, acc[2] = {0.0f, 0.0f};
+  for (int s0 = 0; s0 < used; s0 += 64) {
+    float w = 0.0f;
+    if (s0 + lane < used) {
+      const float* q = pp + (s0 + lane) * stride + nc * HD + col;
+      w = q[nc] * exp2f(q[0] - ref);
+    }
+    float ws = w;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) ws += __shfl_xor(ws, o, 64);
+    l += ws;
+    const int k = used - s0 < 64 ? used - s0 : 64;
+    for (int s = 0; s < k; ++s) {
+      const float f = __shfl(w, s, 64);
+      const float* o = pp + (s0 + s) * stride + col * HD;
+      acc[0] = fmaf(f, o[lane], acc[0]);
+      if (lane + 64 < HD) acc[1] = fmaf(f, o[lane + 64], acc[1]);
+    }
+  }
+  T* op = out + (((int64_t)row * n + col / G) * heads + head * G + col % G) * HD;
+  st_val(op + lane, acc[0] / l);
+  if (lane + 64 < HD) st_val(op + lane + 64, acc[1] / l);
+}
+
+// ---------------------------------------------------------------------------
 // Launches
 // ---------------------------------------------------------------------------
 namespace {
@@ -460,6 +986,15 @@ CacheView view_of(const termezo_kvcache* c) {
     else { CALL(float, 128); }                                     \
   }
 
+// Work groups over a row's tokens for `units` rows x heads and nt column tiles: as many as fill the
+// device a few times (kSplitGroups), but at least a block for each of a work group's four waves
+// at max_len.  The kernels divide the tokens that there are, so no length is known here.
+constexpr int64_t kSplitGroups = 1024;
+int row_splits(const termezo_kvcache* c, int64_t units, int nt) {
+  const int64_t most = (c->max_blocks + 3) / 4;
+  return (int)std::max<int64_t>(1, std::min(most, kSplitGroups / units));
+}
+
 int64_t rows_of(const termezo_kvcache* c) { return (int64_t)c->cfg.groups * c->width; }
 
 }  // namespace
@@ -487,8 +1022,28 @@ hipError_t cache_attention_on(termezo_kvcache* c, int layer, const void* q, cons
     counts = nullptr;                                  // attention takes the pending counts
   }
   const CacheView w = view_of(c);
-  const int H = c->cfg.n_heads;
+  const int H = c->cfg.n_heads, Hkv = c->cfg.n_kv_heads;
   const float scale = (float)(1.0 / std::sqrt((double)c->cfg.head_dim));
+  const int64_t cols = n * (H / Hkv), rows = rows_of(c);
+  if (cols <= 32) {
+    const int nt = cols <= 16 ? 1 : 2;
+    const int splits = row_splits(c, rows * Hkv, nt);
+    const dim3 grid((unsigned)splits, (unsigned)Hkv, (unsigned)rows);
+    const dim3 jgrid((unsigned)((cols + 3) / 4), (unsigned)Hkv, (unsigned)rows);
+#define TMZ_CALL(T, HD)                                                                         \
+  if (nt == 1)                                                                                  \
+    hipLaunchKernelGGL((k_attend_rows<T, HD, 1>), grid, dim3(256), 0, s, w, layer, (const T*)q,  \
+                       (T*)out, (int)n, counts, H, scale, c->part);                             \
+  else                                                                                          \
+    hipLaunchKernelGGL((k_attend_rows<T, HD, 2>), grid, dim3(256), 0, s, w, layer, (const T*)q,  \
+                       (T*)out, (int)n, counts, H, scale, c->part);                             \
+  if (splits > 1)                                                                               \
+    hipLaunchKernelGGL((k_attend_join<T, HD>), jgrid, dim3(256), 0, s, w, c->part, (T*)out,      \
+                       (int)n, counts, H, splits, 16 * nt)
+    TMZ_CACHE_TYPES(c, TMZ_CALL)
+#undef TMZ_CALL
+    return hipGetLastError();
+  }
   const dim3 grid((unsigned)((n * H + 3) / 4), (unsigned)rows_of(c));
 #define TMZ_CALL(T, HD)                                                                       \
   hipLaunchKernelGGL((k_attend_plain<T, HD>), grid, dim3(256), 0, s, w, layer, (const T*)q,    \
@@ -620,6 +1175,8 @@ termezo_status termezo_kvcache_create(termezo_ctx* ctx, const termezo_kvcache_co
     A((void**)&c->tail_of, slots * 4);
     A((void**)&c->table, slots * nblk * 4);
     if (f.rope_base > 0.0f) A((void**)&c->rope, f.max_len * (hd / 2) * 8);
+    // parts of at most kSplitGroups work groups of 32 columns (fewer units never need more)
+    A((void**)&c->part, kSplitGroups * 32 * (hd + 2) * 4);
   }
   termezo_status st = hip_status(c, e, "kvcache_create");
   if (st == TERMEZO_OK) {
