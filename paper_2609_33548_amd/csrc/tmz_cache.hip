@@ -334,92 +334,6 @@ __global__ void __launch_bounds__(256) k_cache_read(CacheView c, int layer, int6
 }
 
 // ---------------------------------------------------------------------------
-// Attention, one wave per query and head: a lane scores one token of a block, then owns dims.
-// ---------------------------------------------------------------------------
-template <typename T, int HD>
-__global__ void __launch_bounds__(256) k_attend_plain(CacheView c, int layer, const T* q, T* out,
-                                                      int n, const int32_t* counts, int heads,
-                                                      float scale) {
-  __shared__ float qs[4][HD];
-  __shared__ float ps[4][kBlock];
-  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, row = blockIdx.y;
-  const int g = row / c.width;
-  const int cnt = query_count(c, g, n, counts);
-  const int64_t at = (int64_t)blockIdx.x * 4 + w;
-  const int i = (int)(at / heads), h = (int)(at % heads);
-  if (i >= cnt) return;                                  // whole wave
-  const int64_t slot = (int64_t)g * c.beams + row % c.width;
-  const int len = c.len[g], total = len + cnt, seen = len + i + 1;
-  const int head = h / (heads / c.heads_kv);
-  const T* qp = q + (((int64_t)row * n + i) * heads + h) * HD;
-  for (int d = lane; d < HD / 2; d += 64) {
-    float a = ld_val(qp + d), b = ld_val(qp + d + HD / 2);
-    if (c.rope) {
-      const float2 r = c.rope[(int64_t)(seen - 1) * (HD / 2) + d];
-      const float a2 = a * r.x - b * r.y, b2 = b * r.x + a * r.y;
-      a = a2;
-      b = b2;
-    }
-    qs[w][d] = a * scale;
-    qs[w][d + HD / 2] = b * scale;
-  }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  float m = -INFINITY, l = 0.0f, o[2] = {0.0f, 0.0f};
-  for (int t0 = 0; t0 < seen; t0 += kBlock) {
-    const int64_t blk = t0 / kBlock;
-    const bool coded = t0 + kBlock <= total;
-    const int64_t ph = c.page_head(layer, coded ? c.page_of(slot, blk, len) : 0, head);
-    const float2 d = coded ? c.step[ph] : make_float2(1.0f, 1.0f);
-    const int64_t th = c.tail_head(layer, c.sel[g] ^ (blk != len / kBlock), c.tail_of[slot], head) * (kBlock * HD);
-    const bool ok = t0 + lane < seen;
-    float s = -INFINITY;
-    if (ok) {
-      float acc = 0.0f;
-      for (int e = 0; e < HD; ++e) {
-        const float kx = coded ? (float)((int)c.kpage[ph * (kBlock * HD) + key_at<HD>(lane, e)] - 128)
-                               : ld_val((const T*)c.ktail + th + lane * HD + e);
-        acc = fmaf(qs[w][e], kx, acc);
-      }
-      s = acc * d.x;
-    }
-    float bm = s;
-#pragma unroll
-    for (int x = 32; x > 0; x >>= 1) bm = fmaxf(bm, __shfl_xor(bm, x, 64));
-    const float nm = fmaxf(m, bm);
-    const float p = ok ? expf(s - nm) : 0.0f;
-    float ls = p;
-#pragma unroll
-    for (int x = 32; x > 0; x >>= 1) ls += __shfl_xor(ls, x, 64);
-    const float al = m == -INFINITY ? 0.0f : expf(m - nm);
-    l = l * al + ls;
-    m = nm;
-    __builtin_amdgcn_wave_barrier();
-    ps[w][lane] = p;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    const int tn = seen - t0 < kBlock ? seen - t0 : kBlock;
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int e = lane + 64 * x;
-      if (e >= HD) break;
-      float acc = 0.0f;
-      for (int t = 0; t < tn; ++t) {
-        const float vx = coded ? (float)((int)c.vpage[ph * (kBlock * HD) + value_at(t, e)] - 128)
-                               : ld_val((const T*)c.vtail + th + e * kBlock + t);
-        acc = fmaf(ps[w][t], vx, acc);
-      }
-      o[x] = o[x] * al + acc * d.y;
-    }
-    __builtin_amdgcn_wave_barrier();
-  }
-  T* op = out + (((int64_t)row * n + i) * heads + h) * HD;
-#pragma unroll
-  for (int x = 0; x < 2; ++x)
-    if (lane + 64 * x < HD) st_val(op + lane + 64 * x, o[x] / l);
-}
-
-// ---------------------------------------------------------------------------
 // Attention of a few queries (up to 32 (query, head) columns of a key/value head) over a long cache.
 //
 // Scores are formed as S^T = K Q^T and the output as O^T += V^T P^T with 16x16x32 fp16 matrix
@@ -656,10 +570,182 @@ __device__ __forceinline__ void take_block(Running<HD, NT>& run, v4f (&s)[NT][4]
       }
 }
 
+// Takes the tokens behind the last complete block in: scaled, in NS parts.
+template <typename T, int HD, int NT, int NS>
+__device__ __forceinline__ void take_tail(const CacheView& c, int layer, int head, int g, int64_t slot,
+                                          int len, int total, const v8h (&qf)[NT][HD / 32][NS],
+                                          const float (&qs)[NT], const int (&last)[NT],
+                                          Running<HD, NT>& run) {
+  const int lane = threadIdx.x & 63, it = total / kBlock;
+  v4f s[NT][4];
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int t = 0; t < 4; ++t) s[j][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  const int64_t th = c.tail_head(layer, c.sel[g] ^ (it != len / kBlock), c.tail_of[slot], head) * (kBlock * HD);
+  const T* kt = (const T*)c.ktail + th;
+  const T* vt = (const T*)c.vtail + th;
+  const int have = total - it * kBlock;              // tokens of the block
+  float2 step;
+  {
+    // keys, a 16-token tile at a time: first their largest magnitude
+    float m = 0.0f;
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int k = 0; k < HD / 32; ++k) {
+        const int tk = t * 16 + (lane & 15);
+        float x[8];
+        if (tk < have) {
+          load8(kt + tk * HD + k * 32 + (lane >> 4) * 8, x);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) m = fmaxf(m, finite_abs(x[j]));
+        }
+      }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    const int e = exponent_of(m) - 7;
+    step.x = ldexpf(1.0f, e);
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int k = 0; k < HD / 32; ++k) {
+        const int tk = t * 16 + (lane & 15);
+        float x[8] = {};
+        if (tk < have) load8(kt + tk * HD + k * 32 + (lane >> 4) * 8, x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          x[j] = fabsf(x[j]) < INFINITY ? ldexpf(x[j], -e) : __builtin_nanf("");
+        v8h a[NS];
+        split_f16<NS>(x, a);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          s[j][t] = mma(a[0], qf[j][k][0], s[j][t]);
+          if constexpr (NS == 2) {
+            s[j][t] = mma(a[0], qf[j][k][1], s[j][t]);
+            s[j][t] = mma(a[1], qf[j][k][0], s[j][t]);
+          }
+        }
+      }
+  }
+  // values: their largest magnitude, and which tokens have one that is not finite
+  auto value_rows = [&](int d, int h, float (&x)[8]) __attribute__((always_inline)) {
+    const T* p = vt + (d * 16 + (lane & 15)) * kBlock + h * 32 + (lane >> 4) * 4;
+    const int t0 = h * 32 + (lane >> 4) * 4;
+    load4(p, x);
+    load4(p + 16, x + 4);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (t0 + (j / 4) * 16 + j % 4 >= have) x[j] = 0.0f;
+  };
+  float m = 0.0f;
+  uint32_t bad = 0;
+#pragma unroll 1
+  for (int d = 0; d < HD / 16; ++d)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float x[8];
+      value_rows(d, h, x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        m = fmaxf(m, finite_abs(x[j]));
+        if (!(fabsf(x[j]) < INFINITY)) bad |= 1u << (h * 8 + j);
+      }
+    }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) bad |= __shfl_xor(bad, o, 64);
+  const int e = exponent_of(m) - 7;
+  step.y = ldexpf(1.0f, e);
+  v8h a[NS];
+  take_block<HD, NT, NS, NS>(run, s, step, qs, last, true, bad, [&](int d, int h, int b) {
+    if (b == 0) {
+      float x[8];
+      value_rows(d, h, x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = bad >> (h * 8 + j) & 1 ? 0.0f : ldexpf(x[j], -e);
+      split_f16<NS>(x, a);
+    }
+    return a[b];
+  });
+}
+
+// Blocks that columns below c1 of a row see, its incomplete one among them.
+__device__ __forceinline__ int items_of(int len, int cnt, int cols, int c1, int G) {
+  const int last = c1 < cols ? (c1 - 1) / G : cnt - 1;   // the last query among them
+  return (len + last) / kBlock + 1;
+}
+
 // The split of a row's blocks (its last, incomplete one among them) over work groups: how many are
 // used and how many blocks each takes.  Attention and the joining of its parts share it.
 __device__ __forceinline__ int blocks_per_split(int items, int splits) {
   return (items + splits - 1) / splits;
+}
+
+// A wave's NT column tiles from column c0 on: operands, factors and positions.
+template <typename T, int HD, int NT, int NS>
+__device__ __forceinline__ void load_columns(const CacheView& c, const T* q, int row, int n, int heads,
+                                             int head, int len, int cnt, int c0, float scale,
+                                             v8h (&qf)[NT][HD / 32][NS], float (&qs)[NT],
+                                             int (&pos)[NT]) {
+  const int lane = threadIdx.x & 63, G = heads / c.heads_kv, cols = cnt * G;
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const int col = c0 + j * 16 + (lane & 15);
+    const int i = col < cols ? col / G : cnt - 1, hq = col % G;
+    pos[j] = len + i;
+    const T* qp = col < cols ? q + (((int64_t)row * n + i) * heads + head * G + hq) * HD : nullptr;
+    qs[j] = query_operand<T, HD, NS>(qp, c.rope ? c.rope + (int64_t)pos[j] * (HD / 2) : nullptr, scale,
+                                     qf[j]);
+  }
+}
+
+template <int HD, int NT>
+__device__ __forceinline__ void start(Running<HD, NT>& run) {
+  run.unit = 0.0f;
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    run.m[j] = -INFINITY;
+    run.l[j] = 0.0f;
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d) run.o[j][d] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+}
+
+// Outputs as such, with the sums over all tokens.
+template <int HD, int NT>
+__device__ __forceinline__ void finish(Running<HD, NT>& run) {
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const float l = run.l[j] = col_sum(run.l[j]);
+    const float f = l == 0.0f ? 0.0f : run.unit / l;
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d) run.o[j][d] *= f;
+  }
+}
+
+// A wave's columns from c0 on: to out, or as a part (nc columns) for k_attend_join.
+template <typename T, int HD, int NT>
+__device__ __forceinline__ void store_columns(const Running<HD, NT>& run, T* out, float* pp, int nc, int c0,
+                                              int p0, int row, int n, int heads, int head, int G, int cols) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const int col = c0 + j * 16 + (lane & 15), pc = p0 + j * 16 + (lane & 15), d0 = (lane >> 4) * 4;
+    if (col >= cols) continue;
+    if (pp) {
+#pragma unroll
+      for (int d = 0; d < HD / 16; ++d) store4(pp + pc * HD + d * 16 + d0, run.o[j][d]);
+      if (lane < 16) {
+        pp[nc * HD + pc] = run.m[j];
+        pp[nc * HD + nc + pc] = run.l[j];
+      }
+    } else {
+      T* op = out + (((int64_t)row * n + col / G) * heads + head * G + col % G) * HD + d0;
+#pragma unroll
+      for (int d = 0; d < HD / 16; ++d) store4(op + d * 16, run.o[j][d]);
+    }
+  }
 }
 
 // grid: splits, key/value heads, rows.  A wave takes every fourth block of its work group's share.
@@ -682,27 +768,12 @@ __global__ void __launch_bounds__(256) k_attend_rows(CacheView c, int layer, con
   const int per = blocks_per_split(items, gridDim.x);
   const int i0 = blockIdx.x * per, i1 = i0 + per < items ? i0 + per : items;
   if (i0 >= i1) return;
-  // queries: column -> (query, head of the group)
   v8h qf[NT][HD / 32][NS];
   float qs[NT];
-  int pos[NT];                                           // the column's position
-#pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    const int col = j * 16 + (lane & 15);
-    const int i = col < cols ? col / G : cnt - 1, hq = col % G;
-    pos[j] = len + i;
-    const T* qp = col < cols ? q + (((int64_t)row * n + i) * heads + head * G + hq) * HD : nullptr;
-    qs[j] = query_operand<T, HD, NS>(qp, c.rope ? c.rope + (int64_t)pos[j] * (HD / 2) : nullptr, scale, qf[j]);
-  }
+  int pos[NT];
+  load_columns<T, HD, NT, NS>(c, q, row, n, heads, head, len, cnt, 0, scale, qf, qs, pos);
   Running<HD, NT> run;
-  run.unit = 0.0f;
-#pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    run.m[j] = -INFINITY;
-    run.l[j] = 0.0f;
-#pragma unroll
-    for (int d = 0; d < HD / 16; ++d) run.o[j][d] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-  }
+  start(run);
   for (int it = i0 + wave; it < i1; it += 4) {
     int last[NT];
 #pragma unroll
@@ -742,102 +813,11 @@ __global__ void __launch_bounds__(256) k_attend_rows(CacheView c, int layer, con
         return h == 0 ? codes_f16(vr[d].x, vr[d].y) : codes_f16(vr[d].z, vr[d].w);
       });
     } else {
-      const int64_t th = c.tail_head(layer, c.sel[g] ^ (it != len / kBlock), c.tail_of[slot], head) * (kBlock * HD);
-      const T* kt = (const T*)c.ktail + th;
-      const T* vt = (const T*)c.vtail + th;
-      const int have = total - it * kBlock;              // tokens of the block
-      float2 step;
-      {
-        // keys, a 16-token tile at a time: first their largest magnitude
-        float m = 0.0f;
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int k = 0; k < HD / 32; ++k) {
-            const int tk = t * 16 + (lane & 15);
-            float x[8];
-            if (tk < have) {
-              load8(kt + tk * HD + k * 32 + (lane >> 4) * 8, x);
-#pragma unroll
-              for (int j = 0; j < 8; ++j) m = fmaxf(m, finite_abs(x[j]));
-            }
-          }
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-        const int e = exponent_of(m) - 7;
-        step.x = ldexpf(1.0f, e);
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int k = 0; k < HD / 32; ++k) {
-            const int tk = t * 16 + (lane & 15);
-            float x[8] = {};
-            if (tk < have) load8(kt + tk * HD + k * 32 + (lane >> 4) * 8, x);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              x[j] = fabsf(x[j]) < INFINITY ? ldexpf(x[j], -e) : __builtin_nanf("");
-            v8h a[NS];
-            split_f16<NS>(x, a);
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-              s[j][t] = mma(a[0], qf[j][k][0], s[j][t]);
-              if constexpr (NS == 2) {
-                s[j][t] = mma(a[0], qf[j][k][1], s[j][t]);
-                s[j][t] = mma(a[1], qf[j][k][0], s[j][t]);
-              }
-            }
-          }
-      }
-      // values: their largest magnitude, and which tokens have one that is not finite
-      auto value_rows = [&](int d, int h, float (&x)[8]) __attribute__((always_inline)) {
-        const T* p = vt + (d * 16 + (lane & 15)) * kBlock + h * 32 + (lane >> 4) * 4;
-        const int t0 = h * 32 + (lane >> 4) * 4;
-        load4(p, x);
-        load4(p + 16, x + 4);
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (t0 + (j / 4) * 16 + j % 4 >= have) x[j] = 0.0f;
-      };
-      float m = 0.0f;
-      uint32_t bad = 0;
-#pragma unroll 1
-      for (int d = 0; d < HD / 16; ++d)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float x[8];
-          value_rows(d, h, x);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            m = fmaxf(m, finite_abs(x[j]));
-            if (!(fabsf(x[j]) < INFINITY)) bad |= 1u << (h * 8 + j);
-          }
-        }
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-#pragma unroll
-      for (int o = 8; o > 0; o >>= 1) bad |= __shfl_xor(bad, o, 64);
-      const int e = exponent_of(m) - 7;
-      step.y = ldexpf(1.0f, e);
-      v8h a[NS];
-      take_block<HD, NT, NS, NS>(run, s, step, qs, last, true, bad, [&](int d, int h, int b) {
-        if (b == 0) {
-          float x[8];
-          value_rows(d, h, x);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) x[j] = bad >> (h * 8 + j) & 1 ? 0.0f : ldexpf(x[j], -e);
-          split_f16<NS>(x, a);
-        }
-        return a[b];
-      });
+      take_tail<T, HD, NT>(c, layer, head, g, slot, len, total, qf, qs, last, run);
     }
   }
-  // the wave's result: outputs as such, with maximum and sum; joined in two rounds
-#pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    const float l = run.l[j] = col_sum(run.l[j]);
-    const float f = l == 0.0f ? 0.0f : run.unit / l;
-#pragma unroll
-    for (int d = 0; d < HD / 16; ++d) run.o[j][d] *= f;
-  }
+  // joined in two rounds
+  finish(run);
 #pragma unroll
   for (int half = 2; half > 0; half >>= 1) {
     if (wave >= half && wave < 2 * half) {
@@ -872,31 +852,125 @@ __global__ void __launch_bounds__(256) k_attend_rows(CacheView c, int layer, con
     __syncthreads();
   }
   if (wave != 0) return;
-  if (items <= per) {                                    // the only part
+  float* pp = items <= per ? nullptr :
+      part + (((int64_t)row * c.heads_kv + head) * gridDim.x + blockIdx.x) * NC * (HD + 2);
+  store_columns<T, HD, NT>(run, out, pp, NC, 0, 0, row, n, heads, head, G, cols);
+}
+
+// ---------------------------------------------------------------------------
+// Attention of many queries (prompts and their pieces): a work group of eight waves takes kTileCols
+// columns of a key/value head, 32 a wave, so the blocks that it walks are converted to fp16 once, into
+// LDS, for all of them.  Two LDS buffers: while a block is used the next one's codes are on their way
+// in registers.  Every wave takes the incomplete block by itself at the end.
+// grid: splits x tiles (the longest first), key/value heads, rows.
+// ---------------------------------------------------------------------------
+constexpr int kTileCols = 256;
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(512) k_attend_tile(CacheView c, int layer, const T* q, T* out, int n,
+                                                     const int32_t* counts, int heads, float scale,
+                                                     int splits, float* part) {
+  constexpr int NS = sizeof(T) == 2 ? 1 : 2, NT = 2, KS = HD / 32;
+  constexpr int kPieces = kBlock * HD / 16;              // 16-byte pieces of a page
+  constexpr int kLoads = (2 * kPieces + 511) / 512;      // of keys and values, a thread
+  __shared__ uint4 lds[2][4 * kPieces];                  // keys [16 tokens][32 dims], values [16 dims][32 tokens]
+  const int head = blockIdx.y, row = blockIdx.z, tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tiles = gridDim.x / splits, tile = tiles - 1 - blockIdx.x / splits, split = blockIdx.x % splits;
+  const int g = row / c.width;
+  const int cnt = query_count(c, g, n, counts);
+  const int G = heads / c.heads_kv, cols = cnt * G, c0 = tile * kTileCols;
+  if (c0 >= cols) return;
+  const int64_t slot = (int64_t)g * c.beams + row % c.width;
+  const int len = c.len[g], total = len + cnt, full = total / kBlock;
+  const int items = items_of(len, cnt, cols, c0 + kTileCols, G);
+  const int per = blocks_per_split(items, splits);
+  const int i0 = split * per, i1 = i0 + per < items ? i0 + per : items;
+  if (i0 >= i1) return;
+  const int wc = c0 + wave * 32;                         // the wave's first column
+  const int mine = wc < cols ? items_of(len, cnt, cols, wc + 32, G) : 0;   // blocks it needs
+  v8h qf[NT][KS][NS];
+  float qs[NT];
+  int pos[NT];
+  load_columns<T, HD, NT, NS>(c, q, row, n, heads, head, len, cnt, wc, scale, qf, qs, pos);
+  Running<HD, NT> run;
+  start(run);
+  const int c1 = i1 < full ? i1 : full;                  // coded blocks end here
+  uint4 raw[kLoads];
+  float2 step_next = make_float2(0.0f, 0.0f);
+  auto fetch = [&](int it) __attribute__((always_inline)) {
+    const int64_t ph = c.page_head(layer, c.page_of(slot, it, len), head);
+    const uint4* kp = (const uint4*)(c.kpage + ph * (kBlock * HD));
+    const uint4* vp = (const uint4*)(c.vpage + ph * (kBlock * HD));
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      const int col = j * 16 + (lane & 15);
-      if (col < cols) {
-        T* op = out + (((int64_t)row * n + col / G) * heads + head * G + col % G) * HD + (lane >> 4) * 4;
+    for (int x = 0; x < kLoads; ++x) {
+      const int i = x * 512 + tid;
+      if (i < 2 * kPieces) raw[x] = i < kPieces ? kp[i] : vp[i - kPieces];
+    }
+    step_next = c.step[ph];
+  };
+  auto place = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
-        for (int d = 0; d < HD / 16; ++d) store4(op + d * 16, run.o[j][d]);
+    for (int x = 0; x < kLoads; ++x) {
+      const int i = x * 512 + tid;
+      if (i < 2 * kPieces) {
+        const v8h a = codes_f16(raw[x].x, raw[x].y), b = codes_f16(raw[x].z, raw[x].w);
+        // keys: piece (pair p, dims k) holds 16 tokens 2 p and 2 p + 1; values: (dims d) both halves
+        const bool key = i < kPieces;
+        const int f = (key ? i : i - kPieces) >> 6;
+        const int fa = key ? (f / KS * 2) * KS + f % KS : 4 * KS + 2 * f, fb = key ? fa + KS : fa + 1;
+        lds[buf][fa * 64 + lane] = __builtin_bit_cast(uint4, a);
+        lds[buf][fb * 64 + lane] = __builtin_bit_cast(uint4, b);
       }
     }
-    return;
+  };
+  if (i0 < c1) {
+    fetch(i0);
+    place(0);
   }
-  float* pp = part + (((int64_t)row * c.heads_kv + head) * gridDim.x + blockIdx.x) * NC * (HD + 2);
+  __syncthreads();
+  for (int it = i0; it < c1; ++it) {
+    const int buf = (it - i0) & 1;
+    const float2 step = step_next;
+    if (it + 1 < c1) fetch(it + 1);
+    if (it < mine) {
+      int last[NT];
 #pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    const int col = j * 16 + (lane & 15);
-    if (col < cols) {
+      for (int j = 0; j < NT; ++j) last[j] = pos[j] - it * kBlock;
+      v4f s[NT][4];
 #pragma unroll
-      for (int d = 0; d < HD / 16; ++d) store4(pp + col * HD + d * 16 + (lane >> 4) * 4, run.o[j][d]);
-      if (lane < 16) {
-        pp[NC * HD + col] = run.m[j];
-        pp[NC * HD + NC + col] = run.l[j];
+      for (int t = 0; t < 4; ++t) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) s[j][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          const v8h a = __builtin_bit_cast(v8h, lds[buf][(t * KS + k) * 64 + lane]);
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int x = 0; x < NS; ++x) s[j][t] = mma(a, qf[j][k][x], s[j][t]);
+        }
       }
+      // the wave's first column sees the fewest tokens
+      const bool hidden = it * kBlock + kBlock > len + wc / G + 1;
+      take_block<HD, NT, NS, 1>(run, s, step, qs, last, hidden, 0u, [&](int d, int h, int) {
+        return __builtin_bit_cast(v8h, lds[buf][(4 * KS + 2 * d + h) * 64 + lane]);
+      });
     }
+    if (it + 1 < c1) place(buf ^ 1);
+    __syncthreads();
   }
+  if (i1 > full && full < mine) {
+    int last[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) last[j] = pos[j] - full * kBlock;
+    take_tail<T, HD, NT>(c, layer, head, g, slot, len, total, qf, qs, last, run);
+  }
+  if (wc >= cols) return;
+  finish(run);
+  float* pp = items <= per ? nullptr :
+      part + ((((int64_t)row * c.heads_kv + head) * tiles + tile) * splits + split) * kTileCols * (HD + 2);
+  store_columns<T, HD, NT>(run, out, pp, kTileCols, wc, wave * 32, row, n, heads, head, G, cols);
 }
 
 // Joins the parts of a row's columns: a wave per column, a lane per split for the weights, then per
@@ -904,20 +978,21 @@ __global__ void __launch_bounds__(256) k_attend_rows(CacheView c, int layer, con
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) k_attend_join(CacheView c, const float* part, T* out, int n,
                                                      const int32_t* counts, int heads, int splits,
-                                                     int nc) {
+                                                     int nc, int tiles) {
   const int lane = threadIdx.x & 63, head = blockIdx.y, row = blockIdx.z;
   const int g = row / c.width;
   const int cnt = query_count(c, g, n, counts);
   const int G = heads / c.heads_kv, cols = cnt * G;
   const int col = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (col >= cols) return;                               // whole wave
-  const int items = (c.len[g] + cnt + kBlock - 1) / kBlock, per = blocks_per_split(items, splits);
+  const int tile = col / nc, pc = col % nc;
+  const int items = items_of(c.len[g], cnt, cols, (tile + 1) * nc, G), per = blocks_per_split(items, splits);
   if (items <= per) return;                              // written already
   const int used = (items + per - 1) / per;
-  const float* pp = part + ((int64_t)row * c.heads_kv + head) * splits * nc * (HD + 2);
+  const float* pp = part + (((int64_t)row * c.heads_kv + head) * tiles + tile) * splits * nc * (HD + 2);
   const int64_t stride = (int64_t)nc * (HD + 2);
   float m = -INFINITY;
-  for (int s = lane; s < used; s += 64) m = fmaxf(m, pp[s * stride + nc * HD + col]);
+  for (int s = lane; s < used; s += 64) m = fmaxf(m, pp[s * stride + nc * HD + pc]);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
   const float ref = m == -INFINITY ? 0.0f : m;
@@ -925,7 +1000,7 @@ __global__ void __launch_bounds__(256) k_attend_join(CacheView c, const float* p
   for (int s0 = 0; s0 < used; s0 += 64) {
     float w = 0.0f;
     if (s0 + lane < used) {
-      const float* q = pp + (s0 + lane) * stride + nc * HD + col;
+      const float* q = pp + (s0 + lane) * stride + nc * HD + pc;
       w = q[nc] * exp2f(q[0] - ref);
     }
     float ws = w;
@@ -935,7 +1010,7 @@ __global__ void __launch_bounds__(256) k_attend_join(CacheView c, const float* p
     const int k = used - s0 < 64 ? used - s0 : 64;
     for (int s = 0; s < k; ++s) {
       const float f = __shfl(w, s, 64);
-      const float* o = pp + (s0 + s) * stride + col * HD;
+      const float* o = pp + (s0 + s) * stride + pc * HD;
       acc[0] = fmaf(f, o[lane], acc[0]);
       if (lane + 64 < HD) acc[1] = fmaf(f, o[lane + 64], acc[1]);
     }
@@ -995,6 +1070,12 @@ int row_splits(const termezo_kvcache* c, int64_t units, int nt) {
   return (int)std::max<int64_t>(1, std::min(most, kSplitGroups / units));
 }
 
+// The same for tiles of many columns: at least four blocks a work group.
+constexpr int64_t kTileGroups = 512;
+int tile_splits(const termezo_kvcache* c, int64_t units) {
+  return (int)std::max<int64_t>(1, std::min(c->max_blocks / 4, kTileGroups / units));
+}
+
 int64_t rows_of(const termezo_kvcache* c) { return (int64_t)c->cfg.groups * c->width; }
 
 }  // namespace
@@ -1039,15 +1120,21 @@ hipError_t cache_attention_on(termezo_kvcache* c, int layer, const void* q, cons
                        (T*)out, (int)n, counts, H, scale, c->part);                             \
   if (splits > 1)                                                                               \
     hipLaunchKernelGGL((k_attend_join<T, HD>), jgrid, dim3(256), 0, s, w, c->part, (T*)out,      \
-                       (int)n, counts, H, splits, 16 * nt)
+                       (int)n, counts, H, splits, 16 * nt, 1)
     TMZ_CACHE_TYPES(c, TMZ_CALL)
 #undef TMZ_CALL
     return hipGetLastError();
   }
-  const dim3 grid((unsigned)((n * H + 3) / 4), (unsigned)rows_of(c));
-#define TMZ_CALL(T, HD)                                                                       \
-  hipLaunchKernelGGL((k_attend_plain<T, HD>), grid, dim3(256), 0, s, w, layer, (const T*)q,    \
-                     (T*)out, (int)n, counts, H, scale)
+  const int tiles = (int)((cols + kTileCols - 1) / kTileCols);
+  const int splits = tile_splits(c, rows * Hkv * tiles);
+  const dim3 grid((unsigned)(tiles * splits), (unsigned)Hkv, (unsigned)rows);
+  const dim3 jgrid((unsigned)((cols + 3) / 4), (unsigned)Hkv, (unsigned)rows);
+#define TMZ_CALL(T, HD)                                                                         \
+  hipLaunchKernelGGL((k_attend_tile<T, HD>), grid, dim3(512), 0, s, w, layer, (const T*)q,       \
+                     (T*)out, (int)n, counts, H, scale, splits, c->part);                       \
+  if (splits > 1)                                                                               \
+    hipLaunchKernelGGL((k_attend_join<T, HD>), jgrid, dim3(256), 0, s, w, c->part, (T*)out,      \
+                       (int)n, counts, H, splits, kTileCols, tiles)
   TMZ_CACHE_TYPES(c, TMZ_CALL)
 #undef TMZ_CALL
   return hipGetLastError();
@@ -1175,8 +1262,8 @@ termezo_status termezo_kvcache_create(termezo_ctx* ctx, const termezo_kvcache_co
     A((void**)&c->tail_of, slots * 4);
     A((void**)&c->table, slots * nblk * 4);
     if (f.rope_base > 0.0f) A((void**)&c->rope, f.max_len * (hd / 2) * 8);
-    // parts of at most kSplitGroups work groups of 32 columns (fewer units never need more)
-    A((void**)&c->part, kSplitGroups * 32 * (hd + 2) * 4);
+    // parts of at most that many work groups (where there are more units nothing is split)
+    A((void**)&c->part, std::max(kSplitGroups * 32, kTileGroups * kTileCols) * (hd + 2) * 4);
   }
   termezo_status st = hip_status(c, e, "kvcache_create");
   if (st == TERMEZO_OK) {
