@@ -9,45 +9,146 @@
 
 namespace tmz {
 
-// Logits: a wave per vocabulary row and hidden state.
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+// ---------------------------------------------------------------------------
+// Logits of few rows: out[m][t] = x[m] . E[t].  Bound by the bytes of E (2 M flops a byte of bf16), so E
+// is read once for up to 64 rows, straight into matrix operands: lane l of a wave loads 16 bytes of
+// vocabulary row l % 16 at byte 16 (l / 16) of a 64-byte step, the same piece of hidden state l % 16 is the
+// other operand (from the caches: all of x is small), and no LDS or barrier stands in the loop.  bf16: a
+// 16x16x32 instruction a step; fp32: four 16x16x4, the lane's k-th value in the k-th.  The four waves of a
+// work group share VT x 16 vocabulary rows and divide the steps, so that few rows of a small vocabulary fill the
+// device too; their sums are joined in LDS in a fixed order.
+// grid: tiles of hidden states x vocabulary tiles (the former fastest: they meet in the caches).
+// ---------------------------------------------------------------------------
 template <typename T>
-__global__ void __launch_bounds__(256) k_logits_plain(const T* x, const T* E, int64_t M, int64_t d,
-                                                      int64_t V, float* out) {
-  const int lane = threadIdx.x & 63;
-  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), m = blockIdx.y;
-  if (t >= V) return;
-  float acc = 0.0f;
-  for (int64_t i = lane; i < d; i += 64) {
-    float a, b;
-    if constexpr (sizeof(T) == 2) {
-      a = bf16_to_f32(x[m * d + i]);
-      b = bf16_to_f32(E[t * d + i]);
-    } else {
-      a = x[m * d + i];
-      b = E[t * d + i];
-    }
-    acc = fmaf(a, b, acc);
+__device__ __forceinline__ v4f logits_step(uint4 a, uint4 b, v4f c) {
+  if constexpr (sizeof(T) == 2) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b),
+                                                   c, 0, 0, 0);
+  } else {
+    const v4f x = __builtin_bit_cast(v4f, a), y = __builtin_bit_cast(v4f, b);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], c, 0, 0, 0);
+    return c;
+  }
+}
+
+template <typename T, int MT, int VT>
+__global__ void __launch_bounds__(256) k_logits(const T* __restrict__ x, const T* __restrict__ E, int64_t M,
+                                                int64_t d, int64_t V, float* __restrict__ out,
+                                                int mtiles) {
+  __shared__ v4f red[3][MT * VT][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t m0 = (int64_t)(blockIdx.x % mtiles) * 16 * MT, t0 = (int64_t)(blockIdx.x / mtiles) * 16 * VT;
+  const int64_t bytes = d * (int64_t)sizeof(T);
+  const int steps = (int)((bytes + 63) / 64), per = (steps + 3) / 4;
+  const int s0 = wave * per, s1 = s0 + per < steps ? s0 + per : steps;
+  // rows past the end are read as the last one and not stored
+  const char *xp[MT], *ep[VT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int64_t m = m0 + 16 * i + (lane & 15);
+    xp[i] = (const char*)(x + (m < M ? m : M - 1) * d) + (lane >> 4) * 16;
   }
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) acc += __shfl_xor(acc, o, 64);
-  if (lane == 0) out[m * V + t] = acc;
+  for (int i = 0; i < VT; ++i) {
+    const int64_t t = t0 + 16 * i + (lane & 15);
+    ep[i] = (const char*)(E + (t < V ? t : V - 1) * d) + (lane >> 4) * 16;
+  }
+  v4f acc[MT][VT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < VT; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  const int whole = (int)(bytes / 64) < s1 ? (int)(bytes / 64) : s1;
+  auto take = [&](int s) __attribute__((always_inline)) {
+    uint4 a[VT], b[MT];
+#pragma unroll
+    for (int j = 0; j < VT; ++j) a[j] = *(const uint4*)(ep[j] + (int64_t)s * 64);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) b[i] = *(const uint4*)(xp[i] + (int64_t)s * 64);
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < VT; ++j) acc[i][j] = logits_step<T>(a[j], b[i], acc[i][j]);
+  };
+#pragma unroll 4
+  for (int s = s0; s < whole; ++s) take(s);
+  if (s0 <= whole && whole < s1) {                       // the last step is half a one
+    const bool in = (lane >> 4) * 16 < bytes - (int64_t)whole * 64;
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+    uint4 a[VT], b[MT];
+#pragma unroll
+    for (int j = 0; j < VT; ++j) a[j] = in ? *(const uint4*)(ep[j] + (int64_t)whole * 64) : zero;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) b[i] = in ? *(const uint4*)(xp[i] + (int64_t)whole * 64) : zero;
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < VT; ++j) acc[i][j] = logits_step<T>(a[j], b[i], acc[i][j]);
+  }
+  if (wave > 0)
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < VT; ++j) red[wave - 1][i * VT + j][lane] = acc[i][j];
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < VT; ++j) {
+#pragma unroll
+      for (int w = 0; w < 3; ++w) acc[i][j] += red[w][i * VT + j][lane];
+      const int64_t m = m0 + 16 * i + (lane & 15), t = t0 + 16 * j + (lane >> 4) * 4;
+      if (m >= M) continue;
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (t + r < V) out[m * V + t + r] = acc[i][j][r];
+    }
+}
+
+template <typename T, int MT>
+static void logits_as(const T* x, const T* E, int64_t M, int64_t d, int64_t V, float* out, int n_cu,
+                      hipStream_t s) {
+  const int mt = (int)((M + 16 * MT - 1) / (16 * MT));
+  // 64 vocabulary rows a work group where that still makes two for every compute unit
+  if ((V + 63) / 64 * mt >= 2 * n_cu)
+    hipLaunchKernelGGL((k_logits<T, MT, 4>), dim3((unsigned)((V + 63) / 64 * mt)), dim3(256), 0, s, x, E, M, d,
+                       V, out, mt);
+  else
+    hipLaunchKernelGGL((k_logits<T, MT, 1>), dim3((unsigned)((V + 15) / 16 * mt)), dim3(256), 0, s, x, E, M, d,
+                       V, out, mt);
 }
 
 hipError_t launch_logits(const void* x, const void* E, termezo_dtype dt, int64_t M, int64_t d,
                          int64_t V, float* out, int n_cu, hipStream_t s) {
-  const dim3 grid((unsigned)((V + 3) / 4), (unsigned)M);
-  if (dt == TERMEZO_BF16)
-    hipLaunchKernelGGL(k_logits_plain<uint16_t>, grid, dim3(256), 0, s, (const uint16_t*)x,
-                       (const uint16_t*)E, M, d, V, out);
-  else
-    hipLaunchKernelGGL(k_logits_plain<float>, grid, dim3(256), 0, s, (const float*)x,
-                       (const float*)E, M, d, V, out);
+#define TMZ_LOGITS(T)                                                                     \
+  if (M <= 16) logits_as<T, 1>((const T*)x, (const T*)E, M, d, V, out, n_cu, s);          \
+  else if (M <= 32) logits_as<T, 2>((const T*)x, (const T*)E, M, d, V, out, n_cu, s);     \
+  else logits_as<T, 4>((const T*)x, (const T*)E, M, d, V, out, n_cu, s)
+  if (dt == TERMEZO_BF16) {
+    TMZ_LOGITS(uint16_t);
+  } else {
+    TMZ_LOGITS(float);
+  }
+#undef TMZ_LOGITS
   return hipGetLastError();
 }
 
 // ---------------------------------------------------------------------------
-// Beam selection: a work group per search.  First each beam's log-sum-exp, then n_out rounds that
-// each find the best continuation behind the one found before (score descending, then index).
+// Beam selection in two launches.
+//
+// k_beam_scan reads the logits once, a wave 4096 of them at a time in registers, and leaves per wave the
+// largest and the sum of exp(x - largest), and the largest of every segment (16 .. 4096 logits).
+// k_beam_pick, a work group per search, forms the beams' log-sum-exps (fp64) and the segments' best scores
+// score + x - lse (fp64).  A lower bound of the n_out-th best score is the n_out-th largest of the
+// maxima of 64 disjoint sets of segments: no continuation below it can be chosen, and only segments that reach
+// it are looked at again.  The few continuations found are ranked by counting; where they are many (many
+// equal logits) they are taken in rounds, best first.  Continuations of score -inf fill what
+// is left, lowest index first.  Bound by the bytes of the logits.
 // ---------------------------------------------------------------------------
 struct BeamArgs {
   const float *logits, *scores;
@@ -59,94 +160,274 @@ struct BeamArgs {
   const int32_t* history;
   int32_t* out_history;
   int64_t hist_len;
+  // scratch: [row][waves] (largest, sum), [row][segs]
+  float2* part;
+  float* seg;
+  int32_t waves, segs, seg_shift;
 };
 
+constexpr int kScan = 4096;           // logits a wave
+
+struct __attribute__((packed, aligned(4))) Float4 {
+  float v[4];
+};
+
+// NaN counts as -inf, -0 as 0.
 __device__ __forceinline__ float clean_logit(float x) { return x == x ? x + 0.0f : -INFINITY; }
 
-__global__ void __launch_bounds__(256) k_beam_plain(BeamArgs a) {
-  constexpr int kMaxBeams = 64;
-  __shared__ double lse[kMaxBeams], rv[4];
-  __shared__ int64_t ri[4];
-  const int g = blockIdx.x, tid = threadIdx.x, W = a.beams, V = a.vocab;
-  for (int b = 0; b < W; ++b) {
-    const float* x = a.logits + ((int64_t)g * W + b) * V;
-    float m = -INFINITY;
-    for (int t = tid; t < V; t += 256) m = fmaxf(m, clean_logit(x[t]));
+__global__ void __launch_bounds__(256) k_beam_scan(BeamArgs a) {
+  const int lane = threadIdx.x & 63, w = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t row = blockIdx.y;
+  if (w >= a.waves || (a.finished && a.finished[row])) return;   // whole wave
+  const float* x = a.logits + row * a.vocab;
+  const int t0 = w * kScan + lane * 4;
+  float v[16][4];
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-    if ((tid & 63) == 0) rv[tid >> 6] = m;
-    __syncthreads();
-    m = (float)fmax(fmax(rv[0], rv[1]), fmax(rv[2], rv[3]));
-    __syncthreads();
-    double s = 0.0;
-    for (int t = tid; t < V; t += 256) s += exp((double)clean_logit(x[t]) - (double)m);
+  for (int i = 0; i < 16; ++i) {
+    const int t = t0 + i * 256;
+    if (t + 3 < a.vocab) {
+      const Float4 f = *(const Float4*)(x + t);
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-    if ((tid & 63) == 0) rv[tid >> 6] = s;
-    __syncthreads();
-    if (tid == 0) {
-      const double l = (double)m + log(rv[0] + rv[1] + rv[2] + rv[3]);
-      lse[b] = l > -INFINITY && l < INFINITY ? l : INFINITY;   // no continuations
+      for (int j = 0; j < 4; ++j) v[i][j] = f.v[j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[i][j] = t + j < a.vocab ? x[t + j] : -INFINITY;
     }
-    __syncthreads();
   }
-  double pv = INFINITY;
-  int64_t pi = -1;
-  for (int r = 0; r < a.n_out; ++r) {
-    double bv = -INFINITY;
-    int64_t bi = INT64_MAX;
-    for (int b = 0; b < W; ++b) {
-      const float* x = a.logits + ((int64_t)g * W + b) * V;
-      const float sc = a.scores[(int64_t)g * W + b];
-      const bool fin = a.finished && a.finished[(int64_t)g * W + b];
-      for (int t = tid; t < V; t += 256) {
-        double v = fin ? (t == a.eos ? (double)sc : -INFINITY)
-                       : lse[b] < INFINITY ? (double)sc + (double)clean_logit(x[t]) - lse[b] : -INFINITY;
-        if (!(v == v)) v = -INFINITY;
-        const int64_t i = (int64_t)b * V + t;
-        const bool later = v < pv || (v == pv && i > pi);
-        if (later && (v > bv || (v == bv && i < bi))) {
-          bv = v;
-          bi = i;
+  float m = -INFINITY;
+  float* seg = a.seg + row * a.segs;
+  float run = -INFINITY;                                // of segments longer than 256
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[i][j] = clean_logit(v[i][j]);
+    float b = fmaxf(fmaxf(v[i][0], v[i][1]), fmaxf(v[i][2], v[i][3]));
+    m = fmaxf(m, b);
+    b = fmaxf(b, __shfl_xor(b, 1, 64));
+    b = fmaxf(b, __shfl_xor(b, 2, 64));
+    const int t = t0 + i * 256;
+    if (a.seg_shift == 4) {
+      if (lane % 4 == 0 && t < a.vocab) seg[t >> 4] = b;
+      continue;
+    }
+    b = fmaxf(b, __shfl_xor(b, 4, 64));
+    b = fmaxf(b, __shfl_xor(b, 8, 64));
+    if (a.seg_shift == 6) {
+      if (lane % 16 == 0 && t < a.vocab) seg[t >> 6] = b;
+      continue;
+    }
+    b = fmaxf(b, __shfl_xor(b, 16, 64));
+    b = fmaxf(b, __shfl_xor(b, 32, 64));
+    run = fmaxf(run, b);
+    if (((i + 1) << 8 & ((1 << a.seg_shift) - 1)) == 0) {
+      const int first = (w * kScan + i * 256) >> a.seg_shift;
+      if (lane == 0 && (int64_t)first << a.seg_shift < a.vocab) seg[first] = run;
+      run = -INFINITY;
+    }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  const float ref = m == -INFINITY ? 0.0f : m;
+  float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      s[j] += __builtin_amdgcn_exp2f((v[i][j] - ref) * 1.4426950408889634f);
+  double sum = (double)(s[0] + s[1]) + (double)(s[2] + s[3]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+  if (lane == 0) a.part[row * a.waves + w] = make_float2(m, (float)sum);
+}
+
+constexpr int kPickWaves = 8, kMaxList = 1024, kMaxCand = 512, kMaxOut = 64;
+
+__device__ __forceinline__ bool before(double v, int i, double w, int j) {
+  return v > w || (v == w && i < j);
+}
+
+__global__ void __launch_bounds__(64 * kPickWaves) k_beam_pick(BeamArgs a) {
+  __shared__ double lse[64], lmax[kPickWaves][64], cv[kMaxCand], bound, rv[kPickWaves];
+  __shared__ int list[kMaxList], ci[kMaxCand], ri[kPickWaves], n_list, n_cand, pick[kMaxOut], n_pick;
+  __shared__ float pv[kMaxOut];
+  const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int W = a.beams, V = a.vocab, S = W * a.segs;
+  const int64_t row0 = (int64_t)g * W;
+  if (tid == 0) n_list = n_cand = 0;
+  for (int b = wave; b < W; b += kPickWaves) {           // infinite: no continuations
+    double l = INFINITY;
+    if (!(a.finished && a.finished[row0 + b])) {
+      float m = -INFINITY;
+      for (int i = lane; i < a.waves; i += 64) m = fmaxf(m, a.part[(row0 + b) * a.waves + i].x);
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+      double s = 0.0;
+      for (int i = lane; i < a.waves; i += 64) {
+        const float2 p = a.part[(row0 + b) * a.waves + i];
+        if (p.x > -INFINITY) s += (double)p.y * exp((double)p.x - (double)m);
+      }
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+      l = (double)m + log(s);
+      if (!(l > -INFINITY && l < INFINITY)) l = INFINITY;
+    }
+    if (lane == 0) lse[b] = l;
+  }
+  __syncthreads();
+  // score of a logit of beam b (not finished), NaN as -inf
+  auto score_of = [&](int b, float x) __attribute__((always_inline)) {
+    if (!(lse[b] < INFINITY)) return (double)-INFINITY;
+    const double v = (double)a.scores[row0 + b] + (double)x - lse[b];
+    return v == v ? v : (double)-INFINITY;
+  };
+  auto is_done = [&](int b) __attribute__((always_inline)) { return a.finished && a.finished[row0 + b]; };
+  auto own_score = [&](int b) __attribute__((always_inline)) {
+    const float s = a.scores[row0 + b];
+    return s == s ? (double)s : (double)-INFINITY;
+  };
+  // continuation (b, t)
+  auto element = [&](int b, int t) __attribute__((always_inline)) {
+    if (is_done(b)) return t == a.eos ? own_score(b) : (double)-INFINITY;
+    return score_of(b, clean_logit(a.logits[(row0 + b) * V + t]));
+  };
+  auto segment = [&](int s) __attribute__((always_inline)) {
+    const int b = s / a.segs, j = s % a.segs;
+    if (is_done(b)) return a.eos >> a.seg_shift == j ? own_score(b) : (double)-INFINITY;
+    return score_of(b, a.seg[(row0 + b) * a.segs + j]);
+  };
+  double best = -INFINITY;
+  for (int s = tid; s < S; s += 64 * kPickWaves) best = fmax(best, segment(s));
+  lmax[wave][lane] = best;
+  __syncthreads();
+  if (wave == 0) {
+#pragma unroll
+    for (int w = 1; w < kPickWaves; ++w) best = fmax(best, lmax[w][lane]);
+    lmax[0][lane] = best;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    int rank = 0;
+    for (int i = 0; i < 64; ++i) rank += before(lmax[0][i], i, best, lane);
+    if (rank == a.n_out - 1) bound = best;
+  }
+  __syncthreads();
+  const double T = bound;
+  auto wanted = [&](double v) __attribute__((always_inline)) { return v >= T && v > -INFINITY; };
+  for (int s = tid; s < S; s += 64 * kPickWaves)
+    if (wanted(segment(s))) {
+      const int i = atomicAdd(&n_list, 1);
+      if (i < kMaxList) list[i] = s;
+    }
+  __syncthreads();
+  const int nl = n_list <= kMaxList ? n_list : S;        // too many to list: all of them
+  auto listed = [&](int i) __attribute__((always_inline)) { return n_list <= kMaxList ? list[i] : i; };
+  const int len = 1 << a.seg_shift;
+  if (n_list <= kMaxList)
+    for (int i = wave; i < nl; i += kPickWaves) {
+      const int s = list[i], b = s / a.segs, t0 = (s % a.segs) << a.seg_shift;
+      for (int t = t0 + lane; t < t0 + len && t < V; t += 64) {
+        const double v = element(b, t);
+        if (wanted(v)) {
+          const int k = atomicAdd(&n_cand, 1);
+          if (k < kMaxCand) {
+            cv[k] = v;
+            ci[k] = b * V + t;
+          }
         }
       }
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      const double v = __shfl_xor(bv, o, 64);
-      const int64_t i = __shfl_xor(bi, o, 64);
-      if (v > bv || (v == bv && i < bi)) {
-        bv = v;
-        bi = i;
+  __syncthreads();
+  if (n_list <= kMaxList && n_cand <= kMaxCand) {
+    const int nc = n_cand;
+    for (int i = tid; i < nc; i += 64 * kPickWaves) {
+      const double v = cv[i];
+      const int x = ci[i];
+      int rank = 0;
+      for (int j = 0; j < nc; ++j) rank += before(cv[j], ci[j], v, x);
+      if (rank < a.n_out) {
+        pick[rank] = x;
+        pv[rank] = (float)v;
       }
     }
-    if ((tid & 63) == 0) {
-      rv[tid >> 6] = bv;
-      ri[tid >> 6] = bi;
-    }
+    if (tid == 0) n_pick = nc < a.n_out ? nc : a.n_out;
     __syncthreads();
-    for (int w = 0; w < 4; ++w)
-      if (rv[w] > bv || (rv[w] == bv && ri[w] < bi)) {
-        bv = rv[w];
-        bi = ri[w];
+  } else {                                               // rounds: the best one behind the last
+    double lv = INFINITY;
+    int li = -1, r = 0;
+    for (; r < a.n_out; ++r) {
+      double bv = -INFINITY;
+      int bi = INT32_MAX;
+      for (int i = wave; i < nl; i += kPickWaves) {
+        const int s = listed(i), b = s / a.segs, t0 = (s % a.segs) << a.seg_shift;
+        for (int t = t0 + lane; t < t0 + len && t < V; t += 64) {
+          const double v = element(b, t);
+          const int x = b * V + t;
+          if (wanted(v) && before(lv, li, v, x) && before(v, x, bv, bi)) {
+            bv = v;
+            bi = x;
+          }
+        }
       }
-    pv = bv;
-    pi = bi;
-    const int64_t o = (int64_t)g * a.n_out + r;
-    const int b = (int)(bi / V), t = (int)(bi % V);
-    if (tid == 0) {
-      a.out_scores[o] = (float)bv;
-      a.out_tokens[o] = t;
-      a.out_parents[o] = b;
-      if (a.out_finished)
-        a.out_finished[o] = (a.finished && a.finished[(int64_t)g * W + b]) || t == a.eos;
-      if (a.out_history) a.out_history[o * (a.hist_len + 1) + a.hist_len] = t;
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) {
+        const double v = __shfl_xor(bv, o, 64);
+        const int x = __shfl_xor(bi, o, 64);
+        if (before(v, x, bv, bi)) {
+          bv = v;
+          bi = x;
+        }
+      }
+      if (lane == 0) {
+        rv[wave] = bv;
+        ri[wave] = bi;
+      }
+      __syncthreads();
+      for (int w = 0; w < kPickWaves; ++w)
+        if (before(rv[w], ri[w], bv, bi)) {
+          bv = rv[w];
+          bi = ri[w];
+        }
+      __syncthreads();
+      if (!(bv > -INFINITY)) break;                      // the same in every thread
+      lv = bv;
+      li = bi;
+      if (tid == 0) {
+        pick[r] = bi;
+        pv[r] = (float)bv;
+      }
     }
-    if (a.out_history)
-      for (int64_t i = tid; i < a.hist_len; i += 256)
-        a.out_history[o * (a.hist_len + 1) + i] = a.history[((int64_t)g * W + b) * a.hist_len + i];
+    if (tid == 0) n_pick = r;
     __syncthreads();
   }
+  if (wave == 0 && n_pick < a.n_out) {                   // all finite ones are in: the first others
+    int have = n_pick;
+    for (int64_t x0 = 0; have < a.n_out && x0 < (int64_t)W * V; x0 += 64) {
+      const int64_t x = x0 + lane;
+      const bool free = x < (int64_t)W * V && !(element((int)(x / V), (int)(x % V)) > -INFINITY);
+      const unsigned long long mask = __ballot(free);
+      const int at = have + __popcll(mask & ((1ull << lane) - 1));
+      if (free && at < a.n_out) {
+        pick[at] = (int)x;
+        pv[at] = -INFINITY;
+      }
+      have += __popcll(mask);
+    }
+  }
+  __syncthreads();
+  const int64_t o0 = (int64_t)g * a.n_out;
+  for (int r = tid; r < a.n_out; r += 64 * kPickWaves) {
+    const int b = pick[r] / V, t = pick[r] % V;
+    a.out_scores[o0 + r] = pv[r];
+    a.out_tokens[o0 + r] = t;
+    a.out_parents[o0 + r] = b;
+    if (a.out_finished) a.out_finished[o0 + r] = is_done(b) || t == a.eos;
+    if (a.out_history) a.out_history[(o0 + r) * (a.hist_len + 1) + a.hist_len] = t;
+  }
+  if (a.out_history)
+    for (int r = wave; r < a.n_out; r += kPickWaves) {
+      const int32_t* from = a.history + (row0 + pick[r] / V) * a.hist_len;
+      int32_t* to = a.out_history + (o0 + r) * (a.hist_len + 1);
+      for (int64_t i = lane; i < a.hist_len; i += 64) to[i] = from[i];
+    }
 }
 
 }  // namespace tmz
@@ -201,9 +482,34 @@ termezo_status termezo_beam_select(termezo_ctx* c, const float* logits, const fl
     return gfail(c, "beam_select: a size or eos is out of range");
   DeviceScope scope(c->device);
   if (scope.err != hipSuccess) return hip_status(c, scope.err, "beam_select");
+  // segments: as short as keeps a search at 4096 of them
+  int shift = 4;
+  while (shift < 12 && (int64_t)beams * (((int64_t)vocab + (1 << shift) - 1) >> shift) > 4096) shift += 2;
+  const int segs = (int)(((int64_t)vocab + (1 << shift) - 1) >> shift);
+  const int waves = (vocab + kScan - 1) / kScan;
+  const int64_t rows = (int64_t)groups * beams, need = rows * (waves * 8 + (int64_t)segs * 4);
+  if (need > c->beam_cap) {
+    if (c->d_beam) (void)hipFree(c->d_beam);
+    c->d_beam = nullptr;
+    c->beam_cap = 0;
+    const hipError_t e = hipMalloc(&c->d_beam, (size_t)need);
+    if (e != hipSuccess) return hip_status(c, e, "beam_select");
+    c->beam_cap = need;
+  }
   BeamArgs a{logits, scores, finished, beams, vocab, n_out, eos, out_scores, out_tokens, out_parents,
-             out_finished, history, out_history, hist_len};
-  hipLaunchKernelGGL(k_beam_plain, dim3((unsigned)groups), dim3(256), 0, c->stream, a);
+             out_finished, history, out_history, hist_len, (float2*)c->d_beam,
+             (float*)((char*)c->d_beam + rows * waves * 8), waves, segs, shift};
+  // grid.y holds 65535 rows: further ones in launches of their own
+  for (int64_t r0 = 0; r0 < rows; r0 += 65535) {
+    BeamArgs p = a;
+    p.logits += r0 * vocab;
+    if (p.finished) p.finished += r0;
+    p.part += r0 * waves;
+    p.seg += r0 * segs;
+    hipLaunchKernelGGL(k_beam_scan, dim3((unsigned)((waves + 3) / 4), (unsigned)std::min<int64_t>(65535, rows - r0)),
+                       dim3(256), 0, c->stream, p);
+  }
+  hipLaunchKernelGGL(k_beam_pick, dim3((unsigned)groups), dim3(64 * kPickWaves), 0, c->stream, a);
   return hip_status(c, hipGetLastError(), "beam_select");
 }
 
