@@ -356,6 +356,7 @@ __global__ void __launch_bounds__(256) k_cache_read(CacheView c, int layer, int6
 // ---------------------------------------------------------------------------
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+typedef float v2f __attribute__((ext_vector_type(2)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -385,9 +386,15 @@ __device__ __forceinline__ v8h codes_f16(uint32_t w0, uint32_t w1) {
 template <int NS>
 __device__ __forceinline__ void split_f16(const float (&v)[8], v8h (&out)[NS]) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    out[0][j] = (_Float16)v[j];
-    if constexpr (NS == 2) out[1][j] = (_Float16)(v[j] - (float)out[0][j]);
+  for (int j = 0; j < 8; j += 2) {
+    const v2h h = __builtin_convertvector((v2f{v[j], v[j + 1]}), v2h);
+    out[0][j] = h[0];
+    out[0][j + 1] = h[1];
+    if constexpr (NS == 2) {
+      const v2h l = __builtin_convertvector((v2f{v[j] - (float)h[0], v[j + 1] - (float)h[1]}), v2h);
+      out[1][j] = l[0];
+      out[1][j + 1] = l[1];
+    }
   }
 }
 
@@ -497,56 +504,74 @@ struct Running {
   float unit;                         // of o: the largest step of the values so far (0: none)
 };
 
-// Takes a block in: s[j][t] the products of column tile j with tokens 16 t + 4 (lane / 16) + r,
-// step its steps, qf the columns' factors, last[j] the last token of the block that the column sees
-// (63 and more: all), values(dt, h, part) the operand of dims 16 dt.. and tokens 32 h...
-// NV: parts of the values, NS: parts of the probabilities.
-template <int HD, int NT, int NS, int NV, typename Values>
-__device__ __forceinline__ void take_block(Running<HD, NT>& run, v4f (&s)[NT][4], float2 step,
-                                           const float (&qf)[NT], const int (&last)[NT], bool hidden,
-                                           uint32_t bad, Values values) {
+// Takes TT tiles of 16 tokens in (a block: 4): s[j][t] the products of column tile j with tokens
+// 16 t + 4 (lane / 16) + r, step their steps, qf the columns' factors, last[j] the last of the tokens that the
+// column sees (hidden: some column does not see them all), bad the lane's tokens whose values are not
+// finite, values(d, h, part) the operand of dims 16 d .. and tokens 32 h ...  NV: parts of the values,
+// NS: parts of the probabilities.
+//
+// The weights exp2(s f - max + 15) take the ratio of the values' step to the unit of o as a summand of the
+// exponent (a fused multiply-add a score either way), and their sum takes its inverse.
+template <int TT, int HD, int NT, int NS, int NV, typename Values>
+__device__ __forceinline__ void take_tokens(Running<HD, NT>& run, v4f (&s)[NT][TT], float2 step,
+                                            const float (&qf)[NT], const int (&last)[NT], bool hidden,
+                                            uint32_t bad, Values values) {
+  constexpr int HH = (TT + 1) / 2;                       // operands of 32 tokens
   const int tok = (threadIdx.x & 63) >> 4 << 2;
   const bool nan = !(step.x < INFINITY) || !(step.y < INFINITY);
   const float vstep = nan ? 0.0f : step.y;
   const float unit = fmaxf(run.unit, vstep);
-  const float ratio = vstep > 0.0f ? vstep / unit : 0.0f;
+  const float ratio = vstep > 0.0f ? vstep / unit : 1.0f;
   const float shrink = run.unit > 0.0f ? run.unit / unit : 0.0f;
+  const float lr = __builtin_amdgcn_logf(ratio);         // log2
+  const float inverse = 1.0f / ratio;
   run.unit = unit;
-  v8h p[NT][2][NS];
+  if (nan || bad)
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int t = 0; t < TT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (nan || (bad >> (t * 4 + r) & 1)) s[j][t][r] = __builtin_nanf("");
+  if (hidden)
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int t = 0; t < TT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (t * 16 + tok + r > last[j]) s[j][t][r] = -INFINITY;
+  v8h p[NT][HH][NS];
   float al[NT];
   bool same = shrink == 1.0f;
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
-    const float f = qf[j] * (nan ? __builtin_nanf("") : step.x);
-    float bm = -INFINITY;
+    const float f = nan ? 1.0f : qf[j] * step.x;
+    float bm = s[j][0][0];
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < TT; ++t)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float x = s[j][t][r] * f;
-        if (bad >> (t * 4 + r) & 1) x = __builtin_nanf("");
-        if (hidden && t * 16 + tok + r > last[j]) x = -INFINITY;
-        s[j][t][r] = x;
-        bm = fmaxf(bm, x);
-      }
-    const float m = fmaxf(run.m[j], col_max(bm));
+      for (int r = 0; r < 4; ++r) bm = fmaxf(bm, s[j][t][r]);
+    const float m = fmaxf(run.m[j], col_max(bm) * f);
     const float ref = m == -INFINITY ? 0.0f : m;
-    al[j] = exp2f(run.m[j] - ref);
+    al[j] = __builtin_amdgcn_exp2f(run.m[j] - ref);
     run.m[j] = m;
     same = same && al[j] == 1.0f;
+    const float off = (15.0f + lr) - ref;
     float sum = 0.0f;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < HH; ++h) {
       float w[8];
 #pragma unroll
       for (int r = 0; r < 8; ++r) {
-        const float e = __builtin_amdgcn_exp2f(s[j][2 * h + r / 4][r % 4] - ref + 15.0f);
-        sum += e;
-        w[r] = e * ratio;
+        w[r] = 2 * h + r / 4 < TT ? __builtin_amdgcn_exp2f(fmaf(s[j][2 * h + r / 4 < TT ? 2 * h + r / 4 : 0][r % 4], f, off))
+                                  : 0.0f;
+        sum += w[r];
       }
       split_f16<NS>(w, p[j][h]);
     }
-    run.l[j] = run.l[j] * al[j] + sum;
+    run.l[j] = fmaf(sum, inverse, run.l[j] * al[j]);
     al[j] *= shrink;
   }
   if (!__all(same)) {
@@ -558,7 +583,7 @@ __device__ __forceinline__ void take_block(Running<HD, NT>& run, v4f (&s)[NT][4]
 #pragma unroll
   for (int d = 0; d < HD / 16; ++d)
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < HH; ++h)
 #pragma unroll
       for (int a = 0; a < NV; ++a) {
         const v8h v = values(d, h, a);
@@ -570,103 +595,76 @@ __device__ __forceinline__ void take_block(Running<HD, NT>& run, v4f (&s)[NT][4]
       }
 }
 
-// Takes the tokens behind the last complete block in: scaled, in NS parts.
+// Takes 16 tokens behind the last complete block in, from token t0 of that block on (have: the tokens
+// it holds, more than t0), scaled, in NS parts.  A lane loads its rows once, all at a time.
 template <typename T, int HD, int NT, int NS>
-__device__ __forceinline__ void take_tail(const CacheView& c, int layer, int head, int g, int64_t slot,
-                                          int len, int total, const v8h (&qf)[NT][HD / 32][NS],
-                                          const float (&qs)[NT], const int (&last)[NT],
-                                          Running<HD, NT>& run) {
-  const int lane = threadIdx.x & 63, it = total / kBlock;
-  v4f s[NT][4];
+__device__ __forceinline__ void take_tail(const T* kt, const T* vt, int t0, int have,
+                                          const v8h (&qf)[NT][HD / 32][NS], const float (&qs)[NT],
+                                          const int (&pos)[NT], int first, Running<HD, NT>& run) {
+  const int lane = threadIdx.x & 63;
+  float kx[HD / 32][8], vx[HD / 16][4];
+  const bool in = t0 + (lane & 15) < have;
 #pragma unroll
-  for (int j = 0; j < NT; ++j)
+  for (int k = 0; k < HD / 32; ++k)
+    load8(kt + (t0 + (in ? lane & 15 : 0)) * HD + k * 32 + (lane >> 4) * 8, kx[k]);
+  const int vt0 = t0 + (lane >> 4) * 4;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) s[j][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-  const int64_t th = c.tail_head(layer, c.sel[g] ^ (it != len / kBlock), c.tail_of[slot], head) * (kBlock * HD);
-  const T* kt = (const T*)c.ktail + th;
-  const T* vt = (const T*)c.vtail + th;
-  const int have = total - it * kBlock;              // tokens of the block
-  float2 step;
-  {
-    // keys, a 16-token tile at a time: first their largest magnitude
-    float m = 0.0f;
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int k = 0; k < HD / 32; ++k) {
-        const int tk = t * 16 + (lane & 15);
-        float x[8];
-        if (tk < have) {
-          load8(kt + tk * HD + k * 32 + (lane >> 4) * 8, x);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) m = fmaxf(m, finite_abs(x[j]));
-        }
-      }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-    const int e = exponent_of(m) - 7;
-    step.x = ldexpf(1.0f, e);
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int k = 0; k < HD / 32; ++k) {
-        const int tk = t * 16 + (lane & 15);
-        float x[8] = {};
-        if (tk < have) load8(kt + tk * HD + k * 32 + (lane >> 4) * 8, x);
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          x[j] = fabsf(x[j]) < INFINITY ? ldexpf(x[j], -e) : __builtin_nanf("");
-        v8h a[NS];
-        split_f16<NS>(x, a);
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          s[j][t] = mma(a[0], qf[j][k][0], s[j][t]);
-          if constexpr (NS == 2) {
-            s[j][t] = mma(a[0], qf[j][k][1], s[j][t]);
-            s[j][t] = mma(a[1], qf[j][k][0], s[j][t]);
-          }
-        }
-      }
-  }
-  // values: their largest magnitude, and which tokens have one that is not finite
-  auto value_rows = [&](int d, int h, float (&x)[8]) __attribute__((always_inline)) {
-    const T* p = vt + (d * 16 + (lane & 15)) * kBlock + h * 32 + (lane >> 4) * 4;
-    const int t0 = h * 32 + (lane >> 4) * 4;
-    load4(p, x);
-    load4(p + 16, x + 4);
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (t0 + (j / 4) * 16 + j % 4 >= have) x[j] = 0.0f;
-  };
-  float m = 0.0f;
+  for (int d = 0; d < HD / 16; ++d) load4(vt + (d * 16 + (lane & 15)) * kBlock + vt0, vx[d]);
+  float km = 0.0f, vm = 0.0f;
   uint32_t bad = 0;
-#pragma unroll 1
+#pragma unroll
+  for (int k = 0; k < HD / 32; ++k)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) km = fmaxf(km, in ? finite_abs(kx[k][j]) : 0.0f);
+#pragma unroll
   for (int d = 0; d < HD / 16; ++d)
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float x[8];
-      value_rows(d, h, x);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        m = fmaxf(m, finite_abs(x[j]));
-        if (!(fabsf(x[j]) < INFINITY)) bad |= 1u << (h * 8 + j);
-      }
+    for (int r = 0; r < 4; ++r) {
+      if (vt0 + r >= have) vx[d][r] = 0.0f;
+      vm = fmaxf(vm, finite_abs(vx[d][r]));
+      if (!(fabsf(vx[d][r]) < INFINITY)) bad |= 1u << r;
     }
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  for (int o = 32; o > 0; o >>= 1) {
+    km = fmaxf(km, __shfl_xor(km, o, 64));
+    vm = fmaxf(vm, __shfl_xor(vm, o, 64));
+  }
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) bad |= __shfl_xor(bad, o, 64);
-  const int e = exponent_of(m) - 7;
-  step.y = ldexpf(1.0f, e);
-  v8h a[NS];
-  take_block<HD, NT, NS, NS>(run, s, step, qs, last, true, bad, [&](int d, int h, int b) {
-    if (b == 0) {
-      float x[8];
-      value_rows(d, h, x);
+  const int ke = exponent_of(km) - 7, ve = exponent_of(vm) - 7;
+  v4f s[NT][1];
+  int last[NT];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = bad >> (h * 8 + j) & 1 ? 0.0f : ldexpf(x[j], -e);
+  for (int j = 0; j < NT; ++j) {
+    s[j][0] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    last[j] = pos[j] - first - t0;
+  }
+#pragma unroll
+  for (int k = 0; k < HD / 32; ++k) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      kx[k][j] = !in ? 0.0f : fabsf(kx[k][j]) < INFINITY ? ldexpf(kx[k][j], -ke) : __builtin_nanf("");
+    v8h a[NS];
+    split_f16<NS>(kx[k], a);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      s[j][0] = mma(a[0], qf[j][k][0], s[j][0]);
+      if constexpr (NS == 2) {
+        s[j][0] = mma(a[0], qf[j][k][1], s[j][0]);
+        s[j][0] = mma(a[1], qf[j][k][0], s[j][0]);
+      }
+    }
+  }
+  v8h a[NS];
+  take_tokens<1, HD, NT, NS, NS>(run, s, make_float2(ldexpf(1.0f, ke), ldexpf(1.0f, ve)), qs, last, true,
+                                 bad, [&](int d, int, int part) {
+    if (part == 0) {
+      float x[8] = {};
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[r] = bad >> r & 1 ? 0.0f : ldexpf(vx[d][r], -ve);
       split_f16<NS>(x, a);
     }
-    return a[b];
+    return a[part];
   });
 }
 
@@ -750,7 +748,7 @@ __device__ __forceinline__ void store_columns(const Running<HD, NT>& run, T* out
 
 // grid: splits, key/value heads, rows.  A wave takes every fourth block of its work group's share.
 template <typename T, int HD, int NT>
-__global__ void __launch_bounds__(256) k_attend_rows(CacheView c, int layer, const T* q, T* out, int n,
+__global__ void __launch_bounds__(256, NT == 1 ? 3 : 2) k_attend_rows(CacheView c, int layer, const T* q, T* out, int n,
                                                      const int32_t* counts, int heads, float scale,
                                                      float* part) {
   constexpr int NS = sizeof(T) == 2 ? 1 : 2, NC = 16 * NT;
@@ -774,7 +772,8 @@ __global__ void __launch_bounds__(256) k_attend_rows(CacheView c, int layer, con
   load_columns<T, HD, NT, NS>(c, q, row, n, heads, head, len, cnt, 0, scale, qf, qs, pos);
   Running<HD, NT> run;
   start(run);
-  for (int it = i0 + wave; it < i1; it += 4) {
+  const int ic = i1 < full ? i1 : full;                  // coded blocks end here
+  for (int it = i0 + wave; it < ic; it += 4) {
     int last[NT];
 #pragma unroll
     for (int j = 0; j < NT; ++j) last[j] = pos[j] - it * kBlock;
@@ -784,37 +783,38 @@ __global__ void __launch_bounds__(256) k_attend_rows(CacheView c, int layer, con
     for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int t = 0; t < 4; ++t) s[j][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    if (it < full) {
-      const int64_t ph = c.page_head(layer, c.page_of(slot, it, len), head);
-      const uint4* kp = (const uint4*)(c.kpage + ph * (kBlock * HD)) + lane;
-      const uint4* vp = (const uint4*)(c.vpage + ph * (kBlock * HD)) + lane;
-      uint4 kr[2][HD / 32], vr[HD / 16];
+    const int64_t ph = c.page_head(layer, c.page_of(slot, it, len), head);
+    const uint4* kp = (const uint4*)(c.kpage + ph * (kBlock * HD)) + lane;
+    const uint4* vp = (const uint4*)(c.vpage + ph * (kBlock * HD)) + lane;
+    uint4 kr[2][HD / 32], vr[HD / 16];
 #pragma unroll
-      for (int p = 0; p < 2; ++p)
+    for (int p = 0; p < 2; ++p)
 #pragma unroll
-        for (int k = 0; k < HD / 32; ++k) kr[p][k] = kp[(p * (HD / 32) + k) * 64];
+      for (int k = 0; k < HD / 32; ++k) kr[p][k] = kp[(p * (HD / 32) + k) * 64];
 #pragma unroll
-      for (int d = 0; d < HD / 16; ++d) vr[d] = vp[d * 64];
-      const float2 step = c.step[ph];
+    for (int d = 0; d < HD / 16; ++d) vr[d] = vp[d * 64];
+    const float2 step = c.step[ph];
 #pragma unroll
-      for (int p = 0; p < 2; ++p)
+    for (int p = 0; p < 2; ++p)
 #pragma unroll
-        for (int k = 0; k < HD / 32; ++k) {
-          const v8h a = codes_f16(kr[p][k].x, kr[p][k].y), b = codes_f16(kr[p][k].z, kr[p][k].w);
+      for (int k = 0; k < HD / 32; ++k) {
+        const v8h a = codes_f16(kr[p][k].x, kr[p][k].y), b = codes_f16(kr[p][k].z, kr[p][k].w);
 #pragma unroll
-          for (int j = 0; j < NT; ++j)
+        for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int x = 0; x < NS; ++x) {
-              s[j][2 * p] = mma(a, qf[j][k][x], s[j][2 * p]);
-              s[j][2 * p + 1] = mma(b, qf[j][k][x], s[j][2 * p + 1]);
-            }
-        }
-      take_block<HD, NT, NS, 1>(run, s, step, qs, last, hidden, 0u, [&](int d, int h, int) {
-        return h == 0 ? codes_f16(vr[d].x, vr[d].y) : codes_f16(vr[d].z, vr[d].w);
-      });
-    } else {
-      take_tail<T, HD, NT>(c, layer, head, g, slot, len, total, qf, qs, last, run);
-    }
+          for (int x = 0; x < NS; ++x) {
+            s[j][2 * p] = mma(a, qf[j][k][x], s[j][2 * p]);
+            s[j][2 * p + 1] = mma(b, qf[j][k][x], s[j][2 * p + 1]);
+          }
+      }
+    take_tokens<4, HD, NT, NS, 1>(run, s, step, qs, last, hidden, 0u, [&](int d, int h, int) {
+      return h == 0 ? codes_f16(vr[d].x, vr[d].y) : codes_f16(vr[d].z, vr[d].w);
+    });
+  }
+  if (i1 > full && wave * 16 < total - full * kBlock) {  // a wave, 16 of the tokens behind
+    const int64_t th = c.tail_head(layer, c.sel[g] ^ (full != len / kBlock), c.tail_of[slot], head) * (kBlock * HD);
+    take_tail<T, HD, NT, NS>((const T*)c.ktail + th, (const T*)c.vtail + th, wave * 16,
+                             total - full * kBlock, qf, qs, pos, full * kBlock, run);
   }
   // joined in two rounds
   finish(run);
@@ -953,7 +953,7 @@ __global__ void __launch_bounds__(512) k_attend_tile(CacheView c, int layer, con
       }
       // the wave's first column sees the fewest tokens
       const bool hidden = it * kBlock + kBlock > len + wc / G + 1;
-      take_block<HD, NT, NS, 1>(run, s, step, qs, last, hidden, 0u, [&](int d, int h, int) {
+      take_tokens<4, HD, NT, NS, 1>(run, s, step, qs, last, hidden, 0u, [&](int d, int h, int) {
         return __builtin_bit_cast(v8h, lds[buf][(4 * KS + 2 * d + h) * 64 + lane]);
       });
     }
@@ -961,10 +961,12 @@ __global__ void __launch_bounds__(512) k_attend_tile(CacheView c, int layer, con
     __syncthreads();
   }
   if (i1 > full && full < mine) {
-    int last[NT];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) last[j] = pos[j] - full * kBlock;
-    take_tail<T, HD, NT>(c, layer, head, g, slot, len, total, qf, qs, last, run);
+    const int64_t th = c.tail_head(layer, c.sel[g] ^ (full != len / kBlock), c.tail_of[slot], head) * (kBlock * HD);
+    const int have = total - full * kBlock;
+#pragma unroll 1
+    for (int t0 = 0; t0 < have; t0 += 16)
+      take_tail<T, HD, NT, NS>((const T*)c.ktail + th, (const T*)c.vtail + th, t0, have, qf, qs, pos,
+                               full * kBlock, run);
   }
   if (wc >= cols) return;
   finish(run);
@@ -973,51 +975,50 @@ __global__ void __launch_bounds__(512) k_attend_tile(CacheView c, int layer, con
   store_columns<T, HD, NT>(run, out, pp, kTileCols, wc, wave * 32, row, n, heads, head, G, cols);
 }
 
-// Joins the parts of a row's columns: a wave per column, a lane per split for the weights, then per
-// dim for the sum.
+// Joins the parts of a column: a work group per column, its waves take every fourth part, a lane two dims.
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) k_attend_join(CacheView c, const float* part, T* out, int n,
                                                      const int32_t* counts, int heads, int splits,
                                                      int nc, int tiles) {
-  const int lane = threadIdx.x & 63, head = blockIdx.y, row = blockIdx.z;
+  __shared__ float lo[4][HD], ll[4], lm[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, head = blockIdx.y, row = blockIdx.z;
   const int g = row / c.width;
   const int cnt = query_count(c, g, n, counts);
-  const int G = heads / c.heads_kv, cols = cnt * G;
-  const int col = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (col >= cols) return;                               // whole wave
+  const int G = heads / c.heads_kv, cols = cnt * G, col = blockIdx.x;
+  if (col >= cols) return;
   const int tile = col / nc, pc = col % nc;
   const int items = items_of(c.len[g], cnt, cols, (tile + 1) * nc, G), per = blocks_per_split(items, splits);
   if (items <= per) return;                              // written already
   const int used = (items + per - 1) / per;
-  const float* pp = part + (((int64_t)row * c.heads_kv + head) * tiles + tile) * splits * nc * (HD + 2);
   const int64_t stride = (int64_t)nc * (HD + 2);
+  const float* pp = part + (((int64_t)row * c.heads_kv + head) * tiles + tile) * splits * stride;
   float m = -INFINITY;
-  for (int s = lane; s < used; s += 64) m = fmaxf(m, pp[s * stride + nc * HD + pc]);
+  for (int s = threadIdx.x; s < used; s += 256) m = fmaxf(m, pp[s * stride + nc * HD + pc]);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  if (lane == 0) lm[wave] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(lm[0], lm[1]), fmaxf(lm[2], lm[3]));
   const float ref = m == -INFINITY ? 0.0f : m;
-  float l = 0.0f, acc[2] = {0.0f, 0.0f};
-  for (int s0 = 0; s0 < used; s0 += 64) {
-    float w = 0.0f;
-    if (s0 + lane < used) {
-      const float* q = pp + (s0 + lane) * stride + nc * HD + pc;
-      w = q[nc] * exp2f(q[0] - ref);
-    }
-    float ws = w;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) ws += __shfl_xor(ws, o, 64);
-    l += ws;
-    const int k = used - s0 < 64 ? used - s0 : 64;
-    for (int s = 0; s < k; ++s) {
-      const float f = __shfl(w, s, 64);
-      const float* o = pp + (s0 + s) * stride + pc * HD;
-      acc[0] = fmaf(f, o[lane], acc[0]);
-      if (lane + 64 < HD) acc[1] = fmaf(f, o[lane + 64], acc[1]);
-    }
+  float l = 0.0f, a0 = 0.0f, a1 = 0.0f;
+  const bool mine = 2 * lane < HD;
+#pragma unroll 8
+  for (int s = wave; s < used; s += 4) {
+    const float* q = pp + s * stride;
+    const float w = q[nc * HD + nc + pc] * __builtin_amdgcn_exp2f(q[nc * HD + pc] - ref);
+    const float2 o = mine ? *(const float2*)(q + pc * HD + 2 * lane) : make_float2(0.0f, 0.0f);
+    l += w;
+    a0 = fmaf(w, o.x, a0);
+    a1 = fmaf(w, o.y, a1);
   }
-  T* op = out + (((int64_t)row * n + col / G) * heads + head * G + col % G) * HD;
-  st_val(op + lane, acc[0] / l);
-  if (lane + 64 < HD) st_val(op + lane + 64, acc[1] / l);
+  if (mine) *(float2*)&lo[wave][2 * lane] = make_float2(a0, a1);
+  if (lane == 0) ll[wave] = l;
+  __syncthreads();
+  const int e = threadIdx.x;
+  if (e < HD) {
+    T* op = out + (((int64_t)row * n + col / G) * heads + head * G + col % G) * HD;
+    st_val(op + e, (lo[0][e] + lo[1][e] + lo[2][e] + lo[3][e]) / (ll[0] + ll[1] + ll[2] + ll[3]));
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -1110,7 +1111,7 @@ hipError_t cache_attention_on(termezo_kvcache* c, int layer, const void* q, cons
     const int nt = cols <= 16 ? 1 : 2;
     const int splits = row_splits(c, rows * Hkv, nt);
     const dim3 grid((unsigned)splits, (unsigned)Hkv, (unsigned)rows);
-    const dim3 jgrid((unsigned)((cols + 3) / 4), (unsigned)Hkv, (unsigned)rows);
+    const dim3 jgrid((unsigned)cols, (unsigned)Hkv, (unsigned)rows);
 #define TMZ_CALL(T, HD)                                                                         \
   if (nt == 1)                                                                                  \
     hipLaunchKernelGGL((k_attend_rows<T, HD, 1>), grid, dim3(256), 0, s, w, layer, (const T*)q,  \
@@ -1128,7 +1129,7 @@ hipError_t cache_attention_on(termezo_kvcache* c, int layer, const void* q, cons
   const int tiles = (int)((cols + kTileCols - 1) / kTileCols);
   const int splits = tile_splits(c, rows * Hkv * tiles);
   const dim3 grid((unsigned)(tiles * splits), (unsigned)Hkv, (unsigned)rows);
-  const dim3 jgrid((unsigned)((cols + 3) / 4), (unsigned)Hkv, (unsigned)rows);
+  const dim3 jgrid((unsigned)cols, (unsigned)Hkv, (unsigned)rows);
 #define TMZ_CALL(T, HD)                                                                         \
   hipLaunchKernelGGL((k_attend_tile<T, HD>), grid, dim3(512), 0, s, w, layer, (const T*)q,       \
                      (T*)out, (int)n, counts, H, scale, splits, c->part);                       \
