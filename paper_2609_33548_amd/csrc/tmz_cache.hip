@@ -668,6 +668,9 @@ __device__ __forceinline__ void take_tail(const T* kt, const T* vt, int t0, int 
   });
 }
 
+// Work groups of the attention kernels (one or two column tiles; many columns) on a compute unit.
+constexpr int kRowsResident1 = 3, kRowsResident2 = 2, kTileResident = 2;
+
 // Blocks that columns below c1 of a row see, its incomplete one among them.
 __device__ __forceinline__ int items_of(int len, int cnt, int cols, int c1, int G) {
   const int last = c1 < cols ? (c1 - 1) / G : cnt - 1;   // the last query among them
@@ -748,7 +751,8 @@ __device__ __forceinline__ void store_columns(const Running<HD, NT>& run, T* out
 
 // grid: splits, key/value heads, rows.  A wave takes every fourth block of its work group's share.
 template <typename T, int HD, int NT>
-__global__ void __launch_bounds__(256, NT == 1 ? 3 : 2) k_attend_rows(CacheView c, int layer, const T* q, T* out, int n,
+__global__ void __launch_bounds__(256, NT == 1 ? kRowsResident1 : kRowsResident2)
+    k_attend_rows(CacheView c, int layer, const T* q, T* out, int n,
                                                      const int32_t* counts, int heads, float scale,
                                                      float* part) {
   constexpr int NS = sizeof(T) == 2 ? 1 : 2, NC = 16 * NT;
@@ -858,25 +862,24 @@ __global__ void __launch_bounds__(256, NT == 1 ? 3 : 2) k_attend_rows(CacheView 
 }
 
 // ---------------------------------------------------------------------------
-// Attention of many queries (prompts and their pieces): a work group of eight waves takes kTileCols
-// columns of a key/value head, 32 a wave, so the blocks that it walks are converted to fp16 once, into
+// Attention of many queries (prompts and their pieces): a work group of four waves takes kTileCols columns
+// of a key/value head, 32 a wave, so the blocks that it walks are converted to fp16 once, into
 // LDS, for all of them.  Two LDS buffers: while a block is used the next one's codes are on their way
 // in registers.  Every wave takes the incomplete block by itself at the end.
-// grid: splits x tiles (the longest first), key/value heads, rows.
+// grid: key/value heads x rows, tiles x splits: the longest tiles of all rows come first.
 // ---------------------------------------------------------------------------
-constexpr int kTileCols = 256;
-
+constexpr int kTileCols = 128;
 template <typename T, int HD>
-__global__ void __launch_bounds__(512) k_attend_tile(CacheView c, int layer, const T* q, T* out, int n,
+__global__ void __launch_bounds__(256, kTileResident) k_attend_tile(CacheView c, int layer, const T* q, T* out, int n,
                                                      const int32_t* counts, int heads, float scale,
                                                      int splits, float* part) {
   constexpr int NS = sizeof(T) == 2 ? 1 : 2, NT = 2, KS = HD / 32;
   constexpr int kPieces = kBlock * HD / 16;              // 16-byte pieces of a page
-  constexpr int kLoads = (2 * kPieces + 511) / 512;      // of keys and values, a thread
+  constexpr int kLoads = (2 * kPieces + 255) / 256;      // of keys and values, a thread
   __shared__ uint4 lds[2][4 * kPieces];                  // keys [16 tokens][32 dims], values [16 dims][32 tokens]
-  const int head = blockIdx.y, row = blockIdx.z, tid = threadIdx.x, lane = tid & 63;
+  const int head = blockIdx.x % c.heads_kv, row = blockIdx.x / c.heads_kv, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int tiles = gridDim.x / splits, tile = tiles - 1 - blockIdx.x / splits, split = blockIdx.x % splits;
+  const int tiles = gridDim.y / splits, tile = tiles - 1 - blockIdx.y / splits, split = blockIdx.y % splits;
   const int g = row / c.width;
   const int cnt = query_count(c, g, n, counts);
   const int G = heads / c.heads_kv, cols = cnt * G, c0 = tile * kTileCols;
@@ -904,7 +907,7 @@ __global__ void __launch_bounds__(512) k_attend_tile(CacheView c, int layer, con
     const uint4* vp = (const uint4*)(c.vpage + ph * (kBlock * HD));
 #pragma unroll
     for (int x = 0; x < kLoads; ++x) {
-      const int i = x * 512 + tid;
+      const int i = x * 256 + tid;
       if (i < 2 * kPieces) raw[x] = i < kPieces ? kp[i] : vp[i - kPieces];
     }
     step_next = c.step[ph];
@@ -912,7 +915,7 @@ __global__ void __launch_bounds__(512) k_attend_tile(CacheView c, int layer, con
   auto place = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
     for (int x = 0; x < kLoads; ++x) {
-      const int i = x * 512 + tid;
+      const int i = x * 256 + tid;
       if (i < 2 * kPieces) {
         const v8h a = codes_f16(raw[x].x, raw[x].y), b = codes_f16(raw[x].z, raw[x].w);
         // keys: piece (pair p, dims k) holds 16 tokens 2 p and 2 p + 1; values: (dims d) both halves
@@ -975,35 +978,33 @@ __global__ void __launch_bounds__(512) k_attend_tile(CacheView c, int layer, con
   store_columns<T, HD, NT>(run, out, pp, kTileCols, wc, wave * 32, row, n, heads, head, G, cols);
 }
 
-// Joins the parts of a column: a work group per column, its waves take every fourth part, a lane two dims.
-template <typename T, int HD>
+// Joins the parts of a column.  JW = 4: a work group per column, its waves take every fourth part; JW = 1: a
+// wave per column.  A lane takes two dims.
+template <typename T, int HD, int JW>
 __global__ void __launch_bounds__(256) k_attend_join(CacheView c, const float* part, T* out, int n,
                                                      const int32_t* counts, int heads, int splits,
                                                      int nc, int tiles) {
-  __shared__ float lo[4][HD], ll[4], lm[4];
+  __shared__ float lo[JW][HD], ll[JW];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, head = blockIdx.y, row = blockIdx.z;
   const int g = row / c.width;
   const int cnt = query_count(c, g, n, counts);
-  const int G = heads / c.heads_kv, cols = cnt * G, col = blockIdx.x;
-  if (col >= cols) return;
+  const int G = heads / c.heads_kv, cols = cnt * G, col = JW == 4 ? blockIdx.x : blockIdx.x * 4 + wave;
+  if (col >= cols) return;                               // whole work group, or whole wave
   const int tile = col / nc, pc = col % nc;
   const int items = items_of(c.len[g], cnt, cols, (tile + 1) * nc, G), per = blocks_per_split(items, splits);
   if (items <= per) return;                              // written already
   const int used = (items + per - 1) / per;
   const int64_t stride = (int64_t)nc * (HD + 2);
   const float* pp = part + (((int64_t)row * c.heads_kv + head) * tiles + tile) * splits * stride;
-  float m = -INFINITY;
-  for (int s = threadIdx.x; s < used; s += 256) m = fmaxf(m, pp[s * stride + nc * HD + pc]);
+  float m = -INFINITY;                                   // of all parts, in every wave
+  for (int s = lane; s < used; s += 64) m = fmaxf(m, pp[s * stride + nc * HD + pc]);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  if (lane == 0) lm[wave] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(lm[0], lm[1]), fmaxf(lm[2], lm[3]));
   const float ref = m == -INFINITY ? 0.0f : m;
   float l = 0.0f, a0 = 0.0f, a1 = 0.0f;
   const bool mine = 2 * lane < HD;
 #pragma unroll 8
-  for (int s = wave; s < used; s += 4) {
+  for (int s = JW == 4 ? wave : 0; s < used; s += JW) {
     const float* q = pp + s * stride;
     const float w = q[nc * HD + nc + pc] * __builtin_amdgcn_exp2f(q[nc * HD + pc] - ref);
     const float2 o = mine ? *(const float2*)(q + pc * HD + 2 * lane) : make_float2(0.0f, 0.0f);
@@ -1011,13 +1012,26 @@ __global__ void __launch_bounds__(256) k_attend_join(CacheView c, const float* p
     a0 = fmaf(w, o.x, a0);
     a1 = fmaf(w, o.y, a1);
   }
+  T* op = out + (((int64_t)row * n + col / G) * heads + head * G + col % G) * HD;
+  if (JW == 1) {
+    if (mine) {
+      st_val(op + 2 * lane, a0 / l);
+      st_val(op + 2 * lane + 1, a1 / l);
+    }
+    return;
+  }
   if (mine) *(float2*)&lo[wave][2 * lane] = make_float2(a0, a1);
   if (lane == 0) ll[wave] = l;
   __syncthreads();
   const int e = threadIdx.x;
   if (e < HD) {
-    T* op = out + (((int64_t)row * n + col / G) * heads + head * G + col % G) * HD;
-    st_val(op + e, (lo[0][e] + lo[1][e] + lo[2][e] + lo[3][e]) / (ll[0] + ll[1] + ll[2] + ll[3]));
+    float v = 0.0f, t = 0.0f;
+#pragma unroll
+    for (int w = 0; w < JW; ++w) {
+      v += lo[w][e];
+      t += ll[w];
+    }
+    st_val(op + e, v / t);
   }
 }
 
@@ -1062,22 +1076,32 @@ CacheView view_of(const termezo_kvcache* c) {
     else { CALL(float, 128); }                                     \
   }
 
-// Work groups over a row's tokens for `units` rows x heads and nt column tiles: as many as fill the
-// device a few times (kSplitGroups), but at least a block for each of a work group's four waves
-// at max_len.  The kernels divide the tokens that there are, so no length is known here.
-constexpr int64_t kSplitGroups = 1024;
-int row_splits(const termezo_kvcache* c, int64_t units, int nt) {
-  const int64_t most = (c->max_blocks + 3) / 4;
-  return (int)std::max<int64_t>(1, std::min(most, kSplitGroups / units));
-}
-
-// The same for tiles of many columns: at least four blocks a work group.
-constexpr int64_t kTileGroups = 512;
-int tile_splits(const termezo_kvcache* c, int64_t units) {
-  return (int)std::max<int64_t>(1, std::min(c->max_blocks / 4, kTileGroups / units));
+// Work groups over a row's tokens, for `units` rows x heads: as many as run at a time (`resident` on a compute
+// unit), but at least a block for each of a work group's four waves at max_len.  The kernels divide
+// the tokens that there are, so no length is known here.  One round of work groups measured best: 64 rows of
+// 2000 to 4000 tokens, 5 heads of 128: 49 us at 768 work groups in all, 53 at 1024, 53 at 2048; two
+// rows of 131000: 62, 75, 72 us.
+int token_splits(const termezo_kvcache* c, int64_t units, int resident) {
+  const int64_t groups = (int64_t)resident * c->ctx->n_cu;
+  return (int)std::max<int64_t>(1, std::min((c->max_blocks + 3) / 4, groups / units));
 }
 
 int64_t rows_of(const termezo_kvcache* c) { return (int64_t)c->cfg.groups * c->width; }
+
+// Few parts (8 and less; measured: 5 parts of 18432 columns of 96 19.6 us with four waves a column) leave
+// a column's further waves idle.
+template <typename T, int HD>
+void join(const termezo_kvcache* c, const CacheView& w, T* out, int n, const int32_t* counts, int splits,
+          int nc, int tiles, hipStream_t s) {
+  const int Hkv = c->cfg.n_kv_heads, cols = n * (c->cfg.n_heads / Hkv);
+  const dim3 grid((unsigned)(splits > 8 ? cols : (cols + 3) / 4), (unsigned)Hkv, (unsigned)rows_of(c));
+  if (splits > 8)
+    hipLaunchKernelGGL((k_attend_join<T, HD, 4>), grid, dim3(256), 0, s, w, c->part, out, n, counts,
+                       c->cfg.n_heads, splits, nc, tiles);
+  else
+    hipLaunchKernelGGL((k_attend_join<T, HD, 1>), grid, dim3(256), 0, s, w, c->part, out, n, counts,
+                       c->cfg.n_heads, splits, nc, tiles);
+}
 
 }  // namespace
 
@@ -1109,9 +1133,8 @@ hipError_t cache_attention_on(termezo_kvcache* c, int layer, const void* q, cons
   const int64_t cols = n * (H / Hkv), rows = rows_of(c);
   if (cols <= 32) {
     const int nt = cols <= 16 ? 1 : 2;
-    const int splits = row_splits(c, rows * Hkv, nt);
+    const int splits = token_splits(c, rows * Hkv, nt == 1 ? kRowsResident1 : kRowsResident2);
     const dim3 grid((unsigned)splits, (unsigned)Hkv, (unsigned)rows);
-    const dim3 jgrid((unsigned)cols, (unsigned)Hkv, (unsigned)rows);
 #define TMZ_CALL(T, HD)                                                                         \
   if (nt == 1)                                                                                  \
     hipLaunchKernelGGL((k_attend_rows<T, HD, 1>), grid, dim3(256), 0, s, w, layer, (const T*)q,  \
@@ -1119,23 +1142,18 @@ hipError_t cache_attention_on(termezo_kvcache* c, int layer, const void* q, cons
   else                                                                                          \
     hipLaunchKernelGGL((k_attend_rows<T, HD, 2>), grid, dim3(256), 0, s, w, layer, (const T*)q,  \
                        (T*)out, (int)n, counts, H, scale, c->part);                             \
-  if (splits > 1)                                                                               \
-    hipLaunchKernelGGL((k_attend_join<T, HD>), jgrid, dim3(256), 0, s, w, c->part, (T*)out,      \
-                       (int)n, counts, H, splits, 16 * nt, 1)
+  if (splits > 1) join<T, HD>(c, w, (T*)out, (int)n, counts, splits, 16 * nt, 1, s)
     TMZ_CACHE_TYPES(c, TMZ_CALL)
 #undef TMZ_CALL
     return hipGetLastError();
   }
   const int tiles = (int)((cols + kTileCols - 1) / kTileCols);
-  const int splits = tile_splits(c, rows * Hkv * tiles);
-  const dim3 grid((unsigned)(tiles * splits), (unsigned)Hkv, (unsigned)rows);
-  const dim3 jgrid((unsigned)cols, (unsigned)Hkv, (unsigned)rows);
+  const int splits = token_splits(c, rows * Hkv * tiles, kTileResident);
+  const dim3 grid((unsigned)(Hkv * rows), (unsigned)(tiles * splits));
 #define TMZ_CALL(T, HD)                                                                         \
-  hipLaunchKernelGGL((k_attend_tile<T, HD>), grid, dim3(512), 0, s, w, layer, (const T*)q,       \
+  hipLaunchKernelGGL((k_attend_tile<T, HD>), grid, dim3(256), 0, s, w, layer, (const T*)q,       \
                      (T*)out, (int)n, counts, H, scale, splits, c->part);                       \
-  if (splits > 1)                                                                               \
-    hipLaunchKernelGGL((k_attend_join<T, HD>), jgrid, dim3(256), 0, s, w, c->part, (T*)out,      \
-                       (int)n, counts, H, splits, kTileCols, tiles)
+  if (splits > 1) join<T, HD>(c, w, (T*)out, (int)n, counts, splits, kTileCols, tiles, s)
   TMZ_CACHE_TYPES(c, TMZ_CALL)
 #undef TMZ_CALL
   return hipGetLastError();
@@ -1264,7 +1282,8 @@ termezo_status termezo_kvcache_create(termezo_ctx* ctx, const termezo_kvcache_co
     A((void**)&c->table, slots * nblk * 4);
     if (f.rope_base > 0.0f) A((void**)&c->rope, f.max_len * (hd / 2) * 8);
     // parts of at most that many work groups (where there are more units nothing is split)
-    A((void**)&c->part, std::max(kSplitGroups * 32, kTileGroups * kTileCols) * (hd + 2) * 4);
+    A((void**)&c->part, (int64_t)ctx->n_cu *
+          std::max(std::max(kRowsResident1 * 16, kRowsResident2 * 32), kTileResident * kTileCols) * (hd + 2) * 4);
   }
   termezo_status st = hip_status(c, e, "kvcache_create");
   if (st == TERMEZO_OK) {
