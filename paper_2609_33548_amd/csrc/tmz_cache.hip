@@ -60,6 +60,58 @@ __device__ __forceinline__ void st_val(uint16_t* p, float v) {
 __device__ __forceinline__ float as_type(const float*, float v) { return v; }
 __device__ __forceinline__ float as_type(const uint16_t*, float v) { return (float)(__bf16)v; }
 
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
+  const float4 a = ((const float4*)p)[0], b = ((const float4*)p)[1];
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ void load8(const uint16_t* p, float (&v)[8]) {
+  const uint4 r = *(const uint4*)p;
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    v[2 * j] = __uint_as_float(w[j] << 16);
+    v[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ void load4(const float* p, float* v) {
+  const float4 a = *(const float4*)p;
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+}
+__device__ __forceinline__ void load4(const uint16_t* p, float* v) {
+  const uint2 r = *(const uint2*)p;
+  v[0] = __uint_as_float(r.x << 16);
+  v[1] = __uint_as_float(r.x & 0xFFFF0000u);
+  v[2] = __uint_as_float(r.y << 16);
+  v[3] = __uint_as_float(r.y & 0xFFFF0000u);
+}
+__device__ __forceinline__ void store4(float* p, v4f v) {
+  *(float4*)p = make_float4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ void store4(uint16_t* p, v4f v) {
+  uint2 r;
+  r.x = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[0]) |
+        ((uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[1]) << 16);
+  r.y = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2]) |
+        ((uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[3]) << 16);
+  *(uint2*)p = r;
+}
+
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+  store4(p, v4f{v[0], v[1], v[2], v[3]});
+  store4(p + 4, v4f{v[4], v[5], v[6], v[7]});
+}
+__device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    w[j] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * j]) |
+           ((uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * j + 1]) << 16);
+  *(uint4*)p = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // Tokens that an append takes for group g: counts[g], or n; 0 and a deferred error for counts
 // outside 0 .. n and for tokens past the end.
 __device__ __forceinline__ int append_count(const CacheView& c, int g, int n, const int32_t* counts) {
@@ -101,98 +153,170 @@ __global__ void __launch_bounds__(256) k_rope_table(float2* t, int64_t n, int ha
 }
 
 // ---------------------------------------------------------------------------
-// Append: block y / head / row.  A work group takes one block of one head: the tokens that the tail
-// holds already and the new ones go to LDS (keys rotated and rounded to the activation type), and
-// the block leaves as a page when it is complete, else the new tokens go to a tail: the buffer in
-// use when the block had begun, the other one otherwise (so that the call can be made again until
-// the tokens are advanced).  Bound by the bytes moved; a block's 64 x hd values are read once.
+// Append: grid blocks, heads, rows.  A work group takes one block of one head; its values go through
+// registers once: a thread holds pieces of 8 dims and their partners HD / 2 further (keys, which are rotated and
+// rounded to the activation type) and 4 tokens x 8 dims (values).  A complete block takes the largest
+// magnitudes over the work group and leaves as a page, put into its byte order in LDS (the values' 16-byte units
+// exchanged by their piece of dims, so that a store's lanes fall on different banks); else the new tokens
+// go to a tail: the buffer in use when the block had begun, the other one otherwise (so that the
+// call can be made again until the tokens are advanced).  Bound by the bytes moved.
 // ---------------------------------------------------------------------------
+// Codes of eight or four values, byte j the j-th.
+__device__ __forceinline__ uint32_t code4(float a, float b, float c, float d, float s) {
+  auto q = [&](float x) __attribute__((always_inline)) {
+    return (uint32_t)((int)fminf(fmaxf(__builtin_rintf(x * s), -127.0f), 127.0f) + 128);
+  };
+  return q(a) | q(b) << 8 | q(c) << 16 | q(d) << 24;
+}
+// Where the unit of 16 bytes u of a values page lies in LDS.
+__device__ __forceinline__ int unit_at(int u) { return u ^ ((u >> 6 & 3) << 1 | (u >> 3 & 1)); }
+
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) k_cache_append(CacheView c, int layer, const T* k, const T* v,
                                                       int n, const int32_t* counts) {
-  constexpr int LD = HD + 8;
-  __shared__ T tile[kBlock * LD];
-  __shared__ float red[4];
-  __shared__ int bad[4];
+  constexpr int PC = HD / 16, KU = kBlock * PC;          // pairs of pieces of a token, of a block
+  constexpr int KL = (KU + 255) / 256;
+  constexpr int VC = HD / 8, VU = 16 * VC;               // (4 tokens, 8 dims)
+  __shared__ uint4 page[2][kBlock * HD / 16];
+  __shared__ float red[4][2];
   const int head = blockIdx.y, row = blockIdx.z, tid = threadIdx.x;
   const int g = row / c.width;
   const int64_t slot = (int64_t)g * c.beams + row % c.width;
-  const int len = c.len[g], cnt = append_count(c, g, n, counts);
+  const int64_t tail = c.tail_of[slot];
+  const int len = c.len[g], buf = c.sel[g], cnt = append_count(c, g, n, counts);
   if (blockIdx.x == 0 && head == 0 && row % c.width == 0 && tid == 0) c.pend[g] = cnt;
   const int64_t blk = len / kBlock + blockIdx.x;
   const int64_t t0 = blk * kBlock;                       // first token of the block
   if (cnt == 0 || t0 >= (int64_t)len + cnt) return;
   const int begun = blockIdx.x == 0 ? len % kBlock : 0;  // tokens in the tail
   const int end = (int)std::min<int64_t>((int64_t)len + cnt - t0, kBlock);
-  const int buf = c.sel[g];
-  const int64_t tail = c.tail_of[slot];
-  T* kt = (T*)c.ktail + c.tail_head(layer, blockIdx.x == 0 ? buf : buf ^ 1, tail, head) * (kBlock * HD);
-  T* vt = (T*)c.vtail + c.tail_head(layer, blockIdx.x == 0 ? buf : buf ^ 1, tail, head) * (kBlock * HD);
+  const int64_t th = c.tail_head(layer, blockIdx.x == 0 ? buf : buf ^ 1, tail, head) * (kBlock * HD);
+  T* kt = (T*)c.ktail + th;
+  T* vt = (T*)c.vtail + th;
   const bool whole = end == kBlock;
-  const int64_t ph = c.page_head(layer, c.own_page(slot, blk), head);
-  float steps[2];
-  for (int part = 0; part < 2; ++part) {
-    const T* src = part ? v : k;
-    // new tokens
-    for (int i = tid; i < (end - begun) * (HD / 2); i += 256) {
-      const int t = begun + i / (HD / 2), d = i % (HD / 2);
-      const int64_t pos = t0 + t;
-      const T* x = src + ((((int64_t)row * n + (pos - len)) * c.heads_kv + head) * HD);
-      float a = ld_val(x + d), b = ld_val(x + d + HD / 2);
-      if (part == 0 && c.rope) {
-        const float2 r = c.rope[pos * (HD / 2) + d];
-        const float a2 = a * r.x - b * r.y, b2 = b * r.x + a * r.y;
-        a = a2;
-        b = b2;
-      }
-      st_val(&tile[t * LD + d], a);
-      st_val(&tile[t * LD + d + HD / 2], b);
-    }
-    if (whole)
-      for (int i = tid; i < begun * HD; i += 256) {
-        const int t = i / HD, d = i % HD;
-        tile[t * LD + d] = part ? vt[d * kBlock + t] : kt[t * HD + d];
-      }
-    __syncthreads();
-    if (!whole) {
-      for (int i = tid; i < (end - begun) * HD; i += 256) {
-        const int t = begun + i / HD, d = i % HD;
-        if (part)
-          vt[d * kBlock + t] = tile[t * LD + d];
-        else
-          kt[t * HD + d] = tile[t * LD + d];
-      }
-    } else {
-      float a = 0.0f;
-      int inf = 0;
-      for (int i = tid; i < kBlock * HD; i += 256) {
-        const float x = fabsf(ld_val(&tile[(i / HD) * LD + i % HD]));
-        inf |= !(x < INFINITY);
-        a = fmaxf(a, x);
-      }
+  // rows of this block's tokens in the caller's arrays: token t at (t0 - len + t)
+  const int64_t rs = (int64_t)c.heads_kv * HD;
+  const int64_t base = ((int64_t)row * n + (t0 - len)) * rs + (int64_t)head * HD;
+  float ka[KL][8], kb[KL][8], vx[4][8];
 #pragma unroll
-      for (int o = 32; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor(a, o, 64));
-      inf = __any(inf);
-      if ((tid & 63) == 0) {
-        red[tid >> 6] = a;
-        bad[tid >> 6] = inf;
+  for (int x = 0; x < KL; ++x) {
+    const int i = x * 256 + tid, t = i / PC, d = i % PC * 8;
+    if (KU % 256 != 0 && i >= KU) continue;
+    if (t >= begun && t < end) {
+      const T* src = k + base + t * rs + d;
+      load8(src, ka[x]);
+      load8(src + HD / 2, kb[x]);
+      if (c.rope) {
+        float r[16];
+        const float* rp = (const float*)(c.rope + (t0 + t) * (HD / 2) + d);
+        load4(rp, r); load4(rp + 4, r + 4); load4(rp + 8, r + 8); load4(rp + 12, r + 12);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float a = ka[x][j], b = kb[x][j];
+          ka[x][j] = as_type(src, a * r[2 * j] - b * r[2 * j + 1]);
+          kb[x][j] = as_type(src, b * r[2 * j] + a * r[2 * j + 1]);
+        }
       }
-      __syncthreads();
-      a = fmaxf(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])), kStepFloor);
-      inf = bad[0] | bad[1] | bad[2] | bad[3];
-      const float s = inf ? 0.0f : 127.0f * __fdiv_rn(1.0f, a);
-      steps[part] = inf ? __builtin_nanf("") : a * (1.0f / 127.0f);
-      uint8_t* page = (part ? c.vpage : c.kpage) + ph * (kBlock * HD);
-      for (int i = tid; i < kBlock * HD; i += 256) {
-        const int t = i / HD, d = i % HD;
-        const float x = inf ? 0.0f : ld_val(&tile[t * LD + d]);
-        const int q = (int)fminf(fmaxf(__builtin_rintf(x * s), -127.0f), 127.0f);
-        page[part ? value_at(t, d) : key_at<HD>(t, d)] = (uint8_t)(q + 128);
+      if (!whole) {
+        store8(kt + t * HD + d, ka[x]);
+        store8(kt + t * HD + d + HD / 2, kb[x]);
+      }
+    } else if (whole) {
+      load8(kt + t * HD + d, ka[x]);
+      load8(kt + t * HD + d + HD / 2, kb[x]);
+    }
+  }
+  const int vq = tid / VC * 4, vd = tid % VC * 8;        // the thread's tokens and dims
+  if (VU == 256 || tid < VU) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int t = vq + r;
+      if (t >= begun && t < end) {
+        load8(v + base + t * rs + vd, vx[r]);
+      } else if (whole) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) vx[r][j] = ld_val(vt + (vd + j) * kBlock + t);
       }
     }
-    __syncthreads();
+    if (!whole) {
+      if (vq >= begun && vq + 4 <= end) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          store4(vt + (vd + j) * kBlock + vq, v4f{vx[0][j], vx[1][j], vx[2][j], vx[3][j]});
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (vq + r >= begun && vq + r < end)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) st_val(vt + (vd + j) * kBlock + vq + r, vx[r][j]);
+      }
+    }
   }
-  if (whole && tid == 0) c.step[ph] = make_float2(steps[0], steps[1]);
+  if (!whole) return;
+  // largest magnitudes; infinity stands for a value that is not finite
+  auto mag = [](float m, float x) { return fmaxf(m, fabsf(x) < INFINITY ? fabsf(x) : INFINITY); };
+  float mk = 0.0f, mv = 0.0f;
+#pragma unroll
+  for (int x = 0; x < KL; ++x)
+    if (KU % 256 == 0 || x * 256 + tid < KU)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) mk = mag(mag(mk, ka[x][j]), kb[x][j]);
+  if (VU == 256 || tid < VU)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) mv = mag(mv, vx[r][j]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    mk = fmaxf(mk, __shfl_xor(mk, o, 64));
+    mv = fmaxf(mv, __shfl_xor(mv, o, 64));
+  }
+  if ((tid & 63) == 0) {
+    red[tid >> 6][0] = mk;
+    red[tid >> 6][1] = mv;
+  }
+  __syncthreads();
+  float scale[2], step[2];
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    const float m = fmaxf(fmaxf(fmaxf(red[0][p], red[1][p]), fmaxf(red[2][p], red[3][p])), kStepFloor);
+    const bool fine = m < INFINITY;
+    scale[p] = fine ? 127.0f * __fdiv_rn(1.0f, m) : 0.0f;
+    step[p] = fine ? m * (1.0f / 127.0f) : __builtin_nanf("");
+  }
+  const bool k_fine = scale[0] > 0.0f, v_fine = scale[1] > 0.0f;
+  uint8_t* kp = (uint8_t*)page[0];
+  uint8_t* vp = (uint8_t*)page[1];
+#pragma unroll
+  for (int x = 0; x < KL; ++x) {
+    const int i = x * 256 + tid, t = i / PC, d = i % PC * 8;
+    if (KU % 256 != 0 && i >= KU) continue;
+    auto put = [&](const float (&f)[8], int e) __attribute__((always_inline)) {
+      uint2 w = make_uint2(0x80808080u, 0x80808080u);
+      if (k_fine)
+        w = make_uint2(code4(f[0], f[1], f[2], f[3], scale[0]), code4(f[4], f[5], f[6], f[7], scale[0]));
+      *(uint2*)(kp + key_at<HD>(t, e)) = w;
+    };
+    put(ka[x], d);
+    put(kb[x], d + HD / 2);
+  }
+  if (VU == 256 || tid < VU)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int at = value_at(vq, vd + j);
+      const uint32_t w = v_fine ? code4(vx[0][j], vx[1][j], vx[2][j], vx[3][j], scale[1]) : 0x80808080u;
+      *(uint32_t*)(vp + unit_at(at >> 4) * 16 + (at & 15)) = w;
+    }
+  __syncthreads();
+  const int64_t ph = c.page_head(layer, tail * c.max_blocks + blk, head);
+  uint4* ko = (uint4*)(c.kpage + ph * (kBlock * HD));
+  uint4* vo = (uint4*)(c.vpage + ph * (kBlock * HD));
+#pragma unroll
+  for (int i = tid; i < kBlock * HD / 16; i += 256) {
+    ko[i] = page[0][i];
+    vo[i] = page[1][unit_at(i)];
+  }
+  if (tid == 0) c.step[ph] = make_float2(step[0], step[1]);
 }
 
 __global__ void __launch_bounds__(64) k_cache_begin(CacheView c, int n, const int32_t* counts) {
@@ -298,38 +422,63 @@ __global__ void __launch_bounds__(256) k_reorder_table(CacheView c, const int32_
 }
 
 // ---------------------------------------------------------------------------
-// Values of a range of positions.  A work group takes up to 64 positions of one block of a head.
+// Values of a range of positions: grid blocks, heads, rows.  A thread takes 4 tokens x 8 dims: keys 8 bytes a
+// token, values 4 bytes a dim (from the caches after the first), 8 values a store.
 // ---------------------------------------------------------------------------
 template <typename T, int HD, typename O>
 __global__ void __launch_bounds__(256) k_cache_read(CacheView c, int layer, int64_t first, int64_t n,
                                                     O* ko, O* vo) {
-  const int head = blockIdx.y, row = blockIdx.z;
+  constexpr int VC = HD / 8;
+  const int head = blockIdx.y, row = blockIdx.z, tid = threadIdx.x;
   const int g = row / c.width;
   const int64_t slot = (int64_t)g * c.beams + row % c.width;
-  const int len = c.len[g], total = len + c.pend[g];
-  const int64_t blk = first / kBlock + blockIdx.x;
-  const int64_t lo = std::max(first, blk * kBlock),
-                hi = std::min(std::min(first + n, (blk + 1) * kBlock), (int64_t)total);
-  if (lo >= hi) return;
-  const bool coded = (blk + 1) * kBlock <= total;
-  const int64_t ph = c.page_head(layer, coded ? c.page_of(slot, blk, len) : 0, head);
-  const float2 d = coded ? c.step[ph] : make_float2(0.0f, 0.0f);
-  const int buf = c.sel[g] ^ (blk != len / kBlock);
-  const int64_t th = c.tail_head(layer, buf, c.tail_of[slot], head) * (kBlock * HD);
-  for (int64_t i = threadIdx.x; i < (hi - lo) * HD; i += 256) {
-    const int64_t pos = lo + i / HD;
-    const int t = (int)(pos - blk * kBlock), e = (int)(i % HD);
-    const int64_t out = (((int64_t)row * n + (pos - first)) * c.heads_kv + head) * HD + e;
-    float kx, vx;
-    if (coded) {
-      kx = (float)((int)c.kpage[ph * (kBlock * HD) + key_at<HD>(t, e)] - 128) * d.x;
-      vx = (float)((int)c.vpage[ph * (kBlock * HD) + value_at(t, e)] - 128) * d.y;
-    } else {
-      kx = ld_val((const T*)c.ktail + th + t * HD + e);
-      vx = ld_val((const T*)c.vtail + th + e * kBlock + t);
+  const int64_t tail = c.tail_of[slot];
+  const int len = c.len[g], total = len + c.pend[g], sel = c.sel[g];
+  const int64_t blk = first / kBlock + blockIdx.x, t0 = blk * kBlock;
+  const int64_t stop = std::min(first + n, (int64_t)total);
+  const int tq = tid / VC * 4, d = tid % VC * 8;
+  if (t0 >= stop || tid >= 16 * VC) return;
+  const bool coded = t0 + kBlock <= total;
+  const int64_t page = !coded ? 0 : blk < len / kBlock ? c.table[slot * c.max_blocks + blk] : tail * c.max_blocks + blk;
+  const int64_t ph = c.page_head(layer, page, head);
+  const int64_t th = c.tail_head(layer, sel ^ (blk != len / kBlock), tail, head) * (kBlock * HD);
+  const float2 step = coded ? c.step[ph] : make_float2(0.0f, 0.0f);
+  const int64_t rs = (int64_t)c.heads_kv * HD;
+  const int64_t base = ((int64_t)row * n + (t0 - first)) * rs + (int64_t)head * HD + d;
+  float kx[4][8], vx[4][8];
+  if (coded) {
+    const uint8_t* kp = c.kpage + ph * (kBlock * HD);
+    const uint8_t* vp = c.vpage + ph * (kBlock * HD);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const uint2 w = *(const uint2*)(kp + key_at<HD>(tq + r, d));
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        kx[r][j] = (float)((int)((j < 4 ? w.x : w.y) >> (8 * (j & 3)) & 255) - 128) * step.x;
     }
-    if (ko) st_val(ko + out, kx);
-    if (vo) st_val(vo + out, vx);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t w = *(const uint32_t*)(vp + value_at(tq, d + j));
+#pragma unroll
+      for (int r = 0; r < 4; ++r) vx[r][j] = (float)((int)(w >> (8 * r) & 255) - 128) * step.y;
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) load8((const T*)c.ktail + th + (tq + r) * HD + d, kx[r]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      float x[4];
+      load4((const T*)c.vtail + th + (d + j) * kBlock + tq, x);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) vx[r][j] = x[r];
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int64_t pos = t0 + tq + r;
+    if (pos < first || pos >= stop) continue;
+    if (ko) store8(ko + base + (tq + r) * rs, kx[r]);
+    if (vo) store8(vo + base + (tq + r) * rs, vx[r]);
   }
 }
 
@@ -356,8 +505,6 @@ __global__ void __launch_bounds__(256) k_cache_read(CacheView c, int layer, int6
 // ---------------------------------------------------------------------------
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
-typedef float v2f __attribute__((ext_vector_type(2)));
-typedef float v4f __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -406,42 +553,6 @@ __device__ __forceinline__ int exponent_of(float m) {
 __device__ __forceinline__ float finite_abs(float x) {
   const float a = fabsf(x);
   return a < INFINITY ? a : 0.0f;
-}
-
-__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
-  const float4 a = ((const float4*)p)[0], b = ((const float4*)p)[1];
-  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-}
-__device__ __forceinline__ void load8(const uint16_t* p, float (&v)[8]) {
-  const uint4 r = *(const uint4*)p;
-  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    v[2 * j] = __uint_as_float(w[j] << 16);
-    v[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
-  }
-}
-__device__ __forceinline__ void load4(const float* p, float* v) {
-  const float4 a = *(const float4*)p;
-  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-}
-__device__ __forceinline__ void load4(const uint16_t* p, float* v) {
-  const uint2 r = *(const uint2*)p;
-  v[0] = __uint_as_float(r.x << 16);
-  v[1] = __uint_as_float(r.x & 0xFFFF0000u);
-  v[2] = __uint_as_float(r.y << 16);
-  v[3] = __uint_as_float(r.y & 0xFFFF0000u);
-}
-__device__ __forceinline__ void store4(float* p, v4f v) {
-  *(float4*)p = make_float4(v[0], v[1], v[2], v[3]);
-}
-__device__ __forceinline__ void store4(uint16_t* p, v4f v) {
-  uint2 r;
-  r.x = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[0]) |
-        ((uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[1]) << 16);
-  r.y = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2]) |
-        ((uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[3]) << 16);
-  *(uint2*)p = r;
 }
 
 // Largest and sum over the four lanes of a column.
