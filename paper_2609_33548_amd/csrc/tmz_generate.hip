@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <cmath>
 #include <string>
+#include <type_traits>
 
 #include "tmz_device.h"
 #include "tmz_internal.h"
@@ -43,8 +44,7 @@ __global__ void __launch_bounds__(256) k_logits(const T* __restrict__ x, const T
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t m0 = (int64_t)(blockIdx.x % mtiles) * 16 * MT, t0 = (int64_t)(blockIdx.x / mtiles) * 16 * VT;
   const int64_t bytes = d * (int64_t)sizeof(T);
-  const int steps = (int)((bytes + 63) / 64), per = (steps + 3) / 4;
-  const int s0 = wave * per, s1 = s0 + per < steps ? s0 + per : steps;
+  const int whole = (int)(bytes / 64);                   // steps
   // rows past the end are read as the last one and not stored
   const char *xp[MT], *ep[VT];
 #pragma unroll
@@ -62,21 +62,30 @@ __global__ void __launch_bounds__(256) k_logits(const T* __restrict__ x, const T
   for (int i = 0; i < MT; ++i)
 #pragma unroll
     for (int j = 0; j < VT; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-  const int whole = (int)(bytes / 64) < s1 ? (int)(bytes / 64) : s1;
-  auto take = [&](int s) __attribute__((always_inline)) {
-    uint4 a[VT], b[MT];
+  // GS steps at a time, the waves in turn: all their loads first, a row's pieces next to each other
+  constexpr int GS = MT * VT >= 16 ? 2 : 4;
+  auto take = [&](int s, auto count) __attribute__((always_inline)) {
+    constexpr int C = decltype(count)::value;
+    uint4 a[VT][C], b[MT][C];
 #pragma unroll
-    for (int j = 0; j < VT; ++j) a[j] = *(const uint4*)(ep[j] + (int64_t)s * 64);
+    for (int j = 0; j < VT; ++j)
 #pragma unroll
-    for (int i = 0; i < MT; ++i) b[i] = *(const uint4*)(xp[i] + (int64_t)s * 64);
+      for (int u = 0; u < C; ++u) a[j][u] = *(const uint4*)(ep[j] + (int64_t)(s + u) * 64);
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
-      for (int j = 0; j < VT; ++j) acc[i][j] = logits_step<T>(a[j], b[i], acc[i][j]);
+      for (int u = 0; u < C; ++u) b[i][u] = *(const uint4*)(xp[i] + (int64_t)(s + u) * 64);
+#pragma unroll
+    for (int u = 0; u < C; ++u)
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < VT; ++j) acc[i][j] = logits_step<T>(a[j][u], b[i][u], acc[i][j]);
   };
-#pragma unroll 4
-  for (int s = s0; s < whole; ++s) take(s);
-  if (s0 <= whole && whole < s1) {                       // the last step is half a one
+  int s = wave * GS;
+  for (; s + GS <= whole; s += 4 * GS) take(s, std::integral_constant<int, GS>());
+  for (; s < whole; ++s) take(s, std::integral_constant<int, 1>());
+  if (wave == 0 && whole * 64 < bytes) {                 // the last step is half a one
     const bool in = (lane >> 4) * 16 < bytes - (int64_t)whole * 64;
     const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
     uint4 a[VT], b[MT];
@@ -114,8 +123,9 @@ template <typename T, int MT>
 static void logits_as(const T* x, const T* E, int64_t M, int64_t d, int64_t V, float* out, int n_cu,
                       hipStream_t s) {
   const int mt = (int)((M + 16 * MT - 1) / (16 * MT));
-  // 64 vocabulary rows a work group where that still makes two for every compute unit
-  if ((V + 63) / 64 * mt >= 2 * n_cu)
+  // 64 vocabulary rows a work group where that still makes one for every compute unit (M = 32, 32003 x 1536: 501
+  // work groups of 64 rows 24 us, 2001 of 16 rows 36)
+  if ((V + 63) / 64 * mt >= n_cu)
     hipLaunchKernelGGL((k_logits<T, MT, 4>), dim3((unsigned)((V + 63) / 64 * mt)), dim3(256), 0, s, x, E, M, d,
                        V, out, mt);
   else
@@ -141,14 +151,14 @@ hipError_t launch_logits(const void* x, const void* E, termezo_dtype dt, int64_t
 // ---------------------------------------------------------------------------
 // Beam selection in two launches.
 //
-// k_beam_scan reads the logits once, a wave 4096 of them at a time in registers, and leaves per wave the
-// largest and the sum of exp(x - largest), and the largest of every segment (16 .. 4096 logits).
+// k_beam_scan reads the logits once, a wave 1024 of them in registers, and leaves per wave the largest and
+// the sum of exp(x - largest), and the largest of every segment (16, 64, 256 or 1024 logits).
 // k_beam_pick, a work group per search, forms the beams' log-sum-exps (fp64) and the segments' best scores
-// score + x - lse (fp64).  A lower bound of the n_out-th best score is the n_out-th largest of the
-// maxima of 64 disjoint sets of segments: no continuation below it can be chosen, and only segments that reach
-// it are looked at again.  The few continuations found are ranked by counting; where they are many (many
-// equal logits) they are taken in rounds, best first.  Continuations of score -inf fill what
-// is left, lowest index first.  Bound by the bytes of the logits.
+// (score + x) - lse (fp64).  A lower bound of the n_out-th best score is the n_out-th largest of the
+// maxima of 64 disjoint sets of segments: no continuation below it can be chosen, and only segments that
+// reach it are looked at again.  The few continuations found are ranked by counting; where they are many
+// (many equal logits) they are taken in rounds, best first.  Continuations of score -inf fill what is left,
+// lowest index first.  The scan is bound by the bytes of the logits, the pick by its chain of reads.
 // ---------------------------------------------------------------------------
 struct BeamArgs {
   const float *logits, *scores;
@@ -166,7 +176,7 @@ struct BeamArgs {
   int32_t waves, segs, seg_shift;
 };
 
-constexpr int kScan = 4096;           // logits a wave
+constexpr int kScan = 1024;           // logits a wave
 
 struct __attribute__((packed, aligned(4))) Float4 {
   float v[4];
@@ -175,88 +185,96 @@ struct __attribute__((packed, aligned(4))) Float4 {
 // NaN counts as -inf, -0 as 0.
 __device__ __forceinline__ float clean_logit(float x) { return x == x ? x + 0.0f : -INFINITY; }
 
+// v of the lane that a data-parallel move names (quad permutation, rotation of 16 lanes).
+template <int CTRL>
+__device__ __forceinline__ float moved(float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xF, 0xF, false));
+}
+constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E, kTurn4 = 0x124, kTurn8 = 0x128;
+
+template <int SHIFT>
 __global__ void __launch_bounds__(256) k_beam_scan(BeamArgs a) {
   const int lane = threadIdx.x & 63, w = blockIdx.x * 4 + (threadIdx.x >> 6);
   const int64_t row = blockIdx.y;
   if (w >= a.waves || (a.finished && a.finished[row])) return;   // whole wave
   const float* x = a.logits + row * a.vocab;
   const int t0 = w * kScan + lane * 4;
-  float v[16][4];
+  float v[4][4], b[4];
+  if (w * kScan + kScan <= a.vocab) {                    // whole wave
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int t = t0 + i * 256;
-    if (t + 3 < a.vocab) {
-      const Float4 f = *(const Float4*)(x + t);
+    for (int i = 0; i < 4; ++i) {
+      const Float4 f = *(const Float4*)(x + t0 + i * 256);
 #pragma unroll
       for (int j = 0; j < 4; ++j) v[i][j] = f.v[j];
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v[i][j] = t + j < a.vocab ? x[t + j] : -INFINITY;
     }
-  }
-  float m = -INFINITY;
-  float* seg = a.seg + row * a.segs;
-  float run = -INFINITY;                                // of segments longer than 256
+  } else {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int t = t0 + i * 256 + j;
+        const float f = x[t < a.vocab ? t : a.vocab - 1];
+        v[i][j] = t < a.vocab ? f : -INFINITY;
+      }
+  }
+  float* seg = a.seg + row * a.segs;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[i][j] = clean_logit(v[i][j]);
-    float b = fmaxf(fmaxf(v[i][0], v[i][1]), fmaxf(v[i][2], v[i][3]));
-    m = fmaxf(m, b);
-    b = fmaxf(b, __shfl_xor(b, 1, 64));
-    b = fmaxf(b, __shfl_xor(b, 2, 64));
+    b[i] = fmaxf(fmaxf(v[i][0], v[i][1]), fmaxf(v[i][2], v[i][3]));
+    b[i] = fmaxf(b[i], moved<kSwap1>(b[i]));
+    b[i] = fmaxf(b[i], moved<kSwap2>(b[i]));
     const int t = t0 + i * 256;
-    if (a.seg_shift == 4) {
-      if (lane % 4 == 0 && t < a.vocab) seg[t >> 4] = b;
-      continue;
-    }
-    b = fmaxf(b, __shfl_xor(b, 4, 64));
-    b = fmaxf(b, __shfl_xor(b, 8, 64));
-    if (a.seg_shift == 6) {
-      if (lane % 16 == 0 && t < a.vocab) seg[t >> 6] = b;
-      continue;
-    }
-    b = fmaxf(b, __shfl_xor(b, 16, 64));
-    b = fmaxf(b, __shfl_xor(b, 32, 64));
-    run = fmaxf(run, b);
-    if (((i + 1) << 8 & ((1 << a.seg_shift) - 1)) == 0) {
-      const int first = (w * kScan + i * 256) >> a.seg_shift;
-      if (lane == 0 && (int64_t)first << a.seg_shift < a.vocab) seg[first] = run;
-      run = -INFINITY;
+    if (SHIFT == 4 && lane % 4 == 0 && t < a.vocab) seg[t >> 4] = b[i];
+    b[i] = fmaxf(b[i], moved<kTurn4>(b[i]));
+    b[i] = fmaxf(b[i], moved<kTurn8>(b[i]));
+    if (SHIFT == 6 && lane % 16 == 0 && t < a.vocab) seg[t >> 6] = b[i];
+    if (SHIFT == 8) {
+      b[i] = fmaxf(b[i], __shfl_xor(b[i], 16, 64));
+      b[i] = fmaxf(b[i], __shfl_xor(b[i], 32, 64));
+      if (lane == 0 && t < a.vocab) seg[t >> 8] = b[i];
     }
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  float m = fmaxf(fmaxf(b[0], b[1]), fmaxf(b[2], b[3]));
+  if (SHIFT != 8) {
+    m = fmaxf(m, __shfl_xor(m, 16, 64));
+    m = fmaxf(m, __shfl_xor(m, 32, 64));
+  }
+  if (SHIFT == 10 && lane == 0) seg[w] = m;
   const float ref = m == -INFINITY ? 0.0f : m;
   float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-  for (int i = 0; i < 16; ++i)
+  for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       s[j] += __builtin_amdgcn_exp2f((v[i][j] - ref) * 1.4426950408889634f);
-  double sum = (double)(s[0] + s[1]) + (double)(s[2] + s[3]);
+  float sum = (s[0] + s[1]) + (s[2] + s[3]);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-  if (lane == 0) a.part[row * a.waves + w] = make_float2(m, (float)sum);
+  if (lane == 0) a.part[row * a.waves + w] = make_float2(m, sum);
 }
 
-constexpr int kPickWaves = 8, kMaxList = 1024, kMaxCand = 512, kMaxOut = 64;
+constexpr int kPickWaves = 8, kPick = 64 * kPickWaves, kMaxList = 1024, kMaxCand = 512, kMaxOut = 64;
 
 __device__ __forceinline__ bool before(double v, int i, double w, int j) {
   return v > w || (v == w && i < j);
 }
 
-__global__ void __launch_bounds__(64 * kPickWaves) k_beam_pick(BeamArgs a) {
-  __shared__ double lse[64], lmax[kPickWaves][64], cv[kMaxCand], bound, rv[kPickWaves];
+__global__ void __launch_bounds__(kPick) k_beam_pick(BeamArgs a) {
+  __shared__ double lse[64], own[64], lmax[kPickWaves][64], cv[kMaxCand], bound, rv[kPickWaves];
   __shared__ int list[kMaxList], ci[kMaxCand], ri[kPickWaves], n_list, n_cand, pick[kMaxOut], n_pick;
   __shared__ float pv[kMaxOut];
+  __shared__ bool done[64];
   const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int W = a.beams, V = a.vocab, S = W * a.segs;
+  const int W = a.beams, V = a.vocab, segs = a.segs, shift = a.seg_shift, eos = a.eos;
   const int64_t row0 = (int64_t)g * W;
   if (tid == 0) n_list = n_cand = 0;
-  for (int b = wave; b < W; b += kPickWaves) {           // infinite: no continuations
-    double l = INFINITY;
-    if (!(a.finished && a.finished[row0 + b])) {
+  for (int b = wave; b < W; b += kPickWaves) {
+    const bool fin = a.finished && a.finished[row0 + b];
+    const float sc = a.scores[row0 + b];
+    double l = INFINITY;                                 // no continuations
+    if (!fin) {
       float m = -INFINITY;
       for (int i = lane; i < a.waves; i += 64) m = fmaxf(m, a.part[(row0 + b) * a.waves + i].x);
 #pragma unroll
@@ -271,32 +289,63 @@ __global__ void __launch_bounds__(64 * kPickWaves) k_beam_pick(BeamArgs a) {
       l = (double)m + log(s);
       if (!(l > -INFINITY && l < INFINITY)) l = INFINITY;
     }
-    if (lane == 0) lse[b] = l;
+    if (lane == 0) {
+      lse[b] = l;
+      own[b] = sc == sc ? (double)sc : -INFINITY;
+      done[b] = fin;
+    }
   }
   __syncthreads();
-  // score of a logit of beam b (not finished), NaN as -inf
-  auto score_of = [&](int b, float x) __attribute__((always_inline)) {
-    if (!(lse[b] < INFINITY)) return (double)-INFINITY;
-    const double v = (double)a.scores[row0 + b] + (double)x - lse[b];
+  // score of a logit of beam b; x (clean) is not looked at where the beam is finished: eos has its score
+  auto score = [&](int b, float x, bool is_eos) __attribute__((always_inline)) {
+    const double v = lse[b] < INFINITY ? (own[b] + (double)x) - lse[b] : -INFINITY;
+    if (done[b]) return is_eos ? own[b] : (double)-INFINITY;
     return v == v ? v : (double)-INFINITY;
   };
-  auto is_done = [&](int b) __attribute__((always_inline)) { return a.finished && a.finished[row0 + b]; };
-  auto own_score = [&](int b) __attribute__((always_inline)) {
-    const float s = a.scores[row0 + b];
-    return s == s ? (double)s : (double)-INFINITY;
+  // every segment's best, eight loads at a time: f(segment, score)
+  auto segments = [&](auto f) __attribute__((always_inline)) {
+    for (int j = tid; j < segs; j += kPick)
+      for (int b0 = 0; b0 < W; b0 += 8) {
+        float x[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) x[u] = a.seg[(row0 + (b0 + u < W ? b0 + u : W - 1)) * segs + j];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+          if (b0 + u < W) f((b0 + u) * segs + j, score(b0 + u, x[u], eos >> shift == j));
+      }
   };
-  // continuation (b, t)
-  auto element = [&](int b, int t) __attribute__((always_inline)) {
-    if (is_done(b)) return t == a.eos ? own_score(b) : (double)-INFINITY;
-    return score_of(b, clean_logit(a.logits[(row0 + b) * V + t]));
-  };
-  auto segment = [&](int s) __attribute__((always_inline)) {
-    const int b = s / a.segs, j = s % a.segs;
-    if (is_done(b)) return a.eos >> a.seg_shift == j ? own_score(b) : (double)-INFINITY;
-    return score_of(b, a.seg[(row0 + b) * a.segs + j]);
+  // all logits of listed segments, eight of a thread at a time: f(index, score)
+  auto elements = [&](int n, bool all, auto f) __attribute__((always_inline)) {
+    const int64_t total = (int64_t)n << shift;
+    for (int64_t e0 = (int64_t)tid * 4; e0 < total; e0 += 2 * 4 * kPick) {
+      float x[2][4];
+      int bb[2], tt[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int64_t e = e0 + u * 4 * kPick;
+        const int at = e < total ? (int)(e >> shift) : n - 1, s = all ? at : list[at];
+        bb[u] = s / segs;
+        tt[u] = ((s - bb[u] * segs) << shift) + (int)(e & ((1 << shift) - 1));
+        const float* row = a.logits + (row0 + bb[u]) * V;
+        if (tt[u] + 3 < V) {
+          const Float4 y = *(const Float4*)(row + tt[u]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[u][j] = y.v[j];
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[u][j] = row[tt[u] + j < V ? tt[u] + j : V - 1];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (e0 + u * 4 * kPick < total && tt[u] + j < V)
+            f(bb[u] * V + tt[u] + j, score(bb[u], clean_logit(x[u][j]), tt[u] + j == eos));
+    }
   };
   double best = -INFINITY;
-  for (int s = tid; s < S; s += 64 * kPickWaves) best = fmax(best, segment(s));
+  segments([&](int, double v) { best = fmax(best, v); });
   lmax[wave][lane] = best;
   __syncthreads();
   if (wave == 0) {
@@ -306,42 +355,40 @@ __global__ void __launch_bounds__(64 * kPickWaves) k_beam_pick(BeamArgs a) {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
     int rank = 0;
+#pragma unroll 16
     for (int i = 0; i < 64; ++i) rank += before(lmax[0][i], i, best, lane);
     if (rank == a.n_out - 1) bound = best;
   }
   __syncthreads();
   const double T = bound;
   auto wanted = [&](double v) __attribute__((always_inline)) { return v >= T && v > -INFINITY; };
-  for (int s = tid; s < S; s += 64 * kPickWaves)
-    if (wanted(segment(s))) {
+  segments([&](int s, double v) {
+    if (wanted(v)) {
       const int i = atomicAdd(&n_list, 1);
       if (i < kMaxList) list[i] = s;
     }
+  });
   __syncthreads();
-  const int nl = n_list <= kMaxList ? n_list : S;        // too many to list: all of them
-  auto listed = [&](int i) __attribute__((always_inline)) { return n_list <= kMaxList ? list[i] : i; };
-  const int len = 1 << a.seg_shift;
-  if (n_list <= kMaxList)
-    for (int i = wave; i < nl; i += kPickWaves) {
-      const int s = list[i], b = s / a.segs, t0 = (s % a.segs) << a.seg_shift;
-      for (int t = t0 + lane; t < t0 + len && t < V; t += 64) {
-        const double v = element(b, t);
-        if (wanted(v)) {
-          const int k = atomicAdd(&n_cand, 1);
-          if (k < kMaxCand) {
-            cv[k] = v;
-            ci[k] = b * V + t;
-          }
+  const bool all = n_list > kMaxList;                    // too many to list
+  const int nl = all ? W * segs : n_list;
+  if (!all)
+    elements(nl, false, [&](int x, double v) {
+      if (wanted(v)) {
+        const int k = atomicAdd(&n_cand, 1);
+        if (k < kMaxCand) {
+          cv[k] = v;
+          ci[k] = x;
         }
       }
-    }
+    });
   __syncthreads();
-  if (n_list <= kMaxList && n_cand <= kMaxCand) {
+  if (!all && n_cand <= kMaxCand) {
     const int nc = n_cand;
-    for (int i = tid; i < nc; i += 64 * kPickWaves) {
+    for (int i = tid; i < nc; i += kPick) {
       const double v = cv[i];
       const int x = ci[i];
       int rank = 0;
+#pragma unroll 8
       for (int j = 0; j < nc; ++j) rank += before(cv[j], ci[j], v, x);
       if (rank < a.n_out) {
         pick[rank] = x;
@@ -356,17 +403,12 @@ __global__ void __launch_bounds__(64 * kPickWaves) k_beam_pick(BeamArgs a) {
     for (; r < a.n_out; ++r) {
       double bv = -INFINITY;
       int bi = INT32_MAX;
-      for (int i = wave; i < nl; i += kPickWaves) {
-        const int s = listed(i), b = s / a.segs, t0 = (s % a.segs) << a.seg_shift;
-        for (int t = t0 + lane; t < t0 + len && t < V; t += 64) {
-          const double v = element(b, t);
-          const int x = b * V + t;
-          if (wanted(v) && before(lv, li, v, x) && before(v, x, bv, bi)) {
-            bv = v;
-            bi = x;
-          }
+      elements(nl, all, [&](int x, double v) {
+        if (wanted(v) && before(lv, li, v, x) && before(v, x, bv, bi)) {
+          bv = v;
+          bi = x;
         }
-      }
+      });
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) {
         const double v = __shfl_xor(bv, o, 64);
@@ -402,7 +444,11 @@ __global__ void __launch_bounds__(64 * kPickWaves) k_beam_pick(BeamArgs a) {
     int have = n_pick;
     for (int64_t x0 = 0; have < a.n_out && x0 < (int64_t)W * V; x0 += 64) {
       const int64_t x = x0 + lane;
-      const bool free = x < (int64_t)W * V && !(element((int)(x / V), (int)(x % V)) > -INFINITY);
+      bool free = x < (int64_t)W * V;
+      if (free) {
+        const int b = (int)(x / V), t = (int)(x % V);
+        free = !(score(b, clean_logit(a.logits[(row0 + b) * V + t]), t == eos) > -INFINITY);
+      }
       const unsigned long long mask = __ballot(free);
       const int at = have + __popcll(mask & ((1ull << lane) - 1));
       if (free && at < a.n_out) {
@@ -414,18 +460,19 @@ __global__ void __launch_bounds__(64 * kPickWaves) k_beam_pick(BeamArgs a) {
   }
   __syncthreads();
   const int64_t o0 = (int64_t)g * a.n_out;
-  for (int r = tid; r < a.n_out; r += 64 * kPickWaves) {
+  for (int r = tid; r < a.n_out; r += kPick) {
     const int b = pick[r] / V, t = pick[r] % V;
     a.out_scores[o0 + r] = pv[r];
     a.out_tokens[o0 + r] = t;
     a.out_parents[o0 + r] = b;
-    if (a.out_finished) a.out_finished[o0 + r] = is_done(b) || t == a.eos;
+    if (a.out_finished) a.out_finished[o0 + r] = done[b] || t == eos;
     if (a.out_history) a.out_history[(o0 + r) * (a.hist_len + 1) + a.hist_len] = t;
   }
   if (a.out_history)
     for (int r = wave; r < a.n_out; r += kPickWaves) {
       const int32_t* from = a.history + (row0 + pick[r] / V) * a.hist_len;
       int32_t* to = a.out_history + (o0 + r) * (a.hist_len + 1);
+#pragma unroll 4
       for (int64_t i = lane; i < a.hist_len; i += 64) to[i] = from[i];
     }
 }
@@ -484,7 +531,7 @@ termezo_status termezo_beam_select(termezo_ctx* c, const float* logits, const fl
   if (scope.err != hipSuccess) return hip_status(c, scope.err, "beam_select");
   // segments: as short as keeps a search at 4096 of them
   int shift = 4;
-  while (shift < 12 && (int64_t)beams * (((int64_t)vocab + (1 << shift) - 1) >> shift) > 4096) shift += 2;
+  while (shift < 10 && (int64_t)beams * (((int64_t)vocab + (1 << shift) - 1) >> shift) > 4096) shift += 2;
   const int segs = (int)(((int64_t)vocab + (1 << shift) - 1) >> shift);
   const int waves = (vocab + kScan - 1) / kScan;
   const int64_t rows = (int64_t)groups * beams, need = rows * (waves * 8 + (int64_t)segs * 4);
@@ -506,10 +553,15 @@ termezo_status termezo_beam_select(termezo_ctx* c, const float* logits, const fl
     if (p.finished) p.finished += r0;
     p.part += r0 * waves;
     p.seg += r0 * segs;
-    hipLaunchKernelGGL(k_beam_scan, dim3((unsigned)((waves + 3) / 4), (unsigned)std::min<int64_t>(65535, rows - r0)),
-                       dim3(256), 0, c->stream, p);
+    const dim3 grid((unsigned)((waves + 3) / 4), (unsigned)std::min<int64_t>(65535, rows - r0));
+    switch (shift) {
+      case 4: hipLaunchKernelGGL(k_beam_scan<4>, grid, dim3(256), 0, c->stream, p); break;
+      case 6: hipLaunchKernelGGL(k_beam_scan<6>, grid, dim3(256), 0, c->stream, p); break;
+      case 8: hipLaunchKernelGGL(k_beam_scan<8>, grid, dim3(256), 0, c->stream, p); break;
+      default: hipLaunchKernelGGL(k_beam_scan<10>, grid, dim3(256), 0, c->stream, p);
+    }
   }
-  hipLaunchKernelGGL(k_beam_pick, dim3((unsigned)groups), dim3(64 * kPickWaves), 0, c->stream, a);
+  hipLaunchKernelGGL(k_beam_pick, dim3((unsigned)groups), dim3(kPick), 0, c->stream, a);
   return hip_status(c, hipGetLastError(), "beam_select");
 }
 
