@@ -470,7 +470,7 @@ termezo_status termezo_kvcache_append(termezo_kvcache* cache, int32_t layer, con
  * h / (n_heads / n_kv_heads).  q, out: [rows][n][n_heads][head_dim] in act_dtype; rows'
  * queries from the pending count on are neither read nor written.  k and v, both or
  * neither: when given, they are appended first (termezo_kvcache_append), for one token
- * a row in the same launch.  counts: as in append; without k and v it may be NULL (the
+ * a row and up to 32 heads a key/value head in the same launch.  counts: as in append; without k and v it may be NULL (the
  * pending counts), and counts that differ from the pending ones, as pending counts above n,
  * raise a deferred INVALID_ARG and leave their group's rows out.  out must not overlap q,
  * k or v.  Errors: INVALID_ARG (as append; one of k, v null), STATE (k and v null and

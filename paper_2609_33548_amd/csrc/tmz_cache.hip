@@ -171,26 +171,28 @@ __device__ __forceinline__ uint32_t code4(float a, float b, float c, float d, fl
 // Where the unit of 16 bytes u of a values page lies in LDS.
 __device__ __forceinline__ int unit_at(int u) { return u ^ ((u >> 6 & 3) << 1 | (u >> 3 & 1)); }
 
+template <int HD>
+struct AppendShared {
+  uint4 page[2][kBlock * HD / 16];
+  float red[4][2];
+};
+
+// The nth block that a row's cnt new tokens touch.
 template <typename T, int HD>
-__global__ void __launch_bounds__(256) k_cache_append(CacheView c, int layer, const T* k, const T* v,
-                                                      int n, const int32_t* counts) {
+__device__ __forceinline__ void append_block(const CacheView& c, int layer, const T* k, const T* v, int n,
+                                             int row, int head, int64_t tail, int len, int buf, int cnt,
+                                             int nth, AppendShared<HD>& shared) {
   constexpr int PC = HD / 16, KU = kBlock * PC;          // pairs of pieces of a token, of a block
   constexpr int KL = (KU + 255) / 256;
   constexpr int VC = HD / 8, VU = 16 * VC;               // (4 tokens, 8 dims)
-  __shared__ uint4 page[2][kBlock * HD / 16];
-  __shared__ float red[4][2];
-  const int head = blockIdx.y, row = blockIdx.z, tid = threadIdx.x;
-  const int g = row / c.width;
-  const int64_t slot = (int64_t)g * c.beams + row % c.width;
-  const int64_t tail = c.tail_of[slot];
-  const int len = c.len[g], buf = c.sel[g], cnt = append_count(c, g, n, counts);
-  if (blockIdx.x == 0 && head == 0 && row % c.width == 0 && tid == 0) c.pend[g] = cnt;
-  const int64_t blk = len / kBlock + blockIdx.x;
+  auto& page = shared.page;
+  auto& red = shared.red;
+  const int tid = threadIdx.x;
+  const int64_t blk = len / kBlock + nth;
   const int64_t t0 = blk * kBlock;                       // first token of the block
-  if (cnt == 0 || t0 >= (int64_t)len + cnt) return;
-  const int begun = blockIdx.x == 0 ? len % kBlock : 0;  // tokens in the tail
+  const int begun = nth == 0 ? len % kBlock : 0;         // tokens in the tail
   const int end = (int)std::min<int64_t>((int64_t)len + cnt - t0, kBlock);
-  const int64_t th = c.tail_head(layer, blockIdx.x == 0 ? buf : buf ^ 1, tail, head) * (kBlock * HD);
+  const int64_t th = c.tail_head(layer, nth == 0 ? buf : buf ^ 1, tail, head) * (kBlock * HD);
   T* kt = (T*)c.ktail + th;
   T* vt = (T*)c.vtail + th;
   const bool whole = end == kBlock;
@@ -317,6 +319,19 @@ __global__ void __launch_bounds__(256) k_cache_append(CacheView c, int layer, co
     vo[i] = page[1][unit_at(i)];
   }
   if (tid == 0) c.step[ph] = make_float2(step[0], step[1]);
+}
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) k_cache_append(CacheView c, int layer, const T* k, const T* v,
+                                                      int n, const int32_t* counts) {
+  __shared__ AppendShared<HD> shared;
+  const int head = blockIdx.y, row = blockIdx.z;
+  const int g = row / c.width;
+  const int64_t tail = c.tail_of[(int64_t)g * c.beams + row % c.width];
+  const int len = c.len[g], buf = c.sel[g], cnt = append_count(c, g, n, counts);
+  if (blockIdx.x == 0 && head == 0 && row % c.width == 0 && threadIdx.x == 0) c.pend[g] = cnt;
+  if (cnt == 0 || (int64_t)(len / kBlock + blockIdx.x) * kBlock >= (int64_t)len + cnt) return;
+  append_block<T, HD>(c, layer, k, v, n, row, head, tail, len, buf, cnt, blockIdx.x, shared);
 }
 
 __global__ void __launch_bounds__(64) k_cache_begin(CacheView c, int n, const int32_t* counts) {
@@ -861,26 +876,43 @@ __device__ __forceinline__ void store_columns(const Running<HD, NT>& run, T* out
 }
 
 // grid: splits, key/value heads, rows.  A wave takes every fourth block of its work group's share.
-template <typename T, int HD, int NT>
+// APPEND (n = 1): the rows' new tokens are appended first, each by the work group that takes the block it
+// falls into.
+template <typename T, int HD, int NT, bool APPEND>
 __global__ void __launch_bounds__(256, NT == 1 ? kRowsResident1 : kRowsResident2)
-    k_attend_rows(CacheView c, int layer, const T* q, T* out, int n,
-                                                     const int32_t* counts, int heads, float scale,
-                                                     float* part) {
+    k_attend_rows(CacheView c, int layer, const T* q, const T* k, const T* v, T* out, int n,
+                  const int32_t* counts, int heads, float scale, float* part) {
   constexpr int NS = sizeof(T) == 2 ? 1 : 2, NC = 16 * NT;
-  __shared__ float lo[2][NC][HD + 4];
-  __shared__ float lm[2][NC], ll[2][NC];
+  struct Joining {
+    float o[2][NC][HD + 4], m[2][NC], l[2][NC];
+  };
+  __shared__ union {
+    Joining join;
+    AppendShared<HD> append;
+  } shared;
+  auto& lo = shared.join.o;
+  auto& lm = shared.join.m;
+  auto& ll = shared.join.l;
   const int head = blockIdx.y, row = blockIdx.z, lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = row / c.width;
-  const int cnt = query_count(c, g, n, counts);
-  if (cnt == 0) return;
   const int64_t slot = (int64_t)g * c.beams + row % c.width;
-  const int len = c.len[g], total = len + cnt;
+  const int64_t tail = c.tail_of[slot];
+  const int len = c.len[g], sel = c.sel[g];
+  const int cnt = APPEND ? append_count(c, g, n, counts) : query_count(c, g, n, counts);
+  if (APPEND && blockIdx.x == 0 && head == 0 && row % c.width == 0 && threadIdx.x == 0) c.pend[g] = cnt;
+  if (cnt == 0) return;
+  const int total = len + cnt;
   const int G = heads / c.heads_kv, cols = cnt * G;
   const int full = total / kBlock, items = (total + kBlock - 1) / kBlock;
   const int per = blocks_per_split(items, gridDim.x);
   const int i0 = blockIdx.x * per, i1 = i0 + per < items ? i0 + per : items;
   if (i0 >= i1) return;
+  if (APPEND && i1 == items) {                           // the new token's block is the last one
+    append_block<T, HD>(c, layer, k, v, n, row, head, tail, len, sel, cnt, 0, shared.append);
+    __threadfence_block();
+    __syncthreads();
+  }
   v8h qf[NT][HD / 32][NS];
   float qs[NT];
   int pos[NT];
@@ -927,7 +959,7 @@ __global__ void __launch_bounds__(256, NT == 1 ? kRowsResident1 : kRowsResident2
     });
   }
   if (i1 > full && wave * 16 < total - full * kBlock) {  // a wave, 16 of the tokens behind
-    const int64_t th = c.tail_head(layer, c.sel[g] ^ (full != len / kBlock), c.tail_of[slot], head) * (kBlock * HD);
+    const int64_t th = c.tail_head(layer, sel ^ (full != len / kBlock), tail, head) * (kBlock * HD);
     take_tail<T, HD, NT, NS>((const T*)c.ktail + th, (const T*)c.vtail + th, wave * 16,
                              total - full * kBlock, qf, qs, pos, full * kBlock, run);
   }
@@ -1233,29 +1265,34 @@ hipError_t cache_append_on(termezo_kvcache* c, int layer, const void* k, const v
 hipError_t cache_attention_on(termezo_kvcache* c, int layer, const void* q, const void* k,
                               const void* v, int64_t n, const int32_t* counts, void* out,
                               hipStream_t s) {
-  if (k) {
+  const int64_t group = c->cfg.n_heads / c->cfg.n_kv_heads;
+  if (k && (n > 1 || group > 32)) {
     const hipError_t e = cache_append_on(c, layer, k, v, n, counts, s);
     if (e != hipSuccess) return e;
+    k = nullptr;
     counts = nullptr;                                  // attention takes the pending counts
   }
   const CacheView w = view_of(c);
   const int H = c->cfg.n_heads, Hkv = c->cfg.n_kv_heads;
   const float scale = (float)(1.0 / std::sqrt((double)c->cfg.head_dim));
-  const int64_t cols = n * (H / Hkv), rows = rows_of(c);
+  const int64_t cols = n * group, rows = rows_of(c);
   if (cols <= 32) {
     const int nt = cols <= 16 ? 1 : 2;
     const int splits = token_splits(c, rows * Hkv, nt == 1 ? kRowsResident1 : kRowsResident2);
     const dim3 grid((unsigned)splits, (unsigned)Hkv, (unsigned)rows);
-#define TMZ_CALL(T, HD)                                                                         \
-  if (nt == 1)                                                                                  \
-    hipLaunchKernelGGL((k_attend_rows<T, HD, 1>), grid, dim3(256), 0, s, w, layer, (const T*)q,  \
-                       (T*)out, (int)n, counts, H, scale, c->part);                             \
-  else                                                                                          \
-    hipLaunchKernelGGL((k_attend_rows<T, HD, 2>), grid, dim3(256), 0, s, w, layer, (const T*)q,  \
-                       (T*)out, (int)n, counts, H, scale, c->part);                             \
-  if (splits > 1) join<T, HD>(c, w, (T*)out, (int)n, counts, splits, 16 * nt, 1, s)
+#define TMZ_ROWS(T, HD, NT, APPEND)                                                            \
+  hipLaunchKernelGGL((k_attend_rows<T, HD, NT, APPEND>), grid, dim3(256), 0, s, w, layer,       \
+                     (const T*)q, (const T*)k, (const T*)v, (T*)out, (int)n, counts, H, scale, c->part)
+#define TMZ_CALL(T, HD)                                                                        \
+  if (nt == 1) {                                                                               \
+    if (k) TMZ_ROWS(T, HD, 1, true); else TMZ_ROWS(T, HD, 1, false);                           \
+  } else {                                                                                     \
+    if (k) TMZ_ROWS(T, HD, 2, true); else TMZ_ROWS(T, HD, 2, false);                           \
+  }                                                                                            \
+  if (splits > 1) join<T, HD>(c, w, (T*)out, (int)n, k ? nullptr : counts, splits, 16 * nt, 1, s)
     TMZ_CACHE_TYPES(c, TMZ_CALL)
 #undef TMZ_CALL
+#undef TMZ_ROWS
     return hipGetLastError();
   }
   const int tiles = (int)((cols + kTileCols - 1) / kTileCols);

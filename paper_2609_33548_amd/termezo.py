@@ -152,15 +152,12 @@ def _dtype_code(t) -> int:
     raise TypeError(f"unsupported dtype {t.dtype}")
 
 
-def _tensor(t, name, shape, dtypes, device):
-    """Device address of a contiguous tensor of one of the given types; None in shape: any size."""
-    dtypes = dtypes if isinstance(dtypes, tuple) else (dtypes,)
-    if (t.dtype not in dtypes or t.dim() != len(shape) or not t.is_contiguous() or t.device != device
-            or any(s is not None and s != n for s, n in zip(shape, t.shape))):
-        want = "x".join("*" if s is None else str(s) for s in shape)
-        raise ValueError(f"{name} must be a contiguous {'/'.join(str(d) for d in dtypes)} tensor "
-                         f"[{want}] on {device}, not {t.dtype} {tuple(t.shape)} on {t.device}")
-    return int(t.data_ptr())
+def _tensor(t, name, shape, dtype, device):
+    """Device address of a contiguous tensor of that shape, type and device."""
+    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on {device}, not "
+                         f"{t.dtype} {list(t.shape)} on {t.device}")
+    return t.data_ptr()
 
 
 def _stream_handle(stream) -> Optional[int]:
@@ -403,13 +400,13 @@ class Context:
         """out[m, t] = x[m] . embedding[t]: x [M, d] and embedding [vocab, d] in fp32 or bf16, out
         fp32 [M, vocab]."""
         import torch
-        types = (torch.float32, torch.bfloat16)
+        code = _dtype_code(x)
         M, d = x.shape
         V = embedding.shape[0]
-        px = _tensor(x, "x", (M, d), types, self.device)
+        px = _tensor(x, "x", (M, d), x.dtype, self.device)
         pe = _tensor(embedding, "embedding", (V, d), x.dtype, self.device)
         po = _tensor(out, "out", (M, V), torch.float32, self.device)
-        self._check(_lib.termezo_logits(self.handle, px, pe, _dtype_code(x), M, d, V, po), "logits")
+        self._check(_lib.termezo_logits(self.handle, px, pe, code, M, d, V, po), "logits")
 
     def beam_select(self, logits, scores, out_scores, out_tokens, out_parents, eos: int = -1,
                     finished=None, out_finished=None, history=None, out_history=None):
@@ -465,16 +462,17 @@ class KVCache:
         return None if counts is None else _tensor(counts, "counts", (self.groups,), torch.int32,
                                                    self.ctx.device)
 
-    def _heads(self, t, name, heads, n=None):
-        return _tensor(t, name, (self.rows, n, heads, self.head_dim), self.dtype, self.ctx.device)
+    def _heads(self, t, name, heads, n):
+        return _tensor(t, name, (self.groups * self._width, n, heads, self.head_dim), self.dtype,
+                       self.ctx.device)
 
     def append(self, layer: int, k, v, counts=None):
         """k, v [rows, n, n_kv_heads, head_dim]: the first counts[g] (None: n) tokens of every row
         become pending in one layer."""
         n = k.shape[1]
         self.ctx._check(_lib.termezo_kvcache_append(
-            self.handle, layer, self._heads(k, "k", self.n_kv_heads), self._heads(v, "v", self.n_kv_heads, n),
-            n, self._counts(counts)), "kvcache_append")
+            self.handle, layer, self._heads(k, "k", self.n_kv_heads, n),
+            self._heads(v, "v", self.n_kv_heads, n), n, self._counts(counts)), "kvcache_append")
 
     def attention(self, layer: int, q, out, k=None, v=None, counts=None):
         """Causal attention of the pending tokens' queries q [rows, n, n_heads, head_dim] into out
@@ -482,7 +480,7 @@ class KVCache:
         n = q.shape[1]
         opt = lambda t, name: None if t is None else self._heads(t, name, self.n_kv_heads, n)
         self.ctx._check(_lib.termezo_kvcache_attention(
-            self.handle, layer, self._heads(q, "q", self.n_heads), opt(k, "k"), opt(v, "v"), n,
+            self.handle, layer, self._heads(q, "q", self.n_heads, n), opt(k, "k"), opt(v, "v"), n,
             self._counts(counts), self._heads(out, "out", self.n_heads, n)), "kvcache_attention")
 
     def advance(self):

@@ -126,7 +126,7 @@ def test_binding_refuses_wrong_tensors():
     from paper_2609_33548_amd import termezo as T
     dev = torch.device("cpu")
     x = torch.zeros(2, 3, 4)
-    assert T._tensor(x, "x", (2, None, 4), torch.float32, dev) == x.data_ptr()
+    assert T._tensor(x, "x", (2, 3, 4), torch.float32, dev) == x.data_ptr()
     for bad in (x.double(), x[0], x.transpose(0, 1), x[:, :, :2], torch.zeros(2, 3, 5)):
         with pytest.raises(ValueError, match="x must be"):
             T._tensor(bad, "x", (2, 3, 4), torch.float32, dev)
