@@ -508,8 +508,8 @@ __global__ void __launch_bounds__(256) k_cache_read(CacheView c, int layer, int6
 // Codes are exact in fp16: a byte u beside 0x64 is the fp16 number 1024 + u, less 1152 is q.  A query
 // is scaled by a power of two to a largest magnitude in [512, 1024) and rounded to fp16 (2^-11; one
 // rounding less than the bf16 that the rotated query would be stored in); fp32 activations take it in
-// two parts (2^-22).  Probabilities are scaled by 2^15 and rounded to fp16, again in two parts for
-// fp32.  Maxima, sums and outputs are fp32.  O is kept in units of the largest step of the values so
+// two parts (2^-22).  Probabilities are scaled to at most 2^15 and rounded to fp16, again in two parts
+// for fp32.  Maxima, sums and outputs are fp32.  O is kept in units of the largest step of the values so
 // far (Lv): a block's probabilities take the ratio of its step to that one.  The newest tokens, not
 // coded yet, pass the same way: scaled by powers of two to magnitudes below 128, bf16 values are exact in
 // fp16 and fp32 ones taken in two parts.
@@ -630,13 +630,17 @@ struct Running {
   float unit;                         // of o: the largest step of the values so far (0: none)
 };
 
+template <int NS>
+constexpr float kScaleBits = NS == 1 ? 7.0f : 15.0f;
+
 // Takes TT tiles of 16 tokens in (a block: 4): s[j][t] the products of column tile j with tokens
 // 16 t + 4 (lane / 16) + r, step their steps, qf the columns' factors, last[j] the last of the tokens that the
 // column sees (hidden: some column does not see them all), bad the lane's tokens whose values are not
 // finite, values(d, h, part) the operand of dims 16 d .. and tokens 32 h ...  NV: parts of the values,
 // NS: parts of the probabilities.
 //
-// The weights exp2(s f - max + 15) take the ratio of the values' step to the unit of o as a summand of the
+// The weights exp2(s f - m + bits): m is a column's running maximum (fp32 activations, bits 15), or
+// lags behind it by up to 8 (bf16, bits 7: at most 2^15 either way), so that o is seldom rescaled.  They take the ratio of the values' step to the unit of o as a summand of the
 // exponent (a fused multiply-add a score either way), and their sum takes its inverse.
 template <int TT, int HD, int NT, int NS, int NV, typename Values>
 __device__ __forceinline__ void take_tokens(Running<HD, NT>& run, v4f (&s)[NT][TT], float2 step,
@@ -679,12 +683,13 @@ __device__ __forceinline__ void take_tokens(Running<HD, NT>& run, v4f (&s)[NT][T
     for (int t = 0; t < TT; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) bm = fmaxf(bm, s[j][t][r]);
-    const float m = fmaxf(run.m[j], col_max(bm) * f);
+    bm = col_max(bm) * f;
+    const float m = bm > run.m[j] + (15.0f - kScaleBits<NS>) ? bm : run.m[j];
     const float ref = m == -INFINITY ? 0.0f : m;
     al[j] = __builtin_amdgcn_exp2f(run.m[j] - ref);
     run.m[j] = m;
     same = same && al[j] == 1.0f;
-    const float off = (15.0f + lr) - ref;
+    const float off = (kScaleBits<NS> + lr) - ref;
     float sum = 0.0f;
 #pragma unroll
     for (int h = 0; h < HH; ++h) {
@@ -693,9 +698,15 @@ __device__ __forceinline__ void take_tokens(Running<HD, NT>& run, v4f (&s)[NT][T
       for (int r = 0; r < 8; ++r) {
         w[r] = 2 * h + r / 4 < TT ? __builtin_amdgcn_exp2f(fmaf(s[j][2 * h + r / 4 < TT ? 2 * h + r / 4 : 0][r % 4], f, off))
                                   : 0.0f;
-        sum += w[r];
+        if (NS == 2) sum += w[r];
       }
       split_f16<NS>(w, p[j][h]);
+      if (NS == 1) {                                     // the sum of the weights as rounded
+        const v2h one = {(_Float16)1.0f, (_Float16)1.0f};
+#pragma unroll
+        for (int r = 0; r < 8; r += 2)
+          sum = __builtin_amdgcn_fdot2(v2h{p[j][h][0][r], p[j][h][0][r + 1]}, one, sum, false);
+      }
     }
     run.l[j] = fmaf(sum, inverse, run.l[j] * al[j]);
     al[j] *= shrink;

@@ -7,9 +7,10 @@ rounding of q (2^-11 for bf16, whose queries are rounded to fp16 after their rot
 whose queries are taken in two parts); the hd terms are summed in fp32.  Weights move by a factor within
 exp(+-2 ds), are rounded by 2^-11 (bf16) or 2^-21 (fp32) themselves, and are summed in fp32 over T
 tokens; the result is rounded to its type.  So |error| <= half a step of |o| + (2 ds + w +
-(T + 64) 2^-24 + 2^-20) sum p|v| + T 2^-40 max|v|, 2^-20 for the exponentials.  The last term is that of
-weights too small for their type: the largest weight is 2^15 in fp16, whose smallest step is 2^-24, so a
-weight is off by at most 2^-25 2^-15 = 2^-40 of the largest one, which the sum of all is no less than."""
+(T + 64) 2^-24 + 2^-20) sum p|v| + T 2^-40 (bf16: 2^-32) max|v|, 2^-20 for the exponentials.  The last term is that of
+weights too small for their type: the largest weight is 2^15 in fp16 (bf16: at least 2^7, the maximum may
+lag by 2^8), whose smallest step is 2^-24, so a weight is off by at most 2^-25 2^-15 = 2^-40 (bf16: 2^-32) of
+the largest one, which the sum of all is no less than."""
 import numpy as np
 import pytest
 
@@ -79,7 +80,7 @@ def _check_attention(ref_seq, q, got, bf16):
     ds = (u + hd * 2.0 ** -24) * big
     tol = (2.0 ** -8 if bf16 else 2.0 ** -24) * np.abs(out) \
         + (np.expm1(2 * ds) + u + (T + 64) * 2.0 ** -24 + 2.0 ** -20) * mag \
-        + T * 2.0 ** -40 * np.abs(ref_seq.values()[1]).max() + 1e-37
+        + T * 2.0 ** (-32 if bf16 else -40) * np.abs(ref_seq.values()[1]).max() + 1e-37
     err = np.abs(got.astype(np.float64) - out)
     assert (err <= tol).all(), (float((err / tol).max()), np.unravel_index((err / tol).argmax(), err.shape))
 
