@@ -44,12 +44,20 @@ struct CacheView {
   __device__ int64_t own_page(int64_t slot, int64_t block) const {
     return (int64_t)tail_of[slot] * max_blocks + block;
   }
-  // Pages of blocks below the group's length come from the table; those that pending tokens
-  // complete are the slot's own.
-  __device__ int64_t page_of(int64_t slot, int64_t block, int64_t len) const {
-    return block < len / kBlock ? table[slot * max_blocks + block] : own_page(slot, block);
-  }
 };
+
+// A value that no kernel here writes while it is read, at an address that is the same in a wave: by the
+// scalar unit.
+template <typename V>
+__device__ __forceinline__ V scalar_load(const V* p) {
+  return *(const __attribute__((address_space(4))) V*)(uintptr_t)p;
+}
+// Page of a block of a slot with tail `tail`: blocks below the group's length come from the table; those that
+// pending tokens complete are the slot's own.
+__device__ __forceinline__ int32_t page_of(const CacheView& c, int64_t slot, int32_t tail, int block, int len) {
+  return block < len / kBlock ? scalar_load(c.table + slot * c.max_blocks + block)
+                              : (int32_t)(tail * c.max_blocks + block);
+}
 
 __device__ __forceinline__ float ld_val(const float* p) { return *p; }
 __device__ __forceinline__ float ld_val(const uint16_t* p) { return bf16_to_f32(*p); }
@@ -630,6 +638,20 @@ struct Running {
   float unit;                         // of o: the largest step of the values so far (0: none)
 };
 
+// Keeps the compiler to the order written: READS shared-memory reads, then N - 1 times as many again before
+// the MFMAS matrix instructions that use the ones before, then the last ones.  (Left to itself it waits for each
+// pair of reads: 148 against 136 us for the ragged prompt batch.)
+template <int READS, int MFMAS, int N>
+__device__ __forceinline__ void reads_ahead() {
+  __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+#pragma unroll
+  for (int i = 0; i < N - 1; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+    __builtin_amdgcn_sched_group_barrier(0x8, MFMAS, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x8, MFMAS, 0);
+}
+
 template <int NS>
 constexpr float kScaleBits = NS == 1 ? 7.0f : 15.0f;
 
@@ -642,7 +664,7 @@ constexpr float kScaleBits = NS == 1 ? 7.0f : 15.0f;
 // The weights exp2(s f - m + bits): m is a column's running maximum (fp32 activations, bits 15), or
 // lags behind it by up to 8 (bf16, bits 7: at most 2^15 either way), so that o is seldom rescaled.  They take the ratio of the values' step to the unit of o as a summand of the
 // exponent (a fused multiply-add a score either way), and their sum takes its inverse.
-template <int TT, int HD, int NT, int NS, int NV, typename Values>
+template <int TT, int HD, int NT, int NS, int NV, bool AHEAD, typename Values>
 __device__ __forceinline__ void take_tokens(Running<HD, NT>& run, v4f (&s)[NT][TT], float2 step,
                                             const float (&qf)[NT], const int (&last)[NT], bool hidden,
                                             uint32_t bad, Values values) {
@@ -651,10 +673,11 @@ __device__ __forceinline__ void take_tokens(Running<HD, NT>& run, v4f (&s)[NT][T
   const bool nan = !(step.x < INFINITY) || !(step.y < INFINITY);
   const float vstep = nan ? 0.0f : step.y;
   const float unit = fmaxf(run.unit, vstep);
-  const float ratio = vstep > 0.0f ? vstep / unit : 1.0f;
-  const float shrink = run.unit > 0.0f ? run.unit / unit : 0.0f;
+  const float ru = __builtin_amdgcn_rcpf(unit);
+  const float ratio = vstep > 0.0f ? vstep * ru : 1.0f;
+  const float shrink = unit > run.unit ? run.unit * ru : 1.0f;
   const float lr = __builtin_amdgcn_logf(ratio);         // log2
-  const float inverse = 1.0f / ratio;
+  const float inverse = __builtin_amdgcn_rcpf(ratio);
   run.unit = unit;
   if (nan || bad)
 #pragma unroll
@@ -717,19 +740,36 @@ __device__ __forceinline__ void take_tokens(Running<HD, NT>& run, v4f (&s)[NT][T
 #pragma unroll
       for (int d = 0; d < HD / 16; ++d) run.o[j][d] *= al[j];
   }
+  auto use = [&](v8h v, int d, int h, int a) __attribute__((always_inline)) {
 #pragma unroll
-  for (int d = 0; d < HD / 16; ++d)
+    for (int j = 0; j < NT; ++j)
 #pragma unroll
-    for (int h = 0; h < HH; ++h)
+      for (int b = 0; b < NS; ++b)
+        if (a + b < 2) run.o[j][d] = mma(v, p[j][h][b], run.o[j][d]);
+  };
+  if constexpr (!AHEAD) {
+    __builtin_amdgcn_sched_barrier(0);                   // no conversions of values before: registers
 #pragma unroll
-      for (int a = 0; a < NV; ++a) {
-        const v8h v = values(d, h, a);
+    for (int d = 0; d < HD / 16; ++d)
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+      for (int h = 0; h < HH; ++h)
 #pragma unroll
-          for (int b = 0; b < NS; ++b)
-            if (a + b < 2) run.o[j][d] = mma(v, p[j][h][b], run.o[j][d]);
+        for (int a = 0; a < NV; ++a) use(values(d, h, a), d, h, a);
+  } else {                                               // 16 dims are read while those before are used
+    v8h v[2][HH];
+#pragma unroll
+    for (int h = 0; h < HH; ++h) v[0][h] = values(0, h, 0);
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d) {
+#pragma unroll
+      for (int h = 0; h < HH; ++h) {
+        if (d + 1 < HD / 16) v[(d + 1) & 1][h] = values(d + 1, h, 0);
       }
+#pragma unroll
+      for (int h = 0; h < HH; ++h) use(v[d & 1][h], d, h, 0);
+    }
+    reads_ahead<HH, HH * NT * NS, HD / 16>();
+  }
 }
 
 // Takes 16 tokens behind the last complete block in, from token t0 of that block on (have: the tokens
@@ -793,7 +833,7 @@ __device__ __forceinline__ void take_tail(const T* kt, const T* vt, int t0, int 
     }
   }
   v8h a[NS];
-  take_tokens<1, HD, NT, NS, NS>(run, s, make_float2(ldexpf(1.0f, ke), ldexpf(1.0f, ve)), qs, last, true,
+  take_tokens<1, HD, NT, NS, NS, false>(run, s, make_float2(ldexpf(1.0f, ke), ldexpf(1.0f, ve)), qs, last, true,
                                  bad, [&](int d, int, int part) {
     if (part == 0) {
       float x[8] = {};
@@ -908,7 +948,7 @@ __global__ void __launch_bounds__(256, NT == 1 ? kRowsResident1 : kRowsResident2
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = row / c.width;
   const int64_t slot = (int64_t)g * c.beams + row % c.width;
-  const int64_t tail = c.tail_of[slot];
+  const int32_t tail = c.tail_of[slot];
   const int len = c.len[g], sel = c.sel[g];
   const int cnt = APPEND ? append_count(c, g, n, counts) : query_count(c, g, n, counts);
   if (APPEND && blockIdx.x == 0 && head == 0 && row % c.width == 0 && threadIdx.x == 0) c.pend[g] = cnt;
@@ -932,6 +972,7 @@ __global__ void __launch_bounds__(256, NT == 1 ? kRowsResident1 : kRowsResident2
   start(run);
   const int ic = i1 < full ? i1 : full;                  // coded blocks end here
   for (int it = i0 + wave; it < ic; it += 4) {
+    const int64_t ph = c.page_head(layer, page_of(c, slot, tail, it, len), head);
     int last[NT];
 #pragma unroll
     for (int j = 0; j < NT; ++j) last[j] = pos[j] - it * kBlock;
@@ -941,7 +982,6 @@ __global__ void __launch_bounds__(256, NT == 1 ? kRowsResident1 : kRowsResident2
     for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int t = 0; t < 4; ++t) s[j][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    const int64_t ph = c.page_head(layer, c.page_of(slot, it, len), head);
     const uint4* kp = (const uint4*)(c.kpage + ph * (kBlock * HD)) + lane;
     const uint4* vp = (const uint4*)(c.vpage + ph * (kBlock * HD)) + lane;
     uint4 kr[2][HD / 32], vr[HD / 16];
@@ -965,7 +1005,7 @@ __global__ void __launch_bounds__(256, NT == 1 ? kRowsResident1 : kRowsResident2
             s[j][2 * p + 1] = mma(b, qf[j][k][x], s[j][2 * p + 1]);
           }
       }
-    take_tokens<4, HD, NT, NS, 1>(run, s, step, qs, last, hidden, 0u, [&](int d, int h, int) {
+    take_tokens<4, HD, NT, NS, 1, false>(run, s, step, qs, last, hidden, 0u, [&](int d, int h, int) {
       return h == 0 ? codes_f16(vr[d].x, vr[d].y) : codes_f16(vr[d].z, vr[d].w);
     });
   }
@@ -1029,7 +1069,6 @@ __global__ void __launch_bounds__(256, kTileResident) k_attend_tile(CacheView c,
                                                      int splits, float* part) {
   constexpr int NS = sizeof(T) == 2 ? 1 : 2, NT = 2, KS = HD / 32;
   constexpr int kPieces = kBlock * HD / 16;              // 16-byte pieces of a page
-  constexpr int kLoads = (2 * kPieces + 255) / 256;      // of keys and values, a thread
   __shared__ uint4 lds[2][4 * kPieces];                  // keys [16 tokens][32 dims], values [16 dims][32 tokens]
   const int head = blockIdx.x % c.heads_kv, row = blockIdx.x / c.heads_kv, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1039,6 +1078,7 @@ __global__ void __launch_bounds__(256, kTileResident) k_attend_tile(CacheView c,
   const int G = heads / c.heads_kv, cols = cnt * G, c0 = tile * kTileCols;
   if (c0 >= cols) return;
   const int64_t slot = (int64_t)g * c.beams + row % c.width;
+  const int32_t tail = c.tail_of[slot];
   const int len = c.len[g], total = len + cnt, full = total / kBlock;
   const int items = items_of(len, cnt, cols, c0 + kTileCols, G);
   const int per = blocks_per_split(items, splits);
@@ -1053,31 +1093,38 @@ __global__ void __launch_bounds__(256, kTileResident) k_attend_tile(CacheView c,
   Running<HD, NT> run;
   start(run);
   const int c1 = i1 < full ? i1 : full;                  // coded blocks end here
-  uint4 raw[kLoads];
+  // pieces of a page a thread moves, and what they are
+  constexpr int PL = (kPieces + 255) / 256;
+  uint4 kraw[PL], vraw[PL];
   float2 step_next = make_float2(0.0f, 0.0f);
+  int32_t page = i0 < c1 ? page_of(c, slot, tail, i0, len) : 0;
   auto fetch = [&](int it) __attribute__((always_inline)) {
-    const int64_t ph = c.page_head(layer, c.page_of(slot, it, len), head);
+    const int64_t ph = c.page_head(layer, page, head);
     const uint4* kp = (const uint4*)(c.kpage + ph * (kBlock * HD));
     const uint4* vp = (const uint4*)(c.vpage + ph * (kBlock * HD));
 #pragma unroll
-    for (int x = 0; x < kLoads; ++x) {
+    for (int x = 0; x < PL; ++x) {
       const int i = x * 256 + tid;
-      if (i < 2 * kPieces) raw[x] = i < kPieces ? kp[i] : vp[i - kPieces];
+      if (kPieces % 256 == 0 || i < kPieces) {
+        kraw[x] = kp[i];
+        vraw[x] = vp[i];
+      }
     }
-    step_next = c.step[ph];
+    const v2f st = scalar_load((const v2f*)(c.step + ph));
+    step_next = make_float2(st[0], st[1]);
+    if (it + 1 < c1) page = page_of(c, slot, tail, it + 1, len);
   };
   auto place = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
-    for (int x = 0; x < kLoads; ++x) {
+    for (int x = 0; x < PL; ++x) {
       const int i = x * 256 + tid;
-      if (i < 2 * kPieces) {
-        const v8h a = codes_f16(raw[x].x, raw[x].y), b = codes_f16(raw[x].z, raw[x].w);
+      if (kPieces % 256 == 0 || i < kPieces) {
         // keys: piece (pair p, dims k) holds 16 tokens 2 p and 2 p + 1; values: (dims d) both halves
-        const bool key = i < kPieces;
-        const int f = (key ? i : i - kPieces) >> 6;
-        const int fa = key ? (f / KS * 2) * KS + f % KS : 4 * KS + 2 * f, fb = key ? fa + KS : fa + 1;
-        lds[buf][fa * 64 + lane] = __builtin_bit_cast(uint4, a);
-        lds[buf][fb * 64 + lane] = __builtin_bit_cast(uint4, b);
+        const int f = i >> 6, fk = f / KS * 2 * KS + f % KS, fv = 4 * KS + 2 * f;
+        lds[buf][fk * 64 + lane] = __builtin_bit_cast(uint4, codes_f16(kraw[x].x, kraw[x].y));
+        lds[buf][(fk + KS) * 64 + lane] = __builtin_bit_cast(uint4, codes_f16(kraw[x].z, kraw[x].w));
+        lds[buf][fv * 64 + lane] = __builtin_bit_cast(uint4, codes_f16(vraw[x].x, vraw[x].y));
+        lds[buf][(fv + 1) * 64 + lane] = __builtin_bit_cast(uint4, codes_f16(vraw[x].z, vraw[x].w));
       }
     }
   };
@@ -1094,23 +1141,30 @@ __global__ void __launch_bounds__(256, kTileResident) k_attend_tile(CacheView c,
       int last[NT];
 #pragma unroll
       for (int j = 0; j < NT; ++j) last[j] = pos[j] - it * kBlock;
+      // a tile's operands are read while the one before is used
       v4f s[NT][4];
+      v8h a[2][KS];
+      auto read_keys = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < KS; ++k) a[t & 1][k] = __builtin_bit_cast(v8h, lds[buf][(t * KS + k) * 64 + lane]);
+      };
+      read_keys(0);
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
+        if (t < 3) read_keys(t + 1);
 #pragma unroll
         for (int j = 0; j < NT; ++j) s[j][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          const v8h a = __builtin_bit_cast(v8h, lds[buf][(t * KS + k) * 64 + lane]);
+        for (int k = 0; k < KS; ++k)
 #pragma unroll
           for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int x = 0; x < NS; ++x) s[j][t] = mma(a, qf[j][k][x], s[j][t]);
-        }
+            for (int x = 0; x < NS; ++x) s[j][t] = mma(a[t & 1][k], qf[j][k][x], s[j][t]);
       }
+      reads_ahead<KS, KS * NT * NS, 4>();
       // the wave's first column sees the fewest tokens
       const bool hidden = it * kBlock + kBlock > len + wc / G + 1;
-      take_tokens<4, HD, NT, NS, 1>(run, s, step, qs, last, hidden, 0u, [&](int d, int h, int) {
+      take_tokens<4, HD, NT, NS, 1, true>(run, s, step, qs, last, hidden, 0u, [&](int d, int h, int) {
         return __builtin_bit_cast(v8h, lds[buf][(4 * KS + 2 * d + h) * 64 + lane]);
       });
     }
