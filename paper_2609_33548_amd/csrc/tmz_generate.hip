@@ -262,7 +262,8 @@ __device__ __forceinline__ bool before(double v, int i, double w, int j) {
 }
 
 __global__ void __launch_bounds__(kPick) k_beam_pick(BeamArgs a) {
-  __shared__ double lse[64], own[64], lmax[kPickWaves][64], cv[kMaxCand], bound, rv[kPickWaves];
+  __shared__ double lse[64], own[64], cv[kMaxCand], rv[kPickWaves];
+  __shared__ float lmax[kPickWaves][64], bound;
   __shared__ int list[kMaxList], ci[kMaxCand], ri[kPickWaves], n_list, n_cand, pick[kMaxOut], n_pick;
   __shared__ float pv[kMaxOut];
   __shared__ bool done[64];
@@ -270,20 +271,33 @@ __global__ void __launch_bounds__(kPick) k_beam_pick(BeamArgs a) {
   const int W = a.beams, V = a.vocab, segs = a.segs, shift = a.seg_shift, eos = a.eos;
   const int64_t row0 = (int64_t)g * W;
   if (tid == 0) n_list = n_cand = 0;
+  // The usual search's segments (eight beams, a segment a thread) stay in registers; their loads and
+  // those of the parts go out together.
+  const bool held = W <= 8 && segs <= kPick;
+  float seg_max[8];
+  if (held)
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      seg_max[u] = a.seg[(row0 + (u < W ? u : W - 1)) * segs + (tid < segs ? tid : segs - 1)];
   for (int b = wave; b < W; b += kPickWaves) {
     const bool fin = a.finished && a.finished[row0 + b];
     const float sc = a.scores[row0 + b];
+    const float2* part = a.part + (row0 + b) * a.waves;
+    const float2 none = make_float2(-INFINITY, 0.0f);
+    const float2 p0 = lane < a.waves ? part[lane] : none, p1 = lane + 64 < a.waves ? part[lane + 64] : none;
     double l = INFINITY;                                 // no continuations
     if (!fin) {
-      float m = -INFINITY;
-      for (int i = lane; i < a.waves; i += 64) m = fmaxf(m, a.part[(row0 + b) * a.waves + i].x);
+      float m = fmaxf(p0.x, p1.x);
+      for (int i = lane + 128; i < a.waves; i += 64) m = fmaxf(m, part[i].x);
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
       double s = 0.0;
-      for (int i = lane; i < a.waves; i += 64) {
-        const float2 p = a.part[(row0 + b) * a.waves + i];
+      auto add = [&](float2 p) __attribute__((always_inline)) {
         if (p.x > -INFINITY) s += (double)p.y * exp((double)p.x - (double)m);
-      }
+      };
+      add(p0);
+      add(p1);
+      for (int i = lane + 128; i < a.waves; i += 64) add(part[i]);
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
       l = (double)m + log(s);
@@ -304,6 +318,12 @@ __global__ void __launch_bounds__(kPick) k_beam_pick(BeamArgs a) {
   };
   // every segment's best, eight loads at a time: f(segment, score)
   auto segments = [&](auto f) __attribute__((always_inline)) {
+    if (held) {
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (u < W && tid < segs) f(u * segs + tid, score(u, seg_max[u], eos >> shift == tid));
+      return;
+    }
     for (int j = tid; j < segs; j += kPick)
       for (int b0 = 0; b0 < W; b0 += 8) {
         float x[8];
@@ -314,14 +334,14 @@ __global__ void __launch_bounds__(kPick) k_beam_pick(BeamArgs a) {
           if (b0 + u < W) f((b0 + u) * segs + j, score(b0 + u, x[u], eos >> shift == j));
       }
   };
-  // all logits of listed segments, eight of a thread at a time: f(index, score)
+  // all logits of listed segments, sixteen of a thread at a time: f(index, score)
   auto elements = [&](int n, bool all, auto f) __attribute__((always_inline)) {
     const int64_t total = (int64_t)n << shift;
-    for (int64_t e0 = (int64_t)tid * 4; e0 < total; e0 += 2 * 4 * kPick) {
-      float x[2][4];
-      int bb[2], tt[2];
+    for (int64_t e0 = (int64_t)tid * 4; e0 < total; e0 += 4 * 4 * kPick) {
+      float x[4][4];
+      int bb[4], tt[4];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int u = 0; u < 4; ++u) {
         const int64_t e = e0 + u * 4 * kPick;
         const int at = e < total ? (int)(e >> shift) : n - 1, s = all ? at : list[at];
         bb[u] = s / segs;
@@ -337,30 +357,32 @@ __global__ void __launch_bounds__(kPick) k_beam_pick(BeamArgs a) {
         }
       }
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < 4; ++u)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           if (e0 + u * 4 * kPick < total && tt[u] + j < V)
             f(bb[u] * V + tt[u] + j, score(bb[u], clean_logit(x[u][j]), tt[u] + j == eos));
     }
   };
+  // the bound in fp32, rounded down (a score between it and the exact one does no harm)
   double best = -INFINITY;
   segments([&](int, double v) { best = fmax(best, v); });
-  lmax[wave][lane] = best;
+  lmax[wave][lane] = __double2float_rd(best);
   __syncthreads();
   if (wave == 0) {
+    float m = lmax[0][lane];
 #pragma unroll
-    for (int w = 1; w < kPickWaves; ++w) best = fmax(best, lmax[w][lane]);
-    lmax[0][lane] = best;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+    for (int w = 1; w < kPickWaves; ++w) m = fmaxf(m, lmax[w][lane]);
     int rank = 0;
-#pragma unroll 16
-    for (int i = 0; i < 64; ++i) rank += before(lmax[0][i], i, best, lane);
-    if (rank == a.n_out - 1) bound = best;
+#pragma unroll
+    for (int i = 0; i < 64; ++i) {
+      const float o = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(m), i));
+      rank += o > m || (o == m && i < lane);
+    }
+    if (rank == a.n_out - 1) bound = m;
   }
   __syncthreads();
-  const double T = bound;
+  const double T = (double)bound;
   auto wanted = [&](double v) __attribute__((always_inline)) { return v >= T && v > -INFINITY; };
   segments([&](int s, double v) {
     if (wanted(v)) {
@@ -468,13 +490,24 @@ __global__ void __launch_bounds__(kPick) k_beam_pick(BeamArgs a) {
     if (a.out_finished) a.out_finished[o0 + r] = done[b] || t == eos;
     if (a.out_history) a.out_history[(o0 + r) * (a.hist_len + 1) + a.hist_len] = t;
   }
-  if (a.out_history)
-    for (int r = wave; r < a.n_out; r += kPickWaves) {
-      const int32_t* from = a.history + (row0 + pick[r] / V) * a.hist_len;
-      int32_t* to = a.out_history + (o0 + r) * (a.hist_len + 1);
-#pragma unroll 4
-      for (int64_t i = lane; i < a.hist_len; i += 64) to[i] = from[i];
+  if (a.out_history) {                                   // eight loads of a thread at a time
+    const int T = (int)a.hist_len, total = a.n_out * T;  // at most 64 x 2^24
+    for (int i0 = tid; i0 < total; i0 += 8 * kPick) {
+      int32_t x[8];
+      int r[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int i = i0 + u * kPick < total ? i0 + u * kPick : total - 1;
+        r[u] = i / T;
+        x[u] = a.history[(row0 + pick[r[u]] / V) * T + (i - r[u] * T)];
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int i = i0 + u * kPick;
+        if (i < total) a.out_history[(o0 + r[u]) * (T + 1) + (i - r[u] * T)] = x[u];
+      }
     }
+  }
 }
 
 }  // namespace tmz
