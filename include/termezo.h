@@ -407,7 +407,8 @@ termezo_status termezo_model_timing(termezo_model* model, int32_t cls, double* m
  * while another device is current.  Creating a cache allocates all that its calls need;
  * termezo_beam_select and termezo_model_decode allocate when a call needs more scratch
  * than every earlier one, so that after one of the largest size they can be captured in
- * graphs, as the other calls here can at once.
+ * graphs, as the other calls here can at once.  Work of one context or cache is ordered on
+ * one stream: graphs of its calls must not run at the same time.
  *
  * A cache holds the keys and values of groups * beams sequences of up to max_len
  * tokens for n_layers attention layers.  The sequences of a group (the beams of a
@@ -441,8 +442,8 @@ termezo_status termezo_kvcache_create(termezo_ctx* ctx, const termezo_kvcache_co
 /* Waits for the stream and frees the cache.  NULL is a no-op. */
 void termezo_kvcache_destroy(termezo_kvcache* cache);
 
-/* Empty one group (group >= 0), or all of them (-1), which also makes the first beam of
- * every group the only one in use again.  Errors: INVALID_ARG (group out of range). */
+/* Empty one group (group >= 0; its sequences in use stay in use), or all of them (-1), which
+ * also makes the first beam of every group the only one in use again.  Errors: INVALID_ARG (group out of range). */
 termezo_status termezo_kvcache_reset(termezo_kvcache* cache, int32_t group);
 
 /* Sequences in use: row r is sequence r.  After creation and a reset of all groups
@@ -472,8 +473,10 @@ termezo_status termezo_kvcache_append(termezo_kvcache* cache, int32_t layer, con
  * neither: when given, they are appended first (termezo_kvcache_append), for one token
  * a row and up to 32 heads a key/value head in the same launch.  counts: as in append; without k and v it may be NULL (the
  * pending counts), and counts that differ from the pending ones, as pending counts above n,
- * raise a deferred INVALID_ARG and leave their group's rows out.  out must not overlap q,
- * k or v.  Errors: INVALID_ARG (as append; one of k, v null), STATE (k and v null and
+ * raise a deferred INVALID_ARG and leave their group's rows out.  A cached key or value
+ * that is not finite makes the whole output (of its heads) NaN for every query that sees its
+ * block, once that is complete, or its token, before; queries that do not are as without it.
+ * out must not overlap q, k or v.  Errors: INVALID_ARG (as append; one of k, v null), STATE (k and v null and
  * nothing pending). */
 termezo_status termezo_kvcache_attention(termezo_kvcache* cache, int32_t layer, const void* q,
                                          const void* k, const void* v, int64_t n,
@@ -537,7 +540,9 @@ termezo_status termezo_beam_select(termezo_ctx* ctx, const float* logits, const 
  * new token (0 for rows without one).  The cache's layers, heads, head size
  * and act_dtype must be the model's, its rope_base too.  Token ids are checked as in
  * termezo_model_loss.  The call allocates activations when rows * n exceeds every earlier
- * call's.  Errors: INVALID_ARG, STATE (no current codes; tokens pending), OOM. */
+ * call's.  A model with a stream of its own runs all of this there, the cache's work too:
+ * termezo_model_join before other calls on the cache or the logits.
+ * Errors: INVALID_ARG (2^24 tokens or more), STATE (no current codes; tokens pending), OOM. */
 termezo_status termezo_model_decode(termezo_model* model, termezo_kvcache* cache,
                                     const int32_t* tokens, int64_t n, const int32_t* counts,
                                     float* logits);

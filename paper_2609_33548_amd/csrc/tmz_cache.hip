@@ -1060,7 +1060,7 @@ __global__ void __launch_bounds__(256, NT == 1 ? kRowsResident1 : kRowsResident2
 // of a key/value head, 32 a wave, so the blocks that it walks are converted to fp16 once, into
 // LDS, for all of them.  Two LDS buffers: while a block is used the next one's codes are on their way
 // in registers.  Every wave takes the incomplete block by itself at the end.
-// grid: key/value heads x rows, tiles x splits: the longest tiles of all rows come first.
+// grid (one dimension): key/value heads fastest, then rows, splits, tiles: the longest tiles of all rows first.
 // ---------------------------------------------------------------------------
 constexpr int kTileCols = 128;
 template <typename T, int HD>
@@ -1070,9 +1070,10 @@ __global__ void __launch_bounds__(256, kTileResident) k_attend_tile(CacheView c,
   constexpr int NS = sizeof(T) == 2 ? 1 : 2, NT = 2, KS = HD / 32;
   constexpr int kPieces = kBlock * HD / 16;              // 16-byte pieces of a page
   __shared__ uint4 lds[2][4 * kPieces];                  // keys [16 tokens][32 dims], values [16 dims][32 tokens]
-  const int head = blockIdx.x % c.heads_kv, row = blockIdx.x / c.heads_kv, tid = threadIdx.x, lane = tid & 63;
+  const int units = c.heads_kv * c.groups * c.width, unit = blockIdx.x % units, turn = blockIdx.x / units;
+  const int head = unit % c.heads_kv, row = unit / c.heads_kv, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int tiles = gridDim.y / splits, tile = tiles - 1 - blockIdx.y / splits, split = blockIdx.y % splits;
+  const int tiles = gridDim.x / units / splits, tile = tiles - 1 - turn / splits, split = turn % splits;
   const int g = row / c.width;
   const int cnt = query_count(c, g, n, counts);
   const int G = heads / c.heads_kv, cols = cnt * G, c0 = tile * kTileCols;
@@ -1362,7 +1363,7 @@ hipError_t cache_attention_on(termezo_kvcache* c, int layer, const void* q, cons
   }
   const int tiles = (int)((cols + kTileCols - 1) / kTileCols);
   const int splits = token_splits(c, rows * Hkv * tiles, kTileResident);
-  const dim3 grid((unsigned)(Hkv * rows), (unsigned)(tiles * splits));
+  const dim3 grid((unsigned)(Hkv * rows * tiles * splits));
 #define TMZ_CALL(T, HD)                                                                         \
   hipLaunchKernelGGL((k_attend_tile<T, HD>), grid, dim3(256), 0, s, w, layer, (const T*)q,       \
                      (T*)out, (int)n, counts, H, scale, splits, c->part);                       \

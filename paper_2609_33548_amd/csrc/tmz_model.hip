@@ -2394,7 +2394,7 @@ termezo_status termezo_model_decode(termezo_model* m, termezo_kvcache* kv, const
       kc.rope_base != cf.rope_base)
     return refuse(TERMEZO_ERR_INVALID_ARG, "model_decode: the cache was not made for this model");
   const int64_t rows = (int64_t)kc.groups * kv->width, M = rows * n;
-  if (n > kc.max_len || M > INT32_MAX / 4)
+  if (n > kc.max_len || M >= (1 << 24))
     return refuse(TERMEZO_ERR_INVALID_ARG, "model_decode: more tokens than the cache or a call takes");
   if (kv->pending) return refuse(TERMEZO_ERR_STATE, "model_decode: appended tokens are pending");
   if (m->use_snap ? !c->snap_valid : !c->codes_valid)

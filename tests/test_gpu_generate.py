@@ -285,6 +285,72 @@ def test_non_finite_values_stay_in_their_row(ctx, orc, bf16, n):
     c.close()
 
 
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("H,Hkv,P,n,at", [(4, 4, 40, 8, 44), (8, 2, 40, 8, 45), (8, 2, 40, 20, 44),
+                                          (4, 4, 200, 90, 230), (8, 2, 200, 90, 288), (4, 2, 10, 300, 150)])
+def test_non_finite_values_behind_a_query(ctx, orc, bf16, H, Hkv, P, n, at):
+    """Position `at` of the new tokens holds an infinity or NaN: queries that see it, or its block where
+    that is complete, are NaN, the ones before are as without it."""
+    torch = _torch()
+    from oracle import generate_ref as ref
+    rng = np.random.default_rng(at)
+    hd = 64
+    for which, value in (("k", np.inf), ("k", np.nan), ("v", -np.inf), ("v", np.nan)):
+        c = _cache(ctx, H, Hkv, hd, P + n, 1, bf16)
+        k, v, kd, vd = _kv(rng, 1, P + n, Hkv, hd, bf16)
+        c.append(0, kd[:, :P].contiguous(), vd[:, :P].contiguous())
+        c.advance()
+        q = ref.to_type(rng.standard_normal((1, n, H, hd)), bf16)
+        (kd if which == "k" else vd)[0, at, :, 7] = value
+        out = torch.zeros((1, n, H, hd), dtype=kd.dtype, device="cuda")
+        c.attention(0, torch.from_numpy(q).cuda().to(kd.dtype), out, k=kd[:, P:].contiguous(),
+                    v=vd[:, P:].contiguous())
+        got = out[0].float().cpu().numpy()
+        first = at // 64 * 64 if at // 64 * 64 + 64 <= P + n else at     # position from which it is seen
+        ok = max(0, min(n, first - P))
+        assert np.isnan(got[ok:]).all()
+        if ok:
+            s = ref.Sequence(bf16, 10000.0)
+            s.append(k[0], v[0])
+            want, mag, big = ref.attend(s, q[0])
+            u = 2.0 ** -11 if bf16 else 2.0 ** -21
+            ds = (u + hd * 2.0 ** -24) * big
+            tol = (2.0 ** -8 if bf16 else 2.0 ** -24) * np.abs(want) \
+                + (np.expm1(2 * ds) + u + (P + n + 64) * 2.0 ** -24 + 2.0 ** -20) * mag \
+                + (P + n) * 2.0 ** (-32 if bf16 else -40) * np.abs(s.values()[1]).max() + 1e-37
+            assert (np.abs(got[:ok] - want[:ok]) <= tol[:ok]).all()
+        c.close()
+
+
+def test_pages_beyond_32_bits(ctx, orc):
+    """A cache of more than 2^32 bytes of keys: its last sequence's pages lie behind that."""
+    torch = _torch()
+    from oracle import generate_ref as ref
+    rng = np.random.default_rng(30)
+    H, Hkv, hd, G, P = 4, 4, 128, 10, 150
+    c = _cache(ctx, H, Hkv, hd, 1 << 20, G, True)
+    assert (G - 1) * (1 << 20) * Hkv * hd > 1 << 32
+    counts = torch.zeros(G, dtype=torch.int32, device="cuda")
+    counts[0], counts[-1] = 70, P
+    k, v, kd, vd = _kv(rng, G, P, Hkv, hd, True)
+    c.append(0, kd, vd, counts=counts)
+    c.advance()
+    refs = [ref.Sequence(True, 10000.0) for _ in range(G)]
+    refs[0].append(k[0, :70], v[0, :70])
+    refs[-1].append(k[-1], v[-1])
+    _check_values(c, refs)
+    for n in (1, 50):
+        k, v, kd, vd = _kv(rng, G, n, Hkv, hd, True)
+        q = ref.to_type(rng.standard_normal((G, n, H, hd)), True)
+        out = torch.zeros((G, n, H, hd), dtype=torch.bfloat16, device="cuda")
+        c.attention(0, torch.from_numpy(q).cuda().bfloat16(), out, k=kd, v=vd)
+        c.advance()
+        for r in (0, G - 1):
+            refs[r].append(k[r], v[r])
+            _check_attention(refs[r], q[r], out[r].float().cpu().numpy(), True)
+    c.close()
+
+
 def test_extreme_scores(ctx, orc):
     """Scores far apart (one token takes everything), all equal, and values near the types' ends."""
     torch = _torch()
