@@ -119,12 +119,118 @@ __global__ void __launch_bounds__(256) k_logits(const T* __restrict__ x, const T
     }
 }
 
+// The same with all of x in LDS: work groups, as many as LDS lets run, walk the vocabulary, a wave 16 rows of E at
+// a time, GS steps ahead of the matrix instructions.  E's bytes are then all that passes the caches
+// (one row of 128256 x 2560 139 -> 110 us, 5.9 TB/s; 16 rows 156 -> 131, 32 rows 166 -> 137).  16 rows' reads fall
+// on all banks: rows are 16 bytes apart beyond their length, or (DENSE, whole 128 bytes) piece c of 16 bytes of row m
+// lies at c ^ (m % 8).
+template <typename T, int MT, int KB, int NW, int GS, bool DENSE>
+__global__ void __launch_bounds__(64 * NW) k_logits_walk(const T* __restrict__ x, const T* __restrict__ E,
+                                                     int M, int d, int64_t V, float* __restrict__ out) {
+  __shared__ __align__(16) char xs[KB * 1024];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int bytes = d * (int)sizeof(T), pitch = DENSE ? bytes : bytes + 16, row16 = bytes / 16;
+  constexpr int turn = DENSE ? 7 : 0;
+  for (int i = threadIdx.x; i < M * row16; i += 64 * NW) {
+    const int m = i / row16, c = i - m * row16;
+    *(uint4*)(xs + m * pitch + (c ^ (m & turn)) * 16) = ((const uint4*)x)[i];
+  }
+  __syncthreads();
+  const int whole = bytes / 64;
+  const int g16 = (lane >> 4) * 16;
+  int xo[MT], xm[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int m = 16 * i + (lane & 15) < M ? 16 * i + (lane & 15) : M - 1;
+    xo[i] = m * pitch;
+    xm[i] = (m & turn) * 16;
+  }
+  const int64_t tiles = (V + 15) / 16;
+  for (int64_t tile = (int64_t)blockIdx.x * NW + wave; tile < tiles; tile += (int64_t)gridDim.x * NW) {
+    const int64_t t = tile * 16 + (lane & 15);
+    const char* ep = (const char*)(E + (t < V ? t : V - 1) * d) + g16;
+    v4f acc[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) acc[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    auto use = [&](uint4 a, int s) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i) acc[i] = logits_step<T>(a, *(const uint4*)(xs + xo[i] + ((s * 64 + g16) ^ xm[i])), acc[i]);
+    };
+    uint4 a[2][GS];
+    int s = 0;
+    if (GS <= whole)
+#pragma unroll
+      for (int u = 0; u < GS; ++u) a[0][u] = *(const uint4*)(ep + u * 64);
+    // two groups in turn, so that registers need no index
+    for (; s + 2 * GS <= whole; s += 2 * GS) {
+#pragma unroll
+      for (int u = 0; u < GS; ++u) a[1][u] = *(const uint4*)(ep + (s + GS + u) * 64);
+#pragma unroll
+      for (int u = 0; u < GS; ++u) use(a[0][u], s + u);
+      if (s + 3 * GS <= whole)
+#pragma unroll
+        for (int u = 0; u < GS; ++u) a[0][u] = *(const uint4*)(ep + (s + 2 * GS + u) * 64);
+#pragma unroll
+      for (int u = 0; u < GS; ++u) use(a[1][u], s + GS + u);
+    }
+    if (s + GS <= whole) {
+#pragma unroll
+      for (int u = 0; u < GS; ++u) use(a[0][u], s + u);
+      s += GS;
+    }
+    for (; s < whole; ++s) use(*(const uint4*)(ep + s * 64), s);
+    if (whole * 64 < bytes) {                            // half a step
+      const bool in = g16 < bytes - whole * 64;
+      const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+      const uint4 e = in ? *(const uint4*)(ep + whole * 64) : zero;
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+        acc[i] = logits_step<T>(e, in ? *(const uint4*)(xs + xo[i] + ((whole * 64 + g16) ^ xm[i])) : zero, acc[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int m = 16 * i + (lane & 15);
+      const int64_t t4 = tile * 16 + (lane >> 4) * 4;
+      if (m < M)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (t4 + r < V) out[m * V + t4 + r] = acc[i][r];
+    }
+  }
+}
+
 template <typename T, int MT>
 static void logits_as(const T* x, const T* E, int64_t M, int64_t d, int64_t V, float* out, int n_cu,
                       hipStream_t s) {
+  // x in LDS: two work groups of eight waves on a compute unit while it takes half of LDS; else one, of sixteen waves
+  // where there are 16 vocabulary rows for each (32 rows: 128256 x 2560 188 against 137 us, 32003 x 1536 24 against 33)
+  const int64_t bytes = d * (int64_t)sizeof(T), tiles = (V + 15) / 16, lds = M * (bytes + 16);
+  const unsigned two = (unsigned)std::min<int64_t>((tiles + 7) / 8, 2 * n_cu);
+  const unsigned one = (unsigned)std::min<int64_t>((tiles + 15) / 16, n_cu);
+#define TMZ_WALK(MTV, KB, NW, GS, DENSE, GRID)                                                              \
+  hipLaunchKernelGGL((k_logits_walk<T, MTV, KB, NW, GS, DENSE>), dim3(GRID), dim3(64 * NW), 0, s, x, E, (int)M, \
+                     (int)d, V, out)
+  if constexpr (MT == 1) {
+    if (lds <= 80 * 1024) {
+      TMZ_WALK(1, 80, 8, 8, false, two);
+      return;
+    }
+  }
+  if (M <= 16 * MT && tiles >= 16 * (int64_t)n_cu) {
+    if (bytes % 128 == 0 && M * bytes <= 160 * 1024) {
+      TMZ_WALK(MT, 160, 16, 4, true, one);
+      return;
+    }
+  } else if constexpr (MT == 2) {
+    if (lds <= 160 * 1024) {
+      TMZ_WALK(2, 160, 8, 8, false, std::min(two, (unsigned)n_cu));
+      return;
+    }
+  }
+#undef TMZ_WALK
   const int mt = (int)((M + 16 * MT - 1) / (16 * MT));
-  // 64 vocabulary rows a work group where that still makes one for every compute unit (M = 32, 32003 x 1536: 501
-  // work groups of 64 rows 24 us, 2001 of 16 rows 36)
+  // 64 vocabulary rows a work group where that still makes one for every compute unit (M = 32, 32003 x 1536:
+  // 501 work groups of 64 rows 24 us, 2001 of 16 rows 36)
   if ((V + 63) / 64 * mt >= n_cu)
     hipLaunchKernelGGL((k_logits<T, MT, 4>), dim3((unsigned)((V + 63) / 64 * mt)), dim3(256), 0, s, x, E, M, d,
                        V, out, mt);
