@@ -557,7 +557,7 @@ def test_cache_refusals(ctx, orc):
                                    (31, 48, 1000), (33, 2560, 129), (64, 1536, 250), (65, 80, 77),
                                    (130, 272, 331), (300, 64, 20), (24, 1536, 900), (10, 2560, 65600),
                                    (16, 2688, 65537), (32, 2560, 66001), (45, 1536, 65999),
-                                   (20, 2576, 65601)])
+                                   (20, 2576, 65601), (16, 2576, 17001), (16, 2688, 700)])
 def test_logits(ctx, orc, bf16, M, d, V):
     torch = _torch()
     g = torch.Generator().manual_seed(M * d + V)
