@@ -406,8 +406,10 @@ termezo_status termezo_model_timing(termezo_model* model, int32_t cls, double* m
  * return as soon as their work is queued on the context's stream and may be called
  * while another device is current.  Creating a cache allocates all that its calls need;
  * termezo_beam_select and termezo_model_decode allocate when a call needs more scratch
- * than every earlier one, so that after one of the largest size they can be captured in
- * graphs, as the other calls here can at once.  Work of one context or cache is ordered on
+ * than every earlier one, so that after one of their size they can be captured in
+ * graphs, as the other calls here can at once (a captured call that would have to allocate is
+ * refused: STATE).  Graphs stay valid when a later call takes more: what they use is kept until the
+ * context, model or cache is destroyed.  Work of one context or cache is ordered on
  * one stream: graphs of its calls must not run at the same time.
  *
  * A cache holds the keys and values of groups * beams sequences of up to max_len
@@ -525,7 +527,7 @@ termezo_status termezo_logits(termezo_ctx* ctx, const void* x, const void* E, te
  * is none (finished must be null).  No output may overlap an input.  Errors: INVALID_ARG (groups 1 .. 65535, beams
  * 1 .. 64, vocab 1 .. 2^24, n_out 1 .. 64 and at most beams * vocab, hist_len 0 .. 2^24,
  * eos < -1 or >= vocab, null pointers, history without out_history or the
- * other way round, finished with eos -1). */
+ * other way round, finished with eos -1), STATE (captured, with scratch to be allocated), OOM. */
 termezo_status termezo_beam_select(termezo_ctx* ctx, const float* logits, const float* scores,
                                    const uint8_t* finished, int32_t groups, int32_t beams,
                                    int32_t vocab, int32_t n_out, int32_t eos, float* out_scores,
@@ -542,7 +544,8 @@ termezo_status termezo_beam_select(termezo_ctx* ctx, const float* logits, const 
  * termezo_model_loss.  The call allocates activations when rows * n exceeds every earlier
  * call's.  A model with a stream of its own runs all of this there, the cache's work too:
  * termezo_model_join before other calls on the cache or the logits.
- * Errors: INVALID_ARG (2^24 tokens or more), STATE (no current codes; tokens pending), OOM. */
+ * Errors: INVALID_ARG (2^24 tokens or more), STATE (no current codes; tokens pending; captured, with
+ * activations to be allocated), OOM. */
 termezo_status termezo_model_decode(termezo_model* model, termezo_kvcache* cache,
                                     const int32_t* tokens, int64_t n, const int32_t* counts,
                                     float* logits);

@@ -674,14 +674,22 @@ termezo_status termezo_beam_select(termezo_ctx* c, const float* logits, const fl
   const int segs = (int)(((int64_t)vocab + (1 << shift) - 1) >> shift);
   const int waves = (vocab + kScan - 1) / kScan;
   const int64_t rows = (int64_t)groups * beams, need = rows * (waves * 8 + (int64_t)segs * 4);
+  const bool graph = capturing(c->stream);
   if (need > c->beam_cap) {
-    if (c->d_beam) (void)hipFree(c->d_beam);
+    if (graph) {
+      c->last_error = "beam_select: a captured call needs scratch; make one of its size before";
+      return TERMEZO_ERR_STATE;
+    }
+    if (c->beam_held) c->held.push_back(c->d_beam);
+    else if (c->d_beam) (void)hipFree(c->d_beam);
     c->d_beam = nullptr;
     c->beam_cap = 0;
+    c->beam_held = false;
     const hipError_t e = hipMalloc(&c->d_beam, (size_t)need);
     if (e != hipSuccess) return hip_status(c, e, "beam_select");
     c->beam_cap = need;
   }
+  c->beam_held |= graph;
   BeamArgs a{logits, scores, finished, beams, vocab, n_out, eos, out_scores, out_tokens, out_parents,
              out_finished, history, out_history, hist_len, (float2*)c->d_beam,
              (float*)((char*)c->d_beam + rows * waves * 8), waves, segs, shift};

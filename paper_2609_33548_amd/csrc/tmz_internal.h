@@ -224,6 +224,8 @@ struct termezo_ctx {
   bool pending_perturb = false;
   void* d_beam = nullptr;            // beam selection: the chunks' candidates, maxima and sums
   int64_t beam_cap = 0;              // its bytes
+  bool beam_held = false;            // a captured graph uses it
+  std::vector<void*> held;           // outgrown ones that graphs use, freed with the context
   uint64_t last_seed = 0;
   float last_eps = 0.f;
   float delta = 1e-5f;
@@ -398,6 +400,14 @@ struct DeviceScope {
   DeviceScope(const DeviceScope&) = delete;
   DeviceScope& operator=(const DeviceScope&) = delete;
 };
+
+// Whether work on s goes into a graph: the scratch that it uses must then live as long as its owner does.
+inline bool capturing(hipStream_t s) {
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(s, &st) == hipSuccess) return st != hipStreamCaptureStatusNone;
+  (void)hipGetLastError();
+  return false;
+}
 
 // The cache's calls on a stream of the caller's choice (checked arguments).
 hipError_t cache_append_on(termezo_kvcache* c, int layer, const void* k, const void* v, int64_t n,

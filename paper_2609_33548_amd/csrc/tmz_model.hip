@@ -1788,6 +1788,8 @@ struct termezo_model {
   void* vt = nullptr;
   Acts dec;                                  // of generation steps (termezo_model_decode)
   int64_t cap_dec = 0;                       // tokens they hold
+  bool dec_held = false;                     // a captured graph uses them
+  std::vector<Acts> held;                    // outgrown ones that graphs use, freed with the model
   float *pmax = nullptr, *psum = nullptr, *lab = nullptr, *row = nullptr;
   int32_t* labels = nullptr;
   float *rope_c = nullptr, *rope_s = nullptr;
@@ -2240,6 +2242,7 @@ void termezo_model_destroy(termezo_model* m) {
   if (m->ev_out) (void)hipEventDestroy(m->ev_out);
   model_free_buffers(m);
   acts_free(m->dec);
+  for (Acts& a : m->held) acts_free(a);
   delete m;
 }
 
@@ -2409,14 +2412,21 @@ termezo_status termezo_model_decode(termezo_model* m, termezo_kvcache* kv, const
     c->last_error = std::string("model_decode: ") + hipGetErrorString(e);
     return e == hipErrorOutOfMemory ? TERMEZO_ERR_OOM : TERMEZO_ERR_DEVICE;
   };
+  const bool graph = capturing(c->stream) || capturing(m->stream);
   if (e == hipSuccess && M > m->cap_dec) {
-    acts_free(m->dec);
+    if (graph)
+      return refuse(TERMEZO_ERR_STATE, "model_decode: a captured call needs scratch; make one of its size before");
+    if (m->dec_held) m->held.push_back(m->dec);
+    else acts_free(m->dec);
+    m->dec = Acts();
+    m->dec_held = false;
     m->cap_dec = 0;
     e = acts_alloc(m->dec, cf, m->hd, M);
     if (e != hipSuccess) acts_free(m->dec);
     else m->cap_dec = M;
   }
   if (e != hipSuccess) return failed();
+  m->dec_held |= graph;
   if (!after_context(m)) return refuse(TERMEZO_ERR_DEVICE, "model_decode: event record / wait");
   hipStream_t s = m->stream;
   const uint32_t* codes = m->use_snap ? c->d_codes_snap : c->d_codes;

@@ -213,6 +213,8 @@ void free_all(termezo_ctx* c) {
   dfree(c->d_loss);
   dfree(c->d_scal);
   dfree(c->d_beam);
+  for (void* p : c->held) (void)hipFree(p);
+  c->held.clear();
   dfree(c->d_xq);
   dfree(c->d_xs);
   dfree(c->d_xrs);

@@ -973,3 +973,63 @@ def test_decode_captured_and_refused(orc):
         ctx.update(0.1, 1e-4)
         refused(T.ERR_STATE, model.decode, c, step, lb)
         ctx.close()
+
+
+def test_graphs_outlive_larger_calls(orc):
+    """Captured steps whose scratch a later, larger call outgrows replay as before, between larger calls; a
+    captured call that would have to allocate is refused and leaves the cache as it was."""
+    torch = _torch()
+    from oracle import decoder_ref as dec
+    from paper_2609_33548_amd import synth, termezo as T
+    cfg = dec.DecoderConfig(n_blocks=2, d_model=512, n_heads=4, n_kv_heads=2, d_ffn=1024, vocab=1000, bf16=True)
+    stream = torch.cuda.Stream()
+    B, N = 2, 6
+    with torch.cuda.stream(stream):
+        ref, ctx, model, emb, E, w = _decoder(orc, cfg, 83)
+        ctx.perturb(0, 1e-3, 1)
+        tok = torch.from_numpy(synth.tokens(84, B, N, cfg.vocab)).cuda()
+        long = torch.from_numpy(synth.tokens(85, 4, 300, cfg.vocab)).cuda()
+        a, b, big = _model_cache(ctx, cfg, N, B), _model_cache(ctx, cfg, N, B), _model_cache(ctx, cfg, 300, 4)
+        la, lb = (torch.zeros((B, cfg.vocab), device="cuda") for _ in range(2))
+        lbig = torch.zeros((4, cfg.vocab), device="cuda")
+        scores = torch.zeros((1, B), device="cuda")
+        new = lambda k: (torch.zeros((1, k), device="cuda"),
+                         *(torch.zeros((1, k), dtype=torch.int32, device="cuda") for _ in range(2)))
+        oa, ob = new(3), new(3)
+        xbig, sbig, obig = torch.randn((40, 8, 5000), device="cuda"), torch.zeros((40, 8), device="cuda"), \
+            tuple(x.repeat(40, 1) for x in new(8))
+        step = tok[:, :1].contiguous()
+        model.decode(b, step, lb)                           # takes the scratch of this size
+        ctx.beam_select(lb.view(1, B, -1), scores, *ob)
+        b.reset()
+    stream.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        model.decode(b, step, lb)
+        ctx.beam_select(lb.view(1, B, -1), scores, *ob)
+    refusals = []
+    with torch.cuda.graph(torch.cuda.CUDAGraph(), stream=stream):
+        lb.add_(0)
+        for f, args in ((model.decode, (big, long, lbig)), (ctx.beam_select, (xbig, sbig, *obig))):
+            try:
+                f(*args)
+            except T.TermezoError as err:
+                refusals.append(err.status)
+    assert refusals == [T.ERR_STATE] * 2
+    with torch.cuda.stream(stream):
+        for t in range(N):
+            big.reset()
+            model.decode(big, long[:, :60 * (t + 1) - 60 + 1].contiguous() if t < 5 else long, lbig)
+            ctx.beam_select(xbig, sbig, *obig)
+            fill = torch.full((1 << 22,), float("nan"), device="cuda")      # takes freed memory, if there is any
+            step.copy_(tok[:, t:t + 1])
+            graph.replay()
+            got = [x.clone() for x in (lb, *ob)]
+            model.decode(a, step, la)
+            ctx.beam_select(la.view(1, B, -1), scores, *oa)
+            assert all(torch.equal(x, y) for x, y in zip(got, (la, *oa))), t
+            del fill
+        ctx.sync()
+        assert int(big.lengths()[0]) == 300
+        model.close()
+        ctx.close()
