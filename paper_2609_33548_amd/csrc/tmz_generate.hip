@@ -202,28 +202,35 @@ __global__ void __launch_bounds__(64 * NW) k_logits_walk(const T* __restrict__ x
 template <typename T, int MT>
 static void logits_as(const T* x, const T* E, int64_t M, int64_t d, int64_t V, float* out, int n_cu,
                       hipStream_t s) {
-  // x in LDS: two work groups of eight waves on a compute unit while it takes half of LDS; else one, of sixteen waves
-  // where there are 16 vocabulary rows for each (32 rows: 128256 x 2560 188 against 137 us, 32003 x 1536 24 against 33)
+  // x in LDS where the vocabulary gives every compute unit four tiles of 16 rows (M = 3, d = 2560 in bf16: 16500 rows
+  // 24 against 33 us of k_logits, 16000 rows 23 against 17, 1000 rows 20 against 6): two work groups of eight waves
+  // on a compute unit while x takes half of LDS, else one, of sixteen waves where eight have more than a tile each
+  // (M = 32, d = 1536: 33000 rows 38 -> 34 us; 32003 rows 24 with eight, 33 with sixteen).
   const int64_t bytes = d * (int64_t)sizeof(T), tiles = (V + 15) / 16, lds = M * (bytes + 16);
   const unsigned two = (unsigned)std::min<int64_t>((tiles + 7) / 8, 2 * n_cu);
   const unsigned one = (unsigned)std::min<int64_t>((tiles + 15) / 16, n_cu);
 #define TMZ_WALK(MTV, KB, NW, GS, DENSE, GRID)                                                              \
   hipLaunchKernelGGL((k_logits_walk<T, MTV, KB, NW, GS, DENSE>), dim3(GRID), dim3(64 * NW), 0, s, x, E, (int)M, \
                      (int)d, V, out)
-  if constexpr (MT == 1) {
-    if (lds <= 80 * 1024) {
-      TMZ_WALK(1, 80, 8, 8, false, two);
-      return;
+  if (M <= 16 * MT && tiles >= 4 * (int64_t)n_cu) {
+    const bool dense = bytes % 128 == 0 && M * bytes <= 160 * 1024;
+    const unsigned half = std::min(two, (unsigned)n_cu);
+    if constexpr (MT == 1) {
+      if (lds <= 80 * 1024) {
+        TMZ_WALK(1, 80, 8, 8, false, two);
+        return;
+      }
     }
-  }
-  if (M <= 16 * MT && tiles >= 16 * (int64_t)n_cu) {
-    if (bytes % 128 == 0 && M * bytes <= 160 * 1024) {
+    if (dense && tiles > 8 * (int64_t)n_cu) {
       TMZ_WALK(MT, 160, 16, 4, true, one);
       return;
     }
-  } else if constexpr (MT == 2) {
     if (lds <= 160 * 1024) {
-      TMZ_WALK(2, 160, 8, 8, false, std::min(two, (unsigned)n_cu));
+      TMZ_WALK(MT, 160, 8, 8, false, half);
+      return;
+    }
+    if (dense) {
+      TMZ_WALK(MT, 160, 8, 8, true, half);
       return;
     }
   }

@@ -557,7 +557,11 @@ def test_cache_refusals(ctx, orc):
                                    (31, 48, 1000), (33, 2560, 129), (64, 1536, 250), (65, 80, 77),
                                    (130, 272, 331), (300, 64, 20), (24, 1536, 900), (10, 2560, 65600),
                                    (16, 2688, 65537), (32, 2560, 66001), (45, 1536, 65999),
-                                   (20, 2576, 65601), (16, 2576, 17001), (16, 2688, 700)])
+                                   (20, 2576, 65601), (16, 2576, 17001), (16, 2688, 700),
+                                   (5, 272, 16411), (20, 2576, 16411), (32, 2560, 16411), (45, 1536, 16411),
+                                   (64, 1280, 16411), (64, 640, 16411), (16, 5120, 16411), (16, 2560, 33001),
+                                   (32, 1280, 33001), (64, 640, 40001), (24, 16, 32801), (40, 80, 16501),
+                                   (3, 2560, 16383)])
 def test_logits(ctx, orc, bf16, M, d, V):
     torch = _torch()
     g = torch.Generator().manual_seed(M * d + V)
