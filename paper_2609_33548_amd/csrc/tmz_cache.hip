@@ -1066,7 +1066,7 @@ __global__ void __launch_bounds__(256, NT == 1 ? kRowsResident1 : kRowsResident2
 // Attention of many queries (prompts and their pieces): a work group of four waves takes kTileCols columns
 // of a key/value head, 32 a wave, so the blocks that it walks are converted to fp16 once, into
 // LDS, for all of them.  Two LDS buffers: while a block is used the next one's codes are on their way
-// in registers.  Every wave takes the incomplete block by itself at the end.  Four prompts of up to 2000
+// in registers; the incomplete block passes the same way (bf16).  Four prompts of up to 2000
 // tokens, 20 heads of 128 on 5: 131 us, 0.57 PFLOP/s; the matrix cores are busy 28% of it, the vector units 52%
 // (exponentials, rescaling and the packing of weights), so those bound it.
 // grid (one dimension): key/value heads fastest, then rows, splits, tiles: the longest tiles of all rows first.
@@ -1078,7 +1078,10 @@ __global__ void __launch_bounds__(256, kTileResident) k_attend_tile(CacheView c,
                                                      int splits, float* part) {
   constexpr int NS = sizeof(T) == 2 ? 1 : 2, NT = 2, KS = HD / 32;
   constexpr int kPieces = kBlock * HD / 16;              // 16-byte pieces of a page
+  constexpr bool kWhole = NS == 1;                       // the incomplete block is taken whole
   __shared__ uint4 lds[2][4 * kPieces];                  // keys [16 tokens][32 dims], values [16 dims][32 tokens]
+  __shared__ float tail_max[2][4];
+  __shared__ uint32_t tail_bad[2];
   const int units = c.heads_kv * c.groups * c.width, unit = blockIdx.x % units, turn = blockIdx.x / units;
   const int head = unit % c.heads_kv, row = unit / c.heads_kv, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1096,12 +1099,6 @@ __global__ void __launch_bounds__(256, kTileResident) k_attend_tile(CacheView c,
   if (i0 >= i1) return;
   const int wc = c0 + wave * 32;                         // the wave's first column
   const int mine = wc < cols ? items_of(len, cnt, cols, wc + 32, G) : 0;   // blocks it needs
-  v8h qf[NT][KS][NS];
-  float qs[NT];
-  int pos[NT];
-  load_columns<T, HD, NT, NS>(c, q, row, n, heads, head, len, cnt, wc, scale, qf, qs, pos);
-  Running<HD, NT> run;
-  start(run);
   const int c1 = i1 < full ? i1 : full;                  // coded blocks end here
   // pieces of a page a thread moves, and what they are
   constexpr int PL = (kPieces + 255) / 256;
@@ -1138,56 +1135,156 @@ __global__ void __launch_bounds__(256, kTileResident) k_attend_tile(CacheView c,
       }
     }
   };
-  if (i0 < c1) {
-    fetch(i0);
-    place(0);
-  }
+  // The incomplete block becomes one of the same form (bf16): scaled by powers of two to magnitudes below 128.  Wave w
+  // converts the keys of tokens 16 w .. and HD / 4 dims of the values.  (16 tokens at a time in every wave, as fp32 takes
+  // them below for want of registers, measured 25 against 15 us for 16 prompts of 63 tokens, 43 against 37 for 6 pieces
+  // of 96 behind 1500, and 15 against 16.5 where the block holds 11 tokens.)  Returns the lane's tokens whose values
+  // are not finite.
+  auto place_tail = [&]() __attribute__((always_inline)) -> uint32_t {
+    const int64_t th = c.tail_head(layer, c.sel[g] ^ (full != len / kBlock), tail, head) * (kBlock * HD);
+    const int have = total - full * kBlock;
+    const T *kt = (const T*)c.ktail + th, *vt = (const T*)c.vtail + th;
+    const int t = wave * 16 + (lane & 15), v0 = (lane >> 4) * 4;
+    const bool in = t < have;
+    uint4 kr[KS];
+    uint2 vr[KS][2];
+#pragma unroll
+    for (int x = 0; x < KS; ++x) {
+      kr[x] = *(const uint4*)(kt + (in ? t : 0) * HD + x * 32 + (lane >> 4) * 8);
+      const int f = wave * KS + x;                       // dims 16 (f / 2) .., tokens 32 (f % 2) + v0 .. and 16 further
+      const T* vp = vt + (f / 2 * 16 + (lane & 15)) * kBlock + f % 2 * 32 + v0;
+      vr[x][0] = *(const uint2*)vp;
+      vr[x][1] = *(const uint2*)(vp + 16);
+    }
+    auto key = [&](int x, float (&k)[8]) __attribute__((always_inline)) { load8((const T*)&kr[x], k); };
+    auto value = [&](int x, float (&v)[8]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        load4((const T*)&vr[x][r], v + 4 * r);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if ((wave * KS + x) % 2 * 32 + v0 + r * 16 + e >= have) v[4 * r + e] = 0.0f;
+      }
+    };
+    float km = 0.0f, vm = 0.0f;
+    uint32_t off[2] = {0, 0};                            // tokens 32 i + v0 + .. with a value that is not finite
+#pragma unroll
+    for (int x = 0; x < KS; ++x) {
+      float k[8], v[8];
+      key(x, k);
+      value(x, v);
+      uint32_t b = 0;
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        if (!(fabsf(v[r]) < INFINITY)) b |= 1u << (r / 4 * 16 + r % 4);
+        km = fmaxf(km, in ? finite_abs(k[r]) : 0.0f);
+        vm = fmaxf(vm, finite_abs(v[r]));
+      }
+      off[0] |= (wave * KS + x) % 2 ? 0 : b;
+      off[1] |= (wave * KS + x) % 2 ? b : 0;
+    }
+    if (__any(off[0] | off[1])) {
+      if (off[0]) atomicOr(&tail_bad[0], off[0] << v0);
+      if (off[1]) atomicOr(&tail_bad[1], off[1] << v0);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      km = fmaxf(km, __shfl_xor(km, o, 64));
+      vm = fmaxf(vm, __shfl_xor(vm, o, 64));
+    }
+    if (lane == 0) {
+      tail_max[0][wave] = km;
+      tail_max[1][wave] = vm;
+    }
+    __syncthreads();
+    km = fmaxf(fmaxf(tail_max[0][0], tail_max[0][1]), fmaxf(tail_max[0][2], tail_max[0][3]));
+    vm = fmaxf(fmaxf(tail_max[1][0], tail_max[1][1]), fmaxf(tail_max[1][2], tail_max[1][3]));
+    const uint32_t b0 = tail_bad[0] >> v0, b1 = tail_bad[1] >> v0;   // the lane's tokens 16 i + v0 + r: bits 4 i + r
+    const uint32_t bad = (b0 & 15) | (b0 >> 12 & 240) | (b1 & 15) << 8 | (b1 >> 12 & 240) << 8;
+    const int ke = exponent_of(km) - 7, ve = exponent_of(vm) - 7;
+    step_next = make_float2(ldexpf(1.0f, ke), ldexpf(1.0f, ve));
+#pragma unroll
+    for (int x = 0; x < KS; ++x) {
+      const int f = wave * KS + x;
+      float k[8], v[8];
+      key(x, k);
+      value(x, v);
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        k[r] = !in ? 0.0f : fabsf(k[r]) < INFINITY ? ldexpf(k[r], -ke) : __builtin_nanf("");
+        v[r] = fabsf(v[r]) < INFINITY ? ldexpf(v[r], -ve) : 0.0f;   // its token is NaN by `bad`
+      }
+      v8h a[1];
+      split_f16<1>(k, a);
+      lds[0][f * 64 + lane] = __builtin_bit_cast(uint4, a[0]);
+      split_f16<1>(v, a);
+      lds[0][(4 * KS + f) * 64 + lane] = __builtin_bit_cast(uint4, a[0]);
+    }
+    return bad;
+  };
+  // the first block is on its way while the queries are
+  if (i0 < c1) fetch(i0);
+  v8h qf[NT][KS][NS];
+  float qs[NT];
+  int pos[NT];
+  load_columns<T, HD, NT, NS>(c, q, row, n, heads, head, len, cnt, wc, scale, qf, qs, pos);
+  Running<HD, NT> run;
+  start(run);
+  if (kWhole && tid < 2) tail_bad[tid] = 0;
+  if (i0 < c1) place(0);
   __syncthreads();
+  auto use_block = [&](int it, int buf, float2 step, uint32_t bad) __attribute__((always_inline)) {
+    int last[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) last[j] = pos[j] - it * kBlock;
+    // a tile's operands are read while the one before is used
+    v4f s[NT][4];
+    v8h a[2][KS];
+    auto read_keys = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+      for (int k = 0; k < KS; ++k) a[t & 1][k] = __builtin_bit_cast(v8h, lds[buf][(t * KS + k) * 64 + lane]);
+    };
+    read_keys(0);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      if (t < 3) read_keys(t + 1);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) s[j][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int x = 0; x < NS; ++x) s[j][t] = mma(a[t & 1][k], qf[j][k][x], s[j][t]);
+    }
+    reads_ahead<KS, KS * NT * NS, 4>();
+    // the wave's first column sees the fewest tokens
+    const bool hidden = it * kBlock + kBlock > len + wc / G + 1;
+    take_tokens<4, HD, NT, NS, 1, true>(run, s, step, qs, last, hidden, bad, [&](int d, int h, int) {
+      return __builtin_bit_cast(v8h, lds[buf][(4 * KS + 2 * d + h) * 64 + lane]);
+    });
+  };
   for (int it = i0; it < c1; ++it) {
     const int buf = (it - i0) & 1;
     const float2 step = step_next;
     if (it + 1 < c1) fetch(it + 1);
-    if (it < mine) {
-      int last[NT];
-#pragma unroll
-      for (int j = 0; j < NT; ++j) last[j] = pos[j] - it * kBlock;
-      // a tile's operands are read while the one before is used
-      v4f s[NT][4];
-      v8h a[2][KS];
-      auto read_keys = [&](int t) __attribute__((always_inline)) {
-#pragma unroll
-        for (int k = 0; k < KS; ++k) a[t & 1][k] = __builtin_bit_cast(v8h, lds[buf][(t * KS + k) * 64 + lane]);
-      };
-      read_keys(0);
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        if (t < 3) read_keys(t + 1);
-#pragma unroll
-        for (int j = 0; j < NT; ++j) s[j][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int k = 0; k < KS; ++k)
-#pragma unroll
-          for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int x = 0; x < NS; ++x) s[j][t] = mma(a[t & 1][k], qf[j][k][x], s[j][t]);
-      }
-      reads_ahead<KS, KS * NT * NS, 4>();
-      // the wave's first column sees the fewest tokens
-      const bool hidden = it * kBlock + kBlock > len + wc / G + 1;
-      take_tokens<4, HD, NT, NS, 1, true>(run, s, step, qs, last, hidden, 0u, [&](int d, int h, int) {
-        return __builtin_bit_cast(v8h, lds[buf][(4 * KS + 2 * d + h) * 64 + lane]);
-      });
-    }
+    if (it < mine) use_block(it, buf, step, 0u);
     if (it + 1 < c1) place(buf ^ 1);
     __syncthreads();
   }
-  if (i1 > full && full < mine) {
-    const int64_t th = c.tail_head(layer, c.sel[g] ^ (full != len / kBlock), c.tail_of[slot], head) * (kBlock * HD);
-    const int have = total - full * kBlock;
+  if (i1 > full) {
+    if constexpr (kWhole) {
+      const uint32_t bad = place_tail();
+      __syncthreads();
+      if (full < mine) use_block(full, 0, step_next, bad);
+    } else if (full < mine) {
+      const int64_t th = c.tail_head(layer, c.sel[g] ^ (full != len / kBlock), tail, head) * (kBlock * HD);
+      const int have = total - full * kBlock;
 #pragma unroll 1
-    for (int t0 = 0; t0 < have; t0 += 16)
-      take_tail<T, HD, NT, NS>((const T*)c.ktail + th, (const T*)c.vtail + th, t0, have, qf, qs, pos,
-                               full * kBlock, run);
+      for (int t0 = 0; t0 < have; t0 += 16)
+        take_tail<T, HD, NT, NS>((const T*)c.ktail + th, (const T*)c.vtail + th, t0, have, qf, qs, pos,
+                                 full * kBlock, run);
+    }
   }
   if (wc >= cols) return;
   finish(run);

@@ -322,6 +322,36 @@ def test_non_finite_values_behind_a_query(ctx, orc, bf16, H, Hkv, P, n, at):
         c.close()
 
 
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("hd", [64, 96, 128])
+def test_non_finite_values_in_the_newest_tokens(ctx, orc, bf16, hd):
+    """Prompts that end inside a block: a NaN or infinity of any of its tokens, in any dim, reaches the queries that
+    see the token.  The others are as without it, but for a step of bf16 or of the sums (the scale of the tokens,
+    a power of two, may be another)."""
+    torch = _torch()
+    rng = np.random.default_rng(hd)
+    H, Hkv, P, n = 8, 2, 64, 61
+    k, v, kd, vd = _kv(rng, 1, P + n, Hkv, hd, bf16)
+    q = torch.from_numpy(rng.standard_normal((1, n, H, hd))).cuda().to(kd.dtype)
+    new = lambda x: x[:, P:].contiguous()
+    c = _cache(ctx, H, Hkv, hd, P + n, 1, bf16)
+    c.append(0, kd[:, :P].contiguous(), vd[:, :P].contiguous())
+    c.advance()
+    clean = torch.zeros_like(q)
+    c.attention(0, q, clean, k=new(kd), v=new(vd))
+    for at in (0, 3, 4, 15, 16, 22, 31, 32, 41, 47, 48, 60):
+        for which, value in ((0, float("nan")), (1, float("inf")), (1, float("nan"))):
+            x = [kd.clone(), vd.clone()]
+            x[which][0, P + at, 1, (at * 37 + 5) % hd] = value
+            out = torch.zeros_like(q)
+            c.attention(0, q, out, k=new(x[0]), v=new(x[1]))
+            assert torch.isnan(out[0, at:, H // 2:].float()).all(), (at, which)
+            same, want = out.float(), clean.float()
+            same[0, at:, H // 2:] = want[0, at:, H // 2:]
+            assert ((same - want).abs() <= 2.0 ** (-7 if bf16 else -18) * (want.abs() + 1)).all(), (at, which)
+    c.close()
+
+
 def test_pages_beyond_32_bits(ctx, orc):
     """A cache of more than 2^32 bytes of keys: its last sequence's pages lie behind that."""
     torch = _torch()
