@@ -215,43 +215,58 @@ static void logits_as(const T* x, const T* E, int64_t M, int64_t d, int64_t V, f
   if (M <= 16 * MT && tiles >= 4 * (int64_t)n_cu) {
     const bool dense = bytes % 128 == 0 && M * bytes <= 160 * 1024;
     const unsigned half = std::min(two, (unsigned)n_cu);
+    constexpr int GS = MT == 8 ? 4 : 8;
     if constexpr (MT == 1) {
       if (lds <= 80 * 1024) {
         TMZ_WALK(1, 80, 8, 8, false, two);
         return;
       }
     }
-    if (dense && tiles > 8 * (int64_t)n_cu) {
-      TMZ_WALK(MT, 160, 16, 4, true, one);
-      return;
+    if constexpr (MT <= 4) {
+      if (dense && tiles > 8 * (int64_t)n_cu) {
+        TMZ_WALK(MT, 160, 16, 4, true, one);
+        return;
+      }
     }
     if (lds <= 160 * 1024) {
-      TMZ_WALK(MT, 160, 8, 8, false, half);
+      TMZ_WALK(MT, 160, 8, GS, false, half);
       return;
     }
-    if (dense) {
-      TMZ_WALK(MT, 160, 8, 8, true, half);
-      return;
+    if constexpr (MT <= 4) {
+      if (dense) {
+        TMZ_WALK(MT, 160, 8, GS, true, half);
+        return;
+      }
     }
   }
 #undef TMZ_WALK
-  const int mt = (int)((M + 16 * MT - 1) / (16 * MT));
-  // 64 vocabulary rows a work group where that still makes one for every compute unit (M = 32, 32003 x 1536:
-  // 501 work groups of 64 rows 24 us, 2001 of 16 rows 36)
-  if ((V + 63) / 64 * mt >= n_cu)
-    hipLaunchKernelGGL((k_logits<T, MT, 4>), dim3((unsigned)((V + 63) / 64 * mt)), dim3(256), 0, s, x, E, M, d,
-                       V, out, mt);
-  else
-    hipLaunchKernelGGL((k_logits<T, MT, 1>), dim3((unsigned)((V + 15) / 16 * mt)), dim3(256), 0, s, x, E, M, d,
-                       V, out, mt);
+  if constexpr (MT <= 4) {
+    const int mt = (int)((M + 16 * MT - 1) / (16 * MT));
+    // 64 vocabulary rows a work group where that still makes one for every compute unit (M = 32, 32003 x 1536:
+    // 501 work groups of 64 rows 24 us, 2001 of 16 rows 36)
+    if ((V + 63) / 64 * mt >= n_cu)
+      hipLaunchKernelGGL((k_logits<T, MT, 4>), dim3((unsigned)((V + 63) / 64 * mt)), dim3(256), 0, s, x, E, M, d,
+                         V, out, mt);
+    else
+      hipLaunchKernelGGL((k_logits<T, MT, 1>), dim3((unsigned)((V + 15) / 16 * mt)), dim3(256), 0, s, x, E, M, d,
+                         V, out, mt);
+  }
 }
 
 hipError_t launch_logits(const void* x, const void* E, termezo_dtype dt, int64_t M, int64_t d,
                          int64_t V, float* out, int n_cu, hipStream_t s) {
+  const int64_t tiles = (V + 15) / 16, bytes = M * d * (dt == TERMEZO_BF16 ? 2 : 4);
+  // rows of x a work group takes: fewer where that still makes no more than one for every compute unit (64 rows,
+  // d = 2560 in bf16, 1000 vocabulary rows: 64 at a time 14.8 us, 32 9.7, 16 7.6; 4000: 18.1, 18.1, 21.3)
+  int mt = M <= 16 ? 1 : M <= 32 ? 2 : 4;
+  while (mt > 1 && tiles * ((M + 8 * mt - 1) / (8 * mt)) <= n_cu) mt /= 2;
+  // all of them, up to 128, if they fit LDS (70 rows of 512 in bf16, 32000 vocabulary rows: 25 -> 16 us; 128: 27 -> 22)
+  if (M > 64 && M <= 128 && bytes + 16 * M <= 160 * 1024 && tiles >= 4 * (int64_t)n_cu) mt = 8;
 #define TMZ_LOGITS(T)                                                                     \
-  if (M <= 16) logits_as<T, 1>((const T*)x, (const T*)E, M, d, V, out, n_cu, s);          \
-  else if (M <= 32) logits_as<T, 2>((const T*)x, (const T*)E, M, d, V, out, n_cu, s);     \
-  else logits_as<T, 4>((const T*)x, (const T*)E, M, d, V, out, n_cu, s)
+  if (mt == 1) logits_as<T, 1>((const T*)x, (const T*)E, M, d, V, out, n_cu, s);          \
+  else if (mt == 2) logits_as<T, 2>((const T*)x, (const T*)E, M, d, V, out, n_cu, s);     \
+  else if (mt == 4) logits_as<T, 4>((const T*)x, (const T*)E, M, d, V, out, n_cu, s);     \
+  else logits_as<T, 8>((const T*)x, (const T*)E, M, d, V, out, n_cu, s)
   if (dt == TERMEZO_BF16) {
     TMZ_LOGITS(uint16_t);
   } else {

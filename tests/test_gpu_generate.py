@@ -591,7 +591,8 @@ def test_cache_refusals(ctx, orc):
                                    (5, 272, 16411), (20, 2576, 16411), (32, 2560, 16411), (45, 1536, 16411),
                                    (64, 1280, 16411), (64, 640, 16411), (16, 5120, 16411), (16, 2560, 33001),
                                    (32, 1280, 33001), (64, 640, 40001), (24, 16, 32801), (40, 80, 16501),
-                                   (3, 2560, 16383)])
+                                   (3, 2560, 16383), (70, 256, 16411), (128, 512, 16501), (97, 272, 33001),
+                                   (64, 512, 1000), (128, 80, 1003), (65, 1264, 16400), (70, 1168, 16400)])
 def test_logits(ctx, orc, bf16, M, d, V):
     torch = _torch()
     g = torch.Generator().manual_seed(M * d + V)
