@@ -519,8 +519,8 @@ __global__ void __launch_bounds__(256) k_cache_read(CacheView c, int layer, int6
 // is scaled by a power of two to a largest magnitude in [512, 1024) and rounded to fp16 (2^-11; one
 // rounding less than the bf16 that the rotated query would be stored in); fp32 activations take it in
 // two parts (2^-22).  Probabilities are scaled to at most 2^15 and rounded to fp16, again in two parts
-// for fp32.  Maxima, sums and outputs are fp32.  O is kept in units of the largest step of the values so
-// far: a block's probabilities take the ratio of its step to that one.  The newest tokens, not
+// for fp32.  Maxima, sums and outputs are fp32.  O is kept in units of a step of the values so
+// far: a block's probabilities take the ratio of its step to that one (take_tokens).  The newest tokens, not
 // coded yet, pass the same way: scaled by powers of two to magnitudes below 128, bf16 values are exact in
 // fp16 and fp32 ones taken in two parts.
 //
@@ -640,7 +640,7 @@ template <int HD, int NT>
 struct Running {
   float m[NT], l[NT];                 // l: this lane's tokens only
   v4f o[NT][HD / 16];
-  float unit;                         // of o: the largest step of the values so far (0: none)
+  float unit, top;                    // of o: a step of the values so far (0: none); the largest of them
 };
 
 // Keeps the compiler to the order written: READS shared-memory reads, then N - 1 times as many again before
@@ -659,6 +659,7 @@ __device__ __forceinline__ void reads_ahead() {
 
 template <int NS>
 constexpr float kScaleBits = NS == 1 ? 7.0f : 15.0f;
+constexpr float kNearStep = 0x1p-4f, kLostStep = 0x1p-80f;
 
 // Takes TT tiles of 16 tokens in (a block: 4): s[j][t] the products of column tile j with tokens
 // 16 t + 4 (lane / 16) + r, step their steps, qf the columns' factors, last[j] the last of the tokens that the
@@ -670,7 +671,10 @@ constexpr float kScaleBits = NS == 1 ? 7.0f : 15.0f;
 // lags behind it by up to 8 (bf16, bits 7: at most 2^15 either way), so that o is seldom rescaled (152 -> 149 us
 // for the ragged prompt batch, with the sums by dot products).  They take the ratio of the values' step to the
 // unit of o as a summand of the exponent (a fused multiply-add a score either way), and their sum takes its
-// inverse.
+// inverse.  The unit is the largest step so far, but falls to that of a block whose step is below kNearStep of it,
+// so that the ratio is never less: the largest weight is then 2^3 at least, and fp16's floor of 2^-25 is 2^-28 of it.
+// Rescaled for such falls, o (at most 2^24 tokens x 2^15 x 127 of the largest unit) stays within fp32 down to kLostStep
+// of the largest; blocks of still smaller steps (zeros, whose step is 1e-30 / 127, among them) count in l alone.
 template <int TT, int HD, int NT, int NS, int NV, bool AHEAD, typename Values>
 __device__ __forceinline__ void take_tokens(Running<HD, NT>& run, v4f (&s)[NT][TT], float2 step,
                                             const float (&qf)[NT], const int (&last)[NT], bool hidden,
@@ -679,13 +683,15 @@ __device__ __forceinline__ void take_tokens(Running<HD, NT>& run, v4f (&s)[NT][T
   const int tok = (threadIdx.x & 63) >> 4 << 2;
   const bool nan = !(step.x < INFINITY) || !(step.y < INFINITY);
   const float vstep = nan ? 0.0f : step.y;
-  const float unit = fmaxf(run.unit, vstep);
+  const bool far = !nan && vstep < run.unit * kNearStep, lost = !nan && vstep < run.top * kLostStep;
+  const float unit = lost ? run.unit : far ? vstep : fmaxf(run.unit, vstep);
   const float ru = __builtin_amdgcn_rcpf(unit);
-  const float ratio = vstep > 0.0f ? vstep * ru : 1.0f;
-  const float shrink = unit > run.unit ? run.unit * ru : 1.0f;
+  const float ratio = nan || lost ? 1.0f : vstep * ru;
+  const float shrink = unit != run.unit ? run.unit * ru : 1.0f;
   const float lr = __builtin_amdgcn_logf(ratio);         // log2
   const float inverse = __builtin_amdgcn_rcpf(ratio);
   run.unit = unit;
+  run.top = fmaxf(run.top, vstep);
   if (nan || bad)
 #pragma unroll
     for (int j = 0; j < NT; ++j)
@@ -704,7 +710,7 @@ __device__ __forceinline__ void take_tokens(Running<HD, NT>& run, v4f (&s)[NT][T
           if (t * 16 + tok + r > last[j]) s[j][t][r] = -INFINITY;
   v8h p[NT][HH][NS];
   float al[NT];
-  bool same = shrink == 1.0f;
+  bool same = shrink == 1.0f && !lost;
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
     const float f = nan ? 1.0f : qf[j] * step.x;
@@ -746,6 +752,13 @@ __device__ __forceinline__ void take_tokens(Running<HD, NT>& run, v4f (&s)[NT][T
     for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int d = 0; d < HD / 16; ++d) run.o[j][d] *= al[j];
+    if (lost)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int h = 0; h < HH; ++h)
+#pragma unroll
+          for (int b = 0; b < NS; ++b) p[j][h][b] = v8h{};
   }
   auto use = [&](v8h v, int d, int h, int a) __attribute__((always_inline)) {
 #pragma unroll
@@ -887,7 +900,7 @@ __device__ __forceinline__ void load_columns(const CacheView& c, const T* q, int
 
 template <int HD, int NT>
 __device__ __forceinline__ void start(Running<HD, NT>& run) {
-  run.unit = 0.0f;
+  run.unit = run.top = 0.0f;
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
     run.m[j] = -INFINITY;
@@ -903,9 +916,9 @@ __device__ __forceinline__ void finish(Running<HD, NT>& run) {
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
     const float l = run.l[j] = col_sum(run.l[j]);
-    const float f = l == 0.0f ? 0.0f : run.unit / l;
+    const float f = l == 0.0f ? 0.0f : 1.0f / l;         // first: unit / l may be below the normal numbers
 #pragma unroll
-    for (int d = 0; d < HD / 16; ++d) run.o[j][d] *= f;
+    for (int d = 0; d < HD / 16; ++d) run.o[j][d] = run.o[j][d] * f * run.unit;
   }
 }
 

@@ -10,7 +10,9 @@ tokens; the result is rounded to its type.  So |error| <= half a step of |o| + (
 (T + 64) 2^-24 + 2^-20) sum p|v| + T 2^-40 (bf16: 2^-32) max|v|, 2^-20 for the exponentials.  The last term is that of
 weights too small for their type: the largest weight is 2^15 in fp16 (bf16: at least 2^7, the maximum may
 lag by 2^8), whose smallest step is 2^-24, so a weight is off by at most 2^-25 2^-15 = 2^-40 (bf16: 2^-32) of
-the largest one, which the sum of all is no less than."""
+the largest one, which the sum of all is no less than.  Weights carry the ratio of their block's step to the
+output's unit, 2^-4 at least: the same error in units of the largest value, but up to 2^4 times as much of the
+largest weight, which in the sum of bf16's weights as rounded is T 2^-28 |o| at most, below the T 2^-24 above."""
 import numpy as np
 import pytest
 
@@ -408,6 +410,122 @@ def test_extreme_scores(ctx, orc):
             s.append(k[r], v[r])
             _check_attention(s, q[r], out[r].float().cpu().numpy(), True)
         c.close()
+
+
+# Rows whose value blocks differ in size: the factor of each of 13 blocks (64 tokens) and of the new tokens.
+# Blocks 0, 4, 8, 12 fall to one wave where a row is not split, as with the 512 rows x heads below.
+STEPS = [
+    ([1, 0, 1, 0], 1.0),                                      # nothing behind ordinary values, and between them
+    ([0, 1, 0, 1], 1.0),
+    ([1, 2.0 ** -20, 2.0 ** -40, 0], 2.0 ** -40),             # falling, tiny new tokens
+    ([0, 2.0 ** -40, 2.0 ** -20, 1], 0.0),
+    ([2.0 ** 30, 0, 2.0 ** -40, 0], 0.0),                     # ratios outside fp32's normal numbers
+    ([2.0 ** -40] * 4, 1.0),
+    ([1, 2.0 ** -3, 2.0 ** -5, 2.0 ** -12], 2.0 ** -9),       # on both sides of what the weights can carry
+    ([2.0 ** -12, 1, 2.0 ** 12, 2.0 ** -30], 2.0 ** 12),
+]
+
+
+def _steps_row(r, P, n):
+    """Factors of the P cached tokens and the n new ones of row r."""
+    by_group, new = STEPS[r]
+    return np.repeat(np.float32([by_group[i // 4 % 4] for i in range(P // 64 + 1)]), 64)[:P].tolist() + [new] * n
+
+
+def _steps_bound(seq, q, bf16):
+    """What `_check_attention` allows, with the floor of the weights by token in place of the largest value
+    of the row: a weight carries the ratio of its block's step to the wave's unit, 2^-4 at least (smaller ratios
+    are multiplied in fp32 behind the products), so it is off by at most 2^-25 2^4 of its type's scale: 2^-28 of the
+    largest weight (bf16, at least 2^7), 2^-36 (fp32, 2^15), and never by more than itself.  A value of the
+    incomplete block is off by 2^-31 of the largest there in fp16, 2^-31 too in two parts' second."""
+    from oracle import generate_ref as ref
+    out, mag, big = ref.attend(seq, q)
+    n, H, hd = q.shape
+    T = len(seq)
+    k, v = (x.astype(np.float64) for x in seq.values())
+    late = np.arange(T)[None] > np.arange(T - n, T)[:, None]
+    tail = np.arange(T) >= T // 64 * 64
+    u = 2.0 ** -11 if bf16 else 2.0 ** -21
+    ds = (u + hd * 2.0 ** -24) * big
+    tol = (2.0 ** -8 if bf16 else 2.0 ** -24) * np.abs(out) \
+        + (np.expm1(2 * ds) + u + (T + 64) * 2.0 ** -24 + 2.0 ** -20) * mag + 1e-37
+    qr = ref.rotate(q, np.arange(T - n, T), seq.base).astype(np.float64)
+    for h in range(H):
+        g = h * k.shape[1] // H
+        s = np.where(late, -np.inf, qr[:, h] @ k[:, g].T / np.sqrt(hd))
+        p = np.exp(s - s.max(1, keepdims=True))
+        p /= p.sum(1, keepdims=True)
+        off = np.minimum(p, (2.0 ** -28 if bf16 else 2.0 ** -36) * p.max(1, keepdims=True))
+        tol[:, h] += off @ np.abs(v[:, g]) + off.sum(1, keepdims=True) * np.abs(out[:, h])
+        if tail.any():
+            tol[:, h] += p[:, tail].sum(1, keepdims=True) * 2.0 ** -31 * np.abs(v[tail, g]).max()
+    return out, tol
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("n", [1, 3, 80])
+def test_value_blocks_of_different_steps(ctx, orc, bf16, n):
+    """Scores close together, so that every block has its share: blocks of zeros and of tiny values before,
+    between and behind ordinary and large ones count in the denominator, and tiny ones in the output."""
+    torch = _torch()
+    from oracle import generate_ref as ref
+    rng = np.random.default_rng(40 + n)
+    H, hd, G, P = 64, 64, len(STEPS), 13 * 64 - 2
+    k, v, _, _ = _kv(rng, G, P + n, H, hd, bf16)
+    v = ref.to_type(v * np.float32([_steps_row(r, P, n) for r in range(G)])[:, :, None, None], bf16)
+    q = ref.to_type(rng.standard_normal((G, n, H, hd)) * 0.05, bf16)
+    dt = torch.bfloat16 if bf16 else torch.float32
+    kd, vd, qd = (torch.from_numpy(x).cuda().to(dt) for x in (k, v, q))
+    c = _cache(ctx, H, H, hd, P + n, G, bf16)
+    c.append(0, kd[:, :P].contiguous(), vd[:, :P].contiguous())
+    c.advance()
+    out = torch.zeros_like(qd)
+    c.attention(0, qd, out, k=kd[:, P:].contiguous(), v=vd[:, P:].contiguous())
+    got = out.float().cpu().numpy()
+    c.close()
+    for r in range(G):
+        s = ref.Sequence(bf16, 10000.0)
+        s.append(k[r], v[r])
+        want, tol = _steps_bound(s, q[r], bf16)
+        err = np.abs(got[r] - want)
+        assert (err <= tol).all(), (r, float((err / tol).max()))
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("n", [1, 3, 80])
+def test_one_token_of_a_small_block_takes_everything(ctx, orc, bf16, n):
+    """One score of 256 among zeros (the others' weights are e^-256): the output is that token's cached value
+    row, whatever its block's size.  Off by the output's rounding, the weight's roundings in numerator and
+    denominator (2^-11 each, bf16; 2^-21) and 2^-20 for the statistics."""
+    torch = _torch()
+    from oracle import generate_ref as ref
+    rng = np.random.default_rng(50 + n)
+    H, hd, G, P = 64, 64, len(STEPS), 13 * 64 - 2
+    dt = torch.bfloat16 if bf16 else torch.float32
+    v = rng.standard_normal((G, P + n, H, hd)).astype(np.float32)
+    v = ref.to_type(v * np.float32([_steps_row(r, P, n) for r in range(G)])[:, :, None, None], bf16)
+    sign = np.where(rng.random((G, 1, H, hd)) < 0.5, np.float32(-2.0), np.float32(2.0))
+    q = np.repeat(sign, n, 1)
+    vd, qd = (torch.from_numpy(x).cuda().to(dt) for x in (v, q))
+    for block in (0, 5, 8, 12):
+        at = block * 64 + 37
+        k = np.zeros_like(v)
+        k[:, at] = sign[:, 0] * 8                             # 64 products of 32, over 8
+        kd = torch.from_numpy(k).cuda().to(dt)
+        c = _cache(ctx, H, H, hd, P + n, G, bf16, base=0.0)
+        c.append(0, kd[:, :P].contiguous(), vd[:, :P].contiguous())
+        c.advance()
+        out = torch.zeros_like(qd)
+        c.attention(0, qd, out, k=kd[:, P:].contiguous(), v=vd[:, P:].contiguous())
+        got = out.float().cpu().numpy()
+        c.close()
+        for r in range(G):
+            s = ref.Sequence(bf16, 0.0)
+            s.append(k[r], v[r])
+            want = s.values()[1][at].astype(np.float64)
+            tol = (2.0 ** -8 + 2.0 ** -10 if bf16 else 2.0 ** -19) * np.abs(want)
+            tail = np.abs(s.values()[1][len(s) // 64 * 64:]).max(initial=0.0) if at >= len(s) // 64 * 64 else 0.0
+            assert (np.abs(got[r] - want) <= tol + 2.0 ** -31 * tail + 1e-37).all(), (r, block)
 
 
 @pytest.mark.parametrize("bf16,beams", [(True, 4), (False, 3), (True, 64)])
