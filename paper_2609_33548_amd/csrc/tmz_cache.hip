@@ -700,26 +700,30 @@ __device__ __forceinline__ void take_tokens(Running<HD, NT>& run, v4f (&s)[NT][T
 #pragma unroll
         for (int r = 0; r < 4; ++r)
           if (nan || (bad >> (t * 4 + r) & 1)) s[j][t][r] = __builtin_nanf("");
+  float f[NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) f[j] = nan ? 1.0f : qf[j] * step.x;
   if (hidden)
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+    for (int j = 0; j < NT; ++j) {
+      f[j] = fmaxf(f[j], 0x1p-126f);                     // -inf times 0 would be NaN
 #pragma unroll
       for (int t = 0; t < TT; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
           if (t * 16 + tok + r > last[j]) s[j][t][r] = -INFINITY;
+    }
   v8h p[NT][HH][NS];
   float al[NT];
   bool same = shrink == 1.0f && !lost;
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
-    const float f = nan ? 1.0f : qf[j] * step.x;
     float bm = s[j][0][0];
 #pragma unroll
     for (int t = 0; t < TT; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) bm = fmaxf(bm, s[j][t][r]);
-    bm = col_max(bm) * f;
+    bm = col_max(bm) * f[j];
     const float m = bm > run.m[j] + (15.0f - kScaleBits<NS>) ? bm : run.m[j];
     const float ref = m == -INFINITY ? 0.0f : m;
     al[j] = __builtin_amdgcn_exp2f(run.m[j] - ref);
@@ -732,7 +736,7 @@ __device__ __forceinline__ void take_tokens(Running<HD, NT>& run, v4f (&s)[NT][T
       float w[8];
 #pragma unroll
       for (int r = 0; r < 8; ++r) {
-        w[r] = 2 * h + r / 4 < TT ? __builtin_amdgcn_exp2f(fmaf(s[j][2 * h + r / 4 < TT ? 2 * h + r / 4 : 0][r % 4], f, off))
+        w[r] = 2 * h + r / 4 < TT ? __builtin_amdgcn_exp2f(fmaf(s[j][2 * h + r / 4 < TT ? 2 * h + r / 4 : 0][r % 4], f[j], off))
                                   : 0.0f;
         if (NS == 2) sum += w[r];
       }

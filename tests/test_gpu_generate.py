@@ -528,6 +528,34 @@ def test_one_token_of_a_small_block_takes_everything(ctx, orc, bf16, n):
             assert (np.abs(got[r] - want) <= tol + 2.0 ** -31 * tail + 1e-37).all(), (r, block)
 
 
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("P,n", [(62, 3), (10, 100), (100, 90)])
+def test_zero_keys_and_tiny_queries(ctx, orc, bf16, P, n):
+    """Blocks of zero keys (step 1e-30 / 127) with queries of 1e-12, whose product is below fp32's numbers, some
+    of their tokens behind a query: every score is 0, so the output is the mean of what is seen."""
+    torch = _torch()
+    from oracle import generate_ref as ref
+    rng = np.random.default_rng(60 + n)
+    H, Hkv, hd, G = 8, 2, 64, 2
+    dt = torch.bfloat16 if bf16 else torch.float32
+    k = np.zeros((G, P + n, Hkv, hd), np.float32)
+    v = ref.to_type(rng.standard_normal((G, P + n, Hkv, hd)), bf16)
+    q = ref.to_type(rng.standard_normal((G, n, H, hd)) * 1e-12, bf16)
+    q[1] = ref.to_type(q[1] * np.float32(1e-20), bf16)
+    kd, vd, qd = (torch.from_numpy(x).cuda().to(dt) for x in (k, v, q))
+    c = _cache(ctx, H, Hkv, hd, P + n, G, bf16)
+    c.append(0, kd[:, :P].contiguous(), vd[:, :P].contiguous())
+    c.advance()
+    out = torch.zeros_like(qd)
+    c.attention(0, qd, out, k=kd[:, P:].contiguous(), v=vd[:, P:].contiguous())
+    got = out.float().cpu().numpy()
+    c.close()
+    for r in range(G):
+        s = ref.Sequence(bf16, 10000.0)
+        s.append(k[r], v[r])
+        _check_attention(s, q[r], got[r], bf16)
+
+
 @pytest.mark.parametrize("bf16,beams", [(True, 4), (False, 3), (True, 64)])
 def test_fork_and_reorder(ctx, orc, bf16, beams):
     """A prompt once per search, then steps whose beams continue each other in every way, over block
