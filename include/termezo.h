@@ -478,6 +478,7 @@ termezo_status termezo_kvcache_append(termezo_kvcache* cache, int32_t layer, con
  * raise a deferred INVALID_ARG and leave their group's rows out.  A cached key or value
  * that is not finite makes the whole output (of its heads) NaN for every query that sees its
  * block, once that is complete, or its token, before; queries that do not are as without it.
+ * A query that is not finite has NaN for its own output.
  * Blocks whose largest value is below 2^-80 of another's of the row may count as zeros in out (their weights
  * count in full).
  * out must not overlap q, k or v.  Errors: INVALID_ARG (as append; one of k, v null), STATE (k and v null and

@@ -629,7 +629,8 @@ __device__ __forceinline__ float query_operand(const T* q, const float2* rope, f
 #pragma unroll
   for (int k = 0; k < HD / 32; ++k) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[k][j] = ldexpf(x[k][j], -e);
+    for (int j = 0; j < 8; ++j)                          // an infinity would leave scores of -inf alone, and no weight
+      x[k][j] = fabsf(x[k][j]) < INFINITY ? ldexpf(x[k][j], -e) : __builtin_nanf("");
     split_f16<NS>(x[k], f[k]);
   }
   return ldexpf(scale * kLog2e, e);

@@ -556,6 +556,34 @@ def test_zero_keys_and_tiny_queries(ctx, orc, bf16, P, n):
         _check_attention(s, q[r], got[r], bf16)
 
 
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("base", [0.0, 10000.0])
+@pytest.mark.parametrize("P,n", [(5, 1), (200, 1), (130, 3), (200, 80)])
+def test_non_finite_queries(ctx, orc, bf16, base, P, n):
+    """A query with an infinity (against keys that are all negative there, so every score is -inf) or NaN gives
+    NaN, its neighbours among the rows, queries and heads are as without it."""
+    torch = _torch()
+    rng = np.random.default_rng(70 + n)
+    H, Hkv, hd, G = 8, 2, 64, 2
+    k, v, kd, vd = _kv(rng, G, P + n, Hkv, hd, bf16)
+    kd[..., 5] = -kd[..., 5].abs() - 1
+    qd = torch.from_numpy(rng.standard_normal((G, n, H, hd))).cuda().to(kd.dtype)
+    c = _cache(ctx, H, Hkv, hd, P + n, G, bf16, base=base)
+    c.append(0, kd[:, :P].contiguous(), vd[:, :P].contiguous())
+    c.advance()
+    c.append(0, kd[:, P:].contiguous(), vd[:, P:].contiguous())
+    clean, out = torch.zeros_like(qd), torch.zeros_like(qd)
+    c.attention(0, qd, clean)
+    bad = torch.zeros((G, n, H), dtype=torch.bool, device="cuda")
+    for (r, i, h), x in (((0, n - 1, 2), float("inf")), ((1, 0, 7), float("-inf")), ((1, n // 2, 3), float("nan"))):
+        qd[r, i, h, 5] = x
+        bad[r, i, h] = True
+    c.attention(0, qd, out)
+    assert torch.isnan(out[bad]).all()
+    assert torch.equal(out[~bad], clean[~bad])
+    c.close()
+
+
 @pytest.mark.parametrize("bf16,beams", [(True, 4), (False, 3), (True, 64)])
 def test_fork_and_reorder(ctx, orc, bf16, beams):
     """A prompt once per search, then steps whose beams continue each other in every way, over block
