@@ -2447,18 +2447,15 @@ termezo_status termezo_model_decode(termezo_model* m, termezo_kvcache* kv, const
   chk(run_blocks(m, A, M, codes, betas, nrm, s, false, [&](int blk) {
     return cache_attention_on(kv, blk, A.q, A.k, A.v, n, kv->pend, A.attn, s);
   }));
-  // the last new token of every row: its hidden state (in A.q's place), norm and logits
-  const void* last = A.h;
-  if (n > 1 || counts) {
-    last = A.q;
+  // the last new token of every row: its hidden state (in A.q's place), norm and logits; zero for a row
+  // without one, with single tokens too (a full group has none)
 #define TMZ_LAST(T)                                                                               \
   hipLaunchKernelGGL(k_last_rows<T>, dim3((unsigned)rows), dim3(256), 0, s, (const T*)A.h, d, (int)n, \
                      kv->width, kv->pend, (T*)A.q)
-    if (bf) TMZ_LAST(uint16_t); else TMZ_LAST(float);
+  if (bf) TMZ_LAST(uint16_t); else TMZ_LAST(float);
 #undef TMZ_LAST
-    chk(hipGetLastError());
-  }
-  chk(norm_rows(m, last, rows, nrm, 2 * cf.n_blocks, A, A.xf, false, s));
+  chk(hipGetLastError());
+  chk(norm_rows(m, A.q, rows, nrm, 2 * cf.n_blocks, A, A.xf, false, s));
   chk(launch_logits(A.xf, emb, cf.act_dtype, rows, d, cf.vocab, logits, c->n_cu, s));
   chk(cache_advance_on(kv, s));
   return e == hipSuccess ? TERMEZO_OK : failed();

@@ -1124,6 +1124,40 @@ def test_beam_search_together(orc):
     ctx.close()
 
 
+@pytest.mark.parametrize("bf16", [False, True])
+def test_decode_of_a_full_group(orc, bf16):
+    """One token past max_len in a ragged batch, counts not given: the full group's logits are 0, the other
+    groups' are those of a step that leaves it out, and the next wait reports it."""
+    torch = _torch()
+    from oracle import decoder_ref as dec
+    from paper_2609_33548_amd import synth, termezo as T
+    cfg = dec.DecoderConfig(n_blocks=2, d_model=256, n_heads=4, n_kv_heads=2, d_ffn=688, vocab=512, bf16=bf16)
+    ref, ctx, model, emb, E, w = _decoder(orc, cfg, 90)
+    ctx.perturb(4, 1e-3, 1)
+    G, N = 3, 20
+    tok = torch.from_numpy(synth.tokens(91, G, N + 1, cfg.vocab)).cuda()
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    for lens in ([20, 12, 7], [9, 20, 20]):
+        caches = [_model_cache(ctx, cfg, N, G) for _ in range(2)]
+        got, want = (torch.full((G, cfg.vocab), 7.0, device="cuda") for _ in range(2))
+        for c in caches:
+            model.decode(c, tok[:, :N].contiguous(), got, counts=i32(*lens))
+        step = tok[:, N:].contiguous()
+        model.decode(caches[0], step, want, counts=i32(*(int(x < N) for x in lens)))
+        ctx.sync()
+        model.decode(caches[1], step, got)
+        for r, x in enumerate(lens):
+            assert torch.equal(got[r], torch.zeros_like(got[r]) if x == N else want[r]), r
+        with pytest.raises(T.TermezoError) as e:
+            ctx.sync()
+        assert e.value.status == T.ERR_INVALID_ARG
+        assert caches[1].lengths().tolist() == [min(N, x + 1) for x in lens]
+        for c in caches:
+            c.close()
+    model.close()
+    ctx.close()
+
+
 def test_decode_captured_and_refused(orc):
     """A step captured and replayed equals the eager steps; another model's cache, pending tokens,
     bad ids and missing codes are refused."""
