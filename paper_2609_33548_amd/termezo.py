@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import atexit
 import ctypes
+import operator
 import os
 import sys
 import weakref
@@ -158,6 +159,14 @@ def _tensor(t, name, shape, dtype, device):
         raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on {device}, not "
                          f"{t.dtype} {list(t.shape)} on {t.device}")
     return t.data_ptr()
+
+
+def _int(v, name, bits: int = 32) -> int:
+    """An integer that its C type holds (ctypes would wrap it around)."""
+    v = operator.index(v)
+    if not -(1 << (bits - 1)) <= v < 1 << (bits - 1):
+        raise ValueError(f"{name} = {v} does not fit {bits} bits")
+    return v
 
 
 def _stream_handle(stream) -> Optional[int]:
@@ -415,6 +424,7 @@ class Context:
         and out_parents int32, all [groups, n_out]; finished uint8 [groups, beams] and out_finished
         [groups, n_out]; history int32 [groups, beams, T] and out_history [groups, n_out, T + 1]."""
         import torch
+        eos = _int(eos, "eos")
         B, W, V = logits.shape
         n = out_scores.shape[-1]
         f32, i32, u8 = torch.float32, torch.int32, torch.uint8
@@ -445,7 +455,9 @@ class KVCache:
             raise TypeError(f"unsupported dtype {dtype}")
         self.groups, self.beams, self._width = groups, beams, 1
         self.n_heads, self.n_kv_heads, self.head_dim, self.max_len = n_heads, n_kv_heads, head_dim, max_len
-        cfg = KVCacheConfig(n_layers, n_heads, n_kv_heads, head_dim, groups, beams, max_len, rope_base,
+        sizes = dict(n_layers=n_layers, n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim, groups=groups,
+                     beams=beams)
+        cfg = KVCacheConfig(*(_int(x, name) for name, x in sizes.items()), _int(max_len, "max_len", 64), rope_base,
                             F32 if dtype == torch.float32 else BF16)
         out = _P()
         ctx._check(_lib.termezo_kvcache_create(ctx.handle, ctypes.byref(cfg), ctypes.byref(out)),
@@ -471,7 +483,7 @@ class KVCache:
         become pending in one layer."""
         n = k.shape[1]
         self.ctx._check(_lib.termezo_kvcache_append(
-            self.handle, layer, self._heads(k, "k", self.n_kv_heads, n),
+            self.handle, _int(layer, "layer"), self._heads(k, "k", self.n_kv_heads, n),
             self._heads(v, "v", self.n_kv_heads, n), n, self._counts(counts)), "kvcache_append")
 
     def attention(self, layer: int, q, out, k=None, v=None, counts=None):
@@ -480,7 +492,7 @@ class KVCache:
         n = q.shape[1]
         opt = lambda t, name: None if t is None else self._heads(t, name, self.n_kv_heads, n)
         self.ctx._check(_lib.termezo_kvcache_attention(
-            self.handle, layer, self._heads(q, "q", self.n_heads, n), opt(k, "k"), opt(v, "v"), n,
+            self.handle, _int(layer, "layer"), self._heads(q, "q", self.n_heads, n), opt(k, "k"), opt(v, "v"), n,
             self._counts(counts), self._heads(out, "out", self.n_heads, n)), "kvcache_attention")
 
     def advance(self):
@@ -488,7 +500,7 @@ class KVCache:
         self.ctx._check(_lib.termezo_kvcache_advance(self.handle), "kvcache_advance")
 
     def reset(self, group: int = -1):
-        self.ctx._check(_lib.termezo_kvcache_reset(self.handle, group), "kvcache_reset")
+        self.ctx._check(_lib.termezo_kvcache_reset(self.handle, _int(group, "group")), "kvcache_reset")
         if group < 0:
             self._width = 1
 
@@ -517,7 +529,7 @@ class KVCache:
         ptr = lambda t, name: None if t is None else _tensor(
             t, name, (self.rows, n, self.n_kv_heads, self.head_dim), some.dtype, self.ctx.device)
         self.ctx._check(_lib.termezo_kvcache_read(
-            self.handle, layer, first, n, ptr(k_out, "k_out"), ptr(v_out, "v_out"), _dtype_code(some)),
+            self.handle, _int(layer, "layer"), _int(first, "first", 64), n, ptr(k_out, "k_out"), ptr(v_out, "v_out"), _dtype_code(some)),
             "kvcache_read")
 
     def lengths(self) -> np.ndarray:

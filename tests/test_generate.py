@@ -134,6 +134,39 @@ def test_binding_refuses_wrong_tensors():
         T._tensor(x, "x", (2, 3, 4), torch.float32, torch.device("cuda", 0))
 
 
+def test_binding_refuses_integers_that_would_wrap():
+    """A layer, group, size or token id beyond the C types must not arrive as another one."""
+    import torch
+    from paper_2609_33548_amd import termezo as T
+
+    class Ctx:
+        device, handle = torch.device("cpu"), None
+
+        def _check(self, st, what):
+            if st != T.OK:
+                raise T.TermezoError(st, what)
+
+    c = T.KVCache.__new__(T.KVCache)
+    c.ctx, c.handle, c.dtype, c.groups, c.beams, c._width = Ctx(), None, torch.float32, 1, 1, 1
+    c.n_heads, c.n_kv_heads, c.head_dim, c.max_len = 2, 2, 64, 8
+    x = torch.zeros(1, 3, 2, 64)
+    for big in (1 << 32, -(1 << 32), (1 << 31), (1 << 64) + 1):
+        for f in (lambda: c.append(big, x, x), lambda: c.attention(big, x, x.clone()), lambda: c.read(big, 0, x),
+                  lambda: c.reset(big), lambda: T.KVCache(Ctx(), big, 2, 2, 64, 8, 1),
+                  lambda: T.KVCache(Ctx(), 1, 2, 2, 64, 8, big), lambda: T.KVCache(Ctx(), 1, 2, 2, 64, 8, 1, big),
+                  lambda: T.KVCache(Ctx(), 1, big, 2, 64, 8, 1), lambda: T.KVCache(Ctx(), 1, 2, 2, big, 8, 1),
+                  lambda: T.Context.beam_select(Ctx(), x, x[..., 0].contiguous(), x[:, :1, 0].contiguous(), None, None,
+                                                eos=big)):
+            with pytest.raises(ValueError, match="32 bits"):
+                f()
+    for big in (1 << 63, (1 << 64) + 5):
+        for f in (lambda: c.read(0, big, x), lambda: T.KVCache(Ctx(), 1, 2, 2, 64, big, 1)):
+            with pytest.raises(ValueError, match="64 bits"):
+                f()
+    with pytest.raises(T.TermezoError):                      # what fits goes on to the library
+        c.append(-1, x, x)
+
+
 def test_null_handles_are_rejected():
     from paper_2609_33548_amd import termezo as T
     import ctypes
