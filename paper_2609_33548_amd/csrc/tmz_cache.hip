@@ -1524,6 +1524,7 @@ termezo_status cfail(termezo_kvcache* c, termezo_status st, const char* msg) {
 
 termezo_status hip_status(termezo_kvcache* c, hipError_t e, const char* what) {
   if (e == hipSuccess) return TERMEZO_OK;
+  (void)hipGetLastError();                               // reported here, not by the next launch
   c->ctx->last_error = std::string(what) + ": " + hipGetErrorString(e);
   return e == hipErrorOutOfMemory ? TERMEZO_ERR_OOM : TERMEZO_ERR_DEVICE;
 }

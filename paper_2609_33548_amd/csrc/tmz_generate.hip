@@ -650,6 +650,7 @@ termezo_status gfail(termezo_ctx* c, const char* msg) {
 }
 termezo_status hip_status(termezo_ctx* c, hipError_t e, const char* what) {
   if (e == hipSuccess) return TERMEZO_OK;
+  (void)hipGetLastError();                               // reported here, not by the next launch
   c->last_error = std::string(what) + ": " + hipGetErrorString(e);
   return e == hipErrorOutOfMemory ? TERMEZO_ERR_OOM : TERMEZO_ERR_DEVICE;
 }

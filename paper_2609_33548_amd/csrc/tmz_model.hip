@@ -1924,6 +1924,7 @@ termezo_status model_reserve(termezo_model* m, int64_t M, int S) {
   A((void**)&m->loss64, 8);
   A((void**)&m->loss32, 4);
   if (e != hipSuccess) {
+    (void)hipGetLastError();                  // reported here, not by the next launch
     model_free_buffers(m);
     return e == hipErrorOutOfMemory ? TERMEZO_ERR_OOM : TERMEZO_ERR_DEVICE;
   }
@@ -2409,6 +2410,7 @@ termezo_status termezo_model_decode(termezo_model* m, termezo_kvcache* kv, const
     if (e == hipSuccess) e = x;
   };
   auto failed = [&]() {
+    (void)hipGetLastError();                  // reported here, not by the next launch
     c->last_error = std::string("model_decode: ") + hipGetErrorString(e);
     return e == hipErrorOutOfMemory ? TERMEZO_ERR_OOM : TERMEZO_ERR_DEVICE;
   };

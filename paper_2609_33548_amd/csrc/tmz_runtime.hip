@@ -46,6 +46,7 @@ termezo_status fail(termezo_ctx* c, termezo_status st, const std::string& msg) {
 }
 
 termezo_status hip_fail(termezo_ctx* c, hipError_t e, const char* what) {
+  (void)hipGetLastError();                               // reported here, not by the next launch
   const termezo_status st = e == hipErrorOutOfMemory ? TERMEZO_ERR_OOM : TERMEZO_ERR_DEVICE;
   return fail(c, st, std::string(what) + ": " + hipGetErrorString(e));
 }

@@ -681,6 +681,29 @@ def test_captured_steps(ctx, orc):
         own.close()
 
 
+def test_calls_after_a_cache_that_does_not_fit(ctx, orc):
+    """A cache beyond the device's memory is refused (8 TB: its first allocation fails), and the calls that
+    follow, the framework's and torch's, do not report its error again."""
+    torch = _torch()
+    from paper_2609_33548_amd import termezo as T
+    rng = np.random.default_rng(15)
+    k, v, kd, vd = _kv(rng, 1, 3, 2, 64, True)
+    c = _cache(ctx, 2, 2, 64, 10, 1, True)
+    for _ in range(2):
+        with pytest.raises(T.TermezoError) as e:
+            T.KVCache(ctx, 60, 8, 8, 128, 1 << 20, 64)
+        assert e.value.status == T.ERR_OOM
+        c.append(0, kd, vd)
+        c.advance()
+        with pytest.raises(T.TermezoError) as e:
+            T.KVCache(ctx, 60, 8, 8, 128, 1 << 20, 64)
+        assert (torch.ones(3, device="cuda") + 1).tolist() == [2.0] * 3
+        _cache(ctx, 2, 2, 64, 10, 1, True).close()
+    assert c.lengths().tolist() == [6]
+    ctx.sync()
+    c.close()
+
+
 def test_cache_refusals(ctx, orc):
     torch = _torch()
     from paper_2609_33548_amd import termezo as T
