@@ -222,7 +222,7 @@ struct termezo_ctx {
   bool has_mask = false;
   bool codes_valid = false;
   bool pending_perturb = false;
-  void* d_beam = nullptr;            // beam selection: the chunks' candidates, maxima and sums
+  void* d_beam = nullptr;            // beam selection: the scan's maxima and sums, the segments' maxima
   int64_t beam_cap = 0;              // its bytes
   bool beam_held = false;            // a captured graph uses it
   std::vector<void*> held;           // outgrown ones that graphs use, freed with the context
@@ -378,7 +378,6 @@ struct termezo_kvcache {
   int32_t *tail_of = nullptr, *table = nullptr;                 // [slots], [slots][max_blocks]
   float2* rope = nullptr;                                       // [max_len][head_dim / 2]
   float* part = nullptr;             // partial results of attention split over the tokens
-  int64_t part_floats = 0;
 };
 
 namespace tmz {
