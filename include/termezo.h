@@ -544,7 +544,8 @@ termezo_status termezo_beam_select(termezo_ctx* ctx, const float* logits, const 
  * appended to it and advanced; logits [rows][vocab] fp32 (16-byte aligned) of each row's last
  * new token (0 for rows without one).  The cache's layers, heads, head size
  * and act_dtype must be the model's, its rope_base too.  Token ids are checked as in
- * termezo_model_loss.  The call allocates activations when rows * n exceeds every earlier
+ * termezo_model_loss; registered theta tensors are read at their values at the time of the call (a snapshot
+ * holds codes and scales alone).  The call allocates activations when rows * n exceeds every earlier
  * call's.  A model with a stream of its own runs all of this there, the cache's work too:
  * termezo_model_join before other calls on the cache or the logits.
  * Errors: INVALID_ARG (2^24 tokens or more), STATE (no current codes; tokens pending; captured, with

@@ -681,6 +681,83 @@ def test_captured_steps(ctx, orc):
         own.close()
 
 
+def test_a_group_begins_again_among_beams(ctx, orc):
+    """After a fork one group is emptied and takes new prompts, another for each beam, while the other group goes
+    on; then both step and reorder over a block border."""
+    torch = _torch()
+    from oracle import generate_ref as ref
+    rng = np.random.default_rng(16)
+    H, Hkv, hd, G, W = 4, 2, 64, 2, 3
+    c = _cache(ctx, H, Hkv, hd, 160, G, True, beams=W)
+    k, v, kd, vd = _kv(rng, G, 70, Hkv, hd, True)
+    c.append(0, kd, vd)
+    c.advance()
+    c.fork()
+    beam = [ref.Sequence(True, 10000.0) for _ in range(G * W)]
+    for r in range(G * W):
+        beam[r].append(k[r // W], v[r // W])
+    c.reorder(torch.tensor([[2, 0, 1], [1, 1, 0]], dtype=torch.int32, device="cuda"))
+    c.reset(0)
+    for r in range(W):
+        beam[r] = ref.Sequence(True, 10000.0)
+    for n, counts in ((61, [61, 0]), (2, [2, 2]), (2, [2, 1]), (1, [1, 1]), (1, [0, 1])):
+        k, v, kd, vd = _kv(rng, G * W, n, Hkv, hd, True)
+        q = ref.to_type(rng.standard_normal((G * W, n, H, hd)), True)
+        out = torch.full((G * W, n, H, hd), 7.0, device="cuda").bfloat16()
+        cd = torch.tensor(counts, dtype=torch.int32, device="cuda")
+        c.attention(0, torch.from_numpy(q).cuda().bfloat16(), out, k=kd, v=vd, counts=cd)
+        c.advance()
+        got = out.float().cpu().numpy()
+        for r in range(G * W):
+            m = counts[r // W]
+            assert (got[r, m:] == 7.0).all()
+            if m:
+                beam[r].append(k[r, :m], v[r, :m])
+                _check_attention(beam[r], q[r, :m], got[r, :m], True)
+        parents = rng.integers(0, W, (G, W))
+        c.reorder(torch.from_numpy(parents.astype(np.int32)).cuda())
+        beam = [beam[g * W + p].copy() for g in range(G) for p in parents[g]]
+        _check_values(c, beam)
+    c.close()
+
+
+def test_one_beam_and_as_many_groups_as_there_may_be(ctx, orc):
+    """65535 rows of one beam: appended, attended at one and several tokens, reordered (each onto itself)."""
+    torch = _torch()
+    from oracle import generate_ref as ref
+    from paper_2609_33548_amd import termezo as T
+    rng = np.random.default_rng(17)
+    G, H, hd = 65535, 2, 64
+    c = _cache(ctx, H, 1, hd, 66, G, True)
+    counts = torch.full((G,), 62, dtype=torch.int32, device="cuda")
+    counts[1::2] = 0
+    g = torch.Generator(device="cuda").manual_seed(1)
+    draw = lambda *s: torch.randn(s, generator=g, device="cuda").bfloat16()
+    at = (0, 1, 32767, 32768, 65533, 65534)
+    refs = {r: ref.Sequence(True, 10000.0) for r in at}
+    host = lambda x: x.float().cpu().numpy()
+    k, v = draw(G, 62, 1, hd), draw(G, 62, 1, hd)
+    c.append(0, k, v, counts=counts)
+    c.advance()
+    for r in at:
+        if r % 2 == 0:
+            refs[r].append(host(k[r]), host(v[r]))
+    for n in (1, 3):
+        k, v, q = draw(G, n, 1, hd), draw(G, n, 1, hd), draw(G, n, H, hd)
+        out = torch.zeros_like(q)
+        c.attention(0, q, out, k=k, v=v)
+        c.advance()
+        c.reorder(torch.zeros((G, 1), dtype=torch.int32, device="cuda"))
+        for r in at:
+            refs[r].append(host(k[r]), host(v[r]))
+            _check_attention(refs[r], host(q[r]), host(out[r]), True)
+    with pytest.raises(T.TermezoError) as e:
+        c.fork()
+    assert e.value.status == T.ERR_STATE
+    ctx.sync()
+    c.close()
+
+
 def test_calls_after_a_cache_that_does_not_fit(ctx, orc):
     """A cache beyond the device's memory is refused (8 TB: its first allocation fails), and the calls that
     follow, the framework's and torch's, do not report its error again."""
@@ -1179,6 +1256,142 @@ def test_decode_of_a_full_group(orc, bf16):
             c.close()
     model.close()
     ctx.close()
+
+
+def test_decode_from_a_snapshot_on_its_own_stream(orc):
+    """The two signs of a perturbation generate at the same time, one from a snapshot of its codes on a
+    stream of its own: both sides' logits are those of one after the other, bit for bit."""
+    torch = _torch()
+    from oracle import decoder_ref as dec
+    from paper_2609_33548_amd import synth, termezo as T
+    cfg = dec.DecoderConfig(n_blocks=2, d_model=256, n_heads=4, n_kv_heads=2, d_ffn=688, vocab=512, bf16=True)
+    ref, ctx, model, emb, E, w = _decoder(orc, cfg, 94)
+    pair = T.Model(ctx, cfg.n_blocks, cfg.d_model, cfg.n_heads, cfg.n_kv_heads, cfg.d_ffn, cfg.vocab, E)
+    G, P, N = 3, 60, 12
+    tok = torch.from_numpy(synth.tokens(95, G, P + N, cfg.vocab)).cuda()
+    pieces = [tok[:, :P].contiguous()] + [tok[:, P + t:P + t + 1].contiguous() for t in range(N)]
+    new = lambda: [torch.zeros((G, cfg.vocab), device="cuda") for _ in pieces]
+    c = _model_cache(ctx, cfg, P + N, G)
+    want = {}
+    for sign in (1, -1):
+        ctx.perturb(3, 1e-2, sign)
+        want[sign] = new()
+        c.reset()
+        for x, l in zip(pieces, want[sign]):
+            model.decode(c, x, l)
+    assert not torch.equal(want[1][-1], want[-1][-1])
+    pair.use_snapshot(True)
+    with pytest.raises(T.TermezoError) as e:
+        pair.decode(c, pieces[1], want[1][0].clone())
+    assert e.value.status == T.ERR_STATE                     # no snapshot yet
+    pair.set_stream(torch.cuda.Stream())
+    d = _model_cache(ctx, cfg, P + N, G)
+    ctx.perturb(3, 1e-2, 1)
+    ctx.codes_snapshot()
+    got = {1: new(), -1: new()}
+    ctx.perturb(3, 1e-2, -1)
+    c.reset()
+    for i, x in enumerate(pieces):
+        pair.decode(d, x, got[1][i])
+        model.decode(c, x, got[-1][i])
+    pair.join()
+    ctx.sync()
+    for sign in (1, -1):
+        for i, (a, b) in enumerate(zip(got[sign], want[sign])):
+            assert torch.equal(a, b), (sign, i)
+    assert d.lengths().tolist() == [P + N] * G
+    for m in (pair, model):
+        m.close()
+    ctx.close()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_decode_reads_perturbed_parameters_and_norm_weights(orc, bf16):
+    """A registered embedding and RMSNorm weights enter the steps at their perturbed values, as in the batch
+    loss (the bars of the comparison within a block)."""
+    torch = _torch()
+    from oracle import decoder_ref as dec
+    from paper_2609_33548_amd import synth
+    cfg = dec.DecoderConfig(n_blocks=2, d_model=256, n_heads=4, n_kv_heads=2, d_ffn=688, vocab=1024, bf16=bf16)
+    ref, ctx, model, emb, E, w = _decoder(orc, cfg, 96)
+    rows = 2 * cfg.n_blocks + 1
+    NW = (torch.from_numpy(synth.activations(97, rows, cfg.d_model)).cuda() * 0.3 + 1.0).to(E.dtype)
+    model.set_norm_weights(NW)
+    ctx.theta_register([E, NW])
+    ctx.build_mask(0.01)
+    B, S = 3, 40
+    tok = synth.tokens(98, B, S, cfg.vocab)
+    tokd = torch.from_numpy(tok).cuda()
+    per = torch.empty(B * S, device="cuda")
+    c = _model_cache(ctx, cfg, S, B)
+    logits = torch.zeros((B, cfg.vocab), device="cuda")
+    seen = []
+    for sign in (1, -1):
+        ctx.perturb(5, 1e-2, sign)
+        model.loss(tokd, row_loss_dev=per)
+        want = per.cpu().numpy().reshape(B, S)
+        c.reset()
+        at = 0
+        for n in (17, 1, 1, 20):
+            model.decode(c, tokd[:, at:at + n].contiguous(), logits)
+            at += n
+            got = _log_prob_rows(logits.cpu().numpy(), tok[:, at].astype(np.int64))
+            rel = np.abs(got - want[:, at - 1]) / np.abs(want[:, at - 1])
+            assert rel.max() <= (5e-3 if bf16 else 1e-3), (sign, n, at, rel)
+        seen.append(logits.clone())
+    assert not torch.equal(*seen)
+    model.close()
+    ctx.close()
+
+
+def test_captured_beam_search(orc):
+    """A whole step of a beam search (decode, select, reorder) captured once and replayed over a block border,
+    between eager steps of the same search on other buffers."""
+    torch = _torch()
+    from oracle import decoder_ref as dec
+    from paper_2609_33548_amd import synth
+    cfg = dec.DecoderConfig(n_blocks=2, d_model=256, n_heads=4, n_kv_heads=2, d_ffn=688, vocab=700, bf16=True)
+    G, W, V, P, N = 2, 4, cfg.vocab, 61, 9
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        ref, ctx, model, emb, E, w = _decoder(orc, cfg, 99)
+        ctx.perturb(2, 1e-3, 1)
+        prompt = torch.from_numpy(synth.tokens(100, G, P, V)).cuda()
+        i32 = dict(dtype=torch.int32, device="cuda")
+
+        def search():
+            c = _model_cache(ctx, cfg, P + N + 2, G, beams=W)
+            first = torch.zeros((G, V), device="cuda")
+            model.decode(c, prompt, first)
+            c.fork()
+            scores = torch.full((G, W), -float("inf"), device="cuda")
+            scores[:, 0] = 0.0
+            b = dict(c=c, logits=first[:, None].repeat(1, W, 1).contiguous(), scores=scores,
+                     new=torch.zeros((G, W), device="cuda"), tok=torch.zeros((G, W), **i32), par=torch.zeros((G, W), **i32))
+            step(b)
+            return b
+
+        def step(b):
+            ctx.beam_select(b["logits"], b["scores"], b["new"], b["tok"], b["par"])
+            b["c"].reorder(b["par"])
+            b["scores"].copy_(b["new"])
+            model.decode(b["c"], b["tok"].view(-1, 1), b["logits"].view(G * W, V))
+        eager, other = search(), search()
+    stream.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        step(other)
+    with torch.cuda.stream(stream):
+        for t in range(N):
+            step(eager)
+            graph.replay()
+            if t % 3 == 1:
+                ctx.sync()
+            for x in ("logits", "scores", "tok", "par"):
+                assert torch.equal(eager[x], other[x]), (t, x)
+        assert eager["c"].lengths().tolist() == other["c"].lengths().tolist() == [P + N + 1] * G
+        model.close()
+        ctx.close()
 
 
 def test_decode_captured_and_refused(orc):
