@@ -523,6 +523,8 @@ termezo_status termezo_logits(termezo_ctx* ctx, const void* x, const void* E, te
  * finished (nullable, [groups][beams], nonzero: finished): a finished beam's logits are not
  * looked at, its only continuation is eos with its score unchanged.  A NaN logit counts as
  * -inf; beams whose logsumexp is not finite and NaN scores give continuations of score -inf.
+ * Scores are compared in fp64, but a logsumexp's exponentials are fp32 (it is off by up to 2^-21),
+ * so continuations of two beams closer than that may come in either order.
  * Outputs, [groups][n_out]: out_scores fp32, out_tokens and out_parents (the beam) int32,
  * out_finished (nullable; the parent was finished or the token is eos).  history (nullable,
  * int32 [groups][beams][hist_len]) and out_history [groups][n_out][hist_len + 1]: the

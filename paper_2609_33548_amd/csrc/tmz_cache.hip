@@ -528,8 +528,9 @@ __global__ void __launch_bounds__(256) k_cache_read(CacheView c, int layer, int6
 // step NaN, which is put into the scores of its visible tokens, and so is a new token whose value row
 // is not finite; weights of hidden tokens are zero and so are the value rows they meet.
 //
-// Bound by the bytes of the pages: 64 rows of 2000 to 4000 tokens (5 heads of 128, 253 MB) 50 us, 5.1 TB/s;
-// two rows of 131000 (336 MB) 62 us, 5.4 TB/s; the joining of their parts 5 and 6 us more.
+// Bound by the bytes of the pages: two rows of 131000 tokens (5 heads of 128, 336 MB) 62 us, 5.4 TB/s; 64 rows of
+// 3000 (249 MB) 61 us from memory, 4.1 TB/s, and 51 us where the 256 MB cache still holds them; the joining of
+// their parts 6 and 5 us more.  16 rows of 2000 with 4 and 8 new tokens (16 and 32 columns) 19 and 23 us, join 5.
 // ---------------------------------------------------------------------------
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
@@ -1085,8 +1086,10 @@ __global__ void __launch_bounds__(256, NT == 1 ? kRowsResident1 : kRowsResident2
 // of a key/value head, 32 a wave, so the blocks that it walks are converted to fp16 once, into
 // LDS, for all of them.  Two LDS buffers: while a block is used the next one's codes are on their way
 // in registers; the incomplete block passes the same way (bf16).  Four prompts of up to 2000
-// tokens, 20 heads of 128 on 5: 131 us, 0.57 PFLOP/s; the matrix cores are busy 28% of it, the vector units 52%
-// (exponentials, rescaling and the packing of weights), so those bound it.
+// tokens, 20 heads of 128 on 5: 122 us, 0.61 PFLOP/s; the matrix cores are busy 27% of it, the vector units 54%
+// (exponentials, rescaling and the packing of weights), and waves wait 28%: none is full, since a wave's scores,
+// exponentials and value product follow one another and registers leave two waves a SIMD.  fp32: four prompts of
+// 1000 77 us (two parts of everything; 8 registers spilled), eight of 512 with heads of 64 19 us, join 12.
 // grid (one dimension): key/value heads fastest, then rows, splits, tiles: the longest tiles of all rows first.
 // ---------------------------------------------------------------------------
 constexpr int kTileCols = 128;
