@@ -677,6 +677,8 @@ constexpr float kNearStep = 0x1p-4f, kLostStep = 0x1p-80f;
 // so that the ratio is never less: the largest weight is then 2^3 at least, and fp16's floor of 2^-25 is 2^-28 of it.
 // Rescaled for such falls, o (at most 2^24 tokens x 2^15 x 127 of the largest unit) stays within fp32 down to kLostStep
 // of the largest; blocks of still smaller steps (zeros, whose step is 1e-30 / 127, among them) count in l alone.
+// The fall costs the prompt batch 118 -> 122 us, 64 rows of 2000 to 4000 tokens none (66.7 -> 65.6); a second set of
+// products scaled in fp32 in its place spilled 26 to 140 registers.
 template <int TT, int HD, int NT, int NS, int NV, bool AHEAD, typename Values>
 __device__ __forceinline__ void take_tokens(Running<HD, NT>& run, v4f (&s)[NT][TT], float2 step,
                                             const float (&qf)[NT], const int (&last)[NT], bool hidden,

@@ -529,8 +529,8 @@ class KVCache:
         ptr = lambda t, name: None if t is None else _tensor(
             t, name, (self.rows, n, self.n_kv_heads, self.head_dim), some.dtype, self.ctx.device)
         self.ctx._check(_lib.termezo_kvcache_read(
-            self.handle, _int(layer, "layer"), _int(first, "first", 64), n, ptr(k_out, "k_out"), ptr(v_out, "v_out"), _dtype_code(some)),
-            "kvcache_read")
+            self.handle, _int(layer, "layer"), _int(first, "first", 64), n, ptr(k_out, "k_out"),
+            ptr(v_out, "v_out"), _dtype_code(some)), "kvcache_read")
 
     def lengths(self) -> np.ndarray:
         """Tokens of every group (waits for the stream)."""
