@@ -556,6 +556,90 @@ termezo_status termezo_model_decode(termezo_model* model, termezo_kvcache* cache
                                     const int32_t* tokens, int64_t n, const int32_t* counts,
                                     float* logits);
 
+/* ---- next tokens: products with 8-bit weights, rules on the logits, drawing ------
+ * These calls too return as soon as their work is queued on the context's stream and may be
+ * made while another device is current.  termezo_linear_i8 and termezo_sample keep scratch in
+ * the context, as termezo_beam_select does: it grows with the largest call, a captured call
+ * that would have to allocate is refused (STATE), and graphs stay valid when it grows later. */
+
+/* Rows of w [N][K] (F32 or BF16) in 8 bits: a = max(max |w|, 1e-30), codes[n][k] =
+ * rne(w * (127 / a)) and steps[n] = a / 127 (fp32, each operation rounded); a row with a value
+ * that is not finite has codes 0 and the step NaN.  codes int8 [N][K] (16-byte aligned), steps
+ * fp32 [N].  No output may overlap w.  Errors: INVALID_ARG (N 1 .. 2^24, K 1 .. 2^17 and a
+ * multiple of 16, dtype, null or misaligned (16 bytes; steps 4) pointers). */
+termezo_status termezo_quantize_rows(termezo_ctx* ctx, const void* w, termezo_dtype dtype, int64_t N,
+                                     int64_t K, int8_t* codes, float* steps);
+
+/* Product of M tokens with N rows of 8-bit weights: every row x of the input is taken in 8 bits
+ * (a = max(max |x|, 1e-5), q[k] = rne(x[k] * (127 / a)), as termezo_bitlinear_forward does),
+ * out[m][n] = (sum_k q[k] codes[n][k]) * ((a / 127) * steps[n]), the sum exact in int32, each
+ * fp32 operation rounded, then to out's type.  x [M][K] in xdt, out [M][N] in ydt (F32 or BF16
+ * each), codes int8 [N][K], -128 .. 127.  An input row with a value that is not finite has NaN
+ * in its whole output row.  out must not overlap an input.  Errors: INVALID_ARG (M 1 .. 2^24,
+ * N 1 .. 2^24, K 1 .. 2^17 and a multiple of 16, dtypes, null or misaligned (16 bytes; steps 4)
+ * pointers), STATE (captured, with scratch to be allocated), OOM. */
+termezo_status termezo_linear_i8(termezo_ctx* ctx, const void* x, termezo_dtype xdt, int64_t M, int64_t K,
+                                 const int8_t* codes, const float* steps, int64_t N, void* out,
+                                 termezo_dtype ydt);
+
+/* Rules on the logits of each row, all optional (null: the rule does not apply).  In this
+ * order, for token t, each fp32 operation rounded:
+ *   history [rows][hist_len] int32, of which the first lengths[r] (null: hist_len) count: a
+ *     token among them has its logit divided by repetition[r] where it is above 0, multiplied
+ *     by it where not; one that appears c > 0 times from place starts[r] (null: 0) on has
+ *     c * frequency[r], then presence[r] subtracted.  Ids outside [0, vocab) do not count.
+ *   bias [n_bias][vocab] fp32: line bias_index[r] is added (-1: none; null: line 0 if n_bias is
+ *     1, line r if it is rows).
+ *   mask [n_masks][(vocab + 31) / 32] 32-bit words: where bit t % 32 of word t / 32 of line
+ *     mask_index[r] (as bias_index) is 0, the logit becomes -inf, whatever it was.  A line
+ *     may leave nothing.
+ * Lengths outside 0 .. hist_len, starts outside 0 .. the length and indices outside -1 ..
+ * lines - 1 raise a deferred INVALID_ARG; their row is then taken without history, or line. */
+typedef struct {
+  const int32_t* history;
+  int64_t hist_len;
+  const int32_t *lengths, *starts;
+  const float *repetition, *presence, *frequency;   /* [rows]                       */
+  const float* bias;
+  int32_t n_bias;
+  const int32_t* bias_index;                        /* [rows]                       */
+  const uint32_t* mask;
+  int32_t n_masks;
+  const int32_t* mask_index;                        /* [rows]                       */
+} termezo_logit_rules;
+
+/* logits fp32 [rows][vocab] under the rules into out (the same array, or one that does not
+ * overlap it; neither may overlap the rules' arrays).  Errors: INVALID_ARG (rows 1 .. 65535, vocab 1 ..
+ * 2^24, hist_len 0 .. 2^24, null or misaligned (4 bytes) pointers, a table with no lines, or without
+ * indices and lines neither 1 nor rows, indices without a table). */
+termezo_status termezo_adjust_logits(termezo_ctx* ctx, const float* logits, int32_t rows, int32_t vocab,
+                                     const termezo_logit_rules* rules, float* out);
+
+/* One token for each row of logits (fp32 [rows][vocab]; NaN counts as -inf, +inf as the largest
+ * finite value).  Weights w = exp((x - max x) / temperature[r]) (null: 1).  In the order of
+ * falling logits, equal ones by index, a row keeps its first top_k[r] tokens (null, 0 or less:
+ * all), of these the ones with w >= min_p[r] (null or 0: all), of these the shortest beginning
+ * whose weights reach top_p[r] of the sum of them all (null or >= 1: all); the first one is
+ * always kept.  tokens[r] is the first kept token, by index, up to which the kept weights
+ * exceed uniforms[r] (in [0, 1)) times their sum; logprobs[r] (nullable) the logarithm of its
+ * share.  Temperature 0 keeps the first token alone.  Weights, shares and sums are fp64 or
+ * finer than 2^-38 of a sum; a weight below 2^-37 of a row's largest may count as zero.
+ * The result depends on nothing but the inputs.  A row without a logit above -inf has the token
+ * -1 and the log probability -inf.  Temperatures that are negative or not finite (read as 0),
+ * NaN limits (read as none) and random numbers outside [0, 1) (read as the nearest) raise a deferred
+ * INVALID_ARG.  No output may overlap an input.  Errors: INVALID_ARG (rows 1 .. 65535, vocab 1 .. 2^24,
+ * null or misaligned (4 bytes) pointers), STATE (captured, with scratch to be allocated), OOM. */
+termezo_status termezo_sample(termezo_ctx* ctx, const float* logits, const float* uniforms, int32_t rows,
+                              int32_t vocab, const float* temperature, const int32_t* top_k,
+                              const float* top_p, const float* min_p, int32_t* tokens, float* logprobs);
+
+/* The model's head in 8 bits: codes int8 [vocab][d_model] (16-byte aligned) and steps fp32
+ * [vocab] as termezo_quantize_rows leaves them, borrowed; termezo_model_decode then forms its
+ * logits as termezo_linear_i8 does (the losses keep the embedding).  Both null: the embedding again.
+ * Captured steps keep the head that they were captured with.  Errors:
+ * INVALID_ARG (one of them null, misaligned pointers). */
+termezo_status termezo_model_set_head(termezo_model* model, const int8_t* codes, const float* steps);
+
 /* ---- inspection and support calls (not part of the four hot-path calls) ---- */
 
 /* Wait for the context's stream; reports a deferred NUMERIC error. */

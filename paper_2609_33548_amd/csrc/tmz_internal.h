@@ -99,6 +99,13 @@ struct ThetaHost {
   void* minus;
 };
 
+// Scratch of the calls on a context that grows with the largest of them (scratch_for).
+struct Scratch {
+  void* p = nullptr;
+  int64_t cap = 0;                   // its bytes
+  bool held = false;                 // a captured graph uses it
+};
+
 struct SelectState {                 // radix-select bookkeeping (device)
   unsigned long long k0;             // budget
   unsigned long long less;           // keys strictly below the current prefix bucket
@@ -226,6 +233,7 @@ struct termezo_ctx {
   int64_t beam_cap = 0;              // its bytes
   bool beam_held = false;            // a captured graph uses it
   std::vector<void*> held;           // outgrown ones that graphs use, freed with the context
+  tmz::Scratch linear, draw;         // of termezo_linear_i8 (codes and steps of x) and termezo_sample
   uint64_t last_seed = 0;
   float last_eps = 0.f;
   float delta = 1e-5f;
@@ -407,6 +415,36 @@ inline bool capturing(hipStream_t s) {
   (void)hipGetLastError();
   return false;
 }
+
+// need bytes in x for a call on c's stream; refused in a capture that would have to allocate.
+inline termezo_status scratch_for(termezo_ctx* c, Scratch& x, int64_t need, const char* what) {
+  const bool graph = capturing(c->stream);
+  if (need > x.cap) {
+    if (graph) {
+      c->last_error = std::string(what) + ": a captured call needs scratch; make one of its size before";
+      return TERMEZO_ERR_STATE;
+    }
+    if (x.held) c->held.push_back(x.p);
+    else if (x.p) (void)hipFree(x.p);                    // waits for the work that uses it
+    x = Scratch();
+    const hipError_t e = hipMalloc(&x.p, (size_t)need);
+    if (e != hipSuccess) {
+      (void)hipGetLastError();
+      x.p = nullptr;
+      c->last_error = std::string(what) + ": " + hipGetErrorString(e);
+      return e == hipErrorOutOfMemory ? TERMEZO_ERR_OOM : TERMEZO_ERR_DEVICE;
+    }
+    x.cap = need;
+  }
+  x.held |= graph;
+  return TERMEZO_OK;
+}
+
+// Products with 8-bit weights.  scratch: linear_i8_scratch(M, K) bytes for the codes and steps of x.
+int64_t linear_i8_scratch(int64_t M, int64_t K);
+hipError_t launch_linear_i8(const void* x, termezo_dtype xdt, int64_t M, int64_t K, const int8_t* codes,
+                            const float* steps, int64_t N, void* out, termezo_dtype ydt, void* scratch,
+                            int n_cu, hipStream_t s);
 
 // The cache's calls on a stream of the caller's choice (checked arguments).
 hipError_t cache_append_on(termezo_kvcache* c, int layer, const void* k, const void* v, int64_t n,

@@ -1780,6 +1780,8 @@ struct termezo_model {
   bool use_snap = false;          // read the context's codes snapshot instead of its current codes
   termezo_model_config cfg{};
   const void* emb = nullptr;
+  const int8_t* head = nullptr;   // the head in 8 bits and its steps (null: the embedding)
+  const float* head_steps = nullptr;
   const void* normw = nullptr;    // RMSNorm weights [2 n_blocks + 1][d] (null: one)
   int hd = 0;
   int64_t cap_M = 0;
@@ -1891,7 +1893,9 @@ hipError_t acts_alloc(Acts& a, const termezo_model_config& c, int hd, int64_t M)
   A(&a.u, M * c.d_ffn * es);
   A(&a.xf, M * c.d_model * es);
   // row-major, or in fragment order for the small calls that this reservation also serves
-  A((void**)&a.xq, std::max(M * kmax, xq_bytes(std::min<int64_t>(M, kGemvMaxM), kmax)));
+  // or with their steps in front of a head in 8 bits
+  A((void**)&a.xq, std::max({M * kmax, xq_bytes(std::min<int64_t>(M, kGemvMaxM), kmax),
+                             linear_i8_scratch(M, c.d_model)}));
   A((void**)&a.xs, M * 4);
   A((void**)&a.xrs, rs_entries(M) * 4);
   return e;
@@ -2380,6 +2384,18 @@ termezo_status termezo_model_loss(termezo_model* m, const int32_t* tokens, int32
 }
 
 
+termezo_status termezo_model_set_head(termezo_model* m, const int8_t* codes, const float* steps) {
+  if (!m) return TERMEZO_ERR_INVALID_ARG;
+  if (!codes != !steps || (reinterpret_cast<uintptr_t>(codes) & 15u) != 0 ||
+      (reinterpret_cast<uintptr_t>(steps) & 3u) != 0) {
+    m->ctx->last_error = "model_set_head: one of codes and steps is null, or a misaligned pointer";
+    return TERMEZO_ERR_INVALID_ARG;
+  }
+  m->head = codes;
+  m->head_steps = steps;
+  return TERMEZO_OK;
+}
+
 termezo_status termezo_model_decode(termezo_model* m, termezo_kvcache* kv, const int32_t* tokens,
                                     int64_t n, const int32_t* counts, float* logits) {
   if (!m || !kv) return TERMEZO_ERR_INVALID_ARG;
@@ -2458,7 +2474,11 @@ termezo_status termezo_model_decode(termezo_model* m, termezo_kvcache* kv, const
 #undef TMZ_LAST
   chk(hipGetLastError());
   chk(norm_rows(m, A.q, rows, nrm, 2 * cf.n_blocks, A, A.xf, false, s));
-  chk(launch_logits(A.xf, emb, cf.act_dtype, rows, d, cf.vocab, logits, c->n_cu, s));
+  if (m->head)
+    chk(launch_linear_i8(A.xf, cf.act_dtype, rows, d, m->head, m->head_steps, cf.vocab, logits, TERMEZO_F32, A.xq,
+                         c->n_cu, s));
+  else
+    chk(launch_logits(A.xf, emb, cf.act_dtype, rows, d, cf.vocab, logits, c->n_cu, s));
   chk(cache_advance_on(kv, s));
   return e == hipSuccess ? TERMEZO_OK : failed();
 }

@@ -97,6 +97,10 @@ termezo_status report_error(termezo_ctx* c, int32_t err) {
       msg += "kvcache: a group's token count lies outside 0 .. n, is not the pending one, or its "
              "tokens do not fit max_len (the group was left out); ";
     if (err & 32) msg += "kvcache_reorder: a parent lies outside the group (its sequence was kept); ";
+    if (err & 64)
+      msg += "adjust_logits: a length, a start or a line of a table is out of range (the row was taken without it); ";
+    if (err & 128)
+      msg += "sample: a temperature, a limit or a random number is out of range (read as 0, none or the nearest); ";
     return fail(c, (err & 7) ? TERMEZO_ERR_NUMERIC : TERMEZO_ERR_INVALID_ARG, msg);
   }
   return TERMEZO_OK;
@@ -214,6 +218,10 @@ void free_all(termezo_ctx* c) {
   dfree(c->d_loss);
   dfree(c->d_scal);
   dfree(c->d_beam);
+  for (Scratch* x : {&c->linear, &c->draw}) {
+    if (x->p) (void)hipFree(x->p);
+    *x = Scratch();
+  }
   for (void* p : c->held) (void)hipFree(p);
   c->held.clear();
   dfree(c->d_xq);

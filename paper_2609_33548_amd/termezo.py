@@ -54,6 +54,15 @@ class KVCacheConfig(ctypes.Structure):
                 ("rope_base", ctypes.c_float), ("act_dtype", ctypes.c_int32)]
 
 
+class LogitRules(ctypes.Structure):
+    _fields_ = [("history", ctypes.c_void_p), ("hist_len", ctypes.c_int64),
+                ("lengths", ctypes.c_void_p), ("starts", ctypes.c_void_p),
+                ("repetition", ctypes.c_void_p), ("presence", ctypes.c_void_p),
+                ("frequency", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("n_bias", ctypes.c_int32),
+                ("bias_index", ctypes.c_void_p), ("mask", ctypes.c_void_p),
+                ("n_masks", ctypes.c_int32), ("mask_index", ctypes.c_void_p)]
+
+
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2609_33548_amd.build`")
 
@@ -114,6 +123,11 @@ _SIGS = {
     "termezo_logits": [_P, _P, _P, _i32, _i64, _i64, _i64, _P],
     "termezo_beam_select": [_P, _P, _P, _P, _i32, _i32, _i32, _i32, _i32, _P, _P, _P, _P, _P, _P, _i64],
     "termezo_model_decode": [_P, _P, _P, _i64, _P, _P],
+    "termezo_quantize_rows": [_P, _P, _i32, _i64, _i64, _P, _P],
+    "termezo_linear_i8": [_P, _P, _i32, _i64, _i64, _P, _P, _i64, _P, _i32],
+    "termezo_adjust_logits": [_P, _P, _i32, _i32, _P, _P],
+    "termezo_sample": [_P, _P, _P, _i32, _i32, _P, _P, _P, _P, _P, _P],
+    "termezo_model_set_head": [_P, _P, _P],
 }
 for _name, _args in _SIGS.items():
     _fn = getattr(_lib, _name)
@@ -440,6 +454,79 @@ class Context:
             opt(out_finished, "out_finished", (B, n), u8), opt(history, "history", (B, W, T), i32),
             opt(out_history, "out_history", (B, n, T + 1), i32), T), "beam_select")
 
+    def quantize_rows(self, w, codes, steps):
+        """Rows of w [N, K] (fp32 or bf16) in 8 bits: codes int8 [N, K] and steps fp32 [N]; a row's
+        values are near codes * step."""
+        import torch
+        N, K = w.shape
+        self._check(_lib.termezo_quantize_rows(
+            self.handle, _tensor(w, "w", (N, K), w.dtype, self.device), _dtype_code(w), N, K,
+            _tensor(codes, "codes", (N, K), torch.int8, self.device),
+            _tensor(steps, "steps", (N,), torch.float32, self.device)), "quantize_rows")
+
+    def linear_i8(self, x, codes, steps, out):
+        """out[m, n] = x[m] . (codes[n] * steps[n]) with every row of x taken in 8 bits, as
+        bitlinear_forward does: x [M, K] and out [M, N] in fp32 or bf16, codes int8 [N, K], steps
+        fp32 [N]."""
+        import torch
+        M, K = x.shape
+        N = codes.shape[0]
+        self._check(_lib.termezo_linear_i8(
+            self.handle, _tensor(x, "x", (M, K), x.dtype, self.device), _dtype_code(x), M, K,
+            _tensor(codes, "codes", (N, K), torch.int8, self.device),
+            _tensor(steps, "steps", (N,), torch.float32, self.device), N,
+            _tensor(out, "out", (M, N), out.dtype, self.device), _dtype_code(out)), "linear_i8")
+
+    def adjust_logits(self, logits, out, history=None, lengths=None, starts=None, repetition=None,
+                      presence=None, frequency=None, bias=None, bias_index=None, mask=None,
+                      mask_index=None):
+        """logits fp32 [rows, vocab] under the rules into out (the same tensor, or another one).
+        Tokens among the first lengths[r] of history int32 [rows, T] are divided (above 0) or
+        multiplied by repetition[r]; those that appear c times from place starts[r] on lose c *
+        frequency[r] + presence[r]; line bias_index[r] of bias fp32 [lines, vocab] is added; tokens
+        whose bit (t % 32 of word t // 32) in line mask_index[r] of mask int32 [lines, ceil(vocab /
+        32)] is 0 become -inf.  Index -1: no line; without indices a table has one line, or one a
+        row."""
+        import torch
+        R, V = logits.shape
+        f32, i32 = torch.float32, torch.int32
+        if history is None and any(t is not None for t in (lengths, starts, repetition, presence, frequency)):
+            raise ValueError("lengths, starts and penalties need a history")
+        if (bias is None and bias_index is not None) or (mask is None and mask_index is not None):
+            raise ValueError("an index needs its table")
+        if any(t is not None and t.shape[0] == 0 for t in (bias, mask)):
+            raise ValueError("a table needs a line")
+        T = 0 if history is None else history.shape[-1]
+        opt = lambda t, *a: None if t is None else _tensor(t, *a, self.device)
+        row = lambda t, name, dt: opt(t, name, (R,), dt)
+        lines = lambda t: 0 if t is None else t.shape[0]
+        rules = LogitRules(
+            opt(history, "history", (R, T), i32), T, row(lengths, "lengths", i32), row(starts, "starts", i32),
+            row(repetition, "repetition", f32), row(presence, "presence", f32), row(frequency, "frequency", f32),
+            opt(bias, "bias", (lines(bias), V), f32), lines(bias), row(bias_index, "bias_index", i32),
+            opt(mask, "mask", (lines(mask), (V + 31) // 32), i32), lines(mask), row(mask_index, "mask_index", i32))
+        self._check(_lib.termezo_adjust_logits(
+            self.handle, _tensor(logits, "logits", (R, V), f32, self.device), R, V, ctypes.byref(rules),
+            _tensor(out, "out", (R, V), f32, self.device)), "adjust_logits")
+
+    def sample(self, logits, uniforms, tokens, logprobs=None, temperature=None, top_k=None, top_p=None,
+               min_p=None):
+        """A token for every row of logits [rows, vocab] (fp32) into tokens int32 [rows], drawn with
+        the random numbers uniforms [rows] in [0, 1) from the weights exp(logit / temperature) of
+        the first top_k tokens (int32; 0: all), of these the ones with at least min_p of the largest
+        weight, of these the fewest best whose weights reach top_p of them all; logprobs fp32 [rows]:
+        its log probability among those.  temperature, top_p and min_p fp32 [rows]; temperature 0
+        takes the best token.  A row without a logit above -inf has token -1."""
+        import torch
+        R, V = logits.shape
+        f32, i32 = torch.float32, torch.int32
+        row = lambda t, name, dt=f32: None if t is None else _tensor(t, name, (R,), dt, self.device)
+        self._check(_lib.termezo_sample(
+            self.handle, _tensor(logits, "logits", (R, V), f32, self.device),
+            _tensor(uniforms, "uniforms", (R,), f32, self.device), R, V, row(temperature, "temperature"),
+            row(top_k, "top_k", i32), row(top_p, "top_p"), row(min_p, "min_p"),
+            _tensor(tokens, "tokens", (R,), i32, self.device), row(logprobs, "logprobs")), "sample")
+
 
 class KVCache:
     """Keys and values of ``groups * beams`` sequences in 8 bits (a step for each block of 64 tokens
@@ -598,6 +685,18 @@ class Model:
             cache._counts(counts),
             _tensor(logits, "logits", (cache.rows, self.embedding.shape[0]), torch.float32, dev)),
             "model_decode")
+
+    def set_head(self, codes, steps):
+        """decode forms its logits with the head in 8 bits: codes int8 [vocab, d_model] and steps fp32
+        [vocab] of quantize_rows, kept alive by the caller; None, None restores the embedding."""
+        import torch
+        V, d = self.embedding.shape
+        dev = self.ctx.device
+        opt = lambda t, *a: None if t is None else _tensor(t, *a, dev)
+        self.ctx._check(_lib.termezo_model_set_head(
+            self.handle, opt(codes, "codes", (V, d), torch.int8), opt(steps, "steps", (V,), torch.float32)),
+            "model_set_head")
+        self.head = (codes, steps)                # kept alive with the model
 
     def set_stream(self, stream):
         """Run this model's forwards on ``stream`` (a torch stream; None: the context's)."""
