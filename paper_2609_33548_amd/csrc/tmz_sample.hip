@@ -116,8 +116,8 @@ __global__ void __launch_bounds__(256) k_adjust(RuleArgs a) {
 // what is kept is one border in that order; the token then comes from the prefix sums of the kept weights in
 // the order of indices.
 //
-// k_draw_scan, a work group for a slice of a row: the slice's largest logit m_s, its weights exp((x - m_s) / T)
-// in fixed point (2^-48; integer sums do not depend on their order), their sum, and sums and counts by bins.
+// k_draw_scan, a work group for a slice of a row: the slice's largest logit m_s, its weights exp((x - m_s) / T),
+// their sum, and sums and counts by bins (in fixed point, 2^-48: integer sums do not depend on their order).
 // A bin is a quarter of T wide on a grid that all slices share (bin = floor(x (4 / T))), counted from the slice's
 // best bin downwards; the last of the 128 holds all that lies lower.
 // k_draw_list, the same grid: the row's bins (slices weighted by exp((m_s - m) / T)) tell in which of them the
@@ -127,21 +127,24 @@ __global__ void __launch_bounds__(256) k_adjust(RuleArgs a) {
 // it goes through the row in the list's place.
 // Without limits the first and the last are enough.
 // ---------------------------------------------------------------------------
-constexpr int kBins = 128, kList = 8192, kMaxDrawRows = 1024, kPickThreads = 512;
+constexpr int kBins = 128, kMaxDrawRows = 1024, kPickThreads = 512, kHeld = 16, kList = kHeld * kPickThreads;
+constexpr int kCopies = 4;           // of the bins, so that neighbouring lanes seldom meet in one
 constexpr double kSliceUnit = 0x1p48;
+constexpr double kLog2e16 = 16.0 * 0x1.71547652b82fep+0, kLn2by16 = 0x1.62e42fefa39efp-5;   // 16 log2(e), ln(2) / 16
 
 struct SliceStat {
   float top;                         // -inf: nothing
   int32_t bin;
-  unsigned long long sum;            // weights relative to top, 2^-48
+  double sum;                        // weights relative to top
 };
 struct RowPlan {                     // what k_draw_list found
   float top, xm;                     // the row's largest logit; the least one that min_p keeps
   int32_t bin;
-  int32_t first, last;               // bins before first are kept, bins first .. last are listed
-  int32_t limited;                   // whether top_k or min_p ends in the listed bins
-  int32_t count0;                    // tokens and weight (relative to top) in the bins before first
-  double mass0;
+  // Bins before first are kept; listed are bins first .. last, where top_p's border lies (or the only one), and
+  // bin limit, where top_k or min_p ends (kBins: they do not)
+  int32_t first, last, limit;
+  int32_t count1;                    // tokens in the bins before limit
+  double mass0, mass1;               // weights (relative to top) in the bins before first, before limit
   double total;                      // of the whole row
 };
 
@@ -152,6 +155,7 @@ struct DrawArgs {
   float* logprobs;
   int32_t vocab, slices;
   SliceStat* stat;                   // [rows][slices]
+  double* sure;                      // [rows][slices]: a slice's weights in the row's bins before first
   unsigned long long* mass;          // [rows][slices][kBins]
   uint32_t* count;
   RowPlan* plan;                     // [rows]
@@ -161,11 +165,11 @@ struct DrawArgs {
 };
 
 struct Settings {
-  double inv_t;                      // 1 / T
+  double inv_t, scale;               // 1 / T and kLog2e16 / T
   float grid;                        // 4 / T
   float p, min_p;                    // p 1: none; min_p 0: none
   int k;                             // 0: none
-  bool bad;
+  bool best, bad;                    // best: the best token alone
 };
 
 __device__ __forceinline__ Settings draw_settings(const DrawArgs& a, int row) {
@@ -177,7 +181,8 @@ __device__ __forceinline__ Settings draw_settings(const DrawArgs& a, int row) {
   s.bad = !(t >= 0.0f && t <= FLT_MAX) || s.p != s.p || s.min_p != s.min_p;
   if (!(s.p < 1.0f)) s.p = 1.0f;
   if (!(s.min_p > 0.0f)) s.min_p = 0.0f;
-  if (!(t > 0.0f && t <= FLT_MAX)) {                     // the best token alone
+  s.best = !(t > 0.0f && t <= FLT_MAX);
+  if (s.best) {
     t = 1.0f;
     s.k = 1;
     s.p = 1.0f;
@@ -185,6 +190,7 @@ __device__ __forceinline__ Settings draw_settings(const DrawArgs& a, int row) {
   }
   if (s.min_p > 1.0f) s.k = 1;                           // no weight reaches it: the first one is kept
   s.inv_t = 1.0 / (double)t;
+  s.scale = kLog2e16 * s.inv_t;
   s.grid = fminf(4.0f / t, FLT_MAX);
   return s;
 }
@@ -193,8 +199,31 @@ __device__ __forceinline__ float draw_clean(float x) { return x == x ? fminf(x +
 __device__ __forceinline__ int draw_bin(float x, float grid) {
   return (int)fminf(fmaxf(floorf(x * grid), -1e9f), 1e9f);
 }
-__device__ __forceinline__ double draw_weight(float x, float top, double inv_t) {
-  return x > -INFINITY ? exp(((double)x - (double)top) * inv_t) : 0.0;
+// exp(z) for z <= 0, given q = 16 z log2(e): q = n + f, |f| <= 1/2; 2^(n / 16) from a table of 2^(j / 16) that lies on
+// sixteen pairs of LDS banks, 2^(f / 16) from its series up to f^5 (what is left out is below 2^-42), fp64 throughout.
+// Half the operations of a series without a table.
+__device__ const double kRoots[16] = {
+    0x1.0000000000000p+0, 0x1.0b5586cf9890fp+0, 0x1.172b83c7d517bp+0, 0x1.2387a6e756238p+0,
+    0x1.306fe0a31b715p+0, 0x1.3dea64c123422p+0, 0x1.4bfdad5362a27p+0, 0x1.5ab07dd485429p+0,
+    0x1.6a09e667f3bcdp+0, 0x1.7a11473eb0187p+0, 0x1.8ace5422aa0dbp+0, 0x1.9c49182a3f090p+0,
+    0x1.ae89f995ad3adp+0, 0x1.c199bdd85529cp+0, 0x1.d5818dcfba487p+0, 0x1.ea4afa2a490dap+0};
+__device__ __forceinline__ double exp_of(double q, const double* roots) {     // q >= -16000: no denormals
+  constexpr double l = kLn2by16;
+  const double shifted = q + 0x1.8p52;                   // rounded to a whole number n
+  const int n = (int)(uint32_t)__double_as_longlong(shifted);
+  const double f = q - (shifted - 0x1.8p52);
+  double p = l * l * l * l * l / 120;
+  p = fma(p, f, l * l * l * l / 24);
+  p = fma(p, f, l * l * l / 6);
+  p = fma(p, f, l * l / 2);
+  p = fma(p, f, l);
+  p = fma(p, f, 1.0);
+  const long long w = __double_as_longlong(p * roots[n & 15]);
+  return __longlong_as_double(w + ((long long)(n >> 4) << 52));
+}
+// The weight of x beside top: exp((x - top) / T), scale = kLog2e16 / T.  -inf has 0, or what rounds to it.
+__device__ __forceinline__ double draw_weight(float x, float top, double scale, const double* roots) {
+  return exp_of(fmax(((double)x - (double)top) * scale, -16000.0), roots);
 }
 // w in [0, 1] in units of 1 / unit (a power of two up to 2^51), rounded to nearest.
 __device__ __forceinline__ unsigned long long draw_fix(double w, double unit) {
@@ -211,60 +240,96 @@ __device__ __forceinline__ float unordered(uint32_t k) {
 __device__ __forceinline__ unsigned long long draw_key(float x, int t) {
   return (unsigned long long)ordered(x) << 32 | (0xFFFFFFFFu - (uint32_t)t);
 }
+__device__ __forceinline__ float key_logit(unsigned long long k) { return unordered((uint32_t)(k >> 32)); }
+__device__ __forceinline__ int key_token(unsigned long long k) { return (int)(0xFFFFFFFFu - (uint32_t)k); }
 
+// v of the lane that a data-parallel move names, `none` where there is no such lane or its row is left out.
+template <int CTRL, int ROWS, typename T>
+__device__ __forceinline__ T moved(T v, T none) {
+  static_assert(sizeof(T) == 4 || sizeof(T) == 8, "32 or 64 bits");
+  if constexpr (sizeof(T) == 4) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, v), CTRL,
+                                                             ROWS, 0xF, false));
+  } else {
+    typedef int v2i __attribute__((ext_vector_type(2)));
+    const v2i a = __builtin_bit_cast(v2i, v), o = __builtin_bit_cast(v2i, none);
+    return __builtin_bit_cast(T, v2i{__builtin_amdgcn_update_dpp(o[0], a[0], CTRL, ROWS, 0xF, false),
+                                     __builtin_amdgcn_update_dpp(o[1], a[1], CTRL, ROWS, 0xF, false)});
+  }
+}
+// The lane up to and including which v is combined by f: steps of 1, 2, 4 and 8 within rows of 16 lanes, then each
+// row's last lane to the next row, then lane 31 to the upper half (a shuffle through LDS takes ten times as long).
+template <typename T, typename F>
+__device__ __forceinline__ T wave_fold(T v, T none, F f) {
+  v = f(v, moved<0x111, 0xF>(v, none));
+  v = f(v, moved<0x112, 0xF>(v, none));
+  v = f(v, moved<0x114, 0xF>(v, none));
+  v = f(v, moved<0x118, 0xF>(v, none));
+  v = f(v, moved<0x142, 0xA>(v, none));
+  v = f(v, moved<0x143, 0xC>(v, none));
+  return v;
+}
+template <typename T>
+__device__ __forceinline__ T last_lane(T v) {
+  if constexpr (sizeof(T) == 4) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+  } else {
+    typedef int v2i __attribute__((ext_vector_type(2)));
+    const v2i a = __builtin_bit_cast(v2i, v);
+    return __builtin_bit_cast(T, v2i{__builtin_amdgcn_readlane(a[0], 63), __builtin_amdgcn_readlane(a[1], 63)});
+  }
+}
+// Inclusive prefix sums over the wave's lanes, and results of all of them in every lane.
+template <typename T>
+__device__ __forceinline__ T wave_scan(T v) {
+  return wave_fold(v, (T)0, [](T a, T b) __attribute__((always_inline)) { return a + b; });
+}
 template <typename T>
 __device__ __forceinline__ T wave_sum(T v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
+  return last_lane(wave_scan(v));
 }
 __device__ __forceinline__ float wave_top(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-  return v;
-}
-// Inclusive prefix sums over the wave's lanes.
-template <typename T>
-__device__ __forceinline__ T wave_scan(T v, int lane) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const T u = __shfl_up(v, o, 64);
-    if (lane >= o) v += u;
-  }
-  return v;
+  return last_lane(wave_fold(v, -INFINITY, [](float a, float b) __attribute__((always_inline)) { return fmaxf(a, b); }));
 }
 
 // A slice's logits, 4 * E of a thread: x[4 i + j] at t0 + 1024 i + 4 tid + j; -inf behind the row's end.
 template <int E>
 __device__ __forceinline__ void draw_load(const float* row, int t0, int V, int tid, float x[4 * E]) {
+  if (t0 + 1024 * E <= V) {                              // whole work group
+    Four f[E];
 #pragma unroll
-  for (int i = 0; i < E; ++i) {
-    const int t = t0 + 1024 * i + 4 * tid;
-    if (t + 3 < V) {
-      const Four f = *(const Four*)(row + t);
+    for (int i = 0; i < E; ++i) f[i] = *(const Four*)(row + t0 + 1024 * i + 4 * tid);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[4 * i + j] = draw_clean(f.v[j]);
-    } else {
+    for (int i = 0; i < 4 * E; ++i) x[i] = draw_clean(f[i / 4].v[i % 4]);
+    return;
+  }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[4 * i + j] = t + j < V ? draw_clean(row[t + j]) : -INFINITY;
-    }
+  for (int i = 0; i < 4 * E; ++i) {
+    const int t = t0 + 1024 * (i / 4) + 4 * tid + i % 4;
+    const float v = row[t < V ? t : V - 1];
+    x[i] = t < V ? draw_clean(v) : -INFINITY;
   }
 }
 
-template <int E, bool LIMITS>
+// LIMITS: bins are wanted, COUNT: their tokens are counted too (top_k).
+template <int E, bool LIMITS, bool COUNT>
 __global__ void __launch_bounds__(256) k_draw_scan(DrawArgs a) {
-  __shared__ unsigned long long mass[kBins], sums[4];
-  __shared__ uint32_t count[kBins];
+  __shared__ unsigned long long mass[LIMITS ? kCopies * kBins : 1];
+  __shared__ double sums[4];
+  __shared__ uint32_t count[COUNT ? kCopies * kBins : 1];
   __shared__ float tops[4];
+  __shared__ double roots[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int row = blockIdx.y, slice = blockIdx.x, V = a.vocab;
+  if (tid < 16) roots[tid] = kRoots[tid];
   const Settings s = draw_settings(a, row);
   float x[4 * E];
   draw_load<E>(a.logits + (int64_t)row * V, slice * 1024 * E, V, tid, x);
-  if (LIMITS && tid < kBins) {
-    mass[tid] = 0;
-    count[tid] = 0;
-  }
+  if (LIMITS)
+    for (int i = tid; i < kCopies * kBins; i += 256) {
+      mass[i] = 0;
+      if (COUNT) count[i] = 0;
+    }
   float top = -INFINITY;
 #pragma unroll
   for (int i = 0; i < 4 * E; ++i) top = fmaxf(top, x[i]);
@@ -273,15 +338,16 @@ __global__ void __launch_bounds__(256) k_draw_scan(DrawArgs a) {
   __syncthreads();
   top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
   const int best = draw_bin(top, s.grid);
-  unsigned long long sum = 0;
+  const int copy = (tid & (kCopies - 1)) * kBins;
+  double sum = 0.0;
 #pragma unroll
   for (int i = 0; i < 4 * E; ++i) {
-    const unsigned long long w = draw_fix(draw_weight(x[i], top, s.inv_t), kSliceUnit);
+    const double w = draw_weight(x[i], top, s.scale, roots);
     sum += w;
     if (LIMITS && x[i] > -INFINITY) {
       const int j = min(best - draw_bin(x[i], s.grid), kBins - 1);
-      atomicAdd(&mass[j], w);
-      atomicAdd(&count[j], 1u);
+      atomicAdd(&mass[copy + j], draw_fix(w, kSliceUnit));
+      if (COUNT) atomicAdd(&count[copy + j], 1u);
     }
   }
   sum = wave_sum(sum);
@@ -289,25 +355,43 @@ __global__ void __launch_bounds__(256) k_draw_scan(DrawArgs a) {
   __syncthreads();
   const int64_t at = (int64_t)row * a.slices + slice;
   if (tid == 0) {
-    a.stat[at] = SliceStat{top, best, sums[0] + sums[1] + sums[2] + sums[3]};
+    a.stat[at] = SliceStat{top, best, top > -INFINITY ? (sums[0] + sums[1]) + (sums[2] + sums[3]) : 0.0};
     if (LIMITS && slice == 0) a.listed[row] = 0;
   }
   if (LIMITS && tid < kBins) {
-    a.mass[at * kBins + tid] = mass[tid];
-    a.count[at * kBins + tid] = count[tid];
+    unsigned long long m = 0;
+    uint32_t c = 0;
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+      m += mass[i * kBins + tid];
+      if (COUNT) c += count[i * kBins + tid];
+    }
+    a.mass[at * kBins + tid] = m;
+    if (COUNT) a.count[at * kBins + tid] = c;
   }
 }
 
-template <int E>
+template <int E, bool COUNT>
 __global__ void __launch_bounds__(256) k_draw_list(DrawArgs a) {
-  __shared__ double mass[kBins], half_mass[kBins], low_mass[4];
-  __shared__ int count[kBins], half_count[kBins], low_count[4];
+  __shared__ double mass[kBins], half_mass[kBins], low_mass[4], factor[64];
+  __shared__ int count[kBins], half_count[kBins], low_count[4], offset[64];
   __shared__ float tops[4];
+  __shared__ unsigned long long parts[4];
+  __shared__ int counts[4], base;
   __shared__ RowPlan plan;
+  __shared__ double roots[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int row = blockIdx.y, slice = blockIdx.x, V = a.vocab;
+  if (tid < 16) roots[tid] = kRoots[tid];
   const Settings s = draw_settings(a, row);
   const SliceStat* stat = a.stat + (int64_t)row * a.slices;
+  const SliceStat own = stat[slice];
+  const int j = tid & (kBins - 1), half = tid >> 7;
+  const unsigned long long own_mass = a.mass[((int64_t)row * a.slices + slice) * kBins + j];
+  // the logits are on their way while the borders are found
+  float x[4 * E];
+  const int t0 = slice * 1024 * E;
+  draw_load<E>(a.logits + (int64_t)row * V, t0, V, tid, x);
   float top = -INFINITY;
   for (int i = tid; i < a.slices; i += 256) top = fmaxf(top, stat[i].top);
   top = wave_top(top);
@@ -315,32 +399,44 @@ __global__ void __launch_bounds__(256) k_draw_list(DrawArgs a) {
   __syncthreads();
   top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
   const int bin = draw_bin(top, s.grid);
-  // The row's bins: thread j of either half of the work group takes bin j of every other slice; bins that are the
-  // row's last one or lower together (a slice's own last bin always is)
-  const int j = tid & (kBins - 1), half = tid >> 7;
+  // The row's bins, 64 slices at a time: thread j of either half of the work group takes bin j of every other slice;
+  // bins that are the row's last one or lower together (a slice's own last bin always is)
   double m = 0.0, lm = 0.0;
   int c = 0, lc = 0;
-  for (int i = half; i < a.slices; i += 2) {
-    const SliceStat t = stat[i];
-    if (!(t.top > -INFINITY)) continue;
-    const double f = exp(((double)t.top - (double)top) * s.inv_t) * (1.0 / kSliceUnit);
-    const int off = bin - t.bin;                         // 0 or more
-    const int64_t at = ((int64_t)row * a.slices + i) * kBins;
-    if (j >= off && j < kBins - 1) {
-      m += f * (double)a.mass[at + j - off];
-      c += (int)a.count[at + j - off];
+  for (int s0 = 0; s0 < a.slices; s0 += 64) {
+    const int n = min(64, a.slices - s0);
+    __syncthreads();
+    if (tid < n) {
+      const SliceStat t = stat[s0 + tid];
+      const bool any = t.top > -INFINITY;
+      factor[tid] = any ? draw_weight(t.top, top, s.scale, roots) * (1.0 / kSliceUnit) : 0.0;
+      offset[tid] = any ? bin - t.bin : kBins;           // 0 or more; an empty slice has nothing in its bins
     }
-    if (off >= kBins - 1 || j >= kBins - 1 - off) {
-      lm += f * (double)a.mass[at + j];
-      lc += (int)a.count[at + j];
+    __syncthreads();
+    const int64_t at = ((int64_t)row * a.slices + s0) * kBins;
+#pragma unroll 4
+    for (int i = half; i < n; i += 2) {
+      const int off = offset[i];
+      const double f = factor[i];
+      // this thread's bin of the slice and the one that falls on this bin of the row
+      const int from = j - off;
+      const unsigned long long w = a.mass[at + i * kBins + j], v = a.mass[at + i * kBins + max(from, 0)];
+      const bool low = off >= kBins - 1 || j >= kBins - 1 - off, here = from >= 0 && j < kBins - 1;
+      if (here) m += f * (double)v;
+      if (low) lm += f * (double)w;
+      if (COUNT) {
+        const int cw = (int)a.count[at + i * kBins + j], cv = (int)a.count[at + i * kBins + max(from, 0)];
+        if (here) c += cv;
+        if (low) lc += cw;
+      }
     }
   }
   if (half) {
     half_mass[j] = m;
-    half_count[j] = c;
+    if (COUNT) half_count[j] = c;
   }
   lm = wave_sum(lm);
-  lc = wave_sum(lc);
+  if (COUNT) lc = wave_sum(lc);
   if (lane == 0) {
     low_mass[wave] = lm;
     low_count[wave] = lc;
@@ -348,7 +444,7 @@ __global__ void __launch_bounds__(256) k_draw_list(DrawArgs a) {
   __syncthreads();
   if (!half) {
     m += half_mass[j];
-    c += half_count[j];
+    if (COUNT) c += half_count[j];
     if (j == kBins - 1) {
       m = (low_mass[0] + low_mass[1]) + (low_mass[2] + low_mass[3]);
       c = low_count[0] + low_count[1] + low_count[2] + low_count[3];
@@ -357,27 +453,28 @@ __global__ void __launch_bounds__(256) k_draw_list(DrawArgs a) {
     count[j] = c;
   }
   __syncthreads();
-  if (wave == 0) {                                       // sums up to each bin
+  if (wave == 0) {                                       // sums up to each bin, and where the borders lie
     const double m0 = mass[2 * lane], m1 = mass[2 * lane + 1];
     const int c0 = count[2 * lane], c1 = count[2 * lane + 1];
-    const double ms = wave_scan(m0 + m1, lane);
-    const int cs = wave_scan(c0 + c1, lane);
-    mass[2 * lane] = ms - m1;
-    mass[2 * lane + 1] = ms;
-    count[2 * lane] = cs - c1;
-    count[2 * lane + 1] = cs;
-  }
-  __syncthreads();
-  if (tid == 0) {
-    RowPlan p{top, -INFINITY, bin, kBins, kBins - 1, 0, 0, 0.0, mass[kBins - 1]};
+    const double me = wave_scan(m0 + m1), mo = me - m1;
+    const int ce = wave_scan(c0 + c1), co = ce - c1;
+    mass[2 * lane] = mo;
+    mass[2 * lane + 1] = me;
+    count[2 * lane] = co;
+    count[2 * lane + 1] = ce;
+    const double total = last_lane(me);
+    const int all = last_lane(ce);
+    // the first bin up to which the sum is not below x (the last one if there is none)
+    auto first_at = [&](bool even, bool odd) {
+      const unsigned long long e = __ballot(even), o = __ballot(odd);
+      const int be = e ? 2 * (__ffsll((long long)e) - 1) : kBins - 1, bo = o ? 2 * (__ffsll((long long)o) - 1) + 1 : kBins - 1;
+      return min(be, bo);
+    };
+    RowPlan p{top, -INFINITY, bin, kBins, -1, kBins, 0, 0.0, 0.0, total};
     if (top > -INFINITY) {
-      auto first_count = [&](int n) {
-        int i = 0;
-        while (i < kBins - 1 && count[i] < n) ++i;
-        return i;
-      };
       int b1 = kBins;                                    // where top_k's or min_p's border lies
-      if (s.k > 0 && s.k < count[kBins - 1]) b1 = s.k == 1 ? 0 : first_count(s.k);
+      if (s.k == 1) b1 = 0;
+      else if (COUNT && s.k > 0 && s.k < all) b1 = first_at(co >= s.k, ce >= s.k);
       if (s.min_p > 0.0f && s.min_p <= 1.0f) {
         // the least logit with (x - top) / T >= ln min_p: an estimate, then its neighbours
         const double z = log((double)s.min_p);
@@ -391,57 +488,72 @@ __global__ void __launch_bounds__(256) k_draw_list(DrawArgs a) {
         const long long down = (long long)bin - draw_bin(xm, s.grid);
         b1 = min(b1, (int)min(down, (long long)(kBins - 1)));
       }
-      p.limited = b1 < kBins;
+      p.limit = b1;
       p.first = b1;
-      p.last = min(b1, kBins - 1);
+      p.last = b1 < kBins ? b1 : -1;
+      if (b1 > 0 && b1 < kBins) {
+        p.count1 = count[b1 - 1];
+        p.mass1 = mass[b1 - 1];
+      }
       if (s.p < 1.0f) {
-        // weight of what top_k and min_p keep: at least that of the bins before the border
-        const double least = b1 == kBins ? mass[kBins - 1] : b1 > 0 ? mass[b1 - 1] : 0.0;
-        int i = 0;
-        while (i < min(b1, kBins - 1) && mass[i] < (double)s.p * least) ++i;
-        p.first = i;
-        p.last = b1 < kBins ? b1 : i;
-      } else if (b1 == kBins) {
-        p.last = -1;                                     // nothing to list
+        // the weight of what top_k and min_p keep lies between that of the bins before theirs and with it
+        const double least = b1 == kBins ? total : p.mass1, most = b1 == kBins ? total : mass[b1];
+        const double goal0 = (double)s.p * least, goal1 = (double)s.p * most;
+        p.first = min(first_at(mo >= goal0, me >= goal0), b1);
+        p.last = min(first_at(mo >= goal1, me >= goal1), b1);
       }
-      if (p.first > 0) {
-        p.count0 = count[p.first < kBins ? p.first - 1 : kBins - 1];
-        p.mass0 = mass[p.first < kBins ? p.first - 1 : kBins - 1];
-      }
-    } else {
-      p.last = -1;
+      if (p.first > 0) p.mass0 = mass[p.first - 1];
     }
-    plan = p;
-    if (slice == 0) a.plan[row] = p;
+    if (lane == 0) {
+      plan = p;
+      if (slice == 0) a.plan[row] = p;
+    }
   }
   __syncthreads();
-  const int first = plan.first, last = plan.last;
+  const int first = plan.first, last = plan.last, limit = plan.limit;
+  // this slice's weights in the bins before first
+  if (first < kBins) {
+    unsigned long long w = !half && bin - own.bin + j < first && own.top > -INFINITY ? own_mass : 0;
+    w = wave_sum(w);
+    if (lane == 0) parts[wave] = w;
+    __syncthreads();
+    if (tid == 0) a.sure[(int64_t)row * a.slices + slice] = (double)(parts[0] + parts[1]) * (1.0 / kSliceUnit);
+  } else if (tid == 0) {
+    a.sure[(int64_t)row * a.slices + slice] = own.sum;
+  }
   if (first > last) return;
-  const SliceStat own = stat[slice];
-  if (!(own.top > -INFINITY) || min(bin - own.bin, kBins - 1) > last) return;
-  float x[4 * E];
-  const int t0 = slice * 1024 * E;
-  draw_load<E>(a.logits + (int64_t)row * V, t0, V, tid, x);
+  if (!(own.top > -INFINITY) || min(bin - own.bin, kBins - 1) > (limit < kBins ? limit : last)) return;
+  uint32_t mine = 0;                                     // which of them are listed
 #pragma unroll
   for (int i = 0; i < 4 * E; ++i) {
     const int at = x[i] > -INFINITY ? min(bin - draw_bin(x[i], s.grid), kBins - 1) : kBins;
-    const bool in = at >= first && at <= last;
-    const unsigned long long who = __ballot(in);
-    if (!who) continue;
-    int base = 0;
-    if (lane == 0) base = atomicAdd(&a.listed[row], __popcll(who));
-    base = __shfl(base, 0, 64) + __popcll(who & ((1ull << lane) - 1));
-    if (in && base < kList)
-      a.list[(int64_t)row * kList + base] = draw_key(x[i], t0 + 1024 * (i / 4) + 4 * tid + i % 4);
+    if ((at >= first && at <= last) || (at == limit && at < kBins)) mine |= 1u << i;
   }
+  const int n = __popc(mine), upto = wave_scan(n);
+  if (lane == 63) counts[wave] = upto;
+  __syncthreads();
+  if (tid == 0) {
+    const int all = counts[0] + counts[1] + counts[2] + counts[3];
+    base = all ? atomicAdd(&a.listed[row], all) : 0;
+  }
+  __syncthreads();
+  int at = base + upto - n;
+  for (int w = 0; w < wave; ++w) at += counts[w];
+  unsigned long long* list = a.list + (int64_t)row * kList;
+#pragma unroll
+  for (int i = 0; i < 4 * E; ++i)
+    if (mine >> i & 1u) {
+      if (at < kList) list[at] = draw_key(x[i], t0 + 1024 * (i / 4) + 4 * tid + i % 4);
+      ++at;
+    }
 }
 
-// sums over the work group's threads up to and including this one's, in the order of threads
+// Sums over the work group's threads up to and including this one's, in the order of threads.  parts must not be in
+// use; it is free again after the next barrier.
 template <typename T>
 __device__ __forceinline__ T group_scan(T v, T* parts, int tid, T& total) {
   const int lane = tid & 63, wave = tid >> 6;
-  v = wave_scan(v, lane);
-  __syncthreads();
+  v = wave_scan(v);
   if (lane == 63) parts[wave] = v;
   __syncthreads();
   T before = 0;
@@ -454,18 +566,23 @@ __device__ __forceinline__ T group_scan(T v, T* parts, int tid, T& total) {
   return v + before;
 }
 
-template <bool LIMITS>
-__global__ void __launch_bounds__(kPickThreads) k_draw_pick(DrawArgs a, int slice_len, int unit_bits) {
-  constexpr int kParts = 1024, NT = kPickThreads, NW = NT / 64;
-  __shared__ unsigned long long list[LIMITS ? kList : 1], pm[LIMITS ? kParts : 1];
+constexpr int kMaxSlices = 2048;
+
+template <bool LIMITS, int E>
+__global__ void __launch_bounds__(kPickThreads) k_draw_pick(DrawArgs a, int unit_bits) {
+  constexpr int kParts = 1024, NT = kPickThreads, NW = NT / 64, SLICE = 1024 * E, EACH = SLICE / NT;
+  __shared__ unsigned long long pm[LIMITS ? kParts : 1], add[LIMITS ? kMaxSlices : 1];
   __shared__ uint32_t pc[LIMITS ? kParts : 1];
-  __shared__ unsigned long long ull[NW];
+  __shared__ unsigned long long lows[NW], highs[NW], ull[2][NW];
   __shared__ int ints[NW];
-  __shared__ double dbl[NW];
+  __shared__ double dbl[2][NW];
   __shared__ float tops[NW];
-  __shared__ int chosen, part, last_kept;
-  __shared__ double share, before_slice;
+  __shared__ int part, part_count, before_count, slice_at, hit, last_kept;
+  __shared__ unsigned long long before_mass;
+  __shared__ double before_slice, all_kept;
+  __shared__ double roots[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = blockIdx.x, V = a.vocab;
+  if (tid < 16) roots[tid] = kRoots[tid];
   const float* x = a.logits + (int64_t)row * V;
   const Settings s = draw_settings(a, row);
   const SliceStat* stat = a.stat + (int64_t)row * a.slices;
@@ -474,9 +591,12 @@ __global__ void __launch_bounds__(kPickThreads) k_draw_pick(DrawArgs a, int slic
   const bool bad = s.bad || !(u >= 0.0f && u < 1.0f);
   u = u >= 1.0f ? 1.0f - 0x1p-24f : u > 0.0f ? u : 0.0f;
   if (bad && tid == 0) atomicOr(a.err, kErrSample);
+  if (!LIMITS && s.best) u = 0.0f;                       // the first of the best
   RowPlan p{};
+  int n_list = 0;
   if (LIMITS) {
     p = a.plan[row];
+    n_list = a.listed[row];
   } else {
     float top = -INFINITY;
     for (int i = tid; i < a.slices; i += NT) top = fmaxf(top, stat[i].top);
@@ -497,243 +617,268 @@ __global__ void __launch_bounds__(kPickThreads) k_draw_pick(DrawArgs a, int slic
     return;
   }
   auto bin_of = [&](float v) __attribute__((always_inline)) { return min(p.bin - draw_bin(v, s.grid), kBins - 1); };
-  auto fixed = [&](float v) __attribute__((always_inline)) { return draw_fix(draw_weight(v, p.top, s.inv_t), unit); };
+  auto fixed = [&](float v) __attribute__((always_inline)) { return draw_fix(draw_weight(v, p.top, s.scale, roots), unit); };
 
   unsigned long long border = 0;                         // listed keys from here on are kept
-  int n_list = 0;
-  bool in_list = true;
-  // all that was listed: f(key); of the row itself where the list did not hold it
-  auto candidates = [&](auto f) __attribute__((always_inline)) {
-    if (in_list) {
-      for (int i = tid; i < n_list; i += NT) f(list[i]);
-    } else {
-      for (int t = tid; t < V; t += NT) {
-        const float v = draw_clean(x[t]);
-        if (!(v > -INFINITY)) continue;
-        const int b = bin_of(v);
-        if (b >= p.first && b <= p.last) f(draw_key(v, t));
-      }
-    }
-  };
   if constexpr (LIMITS) {
+    for (int i = tid; i < a.slices; i += NT) add[i] = 0;
     if (p.first <= p.last) {
-      n_list = a.listed[row];
-      in_list = n_list <= kList;
-      if (in_list)
-        for (int i = tid; i < n_list; i += NT) list[i] = a.list[(int64_t)row * kList + i];
-      __syncthreads();
-      // The border: of the keys from `least` on in falling order, the one at which the count from count0 on reaches
-      // want, or (want 0) the weight from mass0 on reaches goal.
-      auto find = [&](unsigned long long least, int want, double goal) {
+      // The listed keys and weights: in registers, or taken from the row each time where the list did not hold them
+      const bool held = n_list <= kList;
+      unsigned long long key[kHeld], weight[kHeld];
+      if (held) {
+        const unsigned long long* list = a.list + (int64_t)row * kList;
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+          key[i] = 0;
+          if (i * NT < n_list && i * NT + tid < n_list) key[i] = list[i * NT + tid];
+        }
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+          weight[i] = 0;
+          if (i * NT < n_list && key[i]) weight[i] = fixed(key_logit(key[i]));
+        }
+      }
+      auto candidates = [&](auto f) __attribute__((always_inline)) {
+        if (held) {
+#pragma unroll
+          for (int i = 0; i < kHeld; ++i)
+            if (i * NT < n_list && key[i]) f(key[i], weight[i]);       // no key is 0
+        } else {
+          for (int t = tid; t < V; t += NT) {
+            const float v = draw_clean(x[t]);
+            if (!(v > -INFINITY)) continue;
+            const int b = bin_of(v);
+            if ((b >= p.first && b <= p.last) || b == p.limit) f(draw_key(v, t), fixed(v));
+          }
+        }
+      };
+      // The border: of the keys from least to most in falling order, the one at which the count from have on reaches
+      // want, or (want 0) the weight from sum on reaches goal.
+      auto group_max = [&](unsigned long long v) {
+        v = last_lane(wave_fold(v, 0ull, [](unsigned long long x, unsigned long long y) __attribute__((always_inline)) {
+          return max(x, y);
+        }));
+        if (lane == 0) ull[1][wave] = v;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < NW; ++w) v = max(v, ull[1][w]);
+        __syncthreads();
+        return v;
+      };
+      auto find = [&](unsigned long long least, unsigned long long most, int have, int want, unsigned long long sum,
+                      double goal) {
         unsigned long long lo = ~0ull, hi = 0;
-        candidates([&](unsigned long long k) {
-          if (k >= least) {
+        candidates([&](unsigned long long k, unsigned long long) __attribute__((always_inline)) {
+          if (k >= least && k <= most) {
             lo = min(lo, k);
             hi = max(hi, k);
           }
         });
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) {
-          lo = min(lo, __shfl_xor(lo, o, 64));
-          hi = max(hi, __shfl_xor(hi, o, 64));
+        lo = last_lane(wave_fold(lo, ~0ull, [](unsigned long long x, unsigned long long y) __attribute__((always_inline)) {
+          return min(x, y);
+        }));
+        hi = last_lane(wave_fold(hi, 0ull, [](unsigned long long x, unsigned long long y) __attribute__((always_inline)) {
+          return max(x, y);
+        }));
+        if (lane == 0) {
+          lows[wave] = lo;
+          highs[wave] = hi;
         }
         __syncthreads();
-        if (lane == 0) ull[wave] = lo;
-        __syncthreads();
-        for (int w = 0; w < NW; ++w) lo = min(lo, ull[w]);
-        __syncthreads();
-        if (lane == 0) ull[wave] = hi;
-        __syncthreads();
-        for (int w = 0; w < NW; ++w) hi = max(hi, ull[w]);
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+          lo = min(lo, lows[w]);
+          hi = max(hi, highs[w]);
+        }
         if (lo > hi) return least;                       // there are none
-        int have = p.count0;
-        unsigned long long held = (unsigned long long)(p.mass0 * unit);
         while (lo < hi) {
           const int shift = max(0, 64 - __clzll((long long)(hi - lo)) - 10);
-          for (int i = tid; i < kParts; i += NT) {
-            pm[i] = 0;
-            pc[i] = 0;
+#pragma unroll
+          for (int i = 0; i < kParts / NT; ++i) {
+            pm[i * NT + tid] = 0;
+            pc[i * NT + tid] = 0;
           }
+          if (tid == 0) part = INT32_MAX;
           __syncthreads();
-          candidates([&](unsigned long long k) {
+          candidates([&](unsigned long long k, unsigned long long w) __attribute__((always_inline)) {
             if (k < lo || k > hi) return;
             const int i = kParts - 1 - (int)((k - lo) >> shift);       // falling
-            atomicAdd(&pm[i], fixed(unordered((uint32_t)(k >> 32))));
+            atomicAdd(&pm[i], w);
             atomicAdd(&pc[i], 1u);
           });
           __syncthreads();
           const unsigned long long m0 = pm[2 * tid], m1 = pm[2 * tid + 1];
           const int c0 = (int)pc[2 * tid], c1 = (int)pc[2 * tid + 1];
-          unsigned long long mt;
-          int ct;
-          const unsigned long long me = group_scan(m0 + m1, ull, tid, mt) - m1;
-          const int ce = group_scan(c0 + c1, ints, tid, ct) - c1;
-          if (tid == 0) part = INT32_MAX;
+          const unsigned long long ms = wave_scan(m0 + m1);
+          const int cs = wave_scan(c0 + c1);
+          if (lane == 63) {
+            ull[0][wave] = ms;
+            ints[wave] = cs;
+          }
           __syncthreads();
-          auto there = [&](int c, unsigned long long m) {
-            return want > 0 ? have + c >= want : (double)(held + m) >= goal;
+          unsigned long long me = ms - m1;
+          int ce = cs - c1;
+#pragma unroll
+          for (int w = 0; w < NW; ++w)
+            if (w < wave) {
+              me += ull[0][w];
+              ce += ints[w];
+            }
+          auto there = [&](int n, unsigned long long w) __attribute__((always_inline)) {
+            return want > 0 ? have + n >= want : (double)(sum + w) >= goal;
           };
-          if (c0 && there(ce, me)) atomicMin(&part, 2 * tid);
-          else if (c1 && there(ce + c1, me + m1)) atomicMin(&part, 2 * tid + 1);
+          const bool even = c0 && there(ce, me), odd = c1 && there(ce + c1, me + m1);
+          const unsigned long long who = __ballot(even || odd);
+          if (who && lane == __ffsll((long long)who) - 1) atomicMin(&part, 2 * tid + (even ? 0 : 1));
           __syncthreads();
           const int at = part;
           if (at == INT32_MAX) return lo;                // not reached: all of them
-          // what lies before that part
-          if (at / 2 == tid) {
-            ints[0] = at % 2 ? ce : ce - c0;
-            ull[0] = at % 2 ? me : me - m0;
+          if (at / 2 == tid) {                           // what lies before that part
+            before_count = at % 2 ? ce : ce - c0;
+            before_mass = at % 2 ? me : me - m0;
+            part_count = at % 2 ? c1 : c0;
           }
           __syncthreads();
-          have += ints[0];
-          held += ull[0];
+          have += before_count;
+          sum += before_mass;
           const unsigned long long from = lo + ((unsigned long long)(kParts - 1 - at) << shift);
           const unsigned long long to = from + ((1ull << shift) - 1);
           lo = max(lo, from);
           hi = min(hi, to);
-          __syncthreads();
-          if (shift == 0) break;
+          if (part_count == 1) break;                    // the only key from lo to hi
         }
         return lo;
       };
-      unsigned long long least = 0;
-      if (p.limited && p.xm > -INFINITY) least = (unsigned long long)ordered(p.xm) << 32;
-      if (p.limited && s.k > 0) least = max(least, find(least, s.k, 0.0));
-      if (s.p < 1.0f) {
-        unsigned long long sum = 0;
-        candidates([&](unsigned long long k) {
-          if (k >= least) sum += fixed(unordered((uint32_t)(k >> 32)));
+      // Bin limit holds the lowest listed keys.
+      auto in_limit = [&](unsigned long long k) __attribute__((always_inline)) { return bin_of(key_logit(k)) == p.limit; };
+      unsigned long long least = 0, most = 0;            // most: the greatest key of bin limit
+      if (p.limit < kBins) {
+        if (p.xm > -INFINITY) least = (unsigned long long)ordered(p.xm) << 32;
+        candidates([&](unsigned long long k, unsigned long long) __attribute__((always_inline)) {
+          if (in_limit(k)) most = max(most, k);
         });
-        unsigned long long all;
-        if (!p.limited) {
-          border = find(least, 0, (double)s.p * p.total * unit);     // no limit before it
-        } else {
-          group_scan(sum, ull, tid, all);
-          border = find(least, 0, (double)s.p * ((double)all + p.mass0 * unit));
+        most = group_max(most);
+        if (s.k > 0) {
+          least = max(least, find(least, most, p.count1, s.k, 0, 0.0));
+          __syncthreads();                               // lows, highs and part are free again
         }
-      } else {
-        border = least;
       }
+      border = least;
+      if (s.p < 1.0f) {
+        double of = p.total;
+        if (p.limit < kBins) {
+          unsigned long long w = 0;
+          candidates([&](unsigned long long k, unsigned long long v) __attribute__((always_inline)) {
+            if (k >= least && in_limit(k)) w += v;
+          });
+          w = wave_sum(w);
+          if (lane == 0) ull[1][wave] = w;
+          __syncthreads();
+          w = 0;
+#pragma unroll
+          for (int i = 0; i < NW; ++i) w += ull[1][i];
+          of = (double)w / unit + p.mass1;
+        }
+        if (p.last < p.limit) least = max(least, most + 1);            // the border lies before bin limit
+        border = find(least, ~0ull, 0, 0, (unsigned long long)(p.mass0 * unit), (double)s.p * of * unit);
+      }
+      // the listed tokens' share of their slices
+      __syncthreads();
+      candidates([&](unsigned long long k, unsigned long long w) __attribute__((always_inline)) {
+        if (k >= border) atomicAdd(&add[key_token(k) / SLICE], w);
+      });
     }
+    __syncthreads();
   }
-  // Weights kept in each slice, and which slice the token falls into.  The slices' sums are formed by one wave
-  // each, in turn; thread 0 adds them up in their order, so they are kept where the list was.
   auto kept = [&](float v, int t) __attribute__((always_inline)) {
-    if (!LIMITS) return v > -INFINITY;
+    if (!LIMITS) return s.best ? v == p.top : v > -INFINITY;
     if (!(v > -INFINITY)) return false;
     const int b = bin_of(v);
     return b < p.first || (b <= p.last && draw_key(v, t) >= border);
   };
-  // one slice after the other, the listed ones' share by going through them
-  __shared__ unsigned long long add[NW];
-  double sum = 0.0;                                      // of all slices, in every thread
-  // pass 0 sums up, pass 1 finds the slice
-  if (tid == 0) {
-    chosen = -1;
-    last_kept = -1;
-  }
-  __syncthreads();
-  double target = 0.0;
-  for (int pass = 0; pass < 2; ++pass) {
+  // The slices' kept weights, summed up in their order by one wave; the first whose sum passes u times the whole (the
+  // last one with any where rounding leaves none)
+  if (wave == 0) {
+    const double* own = LIMITS ? a.sure + (int64_t)row * a.slices : nullptr;
+    auto of = [&](int i) {
+      if (i >= a.slices) return 0.0;
+      const SliceStat t = stat[i];
+      if (!(t.top > -INFINITY)) return 0.0;
+      if (!LIMITS && s.best) return t.top == p.top ? 1.0 : 0.0;
+      double w = draw_weight(t.top, p.top, s.scale, roots) * (LIMITS ? own[i] : t.sum);
+      if (LIMITS) w += (double)add[i] / unit;
+      return w;
+    };
     double run = 0.0;
-    for (int s0 = 0; s0 < a.slices; s0 += NW) {
-      const int i = s0 + wave;
-      double part_sum = 0.0;
-      if (i < a.slices && stat[i].top > -INFINITY) {
-        const SliceStat t = stat[i];
-        const double f = exp(((double)t.top - (double)p.top) * s.inv_t);
-        if (!LIMITS || p.first >= kBins) {
-          part_sum = f * ((double)t.sum * (1.0 / kSliceUnit));
-        } else {
-          const int off = p.bin - t.bin;
-          unsigned long long m = 0;
-          const int64_t at = ((int64_t)row * a.slices + i) * kBins;
-          for (int b = lane; b < kBins - 1; b += 64)
-            if ((int64_t)off + b < p.first) m += a.mass[at + b];
-          m = wave_sum(m);
-          unsigned long long l = 0;
-          if (p.first <= p.last) {
-            const int from = i * slice_len, to = min(V, from + slice_len);
-            if (in_list) {
-              for (int q = lane; q < n_list; q += 64) {
-                const unsigned long long k = list[q];
-                const int at_t = (int)(0xFFFFFFFFu - (uint32_t)k);
-                if (k >= border && at_t >= from && at_t < to) l += fixed(unordered((uint32_t)(k >> 32)));
-              }
-            } else {
-              for (int q = from + lane; q < to; q += 64) {
-                const float v = draw_clean(x[q]);
-                if (!(v > -INFINITY)) continue;
-                const int b = bin_of(v);
-                if (b >= p.first && b <= p.last && draw_key(v, q) >= border) l += fixed(v);
-              }
-            }
-            l = wave_sum(l);
-          }
-          part_sum = f * ((double)m * (1.0 / kSliceUnit)) + (double)l / unit;
-        }
+    const double w0 = of(lane);
+    for (int s0 = 0; s0 < a.slices; s0 += 64) run += wave_sum(s0 ? of(s0 + lane) : w0);
+    const double target = (double)u * run;
+    double upto = 0.0, before = 0.0;
+    int found = -1;
+    for (int s0 = 0; s0 < a.slices; s0 += 64) {
+      const double w = s0 ? of(s0 + lane) : w0, c = upto + wave_scan(w);
+      const unsigned long long over = __ballot(w > 0.0 && c > target), any = __ballot(w > 0.0);
+      if (any) {
+        const int at = over ? __ffsll((long long)over) - 1 : 63 - __clzll((long long)any);
+        const double b = __shfl(c - w, at, 64);
+        found = s0 + at;
+        before = b;
       }
-      __syncthreads();
-      if (lane == 0) dbl[wave] = part_sum;
-      __syncthreads();
-      for (int w = 0; w < NW; ++w) {
-        const double next = run + dbl[w];
-        if (pass == 1 && tid == 0 && dbl[w] > 0.0) {
-          if (last_kept < 0 || !(share > target)) {      // not found yet: this one, or a later one
-            last_kept = s0 + w;
-            before_slice = run;
-            share = next;
-          }
-        }
-        run = next;
-      }
-      __syncthreads();
+      if (over) break;
+      upto = last_lane(c);
     }
-    if (pass == 0) {
-      sum = run;
-      target = (double)u * sum;
+    if (lane == 0) {
+      slice_at = max(found, 0);
+      before_slice = before;
+      all_kept = run;
+      hit = INT32_MAX;
+      last_kept = -1;
     }
   }
   __syncthreads();
-  // the token in that slice
-  const int s_at = max(last_kept, 0);
-  const double want = target - before_slice;
-  double run = 0.0;
-  const int from = s_at * slice_len, to = min(V, from + slice_len);
-  if (tid == 0) chosen = -1;
-  __syncthreads();
-  for (int t0 = from; t0 < to; t0 += 4 * NT) {
-    const int t = t0 + 4 * tid;
-    double w[4], mine = 0.0;
-    int lastk = -1;
+  // the token in that slice: every thread EACH logits in a row
+  const double want = (double)u * all_kept - before_slice;
+  const int from = slice_at * SLICE, t0 = from + EACH * tid;
+  double w[EACH], mine = 0.0;
+  int last = -1;
+  if (from + SLICE <= V) {
+    Four f[EACH / 4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float v = t + j < to ? draw_clean(x[t + j]) : -INFINITY;
-      w[j] = kept(v, t + j) ? draw_weight(v, p.top, s.inv_t) : 0.0;
-      mine += w[j];
-      if (w[j] > 0.0) lastk = t + j;
-    }
-    double total;
-    const double upto = group_scan(mine, dbl, tid, total);
-    if (tid == 0) part = INT32_MAX;
-    __syncthreads();
-    double c = run + (upto - mine);
-    int hit = INT32_MAX;
+    for (int j = 0; j < EACH / 4; ++j) f[j] = *(const Four*)(x + t0 + 4 * j);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      c += w[j];
-      if (w[j] > 0.0 && c > want && hit == INT32_MAX) hit = t + j;
+    for (int j = 0; j < EACH; ++j) w[j] = f[j / 4].v[j % 4];
+  } else {
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+      const float v = x[t0 + j < V ? t0 + j : V - 1];
+      w[j] = t0 + j < V ? v : -INFINITY;
     }
-    if (hit != INT32_MAX) atomicMin(&part, hit);
-    if (lastk >= 0) atomicMax(&chosen, lastk);           // where rounding leaves none: the last one
-    __syncthreads();
-    if (part != INT32_MAX) break;
-    run += total;
-    __syncthreads();
   }
+#pragma unroll
+  for (int j = 0; j < EACH; ++j) {
+    const float v = draw_clean((float)w[j]);
+    w[j] = kept(v, t0 + j) ? draw_weight(v, p.top, s.scale, roots) : 0.0;
+    mine += w[j];
+    if (w[j] > 0.0) last = t0 + j;
+  }
+  double total;
+  const double upto = group_scan(mine, dbl[0], tid, total);
+  double c = upto - mine;
+  int at = INT32_MAX;
+#pragma unroll
+  for (int j = 0; j < EACH; ++j) {
+    c += w[j];
+    if (w[j] > 0.0 && c > want && at == INT32_MAX) at = t0 + j;
+  }
+  if (at != INT32_MAX) atomicMin(&hit, at);
+  if (last >= 0) atomicMax(&last_kept, last);
+  __syncthreads();
   if (tid == 0) {
-    const int t = part != INT32_MAX ? part : max(chosen, from);
+    const int t = hit != INT32_MAX ? hit : max(last_kept, from);
     a.tokens[row] = t;
-    if (a.logprobs) a.logprobs[row] = (float)(((double)draw_clean(x[t]) - (double)p.top) * s.inv_t - log(sum));
+    if (a.logprobs)
+      a.logprobs[row] = s.best ? 0.0f : (float)(((double)draw_clean(x[t]) - (double)p.top) * s.inv_t - log(all_kept));
   }
 }
 
@@ -797,13 +942,12 @@ termezo_status termezo_sample(termezo_ctx* c, const float* logits, const float* 
   DeviceScope scope(c->device);
   if (scope.err != hipSuccess) return hip_status(c, scope.err, "sample");
   const int64_t most = std::min<int64_t>(rows, kMaxDrawRows);      // rows at a time
+  const bool limits = top_k || top_p || min_p;
   const int long_slices = (vocab + 8191) / 8192;
-  const bool large = most * long_slices >= 2 * (int64_t)c->n_cu || long_slices > 64;
-  const int slice = large ? 8192 : 2048, slices = (vocab + slice - 1) / slice;
-  // temperatures, read on the device, may ask for the best token: limits too
-  const bool limits = temperature || top_k || top_p || min_p;
+  const bool large = (limits && most * long_slices >= 2 * (int64_t)c->n_cu) || long_slices > 64;
+  const int slice = large ? 8192 : 2048, slices = (vocab + slice - 1) / slice;   // kMaxSlices at most
   const int64_t per_row = (int64_t)slices * sizeof(SliceStat) +
-                          (limits ? (int64_t)slices * kBins * 12 + sizeof(RowPlan) + 8 + (int64_t)kList * 8 : 0);
+                          (limits ? (int64_t)slices * (kBins * 12 + 8) + sizeof(RowPlan) + 8 + (int64_t)kList * 8 : 0);
   const termezo_status st = scratch_for(c, c->draw, most * per_row, "sample");
   if (st != TERMEZO_OK) return st;
   DrawArgs a{};
@@ -820,6 +964,7 @@ termezo_status termezo_sample(termezo_ctx* c, const float* logits, const float* 
   if (limits) {
     a.list = (unsigned long long*)take(most * kList * 8);
     a.mass = (unsigned long long*)take(most * slices * kBins * 8);
+    a.sure = (double*)take(most * slices * 8);
     a.plan = (RowPlan*)take(most * sizeof(RowPlan));
     a.listed = (int32_t*)take(most * 8);
     a.count = (uint32_t*)take(most * slices * kBins * 4);
@@ -839,12 +984,20 @@ termezo_status termezo_sample(termezo_ctx* c, const float* logits, const float* 
     a.tokens = tokens + r0;
     a.logprobs = from(logprobs);
     const dim3 grid((unsigned)slices, (unsigned)n);
-#define TMZ_DRAW(E)                                                                        \
-  if (limits) {                                                                            \
-    hipLaunchKernelGGL((k_draw_scan<E, true>), grid, dim3(256), 0, c->stream, a);          \
-    hipLaunchKernelGGL((k_draw_list<E>), grid, dim3(256), 0, c->stream, a);                \
-  } else {                                                                                 \
-    hipLaunchKernelGGL((k_draw_scan<E, false>), grid, dim3(256), 0, c->stream, a);         \
+    const dim3 rows_grid((unsigned)n), wide(kPickThreads);
+#define TMZ_DRAW(E)                                                                                          \
+  if (!limits) {                                                                                             \
+    hipLaunchKernelGGL((k_draw_scan<E, false, false>), grid, dim3(256), 0, c->stream, a);                    \
+    hipLaunchKernelGGL((k_draw_pick<false, E>), rows_grid, wide, 0, c->stream, a, unit);                     \
+  } else {                                                                                                   \
+    if (top_k) {                                                                                             \
+      hipLaunchKernelGGL((k_draw_scan<E, true, true>), grid, dim3(256), 0, c->stream, a);                    \
+      hipLaunchKernelGGL((k_draw_list<E, true>), grid, dim3(256), 0, c->stream, a);                          \
+    } else {                                                                                                 \
+      hipLaunchKernelGGL((k_draw_scan<E, true, false>), grid, dim3(256), 0, c->stream, a);                   \
+      hipLaunchKernelGGL((k_draw_list<E, false>), grid, dim3(256), 0, c->stream, a);                         \
+    }                                                                                                        \
+    hipLaunchKernelGGL((k_draw_pick<true, E>), rows_grid, wide, 0, c->stream, a, unit);                      \
   }
     if (large) {
       TMZ_DRAW(8)
@@ -852,10 +1005,6 @@ termezo_status termezo_sample(termezo_ctx* c, const float* logits, const float* 
       TMZ_DRAW(2)
     }
 #undef TMZ_DRAW
-    if (limits)
-      hipLaunchKernelGGL((k_draw_pick<true>), dim3((unsigned)n), dim3(kPickThreads), 0, c->stream, a, slice, unit);
-    else
-      hipLaunchKernelGGL((k_draw_pick<false>), dim3((unsigned)n), dim3(kPickThreads), 0, c->stream, a, slice, unit);
   }
   return hip_status(c, hipGetLastError(), "sample");
 }
