@@ -199,19 +199,190 @@ __global__ void __launch_bounds__(256) k_linear_rows(const int8_t* __restrict__ 
   }
 }
 
+// ---------------------------------------------------------------------------
+// Many tokens: BM tokens x BN weight rows a work group, K in steps of 128 bytes through a ring of NST stages in LDS that
+// direct loads fill (each lane's 16 bytes go from memory to LDS without registers).  Loads of step k + NST - 1
+// are issued as step k starts; one barrier a step.  Rows past the ends of the matrices are out of their buffers' range
+// and fetch nothing; behind K a weight row is followed by the next one, and the tokens' codes are zeros there.
+//   LDS: rows of 128 bytes, 16-byte chunk c of row r at chunk c ^ (r / 2 % 8), so that the fragment reads of
+// 16 consecutive rows fall on all banks.
+//   v_mfma_i32_32x32x32_i8 with the weights as the first operand: a lane's sixteen sums are one token's, in four
+// runs of four neighbouring outputs, which meet in LDS (32 tokens of a wave at a time) so that whole 16-byte units
+// go out.  In sub-step ks of a step lane l supplies the chunk 4 (l / 32) + ks of row l % 32 of both operands.
+// ---------------------------------------------------------------------------
+typedef int v16i __attribute__((ext_vector_type(16)));
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+constexpr int kStep = 128;
+static_assert(kStep == kPitch, "the tokens' codes come in whole steps");
+
+struct __attribute__((packed, aligned(2))) Unit {        // 16 bytes of a row that may begin anywhere
+  v4u v;
+};
+
+template <typename TY, int BM, int BN, int WM, int WN, int NST, int BPC>
+__global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), BPC * (BM / WM) * (BN / WN) / 4)
+    k_linear_tile(const int8_t* __restrict__ q, const float* __restrict__ xstep, const int8_t* __restrict__ codes,
+                  const float* __restrict__ steps, int64_t M, int64_t K, int64_t N, TY* __restrict__ out) {
+  constexpr int NW = (BM / WM) * (BN / WN), TM = WM / 32, TN = WN / 32, STAGE = (BM + BN) * kStep;
+  constexpr int AJ = BM / 8 / NW, BJ = BN / 8 / NW, DJ = AJ + BJ;      // direct loads of a wave and step: 8 rows each
+  static_assert(AJ * 8 * NW == BM && BJ * 8 * NW == BN && DJ * (NST - 1) < 64, "tile");
+  __shared__ __attribute__((aligned(1024))) int8_t lds[NST * STAGE];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int wm = wave / (BN / WN), wn = wave % (BN / WN);
+  int64_t tm, tn;
+  tile_of_block((M + BM - 1) / BM, (N + BN - 1) / BN, tm, tn);
+  const int64_t m0 = tm * BM, n0 = tn * BN, pitch = pitch_of(K);
+  const int nk = (int)(pitch / kStep);
+  const v4i_rsrc arsrc = buffer_of(q + m0 * pitch, (uint32_t)(min((int64_t)BM, M - m0) * pitch));
+  const v4i_rsrc brsrc = buffer_of(codes + n0 * K, (uint32_t)(min((int64_t)BN, N - n0) * K));
+  uint32_t aoff[AJ], boff[BJ];
+#pragma unroll
+  for (int j = 0; j < AJ; ++j) {
+    const int row = 8 * (AJ * wave + j) + lane / 8;
+    aoff[j] = (uint32_t)(row * pitch) + 16 * ((lane % 8) ^ ((row >> 1) & 7));
+  }
+#pragma unroll
+  for (int j = 0; j < BJ; ++j) {
+    const int row = 8 * (BJ * wave + j) + lane / 8;
+    boff[j] = (uint32_t)(row * K) + 16 * ((lane % 8) ^ ((row >> 1) & 7));
+  }
+  const uint32_t w = __builtin_amdgcn_readfirstlane(wave);
+  auto issue = [&](int kt, int st) __attribute__((always_inline)) {
+    const uint32_t k = (uint32_t)kt * kStep, base = lds_offset(lds) + (uint32_t)(st * STAGE);
+    // the whole offset in the part that the range check covers
+#pragma unroll
+    for (int j = 0; j < AJ; ++j) dma16_buf(aoff[j] + k, arsrc, 0u, base + 1024u * (AJ * w + j));
+#pragma unroll
+    for (int j = 0; j < BJ; ++j) dma16_buf(boff[j] + k, brsrc, 0u, base + (uint32_t)(BM * kStep) + 1024u * (BJ * w + j));
+  };
+  const int h = lane >> 5, n32 = lane & 31;
+  v16i acc[TN][TM];
+#pragma unroll
+  for (int b = 0; b < TN; ++b)
+#pragma unroll
+    for (int a = 0; a < TM; ++a)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[b][a][r] = 0;
+  const int arow = wm * WM + n32, brow = wn * WN + n32;
+  v4i af[2][TM], bf[2][TN];
+  auto fragments = [&](int st, int ks, int slot) __attribute__((always_inline)) {
+    const int8_t* A = lds + st * STAGE;
+    const int8_t* B = A + BM * kStep;
+    const int c = 4 * h + ks;
+#pragma unroll
+    for (int b = 0; b < TN; ++b) {
+      const int row = brow + 32 * b;
+      bf[slot][b] = *(const v4i*)(B + row * kStep + 16 * (c ^ ((row >> 1) & 7)));
+    }
+#pragma unroll
+    for (int a = 0; a < TM; ++a) {
+      const int row = arow + 32 * a;
+      af[slot][a] = *(const v4i*)(A + row * kStep + 16 * (c ^ ((row >> 1) & 7)));
+    }
+  };
+  auto products = [&](int slot) __attribute__((always_inline)) {
+#pragma unroll
+    for (int a = 0; a < TM; ++a)
+#pragma unroll
+      for (int b = 0; b < TN; ++b)
+        acc[b][a] = __builtin_amdgcn_mfma_i32_32x32x32_i8(bf[slot][b], af[slot][a], acc[b][a], 0, 0, 0);
+  };
+  // stages 0 .. NST - 2 on their way, the first one there before the loop
+#pragma unroll
+  for (int p = 0; p < NST - 1; ++p)
+    if (p < nk) issue(p, p);
+  if (NST > 2 && nk >= NST - 1) wait_vmcnt_le<(NST - 2) * DJ>(); else __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+  fragments(0, 0, 0);
+  int cur = 0;
+  for (int kt = 0; kt < nk; ++kt) {
+    const int into = cur == 0 ? NST - 1 : cur - 1, next = cur == NST - 1 ? 0 : cur + 1;
+    // the stage of step kt - 1: every wave had read it before the last barrier
+    if (kt + NST - 1 < nk) issue(kt + NST - 1, into);
+#pragma unroll
+    for (int ks = 0; ks < 3; ++ks) {
+      fragments(cur, ks + 1, (ks + 1) & 1);
+      products(ks & 1);
+    }
+    // step kt + 1 has landed (later ones may be on their way); its first fragments are read ahead of this step's last
+    // products
+    if (NST > 2 && kt + NST - 1 < nk) wait_vmcnt_le<(NST - 2) * DJ>(); else __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (kt + 1 < nk) fragments(next, 0, 0);
+    products(1);
+    cur = next;
+  }
+  // outputs: 32 tokens x WN of a wave at a time
+  constexpr int UB = 16 / (int)sizeof(TY), UPR = WN / UB, RB = WN * (int)sizeof(TY), PER = 32 * UPR / 64;
+  static_assert(NW * 32 * RB <= NST * STAGE, "outputs of a wave in LDS");
+  __syncthreads();
+  int8_t* stage = lds + wave * 32 * RB;
+  const int64_t nw = n0 + wn * WN;
+#pragma unroll
+  for (int a = 0; a < TM; ++a) {
+    const int64_t mw = m0 + wm * WM + 32 * a;
+    const int64_t m = mw + n32;
+    const float d = xstep[m < M ? m : M - 1];
+#pragma unroll
+    for (int b = 0; b < TN; ++b)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int col = 32 * b + 8 * g + 4 * h;          // four outputs from here on
+        float v[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int64_t n = nw + col + r;
+          v[r] = (float)acc[b][a][4 * g + r] * (d * steps[n < N ? n : N - 1]);
+        }
+        int8_t* at = stage + n32 * RB + 16 * ((col / UB) ^ (n32 % UPR)) + (col % UB) * (int)sizeof(TY);
+        if constexpr (sizeof(TY) == 2)
+          *(uint2*)at = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+        else
+          *(float4*)at = make_float4(v[0], v[1], v[2], v[3]);
+      }
+    // a wave's LDS operations are in order: no barrier
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int c = 64 * i + lane, row = c / UPR, u = c % UPR;
+      const int64_t mo = mw + row, no = nw + u * UB;
+      const v4u v = *(const v4u*)(stage + row * RB + 16 * (u ^ (row % UPR)));
+      if (mo >= M || no >= N) continue;
+      TY* p = out + mo * N + no;
+      if (no + UB <= N) {
+        ((Unit*)p)->v = v;
+      } else {
+#pragma unroll
+        for (int k = 0; k < UB; ++k)
+          if (no + k < N) {
+            if constexpr (sizeof(TY) == 2) p[k] = (uint16_t)(v[k / 2] >> (16 * (k % 2)));
+            else p[k] = __uint_as_float(v[k]);
+          }
+      }
+    }
+  }
+}
+
 int64_t linear_i8_scratch(int64_t M, int64_t K) { return M * pitch_of(K) + M * 4; }
 
 template <typename TY>
 static void linear_as(const int8_t* q, const float* xstep, const int8_t* codes, const float* steps, int64_t M,
                       int64_t K, int64_t N, TY* out, hipStream_t s) {
-  const int mt = M <= 16 ? 1 : 4;
-  const int64_t mtiles = (M + 16 * mt - 1) / (16 * mt), ntiles = (N + 63) / 64;
-  if (mt == 1)
-    hipLaunchKernelGGL((k_linear_rows<TY, 1, 4>), dim3((unsigned)(mtiles * ntiles)), dim3(256), 0, s, q, xstep, codes,
-                       steps, M, K, N, out, (int)mtiles);
-  else
-    hipLaunchKernelGGL((k_linear_rows<TY, 4, 4>), dim3((unsigned)(mtiles * ntiles)), dim3(256), 0, s, q, xstep, codes,
-                       steps, M, K, N, out, (int)mtiles);
+  auto tiles = [&](int bm, int bn) { return dim3((unsigned)(((M + bm - 1) / bm) * ((N + bn - 1) / bn))); };
+#define TMZ_TILE(BM, BN, WM, WN, NST, BPC)                                                                        \
+  hipLaunchKernelGGL((k_linear_tile<TY, BM, BN, WM, WN, NST, BPC>), tiles(BM, BN), dim3(64 * (BM / WM) * (BN / WN)), \
+                     0, s, q, xstep, codes, steps, M, K, N, out)
+  if (M <= 16) {
+    hipLaunchKernelGGL((k_linear_rows<TY, 1, 4>), dim3((unsigned)((N + 63) / 64)), dim3(256), 0, s, q, xstep, codes,
+                       steps, M, K, N, out, 1);
+  } else if (M <= 64) {
+    hipLaunchKernelGGL((k_linear_rows<TY, 4, 4>), dim3((unsigned)((N + 63) / 64)), dim3(256), 0, s, q, xstep, codes,
+                       steps, M, K, N, out, 1);
+  } else if (M <= 1024) {
+    TMZ_TILE(128, 128, 64, 64, 3, 1);
+  } else {
+    TMZ_TILE(256, 256, 128, 64, 2, 1);
+  }
+#undef TMZ_TILE
 }
 
 hipError_t launch_linear_i8(const void* x, termezo_dtype xdt, int64_t M, int64_t K, const int8_t* codes,
