@@ -576,7 +576,7 @@ termezo_status termezo_quantize_rows(termezo_ctx* ctx, const void* w, termezo_dt
  * fp32 operation rounded, then to out's type.  x [M][K] in xdt, out [M][N] in ydt (F32 or BF16
  * each), codes int8 [N][K], -128 .. 127.  An input row with a value that is not finite has NaN
  * in its whole output row.  out must not overlap an input.  Errors: INVALID_ARG (M 1 .. 2^24,
- * N 1 .. 2^24, K 1 .. 2^17 and a multiple of 16, dtypes, null or misaligned (16 bytes; steps 4)
+ * N 1 .. 2^24, M N at most 2^38, K 1 .. 2^17 and a multiple of 16, dtypes, null or misaligned (16 bytes; steps 4)
  * pointers), STATE (captured, with scratch to be allocated), OOM. */
 termezo_status termezo_linear_i8(termezo_ctx* ctx, const void* x, termezo_dtype xdt, int64_t M, int64_t K,
                                  const int8_t* codes, const float* steps, int64_t N, void* out,

@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <cmath>
 #include <string>
+#include <type_traits>
 
 #include "tmz_device.h"
 #include "tmz_internal.h"
@@ -15,8 +16,13 @@ constexpr float kTokenFloor = 1e-5f, kWeightFloor = 1e-30f;
 // Codes of tokens lie in rows of whole kPitch bytes, zeros behind K: products of what a weight row is
 // followed by then add nothing (integers have no NaN), and no kernel needs a loop of its own for a last
 // partial step.
+// Eight tokens' 128 bytes lie together: a direct load of 1 KB is then one piece of memory.
 constexpr int64_t kPitch = 128;
 __host__ __device__ inline int64_t pitch_of(int64_t K) { return (K + kPitch - 1) / kPitch * kPitch; }
+// Byte of token m and k (pitch: bytes of a token's row, whole kPitch).
+__device__ __forceinline__ int64_t token_at(int64_t m, int64_t k, int64_t pitch) {
+  return (m >> 3) * 8 * pitch + (k >> 7) * 1024 + (m & 7) * 128 + (k & 127);
+}
 
 // ---------------------------------------------------------------------------
 // Rows in 8 bits: a = max(max |x|, floor), q = rne(x (127 / a)), step a / 127.  One wave a row, 8 values a
@@ -64,13 +70,9 @@ struct Eight {                                           // 8 values as loaded
   }
 };
 
-template <typename T, int C>
-__global__ void __launch_bounds__(256) k_rows_i8(const T* __restrict__ x, int64_t M, int64_t K, int64_t pitch,
-                                                 float floor, int8_t* __restrict__ q, float* __restrict__ step) {
-  const int lane = threadIdx.x & 63;
-  const int64_t m = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (m >= M) return;                                    // whole wave
-  const T* row = x + m * K;
+// One row by one wave: put(k, codes of k .. k + 7) for all k < end (zeros from K on); the step in every lane.
+template <int C, typename T, typename F>
+__device__ __forceinline__ float row_codes(const T* row, int64_t K, int64_t end, float floor, int lane, F put) {
   const bool held = K <= 512 * C;
   Eight<T> e[C];
   uint32_t a = 0;
@@ -95,107 +97,195 @@ __global__ void __launch_bounds__(256) k_rows_i8(const T* __restrict__ x, int64_
   const bool fine = a < 0x7F800000u;
   const float top = fmaxf(__uint_as_float(a), floor);
   const float s = fine ? __fdiv_rn(127.0f, top) : 0.0f;
-  if (lane == 0) step[m] = fine ? __fdiv_rn(top, 127.0f) : __uint_as_float(0x7FC00000u);
-  int8_t* out = q + m * pitch;
   const uint2 none = make_uint2(0u, 0u);
   if (held) {
 #pragma unroll
     for (int i = 0; i < C; ++i) {
       const int64_t k = (int64_t)i * 512 + lane * 8;
-      if (k < pitch) *(uint2*)(out + k) = fine ? e[i].codes(s) : none;     // zeros behind K
+      if (k < end) put(k, fine ? e[i].codes(s) : none);
     }
   } else {
-    for (int64_t k = lane * 8; k < pitch; k += 512) {
+    for (int64_t k = lane * 8; k < end; k += 512) {
       Eight<T> f;
       f.zero();
       if (k < K) f.load(row + k);
-      *(uint2*)(out + k) = fine ? f.codes(s) : none;
+      put(k, fine ? f.codes(s) : none);
     }
   }
+  return fine ? __fdiv_rn(top, 127.0f) : __uint_as_float(0x7FC00000u);
 }
 
-hipError_t launch_rows_i8(const void* x, termezo_dtype dt, int64_t M, int64_t K, int64_t pitch, float floor,
-                          int8_t* q, float* step, hipStream_t s) {
+// TOKENS: into the tokens' layout, else rows of K bytes.
+template <typename T, int C, bool TOKENS>
+__global__ void __launch_bounds__(256) k_rows_i8(const T* __restrict__ x, int64_t M, int64_t K, int64_t pitch,
+                                                 float floor, int8_t* __restrict__ q, float* __restrict__ step) {
+  const int lane = threadIdx.x & 63;
+  const int64_t m = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (m >= M) return;                                    // whole wave
+  const float d = row_codes<C>(x + m * K, K, TOKENS ? pitch : K, floor, lane, [&](int64_t k, uint2 c) __attribute__((always_inline)) {
+    *(uint2*)(q + (TOKENS ? token_at(m, k, pitch) : m * K + k)) = c;
+  });
+  if (lane == 0) step[m] = d;
+}
+
+template <bool TOKENS>
+static hipError_t launch_rows_i8(const void* x, termezo_dtype dt, int64_t M, int64_t K, float floor, int8_t* q,
+                                 float* step, hipStream_t s) {
   const dim3 grid((unsigned)((M + 3) / 4));
+  const int64_t pitch = pitch_of(K);
   if (dt == TERMEZO_BF16)
-    hipLaunchKernelGGL((k_rows_i8<uint16_t, 8>), grid, dim3(256), 0, s, (const uint16_t*)x, M, K, pitch, floor, q, step);
+    hipLaunchKernelGGL((k_rows_i8<uint16_t, 8, TOKENS>), grid, dim3(256), 0, s, (const uint16_t*)x, M, K, pitch, floor, q,
+                       step);
   else
-    hipLaunchKernelGGL((k_rows_i8<float, 8>), grid, dim3(256), 0, s, (const float*)x, M, K, pitch, floor, q, step);
+    hipLaunchKernelGGL((k_rows_i8<float, 8, TOKENS>), grid, dim3(256), 0, s, (const float*)x, M, K, pitch, floor, q, step);
   return hipGetLastError();
 }
 
 // ---------------------------------------------------------------------------
 // Output values: acc (d_m steps[n]), each fp32 operation rounded.
 // ---------------------------------------------------------------------------
+struct __attribute__((packed, aligned(4))) Steps {
+  float v[4];
+};
+struct __attribute__((packed, aligned(2))) Half {        // four bf16 of a row that may begin anywhere
+  uint32_t v[2];
+};
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(uint16_t* p, float v) { *(__bf16*)p = (__bf16)v; }
 
-// Few rows: lane l of a wave loads 16 bytes of weight row l % 16 at byte 16 (l / 16) of a 64-byte step, the
-// same piece of token l % 16 is the other operand.  The four waves of a work group share VT x 16 weight rows and
-// divide the steps; their sums are joined in LDS.
-// grid: tiles of tokens x tiles of weight rows (the former fastest: they meet in the caches).
-template <typename TY, int MT, int VT>
-__global__ void __launch_bounds__(256) k_linear_rows(const int8_t* __restrict__ q, const float* __restrict__ xstep,
-                                                     const int8_t* __restrict__ codes,
-                                                     const float* __restrict__ steps, int64_t M, int64_t K,
-                                                     int64_t N, TY* __restrict__ out, int mtiles) {
-  __shared__ v4i red[3][MT * VT][64];
+// ---------------------------------------------------------------------------
+// Up to 32 tokens: bound by the bytes of the weights, which are read once, straight into matrix operands: lane l of a
+// wave loads 16 bytes of weight row l % 16 at byte 16 (l / 16) of a 64-byte step; the same piece of token l % 16 comes from
+// LDS, which holds all tokens' codes (rows 16 bytes apart beyond their length: 16 rows' reads fall on all
+// banks).  Up to 16 tokens are taken in 8 bits here, by every work group for itself (one launch); more come
+// from the quantiser.  Work groups walk the weights, 16 rows at a time, each wave its own (KW = 1) or all of
+// them together, dividing the steps (KW = NW, few weight rows); GS steps ahead of the products.
+// ---------------------------------------------------------------------------
+template <typename TX, typename TY, int MT, int KB, int NW, int KW, int GS>
+__global__ void __launch_bounds__(64 * NW) k_linear_walk(const TX* __restrict__ x, const int8_t* __restrict__ q,
+                                                     const float* __restrict__ xstep, const int8_t* __restrict__ codes,
+                                                     const float* __restrict__ steps, int M, int K, int64_t N,
+                                                     TY* __restrict__ out) {
+  constexpr int TW = NW / KW;                            // tiles at work
+  __shared__ __align__(16) int8_t xs[KB * 1024];
+  __shared__ float ds[16 * MT];
+  __shared__ v4i red[KW > 1 ? NW : 1][MT][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t m0 = (int64_t)(blockIdx.x % mtiles) * 16 * MT, n0 = (int64_t)(blockIdx.x / mtiles) * 16 * VT;
-  const int64_t pitch = pitch_of(K);
-  const int piece = (lane >> 4) * 16, nsteps = (int)((K + 63) / 64);
-  // rows past the end are read as the last one and not stored
-  const int8_t *xp[MT], *cp[VT];
+  const int kw = wave % KW, tw = wave / KW;
+  const int nsteps = (K + 63) / 64, pitch = nsteps * 64 + 16, g16 = (lane >> 4) * 16;
+  const int64_t tiles = (N + 15) / 16;
+  // this wave's steps: groups of GS, the waves of a tile in turn
+  const int groups = (nsteps + GS - 1) / GS;
+  auto row_of = [&](int64_t tile) __attribute__((always_inline)) {
+    const int64_t n = tile * 16 + (lane & 15);
+    return codes + (n < N ? n : N - 1) * K;
+  };
+  // behind K, and in groups behind the last: any weights, the tokens' codes are 0 there or the products unused
+  auto fetch = [&](const int8_t* row, int g, v4i* a) __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int64_t m = m0 + 16 * i + (lane & 15);
-    xp[i] = q + (m < M ? m : M - 1) * pitch + piece;
-  }
-#pragma unroll
-  for (int j = 0; j < VT; ++j) {
-    const int64_t n = n0 + 16 * j + (lane & 15);
-    cp[j] = codes + (n < N ? n : N - 1) * K;
-  }
-  v4i acc[MT][VT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i)
-#pragma unroll
-    for (int j = 0; j < VT; ++j) acc[i][j] = v4i{0, 0, 0, 0};
-  for (int s = wave; s < nsteps; s += 4) {
-    // behind K: any weights, the token's codes are 0 there
-    const int64_t k = (int64_t)s * 64 + piece < K ? (int64_t)s * 64 + piece : 0;
-    v4i a[VT], b[MT];
-#pragma unroll
-    for (int j = 0; j < VT; ++j) a[j] = *(const v4i*)(cp[j] + k);
-#pragma unroll
-    for (int i = 0; i < MT; ++i) b[i] = *(const v4i*)(xp[i] + (int64_t)s * 64);
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-      for (int j = 0; j < VT; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[j], b[i], acc[i][j], 0, 0, 0);
-  }
-  if (wave > 0)
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-      for (int j = 0; j < VT; ++j) red[wave - 1][i * VT + j][lane] = acc[i][j];
-  __syncthreads();
-  if (wave > 0) return;
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int64_t m = m0 + 16 * i + (lane & 15);
-    if (m >= M) continue;
-    const float d = xstep[m];
-#pragma unroll
-    for (int j = 0; j < VT; ++j) {
-#pragma unroll
-      for (int w = 0; w < 3; ++w) acc[i][j] += red[w][i * VT + j][lane];
-      const int64_t n = n0 + 16 * j + (lane >> 4) * 4;
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (n + r < N) put(out + m * N + n + r, (float)acc[i][j][r] * (d * steps[n + r]));
+    for (int u = 0; u < GS; ++u) {
+      const int k = (g * GS + u) * 64 + g16;
+      a[u] = *(const v4i*)(row + (k < K ? k : 0));
     }
+  };
+  v4i w[2][GS];
+  int64_t tile = (int64_t)blockIdx.x * TW + tw;
+  const int8_t* row = row_of(tile < tiles ? tile : tiles - 1);
+  fetch(row, kw, w[0]);                                  // on its way while the tokens are prepared
+  if constexpr (!std::is_same<TX, void>::value) {
+    for (int m = wave; m < M; m += NW) {
+      const float d = row_codes<8>(x + (int64_t)m * K, K, nsteps * 64, kTokenFloor, lane,
+                                   [&](int64_t k, uint2 c) __attribute__((always_inline)) { *(uint2*)(xs + m * pitch + k) = c; });
+      if (lane == 0) ds[m] = d;
+    }
+  } else {
+    const int64_t from = pitch_of(K);
+    const int pieces = nsteps * 4;
+    for (int i = threadIdx.x; i < M * pieces; i += 64 * NW) {
+      const int m = i / pieces, c = i - m * pieces;
+      *(uint4*)(xs + m * pitch + c * 16) = *(const uint4*)(q + token_at(m, c * 16, from));
+    }
+    if ((int)threadIdx.x < M) ds[threadIdx.x] = xstep[threadIdx.x];
+  }
+  __syncthreads();
+  int xo[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) xo[i] = (16 * i + (lane & 15) < M ? 16 * i + (lane & 15) : M - 1) * pitch + g16;
+  const int64_t stride = (int64_t)gridDim.x * TW;
+  for (int64_t first = (int64_t)blockIdx.x * TW; first < tiles; first += stride, tile += stride) {
+    const bool mine = tile < tiles;                      // whole wave
+    v4i acc[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) acc[i] = v4i{0, 0, 0, 0};
+    const int64_t n = tile * 16 + (lane >> 4) * 4;
+    const int8_t* next = row_of(tile + stride < tiles ? tile + stride : tiles - 1);
+    auto use = [&](int g, const v4i* a) __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < GS; ++u) {
+        if (g * GS + u >= nsteps) break;                 // uniform
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+          acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[u], *(const v4i*)(xs + xo[i] + (g * GS + u) * 64), acc[i], 0, 0, 0);
+      }
+    };
+    // two groups in turn, so that registers need no index; behind the last the next tile's first
+    int g = kw, slot = 0;
+    for (; g < groups; g += 2 * KW) {
+      if (g + KW < groups) fetch(row, g + KW, w[1]);
+      else fetch(next, kw, w[1]);
+      use(g, w[0]);
+      if (g + KW >= groups) {
+        slot = 1;
+        break;
+      }
+      if (g + 2 * KW < groups) fetch(row, g + 2 * KW, w[0]);
+      else fetch(next, kw, w[0]);
+      use(g + KW, w[1]);
+    }
+    if (slot)
+#pragma unroll
+      for (int u = 0; u < GS; ++u) w[0][u] = w[1][u];
+    row = next;
+    if constexpr (KW > 1) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i) red[wave][i][lane] = acc[i];
+      __syncthreads();
+      if (kw == 0)
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int v = 1; v < KW; ++v) acc[i] += red[wave + v][i][lane];
+    }
+    if (mine && kw == 0) {
+      float st[4];
+      if (n + 3 < N) {
+        const Steps f = *(const Steps*)(steps + n);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) st[r] = f.v[r];
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) st[r] = steps[n + r < N ? n + r : N - 1];
+      }
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const int m = 16 * i + (lane & 15);
+        if (m >= M) continue;
+        const float d = ds[m];
+        TY* p = out + (int64_t)m * N + n;
+        float v[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = (float)acc[i][r] * (d * st[r]);
+        if (n + 3 < N) {
+          if constexpr (sizeof(TY) == 4) *(Steps*)p = Steps{{v[0], v[1], v[2], v[3]}};
+          else *(Half*)p = Half{{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])}};
+        } else {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (n + r < N) put(p + r, v[r]);
+        }
+      }
+    }
+    if constexpr (KW > 1) __syncthreads();               // red is free again
   }
 }
 
@@ -212,8 +302,6 @@ __global__ void __launch_bounds__(256) k_linear_rows(const int8_t* __restrict__ 
 // ---------------------------------------------------------------------------
 typedef int v16i __attribute__((ext_vector_type(16)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
-constexpr int kStep = 128;
-static_assert(kStep == kPitch, "the tokens' codes come in whole steps");
 
 struct __attribute__((packed, aligned(2))) Unit {        // 16 bytes of a row that may begin anywhere
   v4u v;
@@ -223,61 +311,68 @@ template <typename TY, int BM, int BN, int WM, int WN, int NST, int BPC>
 __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), BPC * (BM / WM) * (BN / WN) / 4)
     k_linear_tile(const int8_t* __restrict__ q, const float* __restrict__ xstep, const int8_t* __restrict__ codes,
                   const float* __restrict__ steps, int64_t M, int64_t K, int64_t N, TY* __restrict__ out) {
-  constexpr int NW = (BM / WM) * (BN / WN), TM = WM / 32, TN = WN / 32, STAGE = (BM + BN) * kStep;
-  constexpr int AJ = BM / 8 / NW, BJ = BN / 8 / NW, DJ = AJ + BJ;      // direct loads of a wave and step: 8 rows each
-  static_assert(AJ * 8 * NW == BM && BJ * 8 * NW == BN && DJ * (NST - 1) < 64, "tile");
+  constexpr int BK = kPitch, NW = (BM / WM) * (BN / WN), TM = WM / 32, TN = WN / 32, STAGE = (BM + BN) * BK;
+  constexpr int CH = BK / 16, RPL = 64 / CH, KS = BK / 32;            // chunks a row, rows a direct load, sub-steps
+  constexpr int AJ = BM / RPL / NW, BJ = BN / RPL / NW, DJ = AJ + BJ;  // direct loads of a wave and step
+  static_assert(AJ * RPL * NW == BM && BJ * RPL * NW == BN && DJ * (NST - 1) < 64, "tile");
+  auto turn = [](int row) __attribute__((always_inline)) { return (row >> 1) & 7; };
   __shared__ __attribute__((aligned(1024))) int8_t lds[NST * STAGE];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wm = wave / (BN / WN), wn = wave % (BN / WN);
-  int64_t tm, tn;
-  tile_of_block((M + BM - 1) / BM, (N + BN - 1) / BN, tm, tn);
-  const int64_t m0 = tm * BM, n0 = tn * BN, pitch = pitch_of(K);
-  const int nk = (int)(pitch / kStep);
-  const v4i_rsrc arsrc = buffer_of(q + m0 * pitch, (uint32_t)(min((int64_t)BM, M - m0) * pitch));
-  const v4i_rsrc brsrc = buffer_of(codes + n0 * K, (uint32_t)(min((int64_t)BN, N - n0) * K));
+  const int64_t pitch = pitch_of(K);
+  const uint32_t nb_m = (uint32_t)((M + BM - 1) / BM), nb_n = (uint32_t)((N + BN - 1) / BN), tiles = nb_m * nb_n;
+  const int nk = (int)((K + BK - 1) / BK);
+  // This work group's tiles: every XCD takes a contiguous part of the order (groups of kGroupM tile rows, so that the
+  // tiles at work on it share rows of both operands in its L2), its work groups take that in turn
+  const uint32_t xcd = blockIdx.x % kXcd, groups = (gridDim.x - xcd + kXcd - 1) / kXcd;
+  const uint32_t part0 = (uint32_t)xcd_linear(xcd, tiles), part1 = xcd + 1 < kXcd ? (uint32_t)xcd_linear(xcd + 1, tiles) : tiles;
+  uint32_t at = part0 + blockIdx.x / kXcd;
+  if (at >= part1) return;
+  auto place = [&](uint32_t t, int64_t& m, int64_t& n) __attribute__((always_inline)) {
+    const uint32_t span = kGroupM * nb_n, g = t / span, in = t - g * span, gm = min((uint32_t)kGroupM, nb_m - g * kGroupM);
+    m = (int64_t)(g * kGroupM + in % gm) * BM;
+    n = (int64_t)(in / gm) * BN;
+  };
+  v4i_rsrc arsrc, brsrc;
+  int64_t m0, n0;
+  place(at, m0, n0);
   uint32_t aoff[AJ], boff[BJ];
 #pragma unroll
   for (int j = 0; j < AJ; ++j) {
-    const int row = 8 * (AJ * wave + j) + lane / 8;
-    aoff[j] = (uint32_t)(row * pitch) + 16 * ((lane % 8) ^ ((row >> 1) & 7));
+    const int row = RPL * (AJ * wave + j) + lane / CH;
+    aoff[j] = (uint32_t)token_at(row, 16 * ((lane % CH) ^ turn(row)), pitch);
   }
 #pragma unroll
   for (int j = 0; j < BJ; ++j) {
-    const int row = 8 * (BJ * wave + j) + lane / 8;
-    boff[j] = (uint32_t)(row * K) + 16 * ((lane % 8) ^ ((row >> 1) & 7));
+    const int row = RPL * (BJ * wave + j) + lane / CH;
+    boff[j] = (uint32_t)(row * K) + 16 * ((lane % CH) ^ turn(row));
   }
   const uint32_t w = __builtin_amdgcn_readfirstlane(wave);
   auto issue = [&](int kt, int st) __attribute__((always_inline)) {
-    const uint32_t k = (uint32_t)kt * kStep, base = lds_offset(lds) + (uint32_t)(st * STAGE);
+    const uint32_t k = (uint32_t)kt * BK, base = lds_offset(lds) + (uint32_t)(st * STAGE);
     // the whole offset in the part that the range check covers
 #pragma unroll
-    for (int j = 0; j < AJ; ++j) dma16_buf(aoff[j] + k, arsrc, 0u, base + 1024u * (AJ * w + j));
+    for (int j = 0; j < AJ; ++j) dma16_buf(aoff[j] + 8 * k, arsrc, 0u, base + 1024u * (AJ * w + j));
 #pragma unroll
-    for (int j = 0; j < BJ; ++j) dma16_buf(boff[j] + k, brsrc, 0u, base + (uint32_t)(BM * kStep) + 1024u * (BJ * w + j));
+    for (int j = 0; j < BJ; ++j) dma16_buf(boff[j] + k, brsrc, 0u, base + (uint32_t)(BM * BK) + 1024u * (BJ * w + j));
   };
   const int h = lane >> 5, n32 = lane & 31;
   v16i acc[TN][TM];
-#pragma unroll
-  for (int b = 0; b < TN; ++b)
-#pragma unroll
-    for (int a = 0; a < TM; ++a)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[b][a][r] = 0;
   const int arow = wm * WM + n32, brow = wn * WN + n32;
   v4i af[2][TM], bf[2][TN];
   auto fragments = [&](int st, int ks, int slot) __attribute__((always_inline)) {
     const int8_t* A = lds + st * STAGE;
-    const int8_t* B = A + BM * kStep;
-    const int c = 4 * h + ks;
+    const int8_t* B = A + BM * BK;
+    const int c = KS * h + ks;
 #pragma unroll
     for (int b = 0; b < TN; ++b) {
       const int row = brow + 32 * b;
-      bf[slot][b] = *(const v4i*)(B + row * kStep + 16 * (c ^ ((row >> 1) & 7)));
+      bf[slot][b] = *(const v4i*)(B + row * BK + 16 * (c ^ turn(row)));
     }
 #pragma unroll
     for (int a = 0; a < TM; ++a) {
       const int row = arow + 32 * a;
-      af[slot][a] = *(const v4i*)(A + row * kStep + 16 * (c ^ ((row >> 1) & 7)));
+      af[slot][a] = *(const v4i*)(A + row * BK + 16 * (c ^ turn(row)));
     }
   };
   auto products = [&](int slot) __attribute__((always_inline)) {
@@ -287,116 +382,248 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), BPC * (BM / WM) * 
       for (int b = 0; b < TN; ++b)
         acc[b][a] = __builtin_amdgcn_mfma_i32_32x32x32_i8(bf[slot][b], af[slot][a], acc[b][a], 0, 0, 0);
   };
-  // stages 0 .. NST - 2 on their way, the first one there before the loop
+  // outputs meet in LDS SC columns of 32 tokens at a time: UPR 16-byte units of UB outputs, RB bytes a token
+  constexpr int SC = WN < 128 / (int)sizeof(TY) ? WN : 128 / (int)sizeof(TY), UB = 16 / (int)sizeof(TY), UPR = SC / UB;
+  constexpr int RB = SC * (int)sizeof(TY), PER = 32 * UPR / 64;
+  static_assert(NW * 32 * RB <= STAGE, "outputs of the waves in a stage");
+  // The steps of all the work group's tiles are one stream: NST - 1 of them are on their way, across the tiles' ends
+  uint32_t ahead = at;                                   // the tile whose steps are being loaded, its next step
+  int ahead_k = 0, into = 0, flying = 0;
+  auto load = [&]() __attribute__((always_inline)) {
+    if (ahead >= part1) return;
+    if (ahead_k == 0) {
+      int64_t m, n;
+      place(ahead, m, n);
+      arsrc = buffer_of(q + m * pitch, (uint32_t)(min((int64_t)BM, (M - m + 7) / 8 * 8) * pitch));
+      brsrc = buffer_of(codes + n * K, (uint32_t)(min((int64_t)BN, N - n) * K));
+    }
+    issue(ahead_k, into);
+    into = into == NST - 1 ? 0 : into + 1;
+    ++flying;
+    if (++ahead_k == nk) {
+      ahead_k = 0;
+      ahead += groups;
+    }
+  };
+  // the oldest step on its way has landed; NST - 2 later ones may be on theirs
+  auto landed = [&]() __attribute__((always_inline)) {
+    if (NST > 2 && flying == NST - 1) wait_vmcnt_le<(NST - 2) * DJ>(); else __builtin_amdgcn_s_waitcnt(0);
+    --flying;
+    __syncthreads();
+  };
 #pragma unroll
-  for (int p = 0; p < NST - 1; ++p)
-    if (p < nk) issue(p, p);
-  if (NST > 2 && nk >= NST - 1) wait_vmcnt_le<(NST - 2) * DJ>(); else __builtin_amdgcn_s_waitcnt(0);
-  __syncthreads();
+  for (int p = 0; p < NST - 1; ++p) load();
+  landed();
   fragments(0, 0, 0);
   int cur = 0;
-  for (int kt = 0; kt < nk; ++kt) {
-    const int into = cur == 0 ? NST - 1 : cur - 1, next = cur == NST - 1 ? 0 : cur + 1;
-    // the stage of step kt - 1: every wave had read it before the last barrier
-    if (kt + NST - 1 < nk) issue(kt + NST - 1, into);
-#pragma unroll
-    for (int ks = 0; ks < 3; ++ks) {
-      fragments(cur, ks + 1, (ks + 1) & 1);
-      products(ks & 1);
-    }
-    // step kt + 1 has landed (later ones may be on their way); its first fragments are read ahead of this step's last
-    // products
-    if (NST > 2 && kt + NST - 1 < nk) wait_vmcnt_le<(NST - 2) * DJ>(); else __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-    if (kt + 1 < nk) fragments(next, 0, 0);
-    products(1);
-    cur = next;
-  }
-  // outputs: 32 tokens x WN of a wave at a time
-  constexpr int UB = 16 / (int)sizeof(TY), UPR = WN / UB, RB = WN * (int)sizeof(TY), PER = 32 * UPR / 64;
-  static_assert(NW * 32 * RB <= NST * STAGE, "outputs of a wave in LDS");
-  __syncthreads();
-  int8_t* stage = lds + wave * 32 * RB;
-  const int64_t nw = n0 + wn * WN;
-#pragma unroll
-  for (int a = 0; a < TM; ++a) {
-    const int64_t mw = m0 + wm * WM + 32 * a;
-    const int64_t m = mw + n32;
-    const float d = xstep[m < M ? m : M - 1];
+  for (;; at += groups) {
 #pragma unroll
     for (int b = 0; b < TN; ++b)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int col = 32 * b + 8 * g + 4 * h;          // four outputs from here on
-        float v[4];
+      for (int a = 0; a < TM; ++a)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int64_t n = nw + col + r;
-          v[r] = (float)acc[b][a][4 * g + r] * (d * steps[n < N ? n : N - 1]);
+        for (int r = 0; r < 16; ++r) acc[b][a][r] = 0;
+    for (int kt = 0; kt < nk; ++kt) {
+      const int next = cur == NST - 1 ? 0 : cur + 1;
+      load();                                            // into the stage that every wave had read before the last barrier
+#pragma unroll
+      for (int ks = 0; ks + 1 < KS; ++ks) {
+        // one fragment of the next sub-step, one product, and so on (left alone, the compiler reads each fragment right
+        // before its first use and waits for it)
+        fragments(cur, ks + 1, (ks + 1) & 1);
+        products(ks & 1);
+#pragma unroll
+        for (int i = 0; i < TM + TN; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          if (i < TM * TN) __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         }
-        int8_t* at = stage + n32 * RB + 16 * ((col / UB) ^ (n32 % UPR)) + (col % UB) * (int)sizeof(TY);
-        if constexpr (sizeof(TY) == 2)
-          *(uint2*)at = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-        else
-          *(float4*)at = make_float4(v[0], v[1], v[2], v[3]);
+        if (TM * TN > TM + TN) __builtin_amdgcn_sched_group_barrier(0x008, TM * TN - TM - TN, 0);
+        __builtin_amdgcn_sched_barrier(0);
       }
-    // a wave's LDS operations are in order: no barrier
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int c = 64 * i + lane, row = c / UPR, u = c % UPR;
-      const int64_t mo = mw + row, no = nw + u * UB;
-      const v4u v = *(const v4u*)(stage + row * RB + 16 * (u ^ (row % UPR)));
-      if (mo >= M || no >= N) continue;
-      TY* p = out + mo * N + no;
-      if (no + UB <= N) {
-        ((Unit*)p)->v = v;
+      // the next step has landed; its first fragments are read ahead of this one's last products
+      if (flying > 0) {
+        landed();
+        fragments(next, 0, 0);
       } else {
+        __syncthreads();                                 // the last step of all
+      }
+      products((KS - 1) & 1);
+      __builtin_amdgcn_sched_barrier(0);
+      if (kt + 1 < nk) cur = next;
+    }
+    // outputs, through the stage that was just read
+    int8_t* stage = lds + cur * STAGE + wave * 32 * RB;
+    const int64_t nw = n0 + wn * WN;
+    const int64_t mw = m0 + wm * WM;
+    float d[TM];
 #pragma unroll
-        for (int k = 0; k < UB; ++k)
-          if (no + k < N) {
-            if constexpr (sizeof(TY) == 2) p[k] = (uint16_t)(v[k / 2] >> (16 * (k % 2)));
-            else p[k] = __uint_as_float(v[k]);
+    for (int a = 0; a < TM; ++a) {
+      const int64_t m = mw + 32 * a + n32;
+      d[a] = xstep[m < M ? m : M - 1];
+    }
+#pragma unroll
+    for (int c0 = 0; c0 < WN; c0 += SC) {
+      float st[SC / 32][4][4];
+#pragma unroll
+      for (int b = 0; b < SC / 32; ++b)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int64_t n = nw + c0 + 32 * b + 8 * g + 4 * h;          // four outputs from here on
+          if (n + 3 < N) {
+            const Steps f = *(const Steps*)(steps + n);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) st[b][g][r] = f.v[r];
+          } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) st[b][g][r] = steps[n + r < N ? n + r : N - 1];
           }
+        }
+#pragma unroll
+      for (int a = 0; a < TM; ++a) {
+#pragma unroll
+        for (int b = 0; b < SC / 32; ++b)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int col = 32 * b + 8 * g + 4 * h;
+            float v[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] = (float)acc[c0 / 32 + b][a][4 * g + r] * (d[a] * st[b][g][r]);
+            int8_t* to = stage + n32 * RB + 16 * ((col / UB) ^ (n32 % UPR)) + (col % UB) * (int)sizeof(TY);
+            if constexpr (sizeof(TY) == 2)
+              *(uint2*)to = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+            else
+              *(float4*)to = make_float4(v[0], v[1], v[2], v[3]);
+          }
+        // a wave's LDS operations are in order: no barrier
+        v4u o[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const int c = 64 * i + lane, row = c / UPR, u = c % UPR;
+          o[i] = *(const v4u*)(stage + row * RB + 16 * (u ^ (row % UPR)));
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const int c = 64 * i + lane, row = c / UPR, u = c % UPR;
+          const int64_t mo = mw + 32 * a + row, no = nw + c0 + u * UB;
+          if (mo >= M || no >= N) continue;
+          TY* p = out + mo * N + no;
+          if (no + UB <= N) {
+            ((Unit*)p)->v = o[i];
+          } else {
+#pragma unroll
+            for (int k = 0; k < UB; ++k)
+              if (no + k < N) {
+                if constexpr (sizeof(TY) == 2) p[k] = (uint16_t)(o[i][k / 2] >> (16 * (k % 2)));
+                else p[k] = __uint_as_float(o[i][k]);
+              }
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);               // one row tile's values at a time in registers
       }
     }
+    if (at + groups >= part1) return;
+    __syncthreads();                                     // the stage is free again
+    place(at + groups, m0, n0);
+    cur = cur == NST - 1 ? 0 : cur + 1;
   }
 }
 
-int64_t linear_i8_scratch(int64_t M, int64_t K) { return M * pitch_of(K) + M * 4; }
+// What a launch of T tiles takes on cu compute units (us): the first tile of a compute unit c0 + l K, further ones a + b K
+// each (K in thousands), where T is no multiple of cu the last, partial round counts half of its share and half of a
+// whole one.  Fitted to eight weights at 40 to 8192 tokens (rms 6 to 11%); the tile with the least estimate is within 2%
+// of the best on average, 15% at worst.
+struct LinearCost {
+  int bm, bn;
+  float c0, l, a, b;
+};
+constexpr LinearCost kLinearBf16[4] = {{256, 256, 7.00f, 8.44f, 0.00f, 16.94f}, {128, 256, 5.75f, 5.25f, 1.73f, 8.53f},
+                                       {128, 128, 5.03f, 3.41f, 2.41f, 4.31f}, {64, 64, 4.93f, 2.06f, 0.37f, 1.45f}};
+constexpr LinearCost kLinearF32[4] = {{256, 256, 8.18f, 8.50f, 1.35f, 20.08f}, {128, 256, 6.33f, 5.46f, 4.55f, 8.27f},
+                                      {128, 128, 5.31f, 3.43f, 3.39f, 4.16f}, {64, 64, 4.83f, 2.19f, 0.58f, 1.42f}};
 
 template <typename TY>
-static void linear_as(const int8_t* q, const float* xstep, const int8_t* codes, const float* steps, int64_t M,
-                      int64_t K, int64_t N, TY* out, hipStream_t s) {
-  auto tiles = [&](int bm, int bn) { return dim3((unsigned)(((M + bm - 1) / bm) * ((N + bn - 1) / bn))); };
-#define TMZ_TILE(BM, BN, WM, WN, NST, BPC)                                                                        \
-  hipLaunchKernelGGL((k_linear_tile<TY, BM, BN, WM, WN, NST, BPC>), tiles(BM, BN), dim3(64 * (BM / WM) * (BN / WN)), \
-                     0, s, q, xstep, codes, steps, M, K, N, out)
-  if (M <= 16) {
-    hipLaunchKernelGGL((k_linear_rows<TY, 1, 4>), dim3((unsigned)((N + 63) / 64)), dim3(256), 0, s, q, xstep, codes,
-                       steps, M, K, N, out, 1);
-  } else if (M <= 64) {
-    hipLaunchKernelGGL((k_linear_rows<TY, 4, 4>), dim3((unsigned)((N + 63) / 64)), dim3(256), 0, s, q, xstep, codes,
-                       steps, M, K, N, out, 1);
-  } else if (M <= 1024) {
-    TMZ_TILE(128, 128, 64, 64, 3, 1);
-  } else {
-    TMZ_TILE(256, 256, 128, 64, 2, 1);
+static void linear_tiles(const int8_t* q, const float* xstep, const int8_t* codes, const float* steps, int64_t M,
+                         int64_t K, int64_t N, TY* out, int n_cu, hipStream_t s) {
+  auto count = [&](int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
+  int best = 0;
+  float least = 0.0f;
+  for (int t = 0; t < 4; ++t) {
+    const LinearCost& c = (sizeof(TY) == 2 ? kLinearBf16 : kLinearF32)[t];
+    const int64_t T = count(c.bm, c.bn);
+    const float k = 1e-3f * (float)K, r = (float)T / (float)n_cu;
+    const float more = 0.5f * (float)((T + n_cu - 1) / n_cu - 1) + (r > 1.0f ? 0.5f * (r - 1.0f) : 0.0f);
+    const float cost = c.c0 + c.l * k + more * (c.a + c.b * k);
+    if (t == 0 || cost < least) {
+      best = t;
+      least = cost;
+    }
+  }
+#define TMZ_TILE(BM, BN, WM, WN, NST, BPC)                                                                    \
+  hipLaunchKernelGGL((k_linear_tile<TY, BM, BN, WM, WN, NST, BPC>),                                           \
+                     dim3((unsigned)std::min<int64_t>(count(BM, BN), (int64_t)BPC * n_cu)),                   \
+                     dim3(64 * (BM / WM) * (BN / WN)), 0, s, q, xstep, codes, steps, M, K, N, out)
+  switch (best) {
+    case 0: TMZ_TILE(256, 256, 128, 64, 2, 1); break;
+    case 1: TMZ_TILE(128, 256, 64, 64, 3, 1); break;
+    case 2: TMZ_TILE(128, 128, 64, 32, 4, 1); break;
+    default: TMZ_TILE(64, 64, 32, 32, 3, 3);
   }
 #undef TMZ_TILE
+}
+
+// Whether the walk takes M tokens of K values, and whether it quantises them itself.
+static bool walk_ok(int64_t M, int64_t K) { return M <= 32 && M * ((K + 63) / 64 * 64 + 16) <= 140 * 1024; }
+static bool walk_quantises(int64_t M, int64_t K) { return M <= 16 && walk_ok(M, K); }
+
+int64_t linear_i8_scratch(int64_t M, int64_t K) {
+  return walk_quantises(M, K) ? 0 : (M + 7) / 8 * 8 * pitch_of(K) + M * 4;
+}
+
+template <typename TX, typename TY>
+static void linear_walk(const TX* x, const int8_t* q, const float* xstep, const int8_t* codes, const float* steps,
+                        int64_t M, int64_t K, int64_t N, TY* out, int n_cu, hipStream_t s) {
+  constexpr int MT = std::is_same<TX, void>::value ? 2 : 1;
+  const int64_t tiles = (N + 15) / 16, lds = M * ((K + 63) / 64 * 64 + 16);
+#define TMZ_WALK(KB, KW, GRID)                                                                              \
+  hipLaunchKernelGGL((k_linear_walk<TX, TY, MT, KB, 8, KW, 8 / (KW > 1 ? 4 : 1)>), dim3((unsigned)(GRID)), dim3(512), 0, s, \
+                     x, q, xstep, codes, steps, (int)M, (int)K, N, out)
+  if (tiles >= 8 * (int64_t)n_cu) {
+    if (lds <= 72 * 1024) TMZ_WALK(72, 1, std::min<int64_t>((tiles + 7) / 8, 2 * n_cu));
+    else TMZ_WALK(140, 1, std::min<int64_t>((tiles + 7) / 8, n_cu));
+  } else {
+    if (lds <= 36 * 1024) TMZ_WALK(36, 8, std::min<int64_t>(tiles, 3 * n_cu));
+    else TMZ_WALK(140, 8, std::min<int64_t>(tiles, n_cu));
+  }
+#undef TMZ_WALK
+}
+
+template <typename TY>
+static hipError_t linear_as(const void* x, termezo_dtype xdt, int64_t M, int64_t K, const int8_t* codes,
+                            const float* steps, int64_t N, TY* out, void* scratch, int n_cu, hipStream_t s) {
+  if (walk_quantises(M, K)) {
+    if (xdt == TERMEZO_BF16)
+      linear_walk((const uint16_t*)x, nullptr, nullptr, codes, steps, M, K, N, out, n_cu, s);
+    else
+      linear_walk((const float*)x, nullptr, nullptr, codes, steps, M, K, N, out, n_cu, s);
+    return hipGetLastError();
+  }
+  int8_t* q = (int8_t*)scratch;
+  float* xstep = (float*)(q + (M + 7) / 8 * 8 * pitch_of(K));
+  const hipError_t e = launch_rows_i8<true>(x, xdt, M, K, kTokenFloor, q, xstep, s);
+  if (e != hipSuccess) return e;
+  if (walk_ok(M, K))
+    linear_walk((const void*)nullptr, q, xstep, codes, steps, M, K, N, out, n_cu, s);
+  else
+    linear_tiles(q, xstep, codes, steps, M, K, N, out, n_cu, s);
+  return hipGetLastError();
 }
 
 hipError_t launch_linear_i8(const void* x, termezo_dtype xdt, int64_t M, int64_t K, const int8_t* codes,
                             const float* steps, int64_t N, void* out, termezo_dtype ydt, void* scratch,
                             int n_cu, hipStream_t s) {
-  int8_t* q = (int8_t*)scratch;
-  float* xstep = (float*)(q + M * pitch_of(K));
-  const hipError_t e = launch_rows_i8(x, xdt, M, K, pitch_of(K), kTokenFloor, q, xstep, s);
-  if (e != hipSuccess) return e;
   if (ydt == TERMEZO_BF16)
-    linear_as(q, xstep, codes, steps, M, K, N, (uint16_t*)out, s);
-  else
-    linear_as(q, xstep, codes, steps, M, K, N, (float*)out, s);
-  return hipGetLastError();
+    return linear_as(x, xdt, M, K, codes, steps, N, (uint16_t*)out, scratch, n_cu, s);
+  return linear_as(x, xdt, M, K, codes, steps, N, (float*)out, scratch, n_cu, s);
 }
 
 }  // namespace tmz
@@ -434,7 +661,7 @@ termezo_status termezo_quantize_rows(termezo_ctx* c, const void* w, termezo_dtyp
   if (!float_type(dtype) || !sizes_ok(N, K)) return refuse(c, "quantize_rows: a size or the type is out of range");
   DeviceScope scope(c->device);
   if (scope.err != hipSuccess) return hip_status(c, scope.err, "quantize_rows");
-  return hip_status(c, launch_rows_i8(w, dtype, N, K, K, kWeightFloor, codes, steps, c->stream), "quantize_rows");
+  return hip_status(c, launch_rows_i8<false>(w, dtype, N, K, kWeightFloor, codes, steps, c->stream), "quantize_rows");
 }
 
 termezo_status termezo_linear_i8(termezo_ctx* c, const void* x, termezo_dtype xdt, int64_t M, int64_t K,
@@ -443,7 +670,8 @@ termezo_status termezo_linear_i8(termezo_ctx* c, const void* x, termezo_dtype xd
   if (!x || !codes || !steps || !out || !aligned(x, 16) || !aligned(codes, 16) || !aligned(steps, 4) ||
       !aligned(out, 16))
     return refuse(c, "linear_i8: null or misaligned pointer");
-  if (!float_type(xdt) || !float_type(ydt) || !sizes_ok(N, K) || M <= 0 || M > (1 << 24))
+  if (!float_type(xdt) || !float_type(ydt) || !sizes_ok(N, K) || M <= 0 || M > (1 << 24) ||
+      M > (int64_t(1) << 38) / N)
     return refuse(c, "linear_i8: a size or a type is out of range");
   DeviceScope scope(c->device);
   if (scope.err != hipSuccess) return hip_status(c, scope.err, "linear_i8");
