@@ -70,23 +70,26 @@ struct Eight {                                           // 8 values as loaded
   }
 };
 
-// One row by one wave: put(k, codes of k .. k + 7) for all k < end (zeros from K on); the step in every lane.
-template <int C, typename T, typename F>
-__device__ __forceinline__ float row_codes(const T* row, int64_t K, int64_t end, float floor, int lane, F put) {
-  const bool held = K <= 512 * C;
+// One row by W waves (wave: which of them; W > 1: the whole work group): put(k, codes of k .. k + 7) for all k < end
+// (zeros from K on); the step in every lane.
+template <int C, int W, typename T, typename F>
+__device__ __forceinline__ float row_codes(const T* row, int64_t K, int64_t end, float floor, int lane, int wave, F put) {
+  constexpr int PASS = 512 * W;
+  const int64_t k0 = wave * 512 + lane * 8;
+  const bool held = K <= PASS * C;
   Eight<T> e[C];
   uint32_t a = 0;
   if (held) {
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-      const int64_t k = (int64_t)i * 512 + lane * 8;
+      const int64_t k = k0 + i * PASS;
       if (k < K) e[i].load(row + k);
       else e[i].zero();
     }
 #pragma unroll
     for (int i = 0; i < C; ++i) a = max(a, e[i].top());
   } else {
-    for (int64_t k = lane * 8; k < K; k += 512) {
+    for (int64_t k = k0; k < K; k += PASS) {
       Eight<T> f;
       f.load(row + k);
       a = max(a, f.top());
@@ -94,6 +97,13 @@ __device__ __forceinline__ float row_codes(const T* row, int64_t K, int64_t end,
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) a = max(a, (uint32_t)__shfl_xor((int)a, o, 64));
+  if constexpr (W > 1) {
+    __shared__ uint32_t tops[W];
+    if (lane == 0) tops[wave] = a;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < W; ++i) a = max(a, tops[i]);
+  }
   const bool fine = a < 0x7F800000u;
   const float top = fmaxf(__uint_as_float(a), floor);
   const float s = fine ? __fdiv_rn(127.0f, top) : 0.0f;
@@ -101,11 +111,11 @@ __device__ __forceinline__ float row_codes(const T* row, int64_t K, int64_t end,
   if (held) {
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-      const int64_t k = (int64_t)i * 512 + lane * 8;
+      const int64_t k = k0 + i * PASS;
       if (k < end) put(k, fine ? e[i].codes(s) : none);
     }
   } else {
-    for (int64_t k = lane * 8; k < end; k += 512) {
+    for (int64_t k = k0; k < end; k += PASS) {
       Eight<T> f;
       f.zero();
       if (k < K) f.load(row + k);
@@ -116,28 +126,35 @@ __device__ __forceinline__ float row_codes(const T* row, int64_t K, int64_t end,
 }
 
 // TOKENS: into the tokens' layout, else rows of K bytes.
-template <typename T, int C, bool TOKENS>
+// W waves a row: four where the rows are long or do not give every compute unit eight waves (777 x 6912 in fp32
+// 11.3 -> 6 us).
+template <typename T, int C, int W, bool TOKENS>
 __global__ void __launch_bounds__(256) k_rows_i8(const T* __restrict__ x, int64_t M, int64_t K, int64_t pitch,
                                                  float floor, int8_t* __restrict__ q, float* __restrict__ step) {
-  const int lane = threadIdx.x & 63;
-  const int64_t m = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t m = W > 1 ? blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
   if (m >= M) return;                                    // whole wave
-  const float d = row_codes<C>(x + m * K, K, TOKENS ? pitch : K, floor, lane, [&](int64_t k, uint2 c) __attribute__((always_inline)) {
-    *(uint2*)(q + (TOKENS ? token_at(m, k, pitch) : m * K + k)) = c;
-  });
-  if (lane == 0) step[m] = d;
+  const float d = row_codes<C, W>(x + m * K, K, TOKENS ? pitch : K, floor, lane, W > 1 ? wave : 0,
+                                  [&](int64_t k, uint2 c) __attribute__((always_inline)) {
+                                    *(uint2*)(q + (TOKENS ? token_at(m, k, pitch) : m * K + k)) = c;
+                                  });
+  if (lane == 0 && (W == 1 || wave == 0)) step[m] = d;
 }
 
 template <bool TOKENS>
 static hipError_t launch_rows_i8(const void* x, termezo_dtype dt, int64_t M, int64_t K, float floor, int8_t* q,
-                                 float* step, hipStream_t s) {
-  const dim3 grid((unsigned)((M + 3) / 4));
+                                 float* step, int n_cu, hipStream_t s) {
   const int64_t pitch = pitch_of(K);
-  if (dt == TERMEZO_BF16)
-    hipLaunchKernelGGL((k_rows_i8<uint16_t, 8, TOKENS>), grid, dim3(256), 0, s, (const uint16_t*)x, M, K, pitch, floor, q,
-                       step);
-  else
-    hipLaunchKernelGGL((k_rows_i8<float, 8, TOKENS>), grid, dim3(256), 0, s, (const float*)x, M, K, pitch, floor, q, step);
+#define TMZ_ROWS(T, C, W)                                                                                          \
+  hipLaunchKernelGGL((k_rows_i8<T, C, W, TOKENS>), dim3((unsigned)((W) > 1 ? M : (M + 3) / 4)), dim3(256), 0, s, (const T*)x, \
+                     M, K, pitch, floor, q, step)
+  const bool wide = K > 4096 || M < 8 * (int64_t)n_cu;
+  if (dt == TERMEZO_BF16) {
+    if (wide) TMZ_ROWS(uint16_t, 4, 4); else TMZ_ROWS(uint16_t, 8, 1);
+  } else {
+    if (wide) TMZ_ROWS(float, 4, 4); else TMZ_ROWS(float, 8, 1);
+  }
+#undef TMZ_ROWS
   return hipGetLastError();
 }
 
@@ -194,7 +211,7 @@ __global__ void __launch_bounds__(64 * NW) k_linear_walk(const TX* __restrict__ 
   fetch(row, kw, w[0]);                                  // on its way while the tokens are prepared
   if constexpr (!std::is_same<TX, void>::value) {
     for (int m = wave; m < M; m += NW) {
-      const float d = row_codes<8>(x + (int64_t)m * K, K, nsteps * 64, kTokenFloor, lane,
+      const float d = row_codes<8, 1>(x + (int64_t)m * K, K, nsteps * 64, kTokenFloor, lane, 0,
                                    [&](int64_t k, uint2 c) __attribute__((always_inline)) { *(uint2*)(xs + m * pitch + k) = c; });
       if (lane == 0) ds[m] = d;
     }
@@ -587,7 +604,7 @@ static void linear_walk(const TX* x, const int8_t* q, const float* xstep, const 
 #define TMZ_WALK(KB, KW, GRID)                                                                              \
   hipLaunchKernelGGL((k_linear_walk<TX, TY, MT, KB, 8, KW, 8 / (KW > 1 ? 4 : 1)>), dim3((unsigned)(GRID)), dim3(512), 0, s, \
                      x, q, xstep, codes, steps, (int)M, (int)K, N, out)
-  if (tiles >= 8 * (int64_t)n_cu) {
+  if (tiles >= 4 * (int64_t)n_cu) {
     if (lds <= 72 * 1024) TMZ_WALK(72, 1, std::min<int64_t>((tiles + 7) / 8, 2 * n_cu));
     else TMZ_WALK(140, 1, std::min<int64_t>((tiles + 7) / 8, n_cu));
   } else {
@@ -609,7 +626,7 @@ static hipError_t linear_as(const void* x, termezo_dtype xdt, int64_t M, int64_t
   }
   int8_t* q = (int8_t*)scratch;
   float* xstep = (float*)(q + (M + 7) / 8 * 8 * pitch_of(K));
-  const hipError_t e = launch_rows_i8<true>(x, xdt, M, K, kTokenFloor, q, xstep, s);
+  const hipError_t e = launch_rows_i8<true>(x, xdt, M, K, kTokenFloor, q, xstep, n_cu, s);
   if (e != hipSuccess) return e;
   if (walk_ok(M, K))
     linear_walk((const void*)nullptr, q, xstep, codes, steps, M, K, N, out, n_cu, s);
@@ -661,7 +678,7 @@ termezo_status termezo_quantize_rows(termezo_ctx* c, const void* w, termezo_dtyp
   if (!float_type(dtype) || !sizes_ok(N, K)) return refuse(c, "quantize_rows: a size or the type is out of range");
   DeviceScope scope(c->device);
   if (scope.err != hipSuccess) return hip_status(c, scope.err, "quantize_rows");
-  return hip_status(c, launch_rows_i8<false>(w, dtype, N, K, kWeightFloor, codes, steps, c->stream), "quantize_rows");
+  return hip_status(c, launch_rows_i8<false>(w, dtype, N, K, kWeightFloor, codes, steps, c->n_cu, c->stream), "quantize_rows");
 }
 
 termezo_status termezo_linear_i8(termezo_ctx* c, const void* x, termezo_dtype xdt, int64_t M, int64_t K,
