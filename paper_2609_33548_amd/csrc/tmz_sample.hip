@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(256) k_adjust(RuleArgs a) {
 // it goes through the row in the list's place.
 // Without limits the first and the last are enough.
 // ---------------------------------------------------------------------------
-constexpr int kBins = 128, kMaxDrawRows = 1024, kPickThreads = 512, kHeld = 16, kList = kHeld * kPickThreads;
+constexpr int kBins = 128, kMaxDrawRows = 1024, kPickThreads = 512, kList = 8192;
 constexpr int kCopies = 4;           // of the bins, so that neighbouring lanes seldom meet in one
 constexpr double kSliceUnit = 0x1p48;
 constexpr double kLog2e16 = 16.0 * 0x1.71547652b82fep+0, kLn2by16 = 0x1.62e42fefa39efp-5;   // 16 log2(e), ln(2) / 16
@@ -176,6 +176,7 @@ __device__ __forceinline__ Settings draw_settings(const DrawArgs& a, int row) {
   Settings s;
   float t = a.temperature ? a.temperature[row] : 1.0f;
   s.k = a.top_k ? max(a.top_k[row], 0) : 0;
+  if (s.k >= a.vocab) s.k = 0;
   s.p = a.top_p ? a.top_p[row] : 1.0f;
   s.min_p = a.min_p ? a.min_p[row] : 0.0f;
   s.bad = !(t >= 0.0f && t <= FLT_MAX) || s.p != s.p || s.min_p != s.min_p;
@@ -195,9 +196,10 @@ __device__ __forceinline__ Settings draw_settings(const DrawArgs& a, int row) {
   return s;
 }
 
-__device__ __forceinline__ float draw_clean(float x) { return x == x ? fminf(x + 0.0f, FLT_MAX) : -INFINITY; }
+// NaN is -inf, +inf the largest number, -0 is 0.
+__device__ __forceinline__ float draw_clean(float x) { return fminf(fmaxf(x + 0.0f, -INFINITY), FLT_MAX); }
 __device__ __forceinline__ int draw_bin(float x, float grid) {
-  return (int)fminf(fmaxf(floorf(x * grid), -1e9f), 1e9f);
+  return (int)__builtin_amdgcn_fmed3f(floorf(x * grid), -1e9f, 1e9f);
 }
 // exp(z) for z <= 0, given q = 16 z log2(e): q = n + f, |f| <= 1/2; 2^(n / 16) from a table of 2^(j / 16) that lies on
 // sixteen pairs of LDS banks, 2^(f / 16) from its series up to f^5 (what is left out is below 2^-42), fp64 throughout.
@@ -373,8 +375,8 @@ __global__ void __launch_bounds__(256) k_draw_scan(DrawArgs a) {
 
 template <int E, bool COUNT>
 __global__ void __launch_bounds__(256) k_draw_list(DrawArgs a) {
-  __shared__ double mass[kBins], half_mass[kBins], low_mass[4], factor[64];
-  __shared__ int count[kBins], half_count[kBins], low_count[4], offset[64];
+  __shared__ double mass[kBins], half_mass[kBins], factor[64];
+  __shared__ int count[kBins], half_count[kBins], offset[64];
   __shared__ float tops[4];
   __shared__ unsigned long long parts[4];
   __shared__ int counts[4], base;
@@ -399,35 +401,32 @@ __global__ void __launch_bounds__(256) k_draw_list(DrawArgs a) {
   __syncthreads();
   top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
   const int bin = draw_bin(top, s.grid);
-  // The row's bins, 64 slices at a time: thread j of either half of the work group takes bin j of every other slice;
-  // bins that are the row's last one or lower together (a slice's own last bin always is)
-  double m = 0.0, lm = 0.0;
-  int c = 0, lc = 0;
+  // The row's bins, 64 slices at a time: thread j of either half of the work group takes what falls on bin j of every other
+  // slice; the last bin has the rest
+  double m = 0.0, total = 0.0;
+  int c = 0;
   for (int s0 = 0; s0 < a.slices; s0 += 64) {
     const int n = min(64, a.slices - s0);
     __syncthreads();
-    if (tid < n) {
-      const SliceStat t = stat[s0 + tid];
-      const bool any = t.top > -INFINITY;
-      factor[tid] = any ? draw_weight(t.top, top, s.scale, roots) * (1.0 / kSliceUnit) : 0.0;
-      offset[tid] = any ? bin - t.bin : kBins;           // 0 or more; an empty slice has nothing in its bins
+    if (wave == 0) {
+      const SliceStat t = stat[s0 + (lane < n ? lane : 0)];
+      const bool any = lane < n && t.top > -INFINITY;
+      const double f = any ? draw_weight(t.top, top, s.scale, roots) : 0.0;
+      factor[lane] = f * (1.0 / kSliceUnit);
+      offset[lane] = any ? bin - t.bin : kBins;          // 0 or more; nothing of an empty slice
+      total += wave_sum(any ? f * t.sum : 0.0);
     }
     __syncthreads();
-    const int64_t at = ((int64_t)row * a.slices + s0) * kBins;
+    const unsigned long long* at = a.mass + ((int64_t)row * a.slices + s0) * kBins;
+    const uint32_t* ct = a.count + ((int64_t)row * a.slices + s0) * kBins;
 #pragma unroll 4
     for (int i = half; i < n; i += 2) {
-      const int off = offset[i];
-      const double f = factor[i];
-      // this thread's bin of the slice and the one that falls on this bin of the row
-      const int from = j - off;
-      const unsigned long long w = a.mass[at + i * kBins + j], v = a.mass[at + i * kBins + max(from, 0)];
-      const bool low = off >= kBins - 1 || j >= kBins - 1 - off, here = from >= 0 && j < kBins - 1;
-      if (here) m += f * (double)v;
-      if (low) lm += f * (double)w;
-      if (COUNT) {
-        const int cw = (int)a.count[at + i * kBins + j], cv = (int)a.count[at + i * kBins + max(from, 0)];
-        if (here) c += cv;
-        if (low) lc += cw;
+      const int from = j - offset[i], where = i * kBins + max(from, 0);
+      const unsigned long long v = at[where];
+      const int cv = COUNT ? (int)ct[where] : 0;
+      if (from >= 0 && j < kBins - 1) {
+        m += factor[i] * (double)v;
+        c += cv;
       }
     }
   }
@@ -435,35 +434,26 @@ __global__ void __launch_bounds__(256) k_draw_list(DrawArgs a) {
     half_mass[j] = m;
     if (COUNT) half_count[j] = c;
   }
-  lm = wave_sum(lm);
-  if (COUNT) lc = wave_sum(lc);
-  if (lane == 0) {
-    low_mass[wave] = lm;
-    low_count[wave] = lc;
-  }
   __syncthreads();
   if (!half) {
-    m += half_mass[j];
-    if (COUNT) c += half_count[j];
-    if (j == kBins - 1) {
-      m = (low_mass[0] + low_mass[1]) + (low_mass[2] + low_mass[3]);
-      c = low_count[0] + low_count[1] + low_count[2] + low_count[3];
-    }
-    mass[j] = m;
-    count[j] = c;
+    mass[j] = m + half_mass[j];
+    if (COUNT) count[j] = c + half_count[j];
   }
   __syncthreads();
   if (wave == 0) {                                       // sums up to each bin, and where the borders lie
     const double m0 = mass[2 * lane], m1 = mass[2 * lane + 1];
-    const int c0 = count[2 * lane], c1 = count[2 * lane + 1];
-    const double me = wave_scan(m0 + m1), mo = me - m1;
-    const int ce = wave_scan(c0 + c1), co = ce - c1;
+    const double sum = wave_scan(m0 + m1), me = lane == 63 ? fmax(total, sum) : sum, mo = sum - m1;
     mass[2 * lane] = mo;
     mass[2 * lane + 1] = me;
-    count[2 * lane] = co;
-    count[2 * lane + 1] = ce;
-    const double total = last_lane(me);
-    const int all = last_lane(ce);
+    int ce = 0, co = 0;
+    if (COUNT) {
+      const int c0 = count[2 * lane], c1 = count[2 * lane + 1];
+      ce = wave_scan(c0 + c1);
+      co = ce - c1;
+      count[2 * lane] = co;
+      count[2 * lane + 1] = ce;
+    }
+    total = last_lane(me);
     // the first bin up to which the sum is not below x (the last one if there is none)
     auto first_at = [&](bool even, bool odd) {
       const unsigned long long e = __ballot(even), o = __ballot(odd);
@@ -474,7 +464,7 @@ __global__ void __launch_bounds__(256) k_draw_list(DrawArgs a) {
     if (top > -INFINITY) {
       int b1 = kBins;                                    // where top_k's or min_p's border lies
       if (s.k == 1) b1 = 0;
-      else if (COUNT && s.k > 0 && s.k < all) b1 = first_at(co >= s.k, ce >= s.k);
+      else if (COUNT && s.k > 0) b1 = first_at(co >= s.k, ce >= s.k);
       if (s.min_p > 0.0f && s.min_p <= 1.0f) {
         // the least logit with (x - top) / T >= ln min_p: an estimate, then its neighbours
         const double z = log((double)s.min_p);
@@ -492,7 +482,7 @@ __global__ void __launch_bounds__(256) k_draw_list(DrawArgs a) {
       p.first = b1;
       p.last = b1 < kBins ? b1 : -1;
       if (b1 > 0 && b1 < kBins) {
-        p.count1 = count[b1 - 1];
+        if (COUNT) p.count1 = count[b1 - 1];
         p.mass1 = mass[b1 - 1];
       }
       if (s.p < 1.0f) {
@@ -524,10 +514,13 @@ __global__ void __launch_bounds__(256) k_draw_list(DrawArgs a) {
   if (first > last) return;
   if (!(own.top > -INFINITY) || min(bin - own.bin, kBins - 1) > (limit < kBins ? limit : last)) return;
   uint32_t mine = 0;                                     // which of them are listed
+  // as ranges of bins from below; the last bin reaches down to -inf (not included)
+  const int hi1 = bin - first, lo1 = last == kBins - 1 ? INT32_MIN : bin - last;
+  const int hi2 = limit > last && limit < kBins ? bin - limit : INT32_MIN, lo2 = limit == kBins - 1 ? INT32_MIN : bin - limit;
 #pragma unroll
   for (int i = 0; i < 4 * E; ++i) {
-    const int at = x[i] > -INFINITY ? min(bin - draw_bin(x[i], s.grid), kBins - 1) : kBins;
-    if ((at >= first && at <= last) || (at == limit && at < kBins)) mine |= 1u << i;
+    const int at = draw_bin(x[i], s.grid);
+    if (((at >= lo1 && at <= hi1) || (at >= lo2 && at <= hi2)) && x[i] > -INFINITY) mine |= 1u << i;
   }
   const int n = __popc(mine), upto = wave_scan(n);
   if (lane == 63) counts[wave] = upto;
@@ -571,11 +564,11 @@ constexpr int kMaxSlices = 2048;
 template <bool LIMITS, int E>
 __global__ void __launch_bounds__(kPickThreads) k_draw_pick(DrawArgs a, int unit_bits) {
   constexpr int kParts = 1024, NT = kPickThreads, NW = NT / 64, SLICE = 1024 * E, EACH = SLICE / NT;
-  __shared__ unsigned long long pm[LIMITS ? kParts : 1], add[LIMITS ? kMaxSlices : 1];
+  __shared__ unsigned long long keys[LIMITS ? kList : 1], pm[LIMITS ? kParts : 1], add[LIMITS ? kMaxSlices : 1];
   __shared__ uint32_t pc[LIMITS ? kParts : 1];
-  __shared__ unsigned long long lows[NW], highs[NW], ull[2][NW];
+  __shared__ unsigned long long ull[3][NW];
   __shared__ int ints[NW];
-  __shared__ double dbl[2][NW];
+  __shared__ double dbl[NW];
   __shared__ float tops[NW];
   __shared__ int part, part_count, before_count, slice_at, hit, last_kept;
   __shared__ unsigned long long before_mass;
@@ -584,8 +577,10 @@ __global__ void __launch_bounds__(kPickThreads) k_draw_pick(DrawArgs a, int unit
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = blockIdx.x, V = a.vocab;
   if (tid < 16) roots[tid] = kRoots[tid];
   const float* x = a.logits + (int64_t)row * V;
-  const Settings s = draw_settings(a, row);
   const SliceStat* stat = a.stat + (int64_t)row * a.slices;
+  const SliceStat first_stat = stat[lane < a.slices ? lane : 0];       // on their way
+  const double first_sure = LIMITS ? a.sure[(int64_t)row * a.slices + (lane < a.slices ? lane : 0)] : 0.0;
+  const Settings s = draw_settings(a, row);
   const double unit = (double)(1ull << unit_bits);
   float u = a.uniforms[row];
   const bool bad = s.bad || !(u >= 0.0f && u < 1.0f);
@@ -617,83 +612,92 @@ __global__ void __launch_bounds__(kPickThreads) k_draw_pick(DrawArgs a, int unit
     return;
   }
   auto bin_of = [&](float v) __attribute__((always_inline)) { return min(p.bin - draw_bin(v, s.grid), kBins - 1); };
-  auto fixed = [&](float v) __attribute__((always_inline)) { return draw_fix(draw_weight(v, p.top, s.scale, roots), unit); };
+  auto fixed = [&](unsigned long long k) __attribute__((always_inline)) {
+    return draw_fix(draw_weight(key_logit(k), p.top, s.scale, roots), unit);
+  };
 
   unsigned long long border = 0;                         // listed keys from here on are kept
   if constexpr (LIMITS) {
     for (int i = tid; i < a.slices; i += NT) add[i] = 0;
     if (p.first <= p.last) {
-      // The listed keys and weights: in registers, or taken from the row each time where the list did not hold them
+      // The listed keys (no key is 0): in LDS, or taken from the row each time where the list did not hold them.
+      // Loops stay loops: unrolled, this kernel was 40 KB of code, which it waited for.
       const bool held = n_list <= kList;
-      unsigned long long key[kHeld], weight[kHeld];
-      if (held) {
-        const unsigned long long* list = a.list + (int64_t)row * kList;
-#pragma unroll
-        for (int i = 0; i < kHeld; ++i) {
-          key[i] = 0;
-          if (i * NT < n_list && i * NT + tid < n_list) key[i] = list[i * NT + tid];
-        }
-#pragma unroll
-        for (int i = 0; i < kHeld; ++i) {
-          weight[i] = 0;
-          if (i * NT < n_list && key[i]) weight[i] = fixed(key_logit(key[i]));
-        }
+      const int n = held ? n_list : V;
+      const unsigned long long* list = a.list + (int64_t)row * kList;
+      auto from_row = [&](int t) {
+        const float v = draw_clean(x[t]);
+        const int b = bin_of(v);
+        return v > -INFINITY && ((b >= p.first && b <= p.last) || b == p.limit) ? draw_key(v, t) : 0ull;
+      };
+      // the least key of bins first .. last and the greatest of bin limit; the greatest of all
+      unsigned long long low = ~0ull, most = 0, high = 0;
+#pragma unroll 1
+      for (int i = tid; i < n; i += NT) {
+        const unsigned long long k = held ? list[i] : from_row(i);
+        if (held) keys[i] = k;
+        if (!k) continue;
+        low = min(low, k);
+        high = max(high, k);
+        if (bin_of(key_logit(k)) == p.limit) most = max(most, k);
       }
-      auto candidates = [&](auto f) __attribute__((always_inline)) {
-        if (held) {
+      auto greater = [](unsigned long long x, unsigned long long y) __attribute__((always_inline)) { return max(x, y); };
+      auto lesser = [](unsigned long long x, unsigned long long y) __attribute__((always_inline)) { return min(x, y); };
+      low = last_lane(wave_fold(low, ~0ull, lesser));
+      high = last_lane(wave_fold(high, 0ull, greater));
+      most = last_lane(wave_fold(most, 0ull, greater));
+      if (lane == 0) {
+        ull[0][wave] = low;
+        ull[1][wave] = high;
+        ull[2][wave] = most;
+      }
+      __syncthreads();
 #pragma unroll
-          for (int i = 0; i < kHeld; ++i)
-            if (i * NT < n_list && key[i]) f(key[i], weight[i]);       // no key is 0
-        } else {
-          for (int t = tid; t < V; t += NT) {
-            const float v = draw_clean(x[t]);
-            if (!(v > -INFINITY)) continue;
-            const int b = bin_of(v);
-            if ((b >= p.first && b <= p.last) || b == p.limit) f(draw_key(v, t), fixed(v));
+      for (int w = 0; w < NW; ++w) {
+        low = min(low, ull[0][w]);
+        high = max(high, ull[1][w]);
+        most = max(most, ull[2][w]);
+      }
+      unsigned long long least = 0;
+      if (p.limit < kBins && p.xm > -INFINITY) least = (unsigned long long)ordered(p.xm) << 32;
+      // First where top_k ends (in bin limit), then where top_p does: of the keys from lo to hi in falling order, the one
+      // at which the count from have on reaches want, or the weight from sum on reaches goal.
+#pragma unroll 1
+      for (int stage = 0; stage < 2; ++stage) {
+        const bool counting = stage == 0;
+        if (counting ? !(p.limit < kBins && s.k > 0) : !(s.p < 1.0f)) continue;
+        unsigned long long lo = least, hi = most, sum = 0;
+        int have = p.count1;
+        double goal = 0.0;
+        if (!counting) {
+          double of = p.total;
+          if (p.limit < kBins) {                         // what top_k and min_p keep
+            unsigned long long w = 0;
+#pragma unroll 1
+            for (int i = tid; i < n; i += NT) {
+              const unsigned long long k = held ? keys[i] : from_row(i);
+              if (k && k >= least && k <= most) w += fixed(k);
+            }
+            w = wave_sum(w);
+            __syncthreads();
+            if (lane == 0) ull[0][wave] = w;
+            __syncthreads();
+            w = 0;
+#pragma unroll
+            for (int i = 0; i < NW; ++i) w += ull[0][i];
+            of = (double)w / unit + p.mass1;
           }
+          goal = (double)s.p * of * unit;
+          sum = (unsigned long long)(p.mass0 * unit);
+          if (p.last < p.limit) lo = max(lo, most + 1);  // the border lies before bin limit
+          hi = high;
+          least = lo;
         }
-      };
-      // The border: of the keys from least to most in falling order, the one at which the count from have on reaches
-      // want, or (want 0) the weight from sum on reaches goal.
-      auto group_max = [&](unsigned long long v) {
-        v = last_lane(wave_fold(v, 0ull, [](unsigned long long x, unsigned long long y) __attribute__((always_inline)) {
-          return max(x, y);
-        }));
-        if (lane == 0) ull[1][wave] = v;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < NW; ++w) v = max(v, ull[1][w]);
-        __syncthreads();
-        return v;
-      };
-      auto find = [&](unsigned long long least, unsigned long long most, int have, int want, unsigned long long sum,
-                      double goal) {
-        unsigned long long lo = ~0ull, hi = 0;
-        candidates([&](unsigned long long k, unsigned long long) __attribute__((always_inline)) {
-          if (k >= least && k <= most) {
-            lo = min(lo, k);
-            hi = max(hi, k);
-          }
-        });
-        lo = last_lane(wave_fold(lo, ~0ull, [](unsigned long long x, unsigned long long y) __attribute__((always_inline)) {
-          return min(x, y);
-        }));
-        hi = last_lane(wave_fold(hi, 0ull, [](unsigned long long x, unsigned long long y) __attribute__((always_inline)) {
-          return max(x, y);
-        }));
-        if (lane == 0) {
-          lows[wave] = lo;
-          highs[wave] = hi;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-          lo = min(lo, lows[w]);
-          hi = max(hi, highs[w]);
-        }
-        if (lo > hi) return least;                       // there are none
+        lo = max(lo, low);
+        if (lo > hi) continue;                           // there are none
         while (lo < hi) {
           const int shift = max(0, 64 - __clzll((long long)(hi - lo)) - 10);
+          __syncthreads();
 #pragma unroll
           for (int i = 0; i < kParts / NT; ++i) {
             pm[i * NT + tid] = 0;
@@ -701,12 +705,14 @@ __global__ void __launch_bounds__(kPickThreads) k_draw_pick(DrawArgs a, int unit
           }
           if (tid == 0) part = INT32_MAX;
           __syncthreads();
-          candidates([&](unsigned long long k, unsigned long long w) __attribute__((always_inline)) {
-            if (k < lo || k > hi) return;
-            const int i = kParts - 1 - (int)((k - lo) >> shift);       // falling
-            atomicAdd(&pm[i], w);
-            atomicAdd(&pc[i], 1u);
-          });
+#pragma unroll 1
+          for (int i = tid; i < n; i += NT) {
+            const unsigned long long k = held ? keys[i] : from_row(i);
+            if (!k || k < lo || k > hi) continue;
+            const int at = kParts - 1 - (int)((k - lo) >> shift);      // falling
+            atomicAdd(&pc[at], 1u);
+            if (!counting) atomicAdd(&pm[at], fixed(k));
+          }
           __syncthreads();
           const unsigned long long m0 = pm[2 * tid], m1 = pm[2 * tid + 1];
           const int c0 = (int)pc[2 * tid], c1 = (int)pc[2 * tid + 1];
@@ -725,15 +731,15 @@ __global__ void __launch_bounds__(kPickThreads) k_draw_pick(DrawArgs a, int unit
               me += ull[0][w];
               ce += ints[w];
             }
-          auto there = [&](int n, unsigned long long w) __attribute__((always_inline)) {
-            return want > 0 ? have + n >= want : (double)(sum + w) >= goal;
+          auto there = [&](int c, unsigned long long w) __attribute__((always_inline)) {
+            return counting ? have + c >= s.k : (double)(sum + w) >= goal;
           };
           const bool even = c0 && there(ce, me), odd = c1 && there(ce + c1, me + m1);
           const unsigned long long who = __ballot(even || odd);
           if (who && lane == __ffsll((long long)who) - 1) atomicMin(&part, 2 * tid + (even ? 0 : 1));
           __syncthreads();
           const int at = part;
-          if (at == INT32_MAX) return lo;                // not reached: all of them
+          if (at == INT32_MAX) break;                    // not reached: all of them
           if (at / 2 == tid) {                           // what lies before that part
             before_count = at % 2 ? ce : ce - c0;
             before_mass = at % 2 ? me : me - m0;
@@ -748,46 +754,16 @@ __global__ void __launch_bounds__(kPickThreads) k_draw_pick(DrawArgs a, int unit
           hi = min(hi, to);
           if (part_count == 1) break;                    // the only key from lo to hi
         }
-        return lo;
-      };
-      // Bin limit holds the lowest listed keys.
-      auto in_limit = [&](unsigned long long k) __attribute__((always_inline)) { return bin_of(key_logit(k)) == p.limit; };
-      unsigned long long least = 0, most = 0;            // most: the greatest key of bin limit
-      if (p.limit < kBins) {
-        if (p.xm > -INFINITY) least = (unsigned long long)ordered(p.xm) << 32;
-        candidates([&](unsigned long long k, unsigned long long) __attribute__((always_inline)) {
-          if (in_limit(k)) most = max(most, k);
-        });
-        most = group_max(most);
-        if (s.k > 0) {
-          least = max(least, find(least, most, p.count1, s.k, 0, 0.0));
-          __syncthreads();                               // lows, highs and part are free again
-        }
+        least = lo;
       }
       border = least;
-      if (s.p < 1.0f) {
-        double of = p.total;
-        if (p.limit < kBins) {
-          unsigned long long w = 0;
-          candidates([&](unsigned long long k, unsigned long long v) __attribute__((always_inline)) {
-            if (k >= least && in_limit(k)) w += v;
-          });
-          w = wave_sum(w);
-          if (lane == 0) ull[1][wave] = w;
-          __syncthreads();
-          w = 0;
-#pragma unroll
-          for (int i = 0; i < NW; ++i) w += ull[1][i];
-          of = (double)w / unit + p.mass1;
-        }
-        if (p.last < p.limit) least = max(least, most + 1);            // the border lies before bin limit
-        border = find(least, ~0ull, 0, 0, (unsigned long long)(p.mass0 * unit), (double)s.p * of * unit);
-      }
       // the listed tokens' share of their slices
       __syncthreads();
-      candidates([&](unsigned long long k, unsigned long long w) __attribute__((always_inline)) {
-        if (k >= border) atomicAdd(&add[key_token(k) / SLICE], w);
-      });
+#pragma unroll 1
+      for (int i = tid; i < n; i += NT) {
+        const unsigned long long k = held ? keys[i] : from_row(i);
+        if (k && k >= border && bin_of(key_logit(k)) <= p.last) atomicAdd(&add[key_token(k) / SLICE], fixed(k));
+      }
     }
     __syncthreads();
   }
@@ -801,23 +777,26 @@ __global__ void __launch_bounds__(kPickThreads) k_draw_pick(DrawArgs a, int unit
   // last one with any where rounding leaves none)
   if (wave == 0) {
     const double* own = LIMITS ? a.sure + (int64_t)row * a.slices : nullptr;
-    auto of = [&](int i) {
+    auto of = [&](int i, const SliceStat& t, double sure) __attribute__((always_inline)) {
       if (i >= a.slices) return 0.0;
-      const SliceStat t = stat[i];
       if (!(t.top > -INFINITY)) return 0.0;
       if (!LIMITS && s.best) return t.top == p.top ? 1.0 : 0.0;
-      double w = draw_weight(t.top, p.top, s.scale, roots) * (LIMITS ? own[i] : t.sum);
+      double w = draw_weight(t.top, p.top, s.scale, roots) * (LIMITS ? sure : t.sum);
       if (LIMITS) w += (double)add[i] / unit;
       return w;
     };
     double run = 0.0;
-    const double w0 = of(lane);
-    for (int s0 = 0; s0 < a.slices; s0 += 64) run += wave_sum(s0 ? of(s0 + lane) : w0);
+    auto later = [&](int i) {
+      const int k = i < a.slices ? i : 0;
+      return of(i, stat[k], LIMITS ? own[k] : 0.0);
+    };
+    const double w0 = of(lane, first_stat, first_sure);
+    for (int s0 = 0; s0 < a.slices; s0 += 64) run += wave_sum(s0 ? later(s0 + lane) : w0);
     const double target = (double)u * run;
     double upto = 0.0, before = 0.0;
     int found = -1;
     for (int s0 = 0; s0 < a.slices; s0 += 64) {
-      const double w = s0 ? of(s0 + lane) : w0, c = upto + wave_scan(w);
+      const double w = s0 ? later(s0 + lane) : w0, c = upto + wave_scan(w);
       const unsigned long long over = __ballot(w > 0.0 && c > target), any = __ballot(w > 0.0);
       if (any) {
         const int at = over ? __ffsll((long long)over) - 1 : 63 - __clzll((long long)any);
@@ -863,7 +842,7 @@ __global__ void __launch_bounds__(kPickThreads) k_draw_pick(DrawArgs a, int unit
     if (w[j] > 0.0) last = t0 + j;
   }
   double total;
-  const double upto = group_scan(mine, dbl[0], tid, total);
+  const double upto = group_scan(mine, dbl, tid, total);
   double c = upto - mine;
   int at = INT32_MAX;
 #pragma unroll
