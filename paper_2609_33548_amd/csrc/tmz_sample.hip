@@ -11,9 +11,11 @@ namespace tmz {
 
 constexpr int32_t kErrRules = 64, kErrSample = 128;      // bits of the deferred error word
 
-struct __attribute__((packed, aligned(4))) Four {        // rows of any length begin at any multiple of 4 bytes
-  float v[4];
+template <int N>
+struct __attribute__((packed, aligned(4))) Floats {      // rows of any length begin at any multiple of 4 bytes
+  float v[N];
 };
+typedef Floats<4> Four;
 
 // ---------------------------------------------------------------------------
 // Rules on the logits, a work group for a slice of a row.  The history's tokens that fall into the slice
@@ -118,19 +120,19 @@ __global__ void __launch_bounds__(256) k_adjust(RuleArgs a) {
 //
 // k_draw_scan, a work group for a slice of a row: the slice's largest logit m_s, its weights exp((x - m_s) / T),
 // their sum, and sums and counts by bins (in fixed point, 2^-48: integer sums do not depend on their order).
-// A bin is a quarter of T wide on a grid that all slices share (bin = floor(x (4 / T))), counted from the slice's
-// best bin downwards; the last of the 128 holds all that lies lower.
+// A bin is an eighth of T wide on a grid that all slices share (bin = floor(x (8 / T))), counted from the slice's
+// best bin downwards; the last of the 256 holds all that lies lower.
 // k_draw_list, the same grid: the row's bins (slices weighted by exp((m_s - m) / T)) tell in which of them the
 // borders lie; the slice's logits in those bins go to the row's list.
-// k_draw_pick, a work group a row: finds the border in the list by narrowing a range of keys (logit, index) to
-// 1024 parts at a time; then the slice and the token.  Where the list does not hold them (many equal logits)
+// k_draw_pick, a work group a row: finds the border in the list by narrowing a range of keys (logit, index),
+// a part a thread at a time; then the slice and the token.  Where the list does not hold them (many equal logits)
 // it goes through the row in the list's place.
 // Without limits the first and the last are enough.
 // ---------------------------------------------------------------------------
-constexpr int kBins = 128, kMaxDrawRows = 1024, kPickThreads = 512, kList = 8192;
+constexpr int kBins = 256, kMaxDrawRows = 1024, kList = 8192;
 constexpr int kCopies = 4;           // of the bins, so that neighbouring lanes seldom meet in one
 constexpr double kSliceUnit = 0x1p48;
-constexpr double kLog2e16 = 16.0 * 0x1.71547652b82fep+0, kLn2by16 = 0x1.62e42fefa39efp-5;   // 16 log2(e), ln(2) / 16
+constexpr double kLog2e32 = 32.0 * 0x1.71547652b82fep+0, kLn2by32 = 0x1.62e42fefa39efp-6;   // 32 log2(e), ln(2) / 32
 
 struct SliceStat {
   float top;                         // -inf: nothing
@@ -138,7 +140,7 @@ struct SliceStat {
   double sum;                        // weights relative to top
 };
 struct RowPlan {                     // what k_draw_list found
-  float top, xm;                     // the row's largest logit; the least one that min_p keeps
+  float top, xm, x_first;            // the row's largest logit; the least one that min_p keeps; that of the bins before first
   int32_t bin;
   // Bins before first are kept; listed are bins first .. last, where top_p's border lies (or the only one), and
   // bin limit, where top_k or min_p ends (kBins: they do not)
@@ -165,8 +167,8 @@ struct DrawArgs {
 };
 
 struct Settings {
-  double inv_t, scale;               // 1 / T and kLog2e16 / T
-  float grid;                        // 4 / T
+  double inv_t, scale;               // 1 / T and kLog2e32 / T
+  float grid;                        // 8 / T
   float p, min_p;                    // p 1: none; min_p 0: none
   int k;                             // 0: none
   bool best, bad;                    // best: the best token alone
@@ -191,8 +193,8 @@ __device__ __forceinline__ Settings draw_settings(const DrawArgs& a, int row) {
   }
   if (s.min_p > 1.0f) s.k = 1;                           // no weight reaches it: the first one is kept
   s.inv_t = 1.0 / (double)t;
-  s.scale = kLog2e16 * s.inv_t;
-  s.grid = fminf(4.0f / t, FLT_MAX);
+  s.scale = kLog2e32 * s.inv_t;
+  s.grid = fminf(8.0f / t, FLT_MAX);
   return s;
 }
 
@@ -201,31 +203,36 @@ __device__ __forceinline__ float draw_clean(float x) { return fminf(fmaxf(x + 0.
 __device__ __forceinline__ int draw_bin(float x, float grid) {
   return (int)__builtin_amdgcn_fmed3f(floorf(x * grid), -1e9f, 1e9f);
 }
-// exp(z) for z <= 0, given q = 16 z log2(e): q = n + f, |f| <= 1/2; 2^(n / 16) from a table of 2^(j / 16) that lies on
-// sixteen pairs of LDS banks, 2^(f / 16) from its series up to f^5 (what is left out is below 2^-42), fp64 throughout.
-// Half the operations of a series without a table.
-__device__ const double kRoots[16] = {
-    0x1.0000000000000p+0, 0x1.0b5586cf9890fp+0, 0x1.172b83c7d517bp+0, 0x1.2387a6e756238p+0,
-    0x1.306fe0a31b715p+0, 0x1.3dea64c123422p+0, 0x1.4bfdad5362a27p+0, 0x1.5ab07dd485429p+0,
-    0x1.6a09e667f3bcdp+0, 0x1.7a11473eb0187p+0, 0x1.8ace5422aa0dbp+0, 0x1.9c49182a3f090p+0,
-    0x1.ae89f995ad3adp+0, 0x1.c199bdd85529cp+0, 0x1.d5818dcfba487p+0, 0x1.ea4afa2a490dap+0};
-__device__ __forceinline__ double exp_of(double q, const double* roots) {     // q >= -16000: no denormals
-  constexpr double l = kLn2by16;
+// exp(z) for z <= 0, given q = 32 z log2(e): q = n + f, |f| <= 1/2; 2^(n / 32) from a table of 2^(j / 32) whose entries
+// lie on LDS banks of their own, 2^(f / 32) from its series: f^5, the last term that counts, is replaced by the polynomial of
+// lower degree that is nearest to it on [-1/2, 1/2] (f^5 - T5(2 f) / 512), which leaves less than 2^-43.  fp64
+// throughout; half the operations of a series without a table.
+constexpr int kRootCount = 32;
+__device__ const double kRoots[kRootCount] = {
+    0x1.0000000000000p+0, 0x1.059b0d3158574p+0, 0x1.0b5586cf9890fp+0, 0x1.11301d0125b51p+0,
+    0x1.172b83c7d517bp+0, 0x1.1d4873168b9aap+0, 0x1.2387a6e756238p+0, 0x1.29e9df51fdee1p+0,
+    0x1.306fe0a31b715p+0, 0x1.371a7373aa9cbp+0, 0x1.3dea64c123422p+0, 0x1.44e086061892dp+0,
+    0x1.4bfdad5362a27p+0, 0x1.5342b569d4f82p+0, 0x1.5ab07dd485429p+0, 0x1.6247eb03a5585p+0,
+    0x1.6a09e667f3bcdp+0, 0x1.71f75e8ec5f74p+0, 0x1.7a11473eb0187p+0, 0x1.82589994cce13p+0,
+    0x1.8ace5422aa0dbp+0, 0x1.93737b0cdc5e5p+0, 0x1.9c49182a3f090p+0, 0x1.a5503b23e255dp+0,
+    0x1.ae89f995ad3adp+0, 0x1.b7f76f2fb5e47p+0, 0x1.c199bdd85529cp+0, 0x1.cb720dcef9069p+0,
+    0x1.d5818dcfba487p+0, 0x1.dfc97337b9b5fp+0, 0x1.ea4afa2a490dap+0, 0x1.f50765b6e4540p+0};
+__device__ __forceinline__ double exp_of(double q, const double* roots) {     // q >= -32000: no denormals
+  constexpr double l = kLn2by32, l5 = l * l * l * l * l / 120;
   const double shifted = q + 0x1.8p52;                   // rounded to a whole number n
   const int n = (int)(uint32_t)__double_as_longlong(shifted);
   const double f = q - (shifted - 0x1.8p52);
-  double p = l * l * l * l * l / 120;
-  p = fma(p, f, l * l * l * l / 24);
-  p = fma(p, f, l * l * l / 6);
+  double p = l * l * l * l / 24;
+  p = fma(p, f, l * l * l / 6 + l5 * 0.3125);
   p = fma(p, f, l * l / 2);
-  p = fma(p, f, l);
+  p = fma(p, f, l - l5 * 0.01953125);
   p = fma(p, f, 1.0);
-  const long long w = __double_as_longlong(p * roots[n & 15]);
-  return __longlong_as_double(w + ((long long)(n >> 4) << 52));
+  const double w = p * roots[n & (kRootCount - 1)];
+  return __hiloint2double(__double2hiint(w) + ((n >> 5) << 20), __double2loint(w));
 }
-// The weight of x beside top: exp((x - top) / T), scale = kLog2e16 / T.  -inf has 0, or what rounds to it.
+// The weight of x beside top: exp((x - top) / T), scale = kLog2e32 / T.  -inf has 0, or what rounds to it.
 __device__ __forceinline__ double draw_weight(float x, float top, double scale, const double* roots) {
-  return exp_of(fmax(((double)x - (double)top) * scale, -16000.0), roots);
+  return exp_of(fmax(((double)x - (double)top) * scale, -32000.0), roots);
 }
 // w in [0, 1] in units of 1 / unit (a power of two up to 2^51), rounded to nearest.
 __device__ __forceinline__ unsigned long long draw_fix(double w, double unit) {
@@ -294,22 +301,26 @@ __device__ __forceinline__ float wave_top(float v) {
   return last_lane(wave_fold(v, -INFINITY, [](float a, float b) __attribute__((always_inline)) { return fmaxf(a, b); }));
 }
 
-// A slice's logits, 4 * E of a thread: x[4 i + j] at t0 + 1024 i + 4 tid + j; -inf behind the row's end.
+// A slice's logits, 4 * E of a thread: raw[i].v[j] at t0 + 1024 i + 4 tid + j; -inf behind the row's end.
 template <int E>
-__device__ __forceinline__ void draw_load(const float* row, int t0, int V, int tid, float x[4 * E]) {
+__device__ __forceinline__ void draw_fetch(const float* row, int t0, int V, int tid, Four raw[E]) {
+  const uint32_t at = (uint32_t)t0 + 4u * tid;
   if (t0 + 1024 * E <= V) {                              // whole work group
-    Four f[E];
 #pragma unroll
-    for (int i = 0; i < E; ++i) f[i] = *(const Four*)(row + t0 + 1024 * i + 4 * tid);
-#pragma unroll
-    for (int i = 0; i < 4 * E; ++i) x[i] = draw_clean(f[i / 4].v[i % 4]);
+    for (int i = 0; i < E; ++i) raw[i] = *(const Four*)(row + (at + 1024u * i));
     return;
   }
 #pragma unroll
-  for (int i = 0; i < 4 * E; ++i) {
-    const int t = t0 + 1024 * (i / 4) + 4 * tid + i % 4;
-    const float v = row[t < V ? t : V - 1];
-    x[i] = t < V ? draw_clean(v) : -INFINITY;
+  for (int i = 0; i < E; ++i) {
+    const uint32_t t = at + 1024u * i;
+    raw[i] = Four{{-INFINITY, -INFINITY, -INFINITY, -INFINITY}};
+    if (t + 4u <= (uint32_t)V) {
+      raw[i] = *(const Four*)(row + t);
+    } else if (t < (uint32_t)V) {
+      raw[i].v[0] = row[t];
+      if (t + 1u < (uint32_t)V) raw[i].v[1] = row[t + 1u];
+      if (t + 2u < (uint32_t)V) raw[i].v[2] = row[t + 2u];
+    }
   }
 }
 
@@ -320,21 +331,24 @@ __global__ void __launch_bounds__(256) k_draw_scan(DrawArgs a) {
   __shared__ double sums[4];
   __shared__ uint32_t count[COUNT ? kCopies * kBins : 1];
   __shared__ float tops[4];
-  __shared__ double roots[16];
+  __shared__ double roots[kRootCount];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int row = blockIdx.y, slice = blockIdx.x, V = a.vocab;
-  if (tid < 16) roots[tid] = kRoots[tid];
+  if (tid < kRootCount) roots[tid] = kRoots[tid];
   const Settings s = draw_settings(a, row);
-  float x[4 * E];
-  draw_load<E>(a.logits + (int64_t)row * V, slice * 1024 * E, V, tid, x);
+  Four raw[E];
+  draw_fetch<E>(a.logits + (int64_t)row * V, slice * 1024 * E, V, tid, raw);
   if (LIMITS)
     for (int i = tid; i < kCopies * kBins; i += 256) {
       mass[i] = 0;
       if (COUNT) count[i] = 0;
     }
-  float top = -INFINITY;
+  float x[4 * E], top = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < 4 * E; ++i) top = fmaxf(top, x[i]);
+  for (int i = 0; i < 4 * E; ++i) {
+    x[i] = draw_clean(raw[i / 4].v[i % 4]);
+    top = fmaxf(top, x[i]);
+  }
   top = wave_top(top);
   if (lane == 0) tops[wave] = top;
   __syncthreads();
@@ -360,7 +374,8 @@ __global__ void __launch_bounds__(256) k_draw_scan(DrawArgs a) {
     a.stat[at] = SliceStat{top, best, top > -INFINITY ? (sums[0] + sums[1]) + (sums[2] + sums[3]) : 0.0};
     if (LIMITS && slice == 0) a.listed[row] = 0;
   }
-  if (LIMITS && tid < kBins) {
+  static_assert(kBins == 256, "a bin a thread");
+  if (LIMITS) {
     unsigned long long m = 0;
     uint32_t c = 0;
 #pragma unroll
@@ -374,26 +389,22 @@ __global__ void __launch_bounds__(256) k_draw_scan(DrawArgs a) {
 }
 
 template <int E, bool COUNT>
-__global__ void __launch_bounds__(256) k_draw_list(DrawArgs a) {
-  __shared__ double mass[kBins], half_mass[kBins], factor[64];
-  __shared__ int count[kBins], half_count[kBins], offset[64];
-  __shared__ float tops[4];
+__global__ void __launch_bounds__(256, 4) k_draw_list(DrawArgs a) {
+  __shared__ double mass[kBins], factor[64];
+  __shared__ int count[kBins], offset[64];
+  __shared__ float tops[4], edges[4];
   __shared__ unsigned long long parts[4];
   __shared__ int counts[4], base;
   __shared__ RowPlan plan;
-  __shared__ double roots[16];
+  __shared__ double roots[kRootCount];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int row = blockIdx.y, slice = blockIdx.x, V = a.vocab;
-  if (tid < 16) roots[tid] = kRoots[tid];
+  if (tid < kRootCount) roots[tid] = kRoots[tid];
   const Settings s = draw_settings(a, row);
   const SliceStat* stat = a.stat + (int64_t)row * a.slices;
   const SliceStat own = stat[slice];
-  const int j = tid & (kBins - 1), half = tid >> 7;
+  const int j = tid;                                     // this thread's bin
   const unsigned long long own_mass = a.mass[((int64_t)row * a.slices + slice) * kBins + j];
-  // the logits are on their way while the borders are found
-  float x[4 * E];
-  const int t0 = slice * 1024 * E;
-  draw_load<E>(a.logits + (int64_t)row * V, t0, V, tid, x);
   float top = -INFINITY;
   for (int i = tid; i < a.slices; i += 256) top = fmaxf(top, stat[i].top);
   top = wave_top(top);
@@ -401,10 +412,10 @@ __global__ void __launch_bounds__(256) k_draw_list(DrawArgs a) {
   __syncthreads();
   top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
   const int bin = draw_bin(top, s.grid);
-  // The row's bins, 64 slices at a time: thread j of either half of the work group takes what falls on bin j of every other
-  // slice; the last bin has the rest
+  // The row's bins, 64 slices at a time: thread j takes what falls on bin j; the last bin has the rest
   double m = 0.0, total = 0.0;
   int c = 0;
+  Four raw[E];
   for (int s0 = 0; s0 < a.slices; s0 += 64) {
     const int n = min(64, a.slices - s0);
     __syncthreads();
@@ -419,52 +430,69 @@ __global__ void __launch_bounds__(256) k_draw_list(DrawArgs a) {
     __syncthreads();
     const unsigned long long* at = a.mass + ((int64_t)row * a.slices + s0) * kBins;
     const uint32_t* ct = a.count + ((int64_t)row * a.slices + s0) * kBins;
-#pragma unroll 4
-    for (int i = half; i < n; i += 2) {
-      const int from = j - offset[i], where = i * kBins + max(from, 0);
-      const unsigned long long v = at[where];
-      const int cv = COUNT ? (int)ct[where] : 0;
-      if (from >= 0 && j < kBins - 1) {
-        m += factor[i] * (double)v;
-        c += cv;
+    unsigned long long v[8];
+    uint32_t cv[8];
+    for (int i0 = 0; i0 < n; i0 += 8) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int i = min(i0 + k, n - 1), where = i * kBins + max(j - offset[i], 0);
+        v[k] = at[where];
+        cv[k] = COUNT ? ct[where] : 0u;
       }
+      if (s0 == 0 && i0 == 0) {
+        // the slice's logits are on their way while the borders are found (behind the bins: loads return in order)
+        __builtin_amdgcn_sched_barrier(0);
+        draw_fetch<E>(a.logits + (int64_t)row * V, slice * 1024 * E, V, tid, raw);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (i0 + k < n && j >= offset[i0 + k] && j < kBins - 1) {
+          m += factor[i0 + k] * (double)v[k];
+          if (COUNT) c += (int)cv[k];
+        }
     }
   }
-  if (half) {
-    half_mass[j] = m;
-    if (COUNT) half_count[j] = c;
-  }
+  mass[j] = m;
+  if (COUNT) count[j] = c;
   __syncthreads();
-  if (!half) {
-    mass[j] = m + half_mass[j];
-    if (COUNT) count[j] = c + half_count[j];
-  }
-  __syncthreads();
-  if (wave == 0) {                                       // sums up to each bin, and where the borders lie
-    const double m0 = mass[2 * lane], m1 = mass[2 * lane + 1];
-    const double sum = wave_scan(m0 + m1), me = lane == 63 ? fmax(total, sum) : sum, mo = sum - m1;
-    mass[2 * lane] = mo;
-    mass[2 * lane + 1] = me;
-    int ce = 0, co = 0;
+  if (wave == 0) {                                       // sums up to each bin, four a lane, and where the borders lie
+    double b[4], upto[4];
+    int d[4] = {0, 0, 0, 0}, cs[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      b[k] = mass[4 * lane + k];
+      if (COUNT) d[k] = count[4 * lane + k];
+    }
+    const double sum = wave_scan((b[0] + b[1]) + (b[2] + b[3]));
+    upto[0] = sum - ((b[0] + b[1]) + (b[2] + b[3])) + b[0];
+#pragma unroll
+    for (int k = 1; k < 4; ++k) upto[k] = upto[k - 1] + b[k];
+    if (lane == 63) upto[3] = fmax(total, upto[3]);
     if (COUNT) {
-      const int c0 = count[2 * lane], c1 = count[2 * lane + 1];
-      ce = wave_scan(c0 + c1);
-      co = ce - c1;
-      count[2 * lane] = co;
-      count[2 * lane + 1] = ce;
+      cs[0] = wave_scan(d[0] + d[1] + d[2] + d[3]) - d[1] - d[2] - d[3];
+#pragma unroll
+      for (int k = 1; k < 4; ++k) cs[k] = cs[k - 1] + d[k];
     }
-    total = last_lane(me);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      mass[4 * lane + k] = upto[k];
+      if (COUNT) count[4 * lane + k] = cs[k];
+    }
+    total = last_lane(upto[3]);
     // the first bin up to which the sum is not below x (the last one if there is none)
-    auto first_at = [&](bool even, bool odd) {
-      const unsigned long long e = __ballot(even), o = __ballot(odd);
-      const int be = e ? 2 * (__ffsll((long long)e) - 1) : kBins - 1, bo = o ? 2 * (__ffsll((long long)o) - 1) + 1 : kBins - 1;
-      return min(be, bo);
+    auto first_at = [&](bool b0, bool b1, bool b2, bool b3) {
+      const unsigned long long who = __ballot(b0 || b1 || b2 || b3);
+      if (!who) return kBins - 1;
+      const int at = __ffsll((long long)who) - 1, mine = b0 ? 0 : b1 ? 1 : b2 ? 2 : 3;
+      return 4 * at + __builtin_amdgcn_readlane(mine, at);
     };
-    RowPlan p{top, -INFINITY, bin, kBins, -1, kBins, 0, 0.0, 0.0, total};
+    auto first_sum = [&](double x) { return first_at(upto[0] >= x, upto[1] >= x, upto[2] >= x, upto[3] >= x); };
+    RowPlan p{top, -INFINITY, 0.0f, bin, kBins, -1, kBins, 0, 0.0, 0.0, total};
     if (top > -INFINITY) {
       int b1 = kBins;                                    // where top_k's or min_p's border lies
       if (s.k == 1) b1 = 0;
-      else if (COUNT && s.k > 0) b1 = first_at(co >= s.k, ce >= s.k);
+      else if (COUNT && s.k > 0) b1 = first_at(cs[0] >= s.k, cs[1] >= s.k, cs[2] >= s.k, cs[3] >= s.k);
       if (s.min_p > 0.0f && s.min_p <= 1.0f) {
         // the least logit with (x - top) / T >= ln min_p: an estimate, then its neighbours
         const double z = log((double)s.min_p);
@@ -489,39 +517,65 @@ __global__ void __launch_bounds__(256) k_draw_list(DrawArgs a) {
         // the weight of what top_k and min_p keep lies between that of the bins before theirs and with it
         const double least = b1 == kBins ? total : p.mass1, most = b1 == kBins ? total : mass[b1];
         const double goal0 = (double)s.p * least, goal1 = (double)s.p * most;
-        p.first = min(first_at(mo >= goal0, me >= goal0), b1);
-        p.last = min(first_at(mo >= goal1, me >= goal1), b1);
+        p.first = min(first_sum(goal0), b1);
+        p.last = min(first_sum(goal1), b1);
       }
       if (p.first > 0) p.mass0 = mass[p.first - 1];
     }
-    if (lane == 0) {
-      plan = p;
-      if (slice == 0) a.plan[row] = p;
-    }
+    if (lane == 0) plan = p;
   }
   __syncthreads();
   const int first = plan.first, last = plan.last, limit = plan.limit;
+  // The bins' borders as logits, one a wave: the least logit of the bins before first, of those up to last, before
+  // limit, up to limit (NaN: there is none).  A search among the keys, 64 parts at a time.
+  {
+    const int down = wave == 0 ? first - 1 : wave == 1 ? last : wave == 2 ? limit - 1 : limit;
+    uint32_t lo = ordered(-FLT_MAX), span = ordered(FLT_MAX) - lo;     // the border lies from lo to lo + span
+    if (down < 0) {
+      edges[wave] = __uint_as_float(0x7FC00000u);        // no logit is as great
+    } else if (down >= kBins - 1) {
+      edges[wave] = -FLT_MAX;
+    } else {
+      const int least = bin - down;
+      while (span > 0) {
+        const uint32_t step = span / 64 + 1, k = lo + min((uint32_t)(lane + 1) * step - 1, span);
+        const unsigned long long in = __ballot(draw_bin(unordered(k), s.grid) >= least);
+        const int at = __ffsll((long long)in) - 1;       // the row's largest logit is in: there is one
+        lo += (uint32_t)at * step;
+        span = min(step - 1, span - (uint32_t)at * step);
+      }
+      edges[wave] = unordered(lo);
+    }
+  }
+  __syncthreads();
+  if (tid == 0 && slice == 0) {
+    RowPlan p = plan;
+    p.x_first = edges[0];
+    a.plan[row] = p;
+  }
   // this slice's weights in the bins before first
   if (first < kBins) {
-    unsigned long long w = !half && bin - own.bin + j < first && own.top > -INFINITY ? own_mass : 0;
+    unsigned long long w = bin - own.bin + j < first && own.top > -INFINITY ? own_mass : 0;
     w = wave_sum(w);
     if (lane == 0) parts[wave] = w;
     __syncthreads();
-    if (tid == 0) a.sure[(int64_t)row * a.slices + slice] = (double)(parts[0] + parts[1]) * (1.0 / kSliceUnit);
+    if (tid == 0) a.sure[(int64_t)row * a.slices + slice] = (double)((parts[0] + parts[1]) + (parts[2] + parts[3])) * (1.0 / kSliceUnit);
   } else if (tid == 0) {
     a.sure[(int64_t)row * a.slices + slice] = own.sum;
   }
   if (first > last) return;
   if (!(own.top > -INFINITY) || min(bin - own.bin, kBins - 1) > (limit < kBins ? limit : last)) return;
   uint32_t mine = 0;                                     // which of them are listed
-  // as ranges of bins from below; the last bin reaches down to -inf (not included)
-  const int hi1 = bin - first, lo1 = last == kBins - 1 ? INT32_MIN : bin - last;
-  const int hi2 = limit > last && limit < kBins ? bin - limit : INT32_MIN, lo2 = limit == kBins - 1 ? INT32_MIN : bin - limit;
+  const float hi1 = edges[0], lo1 = edges[1], hi2 = edges[2], lo2 = edges[3];
+  const bool two = limit > last && limit < kBins;
+  auto within = [](float v, float lo, float hi) __attribute__((always_inline)) { return v >= lo && !(v >= hi); };
 #pragma unroll
-  for (int i = 0; i < 4 * E; ++i) {
-    const int at = draw_bin(x[i], s.grid);
-    if (((at >= lo1 && at <= hi1) || (at >= lo2 && at <= hi2)) && x[i] > -INFINITY) mine |= 1u << i;
-  }
+  for (int i = 0; i < 4 * E; ++i)
+    if (within(raw[i / 4].v[i % 4], lo1, hi1)) mine |= 1u << i;
+  if (two)
+#pragma unroll
+    for (int i = 0; i < 4 * E; ++i)
+      if (within(raw[i / 4].v[i % 4], lo2, hi2)) mine |= 1u << i;
   const int n = __popc(mine), upto = wave_scan(n);
   if (lane == 63) counts[wave] = upto;
   __syncthreads();
@@ -536,14 +590,14 @@ __global__ void __launch_bounds__(256) k_draw_list(DrawArgs a) {
 #pragma unroll
   for (int i = 0; i < 4 * E; ++i)
     if (mine >> i & 1u) {
-      if (at < kList) list[at] = draw_key(x[i], t0 + 1024 * (i / 4) + 4 * tid + i % 4);
+      if (at < kList) list[at] = draw_key(draw_clean(raw[i / 4].v[i % 4]), slice * 1024 * E + 1024 * (i / 4) + 4 * tid + i % 4);
       ++at;
     }
 }
 
 // Sums over the work group's threads up to and including this one's, in the order of threads.  parts must not be in
 // use; it is free again after the next barrier.
-template <typename T>
+template <int NW, typename T>
 __device__ __forceinline__ T group_scan(T v, T* parts, int tid, T& total) {
   const int lane = tid & 63, wave = tid >> 6;
   v = wave_scan(v);
@@ -552,7 +606,7 @@ __device__ __forceinline__ T group_scan(T v, T* parts, int tid, T& total) {
   T before = 0;
   total = 0;
 #pragma unroll
-  for (int w = 0; w < kPickThreads / 64; ++w) {
+  for (int w = 0; w < NW; ++w) {
     if (w < wave) before += parts[w];
     total += parts[w];
   }
@@ -561,9 +615,12 @@ __device__ __forceinline__ T group_scan(T v, T* parts, int tid, T& total) {
 
 constexpr int kMaxSlices = 2048;
 
+// More threads where slices are long and lists are (128 x 128256: 27 -> 20 us; one row of 32003 12.5 us, 9.6 with 512).
+constexpr int pick_threads(bool limits, int E) { return limits && E > 2 ? 1024 : 512; }
+
 template <bool LIMITS, int E>
-__global__ void __launch_bounds__(kPickThreads) k_draw_pick(DrawArgs a, int unit_bits) {
-  constexpr int kParts = 1024, NT = kPickThreads, NW = NT / 64, SLICE = 1024 * E, EACH = SLICE / NT;
+__global__ void __launch_bounds__(pick_threads(LIMITS, E)) k_draw_pick(DrawArgs a, int unit_bits) {
+  constexpr int NT = pick_threads(LIMITS, E), NW = NT / 64, kParts = NT, SLICE = 1024 * E, EACH = SLICE / NT;
   __shared__ unsigned long long keys[LIMITS ? kList : 1], pm[LIMITS ? kParts : 1], add[LIMITS ? kMaxSlices : 1];
   __shared__ uint32_t pc[LIMITS ? kParts : 1];
   __shared__ unsigned long long ull[3][NW];
@@ -572,10 +629,10 @@ __global__ void __launch_bounds__(kPickThreads) k_draw_pick(DrawArgs a, int unit
   __shared__ float tops[NW];
   __shared__ int part, part_count, before_count, slice_at, hit, last_kept;
   __shared__ unsigned long long before_mass;
-  __shared__ double before_slice, all_kept;
-  __shared__ double roots[16];
+  __shared__ double before_slice, all_kept, log_kept;
+  __shared__ double roots[kRootCount];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = blockIdx.x, V = a.vocab;
-  if (tid < 16) roots[tid] = kRoots[tid];
+  if (tid < kRootCount) roots[tid] = kRoots[tid];
   const float* x = a.logits + (int64_t)row * V;
   const SliceStat* stat = a.stat + (int64_t)row * a.slices;
   const SliceStat first_stat = stat[lane < a.slices ? lane : 0];       // on their way
@@ -616,7 +673,7 @@ __global__ void __launch_bounds__(kPickThreads) k_draw_pick(DrawArgs a, int unit
     return draw_fix(draw_weight(key_logit(k), p.top, s.scale, roots), unit);
   };
 
-  unsigned long long border = 0;                         // listed keys from here on are kept
+  unsigned long long border = draw_key(-FLT_MAX, INT32_MAX);           // keys from here on are kept
   if constexpr (LIMITS) {
     for (int i = tid; i < a.slices; i += NT) add[i] = 0;
     if (p.first <= p.last) {
@@ -632,7 +689,7 @@ __global__ void __launch_bounds__(kPickThreads) k_draw_pick(DrawArgs a, int unit
       };
       // the least key of bins first .. last and the greatest of bin limit; the greatest of all
       unsigned long long low = ~0ull, most = 0, high = 0;
-#pragma unroll 1
+#pragma unroll 4
       for (int i = tid; i < n; i += NT) {
         const unsigned long long k = held ? list[i] : from_row(i);
         if (held) keys[i] = k;
@@ -694,15 +751,15 @@ __global__ void __launch_bounds__(kPickThreads) k_draw_pick(DrawArgs a, int unit
           least = lo;
         }
         lo = max(lo, low);
-        if (lo > hi) continue;                           // there are none
+        if (lo > hi) {                                   // there are none: what lies before
+          least = counting ? least : (unsigned long long)ordered(p.x_first) << 32;
+          continue;
+        }
         while (lo < hi) {
-          const int shift = max(0, 64 - __clzll((long long)(hi - lo)) - 10);
+          const int shift = max(0, 64 - __clzll((long long)(hi - lo)) - (NT == 1024 ? 10 : 9));
           __syncthreads();
-#pragma unroll
-          for (int i = 0; i < kParts / NT; ++i) {
-            pm[i * NT + tid] = 0;
-            pc[i * NT + tid] = 0;
-          }
+          pm[tid] = 0;
+          pc[tid] = 0;
           if (tid == 0) part = INT32_MAX;
           __syncthreads();
 #pragma unroll 1
@@ -714,36 +771,31 @@ __global__ void __launch_bounds__(kPickThreads) k_draw_pick(DrawArgs a, int unit
             if (!counting) atomicAdd(&pm[at], fixed(k));
           }
           __syncthreads();
-          const unsigned long long m0 = pm[2 * tid], m1 = pm[2 * tid + 1];
-          const int c0 = (int)pc[2 * tid], c1 = (int)pc[2 * tid + 1];
-          const unsigned long long ms = wave_scan(m0 + m1);
-          const int cs = wave_scan(c0 + c1);
+          const unsigned long long m0 = pm[tid], ms = wave_scan(m0);
+          const int c0 = (int)pc[tid], cs = wave_scan(c0);
           if (lane == 63) {
             ull[0][wave] = ms;
             ints[wave] = cs;
           }
           __syncthreads();
-          unsigned long long me = ms - m1;
-          int ce = cs - c1;
+          unsigned long long me = ms;
+          int ce = cs;
 #pragma unroll
           for (int w = 0; w < NW; ++w)
             if (w < wave) {
               me += ull[0][w];
               ce += ints[w];
             }
-          auto there = [&](int c, unsigned long long w) __attribute__((always_inline)) {
-            return counting ? have + c >= s.k : (double)(sum + w) >= goal;
-          };
-          const bool even = c0 && there(ce, me), odd = c1 && there(ce + c1, me + m1);
-          const unsigned long long who = __ballot(even || odd);
-          if (who && lane == __ffsll((long long)who) - 1) atomicMin(&part, 2 * tid + (even ? 0 : 1));
+          const bool there = c0 && (counting ? have + ce >= s.k : (double)(sum + me) >= goal);
+          const unsigned long long who = __ballot(there);
+          if (who && lane == __ffsll((long long)who) - 1) atomicMin(&part, tid);
           __syncthreads();
           const int at = part;
           if (at == INT32_MAX) break;                    // not reached: all of them
-          if (at / 2 == tid) {                           // what lies before that part
-            before_count = at % 2 ? ce : ce - c0;
-            before_mass = at % 2 ? me : me - m0;
-            part_count = at % 2 ? c1 : c0;
+          if (at == tid) {                               // what lies before that part
+            before_count = ce - c0;
+            before_mass = me - m0;
+            part_count = c0;
           }
           __syncthreads();
           have += before_count;
@@ -756,23 +808,21 @@ __global__ void __launch_bounds__(kPickThreads) k_draw_pick(DrawArgs a, int unit
         }
         least = lo;
       }
-      border = least;
+      border = max(least, border);
       // the listed tokens' share of their slices
       __syncthreads();
 #pragma unroll 1
       for (int i = tid; i < n; i += NT) {
         const unsigned long long k = held ? keys[i] : from_row(i);
-        if (k && k >= border && bin_of(key_logit(k)) <= p.last) atomicAdd(&add[key_token(k) / SLICE], fixed(k));
+        if (k && k >= border) atomicAdd(&add[key_token(k) / SLICE], fixed(k));
       }
     }
     __syncthreads();
   }
-  auto kept = [&](float v, int t) __attribute__((always_inline)) {
-    if (!LIMITS) return s.best ? v == p.top : v > -INFINITY;
-    if (!(v > -INFINITY)) return false;
-    const int b = bin_of(v);
-    return b < p.first || (b <= p.last && draw_key(v, t) >= border);
-  };
+  // kept: logits above xb, and those equal to it up to token tb
+  const float xb = LIMITS ? key_logit(border) : s.best ? p.top : -FLT_MAX;
+  const uint32_t tb = LIMITS ? (uint32_t)key_token(border) : UINT32_MAX;
+  auto kept = [&](float v, int t) __attribute__((always_inline)) { return v > xb || (v == xb && (uint32_t)t <= tb); };
   // The slices' kept weights, summed up in their order by one wave; the first whose sum passes u times the whole (the
   // last one with any where rounding leaves none)
   if (wave == 0) {
@@ -822,11 +872,12 @@ __global__ void __launch_bounds__(kPickThreads) k_draw_pick(DrawArgs a, int unit
   double w[EACH], mine = 0.0;
   int last = -1;
   if (from + SLICE <= V) {
-    Four f[EACH / 4];
+    constexpr int VW = EACH < 4 ? EACH : 4;
+    Floats<VW> f[EACH / VW];
 #pragma unroll
-    for (int j = 0; j < EACH / 4; ++j) f[j] = *(const Four*)(x + t0 + 4 * j);
+    for (int j = 0; j < EACH / VW; ++j) f[j] = *(const Floats<VW>*)(x + t0 + VW * j);
 #pragma unroll
-    for (int j = 0; j < EACH; ++j) w[j] = f[j / 4].v[j % 4];
+    for (int j = 0; j < EACH; ++j) w[j] = f[j / VW].v[j % VW];
   } else {
 #pragma unroll
     for (int j = 0; j < EACH; ++j) {
@@ -841,23 +892,26 @@ __global__ void __launch_bounds__(kPickThreads) k_draw_pick(DrawArgs a, int unit
     mine += w[j];
     if (w[j] > 0.0) last = t0 + j;
   }
+  if (tid == NT - 1) log_kept = log(all_kept);           // beside the others' weights
   double total;
-  const double upto = group_scan(mine, dbl, tid, total);
+  const double upto = group_scan<NW>(mine, dbl, tid, total);
   double c = upto - mine;
-  int at = INT32_MAX;
+  int at = -1;
+  if (mine > 0.0 && upto > want) {
 #pragma unroll
-  for (int j = 0; j < EACH; ++j) {
-    c += w[j];
-    if (w[j] > 0.0 && c > want && at == INT32_MAX) at = t0 + j;
+    for (int j = 0; j < EACH; ++j) {
+      c += w[j];
+      if (w[j] > 0.0 && c > want && at < 0) at = t0 + j;
+    }
+    if (at >= 0) atomicMin(&hit, at);
   }
-  if (at != INT32_MAX) atomicMin(&hit, at);
-  if (last >= 0) atomicMax(&last_kept, last);
+  if (total <= want && last >= 0) atomicMax(&last_kept, last);         // rounding leaves none: the last one
   __syncthreads();
-  if (tid == 0) {
-    const int t = hit != INT32_MAX ? hit : max(last_kept, from);
-    a.tokens[row] = t;
-    if (a.logprobs)
-      a.logprobs[row] = s.best ? 0.0f : (float)(((double)draw_clean(x[t]) - (double)p.top) * s.inv_t - log(all_kept));
+  if (hit == INT32_MAX && last >= 0 && last == last_kept) at = hit = last;
+  if (tid == 0 && hit == INT32_MAX && last_kept < 0) a.tokens[row] = from;      // cannot be: the slice has weight
+  if (at >= 0 && at == hit) {
+    a.tokens[row] = at;
+    if (a.logprobs) a.logprobs[row] = s.best ? 0.0f : (float)(((double)draw_clean(x[at]) - (double)p.top) * s.inv_t - log_kept);
   }
 }
 
@@ -963,11 +1017,11 @@ termezo_status termezo_sample(termezo_ctx* c, const float* logits, const float* 
     a.tokens = tokens + r0;
     a.logprobs = from(logprobs);
     const dim3 grid((unsigned)slices, (unsigned)n);
-    const dim3 rows_grid((unsigned)n), wide(kPickThreads);
+    const dim3 rows_grid((unsigned)n);
 #define TMZ_DRAW(E)                                                                                          \
   if (!limits) {                                                                                             \
     hipLaunchKernelGGL((k_draw_scan<E, false, false>), grid, dim3(256), 0, c->stream, a);                    \
-    hipLaunchKernelGGL((k_draw_pick<false, E>), rows_grid, wide, 0, c->stream, a, unit);                     \
+    hipLaunchKernelGGL((k_draw_pick<false, E>), rows_grid, dim3(pick_threads(false, E)), 0, c->stream, a, unit);                     \
   } else {                                                                                                   \
     if (top_k) {                                                                                             \
       hipLaunchKernelGGL((k_draw_scan<E, true, true>), grid, dim3(256), 0, c->stream, a);                    \
@@ -976,7 +1030,7 @@ termezo_status termezo_sample(termezo_ctx* c, const float* logits, const float* 
       hipLaunchKernelGGL((k_draw_scan<E, true, false>), grid, dim3(256), 0, c->stream, a);                   \
       hipLaunchKernelGGL((k_draw_list<E, false>), grid, dim3(256), 0, c->stream, a);                         \
     }                                                                                                        \
-    hipLaunchKernelGGL((k_draw_pick<true, E>), rows_grid, wide, 0, c->stream, a, unit);                      \
+    hipLaunchKernelGGL((k_draw_pick<true, E>), rows_grid, dim3(pick_threads(true, E)), 0, c->stream, a, unit);                      \
   }
     if (large) {
       TMZ_DRAW(8)
