@@ -563,7 +563,7 @@ termezo_status termezo_model_decode(termezo_model* model, termezo_kvcache* cache
  * that would have to allocate is refused (STATE), and graphs stay valid when it grows later. */
 
 /* Rows of w [N][K] (F32 or BF16) in 8 bits: a = max(max |w|, 1e-30), codes[n][k] =
- * rne(w * (127 / a)) and steps[n] = a / 127 (fp32, each operation rounded); a row with a value
+ * rne(w * s) with s = 127 * (1 / a), steps[n] = a / 127 (fp32, each operation rounded); a row with a value
  * that is not finite has codes 0 and the step NaN.  codes int8 [N][K] (16-byte aligned), steps
  * fp32 [N].  No output may overlap w.  Errors: INVALID_ARG (N 1 .. 2^24, K 1 .. 2^17 and a
  * multiple of 16, dtype, null or misaligned (16 bytes; steps 4) pointers). */
@@ -571,7 +571,7 @@ termezo_status termezo_quantize_rows(termezo_ctx* ctx, const void* w, termezo_dt
                                      int64_t K, int8_t* codes, float* steps);
 
 /* Product of M tokens with N rows of 8-bit weights: every row x of the input is taken in 8 bits
- * (a = max(max |x|, 1e-5), q[k] = rne(x[k] * (127 / a)), as termezo_bitlinear_forward does),
+ * (a = max(max |x|, 1e-5) as in termezo_bitlinear_forward, q[k] = rne(x[k] * s), s = 127 * (1 / a)),
  * out[m][n] = (sum_k q[k] codes[n][k]) * ((a / 127) * steps[n]), the sum exact in int32, each
  * fp32 operation rounded, then to out's type.  x [M][K] in xdt, out [M][N] in ydt (F32 or BF16
  * each), codes int8 [N][K], -128 .. 127.  An input row with a value that is not finite has NaN

@@ -15,7 +15,7 @@ def quantise(x: np.ndarray, floor: float):
     if not np.isfinite(x).all():
         return np.zeros(x.shape, np.int64), F(np.nan)
     a = max(F(np.abs(x).max()), F(floor))
-    return np.rint(x * (F(127.0) / a)).astype(np.int64), a / F(127.0)
+    return np.rint(x * (F(127.0) * (F(1.0) / a))).astype(np.int64), a / F(127.0)
 
 
 def linear(x: np.ndarray, codes: np.ndarray, steps: np.ndarray) -> np.ndarray:

@@ -25,7 +25,7 @@ __device__ __forceinline__ int64_t token_at(int64_t m, int64_t k, int64_t pitch)
 }
 
 // ---------------------------------------------------------------------------
-// Rows in 8 bits: a = max(max |x|, floor), q = rne(x (127 / a)), step a / 127.  One wave a row, 8 values a
+// Rows in 8 bits: a = max(max |x|, floor), q = rne(x s) with s = 127 (1 / a), step a / 127.  One wave a row, 8 values a
 // lane and load; rows of up to 512 C values stay in registers, longer ones are read twice.  The largest
 // magnitude is taken on the bit patterns, where NaN and infinities are above all numbers: such a row has
 // codes 0 and the step NaN.  Bound by the bytes of x.
@@ -106,7 +106,7 @@ __device__ __forceinline__ float row_codes(const T* row, int64_t K, int64_t end,
   }
   const bool fine = a < 0x7F800000u;
   const float top = fmaxf(__uint_as_float(a), floor);
-  const float s = fine ? __fdiv_rn(127.0f, top) : 0.0f;
+  const float s = fine ? 127.0f * __fdiv_rn(1.0f, top) : 0.0f;
   const uint2 none = make_uint2(0u, 0u);
   if (held) {
 #pragma unroll

@@ -16,6 +16,9 @@ struct __attribute__((packed, aligned(4))) Floats {      // rows of any length b
   float v[N];
 };
 typedef Floats<4> Four;
+struct __attribute__((packed, aligned(4))) Ids {
+  int32_t v[4];
+};
 
 // ---------------------------------------------------------------------------
 // Rules on the logits, a work group for a slice of a row.  The history's tokens that fall into the slice
@@ -31,8 +34,6 @@ struct RuleArgs {
   int32_t* err;
 };
 
-constexpr int kRuleSlice = 4096;
-
 // Line of a table that row takes: -1 none.
 __device__ __forceinline__ int rule_line(const int32_t* index, int lines, int row, bool& bad) {
   const int i = index ? index[row] : (lines == 1 ? 0 : row);
@@ -41,51 +42,89 @@ __device__ __forceinline__ int rule_line(const int32_t* index, int lines, int ro
   return -1;
 }
 
+// A slice of a row, 4 * E values of a thread: raw[i].v[j] at t0 + 1024 i + 4 tid + j; `none` behind the row's end.
+template <int E>
+__device__ __forceinline__ void slice_fetch(const float* row, int t0, int V, int tid, float none, Four raw[E]) {
+  const uint32_t at = (uint32_t)t0 + 4u * tid;
+  if (t0 + 1024 * E <= V) {                              // whole work group
+#pragma unroll
+    for (int i = 0; i < E; ++i) raw[i] = *(const Four*)(row + (at + 1024u * i));
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const uint32_t t = at + 1024u * i;
+    raw[i] = Four{{none, none, none, none}};
+    if (t + 4u <= (uint32_t)V) {
+      raw[i] = *(const Four*)(row + t);
+    } else if (t < (uint32_t)V) {
+      raw[i].v[0] = row[t];
+      if (t + 1u < (uint32_t)V) raw[i].v[1] = row[t + 1u];
+      if (t + 2u < (uint32_t)V) raw[i].v[2] = row[t + 2u];
+    }
+  }
+}
+
+// SLICE logits a work group: 1024 where that gives a compute unit four work groups at most (latency counts); else 8192
+// with a history, which every slice of a row goes through (64 x 128256, 4000 tokens: 16.6 us, 18.5 with 4096, 23.5 with
+// 16384), 4096 without (192 x 32000 with bias and mask: 9.8 us, 5.1 TB/s; 10.9 with 8192).  With the logits on
+// their way while the history is counted the registers leave too few waves: 16.6 -> 19 us.
+template <int SLICE, bool HIST>
 __global__ void __launch_bounds__(256) k_adjust(RuleArgs a) {
-  __shared__ uint32_t count[kRuleSlice];
+  __shared__ uint32_t count[HIST ? SLICE : 1];
   const int tid = threadIdx.x, row = blockIdx.y, V = a.vocab;
-  const int t0 = blockIdx.x * kRuleSlice, n = min(kRuleSlice, V - t0);
+  const int t0 = blockIdx.x * SLICE, n = min(SLICE, V - t0);
   bool bad = false;
-  const bool hist = a.r.history != nullptr;
-  float rep = 1.0f, freq = 0.0f, pres = 0.0f;
-  if (hist) {
+  int64_t len = a.r.hist_len, from = 0;
+  if (HIST && a.r.lengths) len = a.r.lengths[row];
+  if (HIST && a.r.starts) from = a.r.starts[row];
+  const float rep = HIST && a.r.repetition ? a.r.repetition[row] : 1.0f;
+  const float freq = HIST && a.r.frequency ? a.r.frequency[row] : 0.0f;
+  const float pres = HIST && a.r.presence ? a.r.presence[row] : 0.0f;
+  const int bl = a.r.bias ? rule_line(a.r.bias_index, a.r.n_bias, row, bad) : -1;
+  const int ml = a.r.mask ? rule_line(a.r.mask_index, a.r.n_masks, row, bad) : -1;
+  if (HIST)
     for (int i = tid; i < n; i += 256) count[i] = 0u;
-    int64_t len = a.r.hist_len, from = 0;
-    if (a.r.lengths) {
-      const int l = a.r.lengths[row];
-      if (l < 0 || l > len) bad = true;
-      len = bad ? 0 : l;
+  if (HIST) {
+    if (len < 0 || len > a.r.hist_len || from < 0 || from > len) {
+      bad = true;
+      len = 0;
     }
-    if (a.r.starts) {
-      from = a.r.starts[row];
-      if (from < 0 || (from > len && !bad)) {
-        bad = true;
-        len = 0;
-      }
-    }
-    if (a.r.repetition) rep = a.r.repetition[row];
-    if (a.r.frequency) freq = a.r.frequency[row];
-    if (a.r.presence) pres = a.r.presence[row];
     __syncthreads();
     const int32_t* h = a.r.history + row * a.r.hist_len;
-    for (int64_t i = tid; i < len; i += 256) {
-      const uint32_t at = (uint32_t)h[i] - (uint32_t)t0;   // ids outside the vocabulary are outside every slice
+    auto one = [&](int32_t id, int64_t i) __attribute__((always_inline)) {
+      const uint32_t at = (uint32_t)id - (uint32_t)t0;   // ids outside the vocabulary are outside every slice
       if (at < (uint32_t)n) {
         if (i >= from) atomicAdd(&count[at], 2u);
         else atomicOr(&count[at], 1u);
       }
+    };
+    for (int64_t i0 = 4 * tid; i0 < len; i0 += 4096) {
+      Ids id[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int64_t i = i0 + 1024 * k;
+        if (i + 4 <= len) {
+          id[k] = *(const Ids*)(h + i);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) id[k].v[j] = i + j < len ? h[i + j] : -1;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) one(id[k].v[j], i0 + 1024 * k + j);
     }
     __syncthreads();
   }
-  const int bl = a.r.bias ? rule_line(a.r.bias_index, a.r.n_bias, row, bad) : -1;
-  const int ml = a.r.mask ? rule_line(a.r.mask_index, a.r.n_masks, row, bad) : -1;
   if (bad && tid == 0 && blockIdx.x == 0) atomicOr(a.err, kErrRules);
   const float* x = a.logits + (int64_t)row * V;
   float* y = a.out + (int64_t)row * V;
   const float* bias = bl >= 0 ? a.r.bias + (int64_t)bl * V : nullptr;
   const uint32_t* mask = ml >= 0 ? a.r.mask + (int64_t)ml * ((V + 31) / 32) : nullptr;
   auto one = [&](float v, int i, float b, uint32_t allowed) __attribute__((always_inline)) {
-    if (hist) {
+    if (HIST) {
       const uint32_t c = count[i];
       if (c) {
         v = v > 0.0f ? __fdiv_rn(v, rep) : v * rep;
@@ -234,6 +273,21 @@ __device__ __forceinline__ double exp_of(double q, const double* roots) {     //
 __device__ __forceinline__ double draw_weight(float x, float top, double scale, const double* roots) {
   return exp_of(fmax(((double)x - (double)top) * scale, -32000.0), roots);
 }
+// ln x for x >= 2^-60: x = 2^e m with m from 0.7 to 1.42, ln m = 2 artanh((m - 1) / (m + 1)) by its series up to the 15th
+// power of a quotient below 0.18 (what is left out is below 2^-44).  Inline and short: the general function's code
+// had to come from memory for its one call.
+__device__ __forceinline__ double ln_of(double x) {
+  const int hi = __double2hiint(x), e = (hi - 0x3FE6A09E) >> 20;
+  const double m = __hiloint2double(hi - (e << 20), __double2loint(x)), t = (m - 1.0) / (m + 1.0), q = t * t;
+  double p = 1.0 / 15;
+  p = fma(p, q, 1.0 / 13);
+  p = fma(p, q, 1.0 / 11);
+  p = fma(p, q, 1.0 / 9);
+  p = fma(p, q, 1.0 / 7);
+  p = fma(p, q, 1.0 / 5);
+  p = fma(p, q, 1.0 / 3);
+  return fma((double)e, 0x1.62e42fefa39efp-1, 2.0 * fma(t * q, p, t));
+}
 // w in [0, 1] in units of 1 / unit (a power of two up to 2^51), rounded to nearest.
 __device__ __forceinline__ unsigned long long draw_fix(double w, double unit) {
   return (unsigned long long)__double_as_longlong(fma(w, unit, 0x1p52)) & ((1ull << 52) - 1);
@@ -301,29 +355,6 @@ __device__ __forceinline__ float wave_top(float v) {
   return last_lane(wave_fold(v, -INFINITY, [](float a, float b) __attribute__((always_inline)) { return fmaxf(a, b); }));
 }
 
-// A slice's logits, 4 * E of a thread: raw[i].v[j] at t0 + 1024 i + 4 tid + j; -inf behind the row's end.
-template <int E>
-__device__ __forceinline__ void draw_fetch(const float* row, int t0, int V, int tid, Four raw[E]) {
-  const uint32_t at = (uint32_t)t0 + 4u * tid;
-  if (t0 + 1024 * E <= V) {                              // whole work group
-#pragma unroll
-    for (int i = 0; i < E; ++i) raw[i] = *(const Four*)(row + (at + 1024u * i));
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < E; ++i) {
-    const uint32_t t = at + 1024u * i;
-    raw[i] = Four{{-INFINITY, -INFINITY, -INFINITY, -INFINITY}};
-    if (t + 4u <= (uint32_t)V) {
-      raw[i] = *(const Four*)(row + t);
-    } else if (t < (uint32_t)V) {
-      raw[i].v[0] = row[t];
-      if (t + 1u < (uint32_t)V) raw[i].v[1] = row[t + 1u];
-      if (t + 2u < (uint32_t)V) raw[i].v[2] = row[t + 2u];
-    }
-  }
-}
-
 // LIMITS: bins are wanted, COUNT: their tokens are counted too (top_k).
 template <int E, bool LIMITS, bool COUNT>
 __global__ void __launch_bounds__(256) k_draw_scan(DrawArgs a) {
@@ -337,7 +368,7 @@ __global__ void __launch_bounds__(256) k_draw_scan(DrawArgs a) {
   if (tid < kRootCount) roots[tid] = kRoots[tid];
   const Settings s = draw_settings(a, row);
   Four raw[E];
-  draw_fetch<E>(a.logits + (int64_t)row * V, slice * 1024 * E, V, tid, raw);
+  slice_fetch<E>(a.logits + (int64_t)row * V, slice * 1024 * E, V, tid, -INFINITY, raw);
   if (LIMITS)
     for (int i = tid; i < kCopies * kBins; i += 256) {
       mass[i] = 0;
@@ -442,7 +473,7 @@ __global__ void __launch_bounds__(256, 4) k_draw_list(DrawArgs a) {
       if (s0 == 0 && i0 == 0) {
         // the slice's logits are on their way while the borders are found (behind the bins: loads return in order)
         __builtin_amdgcn_sched_barrier(0);
-        draw_fetch<E>(a.logits + (int64_t)row * V, slice * 1024 * E, V, tid, raw);
+        slice_fetch<E>(a.logits + (int64_t)row * V, slice * 1024 * E, V, tid, -INFINITY, raw);
         __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
@@ -892,7 +923,7 @@ __global__ void __launch_bounds__(pick_threads(LIMITS, E)) k_draw_pick(DrawArgs 
     mine += w[j];
     if (w[j] > 0.0) last = t0 + j;
   }
-  if (tid == NT - 1) log_kept = log(all_kept);           // beside the others' weights
+  if (tid == NT - 1) log_kept = ln_of(all_kept);           // beside the others' weights
   double total;
   const double upto = group_scan<NW>(mine, dbl, tid, total);
   double c = upto - mine;
@@ -959,8 +990,18 @@ termezo_status termezo_adjust_logits(termezo_ctx* c, const float* logits, int32_
   if (scope.err != hipSuccess) return hip_status(c, scope.err, "adjust_logits");
   RuleArgs a{logits, out, vocab, rows, r, c->d_err};
   if (a.r.hist_len == 0) a.r.history = nullptr;
-  hipLaunchKernelGGL(k_adjust, dim3((unsigned)((vocab + kRuleSlice - 1) / kRuleSlice), (unsigned)rows), dim3(256), 0,
-                     c->stream, a);
+#define TMZ_ADJUST(SLICE, HIST)                                                                                    \
+  hipLaunchKernelGGL((k_adjust<SLICE, HIST>), dim3((unsigned)((vocab + SLICE - 1) / SLICE), (unsigned)rows), dim3(256), 0, \
+                     c->stream, a)
+  const bool few = (int64_t)rows * ((vocab + 1023) / 1024) <= 4 * (int64_t)c->n_cu;
+  if (a.r.history) {
+    if (few) TMZ_ADJUST(1024, true);
+    else TMZ_ADJUST(8192, true);
+  } else {
+    if (few) TMZ_ADJUST(1024, false);
+    else TMZ_ADJUST(4096, false);
+  }
+#undef TMZ_ADJUST
   return hip_status(c, hipGetLastError(), "adjust_logits");
 }
 

@@ -169,10 +169,10 @@ def _dtype_code(t) -> int:
 
 def _tensor(t, name, shape, dtype, device):
     """Device address of a contiguous tensor of that shape, type and device."""
-    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on {device}, not "
-                         f"{t.dtype} {list(t.shape)} on {t.device}")
-    return t.data_ptr()
+    if t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on {device}, not "
+                     f"{t.dtype} {list(t.shape)} on {t.device}")
 
 
 def _int(v, name, bits: int = 32) -> int:
@@ -465,8 +465,8 @@ class Context:
             _tensor(steps, "steps", (N,), torch.float32, self.device)), "quantize_rows")
 
     def linear_i8(self, x, codes, steps, out):
-        """out[m, n] = x[m] . (codes[n] * steps[n]) with every row of x taken in 8 bits, as
-        bitlinear_forward does: x [M, K] and out [M, N] in fp32 or bf16, codes int8 [N, K], steps
+        """out[m, n] = x[m] . (codes[n] * steps[n]) with every row of x taken in 8 bits by its largest
+        magnitude: x [M, K] and out [M, N] in fp32 or bf16, codes int8 [N, K], steps
         fp32 [N]."""
         import torch
         M, K = x.shape
@@ -489,25 +489,40 @@ class Context:
         row."""
         import torch
         R, V = logits.shape
-        f32, i32 = torch.float32, torch.int32
-        if history is None and any(t is not None for t in (lengths, starts, repetition, presence, frequency)):
+        f32, i32, dev = torch.float32, torch.int32, self.device
+        rules, row = LogitRules(), (R,)
+        if history is not None:
+            rules.hist_len = T = history.shape[-1]
+            rules.history = _tensor(history, "history", (R, T), i32, dev)
+            if lengths is not None:
+                rules.lengths = _tensor(lengths, "lengths", row, i32, dev)
+            if starts is not None:
+                rules.starts = _tensor(starts, "starts", row, i32, dev)
+            if repetition is not None:
+                rules.repetition = _tensor(repetition, "repetition", row, f32, dev)
+            if presence is not None:
+                rules.presence = _tensor(presence, "presence", row, f32, dev)
+            if frequency is not None:
+                rules.frequency = _tensor(frequency, "frequency", row, f32, dev)
+        elif not (lengths is starts is repetition is presence is frequency is None):
             raise ValueError("lengths, starts and penalties need a history")
         if (bias is None and bias_index is not None) or (mask is None and mask_index is not None):
             raise ValueError("an index needs its table")
-        if any(t is not None and t.shape[0] == 0 for t in (bias, mask)):
+        if bias is not None:
+            rules.n_bias = n = bias.shape[0]
+            rules.bias = _tensor(bias, "bias", (n, V), f32, dev)
+            if bias_index is not None:
+                rules.bias_index = _tensor(bias_index, "bias_index", row, i32, dev)
+        if mask is not None:
+            rules.n_masks = n = mask.shape[0]
+            rules.mask = _tensor(mask, "mask", (n, (V + 31) // 32), i32, dev)
+            if mask_index is not None:
+                rules.mask_index = _tensor(mask_index, "mask_index", row, i32, dev)
+        if (bias is not None and not rules.n_bias) or (mask is not None and not rules.n_masks):
             raise ValueError("a table needs a line")
-        T = 0 if history is None else history.shape[-1]
-        opt = lambda t, *a: None if t is None else _tensor(t, *a, self.device)
-        row = lambda t, name, dt: opt(t, name, (R,), dt)
-        lines = lambda t: 0 if t is None else t.shape[0]
-        rules = LogitRules(
-            opt(history, "history", (R, T), i32), T, row(lengths, "lengths", i32), row(starts, "starts", i32),
-            row(repetition, "repetition", f32), row(presence, "presence", f32), row(frequency, "frequency", f32),
-            opt(bias, "bias", (lines(bias), V), f32), lines(bias), row(bias_index, "bias_index", i32),
-            opt(mask, "mask", (lines(mask), (V + 31) // 32), i32), lines(mask), row(mask_index, "mask_index", i32))
         self._check(_lib.termezo_adjust_logits(
-            self.handle, _tensor(logits, "logits", (R, V), f32, self.device), R, V, ctypes.byref(rules),
-            _tensor(out, "out", (R, V), f32, self.device)), "adjust_logits")
+            self.handle, _tensor(logits, "logits", (R, V), f32, dev), R, V, ctypes.byref(rules),
+            _tensor(out, "out", (R, V), f32, dev)), "adjust_logits")
 
     def sample(self, logits, uniforms, tokens, logprobs=None, temperature=None, top_k=None, top_p=None,
                min_p=None):
