@@ -179,7 +179,8 @@ struct SliceStat {
   double sum;                        // weights relative to top
 };
 struct RowPlan {                     // what k_draw_list found
-  float top, xm, x_first;            // the row's largest logit; the least one that min_p keeps; that of the bins before first
+  float top, xm;                     // the row's largest logit; the least one that min_p keeps
+  float x_first, x_last;             // the least one of the bins before first, of those up to last
   int32_t bin;
   // Bins before first are kept; listed are bins first .. last, where top_p's border lies (or the only one), and
   // bin limit, where top_k or min_p ends (kBins: they do not)
@@ -419,6 +420,95 @@ __global__ void __launch_bounds__(256) k_draw_scan(DrawArgs a) {
   }
 }
 
+// One wave: mass and count [kBins] become sums up to each bin, four a lane (total: the whole row's weight at least); where
+// the borders lie.
+template <bool COUNT>
+__device__ __forceinline__ RowPlan draw_plan(double* mass, int* count, double total, float top, int bin,
+                                             const Settings& s, int lane) {
+  double b[4], upto[4];
+  int d[4] = {0, 0, 0, 0}, cs[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    b[k] = mass[4 * lane + k];
+    if (COUNT) d[k] = count[4 * lane + k];
+  }
+  const double sum = wave_scan((b[0] + b[1]) + (b[2] + b[3]));
+  upto[0] = sum - ((b[0] + b[1]) + (b[2] + b[3])) + b[0];
+#pragma unroll
+  for (int k = 1; k < 4; ++k) upto[k] = upto[k - 1] + b[k];
+  if (lane == 63) upto[3] = fmax(total, upto[3]);
+  if (COUNT) {
+    cs[0] = wave_scan(d[0] + d[1] + d[2] + d[3]) - d[1] - d[2] - d[3];
+#pragma unroll
+    for (int k = 1; k < 4; ++k) cs[k] = cs[k - 1] + d[k];
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    mass[4 * lane + k] = upto[k];
+    if (COUNT) count[4 * lane + k] = cs[k];
+  }
+  total = last_lane(upto[3]);
+  // the first bin up to which the sum is not below x (the last one if there is none)
+  auto first_at = [&](bool b0, bool b1, bool b2, bool b3) {
+    const unsigned long long who = __ballot(b0 || b1 || b2 || b3);
+    if (!who) return kBins - 1;
+    const int at = __ffsll((long long)who) - 1, mine = b0 ? 0 : b1 ? 1 : b2 ? 2 : 3;
+    return 4 * at + __builtin_amdgcn_readlane(mine, at);
+  };
+  auto first_sum = [&](double x) { return first_at(upto[0] >= x, upto[1] >= x, upto[2] >= x, upto[3] >= x); };
+  RowPlan p{top, -INFINITY, 0.0f, 0.0f, bin, kBins, -1, kBins, 0, 0.0, 0.0, total};
+  if (top > -INFINITY) {
+    int b1 = kBins;                                    // where top_k's or min_p's border lies
+    if (s.k == 1) b1 = 0;
+    else if (COUNT && s.k > 0) b1 = first_at(cs[0] >= s.k, cs[1] >= s.k, cs[2] >= s.k, cs[3] >= s.k);
+    if (s.min_p > 0.0f && s.min_p <= 1.0f) {
+      // the least logit with (x - top) / T >= ln min_p: an estimate, then its neighbours
+      const double z = log((double)s.min_p);
+      auto in = [&](float x) { return ((double)x - (double)top) * s.inv_t >= z; };
+      float xm = (float)((double)top + z / s.inv_t);
+      if (!(xm > -FLT_MAX)) xm = -FLT_MAX;
+      if (xm > top) xm = top;
+      for (int i = 0; i < 4 && xm > -FLT_MAX && in(unordered(ordered(xm) - 1)); ++i) xm = unordered(ordered(xm) - 1);
+      for (int i = 0; i < 4 && xm < top && !in(xm); ++i) xm = unordered(ordered(xm) + 1);
+      p.xm = xm;
+      const long long down = (long long)bin - draw_bin(xm, s.grid);
+      b1 = min(b1, (int)min(down, (long long)(kBins - 1)));
+    }
+    p.limit = b1;
+    p.first = b1;
+    p.last = b1 < kBins ? b1 : -1;
+    if (b1 > 0 && b1 < kBins) {
+      if (COUNT) p.count1 = count[b1 - 1];
+      p.mass1 = mass[b1 - 1];
+    }
+    if (s.p < 1.0f) {
+      // the weight of what top_k and min_p keep lies between that of the bins before theirs and with it
+      const double least = b1 == kBins ? total : p.mass1, most = b1 == kBins ? total : mass[b1];
+      const double goal0 = (double)s.p * least, goal1 = (double)s.p * most;
+      p.first = min(first_sum(goal0), b1);
+      p.last = min(first_sum(goal1), b1);
+    }
+    if (p.first > 0) p.mass0 = mass[p.first - 1];
+  }
+  return p;
+}
+
+// The least logit of the bins up to `down` below bin (NaN: there is none): a search among the keys, 64 parts at a time, by
+// one wave.
+__device__ __forceinline__ float draw_edge(int down, int bin, float grid, int lane) {
+  if (down < 0) return __uint_as_float(0x7FC00000u);
+  if (down >= kBins - 1) return -FLT_MAX;
+  uint32_t lo = ordered(-FLT_MAX), span = ordered(FLT_MAX) - lo;       // the border lies from lo to lo + span
+  while (span > 0) {
+    const uint32_t step = span / 64 + 1, k = lo + min((uint32_t)(lane + 1) * step - 1, span);
+    const unsigned long long in = __ballot(draw_bin(unordered(k), grid) >= bin - down);
+    const int at = __ffsll((long long)in) - 1;           // the row's largest logit is in: there is one
+    lo += (uint32_t)at * step;
+    span = min(step - 1, span - (uint32_t)at * step);
+  }
+  return unordered(lo);
+}
+
 template <int E, bool COUNT>
 __global__ void __launch_bounds__(256, 4) k_draw_list(DrawArgs a) {
   __shared__ double mass[kBins], factor[64];
@@ -487,101 +577,20 @@ __global__ void __launch_bounds__(256, 4) k_draw_list(DrawArgs a) {
   mass[j] = m;
   if (COUNT) count[j] = c;
   __syncthreads();
-  if (wave == 0) {                                       // sums up to each bin, four a lane, and where the borders lie
-    double b[4], upto[4];
-    int d[4] = {0, 0, 0, 0}, cs[4] = {0, 0, 0, 0};
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      b[k] = mass[4 * lane + k];
-      if (COUNT) d[k] = count[4 * lane + k];
-    }
-    const double sum = wave_scan((b[0] + b[1]) + (b[2] + b[3]));
-    upto[0] = sum - ((b[0] + b[1]) + (b[2] + b[3])) + b[0];
-#pragma unroll
-    for (int k = 1; k < 4; ++k) upto[k] = upto[k - 1] + b[k];
-    if (lane == 63) upto[3] = fmax(total, upto[3]);
-    if (COUNT) {
-      cs[0] = wave_scan(d[0] + d[1] + d[2] + d[3]) - d[1] - d[2] - d[3];
-#pragma unroll
-      for (int k = 1; k < 4; ++k) cs[k] = cs[k - 1] + d[k];
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      mass[4 * lane + k] = upto[k];
-      if (COUNT) count[4 * lane + k] = cs[k];
-    }
-    total = last_lane(upto[3]);
-    // the first bin up to which the sum is not below x (the last one if there is none)
-    auto first_at = [&](bool b0, bool b1, bool b2, bool b3) {
-      const unsigned long long who = __ballot(b0 || b1 || b2 || b3);
-      if (!who) return kBins - 1;
-      const int at = __ffsll((long long)who) - 1, mine = b0 ? 0 : b1 ? 1 : b2 ? 2 : 3;
-      return 4 * at + __builtin_amdgcn_readlane(mine, at);
-    };
-    auto first_sum = [&](double x) { return first_at(upto[0] >= x, upto[1] >= x, upto[2] >= x, upto[3] >= x); };
-    RowPlan p{top, -INFINITY, 0.0f, bin, kBins, -1, kBins, 0, 0.0, 0.0, total};
-    if (top > -INFINITY) {
-      int b1 = kBins;                                    // where top_k's or min_p's border lies
-      if (s.k == 1) b1 = 0;
-      else if (COUNT && s.k > 0) b1 = first_at(cs[0] >= s.k, cs[1] >= s.k, cs[2] >= s.k, cs[3] >= s.k);
-      if (s.min_p > 0.0f && s.min_p <= 1.0f) {
-        // the least logit with (x - top) / T >= ln min_p: an estimate, then its neighbours
-        const double z = log((double)s.min_p);
-        auto in = [&](float x) { return ((double)x - (double)top) * s.inv_t >= z; };
-        float xm = (float)((double)top + z / s.inv_t);
-        if (!(xm > -FLT_MAX)) xm = -FLT_MAX;
-        if (xm > top) xm = top;
-        for (int i = 0; i < 4 && xm > -FLT_MAX && in(unordered(ordered(xm) - 1)); ++i) xm = unordered(ordered(xm) - 1);
-        for (int i = 0; i < 4 && xm < top && !in(xm); ++i) xm = unordered(ordered(xm) + 1);
-        p.xm = xm;
-        const long long down = (long long)bin - draw_bin(xm, s.grid);
-        b1 = min(b1, (int)min(down, (long long)(kBins - 1)));
-      }
-      p.limit = b1;
-      p.first = b1;
-      p.last = b1 < kBins ? b1 : -1;
-      if (b1 > 0 && b1 < kBins) {
-        if (COUNT) p.count1 = count[b1 - 1];
-        p.mass1 = mass[b1 - 1];
-      }
-      if (s.p < 1.0f) {
-        // the weight of what top_k and min_p keep lies between that of the bins before theirs and with it
-        const double least = b1 == kBins ? total : p.mass1, most = b1 == kBins ? total : mass[b1];
-        const double goal0 = (double)s.p * least, goal1 = (double)s.p * most;
-        p.first = min(first_sum(goal0), b1);
-        p.last = min(first_sum(goal1), b1);
-      }
-      if (p.first > 0) p.mass0 = mass[p.first - 1];
-    }
+  if (wave == 0) {
+    const RowPlan p = draw_plan<COUNT>(mass, count, total, top, bin, s, lane);
     if (lane == 0) plan = p;
   }
   __syncthreads();
   const int first = plan.first, last = plan.last, limit = plan.limit;
   // The bins' borders as logits, one a wave: the least logit of the bins before first, of those up to last, before
-  // limit, up to limit (NaN: there is none).  A search among the keys, 64 parts at a time.
-  {
-    const int down = wave == 0 ? first - 1 : wave == 1 ? last : wave == 2 ? limit - 1 : limit;
-    uint32_t lo = ordered(-FLT_MAX), span = ordered(FLT_MAX) - lo;     // the border lies from lo to lo + span
-    if (down < 0) {
-      edges[wave] = __uint_as_float(0x7FC00000u);        // no logit is as great
-    } else if (down >= kBins - 1) {
-      edges[wave] = -FLT_MAX;
-    } else {
-      const int least = bin - down;
-      while (span > 0) {
-        const uint32_t step = span / 64 + 1, k = lo + min((uint32_t)(lane + 1) * step - 1, span);
-        const unsigned long long in = __ballot(draw_bin(unordered(k), s.grid) >= least);
-        const int at = __ffsll((long long)in) - 1;       // the row's largest logit is in: there is one
-        lo += (uint32_t)at * step;
-        span = min(step - 1, span - (uint32_t)at * step);
-      }
-      edges[wave] = unordered(lo);
-    }
-  }
+  // limit, up to limit.
+  edges[wave] = draw_edge(wave == 0 ? first - 1 : wave == 1 ? last : wave == 2 ? limit - 1 : limit, bin, s.grid, lane);
   __syncthreads();
   if (tid == 0 && slice == 0) {
     RowPlan p = plan;
     p.x_first = edges[0];
+    p.x_last = edges[1];
     a.plan[row] = p;
   }
   // this slice's weights in the bins before first
@@ -644,6 +653,144 @@ __device__ __forceinline__ T group_scan(T v, T* parts, int tid, T& total) {
   return v + before;
 }
 
+template <int NT>
+struct BorderShared {
+  unsigned long long pm[NT], ull[3][NT / 64], before_mass;
+  uint32_t pc[NT];
+  int ints[NT / 64], part, part_count, before_count;
+};
+
+// The least kept key among the n listed ones (key_at; 0: none there): by the whole work group of NT threads.
+template <int NT, typename K>
+__device__ __forceinline__ unsigned long long draw_border(const RowPlan& p, const Settings& s, double unit,
+                                                          const double* roots, int n, K key_at, BorderShared<NT>& sh,
+                                                          int tid) {
+  constexpr int NW = NT / 64;
+  const int lane = tid & 63, wave = tid >> 6;
+  // the least key of bins first .. last and the greatest of bin limit; the greatest of all
+  unsigned long long low = ~0ull, most = 0, high = 0;
+#pragma unroll 1
+  for (int i = tid; i < n; i += NT) {
+    const unsigned long long k = key_at(i);
+    if (!k) continue;
+    low = min(low, k);
+    high = max(high, k);
+    if (min(p.bin - draw_bin(key_logit(k), s.grid), kBins - 1) == p.limit) most = max(most, k);
+  }
+  auto greater = [](unsigned long long x, unsigned long long y) __attribute__((always_inline)) { return max(x, y); };
+  auto lesser = [](unsigned long long x, unsigned long long y) __attribute__((always_inline)) { return min(x, y); };
+  low = last_lane(wave_fold(low, ~0ull, lesser));
+  high = last_lane(wave_fold(high, 0ull, greater));
+  most = last_lane(wave_fold(most, 0ull, greater));
+  if (lane == 0) {
+    sh.ull[0][wave] = low;
+    sh.ull[1][wave] = high;
+    sh.ull[2][wave] = most;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    low = min(low, sh.ull[0][w]);
+    high = max(high, sh.ull[1][w]);
+    most = max(most, sh.ull[2][w]);
+  }
+  unsigned long long least = 0;
+  if (p.limit < kBins && p.xm > -INFINITY) least = (unsigned long long)ordered(p.xm) << 32;
+  // First where top_k ends (in bin limit), then where top_p does: of the keys from lo to hi in falling order, the one
+  // at which the count from have on reaches want, or the weight from sum on reaches goal.
+#pragma unroll 1
+  for (int stage = 0; stage < 2; ++stage) {
+    const bool counting = stage == 0;
+    if (counting ? !(p.limit < kBins && s.k > 0) : !(s.p < 1.0f)) continue;
+    unsigned long long lo = least, hi = most, sum = 0;
+    int have = p.count1;
+    double goal = 0.0;
+    if (!counting) {
+      double of = p.total;
+      if (p.limit < kBins) {                         // what top_k and min_p keep
+        unsigned long long w = 0;
+#pragma unroll 1
+        for (int i = tid; i < n; i += NT) {
+          const unsigned long long k = key_at(i);
+          if (k && k >= least && k <= most) w += draw_fix(draw_weight(key_logit(k), p.top, s.scale, roots), unit);
+        }
+        w = wave_sum(w);
+        __syncthreads();
+        if (lane == 0) sh.ull[0][wave] = w;
+        __syncthreads();
+        w = 0;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) w += sh.ull[0][i];
+        of = (double)w / unit + p.mass1;
+      }
+      goal = (double)s.p * of * unit;
+      sum = (unsigned long long)(p.mass0 * unit);
+      // the border lies in bins first .. last; between them and bin limit lie tokens that are not listed
+      if (p.last < p.limit) lo = max(max(lo, most + 1), (unsigned long long)ordered(p.x_last) << 32);
+      hi = high;
+      least = lo;
+    }
+    lo = max(lo, low);
+    if (lo > hi) {                                   // there are none: what lies before
+      least = counting ? least : (unsigned long long)ordered(p.x_first) << 32;
+      continue;
+    }
+    while (lo < hi) {
+      const int shift = max(0, 64 - __clzll((long long)(hi - lo)) - (NT == 1024 ? 10 : NT == 512 ? 9 : 8));
+      __syncthreads();
+      sh.pm[tid] = 0;
+      sh.pc[tid] = 0;
+      if (tid == 0) sh.part = INT32_MAX;
+      __syncthreads();
+#pragma unroll 1
+      for (int i = tid; i < n; i += NT) {
+        const unsigned long long k = key_at(i);
+        if (!k || k < lo || k > hi) continue;
+        const int at = NT - 1 - (int)((k - lo) >> shift);      // falling
+        atomicAdd(&sh.pc[at], 1u);
+        if (!counting) atomicAdd(&sh.pm[at], draw_fix(draw_weight(key_logit(k), p.top, s.scale, roots), unit));
+      }
+      __syncthreads();
+      const unsigned long long m0 = sh.pm[tid], ms = wave_scan(m0);
+      const int c0 = (int)sh.pc[tid], cs = wave_scan(c0);
+      if (lane == 63) {
+        sh.ull[0][wave] = ms;
+        sh.ints[wave] = cs;
+      }
+      __syncthreads();
+      unsigned long long me = ms;
+      int ce = cs;
+#pragma unroll
+      for (int w = 0; w < NW; ++w)
+        if (w < wave) {
+          me += sh.ull[0][w];
+          ce += sh.ints[w];
+        }
+      const bool there = c0 && (counting ? have + ce >= s.k : (double)(sum + me) >= goal);
+      const unsigned long long who = __ballot(there);
+      if (who && lane == __ffsll((long long)who) - 1) atomicMin(&sh.part, tid);
+      __syncthreads();
+      const int at = sh.part;
+      if (at == INT32_MAX) break;                    // not reached: all of them
+      if (at == tid) {                               // what lies before that part
+        sh.before_count = ce - c0;
+        sh.before_mass = me - m0;
+        sh.part_count = c0;
+      }
+      __syncthreads();
+      have += sh.before_count;
+      sum += sh.before_mass;
+      const unsigned long long from = lo + ((unsigned long long)(NT - 1 - at) << shift);
+      const unsigned long long to = from + ((1ull << shift) - 1);
+      lo = max(lo, from);
+      hi = min(hi, to);
+      if (sh.part_count == 1) break;                    // the only key from lo to hi
+    }
+    least = lo;
+  }
+  return least;
+}
+
 constexpr int kMaxSlices = 2048;
 
 // More threads where slices are long and lists are (128 x 128256: 27 -> 20 us; one row of 32003 12.5 us, 9.6 with 512).
@@ -651,15 +798,12 @@ constexpr int pick_threads(bool limits, int E) { return limits && E > 2 ? 1024 :
 
 template <bool LIMITS, int E>
 __global__ void __launch_bounds__(pick_threads(LIMITS, E)) k_draw_pick(DrawArgs a, int unit_bits) {
-  constexpr int NT = pick_threads(LIMITS, E), NW = NT / 64, kParts = NT, SLICE = 1024 * E, EACH = SLICE / NT;
-  __shared__ unsigned long long keys[LIMITS ? kList : 1], pm[LIMITS ? kParts : 1], add[LIMITS ? kMaxSlices : 1];
-  __shared__ uint32_t pc[LIMITS ? kParts : 1];
-  __shared__ unsigned long long ull[3][NW];
-  __shared__ int ints[NW];
+  constexpr int NT = pick_threads(LIMITS, E), NW = NT / 64, SLICE = 1024 * E, EACH = SLICE / NT;
+  __shared__ unsigned long long keys[LIMITS ? kList : 1], add[LIMITS ? kMaxSlices : 1];
+  __shared__ BorderShared<LIMITS ? NT : 64> sh;
   __shared__ double dbl[NW];
   __shared__ float tops[NW];
-  __shared__ int part, part_count, before_count, slice_at, hit, last_kept;
-  __shared__ unsigned long long before_mass;
+  __shared__ int slice_at, hit, last_kept;
   __shared__ double before_slice, all_kept, log_kept;
   __shared__ double roots[kRootCount];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = blockIdx.x, V = a.vocab;
@@ -675,11 +819,13 @@ __global__ void __launch_bounds__(pick_threads(LIMITS, E)) k_draw_pick(DrawArgs 
   u = u >= 1.0f ? 1.0f - 0x1p-24f : u > 0.0f ? u : 0.0f;
   if (bad && tid == 0) atomicOr(a.err, kErrSample);
   if (!LIMITS && s.best) u = 0.0f;                       // the first of the best
-  RowPlan p{};
+  __shared__ RowPlan plan;
+  const RowPlan& p = plan;                               // in LDS
   int n_list = 0;
   if (LIMITS) {
-    p = a.plan[row];
+    if (tid == 0) plan = a.plan[row];
     n_list = a.listed[row];
+    __syncthreads();
   } else {
     float top = -INFINITY;
     for (int i = tid; i < a.slices; i += NT) top = fmaxf(top, stat[i].top);
@@ -688,9 +834,13 @@ __global__ void __launch_bounds__(pick_threads(LIMITS, E)) k_draw_pick(DrawArgs 
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < NW; ++w) top = fmaxf(top, tops[w]);
-    p.top = top;
-    p.first = kBins;
-    p.last = -1;
+    if (tid == 0) {
+      plan = RowPlan{};
+      plan.top = top;
+      plan.first = kBins;
+      plan.last = -1;
+    }
+    __syncthreads();
   }
   if (!(p.top > -INFINITY)) {                            // nothing to draw
     if (tid == 0) {
@@ -718,133 +868,18 @@ __global__ void __launch_bounds__(pick_threads(LIMITS, E)) k_draw_pick(DrawArgs 
         const int b = bin_of(v);
         return v > -INFINITY && ((b >= p.first && b <= p.last) || b == p.limit) ? draw_key(v, t) : 0ull;
       };
-      // the least key of bins first .. last and the greatest of bin limit; the greatest of all
-      unsigned long long low = ~0ull, most = 0, high = 0;
+      if (held) {
 #pragma unroll 4
-      for (int i = tid; i < n; i += NT) {
-        const unsigned long long k = held ? list[i] : from_row(i);
-        if (held) keys[i] = k;
-        if (!k) continue;
-        low = min(low, k);
-        high = max(high, k);
-        if (bin_of(key_logit(k)) == p.limit) most = max(most, k);
+        for (int i = tid; i < n; i += NT) keys[i] = list[i];
+        __syncthreads();
       }
-      auto greater = [](unsigned long long x, unsigned long long y) __attribute__((always_inline)) { return max(x, y); };
-      auto lesser = [](unsigned long long x, unsigned long long y) __attribute__((always_inline)) { return min(x, y); };
-      low = last_lane(wave_fold(low, ~0ull, lesser));
-      high = last_lane(wave_fold(high, 0ull, greater));
-      most = last_lane(wave_fold(most, 0ull, greater));
-      if (lane == 0) {
-        ull[0][wave] = low;
-        ull[1][wave] = high;
-        ull[2][wave] = most;
-      }
-      __syncthreads();
-#pragma unroll
-      for (int w = 0; w < NW; ++w) {
-        low = min(low, ull[0][w]);
-        high = max(high, ull[1][w]);
-        most = max(most, ull[2][w]);
-      }
-      unsigned long long least = 0;
-      if (p.limit < kBins && p.xm > -INFINITY) least = (unsigned long long)ordered(p.xm) << 32;
-      // First where top_k ends (in bin limit), then where top_p does: of the keys from lo to hi in falling order, the one
-      // at which the count from have on reaches want, or the weight from sum on reaches goal.
-#pragma unroll 1
-      for (int stage = 0; stage < 2; ++stage) {
-        const bool counting = stage == 0;
-        if (counting ? !(p.limit < kBins && s.k > 0) : !(s.p < 1.0f)) continue;
-        unsigned long long lo = least, hi = most, sum = 0;
-        int have = p.count1;
-        double goal = 0.0;
-        if (!counting) {
-          double of = p.total;
-          if (p.limit < kBins) {                         // what top_k and min_p keep
-            unsigned long long w = 0;
-#pragma unroll 1
-            for (int i = tid; i < n; i += NT) {
-              const unsigned long long k = held ? keys[i] : from_row(i);
-              if (k && k >= least && k <= most) w += fixed(k);
-            }
-            w = wave_sum(w);
-            __syncthreads();
-            if (lane == 0) ull[0][wave] = w;
-            __syncthreads();
-            w = 0;
-#pragma unroll
-            for (int i = 0; i < NW; ++i) w += ull[0][i];
-            of = (double)w / unit + p.mass1;
-          }
-          goal = (double)s.p * of * unit;
-          sum = (unsigned long long)(p.mass0 * unit);
-          if (p.last < p.limit) lo = max(lo, most + 1);  // the border lies before bin limit
-          hi = high;
-          least = lo;
-        }
-        lo = max(lo, low);
-        if (lo > hi) {                                   // there are none: what lies before
-          least = counting ? least : (unsigned long long)ordered(p.x_first) << 32;
-          continue;
-        }
-        while (lo < hi) {
-          const int shift = max(0, 64 - __clzll((long long)(hi - lo)) - (NT == 1024 ? 10 : 9));
-          __syncthreads();
-          pm[tid] = 0;
-          pc[tid] = 0;
-          if (tid == 0) part = INT32_MAX;
-          __syncthreads();
-#pragma unroll 1
-          for (int i = tid; i < n; i += NT) {
-            const unsigned long long k = held ? keys[i] : from_row(i);
-            if (!k || k < lo || k > hi) continue;
-            const int at = kParts - 1 - (int)((k - lo) >> shift);      // falling
-            atomicAdd(&pc[at], 1u);
-            if (!counting) atomicAdd(&pm[at], fixed(k));
-          }
-          __syncthreads();
-          const unsigned long long m0 = pm[tid], ms = wave_scan(m0);
-          const int c0 = (int)pc[tid], cs = wave_scan(c0);
-          if (lane == 63) {
-            ull[0][wave] = ms;
-            ints[wave] = cs;
-          }
-          __syncthreads();
-          unsigned long long me = ms;
-          int ce = cs;
-#pragma unroll
-          for (int w = 0; w < NW; ++w)
-            if (w < wave) {
-              me += ull[0][w];
-              ce += ints[w];
-            }
-          const bool there = c0 && (counting ? have + ce >= s.k : (double)(sum + me) >= goal);
-          const unsigned long long who = __ballot(there);
-          if (who && lane == __ffsll((long long)who) - 1) atomicMin(&part, tid);
-          __syncthreads();
-          const int at = part;
-          if (at == INT32_MAX) break;                    // not reached: all of them
-          if (at == tid) {                               // what lies before that part
-            before_count = ce - c0;
-            before_mass = me - m0;
-            part_count = c0;
-          }
-          __syncthreads();
-          have += before_count;
-          sum += before_mass;
-          const unsigned long long from = lo + ((unsigned long long)(kParts - 1 - at) << shift);
-          const unsigned long long to = from + ((1ull << shift) - 1);
-          lo = max(lo, from);
-          hi = min(hi, to);
-          if (part_count == 1) break;                    // the only key from lo to hi
-        }
-        least = lo;
-      }
-      border = max(least, border);
+      auto key_at = [&](int i) __attribute__((always_inline)) { return held ? keys[i] : from_row(i); };
+      border = max(border, draw_border<NT>(p, s, unit, roots, n, key_at, sh, tid));
       // the listed tokens' share of their slices
       __syncthreads();
 #pragma unroll 1
       for (int i = tid; i < n; i += NT) {
-        const unsigned long long k = held ? keys[i] : from_row(i);
+        const unsigned long long k = key_at(i);
         if (k && k >= border) atomicAdd(&add[key_token(k) / SLICE], fixed(k));
       }
     }
@@ -946,6 +981,201 @@ __global__ void __launch_bounds__(pick_threads(LIMITS, E)) k_draw_pick(DrawArgs 
   }
 }
 
+// The whole draw of a row of up to 4 NT E logits by one work group, which holds them in registers: the same steps with
+// the row for a slice, one launch and no memory in between (one row of 1000 17 -> 8 us).  Bound by the exponentials of one
+// compute unit.
+template <bool LIMITS, bool COUNT, int NT, int E>
+__global__ void __launch_bounds__(NT) k_draw_row(DrawArgs a, int unit_bits) {
+  constexpr int NW = NT / 64, PASS = 4 * NT;
+  __shared__ unsigned long long keys[LIMITS ? PASS * E : 1], bins[LIMITS ? kCopies * kBins : 1];
+  __shared__ uint32_t counts[COUNT ? kCopies * kBins : 1];
+  __shared__ BorderShared<LIMITS ? NT : 64> sh;
+  __shared__ double mass[kBins], dbl[NW], chunk[E][NW], roots[kRootCount];
+  __shared__ int count[kBins];
+  __shared__ float tops[NW], edges[4];
+  __shared__ RowPlan plan;
+  __shared__ int n_list, chunk_at, hit, last_kept;
+  __shared__ double before_chunk, all_kept, log_kept;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = blockIdx.x, V = a.vocab;
+  if (tid < kRootCount) roots[tid] = kRoots[tid];
+  const float* x = a.logits + (int64_t)row * V;
+  Four raw[E];                                           // raw[i].v[j] at PASS i + 4 tid + j
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const uint32_t t = (uint32_t)PASS * i + 4u * tid;
+    raw[i] = Four{{-INFINITY, -INFINITY, -INFINITY, -INFINITY}};
+    if (t + 4u <= (uint32_t)V) {
+      raw[i] = *(const Four*)(x + t);
+    } else if (t < (uint32_t)V) {
+      raw[i].v[0] = x[t];
+      if (t + 1u < (uint32_t)V) raw[i].v[1] = x[t + 1u];
+      if (t + 2u < (uint32_t)V) raw[i].v[2] = x[t + 2u];
+    }
+  }
+  const Settings s = draw_settings(a, row);
+  const double unit = (double)(1ull << unit_bits);
+  float u = a.uniforms[row];
+  const bool bad = s.bad || !(u >= 0.0f && u < 1.0f);
+  u = u >= 1.0f ? 1.0f - 0x1p-24f : u > 0.0f ? u : 0.0f;
+  if (bad && tid == 0) atomicOr(a.err, kErrSample);
+  if (!LIMITS && s.best) u = 0.0f;                       // the first of the best
+  if (LIMITS)
+    for (int i = tid; i < kCopies * kBins; i += NT) {
+      bins[i] = 0;
+      if (COUNT) counts[i] = 0;
+    }
+  float top = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < E; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      raw[i].v[j] = draw_clean(raw[i].v[j]);
+      top = fmaxf(top, raw[i].v[j]);
+    }
+  top = wave_top(top);
+  if (lane == 0) tops[wave] = top;
+  if (tid == 0) {
+    n_list = 0;
+    hit = INT32_MAX;
+    last_kept = -1;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < NW; ++w) top = fmaxf(top, tops[w]);
+  if (!(top > -INFINITY)) {                              // nothing to draw
+    if (tid == 0) {
+      a.tokens[row] = -1;
+      if (a.logprobs) a.logprobs[row] = -INFINITY;
+    }
+    return;
+  }
+  unsigned long long border = draw_key(-FLT_MAX, INT32_MAX);           // keys from here on are kept
+  if constexpr (LIMITS) {
+    const int bin = draw_bin(top, s.grid), copy = (tid & (kCopies - 1)) * kBins;
+#pragma unroll
+    for (int i = 0; i < 4 * E; ++i) {
+      const float v = raw[i / 4].v[i % 4];
+      if (v > -INFINITY) {
+        const int j = min(bin - draw_bin(v, s.grid), kBins - 1);
+        atomicAdd(&bins[copy + j], draw_fix(draw_weight(v, top, s.scale, roots), kSliceUnit));
+        if (COUNT) atomicAdd(&counts[copy + j], 1u);
+      }
+    }
+    __syncthreads();
+    if (tid < kBins) {
+      unsigned long long m = 0;
+      uint32_t c = 0;
+#pragma unroll
+      for (int i = 0; i < kCopies; ++i) {
+        m += bins[i * kBins + tid];
+        if (COUNT) c += counts[i * kBins + tid];
+      }
+      mass[tid] = (double)m * (1.0 / kSliceUnit);
+      if (COUNT) count[tid] = (int)c;
+    }
+    __syncthreads();
+    if (wave == 0) {
+      const RowPlan p = draw_plan<COUNT>(mass, count, 0.0, top, bin, s, lane);
+      if (lane == 0) plan = p;
+    }
+    __syncthreads();
+    const int first = plan.first, last = plan.last, limit = plan.limit;
+    if (first <= last) {
+      if (wave < 4)
+        edges[wave] = draw_edge(wave == 0 ? first - 1 : wave == 1 ? last : wave == 2 ? limit - 1 : limit, bin, s.grid, lane);
+      __syncthreads();
+      const float hi1 = edges[0], lo1 = edges[1], hi2 = edges[2], lo2 = edges[3];
+      const bool two = limit > last && limit < kBins;
+      uint32_t mine = 0;
+#pragma unroll
+      for (int i = 0; i < 4 * E; ++i) {
+        const float v = raw[i / 4].v[i % 4];
+        if ((v >= lo1 && !(v >= hi1)) || (two && v >= lo2 && !(v >= hi2))) mine |= 1u << i;
+      }
+      const int n = __popc(mine), upto = wave_scan(n), all = last_lane(upto);
+      int at = 0;
+      if (lane == 0 && all) at = atomicAdd(&n_list, all);
+      at = __builtin_amdgcn_readfirstlane(at) + upto - n;
+#pragma unroll
+      for (int i = 0; i < 4 * E; ++i)
+        if (mine >> i & 1u) {
+          keys[at++] = draw_key(raw[i / 4].v[i % 4], PASS * (i / 4) + 4 * tid + i % 4);
+        }
+      if (tid == 0) {
+        plan.x_first = edges[0];
+        plan.x_last = edges[1];
+      }
+      __syncthreads();
+      const RowPlan& p = plan;                           // in LDS
+      auto key_at = [&](int i) __attribute__((always_inline)) { return keys[i]; };
+      border = max(border, draw_border<NT>(p, s, unit, roots, n_list, key_at, sh, tid));
+    }
+  }
+  const float xb = LIMITS ? key_logit(border) : s.best ? top : -FLT_MAX;
+  const uint32_t tb = LIMITS ? (uint32_t)key_token(border) : UINT32_MAX;
+  auto weight = [&](float v, int t) __attribute__((always_inline)) {
+    return v > xb || (v == xb && (uint32_t)t <= tb) ? draw_weight(v, top, s.scale, roots) : 0.0;
+  };
+  // kept weights by pass and wave
+  double part[E];
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    part[i] = 0.0;
+    const float most = fmaxf(fmaxf(raw[i].v[0], raw[i].v[1]), fmaxf(raw[i].v[2], raw[i].v[3]));
+    if (__ballot(most >= xb))
+#pragma unroll
+      for (int j = 0; j < 4; ++j) part[i] += weight(raw[i].v[j], PASS * i + 4 * tid + j);
+    const double w = wave_sum(part[i]);
+    if (lane == 0) chunk[i][wave] = w;
+  }
+  __syncthreads();
+  if (wave == 0) {
+    double w = 0.0;
+    if (lane < E)
+#pragma unroll
+      for (int k = 0; k < NW; ++k) w += chunk[lane][k];
+    const double c = wave_scan(w), all = last_lane(c), target = (double)u * all;
+    const unsigned long long over = __ballot(w > 0.0 && c > target), any = __ballot(w > 0.0);
+    const int at = over ? __ffsll((long long)over) - 1 : any ? 63 - __clzll((long long)any) : 0;
+    if (lane == at) {
+      chunk_at = at;
+      before_chunk = c - w;
+      all_kept = all;
+      log_kept = ln_of(all);
+    }
+  }
+  __syncthreads();
+  const int at_chunk = chunk_at;
+  const double want = (double)u * all_kept - before_chunk;
+  double mine = 0.0;
+#pragma unroll
+  for (int i = 0; i < E; ++i) mine = i == at_chunk ? part[i] : mine;
+  double total;
+  const double upto = group_scan<NW>(mine, dbl, tid, total);
+  const int t0 = PASS * at_chunk + 4 * tid;
+  int at = -1;
+  if (mine > 0.0 && (upto > want || total <= want)) {
+    double c = upto - mine;
+    int last = -1;
+    for (int j = 0; j < 4; ++j) {
+      const float v = t0 + j < V ? draw_clean(x[t0 + j]) : -INFINITY;
+      const double w = weight(v, t0 + j);
+      c += w;
+      if (w > 0.0) last = t0 + j;
+      if (w > 0.0 && c > want && at < 0) at = t0 + j;
+    }
+    if (at >= 0) atomicMin(&hit, at);
+    else if (last >= 0) atomicMax(&last_kept, last);     // where rounding leaves none: the last one
+  }
+  __syncthreads();
+  if (hit == INT32_MAX && t0 <= last_kept && last_kept < t0 + 4) at = last_kept;
+  if (at >= 0 && (at == hit || hit == INT32_MAX)) {
+    a.tokens[row] = at;
+    if (a.logprobs)
+      a.logprobs[row] = s.best ? 0.0f : (float)(((double)draw_clean(x[at]) - (double)top) * s.inv_t - log_kept);
+  }
+}
+
 }  // namespace tmz
 
 using namespace tmz;
@@ -1017,10 +1247,11 @@ termezo_status termezo_sample(termezo_ctx* c, const float* logits, const float* 
   if (scope.err != hipSuccess) return hip_status(c, scope.err, "sample");
   const int64_t most = std::min<int64_t>(rows, kMaxDrawRows);      // rows at a time
   const bool limits = top_k || top_p || min_p;
+  const bool whole = vocab <= 8192;      // a row by one work group
   const int long_slices = (vocab + 8191) / 8192;
   const bool large = (limits && most * long_slices >= 2 * (int64_t)c->n_cu) || long_slices > 64;
   const int slice = large ? 8192 : 2048, slices = (vocab + slice - 1) / slice;   // kMaxSlices at most
-  const int64_t per_row = (int64_t)slices * sizeof(SliceStat) +
+  const int64_t per_row = whole ? 0 : (int64_t)slices * sizeof(SliceStat) +
                           (limits ? (int64_t)slices * (kBins * 12 + 8) + sizeof(RowPlan) + 8 + (int64_t)kList * 8 : 0);
   const termezo_status st = scratch_for(c, c->draw, most * per_row, "sample");
   if (st != TERMEZO_OK) return st;
@@ -1059,6 +1290,21 @@ termezo_status termezo_sample(termezo_ctx* c, const float* logits, const float* 
     a.logprobs = from(logprobs);
     const dim3 grid((unsigned)slices, (unsigned)n);
     const dim3 rows_grid((unsigned)n);
+    if (whole) {
+#define TMZ_ROW(NT, E)                                                                                                 \
+  if (!limits) hipLaunchKernelGGL((k_draw_row<false, false, NT, E>), rows_grid, dim3(NT), 0, c->stream, a, unit);     \
+  else if (top_k) hipLaunchKernelGGL((k_draw_row<true, true, NT, E>), rows_grid, dim3(NT), 0, c->stream, a, unit);    \
+  else hipLaunchKernelGGL((k_draw_row<true, false, NT, E>), rows_grid, dim3(NT), 0, c->stream, a, unit)
+      if (vocab <= 1024) {
+        TMZ_ROW(256, 1);
+      } else if (vocab <= 4096) {
+        TMZ_ROW(256, 4);
+      } else {
+        TMZ_ROW(512, 4);
+      }
+#undef TMZ_ROW
+      continue;
+    }
 #define TMZ_DRAW(E)                                                                                          \
   if (!limits) {                                                                                             \
     hipLaunchKernelGGL((k_draw_scan<E, false, false>), grid, dim3(256), 0, c->stream, a);                    \

@@ -371,6 +371,20 @@ def test_draw_of_many_rows_with_settings_of_their_own(ctx):
     assert tok[7] == tok[9] == -1 and tok[8] == V - 1 and tok[10] % 2 == 1
 
 
+@pytest.mark.parametrize("V", [70, 1000, 30000, 40000, 128256])
+def test_draw_with_limits_far_apart(ctx, V):
+    """top_p's border at the best tokens, top_k's or min_p's far behind: tokens between the two are neither listed
+    nor kept."""
+    rng = np.random.default_rng(V)
+    for R in (4, 40):
+        x = (rng.standard_normal((R, V)) * 8).astype(F)
+        x[::2] = np.round(x[::2])                         # gaps and ties between few values
+        u = rng.random(R).astype(F)
+        for kw in (dict(top_k=V * 5 // 7, top_p=0.9), dict(top_k=V // 2, top_p=0.5), dict(min_p=1e-8, top_p=0.9),
+                   dict(min_p=1e-9, top_k=V // 3, top_p=0.99), dict(top_k=V - 1, top_p=0.3, temperature=2.0)):
+            _check_sample(ctx, x, u, **kw)
+
+
 @pytest.mark.parametrize("V", [4, 4096, 20000])
 def test_draw_ties(ctx, V):
     """Equal logits: the lowest indices are kept, the shares are exact; u on their borders belongs to the next one.
@@ -500,10 +514,10 @@ def test_captured_calls(ctx):
             own.linear_i8(b["x"], b["codes"], b["steps"], b["logits"])
             own.adjust_logits(b["logits"], b["logits"], history=b["h"], repetition=b["rep"])
             own.sample(b["logits"], b["u"], b["tok"], logprobs=b["lp"], top_p=b["top_p"])
-        bufs = [make(200, 256, 3000, 20), make(3, 512, 5000, 9)]
+        bufs = [make(200, 256, 3000, 20), make(3, 512, 5000, 9), make(5, 256, 40000, 30)]
         for b in bufs:
             work(b)
-        big = make(700, 1024, 9000, 5)
+        big = make(300, 1024, 40000, 5)
         stream.synchronize()
     graphs = []
     for b in bufs:
