@@ -167,6 +167,10 @@ __global__ void __launch_bounds__(256) k_adjust(RuleArgs a) {
 // a part a thread at a time; then the slice and the token.  Where the list does not hold them (many equal logits)
 // it goes through the row in the list's place.
 // Without limits the first and the last are enough.
+// The scan is bound by vector instructions (an exponential in fp64 and a bin a logit) beside its reads, the list by
+// them and the bins' sums, which every work group of a row forms for itself, the pick by its chain of barriers: 64 x
+// 128256 with top_p 14 + 17 + 21 us (the logits alone at the rate of a copy: 6.4), one row of 32003 with top_k and top_p 3.9 +
+// 8.0 + 9.0, 256 x 32000 without limits 11 + 6.5.
 // ---------------------------------------------------------------------------
 constexpr int kBins = 256, kMaxDrawRows = 1024, kList = 8192;
 constexpr int kCopies = 4;           // of the bins, so that neighbouring lanes seldom meet in one
@@ -736,7 +740,7 @@ __device__ __forceinline__ unsigned long long draw_border(const RowPlan& p, cons
       continue;
     }
     while (lo < hi) {
-      const int shift = max(0, 64 - __clzll((long long)(hi - lo)) - (NT == 1024 ? 10 : NT == 512 ? 9 : 8));
+      const int shift = max(0, 64 - __clzll((long long)(hi - lo)) - (NT == 512 ? 9 : 8));
       __syncthreads();
       sh.pm[tid] = 0;
       sh.pc[tid] = 0;
@@ -793,8 +797,9 @@ __device__ __forceinline__ unsigned long long draw_border(const RowPlan& p, cons
 
 constexpr int kMaxSlices = 2048;
 
-// More threads where slices are long and lists are (128 x 128256: 27 -> 20 us; one row of 32003 12.5 us, 9.6 with 512).
-constexpr int pick_threads(bool limits, int E) { return limits && E > 2 ? 1024 : 512; }
+// What bounds a row is its chain of barriers, so short slices take few waves (one row of 32003: 9.0 us, 10.3 with 512 threads
+// and 12.5 with 1024); long ones 512 threads (128 x 128256: 19.4 us, 19.8 with 1024).
+constexpr int pick_threads(bool limits, int E) { return limits && E > 2 ? 512 : 256; }
 
 template <bool LIMITS, int E>
 __global__ void __launch_bounds__(pick_threads(LIMITS, E)) k_draw_pick(DrawArgs a, int unit_bits) {
@@ -982,8 +987,8 @@ __global__ void __launch_bounds__(pick_threads(LIMITS, E)) k_draw_pick(DrawArgs 
 }
 
 // The whole draw of a row of up to 4 NT E logits by one work group, which holds them in registers: the same steps with
-// the row for a slice, one launch and no memory in between (one row of 1000 17 -> 8 us).  Bound by the exponentials of one
-// compute unit.
+// the row for a slice, one launch and no memory in between: 512 rows of 1000 47 -> 14 us, one row of 1000 19 -> 11.5, 256 of
+// 8192 27 -> 21; from 16384 on the slices are faster (one row 20 against 27 us).  Few waves, for the barriers.
 template <bool LIMITS, bool COUNT, int NT, int E>
 __global__ void __launch_bounds__(NT) k_draw_row(DrawArgs a, int unit_bits) {
   constexpr int NW = NT / 64, PASS = 4 * NT;
