@@ -320,11 +320,9 @@ __global__ void __launch_bounds__(64 * NW) k_linear_walk(const TX* __restrict__ 
 typedef int v16i __attribute__((ext_vector_type(16)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
-struct __attribute__((packed, aligned(2))) Unit {        // 16 bytes of a row that may begin anywhere
-  v4u v;
-};
+typedef uint32_t Unit __attribute__((ext_vector_type(4), aligned(2)));  // 16 bytes of a row that may begin anywhere
 
-template <typename TY, int BM, int BN, int WM, int WN, int NST, int BPC>
+template <typename TY, int BM, int BN, int WM, int WN, int NST, int BPC, bool PAST>
 __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), BPC * (BM / WM) * (BN / WN) / 4)
     k_linear_tile(const int8_t* __restrict__ q, const float* __restrict__ xstep, const int8_t* __restrict__ codes,
                   const float* __restrict__ steps, int64_t M, int64_t K, int64_t N, TY* __restrict__ out) {
@@ -525,7 +523,8 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), BPC * (BM / WM) * 
           if (mo >= M || no >= N) continue;
           TY* p = out + mo * N + no;
           if (no + UB <= N) {
-            ((Unit*)p)->v = o[i];
+            if (PAST) __builtin_nontemporal_store(o[i], (Unit*)p);
+            else *(Unit*)p = o[i];
           } else {
 #pragma unroll
             for (int k = 0; k < UB; ++k)
@@ -562,6 +561,9 @@ template <typename TY>
 static void linear_tiles(const int8_t* q, const float* xstep, const int8_t* codes, const float* steps, int64_t M,
                          int64_t K, int64_t N, TY* out, int n_cu, hipStream_t s) {
   auto count = [&](int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
+  // An output of more than the eight L2s hold (4 MB each) goes past them and leaves them to the matrices:
+  // 8192 x 2560 -> 13824 295 -> 251 us, 8192 x 6912 -> 2560 180 -> 154.
+  const bool past = M * N * (int64_t)sizeof(TY) >= int64_t(32) << 20;
   int best = 0;
   float least = 0.0f;
   for (int t = 0; t < 4; ++t) {
@@ -575,15 +577,21 @@ static void linear_tiles(const int8_t* q, const float* xstep, const int8_t* code
       least = cost;
     }
   }
-#define TMZ_TILE(BM, BN, WM, WN, NST, BPC)                                                                    \
-  hipLaunchKernelGGL((k_linear_tile<TY, BM, BN, WM, WN, NST, BPC>),                                           \
+#define TMZ_TILE(BM, BN, WM, WN, NST, BPC, PAST)                                                              \
+  hipLaunchKernelGGL((k_linear_tile<TY, BM, BN, WM, WN, NST, BPC, PAST>),                                           \
                      dim3((unsigned)std::min<int64_t>(count(BM, BN), (int64_t)BPC * n_cu)),                   \
                      dim3(64 * (BM / WM) * (BN / WN)), 0, s, q, xstep, codes, steps, M, K, N, out)
   switch (best) {
-    case 0: TMZ_TILE(256, 256, 128, 64, 2, 1); break;
-    case 1: TMZ_TILE(128, 256, 64, 64, 3, 1); break;
-    case 2: TMZ_TILE(128, 128, 64, 32, 4, 1); break;
-    default: TMZ_TILE(64, 64, 32, 32, 3, 3);
+    case 0:
+      if (past) TMZ_TILE(256, 256, 128, 64, 2, 1, true);
+      else TMZ_TILE(256, 256, 128, 64, 2, 1, false);
+      break;
+    case 1:
+      if (past) TMZ_TILE(128, 256, 64, 64, 3, 1, true);
+      else TMZ_TILE(128, 256, 64, 64, 3, 1, false);
+      break;
+    case 2: TMZ_TILE(128, 128, 64, 32, 4, 1, false); break;
+    default: TMZ_TILE(64, 64, 32, 32, 3, 3, false);
   }
 #undef TMZ_TILE
 }
