@@ -162,17 +162,18 @@ __global__ void __launch_bounds__(256) k_adjust(RuleArgs a) {
 // A bin is an eighth of T wide on a grid that all slices share (bin = floor(x (8 / T))), counted from the slice's
 // best bin downwards; the last of the 256 holds all that lies lower.
 // k_draw_list, the same grid: the row's bins (slices weighted by exp((m_s - m) / T)) tell in which of them the
-// borders lie; the slice's logits in those bins go to the row's list.
+// borders lie (long slices: found by k_draw_plan before); the slice's logits in those bins go to the row's list.
 // k_draw_pick, a work group a row: finds the border in the list by narrowing a range of keys (logit, index),
 // a part a thread at a time; then the slice and the token.  Where the list does not hold them (many equal logits)
 // it goes through the row in the list's place.
 // Without limits the first and the last are enough.
 // The scan is bound by vector instructions (an exponential in fp64 and a bin a logit) beside its reads, the list by
-// them and the bins' sums, which every work group of a row forms for itself, the pick by its chain of barriers: 64 x
-// 128256 with top_p 14 + 17 + 21 us (the logits alone at the rate of a copy: 6.4), one row of 32003 with top_k and top_p 3.9 +
-// 8.0 + 9.0, 256 x 32000 without limits 11 + 6.5.
+// its reads, the plan and the pick by their chains of barriers: 64 x 128256 with top_p 14.5 + 6.0 + 12.8 + 20.4 us (the logits
+// alone at the rate of a copy: 6.4), one row of 32003 with top_k and top_p 3.9 + 8.4 + 9.1, 256 x 32000 without
+// limits 11 + 6.8.
 // ---------------------------------------------------------------------------
 constexpr int kBins = 256, kMaxDrawRows = 1024, kList = 8192;
+constexpr bool plan_first(int E) { return E > 2; }       // long slices: plans in a launch of their own
 constexpr int kCopies = 4;           // of the bins, so that neighbouring lanes seldom meet in one
 constexpr double kSliceUnit = 0x1p48;
 constexpr double kLog2e32 = 32.0 * 0x1.71547652b82fep+0, kLn2by32 = 0x1.62e42fefa39efp-6;   // 32 log2(e), ln(2) / 32
@@ -184,7 +185,8 @@ struct SliceStat {
 };
 struct RowPlan {                     // what k_draw_list found
   float top, xm;                     // the row's largest logit; the least one that min_p keeps
-  float x_first, x_last;             // the least one of the bins before first, of those up to last
+  // the least logit of the bins before first, of those up to last, before limit, up to limit (NaN: there is none)
+  float x_first, x_last, x_before, x_limit;
   int32_t bin;
   // Bins before first are kept; listed are bins first .. last, where top_p's border lies (or the only one), and
   // bin limit, where top_k or min_p ends (kBins: they do not)
@@ -460,7 +462,7 @@ __device__ __forceinline__ RowPlan draw_plan(double* mass, int* count, double to
     return 4 * at + __builtin_amdgcn_readlane(mine, at);
   };
   auto first_sum = [&](double x) { return first_at(upto[0] >= x, upto[1] >= x, upto[2] >= x, upto[3] >= x); };
-  RowPlan p{top, -INFINITY, 0.0f, 0.0f, bin, kBins, -1, kBins, 0, 0.0, 0.0, total};
+  RowPlan p{top, -INFINITY, 0.0f, 0.0f, 0.0f, 0.0f, bin, kBins, -1, kBins, 0, 0.0, 0.0, total};
   if (top > -INFINITY) {
     int b1 = kBins;                                    // where top_k's or min_p's border lies
     if (s.k == 1) b1 = 0;
@@ -513,43 +515,41 @@ __device__ __forceinline__ float draw_edge(int down, int bin, float grid, int la
   return unordered(lo);
 }
 
-template <int E, bool COUNT>
-__global__ void __launch_bounds__(256, 4) k_draw_list(DrawArgs a) {
-  __shared__ double mass[kBins], factor[64];
-  __shared__ int count[kBins], offset[64];
-  __shared__ float tops[4], edges[4];
-  __shared__ unsigned long long parts[4];
-  __shared__ int counts[4], base;
-  __shared__ RowPlan plan;
-  __shared__ double roots[kRootCount];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int row = blockIdx.y, slice = blockIdx.x, V = a.vocab;
-  if (tid < kRootCount) roots[tid] = kRoots[tid];
+template <bool COUNT>
+struct PlanShared {
+  double mass[kBins], factor[64], roots[kRootCount];
+  int count[COUNT ? kBins : 1], offset[64];
+  float tops[4], edges[4];
+  RowPlan plan;
+};
+
+// The row's plan into sh.plan, by a work group of 256; fetch() is called when the loads of the bins are on their way.
+template <bool COUNT, typename F>
+__device__ __forceinline__ void draw_row_plan(const DrawArgs& a, int row, PlanShared<COUNT>& sh, int tid, F fetch) {
+  const int lane = tid & 63, wave = tid >> 6;
+  if (tid < kRootCount) sh.roots[tid] = kRoots[tid];
   const Settings s = draw_settings(a, row);
   const SliceStat* stat = a.stat + (int64_t)row * a.slices;
-  const SliceStat own = stat[slice];
   const int j = tid;                                     // this thread's bin
-  const unsigned long long own_mass = a.mass[((int64_t)row * a.slices + slice) * kBins + j];
   float top = -INFINITY;
   for (int i = tid; i < a.slices; i += 256) top = fmaxf(top, stat[i].top);
   top = wave_top(top);
-  if (lane == 0) tops[wave] = top;
+  if (lane == 0) sh.tops[wave] = top;
   __syncthreads();
-  top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+  top = fmaxf(fmaxf(sh.tops[0], sh.tops[1]), fmaxf(sh.tops[2], sh.tops[3]));
   const int bin = draw_bin(top, s.grid);
   // The row's bins, 64 slices at a time: thread j takes what falls on bin j; the last bin has the rest
   double m = 0.0, total = 0.0;
   int c = 0;
-  Four raw[E];
   for (int s0 = 0; s0 < a.slices; s0 += 64) {
     const int n = min(64, a.slices - s0);
     __syncthreads();
     if (wave == 0) {
       const SliceStat t = stat[s0 + (lane < n ? lane : 0)];
       const bool any = lane < n && t.top > -INFINITY;
-      const double f = any ? draw_weight(t.top, top, s.scale, roots) : 0.0;
-      factor[lane] = f * (1.0 / kSliceUnit);
-      offset[lane] = any ? bin - t.bin : kBins;          // 0 or more; nothing of an empty slice
+      const double f = any ? draw_weight(t.top, top, s.scale, sh.roots) : 0.0;
+      sh.factor[lane] = f * (1.0 / kSliceUnit);
+      sh.offset[lane] = any ? bin - t.bin : kBins;       // 0 or more; nothing of an empty slice
       total += wave_sum(any ? f * t.sum : 0.0);
     }
     __syncthreads();
@@ -560,43 +560,79 @@ __global__ void __launch_bounds__(256, 4) k_draw_list(DrawArgs a) {
     for (int i0 = 0; i0 < n; i0 += 8) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const int i = min(i0 + k, n - 1), where = i * kBins + max(j - offset[i], 0);
+        const int i = min(i0 + k, n - 1), where = i * kBins + max(j - sh.offset[i], 0);
         v[k] = at[where];
         cv[k] = COUNT ? ct[where] : 0u;
       }
       if (s0 == 0 && i0 == 0) {
-        // the slice's logits are on their way while the borders are found (behind the bins: loads return in order)
+        // behind the bins: loads return in order
         __builtin_amdgcn_sched_barrier(0);
-        slice_fetch<E>(a.logits + (int64_t)row * V, slice * 1024 * E, V, tid, -INFINITY, raw);
+        fetch();
         __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
       for (int k = 0; k < 8; ++k)
-        if (i0 + k < n && j >= offset[i0 + k] && j < kBins - 1) {
-          m += factor[i0 + k] * (double)v[k];
+        if (i0 + k < n && j >= sh.offset[i0 + k] && j < kBins - 1) {
+          m += sh.factor[i0 + k] * (double)v[k];
           if (COUNT) c += (int)cv[k];
         }
     }
   }
-  mass[j] = m;
-  if (COUNT) count[j] = c;
+  sh.mass[j] = m;
+  if (COUNT) sh.count[j] = c;
   __syncthreads();
   if (wave == 0) {
-    const RowPlan p = draw_plan<COUNT>(mass, count, total, top, bin, s, lane);
-    if (lane == 0) plan = p;
+    const RowPlan p = draw_plan<COUNT>(sh.mass, sh.count, total, top, bin, s, lane);
+    if (lane == 0) sh.plan = p;
   }
   __syncthreads();
-  const int first = plan.first, last = plan.last, limit = plan.limit;
-  // The bins' borders as logits, one a wave: the least logit of the bins before first, of those up to last, before
-  // limit, up to limit.
-  edges[wave] = draw_edge(wave == 0 ? first - 1 : wave == 1 ? last : wave == 2 ? limit - 1 : limit, bin, s.grid, lane);
+  // the bins' borders as logits, one a wave
+  const int first = sh.plan.first, last = sh.plan.last, limit = sh.plan.limit;
+  sh.edges[wave] = draw_edge(wave == 0 ? first - 1 : wave == 1 ? last : wave == 2 ? limit - 1 : limit, bin, s.grid, lane);
   __syncthreads();
-  if (tid == 0 && slice == 0) {
-    RowPlan p = plan;
-    p.x_first = edges[0];
-    p.x_last = edges[1];
-    a.plan[row] = p;
+  if (tid == 0) {
+    sh.plan.x_first = sh.edges[0];
+    sh.plan.x_last = sh.edges[1];
+    sh.plan.x_before = sh.edges[2];
+    sh.plan.x_limit = sh.edges[3];
   }
+  __syncthreads();
+}
+
+// The plans of rows by a work group each, for k_draw_list with long slices, of which there are many: formed by each of
+// its work groups they cost more than this launch (128 x 128256 with top_k and top_p 34 us, 7 + 16 with it; 64 rows with top_p
+// 17, 6 + 13).
+template <bool COUNT>
+__global__ void __launch_bounds__(256) k_draw_plan(DrawArgs a) {
+  __shared__ PlanShared<COUNT> sh;
+  draw_row_plan<COUNT>(a, blockIdx.x, sh, threadIdx.x, []() {});
+  if (threadIdx.x == 0) a.plan[blockIdx.x] = sh.plan;
+}
+
+template <int E, bool COUNT>
+__global__ void __launch_bounds__(256, 4) k_draw_list(DrawArgs a) {
+  constexpr bool PLANNED = plan_first(E);
+  __shared__ PlanShared<COUNT && !PLANNED> sh;
+  __shared__ unsigned long long parts[4];
+  __shared__ int counts[4], base;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int row = blockIdx.y, slice = blockIdx.x, V = a.vocab;
+  const SliceStat own = a.stat[(int64_t)row * a.slices + slice];
+  const int j = tid;                                     // this thread's bin
+  const unsigned long long own_mass = a.mass[((int64_t)row * a.slices + slice) * kBins + j];
+  Four raw[E];                                           // on its way while the borders are found
+  auto fetch = [&]() __attribute__((always_inline)) {
+    slice_fetch<E>(a.logits + (int64_t)row * V, slice * 1024 * E, V, tid, -INFINITY, raw);
+  };
+  if constexpr (PLANNED) {
+    fetch();
+  } else {
+    draw_row_plan<COUNT>(a, row, sh, tid, fetch);
+    if (tid == 0 && slice == 0) a.plan[row] = sh.plan;
+  }
+  const RowPlan& plan = PLANNED ? a.plan[row] : sh.plan;
+  const int first = plan.first, last = plan.last, limit = plan.limit, bin = plan.bin;
+  const float hi1 = plan.x_first, lo1 = plan.x_last, hi2 = plan.x_before, lo2 = plan.x_limit;
   // this slice's weights in the bins before first
   if (first < kBins) {
     unsigned long long w = bin - own.bin + j < first && own.top > -INFINITY ? own_mass : 0;
@@ -610,7 +646,6 @@ __global__ void __launch_bounds__(256, 4) k_draw_list(DrawArgs a) {
   if (first > last) return;
   if (!(own.top > -INFINITY) || min(bin - own.bin, kBins - 1) > (limit < kBins ? limit : last)) return;
   uint32_t mine = 0;                                     // which of them are listed
-  const float hi1 = edges[0], lo1 = edges[1], hi2 = edges[2], lo2 = edges[3];
   const bool two = limit > last && limit < kBins;
   auto within = [](float v, float lo, float hi) __attribute__((always_inline)) { return v >= lo && !(v >= hi); };
 #pragma unroll
@@ -1317,9 +1352,11 @@ termezo_status termezo_sample(termezo_ctx* c, const float* logits, const float* 
   } else {                                                                                                   \
     if (top_k) {                                                                                             \
       hipLaunchKernelGGL((k_draw_scan<E, true, true>), grid, dim3(256), 0, c->stream, a);                    \
+      if (plan_first(E)) hipLaunchKernelGGL((k_draw_plan<true>), rows_grid, dim3(256), 0, c->stream, a);     \
       hipLaunchKernelGGL((k_draw_list<E, true>), grid, dim3(256), 0, c->stream, a);                          \
     } else {                                                                                                 \
       hipLaunchKernelGGL((k_draw_scan<E, true, false>), grid, dim3(256), 0, c->stream, a);                   \
+      if (plan_first(E)) hipLaunchKernelGGL((k_draw_plan<false>), rows_grid, dim3(256), 0, c->stream, a);    \
       hipLaunchKernelGGL((k_draw_list<E, false>), grid, dim3(256), 0, c->stream, a);                         \
     }                                                                                                        \
     hipLaunchKernelGGL((k_draw_pick<true, E>), rows_grid, dim3(pick_threads(true, E)), 0, c->stream, a, unit);                      \
