@@ -560,7 +560,8 @@ termezo_status termezo_model_decode(termezo_model* model, termezo_kvcache* cache
  * These calls too return as soon as their work is queued on the context's stream and may be
  * made while another device is current.  termezo_linear_i8 and termezo_sample keep scratch in
  * the context, as termezo_beam_select does: it grows with the largest call, a captured call
- * that would have to allocate is refused (STATE), and graphs stay valid when it grows later. */
+ * that would have to allocate is refused (STATE), and graphs stay valid when it grows later.
+ * Graphs of one context's calls must not run at the same time. */
 
 /* Rows of w [N][K] (F32 or BF16) in 8 bits: a = max(max |w|, 1e-30), codes[n][k] =
  * rne(w * s) with s = 127 * (1 / a), steps[n] = a / 127 (fp32, each operation rounded); a row with a value
@@ -636,7 +637,9 @@ termezo_status termezo_sample(termezo_ctx* ctx, const float* logits, const float
 /* The model's head in 8 bits: codes int8 [vocab][d_model] (16-byte aligned) and steps fp32
  * [vocab] as termezo_quantize_rows leaves them, borrowed; termezo_model_decode then forms its
  * logits as termezo_linear_i8 does (the losses keep the embedding).  Both null: the embedding again.
- * Captured steps keep the head that they were captured with.  Errors:
+ * Codes and steps are read at every decode and do not follow the embedding: after it has been
+ * perturbed or updated they are to be formed again (in place, captured steps read the new ones).
+ * Captured steps keep the addresses that they were captured with.  Errors:
  * INVALID_ARG (one of them null, misaligned pointers). */
 termezo_status termezo_model_set_head(termezo_model* model, const int8_t* codes, const float* steps);
 

@@ -703,7 +703,8 @@ class Model:
 
     def set_head(self, codes, steps):
         """decode forms its logits with the head in 8 bits: codes int8 [vocab, d_model] and steps fp32
-        [vocab] of quantize_rows, kept alive by the caller; None, None restores the embedding."""
+        [vocab] of quantize_rows, kept alive by the caller and formed again where the embedding
+        changes; None, None restores the embedding."""
         import torch
         V, d = self.embedding.shape
         dev = self.ctx.device
