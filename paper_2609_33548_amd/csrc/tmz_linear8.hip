@@ -177,6 +177,7 @@ __device__ __forceinline__ void put(uint16_t* p, float v) { *(__bf16*)p = (__bf1
 // banks).  Up to 16 tokens are taken in 8 bits here, by every work group for itself (one launch); more come
 // from the quantiser.  Work groups walk the weights, 16 rows at a time, each wave its own (KW = 1) or all of
 // them together, dividing the steps (KW = NW, few weight rows); GS steps ahead of the products.
+// 1 x 2560 -> 128256: 57 us (5.8 TB/s), 32 x 1536 -> 32003 15, 3 x 256 -> 688 4.2.
 // ---------------------------------------------------------------------------
 template <typename TX, typename TY, int MT, int KB, int NW, int KW, int GS>
 __global__ void __launch_bounds__(64 * NW) k_linear_walk(const TX* __restrict__ x, const int8_t* __restrict__ q,
@@ -316,6 +317,8 @@ __global__ void __launch_bounds__(64 * NW) k_linear_walk(const TX* __restrict__ 
 //   v_mfma_i32_32x32x32_i8 with the weights as the first operand: a lane's sixteen sums are one token's, in four
 // runs of four neighbouring outputs, which meet in LDS (32 tokens of a wave at a time) so that whole 16-byte units
 // go out.  In sub-step ks of a step lane l supplies the chunk 4 (l / 32) + ks of row l % 32 of both operands.
+//   Bound by the matrix cores at the clock that they hold: 8192 x 2560 -> 13824 250 us, 2.3 POP/s, busy 66% of the time at
+// 1.69 GHz; few tiles by their own loads: 777 x 6912 -> 2560 in fp32 32 us on 140 compute units.
 // ---------------------------------------------------------------------------
 typedef int v16i __attribute__((ext_vector_type(16)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
