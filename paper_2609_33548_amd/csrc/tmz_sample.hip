@@ -42,18 +42,18 @@ __device__ __forceinline__ int rule_line(const int32_t* index, int lines, int ro
   return -1;
 }
 
-// A slice of a row, 4 * E values of a thread: raw[i].v[j] at t0 + 1024 i + 4 tid + j; `none` behind the row's end.
-template <int E>
+// A slice of a row, 4 * E values of a thread: raw[i].v[j] at t0 + PASS i + 4 tid + j; `none` behind the row's end.
+template <int E, int PASS = 1024>
 __device__ __forceinline__ void slice_fetch(const float* row, int t0, int V, int tid, float none, Four raw[E]) {
   const uint32_t at = (uint32_t)t0 + 4u * tid;
-  if (t0 + 1024 * E <= V) {                              // whole work group
+  if (t0 + PASS * E <= V) {                              // whole work group
 #pragma unroll
-    for (int i = 0; i < E; ++i) raw[i] = *(const Four*)(row + (at + 1024u * i));
+    for (int i = 0; i < E; ++i) raw[i] = *(const Four*)(row + (at + (uint32_t)PASS * i));
     return;
   }
 #pragma unroll
   for (int i = 0; i < E; ++i) {
-    const uint32_t t = at + 1024u * i;
+    const uint32_t t = at + (uint32_t)PASS * i;
     raw[i] = Four{{none, none, none, none}};
     if (t + 4u <= (uint32_t)V) {
       raw[i] = *(const Four*)(row + t);
@@ -168,9 +168,9 @@ __global__ void __launch_bounds__(256) k_adjust(RuleArgs a) {
 // it goes through the row in the list's place.
 // Without limits the first and the last are enough.
 // The scan is bound by vector instructions (an exponential in fp64 and a bin a logit) beside its reads, the list by
-// its reads, the plan and the pick by their chains of barriers: 64 x 128256 with top_p 14.5 + 6.0 + 12.8 + 20.4 us (the logits
+// its reads, the plan and the pick by their chains of barriers: 64 x 128256 with top_p 14.3 + 6.0 + 12.3 + 19.5 us (the logits
 // alone at the rate of a copy: 6.4), one row of 32003 with top_k and top_p 3.9 + 8.4 + 9.1, 256 x 32000 without
-// limits 11 + 6.8.
+// limits 11 + 5.0.
 // ---------------------------------------------------------------------------
 constexpr int kBins = 256, kMaxDrawRows = 1024, kList = 8192;
 constexpr bool plan_first(int E) { return E > 2; }       // long slices: plans in a launch of their own
@@ -674,24 +674,6 @@ __global__ void __launch_bounds__(256, 4) k_draw_list(DrawArgs a) {
     }
 }
 
-// Sums over the work group's threads up to and including this one's, in the order of threads.  parts must not be in
-// use; it is free again after the next barrier.
-template <int NW, typename T>
-__device__ __forceinline__ T group_scan(T v, T* parts, int tid, T& total) {
-  const int lane = tid & 63, wave = tid >> 6;
-  v = wave_scan(v);
-  if (lane == 63) parts[wave] = v;
-  __syncthreads();
-  T before = 0;
-  total = 0;
-#pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    if (w < wave) before += parts[w];
-    total += parts[w];
-  }
-  return v + before;
-}
-
 template <int NT>
 struct BorderShared {
   unsigned long long pm[NT], ull[3][NT / 64], before_mass;
@@ -704,7 +686,8 @@ template <int NT, typename K>
 __device__ __forceinline__ unsigned long long draw_border(const RowPlan& p, const Settings& s, double unit,
                                                           const double* roots, int n, K key_at, BorderShared<NT>& sh,
                                                           int tid) {
-  constexpr int NW = NT / 64;
+  // Keys at a time in a part's sums: the operations of four weights overlap, where lists are long
+  constexpr int NW = NT / 64, AT = NT >= 512 ? 4 : 1;
   const int lane = tid & 63, wave = tid >> 6;
   // the least key of bins first .. last and the greatest of bin limit; the greatest of all
   unsigned long long low = ~0ull, most = 0, high = 0;
@@ -782,12 +765,27 @@ __device__ __forceinline__ unsigned long long draw_border(const RowPlan& p, cons
       if (tid == 0) sh.part = INT32_MAX;
       __syncthreads();
 #pragma unroll 1
-      for (int i = tid; i < n; i += NT) {
-        const unsigned long long k = key_at(i);
-        if (!k || k < lo || k > hi) continue;
-        const int at = NT - 1 - (int)((k - lo) >> shift);      // falling
-        atomicAdd(&sh.pc[at], 1u);
-        if (!counting) atomicAdd(&sh.pm[at], draw_fix(draw_weight(key_logit(k), p.top, s.scale, roots), unit));
+      for (int i = tid; i < n; i += AT * NT) {
+        unsigned long long k[AT];
+        bool in[AT], any = false;
+#pragma unroll
+        for (int j = 0; j < AT; ++j) {
+          k[j] = i + j * NT < n ? key_at(i + j * NT) : 0ull;
+          in[j] = k[j] && k[j] >= lo && k[j] <= hi;
+          any |= in[j];
+        }
+        if (!any) continue;
+        unsigned long long w[AT];
+        if (!counting)
+#pragma unroll
+          for (int j = 0; j < AT; ++j) w[j] = draw_fix(draw_weight(key_logit(k[j]), p.top, s.scale, roots), unit);
+#pragma unroll
+        for (int j = 0; j < AT; ++j)
+          if (in[j]) {
+            const int at = NT - 1 - (int)((k[j] - lo) >> shift);       // falling
+            atomicAdd(&sh.pc[at], 1u);
+            if (!counting) atomicAdd(&sh.pm[at], w[j]);
+          }
       }
       __syncthreads();
       const unsigned long long m0 = sh.pm[tid], ms = wave_scan(m0);
@@ -830,6 +828,97 @@ __device__ __forceinline__ unsigned long long draw_border(const RowPlan& p, cons
   return least;
 }
 
+// The token among a slice's kept weights (raw: its logits from `from` on, pass after pass of four a thread; weight(x, t): 0 if it
+// is not kept): the first whose sum passes want, the last with any where rounding leaves none.  WHOLE: want is a
+// share of the slice's sum, whose logarithm is taken here; else log_kept is the logarithm of the row's kept weights.  Passes
+// stay a loop, and the waves' sums of all passes are gone through at once: one barrier, and code that is run
+// once is short (it comes from memory).  256 x 32000 without limits 16.2 -> 14.6 us, 512 x 1000 6.8 -> 4.7.
+template <int NT, int NP, bool WHOLE, typename F>
+__device__ __forceinline__ void draw_token(const DrawArgs& a, int row, const Four (&raw)[NP], int from, float top,
+                                           const Settings& s, float xb, double want, double log_kept, double* chunk,
+                                           int tid, F weight) {
+  constexpr int NW = NT / 64, PASS = 4 * NT;
+  static_assert(NP * NW <= 64, "a lane a sum");
+  const int lane = tid & 63, wave = tid >> 6;
+  double part[NP];
+#pragma unroll
+  for (int k = 0; k < NP; ++k) part[k] = 0.0;
+#pragma unroll 1
+  for (int i = 0; i < NP; ++i) {
+    Four f = raw[0];                                       // raw[i], without an index into registers
+#pragma unroll
+    for (int k = 1; k < NP; ++k)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f.v[j] = i == k ? raw[k].v[j] : f.v[j];
+    double w = 0.0;
+    const float most = fmaxf(fmaxf(f.v[0], f.v[1]), fmaxf(f.v[2], f.v[3]));
+    if (__ballot(draw_clean(most) >= xb))
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w += weight(draw_clean(f.v[j]), from + PASS * i + 4 * tid + j);
+#pragma unroll
+    for (int k = 0; k < NP; ++k) part[k] = i == k ? w : part[k];
+    w = wave_sum(w);
+    if (lane == 0) chunk[i * NW + wave] = w;
+  }
+  __syncthreads();
+  // the place up to which the sums pass want; before: what lies before it
+  auto place = [&](double w, double c, double& before) __attribute__((always_inline)) {
+    const unsigned long long over = __ballot(w > 0.0 && c > want), any = __ballot(w > 0.0);
+    const int at = over ? __ffsll((long long)over) - 1 : any ? 63 - __clzll((long long)any) : -1;
+    before = __shfl(c - w, max(at, 0), 64);
+    return at;
+  };
+  const double w = lane < NP * NW ? chunk[lane] : 0.0, c = wave_scan(w);
+  if (WHOLE) {
+    const double all = last_lane(c);
+    want *= all;
+    log_kept = ln_of(all);
+  }
+  double before;
+  const int at = __builtin_amdgcn_readfirstlane(place(w, c, before));
+  if (at < 0) {                                            // cannot be: the slice has weight
+    if (tid == 0) a.tokens[row] = from;
+    return;
+  }
+  if (wave != at % NW) return;
+  Four f = raw[0];
+  double mine = part[0];
+#pragma unroll
+  for (int i = 1; i < NP; ++i) {
+    const bool it = i == at / NW;
+    mine = it ? part[i] : mine;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f.v[j] = it ? raw[i].v[j] : f.v[j];
+  }
+  want -= before;
+  const int who = place(mine, wave_scan(mine), before);
+  if (lane != who) return;
+  const int t0 = from + PASS * (at / NW) + 4 * tid;
+  double sum = before;
+  int token = -1, last = t0;
+  float x = 0.0f, last_x = 0.0f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float v = draw_clean(f.v[j]);
+    const double one = weight(v, t0 + j);
+    sum += one;
+    if (one > 0.0) {
+      last = t0 + j;
+      last_x = v;
+      if (sum > want && token < 0) {
+        token = last;
+        x = v;
+      }
+    }
+  }
+  if (token < 0) {
+    token = last;
+    x = last_x;
+  }
+  a.tokens[row] = token;
+  if (a.logprobs) a.logprobs[row] = s.best ? 0.0f : (float)(((double)x - (double)top) * s.inv_t - log_kept);
+}
+
 constexpr int kMaxSlices = 2048;
 
 // What bounds a row is its chain of barriers, so short slices take few waves (one row of 32003: 9.0 us, 10.3 with 512 threads
@@ -838,13 +927,13 @@ constexpr int pick_threads(bool limits, int E) { return limits && E > 2 ? 512 : 
 
 template <bool LIMITS, int E>
 __global__ void __launch_bounds__(pick_threads(LIMITS, E)) k_draw_pick(DrawArgs a, int unit_bits) {
-  constexpr int NT = pick_threads(LIMITS, E), NW = NT / 64, SLICE = 1024 * E, EACH = SLICE / NT;
+  constexpr int NT = pick_threads(LIMITS, E), NW = NT / 64, SLICE = 1024 * E;
   __shared__ unsigned long long keys[LIMITS ? kList : 1], add[LIMITS ? kMaxSlices : 1];
   __shared__ BorderShared<LIMITS ? NT : 64> sh;
-  __shared__ double dbl[NW];
+  __shared__ double chunk[SLICE / 256];
   __shared__ float tops[NW];
-  __shared__ int slice_at, hit, last_kept;
-  __shared__ double before_slice, all_kept, log_kept;
+  __shared__ int slice_at;
+  __shared__ double before_slice, all_kept;
   __shared__ double roots[kRootCount];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = blockIdx.x, V = a.vocab;
   if (tid < kRootCount) roots[tid] = kRoots[tid];
@@ -967,91 +1056,40 @@ __global__ void __launch_bounds__(pick_threads(LIMITS, E)) k_draw_pick(DrawArgs 
       slice_at = max(found, 0);
       before_slice = before;
       all_kept = run;
-      hit = INT32_MAX;
-      last_kept = -1;
     }
   }
   __syncthreads();
-  // the token in that slice: every thread EACH logits in a row
-  const double want = (double)u * all_kept - before_slice;
-  const int from = slice_at * SLICE, t0 = from + EACH * tid;
-  double w[EACH], mine = 0.0;
-  int last = -1;
-  if (from + SLICE <= V) {
-    constexpr int VW = EACH < 4 ? EACH : 4;
-    Floats<VW> f[EACH / VW];
-#pragma unroll
-    for (int j = 0; j < EACH / VW; ++j) f[j] = *(const Floats<VW>*)(x + t0 + VW * j);
-#pragma unroll
-    for (int j = 0; j < EACH; ++j) w[j] = f[j / VW].v[j % VW];
-  } else {
-#pragma unroll
-    for (int j = 0; j < EACH; ++j) {
-      const float v = x[t0 + j < V ? t0 + j : V - 1];
-      w[j] = t0 + j < V ? v : -INFINITY;
-    }
-  }
-#pragma unroll
-  for (int j = 0; j < EACH; ++j) {
-    const float v = draw_clean((float)w[j]);
-    w[j] = kept(v, t0 + j) ? draw_weight(v, p.top, s.scale, roots) : 0.0;
-    mine += w[j];
-    if (w[j] > 0.0) last = t0 + j;
-  }
-  if (tid == NT - 1) log_kept = ln_of(all_kept);           // beside the others' weights
-  double total;
-  const double upto = group_scan<NW>(mine, dbl, tid, total);
-  double c = upto - mine;
-  int at = -1;
-  if (mine > 0.0 && upto > want) {
-#pragma unroll
-    for (int j = 0; j < EACH; ++j) {
-      c += w[j];
-      if (w[j] > 0.0 && c > want && at < 0) at = t0 + j;
-    }
-    if (at >= 0) atomicMin(&hit, at);
-  }
-  if (total <= want && last >= 0) atomicMax(&last_kept, last);         // rounding leaves none: the last one
-  __syncthreads();
-  if (hit == INT32_MAX && last >= 0 && last == last_kept) at = hit = last;
-  if (tid == 0 && hit == INT32_MAX && last_kept < 0) a.tokens[row] = from;      // cannot be: the slice has weight
-  if (at >= 0 && at == hit) {
-    a.tokens[row] = at;
-    if (a.logprobs) a.logprobs[row] = s.best ? 0.0f : (float)(((double)draw_clean(x[at]) - (double)p.top) * s.inv_t - log_kept);
-  }
+  // the token in that slice
+  const int from = slice_at * SLICE;
+  Four raw[SLICE / (4 * NT)];
+  slice_fetch<SLICE / (4 * NT), 4 * NT>(x, from, V, tid, -INFINITY, raw);
+  __builtin_amdgcn_sched_barrier(0);
+  const double log_kept = ln_of(all_kept);                 // while they are on their way
+  draw_token<NT, SLICE / (4 * NT), false>(a, row, raw, from, p.top, s, xb, (double)u * all_kept - before_slice, log_kept,
+                                          chunk, tid, [&](float v, int k) __attribute__((always_inline)) {
+                                            return kept(v, k) ? draw_weight(v, p.top, s.scale, roots) : 0.0;
+                                          });
 }
 
 // The whole draw of a row of up to 4 NT E logits by one work group, which holds them in registers: the same steps with
-// the row for a slice, one launch and no memory in between: 512 rows of 1000 47 -> 14 us, one row of 1000 19 -> 11.5, 256 of
-// 8192 27 -> 21; from 16384 on the slices are faster (one row 20 against 27 us).  Few waves, for the barriers.
+// the row for a slice, one launch and no memory in between: 512 rows of 1000 47 -> 13 us, one row of 1000 19 -> 10.5, 256 of
+// 8192 27 -> 20; from 16384 on the slices are faster (one row 20 against 27 us).  Few waves, for the barriers.
 template <bool LIMITS, bool COUNT, int NT, int E>
 __global__ void __launch_bounds__(NT) k_draw_row(DrawArgs a, int unit_bits) {
   constexpr int NW = NT / 64, PASS = 4 * NT;
   __shared__ unsigned long long keys[LIMITS ? PASS * E : 1], bins[LIMITS ? kCopies * kBins : 1];
   __shared__ uint32_t counts[COUNT ? kCopies * kBins : 1];
   __shared__ BorderShared<LIMITS ? NT : 64> sh;
-  __shared__ double mass[kBins], dbl[NW], chunk[E][NW], roots[kRootCount];
+  __shared__ double mass[kBins], chunk[E * NW], roots[kRootCount];
   __shared__ int count[kBins];
   __shared__ float tops[NW], edges[4];
   __shared__ RowPlan plan;
-  __shared__ int n_list, chunk_at, hit, last_kept;
-  __shared__ double before_chunk, all_kept, log_kept;
+  __shared__ int n_list;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = blockIdx.x, V = a.vocab;
   if (tid < kRootCount) roots[tid] = kRoots[tid];
   const float* x = a.logits + (int64_t)row * V;
-  Four raw[E];                                           // raw[i].v[j] at PASS i + 4 tid + j
-#pragma unroll
-  for (int i = 0; i < E; ++i) {
-    const uint32_t t = (uint32_t)PASS * i + 4u * tid;
-    raw[i] = Four{{-INFINITY, -INFINITY, -INFINITY, -INFINITY}};
-    if (t + 4u <= (uint32_t)V) {
-      raw[i] = *(const Four*)(x + t);
-    } else if (t < (uint32_t)V) {
-      raw[i].v[0] = x[t];
-      if (t + 1u < (uint32_t)V) raw[i].v[1] = x[t + 1u];
-      if (t + 2u < (uint32_t)V) raw[i].v[2] = x[t + 2u];
-    }
-  }
+  Four raw[E];
+  slice_fetch<E, PASS>(x, 0, V, tid, -INFINITY, raw);
   const Settings s = draw_settings(a, row);
   const double unit = (double)(1ull << unit_bits);
   float u = a.uniforms[row];
@@ -1074,11 +1112,7 @@ __global__ void __launch_bounds__(NT) k_draw_row(DrawArgs a, int unit_bits) {
     }
   top = wave_top(top);
   if (lane == 0) tops[wave] = top;
-  if (tid == 0) {
-    n_list = 0;
-    hit = INT32_MAX;
-    last_kept = -1;
-  }
+  if (tid == 0) n_list = 0;
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < NW; ++w) top = fmaxf(top, tops[w]);
@@ -1156,64 +1190,7 @@ __global__ void __launch_bounds__(NT) k_draw_row(DrawArgs a, int unit_bits) {
   auto weight = [&](float v, int t) __attribute__((always_inline)) {
     return v > xb || (v == xb && (uint32_t)t <= tb) ? draw_weight(v, top, s.scale, roots) : 0.0;
   };
-  // kept weights by pass and wave
-  double part[E];
-#pragma unroll
-  for (int i = 0; i < E; ++i) {
-    part[i] = 0.0;
-    const float most = fmaxf(fmaxf(raw[i].v[0], raw[i].v[1]), fmaxf(raw[i].v[2], raw[i].v[3]));
-    if (__ballot(most >= xb))
-#pragma unroll
-      for (int j = 0; j < 4; ++j) part[i] += weight(raw[i].v[j], PASS * i + 4 * tid + j);
-    const double w = wave_sum(part[i]);
-    if (lane == 0) chunk[i][wave] = w;
-  }
-  __syncthreads();
-  if (wave == 0) {
-    double w = 0.0;
-    if (lane < E)
-#pragma unroll
-      for (int k = 0; k < NW; ++k) w += chunk[lane][k];
-    const double c = wave_scan(w), all = last_lane(c), target = (double)u * all;
-    const unsigned long long over = __ballot(w > 0.0 && c > target), any = __ballot(w > 0.0);
-    const int at = over ? __ffsll((long long)over) - 1 : any ? 63 - __clzll((long long)any) : 0;
-    if (lane == at) {
-      chunk_at = at;
-      before_chunk = c - w;
-      all_kept = all;
-      log_kept = ln_of(all);
-    }
-  }
-  __syncthreads();
-  const int at_chunk = chunk_at;
-  const double want = (double)u * all_kept - before_chunk;
-  double mine = 0.0;
-#pragma unroll
-  for (int i = 0; i < E; ++i) mine = i == at_chunk ? part[i] : mine;
-  double total;
-  const double upto = group_scan<NW>(mine, dbl, tid, total);
-  const int t0 = PASS * at_chunk + 4 * tid;
-  int at = -1;
-  if (mine > 0.0 && (upto > want || total <= want)) {
-    double c = upto - mine;
-    int last = -1;
-    for (int j = 0; j < 4; ++j) {
-      const float v = t0 + j < V ? draw_clean(x[t0 + j]) : -INFINITY;
-      const double w = weight(v, t0 + j);
-      c += w;
-      if (w > 0.0) last = t0 + j;
-      if (w > 0.0 && c > want && at < 0) at = t0 + j;
-    }
-    if (at >= 0) atomicMin(&hit, at);
-    else if (last >= 0) atomicMax(&last_kept, last);     // where rounding leaves none: the last one
-  }
-  __syncthreads();
-  if (hit == INT32_MAX && t0 <= last_kept && last_kept < t0 + 4) at = last_kept;
-  if (at >= 0 && (at == hit || hit == INT32_MAX)) {
-    a.tokens[row] = at;
-    if (a.logprobs)
-      a.logprobs[row] = s.best ? 0.0f : (float)(((double)draw_clean(x[at]) - (double)top) * s.inv_t - log_kept);
-  }
+  draw_token<NT, E, true>(a, row, raw, 0, top, s, xb, (double)u, 0.0, chunk, tid, weight);
 }
 
 }  // namespace tmz
