@@ -112,6 +112,31 @@ def test_product(ctx, kind, M, K, N):
         assert (err <= tol).all(), (m, float(err.max()), int((err / tol).argmax()))
 
 
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("M,K,N", [(640, 144, 27003), (300, 48, 60001), (2049, 32, 8200), (40, 64, 420001)])
+def test_product_of_large_outputs(ctx, bf16, M, K, N):
+    """Outputs of 32 MB and more, rows that begin at any multiple of their type; every value."""
+    torch = _torch()
+    from oracle import next_token_ref as ref
+    rng = np.random.default_rng(M + K + N)
+    x = rng.standard_normal((M, K)) * 10.0 ** rng.integers(-2, 3, (M, 1))
+    codes = torch.from_numpy(rng.integers(-128, 128, (N, K), dtype=np.int64).astype(np.int8)).cuda()
+    steps = torch.from_numpy((rng.random(N) * 1e-3).astype(F)).cuda()
+    x, xd = _typed(x, False)
+    out = torch.full((M * N + 64,), 77.0, dtype=torch.bfloat16 if bf16 else torch.float32, device="cuda")
+    assert out.numel() * out.element_size() >= 32 << 20
+    ctx.linear_i8(xd, codes, steps, out[:M * N].view(M, N))
+    assert (out[M * N:] == 77.0).all()
+    pairs = [ref.quantise(r, 1e-5) for r in x]
+    q = torch.from_numpy(np.stack([p for p, _ in pairs]).astype(np.float64)).cuda()
+    d = torch.tensor([float(v) for _, v in pairs], dtype=torch.float64, device="cuda")
+    for m in range(0, M, 64):
+        want = q[m:m + 64] @ codes.double().t().contiguous() * d[m:m + 64, None] * steps.double()
+        got = out[:M * N].view(M, N)[m:m + 64].double()
+        tol = ((2.0 ** -8 if bf16 else 0.0) + 3.0 * 2.0 ** -24 * 1.01) * want.abs() + 1e-40
+        assert ((got - want).abs() <= tol).all(), m
+
+
 def test_product_of_quantised_rows_is_near_the_real_one(ctx):
     """The two calls as they are used: half a step on each side of every product."""
     torch = _torch()
