@@ -549,24 +549,26 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), BPC * (BM / WM) * 
 
 // What a launch of T tiles takes on cu compute units (us): the first tile of a compute unit c0 + l K, further ones a + b K
 // each (K in thousands), where T is no multiple of cu the last, partial round counts half of its share and half of a
-// whole one.  Fitted to eight weights at 40 to 8192 tokens (rms 6 to 11%); the tile with the least estimate is within 2%
-// of the best on average, 15% at worst.
+// whole one.  Fitted to nine weights at 40 to 8192 tokens (rms 9 to 14%); the tile with the least estimate is within 1%
+// of the best on average, 11% at worst.
 struct LinearCost {
   int bm, bn;
   float c0, l, a, b;
 };
-constexpr LinearCost kLinearBf16[4] = {{256, 256, 7.00f, 8.44f, 0.00f, 16.94f}, {128, 256, 5.75f, 5.25f, 1.73f, 8.53f},
-                                       {128, 128, 5.03f, 3.41f, 2.41f, 4.31f}, {64, 64, 4.93f, 2.06f, 0.37f, 1.45f}};
-constexpr LinearCost kLinearF32[4] = {{256, 256, 8.18f, 8.50f, 1.35f, 20.08f}, {128, 256, 6.33f, 5.46f, 4.55f, 8.27f},
-                                      {128, 128, 5.31f, 3.43f, 3.39f, 4.16f}, {64, 64, 4.83f, 2.19f, 0.58f, 1.42f}};
+constexpr LinearCost kLinearBf16[4] = {{256, 256, 6.85f, 8.95f, 6.65f, 16.06f}, {128, 256, 5.56f, 5.71f, 2.18f, 9.58f},
+                                       {128, 128, 4.92f, 3.53f, 1.99f, 5.12f}, {64, 64, 4.67f, 1.96f, 0.36f, 1.68f}};
+constexpr LinearCost kLinearF32[4] = {{256, 256, 8.23f, 9.05f, 38.11f, 6.72f}, {128, 256, 6.35f, 5.79f, 12.85f, 6.77f},
+                                      {128, 128, 5.18f, 3.68f, 4.02f, 4.96f}, {64, 64, 4.62f, 2.10f, 0.70f, 1.68f}};
 
 template <typename TY>
 static void linear_tiles(const int8_t* q, const float* xstep, const int8_t* codes, const float* steps, int64_t M,
                          int64_t K, int64_t N, TY* out, int n_cu, hipStream_t s) {
   auto count = [&](int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
-  // An output of more than the eight L2s hold (4 MB each) goes past them and leaves them to the matrices:
-  // 8192 x 2560 -> 13824 295 -> 251 us, 8192 x 6912 -> 2560 180 -> 154.
-  const bool past = M * N * (int64_t)sizeof(TY) >= int64_t(32) << 20;
+  // An output of more than the eight L2s hold (4 MB each) goes past them and leaves them to the matrices, where whole
+  // 128-byte lines do: 8192 x 2560 -> 13824 295 -> 251 us, 8192 x 6912 -> 2560 180 -> 154 (rows that begin inside
+  // lines, 389 x 1536 -> 32003 in fp32: 36 -> 57).
+  const bool past = M * N * (int64_t)sizeof(TY) >= int64_t(32) << 20 && N * (int64_t)sizeof(TY) % 128 == 0 &&
+                    (reinterpret_cast<uintptr_t>(out) & 127) == 0;
   int best = 0;
   float least = 0.0f;
   for (int t = 0; t < 4; ++t) {

@@ -113,7 +113,8 @@ def test_product(ctx, kind, M, K, N):
 
 
 @pytest.mark.parametrize("bf16", [True, False])
-@pytest.mark.parametrize("M,K,N", [(640, 144, 27003), (300, 48, 60001), (2049, 32, 8200), (40, 64, 420001)])
+@pytest.mark.parametrize("M,K,N", [(640, 144, 27003), (300, 48, 60001), (2049, 32, 8200), (40, 64, 420001),
+                                   (700, 96, 24064), (2048, 512, 13824)])
 def test_product_of_large_outputs(ctx, bf16, M, K, N):
     """Outputs of 32 MB and more, rows that begin at any multiple of their type; every value."""
     torch = _torch()
