@@ -440,11 +440,13 @@ inline termezo_status scratch_for(termezo_ctx* c, Scratch& x, int64_t need, cons
   return TERMEZO_OK;
 }
 
-// Products with 8-bit weights.  scratch: linear_i8_scratch(M, K) bytes for the codes and steps of x.
+// Products with 8-bit weights.  scratch: linear_i8_scratch(M, K) bytes for the codes and steps of x (16-byte aligned);
+// with linear_i8_parts more, a long sum over few tokens is split (the same result sooner).
 int64_t linear_i8_scratch(int64_t M, int64_t K);
+int64_t linear_i8_parts(int64_t M, int64_t K, int64_t N, int n_cu);
 hipError_t launch_linear_i8(const void* x, termezo_dtype xdt, int64_t M, int64_t K, const int8_t* codes,
                             const float* steps, int64_t N, void* out, termezo_dtype ydt, void* scratch,
-                            int n_cu, hipStream_t s);
+                            int64_t bytes, int n_cu, hipStream_t s);
 
 // The cache's calls on a stream of the caller's choice (checked arguments).
 hipError_t cache_append_on(termezo_kvcache* c, int layer, const void* k, const void* v, int64_t n,

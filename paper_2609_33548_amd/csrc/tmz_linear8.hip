@@ -325,10 +325,12 @@ typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
 typedef uint32_t Unit __attribute__((ext_vector_type(4), aligned(2)));  // 16 bytes of a row that may begin anywhere
 
-template <typename TY, int BM, int BN, int WM, int WN, int NST, int BPC, bool PAST>
+// SPLIT (TY float): a tile's steps are dealt to `splits` work groups, whose sums go to out [splits][stride] as they are.
+template <typename TY, int BM, int BN, int WM, int WN, int NST, int BPC, bool PAST, bool SPLIT>
 __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), BPC * (BM / WM) * (BN / WN) / 4)
     k_linear_tile(const int8_t* __restrict__ q, const float* __restrict__ xstep, const int8_t* __restrict__ codes,
-                  const float* __restrict__ steps, int64_t M, int64_t K, int64_t N, TY* __restrict__ out) {
+                  const float* __restrict__ steps, int64_t M, int64_t K, int64_t N, TY* __restrict__ out, int splits,
+                  int64_t stride) {
   constexpr int BK = kPitch, NW = (BM / WM) * (BN / WN), TM = WM / 32, TN = WN / 32, STAGE = (BM + BN) * BK;
   constexpr int CH = BK / 16, RPL = 64 / CH, KS = BK / 32;            // chunks a row, rows a direct load, sub-steps
   constexpr int AJ = BM / RPL / NW, BJ = BN / RPL / NW, DJ = AJ + BJ;  // direct loads of a wave and step
@@ -338,8 +340,12 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), BPC * (BM / WM) * 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wm = wave / (BN / WN), wn = wave % (BN / WN);
   const int64_t pitch = pitch_of(K);
-  const uint32_t nb_m = (uint32_t)((M + BM - 1) / BM), nb_n = (uint32_t)((N + BN - 1) / BN), tiles = nb_m * nb_n;
+  const uint32_t nb_m = (uint32_t)((M + BM - 1) / BM), nb_n = (uint32_t)((N + BN - 1) / BN);
+  const uint32_t tiles = nb_m * nb_n * (SPLIT ? splits : 1);
   const int nk = (int)((K + BK - 1) / BK);
+  // steps of a tile (of its part t % splits, at least one): from, up to
+  auto from_step = [&](uint32_t t) __attribute__((always_inline)) { return SPLIT ? (int)(t % splits) * nk / splits : 0; };
+  auto to_step = [&](uint32_t t) __attribute__((always_inline)) { return SPLIT ? ((int)(t % splits) + 1) * nk / splits : nk; };
   // This work group's tiles: every XCD takes a contiguous part of the order (groups of kGroupM tile rows, so that the
   // tiles at work on it share rows of both operands in its L2), its work groups take that in turn
   const uint32_t xcd = blockIdx.x % kXcd, groups = (gridDim.x - xcd + kXcd - 1) / kXcd;
@@ -347,6 +353,7 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), BPC * (BM / WM) * 
   uint32_t at = part0 + blockIdx.x / kXcd;
   if (at >= part1) return;
   auto place = [&](uint32_t t, int64_t& m, int64_t& n) __attribute__((always_inline)) {
+    if (SPLIT) t /= splits;
     const uint32_t span = kGroupM * nb_n, g = t / span, in = t - g * span, gm = min((uint32_t)kGroupM, nb_m - g * kGroupM);
     m = (int64_t)(g * kGroupM + in % gm) * BM;
     n = (int64_t)(in / gm) * BN;
@@ -406,11 +413,13 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), BPC * (BM / WM) * 
   static_assert(NW * 32 * RB <= STAGE, "outputs of the waves in a stage");
   // The steps of all the work group's tiles are one stream: NST - 1 of them are on their way, across the tiles' ends
   uint32_t ahead = at;                                   // the tile whose steps are being loaded, its next step
-  int ahead_k = 0, into = 0, flying = 0;
+  int ahead_k = from_step(at), into = 0, flying = 0;
+  bool fresh = true;                                     // none of its steps yet
   auto load = [&]() __attribute__((always_inline)) {
     if (ahead >= part1) return;
-    if (ahead_k == 0) {
+    if (fresh) {
       int64_t m, n;
+      fresh = false;
       place(ahead, m, n);
       arsrc = buffer_of(q + m * pitch, (uint32_t)(min((int64_t)BM, (M - m + 7) / 8 * 8) * pitch));
       brsrc = buffer_of(codes + n * K, (uint32_t)(min((int64_t)BN, N - n) * K));
@@ -418,9 +427,10 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), BPC * (BM / WM) * 
     issue(ahead_k, into);
     into = into == NST - 1 ? 0 : into + 1;
     ++flying;
-    if (++ahead_k == nk) {
-      ahead_k = 0;
+    if (++ahead_k == to_step(ahead)) {
       ahead += groups;
+      ahead_k = from_step(ahead);
+      fresh = true;
     }
   };
   // the oldest step on its way has landed; NST - 2 later ones may be on theirs
@@ -441,7 +451,8 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), BPC * (BM / WM) * 
       for (int a = 0; a < TM; ++a)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[b][a][r] = 0;
-    for (int kt = 0; kt < nk; ++kt) {
+    const int here = to_step(at) - from_step(at);
+    for (int kt = 0; kt < here; ++kt) {
       const int next = cur == NST - 1 ? 0 : cur + 1;
       load();                                            // into the stage that every wave had read before the last barrier
 #pragma unroll
@@ -467,7 +478,7 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), BPC * (BM / WM) * 
       }
       products((KS - 1) & 1);
       __builtin_amdgcn_sched_barrier(0);
-      if (kt + 1 < nk) cur = next;
+      if (kt + 1 < here) cur = next;
     }
     // outputs, through the stage that was just read
     int8_t* stage = lds + cur * STAGE + wave * 32 * RB;
@@ -477,7 +488,7 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), BPC * (BM / WM) * 
 #pragma unroll
     for (int a = 0; a < TM; ++a) {
       const int64_t m = mw + 32 * a + n32;
-      d[a] = xstep[m < M ? m : M - 1];
+      d[a] = SPLIT ? 0.0f : xstep[m < M ? m : M - 1];
     }
 #pragma unroll
     for (int c0 = 0; c0 < WN; c0 += SC) {
@@ -487,7 +498,10 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), BPC * (BM / WM) * 
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           const int64_t n = nw + c0 + 32 * b + 8 * g + 4 * h;          // four outputs from here on
-          if (n + 3 < N) {
+          if (SPLIT) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) st[b][g][r] = 0.0f;
+          } else if (n + 3 < N) {
             const Steps f = *(const Steps*)(steps + n);
 #pragma unroll
             for (int r = 0; r < 4; ++r) st[b][g][r] = f.v[r];
@@ -505,7 +519,10 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), BPC * (BM / WM) * 
             const int col = 32 * b + 8 * g + 4 * h;
             float v[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] = (float)acc[c0 / 32 + b][a][4 * g + r] * (d[a] * st[b][g][r]);
+            for (int r = 0; r < 4; ++r) {
+              const int sum = acc[c0 / 32 + b][a][4 * g + r];
+              v[r] = SPLIT ? __int_as_float(sum) : (float)sum * (d[a] * st[b][g][r]);
+            }
             int8_t* to = stage + n32 * RB + 16 * ((col / UB) ^ (n32 % UPR)) + (col % UB) * (int)sizeof(TY);
             if constexpr (sizeof(TY) == 2)
               *(uint2*)to = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
@@ -524,7 +541,7 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), BPC * (BM / WM) * 
           const int c = 64 * i + lane, row = c / UPR, u = c % UPR;
           const int64_t mo = mw + 32 * a + row, no = nw + c0 + u * UB;
           if (mo >= M || no >= N) continue;
-          TY* p = out + mo * N + no;
+          TY* p = out + (SPLIT ? (int64_t)(at % splits) * stride : 0) + mo * N + no;
           if (no + UB <= N) {
             if (PAST) __builtin_nontemporal_store(o[i], (Unit*)p);
             else *(Unit*)p = o[i];
@@ -560,10 +577,71 @@ constexpr LinearCost kLinearBf16[4] = {{256, 256, 6.85f, 8.95f, 6.65f, 16.06f}, 
 constexpr LinearCost kLinearF32[4] = {{256, 256, 8.23f, 9.05f, 38.11f, 6.72f}, {128, 256, 6.35f, 5.79f, 12.85f, 6.77f},
                                       {128, 128, 5.18f, 3.68f, 4.02f, 4.96f}, {64, 64, 4.62f, 2.10f, 0.70f, 1.68f}};
 
+// The parts' sums [splits][stride] together: out as above, four values a lane (in a row or from one to the next).
+template <typename TY>
+__global__ void __launch_bounds__(256) k_linear_join(const int* __restrict__ parts, int splits, int64_t stride,
+                                                     const float* __restrict__ xstep, const float* __restrict__ steps,
+                                                     uint32_t N, uint32_t total, TY* __restrict__ out) {
+  const uint32_t e = 4 * (blockIdx.x * 256 + threadIdx.x);
+  if (e >= total) return;
+  v4i sum = *(const v4i*)(parts + e);                    // stride is a multiple of 4
+  for (int p = 1; p < splits; ++p) sum += *(const v4i*)(parts + p * stride + e);
+  uint32_t m = e / N, n = e - m * N;
+  float v[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    v[j] = e + j < total ? (float)sum[j] * (xstep[m] * steps[n]) : 0.0f;
+    if (++n == N) {
+      n = 0;
+      ++m;
+    }
+  }
+  if (e + 4 <= total) {
+    if constexpr (sizeof(TY) == 4) *(float4*)(out + e) = make_float4(v[0], v[1], v[2], v[3]);
+    else *(uint2*)(out + e) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (e + j < total) put(out + e + j, v[j]);
+  }
+}
+
+static int64_t split_stride(int64_t M, int64_t N) { return (M * N + 3) / 4 * 4; }
+
+// Parts of K that few tokens' tiles of 64 x 64 are dealt out in (1: none), where the tiles leave compute units idle
+// through long sums; the sums are exact, so that the result does not depend on it.  6912 -> 2560: 40 tokens 20.5 us,
+// 7.8 + 3.8 in six parts, 100 tokens 20.6 and 12.0 + 3.9, from 200 on none; 4096 -> 1536: 40 tokens 13.4, 5.1 + 4.6.
+static int splits_of(int64_t M, int64_t K, int64_t N, int n_cu) {
+  const int64_t T = ((M + 63) / 64) * ((N + 63) / 64), nk = (K + kPitch - 1) / kPitch;
+  int best = 1;
+  float least = 4.6f + 2.0f * 1e-3f * (float)K;
+  if (T > n_cu) return 1;
+  for (int S = 2; S <= 8 && S * 4 <= nk; ++S) {
+    const float k = 1e-3f * (float)K / (float)S, r = (float)(T * S) / (float)n_cu;
+    const float more = 0.5f * (float)((T * S + n_cu - 1) / n_cu - 1) + (r > 1.0f ? 0.5f * (r - 1.0f) : 0.0f);
+    const float cost = 4.6f + 2.0f * k + more * (0.4f + 1.7f * k) + 4.0f + (float)((S + 1) * M * N * 4) * 0.33e-6f;
+    if (cost < least) {
+      best = S;
+      least = cost;
+    }
+  }
+  return best;
+}
+
 template <typename TY>
 static void linear_tiles(const int8_t* q, const float* xstep, const int8_t* codes, const float* steps, int64_t M,
-                         int64_t K, int64_t N, TY* out, int n_cu, hipStream_t s) {
+                         int64_t K, int64_t N, TY* out, float* parts, int64_t room, int n_cu, hipStream_t s) {
   auto count = [&](int bm, int bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
+  const int splits = splits_of(M, K, N, n_cu);
+  const int64_t stride = split_stride(M, N);
+  if (splits > 1 && splits * stride * 4 <= room) {
+    hipLaunchKernelGGL((k_linear_tile<float, 64, 64, 32, 32, 3, 3, false, true>),
+                       dim3((unsigned)std::min<int64_t>(count(64, 64) * splits, 3 * (int64_t)n_cu)), dim3(256), 0, s, q, xstep,
+                       codes, steps, M, K, N, parts, splits, stride);
+    hipLaunchKernelGGL((k_linear_join<TY>), dim3((unsigned)((stride / 4 + 255) / 256)), dim3(256), 0, s, (const int*)parts,
+                       splits, stride, xstep, steps, (uint32_t)N, (uint32_t)(M * N), out);
+    return;
+  }
   // An output of more than the eight L2s hold (4 MB each) goes past them and leaves them to the matrices, where whole
   // 128-byte lines do: 8192 x 2560 -> 13824 295 -> 251 us, 8192 x 6912 -> 2560 180 -> 154 (rows that begin inside
   // lines, 389 x 1536 -> 32003 in fp32: 36 -> 57).
@@ -583,9 +661,9 @@ static void linear_tiles(const int8_t* q, const float* xstep, const int8_t* code
     }
   }
 #define TMZ_TILE(BM, BN, WM, WN, NST, BPC, PAST)                                                              \
-  hipLaunchKernelGGL((k_linear_tile<TY, BM, BN, WM, WN, NST, BPC, PAST>),                                           \
+  hipLaunchKernelGGL((k_linear_tile<TY, BM, BN, WM, WN, NST, BPC, PAST, false>),                                           \
                      dim3((unsigned)std::min<int64_t>(count(BM, BN), (int64_t)BPC * n_cu)),                   \
-                     dim3(64 * (BM / WM) * (BN / WN)), 0, s, q, xstep, codes, steps, M, K, N, out)
+                     dim3(64 * (BM / WM) * (BN / WN)), 0, s, q, xstep, codes, steps, M, K, N, out, 1, 0)
   switch (best) {
     case 0:
       if (past) TMZ_TILE(256, 256, 128, 64, 2, 1, true);
@@ -606,7 +684,11 @@ static bool walk_ok(int64_t M, int64_t K) { return M <= 32 && M * ((K + 63) / 64
 static bool walk_quantises(int64_t M, int64_t K) { return M <= 16 && walk_ok(M, K); }
 
 int64_t linear_i8_scratch(int64_t M, int64_t K) {
-  return walk_quantises(M, K) ? 0 : (M + 7) / 8 * 8 * pitch_of(K) + M * 4;
+  return walk_quantises(M, K) ? 0 : ((M + 7) / 8 * 8 * pitch_of(K) + M * 4 + 15) / 16 * 16;
+}
+int64_t linear_i8_parts(int64_t M, int64_t K, int64_t N, int n_cu) {
+  const int splits = walk_ok(M, K) ? 1 : splits_of(M, K, N, n_cu);
+  return splits > 1 ? splits * split_stride(M, N) * 4 : 0;
 }
 
 template <typename TX, typename TY>
@@ -629,7 +711,7 @@ static void linear_walk(const TX* x, const int8_t* q, const float* xstep, const 
 
 template <typename TY>
 static hipError_t linear_as(const void* x, termezo_dtype xdt, int64_t M, int64_t K, const int8_t* codes,
-                            const float* steps, int64_t N, TY* out, void* scratch, int n_cu, hipStream_t s) {
+                            const float* steps, int64_t N, TY* out, void* scratch, int64_t bytes, int n_cu, hipStream_t s) {
   if (walk_quantises(M, K)) {
     if (xdt == TERMEZO_BF16)
       linear_walk((const uint16_t*)x, nullptr, nullptr, codes, steps, M, K, N, out, n_cu, s);
@@ -644,16 +726,17 @@ static hipError_t linear_as(const void* x, termezo_dtype xdt, int64_t M, int64_t
   if (walk_ok(M, K))
     linear_walk((const void*)nullptr, q, xstep, codes, steps, M, K, N, out, n_cu, s);
   else
-    linear_tiles(q, xstep, codes, steps, M, K, N, out, n_cu, s);
+    linear_tiles(q, xstep, codes, steps, M, K, N, out, (float*)((char*)scratch + linear_i8_scratch(M, K)),
+                 bytes - linear_i8_scratch(M, K), n_cu, s);
   return hipGetLastError();
 }
 
 hipError_t launch_linear_i8(const void* x, termezo_dtype xdt, int64_t M, int64_t K, const int8_t* codes,
                             const float* steps, int64_t N, void* out, termezo_dtype ydt, void* scratch,
-                            int n_cu, hipStream_t s) {
+                            int64_t bytes, int n_cu, hipStream_t s) {
   if (ydt == TERMEZO_BF16)
-    return linear_as(x, xdt, M, K, codes, steps, N, (uint16_t*)out, scratch, n_cu, s);
-  return linear_as(x, xdt, M, K, codes, steps, N, (float*)out, scratch, n_cu, s);
+    return linear_as(x, xdt, M, K, codes, steps, N, (uint16_t*)out, scratch, bytes, n_cu, s);
+  return linear_as(x, xdt, M, K, codes, steps, N, (float*)out, scratch, bytes, n_cu, s);
 }
 
 }  // namespace tmz
@@ -705,9 +788,13 @@ termezo_status termezo_linear_i8(termezo_ctx* c, const void* x, termezo_dtype xd
     return refuse(c, "linear_i8: a size or a type is out of range");
   DeviceScope scope(c->device);
   if (scope.err != hipSuccess) return hip_status(c, scope.err, "linear_i8");
-  const termezo_status st = scratch_for(c, c->linear, linear_i8_scratch(M, K), "linear_i8");
+  // without room for the parts of a split a captured call does with what there is
+  int64_t need = linear_i8_scratch(M, K);
+  if (c->linear.cap < need || !capturing(c->stream)) need += linear_i8_parts(M, K, N, c->n_cu);
+  const termezo_status st = scratch_for(c, c->linear, need, "linear_i8");
   if (st != TERMEZO_OK) return st;
-  return hip_status(c, launch_linear_i8(x, xdt, M, K, codes, steps, N, out, ydt, c->linear.p, c->n_cu, c->stream),
+  return hip_status(c, launch_linear_i8(x, xdt, M, K, codes, steps, N, out, ydt, c->linear.p, c->linear.cap, c->n_cu,
+                                        c->stream),
                     "linear_i8");
 }
 

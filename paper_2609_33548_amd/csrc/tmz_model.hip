@@ -2476,7 +2476,7 @@ termezo_status termezo_model_decode(termezo_model* m, termezo_kvcache* kv, const
   chk(norm_rows(m, A.q, rows, nrm, 2 * cf.n_blocks, A, A.xf, false, s));
   if (m->head)
     chk(launch_linear_i8(A.xf, cf.act_dtype, rows, d, m->head, m->head_steps, cf.vocab, logits, TERMEZO_F32, A.xq,
-                         c->n_cu, s));
+                         linear_i8_scratch(rows, d), c->n_cu, s));
   else
     chk(launch_logits(A.xf, emb, cf.act_dtype, rows, d, cf.vocab, logits, c->n_cu, s));
   chk(cache_advance_on(kv, s));

@@ -152,6 +152,44 @@ def test_product_of_quantised_rows_is_near_the_real_one(ctx):
     assert ((out.double().cpu() - xd @ wd.t()).abs() <= tol * 1.01).all()
 
 
+def test_captured_product_without_room_for_a_split(ctx):
+    """A long sum over few tokens: split where the context has room for the parts, whole in a graph that has not; the same
+    bits."""
+    torch = _torch()
+    from paper_2609_33548_amd import termezo
+    g = torch.Generator(device="cuda").manual_seed(3)
+    M, K, N = 100, 4096, 1536
+    x = torch.randn(M, K, generator=g, device="cuda")
+    codes = torch.randint(-128, 128, (N, K), generator=g, device="cuda", dtype=torch.int8)
+    steps, want = torch.rand(N, generator=g, device="cuda"), torch.zeros(M, N, device="cuda")
+    ctx.linear_i8(x, codes, steps, want)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        c = termezo.Context([torch.zeros((16, 16), device="cuda")], stream=stream)
+        big, few, other = torch.zeros(600, 2560, device="cuda"), codes[:64, :2560].contiguous(), torch.zeros(600, 64, device="cuda")
+        c.linear_i8(big, few, steps[:64], other)
+        out = torch.zeros(M, N, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        c.linear_i8(x, codes, steps, out)
+    with torch.cuda.stream(stream):
+        for _ in range(3):
+            out.fill_(7.0)
+            graph.replay()
+            assert torch.equal(out, want)
+        out.fill_(7.0)
+        c.linear_i8(x, codes, steps, out)                 # eager: with room for the parts
+        assert torch.equal(out, want)
+        out.fill_(7.0)
+        graph.replay()
+        assert torch.equal(out, want)
+    torch.cuda.synchronize()
+    del graph
+    c.close()
+
+
 def test_product_refusals(ctx):
     torch = _torch()
     from paper_2609_33548_amd import termezo as T
