@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(256) k_adjust(RuleArgs a) {
 // the order of indices.
 //
 // k_draw_scan, a work group for a slice of a row: the slice's largest logit m_s, its weights exp((x - m_s) / T),
-// their sum, and sums and counts by bins (in fixed point, 2^-48: integer sums do not depend on their order).
+// their sum, and sums and counts by bins (in fixed point: integer sums do not depend on their order).
 // A bin is an eighth of T wide on a grid that all slices share (bin = floor(x (8 / T))), counted from the slice's
 // best bin downwards; the last of the 256 holds all that lies lower.
 // k_draw_list, the same grid: the row's bins (slices weighted by exp((m_s - m) / T)) tell in which of them the
@@ -175,7 +175,9 @@ __global__ void __launch_bounds__(256) k_adjust(RuleArgs a) {
 constexpr int kBins = 256, kMaxDrawRows = 1024, kList = 8192;
 constexpr bool plan_first(int E) { return E > 2; }       // long slices: plans in a launch of their own
 constexpr int kCopies = 4;           // of the bins, so that neighbouring lanes seldom meet in one
-constexpr double kSliceUnit = 0x1p48;
+// A slice's sums by bins are formed in units of 2^-51 of its largest weight (a copy holds those of 2048 logits) and
+// kept in units of 2^-50: 8192 weights are off by 8192 * 2^-52 and a bin by 2^-51, together less than 2^-38.9 of that weight.
+constexpr double kScanUnit = 0x1p51, kSliceUnit = 0x1p50;
 constexpr double kLog2e32 = 32.0 * 0x1.71547652b82fep+0, kLn2by32 = 0x1.62e42fefa39efp-6;   // 32 log2(e), ln(2) / 32
 
 struct SliceStat {
@@ -295,10 +297,27 @@ __device__ __forceinline__ double ln_of(double x) {
   p = fma(p, q, 1.0 / 3);
   return fma((double)e, 0x1.62e42fefa39efp-1, 2.0 * fma(t * q, p, t));
 }
-// w in [0, 1] in units of 1 / unit (a power of two up to 2^51), rounded to nearest.
-__device__ __forceinline__ unsigned long long draw_fix(double w, double unit) {
-  return (unsigned long long)__double_as_longlong(fma(w, unit, 0x1p52)) & ((1ull << 52) - 1);
+// w in [0, 1] in units of 2^-51, rounded to nearest.
+__device__ __forceinline__ unsigned long long scan_fix(double w) {
+  return (unsigned long long)__double_as_longlong(fma(w, kScanUnit, 0x1p52)) & ((1ull << 52) - 1);
 }
+// A bin's sum over its copies, from units of 2^-51 to units of 2^-50 (up to 2^63).
+__device__ __forceinline__ unsigned long long scan_sum(const unsigned long long* copies) {
+  unsigned long long m = 0, low = 0;
+#pragma unroll
+  for (int i = 0; i < kCopies; ++i) {
+    const unsigned long long c = copies[i * kBins];
+    m += c >> 1;
+    low += c & 1;
+  }
+  return m + (low >> 1);
+}
+// The unit of the listed weights: a power of two that takes a row's whole weight (1 to 2^24) to 2^62 .. 2^63, so that each of
+// them is off by at most 2^-63 of the whole, however small it is beside the largest, and all of them by 2^-39.
+__device__ __forceinline__ double list_unit(double total) {
+  return __hiloint2double((2 * 1023 + 62 - (__double2hiint(total) >> 20)) << 20, 0);
+}
+__device__ __forceinline__ unsigned long long list_fix(double w, double unit) { return __double2ull_rn(w * unit); }
 // Keys in the order of the row: greater comes first.
 __device__ __forceinline__ uint32_t ordered(float x) {
   const uint32_t b = __float_as_uint(x);
@@ -400,7 +419,7 @@ __global__ void __launch_bounds__(256) k_draw_scan(DrawArgs a) {
     sum += w;
     if (LIMITS && x[i] > -INFINITY) {
       const int j = min(best - draw_bin(x[i], s.grid), kBins - 1);
-      atomicAdd(&mass[copy + j], draw_fix(w, kSliceUnit));
+      atomicAdd(&mass[copy + j], scan_fix(w));
       if (COUNT) atomicAdd(&count[copy + j], 1u);
     }
   }
@@ -414,15 +433,13 @@ __global__ void __launch_bounds__(256) k_draw_scan(DrawArgs a) {
   }
   static_assert(kBins == 256, "a bin a thread");
   if (LIMITS) {
-    unsigned long long m = 0;
-    uint32_t c = 0;
+    a.mass[at * kBins + tid] = scan_sum(mass + tid);
+    if (COUNT) {
+      uint32_t c = 0;
 #pragma unroll
-    for (int i = 0; i < kCopies; ++i) {
-      m += mass[i * kBins + tid];
-      if (COUNT) c += count[i * kBins + tid];
+      for (int i = 0; i < kCopies; ++i) c += count[i * kBins + tid];
+      a.count[at * kBins + tid] = c;
     }
-    a.mass[at * kBins + tid] = m;
-    if (COUNT) a.count[at * kBins + tid] = c;
   }
 }
 
@@ -734,7 +751,7 @@ __device__ __forceinline__ unsigned long long draw_border(const RowPlan& p, cons
 #pragma unroll 1
         for (int i = tid; i < n; i += NT) {
           const unsigned long long k = key_at(i);
-          if (k && k >= least && k <= most) w += draw_fix(draw_weight(key_logit(k), p.top, s.scale, roots), unit);
+          if (k && k >= least && k <= most) w += list_fix(draw_weight(key_logit(k), p.top, s.scale, roots), unit);
         }
         w = wave_sum(w);
         __syncthreads();
@@ -778,7 +795,7 @@ __device__ __forceinline__ unsigned long long draw_border(const RowPlan& p, cons
         unsigned long long w[AT];
         if (!counting)
 #pragma unroll
-          for (int j = 0; j < AT; ++j) w[j] = draw_fix(draw_weight(key_logit(k[j]), p.top, s.scale, roots), unit);
+          for (int j = 0; j < AT; ++j) w[j] = list_fix(draw_weight(key_logit(k[j]), p.top, s.scale, roots), unit);
 #pragma unroll
         for (int j = 0; j < AT; ++j)
           if (in[j]) {
@@ -926,7 +943,7 @@ constexpr int kMaxSlices = 2048;
 constexpr int pick_threads(bool limits, int E) { return limits && E > 2 ? 512 : 256; }
 
 template <bool LIMITS, int E>
-__global__ void __launch_bounds__(pick_threads(LIMITS, E)) k_draw_pick(DrawArgs a, int unit_bits) {
+__global__ void __launch_bounds__(pick_threads(LIMITS, E)) k_draw_pick(DrawArgs a) {
   constexpr int NT = pick_threads(LIMITS, E), NW = NT / 64, SLICE = 1024 * E;
   __shared__ unsigned long long keys[LIMITS ? kList : 1], add[LIMITS ? kMaxSlices : 1];
   __shared__ BorderShared<LIMITS ? NT : 64> sh;
@@ -942,7 +959,6 @@ __global__ void __launch_bounds__(pick_threads(LIMITS, E)) k_draw_pick(DrawArgs 
   const SliceStat first_stat = stat[lane < a.slices ? lane : 0];       // on their way
   const double first_sure = LIMITS ? a.sure[(int64_t)row * a.slices + (lane < a.slices ? lane : 0)] : 0.0;
   const Settings s = draw_settings(a, row);
-  const double unit = (double)(1ull << unit_bits);
   float u = a.uniforms[row];
   const bool bad = s.bad || !(u >= 0.0f && u < 1.0f);
   u = u >= 1.0f ? 1.0f - 0x1p-24f : u > 0.0f ? u : 0.0f;
@@ -979,8 +995,9 @@ __global__ void __launch_bounds__(pick_threads(LIMITS, E)) k_draw_pick(DrawArgs 
     return;
   }
   auto bin_of = [&](float v) __attribute__((always_inline)) { return min(p.bin - draw_bin(v, s.grid), kBins - 1); };
+  const double unit = LIMITS ? list_unit(p.total) : 1.0;
   auto fixed = [&](unsigned long long k) __attribute__((always_inline)) {
-    return draw_fix(draw_weight(key_logit(k), p.top, s.scale, roots), unit);
+    return list_fix(draw_weight(key_logit(k), p.top, s.scale, roots), unit);
   };
 
   unsigned long long border = draw_key(-FLT_MAX, INT32_MAX);           // keys from here on are kept
@@ -1075,7 +1092,7 @@ __global__ void __launch_bounds__(pick_threads(LIMITS, E)) k_draw_pick(DrawArgs 
 // the row for a slice, one launch and no memory in between: 512 rows of 1000 47 -> 13 us, one row of 1000 19 -> 10.5, 256 of
 // 8192 27 -> 20; from 16384 on the slices are faster (one row 20 against 27 us).  Few waves, for the barriers.
 template <bool LIMITS, bool COUNT, int NT, int E>
-__global__ void __launch_bounds__(NT) k_draw_row(DrawArgs a, int unit_bits) {
+__global__ void __launch_bounds__(NT) k_draw_row(DrawArgs a) {
   constexpr int NW = NT / 64, PASS = 4 * NT;
   __shared__ unsigned long long keys[LIMITS ? PASS * E : 1], bins[LIMITS ? kCopies * kBins : 1];
   __shared__ uint32_t counts[COUNT ? kCopies * kBins : 1];
@@ -1091,7 +1108,6 @@ __global__ void __launch_bounds__(NT) k_draw_row(DrawArgs a, int unit_bits) {
   Four raw[E];
   slice_fetch<E, PASS>(x, 0, V, tid, -INFINITY, raw);
   const Settings s = draw_settings(a, row);
-  const double unit = (double)(1ull << unit_bits);
   float u = a.uniforms[row];
   const bool bad = s.bad || !(u >= 0.0f && u < 1.0f);
   u = u >= 1.0f ? 1.0f - 0x1p-24f : u > 0.0f ? u : 0.0f;
@@ -1131,21 +1147,19 @@ __global__ void __launch_bounds__(NT) k_draw_row(DrawArgs a, int unit_bits) {
       const float v = raw[i / 4].v[i % 4];
       if (v > -INFINITY) {
         const int j = min(bin - draw_bin(v, s.grid), kBins - 1);
-        atomicAdd(&bins[copy + j], draw_fix(draw_weight(v, top, s.scale, roots), kSliceUnit));
+        atomicAdd(&bins[copy + j], scan_fix(draw_weight(v, top, s.scale, roots)));
         if (COUNT) atomicAdd(&counts[copy + j], 1u);
       }
     }
     __syncthreads();
     if (tid < kBins) {
-      unsigned long long m = 0;
-      uint32_t c = 0;
+      mass[tid] = (double)scan_sum(bins + tid) * (1.0 / kSliceUnit);
+      if (COUNT) {
+        uint32_t c = 0;
 #pragma unroll
-      for (int i = 0; i < kCopies; ++i) {
-        m += bins[i * kBins + tid];
-        if (COUNT) c += counts[i * kBins + tid];
+        for (int i = 0; i < kCopies; ++i) c += counts[i * kBins + tid];
+        count[tid] = (int)c;
       }
-      mass[tid] = (double)m * (1.0 / kSliceUnit);
-      if (COUNT) count[tid] = (int)c;
     }
     __syncthreads();
     if (wave == 0) {
@@ -1182,7 +1196,7 @@ __global__ void __launch_bounds__(NT) k_draw_row(DrawArgs a, int unit_bits) {
       __syncthreads();
       const RowPlan& p = plan;                           // in LDS
       auto key_at = [&](int i) __attribute__((always_inline)) { return keys[i]; };
-      border = max(border, draw_border<NT>(p, s, unit, roots, n_list, key_at, sh, tid));
+      border = max(border, draw_border<NT>(p, s, list_unit(p.total), roots, n_list, key_at, sh, tid));
     }
   }
   const float xb = LIMITS ? key_logit(border) : s.best ? top : -FLT_MAX;
@@ -1291,9 +1305,6 @@ termezo_status termezo_sample(termezo_ctx* c, const float* logits, const float* 
     a.listed = (int32_t*)take(most * 8);
     a.count = (uint32_t*)take(most * slices * kBins * 4);
   }
-  int bits = 1;                                          // of a sum of vocab weights, and one more
-  while ((1 << bits) < vocab) ++bits;
-  const int unit = std::min(51, 62 - bits);
   for (int r0 = 0; r0 < rows; r0 += kMaxDrawRows) {
     const int n = std::min(kMaxDrawRows, rows - r0);
     auto from = [&](auto* p) { return p ? p + r0 : p; };
@@ -1309,9 +1320,9 @@ termezo_status termezo_sample(termezo_ctx* c, const float* logits, const float* 
     const dim3 rows_grid((unsigned)n);
     if (whole) {
 #define TMZ_ROW(NT, E)                                                                                                 \
-  if (!limits) hipLaunchKernelGGL((k_draw_row<false, false, NT, E>), rows_grid, dim3(NT), 0, c->stream, a, unit);     \
-  else if (top_k) hipLaunchKernelGGL((k_draw_row<true, true, NT, E>), rows_grid, dim3(NT), 0, c->stream, a, unit);    \
-  else hipLaunchKernelGGL((k_draw_row<true, false, NT, E>), rows_grid, dim3(NT), 0, c->stream, a, unit)
+  if (!limits) hipLaunchKernelGGL((k_draw_row<false, false, NT, E>), rows_grid, dim3(NT), 0, c->stream, a);     \
+  else if (top_k) hipLaunchKernelGGL((k_draw_row<true, true, NT, E>), rows_grid, dim3(NT), 0, c->stream, a);    \
+  else hipLaunchKernelGGL((k_draw_row<true, false, NT, E>), rows_grid, dim3(NT), 0, c->stream, a)
       if (vocab <= 1024) {
         TMZ_ROW(256, 1);
       } else if (vocab <= 4096) {
@@ -1325,7 +1336,7 @@ termezo_status termezo_sample(termezo_ctx* c, const float* logits, const float* 
 #define TMZ_DRAW(E)                                                                                          \
   if (!limits) {                                                                                             \
     hipLaunchKernelGGL((k_draw_scan<E, false, false>), grid, dim3(256), 0, c->stream, a);                    \
-    hipLaunchKernelGGL((k_draw_pick<false, E>), rows_grid, dim3(pick_threads(false, E)), 0, c->stream, a, unit);                     \
+    hipLaunchKernelGGL((k_draw_pick<false, E>), rows_grid, dim3(pick_threads(false, E)), 0, c->stream, a);                     \
   } else {                                                                                                   \
     if (top_k) {                                                                                             \
       hipLaunchKernelGGL((k_draw_scan<E, true, true>), grid, dim3(256), 0, c->stream, a);                    \
@@ -1336,7 +1347,7 @@ termezo_status termezo_sample(termezo_ctx* c, const float* logits, const float* 
       if (plan_first(E)) hipLaunchKernelGGL((k_draw_plan<false>), rows_grid, dim3(256), 0, c->stream, a);    \
       hipLaunchKernelGGL((k_draw_list<E, false>), grid, dim3(256), 0, c->stream, a);                         \
     }                                                                                                        \
-    hipLaunchKernelGGL((k_draw_pick<true, E>), rows_grid, dim3(pick_threads(true, E)), 0, c->stream, a, unit);                      \
+    hipLaunchKernelGGL((k_draw_pick<true, E>), rows_grid, dim3(pick_threads(true, E)), 0, c->stream, a);                      \
   }
     if (large) {
       TMZ_DRAW(8)

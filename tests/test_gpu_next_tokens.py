@@ -491,6 +491,67 @@ def test_draw_on_extreme_values(ctx):
         _check_sample(ctx, x, u, **kw)
 
 
+def _share(v):
+    """exp(-v) of an fp32 number as a fraction (math.exp is right to 2^-52 of it)."""
+    import math
+    from fractions import Fraction
+    return Fraction(math.exp(-float(F(v))))
+
+
+@pytest.mark.parametrize("R,V", [(1, 8000), (2, 20000), (1, 128256), (64, 128256), (1, 1 << 24)])
+@pytest.mark.parametrize("low", [14.0, 18.5, 21.25, 23.0, 24.0])
+def test_draw_among_many_small_weights(ctx, R, V, low):
+    """One token at 0 and all others at -low, 2^-20 to 2^-35 of its weight, whose places tell where top_p's border is.  Sums are
+    off by less than 2^-38 of themselves: the border lies where p times one sum meets another, the token where
+    u times one does, so both are off by 2 * 2^-38 S / w tokens at most, and by one where a sum meets a weight's end."""
+    import math
+    from fractions import Fraction as Q
+    w, S = _share(low), 1 + (V - 1) * _share(low)
+    x = np.full((R, V), -low, F)
+    x[:, 0] = 0.0
+    u = F(1.0 - 2.0 ** -24)
+    # shares of the small ones' weight that are left out, as near as fp32 has them
+    for part in (0.03, 0.4, 0.9):
+        p = F(float((S - Q(part) * (S - 1)) / S))
+        if not 1 / S < Q(float(p)) < 1:
+            continue                                      # they weigh less than fp32 tells apart
+        n = 1 + math.ceil((Q(float(p)) * S - 1) / w)      # kept: the first and n - 1 of the others, by index
+        want = max(0, math.floor((Q(float(u)) * (1 + (n - 1) * w) - 1) / w) + 1)
+        tok, lp = _sample(ctx, x, np.full(R, u), top_p=p)
+        off = math.ceil(4 * 2.0 ** -38 * S / w) + 1
+        assert np.abs(tok.astype(np.int64) - want).max() <= off, (part, tok[:3], want, off)
+        assert tok.max() < n + off
+        exact = math.log(w / (1 + (n - 1) * w)) if want else -math.log(1 + (n - 1) * w)
+        assert np.abs(lp.astype(np.float64) - exact).max() <= 2.0 ** -24 * abs(exact) + 2.0 ** -36
+
+
+def test_draw_behind_slices_of_small_weights(ctx):
+    """Fifteen slices of 8192 with a token at 0 and the others at a weight w1 that lies between two units of the sums by bins,
+    then a hundred slices of weights w2, where top_p's border lies.  A slice's sum is off by less than 2^-38.9, so the
+    border and the token by 15 * 2^-38.9 / w2 at most, and by one."""
+    import math
+    from fractions import Fraction as Q
+    for bits in (48, 50, 51):                             # the most that rounding to 2^-bits does to w1
+        low = min((np.nextafter(F(24.0), F(25.0)) + F(i) * F(2.0 ** -19) for i in range(4000)),
+                  key=lambda v: abs(float(_share(v) * 2 ** bits % 1) - 0.49))
+        w1, w2 = _share(low), _share(24.95)
+        V = 115 * 8192
+        x = np.full((1, V), -24.95, F)
+        x[0, :15 * 8192] = -low
+        x[0, :15 * 8192:8192] = 0.0
+        before = 15 * (1 + 8191 * w1)
+        S = before + 100 * 8192 * w2
+        p, u = F(1.0 - 5 * 2.0 ** -24), F(1.0 - 2.0 ** -24)
+        n = math.ceil((Q(float(p)) * S - before) / w2)
+        assert 10000 < n < 800000
+        want = 15 * 8192 + math.floor((Q(float(u)) * (before + n * w2) - before) / w2)
+        tok, lp = _sample(ctx, x, [u], top_p=p)
+        off = math.ceil(15 * 2.0 ** -38.9 / w2) + 1
+        assert abs(int(tok[0]) - want) <= off, (bits, tok, want, off)
+        exact = math.log(w2 / (before + n * w2))
+        assert abs(float(lp[0]) - exact) <= 2.0 ** -24 * abs(exact) + 2.0 ** -36
+
+
 @pytest.mark.parametrize("limits", [dict(), dict(top_p=0.9), dict(top_k=20)])
 def test_draw_follows_the_shares(ctx, limits):
     """4096 equidistant u of one row: every token comes as often as its share says (to one in 4096 and a step)."""
