@@ -624,7 +624,8 @@ termezo_status termezo_adjust_logits(termezo_ctx* ctx, const float* logits, int3
  * always kept.  tokens[r] is the first kept token, by index, up to which the kept weights
  * exceed uniforms[r] (in [0, 1)) times their sum; logprobs[r] (nullable) the logarithm of its
  * share.  Temperature 0 keeps the first token alone.  Weights, shares and sums are fp64 or
- * finer than 2^-38 of a sum; a weight below 2^-37 of a row's largest may count as zero.
+ * finer than 2^-38 of a sum; a weight below 2^-37 of a row's largest may count as zero, and one
+ * below 2^-1000 does: a token masked with the type's lowest value is not drawn beside others.
  * The result depends on nothing but the inputs.  A row without a logit above -inf has the token
  * -1 and the log probability -inf.  Temperatures that are negative or not finite (read as 0),
  * NaN limits (read as none) and random numbers outside [0, 1) (read as the nearest) raise a deferred

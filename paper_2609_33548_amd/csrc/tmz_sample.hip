@@ -282,6 +282,12 @@ __device__ __forceinline__ double exp_of(double q, const double* roots) {     //
 __device__ __forceinline__ double draw_weight(float x, float top, double scale, const double* roots) {
   return exp_of(fmax(((double)x - (double)top) * scale, -32000.0), roots);
 }
+// The same where a token or its slice can be drawn: 0 below 2^-1000.  A token masked with the type's lowest value weighs
+// nothing, and is not the first one up to which the weights exceed 0 (u = 0, once in 2^24 draws).
+__device__ __forceinline__ double drawn_weight(float x, float top, double scale, const double* roots) {
+  const double q = ((double)x - (double)top) * scale;
+  return q > -32000.0 ? exp_of(q, roots) : 0.0;
+}
 // ln x for x >= 2^-60: x = 2^e m with m from 0.7 to 1.42, ln m = 2 artanh((m - 1) / (m + 1)) by its series up to the 15th
 // power of a quotient below 0.18 (what is left out is below 2^-44).  Inline and short: the general function's code
 // had to come from memory for its one call.
@@ -1043,7 +1049,7 @@ __global__ void __launch_bounds__(pick_threads(LIMITS, E)) k_draw_pick(DrawArgs 
       if (i >= a.slices) return 0.0;
       if (!(t.top > -INFINITY)) return 0.0;
       if (!LIMITS && s.best) return t.top == p.top ? 1.0 : 0.0;
-      double w = draw_weight(t.top, p.top, s.scale, roots) * (LIMITS ? sure : t.sum);
+      double w = drawn_weight(t.top, p.top, s.scale, roots) * (LIMITS ? sure : t.sum);
       if (LIMITS) w += (double)add[i] / unit;
       return w;
     };
@@ -1084,7 +1090,7 @@ __global__ void __launch_bounds__(pick_threads(LIMITS, E)) k_draw_pick(DrawArgs 
   const double log_kept = ln_of(all_kept);                 // while they are on their way
   draw_token<NT, SLICE / (4 * NT), false>(a, row, raw, from, p.top, s, xb, (double)u * all_kept - before_slice, log_kept,
                                           chunk, tid, [&](float v, int k) __attribute__((always_inline)) {
-                                            return kept(v, k) ? draw_weight(v, p.top, s.scale, roots) : 0.0;
+                                            return kept(v, k) ? drawn_weight(v, p.top, s.scale, roots) : 0.0;
                                           });
 }
 
@@ -1202,7 +1208,7 @@ __global__ void __launch_bounds__(NT) k_draw_row(DrawArgs a) {
   const float xb = LIMITS ? key_logit(border) : s.best ? top : -FLT_MAX;
   const uint32_t tb = LIMITS ? (uint32_t)key_token(border) : UINT32_MAX;
   auto weight = [&](float v, int t) __attribute__((always_inline)) {
-    return v > xb || (v == xb && (uint32_t)t <= tb) ? draw_weight(v, top, s.scale, roots) : 0.0;
+    return v > xb || (v == xb && (uint32_t)t <= tb) ? drawn_weight(v, top, s.scale, roots) : 0.0;
   };
   draw_token<NT, E, true>(a, row, raw, 0, top, s, xb, (double)u, 0.0, chunk, tid, weight);
 }

@@ -552,6 +552,31 @@ def test_draw_behind_slices_of_small_weights(ctx):
         assert abs(float(lp[0]) - exact) <= 2.0 ** -24 * abs(exact) + 2.0 ** -36
 
 
+@pytest.mark.parametrize("low", [np.finfo(F).min, -1e30, -1e4])
+@pytest.mark.parametrize("R,V", [(2, 70), (3, 3000), (3, 8192), (2, 20000), (40, 128256)])
+def test_draw_at_zero_passes_tokens_without_weight(ctx, R, V, low):
+    """u = 0 is the first kept token with any weight: one masked with a large negative logit has exp(-10^4) of the best
+    one's at most, 0 in 64 bits, before it in its slice or in slices of their own."""
+    from oracle import next_token_ref as ref
+    rng = np.random.default_rng(V)
+    for lead in (1, V // 3, V - 2, V - 1):
+        x = (rng.standard_normal((R, V)) * 2).astype(F)
+        x[:, :lead] = low
+        x[1::2, ::3] = low
+        x[:, V - 1] = 1.0
+        for kw in (dict(), dict(top_k=V - 1), dict(top_p=0.999), dict(top_k=V), dict(min_p=1e-30), dict(top_k=3, top_p=0.5),
+                   dict(temperature=0.5), dict(temperature=0.0)):
+            tok, lp = _sample(ctx, x, np.zeros(R, F), **kw)
+            for r in range(min(R, 3)):
+                order, w, _ = ref.kept(x[r], **{k: F(v).item() if isinstance(v, float) else v for k, v in kw.items()})
+                drawn = order[w[order] > 0]
+                assert tok[r] == drawn.min(), (lead, kw, r, tok[r])
+                want = np.log(w[tok[r]] / w[order].sum())
+                assert abs(float(lp[r]) - want) <= 2.0 ** -24 * abs(want) + 2.0 ** -36
+    x = np.full((2, V), low, F)                           # nothing else: they are as likely as one another
+    assert _sample(ctx, x, [0.0, 0.999])[0].tolist() == [0, int(F(0.999) * V)]
+
+
 @pytest.mark.parametrize("limits", [dict(), dict(top_p=0.9), dict(top_k=20)])
 def test_draw_follows_the_shares(ctx, limits):
     """4096 equidistant u of one row: every token comes as often as its share says (to one in 4096 and a step)."""
