@@ -626,8 +626,10 @@ termezo_status termezo_adjust_logits(termezo_ctx* ctx, const float* logits, int3
  * share.  Temperature 0 keeps the first token alone.  Weights, shares and sums are fp64 or
  * finer than 2^-38 of a sum; a weight below 2^-37 of a row's largest may count as zero, and one
  * below 2^-1000 does: a token masked with the type's lowest value is not drawn beside others.
- * The result depends on nothing but the inputs.  A row without a logit above -inf has the token
- * -1 and the log probability -inf.  Temperatures that are negative or not finite (read as 0),
+ * The same call gives the same bits.  How a row's sums are divided goes by the call's rows and
+ * limits and by the device, so that a row in another batch may have a log probability whose last
+ * bit differs, or another token where uniforms or top_p lies within these bounds of a sum.  A row
+ * without a logit above -inf has the token -1 and the log probability -inf.  Temperatures that are negative or not finite (read as 0),
  * NaN limits (read as none) and random numbers outside [0, 1) (read as the nearest) raise a deferred
  * INVALID_ARG.  No output may overlap an input.  Errors: INVALID_ARG (rows 1 .. 65535, vocab 1 .. 2^24,
  * null or misaligned (4 bytes) pointers), STATE (captured, with scratch to be allocated), OOM. */

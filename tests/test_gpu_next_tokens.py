@@ -605,6 +605,24 @@ def test_draw_repeats_exactly(ctx):
             assert all(np.array_equal(a, b) for a, b in zip(first, again))
 
 
+@pytest.mark.parametrize("V,R", [(128256, 64), (32003, 256), (9000, 256)])
+def test_draw_of_a_row_in_batches_of_any_size(ctx, V, R):
+    """Rows alone, four together and in a batch that is divided otherwise: the same tokens, each log probability
+    within its bound (2^-24 of the value and 2^-36) on either side."""
+    from oracle import next_token_ref as ref
+    rng = np.random.default_rng(V)
+    x = (rng.standard_normal((R, V)) * 2.5).astype(F)
+    u = rng.random(R).astype(F)
+    for kw in (dict(top_p=0.9), dict(top_k=50, top_p=0.95), dict(min_p=0.01), dict(top_k=20, temperature=0.7)):
+        tok, lp = _sample(ctx, x, u, **kw)
+        for a, b in ((0, 1), (5, 6), (0, 4), (10, 14)):
+            t, l = _sample(ctx, x[a:b], u[a:b], **kw)
+            for r in range(a, b):
+                assert ref.sample(x[r], u[r], **{k: F(v).item() if isinstance(v, float) else v for k, v in kw.items()})[2] > 2.0 ** -36
+            assert np.array_equal(t, tok[a:b])
+            assert (np.abs(l.astype(np.float64) - lp[a:b]) <= 2 * (2.0 ** -24 * np.abs(l) + 2.0 ** -36)).all()
+
+
 def test_draw_of_large_vocabularies_and_many_rows(ctx):
     torch = _torch()
     rng = np.random.default_rng(10)
