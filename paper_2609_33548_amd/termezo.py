@@ -183,6 +183,12 @@ def _int(v, name, bits: int = 32) -> int:
     return v
 
 
+def _sizes(*sizes):
+    """Sizes of tensors that a C int holds (ctypes would wrap them around)."""
+    if max(sizes) >> 31:
+        raise ValueError(f"a size of {max(sizes)} does not fit 32 bits")
+
+
 def _stream_handle(stream) -> Optional[int]:
     if stream is None:
         import torch
@@ -441,6 +447,7 @@ class Context:
         eos = _int(eos, "eos")
         B, W, V = logits.shape
         n = out_scores.shape[-1]
+        _sizes(B, W, V, n)
         f32, i32, u8 = torch.float32, torch.int32, torch.uint8
         opt = lambda t, *a: None if t is None else _tensor(t, *a, self.device)
         T = 0 if history is None else history.shape[-1]
@@ -489,6 +496,7 @@ class Context:
         row."""
         import torch
         R, V = logits.shape
+        _sizes(R, V)
         f32, i32, dev = torch.float32, torch.int32, self.device
         rules, row = LogitRules(), (R,)
         if history is not None:
@@ -509,12 +517,16 @@ class Context:
         if (bias is None and bias_index is not None) or (mask is None and mask_index is not None):
             raise ValueError("an index needs its table")
         if bias is not None:
-            rules.n_bias = n = bias.shape[0]
+            n = bias.shape[0]
+            _sizes(n)
+            rules.n_bias = n
             rules.bias = _tensor(bias, "bias", (n, V), f32, dev)
             if bias_index is not None:
                 rules.bias_index = _tensor(bias_index, "bias_index", row, i32, dev)
         if mask is not None:
-            rules.n_masks = n = mask.shape[0]
+            n = mask.shape[0]
+            _sizes(n)
+            rules.n_masks = n
             rules.mask = _tensor(mask, "mask", (n, (V + 31) // 32), i32, dev)
             if mask_index is not None:
                 rules.mask_index = _tensor(mask_index, "mask_index", row, i32, dev)
@@ -534,6 +546,7 @@ class Context:
         takes the best token.  A row without a logit above -inf has token -1."""
         import torch
         R, V = logits.shape
+        _sizes(R, V)
         f32, i32 = torch.float32, torch.int32
         row = lambda t, name, dt=f32: None if t is None else _tensor(t, name, (R,), dt, self.device)
         self._check(_lib.termezo_sample(

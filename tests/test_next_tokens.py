@@ -118,3 +118,30 @@ def test_binding_refuses_wrong_tensors_and_incomplete_rules():
               lambda: T.Context.quantize_rows(c, z(3, 32), codes, steps)):
         with pytest.raises(T.TermezoError):
             f()
+
+
+def test_sizes_beyond_the_c_types_are_refused():
+    """Sizes that ctypes would wrap around: 2^32 + 9 logits are not 9."""
+    import torch
+    from paper_2609_33548_amd import termezo as T
+
+    class Ctx:
+        device, handle = torch.device("meta"), None
+
+        def _check(self, st, what):
+            raise AssertionError("reached the library")
+
+    c, far = Ctx(), (1 << 32) + 9
+    z = lambda *s, dt=torch.float32: torch.empty(s, dtype=dt, device="meta")
+    i32 = torch.int32
+    for R, V in ((1, far), (far, 1), (1, (1 << 31) + 1), ((1 << 31) + 1, 1)):
+        with pytest.raises(ValueError):
+            T.Context.sample(c, z(R, V), z(R), z(R, dt=i32))
+        with pytest.raises(ValueError):
+            T.Context.adjust_logits(c, z(R, V), z(R, V))
+    for kw in (dict(bias=z(far, 2), bias_index=z(3, dt=i32)), dict(mask=z(far, 1, dt=i32), mask_index=z(3, dt=i32))):
+        with pytest.raises(ValueError):
+            T.Context.adjust_logits(c, z(3, 2), z(3, 2), **kw)
+    for B, W, V, n in ((1, 1, far, 1), (far, 1, 1, 1), (1, far, 1, 1), (1, 1, 2, far)):
+        with pytest.raises(ValueError):
+            T.Context.beam_select(c, z(B, W, V), z(B, W), z(B, n), z(B, n, dt=i32), z(B, n, dt=i32))
