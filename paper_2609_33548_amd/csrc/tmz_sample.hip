@@ -1256,7 +1256,7 @@ termezo_status termezo_adjust_logits(termezo_ctx* c, const float* logits, int32_
   DeviceScope scope(c->device);
   if (scope.err != hipSuccess) return hip_status(c, scope.err, "adjust_logits");
   RuleArgs a{logits, out, vocab, rows, r, c->d_err};
-  if (a.r.hist_len == 0) a.r.history = nullptr;
+  if (a.r.hist_len == 0 && !r.lengths && !r.starts) a.r.history = nullptr;     // nothing to count, nothing to check
 #define TMZ_ADJUST(SLICE, HIST)                                                                                    \
   hipLaunchKernelGGL((k_adjust<SLICE, HIST>), dim3((unsigned)((vocab + SLICE - 1) / SLICE), (unsigned)rows), dim3(256), 0, \
                      c->stream, a)

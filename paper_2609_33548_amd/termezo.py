@@ -501,7 +501,8 @@ class Context:
         rules, row = LogitRules(), (R,)
         if history is not None:
             rules.hist_len = T = history.shape[-1]
-            rules.history = _tensor(history, "history", (R, T), i32, dev)
+            # a tensor without elements has no address, and none of it is read
+            rules.history = _tensor(history, "history", (R, T), i32, dev) or logits.data_ptr()
             if lengths is not None:
                 rules.lengths = _tensor(lengths, "lengths", row, i32, dev)
             if starts is not None:

@@ -363,6 +363,23 @@ def test_rules_refused_and_reported(ctx):
     ctx.sync()
 
 
+def test_rules_of_an_empty_history_check_its_lengths(ctx):
+    """A history without places: lengths and starts other than 0 are reported as with places."""
+    torch = _torch()
+    i = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    x, o = torch.randn(3, 40, device="cuda"), torch.zeros(3, 40, device="cuda")
+    h, pen = i(0, 0, 0).view(3, 1)[:, :0], dict(repetition=torch.full((3,), 2.0, device="cuda"))
+    for kw in (dict(), dict(lengths=i(0, 0, 0)), dict(starts=i(0, 0, 0)), dict(lengths=i(0, 0, 0), starts=i(0, 0, 0))):
+        ctx.adjust_logits(x, o.zero_(), history=h, **pen, **kw)
+        ctx.sync()
+        assert torch.equal(o, x)
+    for kw in (dict(lengths=i(0, 1, 0)), dict(lengths=i(0, 0, -1)), dict(starts=i(1, 0, 0)), dict(starts=i(0, -1, 0)),
+               dict(lengths=i(7, 0, 0), starts=i(3, 0, 0))):
+        ctx.adjust_logits(x, o.zero_(), history=h, **pen, **kw)
+        _refused(ctx.sync)
+        assert torch.equal(o, x)
+
+
 # --------------------------------------------------------------------------------------------
 # the draw
 # --------------------------------------------------------------------------------------------
