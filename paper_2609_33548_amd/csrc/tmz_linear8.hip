@@ -148,7 +148,8 @@ static hipError_t launch_rows_i8(const void* x, termezo_dtype dt, int64_t M, int
 #define TMZ_ROWS(T, C, W)                                                                                          \
   hipLaunchKernelGGL((k_rows_i8<T, C, W, TOKENS>), dim3((unsigned)((W) > 1 ? M : (M + 3) / 4)), dim3(256), 0, s, (const T*)x, \
                      M, K, pitch, floor, q, step)
-  const bool wide = K > 4096 || M < 8 * (int64_t)n_cu;
+  // 2^24 rows of four waves would be 2^32 threads, one more than a launch takes
+  const bool wide = (K > 4096 && M < (int64_t(1) << 24)) || M < 8 * (int64_t)n_cu;
   if (dt == TERMEZO_BF16) {
     if (wide) TMZ_ROWS(uint16_t, 4, 4); else TMZ_ROWS(uint16_t, 8, 1);
   } else {

@@ -70,6 +70,30 @@ def test_rows_in_8_bits(ctx, bf16, N, K):
     assert (got[N] == 77).all() and st[N] == 77.0
 
 
+def test_the_most_rows_of_more_than_4096_values(ctx):
+    """2^24 rows of 4112: a work group of 256 for each would be 2^32 threads, which no launch takes."""
+    torch = _torch()
+    from oracle import next_token_ref as ref
+    N, K = 1 << 24, 4112
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < N * (3 * K + 4) + (8 << 30):
+        pytest.skip("not enough memory")
+    w = torch.zeros((N, K), dtype=torch.bfloat16, device="cuda")
+    rows = [0, 1, 4095, N // 2 + 3, N - 2, N - 1]
+    for i, n in enumerate(rows):
+        w[n].normal_(std=10.0 ** i)
+    codes = torch.full((N, K), 77, dtype=torch.int8, device="cuda")
+    steps = torch.full((N,), 77.0, device="cuda")
+    ctx.quantize_rows(w, codes, steps)
+    for n in rows:
+        q, d = ref.quantise(w[n].float().cpu().numpy(), 1e-30)
+        assert np.array_equal(codes[n].cpu().numpy(), q) and float(steps[n]) == d
+    assert int((steps == F(1e-30) / F(127.0)).sum()) == N - len(rows)
+    assert not codes[2:4095].any() and not codes[N - 1000:N - 2].any()
+    del w, codes, steps
+    torch.cuda.empty_cache()
+
+
 # shapes: one token and many, odd numbers of tokens and rows, sums shorter and longer than a step, heads and projections
 PRODUCTS = [(1, 16, 1), (1, 256, 688), (2, 48, 5), (3, 256, 1024), (15, 80, 33), (16, 1536, 517), (17, 512, 97),
             (1, 2560, 20003), (5, 6912, 300), (8, 2560, 16500), (16, 320, 40000), (31, 1536, 32003), (32, 2560, 20000),
