@@ -834,6 +834,127 @@ def test_decode_with_the_head_in_8_bits(orc, bf16):
     ctx.close()
 
 
+def _hidden_codes(logits, d):
+    """Codes and steps of the hidden states, from the logits of a head with code 1 at k in row k and steps 1: q[k] step,
+    rounded once where q[k] is no power of two, so that such a code's logit gives the step itself."""
+    v = logits[:, :d].astype(np.float64)
+    q = np.rint(v * (127.0 / np.abs(v).max(1, keepdims=True)))
+    power = (np.abs(q) > 0) & (np.log2(np.maximum(np.abs(q), 1)) % 1 == 0)
+    assert power.any(1).all()
+    at = power.argmax(1)[:, None]
+    step = np.take_along_axis(v / np.where(power, q, 1), at, 1)
+    assert (np.abs(v - q * step) <= 2.0 ** -24 * np.abs(v)).all() and (np.abs(q).max(1) == 127).all()
+    return q, step
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("G", [3, 16, 20, 40, 130])
+def test_decode_with_the_head_in_8_bits_is_the_product_of_its_codes(orc, bf16, G):
+    """Logits of a head in 8 bits are the integer products of the hidden states' codes, which a head of known codes reads out:
+    3 * 2^-24 of the value for the three fp32 operations.  Rows for every form of the product (up to 16, up to 32, more); prompts
+    of ragged lengths, a row without tokens, single tokens, captured steps.  The codes belong to the hidden states that the
+    embedding's logits determine: half a step off, and what 257 * 2^-24 of the sums behind a logit make of it."""
+    torch = _torch()
+    from paper_2609_33548_amd import synth, termezo as T
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        cfg, (ref, ctx, model, emb, E, w) = _decoder(orc, bf16)
+        ctx.perturb(2, 1e-3, 1)
+        V, d, P = cfg.vocab, 256, 9
+        codes, steps = torch.zeros((V, d), dtype=torch.int8, device="cuda"), torch.zeros(V, device="cuda")
+        ctx.quantize_rows(E, codes, steps)
+        eye, ones = torch.zeros_like(codes), torch.zeros(V, device="cuda")
+        eye[:d] = torch.eye(d, dtype=torch.int8, device="cuda")
+        ones[:d] = 1.0
+        tokens = torch.from_numpy(synth.tokens(100, G, P + 2, V)).cuda()
+        lengths = 1 + torch.arange(G, dtype=torch.int32, device="cuda") % P
+        lengths[1] = 0
+        make = lambda: T.KVCache(ctx, cfg.n_blocks, cfg.n_heads, cfg.n_kv_heads, cfg.head_dim, 64, G, 1, cfg.rope_base, E.dtype)
+        heads = dict(read=(eye, ones), eight=(codes, steps), plain=(None, None))
+        got = {}
+        for name, head in heads.items():
+            c, got[name] = make(), [torch.full((G, V), 7.0, device="cuda") for _ in range(3)]
+            model.set_head(*head)
+            model.decode(c, tokens[:, :P].contiguous(), got[name][0], counts=lengths)
+            model.decode(c, tokens[:, P:P + 1].contiguous(), got[name][1])
+            one = tokens[:, P + 1:].contiguous()
+            model.decode(c, one, got[name][2])
+            if name == "eight":                           # the last step again, from a graph
+                again = make()
+                model.decode(again, tokens[:, :P].contiguous(), torch.zeros((G, V), device="cuda"), counts=lengths)
+                model.decode(again, tokens[:, P:P + 1].contiguous(), torch.zeros((G, V), device="cuda"))
+                out = torch.full((G, V), 7.0, device="cuda")
+                stream.synchronize()
+                graph = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(graph, stream=stream):
+                    model.decode(again, one, out)
+                graph.replay()
+                assert torch.equal(out, got[name][2])
+                first = out.clone()
+                graph.replay()                            # one more token: the cache's lengths are the device's
+                model.decode(c, one, (more := torch.zeros((G, V), device="cuda")))
+                assert torch.equal(out, more) and not torch.equal(out, first)
+        ctx.sync()
+    c8, s8 = codes.cpu().numpy().astype(np.float64), steps.cpu().numpy().astype(np.float64)
+    e64 = E.double().cpu().numpy()
+    solve = np.linalg.pinv(e64)                           # hidden states from the embedding's logits
+    for i in range(3):
+        read, eight, plain = (got[n][i].cpu().numpy() for n in ("read", "eight", "plain"))
+        rows = np.arange(G) != 1 if i == 0 else np.ones(G, bool)
+        if i == 0:
+            assert not read[1].any() and not eight[1].any() and not plain[1].any()
+        q, step = _hidden_codes(read[rows], d)
+        want = (q @ c8.T) * step * s8
+        assert (np.abs(eight[rows] - want) <= 3.0 * 2.0 ** -24 * 1.01 * np.abs(want) + 1e-40).all()
+        x = plain[rows].astype(np.float64) @ solve.T
+        slack = 1.01 * 257 * 2.0 ** -24 * (np.abs(x) @ np.abs(e64).T) @ np.abs(solve).T
+        assert (np.abs(q * step - x) <= 0.5001 * step + slack).all()
+        assert slack.max() < 10 * step.max()              # the codes are told apart from others' rows and scales
+    model.close()
+    ctx.close()
+
+
+def test_two_models_with_heads_of_their_own_at_once(orc):
+    """Models of one context on streams of their own, one with the head in 8 bits, one with another head in 8 bits, their steps
+    queued in turn: the logits of each one alone."""
+    torch = _torch()
+    from paper_2609_33548_amd import synth, termezo as T
+    cfg, (ref, ctx, model, emb, E, w) = _decoder(orc)
+    ctx.perturb(2, 1e-3, 1)
+    V, G, P, N = cfg.vocab, 40, 30, 6
+    pair = T.Model(ctx, cfg.n_blocks, cfg.d_model, cfg.n_heads, cfg.n_kv_heads, cfg.d_ffn, V, E)
+    codes, steps = torch.zeros((V, 256), dtype=torch.int8, device="cuda"), torch.zeros(V, device="cuda")
+    ctx.quantize_rows(E, codes, steps)
+    heads = [(codes, steps), (codes.flip(0).contiguous(), steps * 0.5)]
+    tokens = [torch.from_numpy(synth.tokens(100 + i, G, P + N, V)).cuda() for i in range(2)]
+    make = lambda: T.KVCache(ctx, cfg.n_blocks, cfg.n_heads, cfg.n_kv_heads, cfg.head_dim, 64, G, 1, cfg.rope_base, E.dtype)
+    pieces = [[t[:, :P].contiguous()] + [t[:, P + i:P + i + 1].contiguous() for i in range(N)] for t in tokens]
+    alone = [[torch.zeros((G, V), device="cuda") for _ in range(N + 1)] for _ in range(2)]
+    both = [[torch.zeros((G, V), device="cuda") for _ in range(N + 1)] for _ in range(2)]
+    for m, head, xs, outs in zip((model, pair), heads, pieces, alone):
+        m.set_head(*head)
+        c = make()
+        for x, o in zip(xs, outs):
+            m.decode(c, x, o)
+        ctx.sync()
+    caches = [make(), make()]
+    torch.cuda.synchronize()
+    for m in (model, pair):
+        m.set_stream(torch.cuda.Stream())
+    for i in range(N + 1):
+        for m, c, xs, outs in zip((model, pair), caches, pieces, both):
+            m.decode(c, xs[i], outs[i])
+    for m in (model, pair):
+        m.join()
+    ctx.sync()
+    for k in range(2):
+        assert all(torch.equal(a, b) for a, b in zip(alone[k], both[k]))
+    assert not torch.equal(alone[0][0], alone[1][0])
+    for m in (model, pair):
+        m.close()
+    ctx.close()
+
+
 def test_generation_by_sampling_together(orc):
     """Rollouts: prompts, then steps of decode (8-bit head), rules and draws, eager and captured; every token is
     what the oracle draws from the step's own logits, obeys its mask, and sampled rows feed the next step."""
