@@ -29,7 +29,7 @@ struct __attribute__((packed, aligned(4))) Ids {
 struct RuleArgs {
   const float* logits;
   float* out;
-  int32_t vocab, rows;
+  int32_t vocab;
   termezo_logit_rules r;
   int32_t* err;
 };
@@ -1255,7 +1255,7 @@ termezo_status termezo_adjust_logits(termezo_ctx* c, const float* logits, int32_
     return refuse(c, "adjust_logits: a table without lines, or without indices and lines neither 1 nor rows");
   DeviceScope scope(c->device);
   if (scope.err != hipSuccess) return hip_status(c, scope.err, "adjust_logits");
-  RuleArgs a{logits, out, vocab, rows, r, c->d_err};
+  RuleArgs a{logits, out, vocab, r, c->d_err};
   if (a.r.hist_len == 0 && !r.lengths && !r.starts) a.r.history = nullptr;     // nothing to count, nothing to check
 #define TMZ_ADJUST(SLICE, HIST)                                                                                    \
   hipLaunchKernelGGL((k_adjust<SLICE, HIST>), dim3((unsigned)((vocab + SLICE - 1) / SLICE), (unsigned)rows), dim3(256), 0, \

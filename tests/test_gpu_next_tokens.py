@@ -162,6 +162,20 @@ def test_product_of_large_outputs(ctx, bf16, M, K, N):
         assert ((got - want).abs() <= tol).all(), m
 
 
+@pytest.mark.parametrize("M,K,N", [(1, 64, 40), (16, 1040, 77), (17, 272, 130), (33, 144, 65), (70, 2064, 129)])
+def test_product_is_the_oracles(ctx, M, K, N):
+    torch = _torch()
+    from oracle import next_token_ref as ref
+    rng = np.random.default_rng(M + K)
+    x = (rng.standard_normal((M, K)) * 10.0 ** rng.integers(-6, 4, (M, 1))).astype(F)
+    codes = rng.integers(-128, 128, (N, K)).astype(np.int8)
+    steps = (rng.random(N) * 1e-2).astype(F)
+    out = torch.zeros(M, N, device="cuda")
+    ctx.linear_i8(*(torch.from_numpy(t).cuda() for t in (x, codes, steps)), out)
+    want = ref.linear(x, codes, steps)
+    assert (np.abs(out.double().cpu().numpy() - want) <= 3.0 * 2.0 ** -24 * 1.01 * np.abs(want)).all()
+
+
 def test_product_of_quantised_rows_is_near_the_real_one(ctx):
     """The two calls as they are used: half a step on each side of every product."""
     torch = _torch()

@@ -21,6 +21,21 @@ def test_oracle_codes_are_half_a_step_off_at_most():
     assert np.isnan(ref.quantise(np.array([1, np.inf], F), 1e-5)[1])
 
 
+def test_oracle_products_of_python_integers():
+    from oracle import next_token_ref as ref
+    rng = np.random.default_rng(2)
+    x = (rng.standard_normal((3, 48)) * 10.0 ** rng.integers(-3, 4, (3, 1))).astype(F)
+    x[1] = 0.0
+    codes = rng.integers(-128, 128, (5, 48)).astype(np.int8)
+    steps = rng.random(5).astype(F)
+    got = ref.linear(x, codes, steps)
+    for m in range(3):
+        q, d = ref.quantise(x[m], 1e-5)
+        for n in range(5):
+            total = sum(int(a) * int(b) for a, b in zip(q, codes[n]))
+            assert got[m, n] == total * float(d) * float(steps[n])
+
+
 def test_oracle_rules_token_by_token():
     """Against a statement in Python numbers, a token at a time (fp32 values whose results are exact)."""
     from oracle import next_token_ref as ref
