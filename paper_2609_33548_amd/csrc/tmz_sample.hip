@@ -848,6 +848,9 @@ __device__ __forceinline__ unsigned long long draw_border(const RowPlan& p, cons
     }
     least = lo;
   }
+  // A border among the keys of -0, which no logit has: all zeros lie above it (compared as numbers, they would equal it and
+  // be kept by their index)
+  if ((uint32_t)(least >> 32) == ordered(-0.0f)) least = (unsigned long long)ordered(0.0f) << 32;
   return least;
 }
 

@@ -607,6 +607,28 @@ def test_draw_behind_slices_of_small_weights(ctx):
         assert abs(float(lp[0]) - exact) <= 2.0 ** -24 * abs(exact) + 2.0 ** -36
 
 
+@pytest.mark.parametrize("R,V", [(1, 6), (3, 700), (2, 3000), (2, 8000), (2, 20000), (40, 128256)])
+def test_draw_of_a_best_logit_of_zero(ctx, R, V):
+    """Logits of exactly 0 behind negative powers of two: the border's search halves the keys between the two, among
+    them those of -0."""
+    rng = np.random.default_rng(V)
+    u = rng.random(R).astype(F)
+    for e in range(-6, 5):
+        for zero in (-0.0, 0.0):
+            x = np.full((R, V), -60.0 * 2.0 ** e, F)
+            x[:, [1, V // 2, V - 2]] = -(2.0 ** e)
+            x[:, V - 1 - V // 3] = zero
+            kw = dict(temperature=1.3 * 2.0 ** e)
+            for k, p in ((2, 0.489), (2, 0.7), (3, 0.45), (4, 0.4), (4, 0.9), (0, 0.3)):
+                tok = _check_sample(ctx, x, u, top_k=k, top_p=p, **kw)
+                if p < 0.49:
+                    assert (tok == V - 1 - V // 3).all()
+            _check_sample(ctx, x, u, min_p=0.4, top_p=0.4, **kw)
+            x[:, V - 1] = zero                            # two of them, the second behind the first
+            for k, p in ((2, 0.489), (3, 0.9), (4, 0.7), (0, 0.6)):
+                _check_sample(ctx, x, u, top_k=k, top_p=p, **kw)
+
+
 @pytest.mark.parametrize("low", [np.finfo(F).min, -1e30, -1e4])
 @pytest.mark.parametrize("R,V", [(2, 70), (3, 3000), (3, 8192), (2, 20000), (40, 128256)])
 def test_draw_at_zero_passes_tokens_without_weight(ctx, R, V, low):
