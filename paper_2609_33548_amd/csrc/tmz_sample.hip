@@ -282,11 +282,10 @@ __device__ __forceinline__ double exp_of(double q, const double* roots) {     //
 __device__ __forceinline__ double draw_weight(float x, float top, double scale, const double* roots) {
   return exp_of(fmax(((double)x - (double)top) * scale, -32000.0), roots);
 }
-// The same where a token or its slice can be drawn: 0 below 2^-1000.  A token masked with the type's lowest value weighs
-// nothing, and is not the first one up to which the weights exceed 0 (u = 0, once in 2^24 draws).
-__device__ __forceinline__ double drawn_weight(float x, float top, double scale, const double* roots) {
-  const double q = ((double)x - (double)top) * scale;
-  return q > -32000.0 ? exp_of(q, roots) : 0.0;
+// The least logit with a weight: 2^-1000 of the best one's.  A token masked with the type's lowest value weighs nothing, and is
+// not the first one up to which the weights exceed 0 (u = 0, once in 2^24 draws).
+__device__ __forceinline__ float draw_floor(float top, const Settings& s) {
+  return fmaxf(__double2float_ru((double)top - 693.1471805599453 / s.inv_t), -FLT_MAX);           // 1000 ln 2
 }
 // ln x for x >= 2^-60: x = 2^e m with m from 0.7 to 1.42, ln m = 2 artanh((m - 1) / (m + 1)) by its series up to the 15th
 // power of a quotient below 0.18 (what is left out is below 2^-44).  Inline and short: the general function's code
@@ -1041,8 +1040,9 @@ __global__ void __launch_bounds__(pick_threads(LIMITS, E)) k_draw_pick(DrawArgs 
     __syncthreads();
   }
   // kept: logits above xb, and those equal to it up to token tb
-  const float xb = LIMITS ? key_logit(border) : s.best ? p.top : -FLT_MAX;
-  const uint32_t tb = LIMITS ? (uint32_t)key_token(border) : UINT32_MAX;
+  const float least = draw_floor(p.top, s), border_x = LIMITS ? key_logit(border) : s.best ? p.top : -FLT_MAX;
+  const float xb = fmaxf(border_x, least);
+  const uint32_t tb = LIMITS && border_x >= least ? (uint32_t)key_token(border) : UINT32_MAX;
   auto kept = [&](float v, int t) __attribute__((always_inline)) { return v > xb || (v == xb && (uint32_t)t <= tb); };
   // The slices' kept weights, summed up in their order by one wave; the first whose sum passes u times the whole (the
   // last one with any where rounding leaves none)
@@ -1052,7 +1052,8 @@ __global__ void __launch_bounds__(pick_threads(LIMITS, E)) k_draw_pick(DrawArgs 
       if (i >= a.slices) return 0.0;
       if (!(t.top > -INFINITY)) return 0.0;
       if (!LIMITS && s.best) return t.top == p.top ? 1.0 : 0.0;
-      double w = drawn_weight(t.top, p.top, s.scale, roots) * (LIMITS ? sure : t.sum);
+      if (t.top < least) return 0.0;
+      double w = draw_weight(t.top, p.top, s.scale, roots) * (LIMITS ? sure : t.sum);
       if (LIMITS) w += (double)add[i] / unit;
       return w;
     };
@@ -1093,7 +1094,7 @@ __global__ void __launch_bounds__(pick_threads(LIMITS, E)) k_draw_pick(DrawArgs 
   const double log_kept = ln_of(all_kept);                 // while they are on their way
   draw_token<NT, SLICE / (4 * NT), false>(a, row, raw, from, p.top, s, xb, (double)u * all_kept - before_slice, log_kept,
                                           chunk, tid, [&](float v, int k) __attribute__((always_inline)) {
-                                            return kept(v, k) ? drawn_weight(v, p.top, s.scale, roots) : 0.0;
+                                            return kept(v, k) ? draw_weight(v, p.top, s.scale, roots) : 0.0;
                                           });
 }
 
@@ -1208,10 +1209,11 @@ __global__ void __launch_bounds__(NT) k_draw_row(DrawArgs a) {
       border = max(border, draw_border<NT>(p, s, list_unit(p.total), roots, n_list, key_at, sh, tid));
     }
   }
-  const float xb = LIMITS ? key_logit(border) : s.best ? top : -FLT_MAX;
-  const uint32_t tb = LIMITS ? (uint32_t)key_token(border) : UINT32_MAX;
+  const float least = draw_floor(top, s), border_x = LIMITS ? key_logit(border) : s.best ? top : -FLT_MAX;
+  const float xb = fmaxf(border_x, least);
+  const uint32_t tb = LIMITS && border_x >= least ? (uint32_t)key_token(border) : UINT32_MAX;
   auto weight = [&](float v, int t) __attribute__((always_inline)) {
-    return v > xb || (v == xb && (uint32_t)t <= tb) ? drawn_weight(v, top, s.scale, roots) : 0.0;
+    return v > xb || (v == xb && (uint32_t)t <= tb) ? draw_weight(v, top, s.scale, roots) : 0.0;
   };
   draw_token<NT, E, true>(a, row, raw, 0, top, s, xb, (double)u, 0.0, chunk, tid, weight);
 }

@@ -715,6 +715,23 @@ def test_draw_of_large_vocabularies_and_many_rows(ctx):
         assert all(np.array_equal(p, w[a:b]) for p, w in zip(part, whole))
 
 
+def test_draw_of_more_rows_than_are_drawn_at_a_time(ctx):
+    """2500 rows in slices, settings of their own: parts of the batch on either side of every 1024 give the same."""
+    rng = np.random.default_rng(12)
+    R, V = 2500, 9000
+    x = (rng.standard_normal((R, V)) * 2.5).astype(F)
+    u = rng.random(R).astype(F)
+    kw = dict(top_k=rng.integers(0, 60, R).astype(np.int32), top_p=(0.5 + 0.5 * rng.random(R)).astype(F),
+              min_p=(0.01 * rng.random(R)).astype(F), temperature=(0.5 + rng.random(R)).astype(F))
+    for names in (("top_k", "top_p"), ("top_p", "min_p", "temperature"), ("temperature",)):
+        lim = {k: kw[k] for k in names}
+        whole = _sample(ctx, x, u, **lim)
+        for a, b in ((0, 40), (1000, 1040), (1024, 1030), (2040, 2060), (2490, 2500)):
+            part = {k: v[a:b] for k, v in lim.items()}
+            tok = _check_sample(ctx, x[a:b], u[a:b], **part)
+            assert np.array_equal(tok, whole[0][a:b])
+
+
 def test_draw_refused_and_reported(ctx):
     torch = _torch()
     z = lambda *s, dt=torch.float32: torch.zeros(s, dtype=dt, device="cuda")
