@@ -572,7 +572,8 @@ termezo_status termezo_quantize_rows(termezo_ctx* ctx, const void* w, termezo_dt
                                      int64_t K, int8_t* codes, float* steps);
 
 /* Product of M tokens with N rows of 8-bit weights: every row x of the input is taken in 8 bits
- * (a = max(max |x|, 1e-5) as in termezo_bitlinear_forward, q[k] = rne(x[k] * s), s = 127 * (1 / a)),
+ * (a = max(max |x|, 1e-5) as in termezo_bitlinear_forward; q[k] = rne(x[k] * s), s = 127 * (1 / a), where that
+ * call takes the quotient 127 / a, so that a code next to a half may be another one),
  * out[m][n] = (sum_k q[k] codes[n][k]) * ((a / 127) * steps[n]), the sum exact in int32, each
  * fp32 operation rounded, then to out's type.  x [M][K] in xdt, out [M][N] in ydt (F32 or BF16
  * each), codes int8 [N][K], -128 .. 127.  An input row with a value that is not finite has NaN

@@ -178,7 +178,9 @@ __device__ __forceinline__ void put(uint16_t* p, float v) { *(__bf16*)p = (__bf1
 // banks).  Up to 16 tokens are taken in 8 bits here, by every work group for itself (one launch); more come
 // from the quantiser.  Work groups walk the weights, 16 rows at a time, each wave its own (KW = 1) or all of
 // them together, dividing the steps (KW = NW, few weight rows); GS steps ahead of the products.
-// 1 x 2560 -> 128256: 57 us (5.8 TB/s), 32 x 1536 -> 32003 15, 3 x 256 -> 688 4.2.
+// 1 x 2560 -> 128256: 57 us (5.8 TB/s), 32 x 1536 -> 32003 15, 3 x 256 -> 688 4.2.  Few weight rows are bound by latency (one
+// row's loads, the join, and up to 16 tokens the row maxima before them): 1 / 4 / 16 tokens x 2560 -> 2560 5.8 / 6.1 / 8.2 us,
+// 6912 -> 2560 12.8 / 14.2 / 22.4, 2560 -> 13824 14.5 / 14.6 / 17.4, whole calls.
 // ---------------------------------------------------------------------------
 template <typename TX, typename TY, int MT, int KB, int NW, int KW, int GS>
 __global__ void __launch_bounds__(64 * NW) k_linear_walk(const TX* __restrict__ x, const int8_t* __restrict__ q,
@@ -567,8 +569,8 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), BPC * (BM / WM) * 
 
 // What a launch of T tiles takes on cu compute units (us): the first tile of a compute unit c0 + l K, further ones a + b K
 // each (K in thousands), where T is no multiple of cu the last, partial round counts half of its share and half of a
-// whole one.  Fitted to nine weights at 40 to 8192 tokens (rms 9 to 14%); the tile with the least estimate is within 1%
-// of the best on average, 11% at worst.
+// whole one.  Fitted to nine weights at 40 to 8192 tokens (rms 9 to 14%); among these the tile with the least estimate is
+// within 1% of the best on average, 11% at worst (no other weights were timed with every tile).
 struct LinearCost {
   int bm, bn;
   float c0, l, a, b;

@@ -164,13 +164,16 @@ __global__ void __launch_bounds__(256) k_adjust(RuleArgs a) {
 // k_draw_list, the same grid: the row's bins (slices weighted by exp((m_s - m) / T)) tell in which of them the
 // borders lie (long slices: found by k_draw_plan before); the slice's logits in those bins go to the row's list.
 // k_draw_pick, a work group a row: finds the border in the list by narrowing a range of keys (logit, index),
-// a part a thread at a time; then the slice and the token.  Where the list does not hold them (many equal logits)
-// it goes through the row in the list's place.
+// a part a thread at a time; then the slice and the token.  Where the list does not hold them it goes through the
+// row in the list's place, alone: many equal logits; a top_k whose border lies 32 T and more below the best logit, all of which is
+// the last bin (a confident row, a low temperature); bins with many tokens (flat rows of a large vocabulary).  64 x 128256 of
+// deviation 2.5 with one logit at 24, T = 0.3, top_k up to 100: 500 us, 40 without that logit; one such row 630 (26); one row of
+// 262144 of deviation 1 with top_p 1270 us, of deviation 2.5 41.
 // Without limits the first and the last are enough.
 // The scan is bound by vector instructions (an exponential in fp64 and a bin a logit) beside its reads, the list by
-// its reads, the plan and the pick by their chains of barriers: 64 x 128256 with top_p 14.3 + 6.0 + 12.3 + 19.5 us (the logits
-// alone at the rate of a copy: 6.4), one row of 32003 with top_k and top_p 3.9 + 8.4 + 9.1, 256 x 32000 without
-// limits 11 + 5.0.
+// its reads, the plan and the pick by their chains of barriers: 64 x 128256 with top_p 14.3 + 5.9 + 12.3 + 20.4 us (the logits
+// alone at the rate of a copy: 6.4), one row of 32003 with top_k and top_p 3.8 + 8.2 + 9.4, 256 x 32000 without
+// limits 11.3 + 5.2.
 // ---------------------------------------------------------------------------
 constexpr int kBins = 256, kMaxDrawRows = 1024, kList = 8192;
 constexpr bool plan_first(int E) { return E > 2; }       // long slices: plans in a launch of their own
